@@ -390,6 +390,122 @@ int32_t mvla_patch_select(mvla_ctx *ctx, int32_t prune_point, int32_t batch, con
                           int32_t *kept_idx, int32_t *out_offsets, int32_t *counts, float *xhat_out,
                           int32_t *info_out, mvla_patch_diag *diag, void *stream);
 
+/*
+ * ---- Around the prune point: what makes the rows that pruning scores, attends over the rows that survive, and keeps the cache
+ * small while action tokens are decoded.  (The paper has no counterpart: its host model does these.)  The calls use the context's
+ * device, type, heads and head_dim; they are stateless and touch no prune state.  q is [rows, n_heads, head_dim], keys and values
+ * are [rows, n_kv_heads, head_dim] as above.  A cache is such a pair of tensors; a sequence owns a run of its rows.  Rows of hidden
+ * states and of attention outputs have the context's hidden type (fp32 contexts: fp32, else bf16).
+ */
+
+/* One sequence of a batch (host array). */
+typedef struct mvla_seq {
+    int64_t q_row;             /* mvla_window_attention: first row of the sequence's queries in q, out, lse, q_pos */
+    int64_t kv_row;            /* first row of the sequence in the cache */
+    int32_t n_q;               /* mvla_window_attention: queries of this call; 0: none */
+    int32_t n_kv;              /* cached rows, those of this call's queries among them; with kv_len the most there can be */
+    int32_t budget;            /* mvla_cache_evict: rows that may stay */
+    int32_t reserved0;
+} mvla_seq;
+
+#define MVLA_ROPE_NORM        1u  /* normalise every head of q and k before the rotation */
+#define MVLA_ROPE_INTERLEAVED 2u  /* pairs (2i, 2i + 1) instead of (i, i + rot_dim / 2) */
+
+typedef struct mvla_qk_rope {
+    const void *q, *k, *v;         /* device, hidden type (bf16 also where the context's q / k / v are e4m3); each nullable.  Rows
+                                      [heads, head_dim] contiguous, q_stride ... elements from one row to the next (slices of a fused
+                                      projection are such rows); bases and strides multiples of 16 bytes */
+    int64_t n_rows;                /* 0: nothing to do */
+    int64_t q_stride, k_stride, v_stride;
+    const void *q_weight, *k_weight;   /* [head_dim], hidden type, nullable (ones); with MVLA_ROPE_NORM only */
+    const int32_t *pos;            /* [n_rows] positions (a prune step's kept_idx are such); needed where rot_dim > 0 */
+    const double *inv_freq;        /* [rot_dim / 2] radians per position, 64 bits: angles of far positions lose their meaning in 32 */
+    int32_t rot_dim;               /* leading elements of a head that are rotated: a multiple of 16, at most head_dim; 0: none */
+    uint32_t flags;                /* MVLA_ROPE_* */
+    double eps;                    /* of the norm, >= 0 */
+    void *q_out;                   /* [n_rows, n_heads, head_dim], context type; nullable with q */
+    void *k_out, *v_out;           /* [kv_rows, n_kv_heads, head_dim], context type: a cache, or packed rows; nullable with k, v */
+    const int32_t *out_rows;       /* [n_rows] row of k_out / v_out that row i goes to, nullable (row i).  A row outside
+                                      [0, kv_rows) is not written; no row may be named twice */
+    int64_t kv_rows;               /* rows of k_out / v_out */
+} mvla_qk_rope;
+
+/*
+ * Per-head norms of queries and keys and the position rotation in one pass; values are copied beside them:
+ *   y = x / sqrt(mean_c x_c^2 + eps) * weight    (each head; MVLA_ROPE_NORM)
+ *   (z_a, z_b) = (y_a cos t - y_b sin t, y_b cos t + y_a sin t),  t = pos * inv_freq[i]   (each pair (a, b) = pair i of the head)
+ * rounded once, at the end (e4m3 saturates).  Angles are taken in 64 bits.  An output may be its own input where their types are
+ * the same and the rows lie alike (q_stride = n_heads head_dim, and no out_rows); other overlaps of inputs and outputs are refused.
+ */
+int32_t mvla_qk_norm_rope(mvla_ctx *ctx, const mvla_qk_rope *args, void *stream);
+
+#define MVLA_WINDOW_ALL 0x7FFFFFFF
+
+typedef struct mvla_attention {
+    const void *q, *k, *v;         /* device, context type, 16-byte aligned */
+    int64_t q_rows, kv_rows;       /* rows of q (and out, lse, q_pos), and of k, v (and kv_pos, mass) */
+    const int32_t *q_pos;          /* [q_rows] positions of the queries, nullable: n_kv - n_q + i for query i of a sequence */
+    const int32_t *kv_pos;         /* [kv_rows] positions of the cached rows, in any order, negative: a row that nobody sees.
+                                      Nullable: row j of a sequence has position j.  With kv_pos, q_pos is needed too */
+    const int32_t *kv_len;         /* DEVICE [batch], nullable: cached rows of every sequence, for captured calls whose caches grow
+                                      between replays; values are taken into [0, n_kv] */
+    int32_t window;                /* >= 1; MVLA_WINDOW_ALL: everything before a query is visible */
+    int32_t n_sink;                /* >= 0: positions below it stay visible outside the window */
+    double scale;                  /* of the dot products; 0: 1 / sqrt(head_dim) */
+    void *out;                     /* [q_rows, n_heads, head_dim], hidden type */
+    float *lse;                    /* [q_rows, n_heads] natural logarithm of the sum of exponentials, nullable */
+    float *mass;                   /* [kv_rows] accumulated attention weights, nullable: added to */
+    void *workspace;               /* device, 256-byte aligned; nullable where mvla_window_attention_workspace says 0 */
+    int64_t workspace_bytes;
+} mvla_attention;
+
+/*
+ * Causal attention with a sliding window and sinks.  Query i (position p_i) sees cached row j (position c_j) of its sequence where
+ *   0 <= c_j <= p_i  and  (p_i - c_j < window  or  c_j < n_sink);
+ * query head h reads key head h / (n_heads / n_kv_heads).  out = softmax over the visible rows, times their values; sums and
+ * exponentials in 32 bits (16-bit types: weights are rounded to bf16 for their product with the values, e4m3: to fp16).  A query
+ * that sees nothing: out 0, lse -infinity.  mass[j] += 1 / n_heads * sum over heads and queries of the weight of row j, in an order
+ * that does not change from run to run.
+ * What q, k and v hold must be finite in rows that some query of the sequence sees; rows behind a sequence's length and rows of
+ * negative position may hold anything.  Rows of q, out and lse outside the sequences are left as they are.  Sequences must not
+ * share query rows, nor cache rows where `mass` is given (INVALID_ARG); without it they may (a common prefix).  out, lse, mass and
+ * the workspace must not overlap the inputs.  The workspace holds nothing between calls, but calls that may run at the same time
+ * (two streams, two graphs) need one each.  Batches of up to max_batch sequences (CAPACITY).
+ */
+int32_t mvla_window_attention(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, const mvla_attention *args, void *stream);
+
+/* Workspace bytes of a call with these arguments (pointers are looked at only for being null). */
+int32_t mvla_window_attention_workspace(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, const mvla_attention *args,
+                                        int64_t *bytes);
+
+typedef struct mvla_eviction {
+    void *k, *v;                   /* device, context type, 16-byte aligned: rows move in place */
+    int64_t kv_rows;
+    const int32_t *pos;            /* [kv_rows] positions, negative: a row that nobody sees */
+    const float *mass;             /* [kv_rows] accumulated weights (mvla_window_attention) */
+    int32_t *pos_out;              /* [kv_rows] the same of the rows that stay; pos and mass themselves, or arrays of their own */
+    float *mass_out;
+    int32_t *kept_idx;             /* [kv_rows], nullable: kept_idx[kv_row + j] = row (relative to kv_row) that is row j now */
+    const int32_t *kv_len;         /* DEVICE [batch], nullable: as above */
+    int32_t *kv_len_out;           /* DEVICE [batch], nullable: rows that stay (may be kv_len) */
+    int32_t n_sink, n_recent;      /* protected: positions below n_sink, and the last n_recent up to the largest of the sequence */
+    void *workspace;               /* device, 256-byte aligned; as above */
+    int64_t workspace_bytes;
+} mvla_eviction;
+
+/*
+ * Eviction by accumulated attention weight.  Of a sequence of n rows, m = min(n, budget) stay: the protected ones first, then those
+ * with the largest mass, then (NaN counts as less than every number) rows of negative position; equal ones by the lower row.  (Should
+ * more rows be protected than the budget holds, the lower rows stay.)  Kept rows below m stay where they are; the kept rows behind
+ * them move, in ascending order, into the rows below m that were given up, in ascending order: nothing else is copied, and the cache
+ * is in no order afterwards, which is why positions go with the rows.  Rows from m on are left as they are.
+ * n_sink + n_recent <= budget (INVALID_ARG); sequences must not share rows (INVALID_ARG).
+ */
+int32_t mvla_cache_evict(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, const mvla_eviction *args, void *stream);
+
+/* Workspace bytes of a call with these arguments (pointers are not looked at). */
+int32_t mvla_cache_evict_workspace(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, const mvla_eviction *args, int64_t *bytes);
+
 /* Free everything the context owns.  NULL is accepted.  The caller must have
  * synchronised any stream that still runs work enqueued through the context. */
 void mvla_prune_destroy(mvla_ctx *ctx);

@@ -1,35 +1,19 @@
 // C-ABI layer: argument validation, host-side budget arithmetic, workspace and smoothed state,
 // tensor-map construction, launch sequencing.  No stream synchronisation anywhere.
+#include "api_util.h"
 #include "common.cuh"
 #include "rules.h"
 #include "sets.h"
 
-#include <cudaTypedefs.h>
-
 #include <cmath>
-#include <cstdlib>
 #include <cstring>
 #include <new>
 #include <vector>
-#include <cstdio>
-
-#include <nvtx3/nvToolsExt.h>
 
 using namespace mvla;
 
 namespace {
-constexpr int kMaxBatch = 64;       // samples per call (mvla_prune_create refuses more)
 constexpr int kMapSlots = 16;       // tensor maps a context remembers
-// Tracing and logging, both on the host and off the device's path: every public call is an NVTX range (a profiler
-// shows the call and, inside mvla_prune_step, its phases around the kernels they enqueue; without a profiler
-// attached a range costs a few nanoseconds), and with MVLA_LOG=1 in the environment every call prints one line
-// with its arguments and its result to stderr.
-struct ApiRange {
-    explicit ApiRange(const char* name) { nvtxRangePushA(name); }
-    ~ApiRange() { nvtxRangePop(); }
-    ApiRange(const ApiRange&) = delete;
-    ApiRange& operator=(const ApiRange&) = delete;
-};
 // The phases of a step inside the call's range: mark() closes the phase before it.
 struct PhaseRange {
     bool open = false;
@@ -41,14 +25,6 @@ struct PhaseRange {
     }
     ~PhaseRange() { if (open) nvtxRangePop(); }
 };
-bool log_enabled()
-{
-    static const bool on = [] {
-        const char* e = std::getenv("MVLA_LOG");
-        return e && *e && *e != '0';
-    }();
-    return on;
-}
 }
 
 struct mvla_ctx {
@@ -127,22 +103,7 @@ struct mvla_ctx {
 
 namespace {
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) return;
-        ok = (prev == dev) || cudaSetDevice(dev) == cudaSuccess;
-    }
-    ~DeviceGuard()
-    {
-        if (ok && prev >= 0) cudaSetDevice(prev);
-    }
-};
-
 inline int32_t rhu(double x) { return static_cast<int32_t>(std::floor(x + 0.5)); }
-inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
 int32_t fail_cuda(mvla_ctx* ctx, cudaError_t e)
 {
@@ -823,6 +784,20 @@ int32_t prune_step_patch(mvla_ctx* ctx, int32_t prune_point, int32_t batch, cons
 }
 
 }  // namespace
+
+namespace mvla {
+int32_t open_call(mvla_ctx* ctx, bool enqueues, CtxView* view)
+{
+    const int32_t rc = check_sticky(ctx);
+    if (rc != MVLA_OK) return rc;
+    if (enqueues) ctx->hist_unknown = true;          // what the stream ran last is no longer a known prune step
+    const mvla_config& c = ctx->cfg;
+    *view = CtxView{{c.dtype, ctx->hidden_dtype, c.n_heads, ctx->kv_heads, c.head_dim, c.max_batch, ctx->sm_count, ctx->qk_elem, ctx->elem},
+                    c.device, ctx->status_dev, ctx->encode};
+    return MVLA_OK;
+}
+int32_t close_call(mvla_ctx* ctx, cudaError_t e) { return e == cudaSuccess ? MVLA_OK : fail_cuda(ctx, e); }
+}  // namespace mvla
 
 extern "C" {
 

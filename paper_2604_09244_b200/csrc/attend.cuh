@@ -1,0 +1,65 @@
+// Device side of the windowed attention that its kernels share: who sees whom, and which tiles of keys a block of queries visits.
+#pragma once
+
+#include "device_utils.cuh"
+#include "serve.h"
+
+#include <cuda_fp8.h>
+
+namespace mvla {
+
+__device__ __forceinline__ int seq_len(const AttArgs& a, const AttSeq& s)
+{
+    return a.kv_len ? min(max(a.kv_len[s.index], 0), s.n_kv) : s.n_kv;
+}
+__device__ __forceinline__ int query_pos(const AttArgs& a, const AttSeq& s, int len, int i)
+{
+    return a.q_pos ? a.q_pos[s.q_row + i] : len - s.n_q + i;
+}
+// Position of row j of a sequence, -1 where nobody sees it.
+__device__ __forceinline__ int key_pos(const AttArgs& a, const AttSeq& s, int len, int j)
+{
+    return j >= len ? -1 : a.kv_pos ? a.kv_pos[s.kv_row + j] : j;
+}
+// (p - c cannot overflow: c is not negative and not above p where it is taken)
+__device__ __forceinline__ bool sees(int p, int c, int window, int n_sink)
+{
+    return c >= 0 && c <= p && (p - c < window || c < n_sink);
+}
+// Whether some query with a position in [lo, hi] may see a key at c.
+__device__ __forceinline__ bool some_sees(int lo, int hi, int c, int window, int n_sink)
+{
+    return c >= 0 && c <= hi && (c >= lo || lo - c < window || c < n_sink);
+}
+// The block of the launch's grid that `blk` is: its sequence.
+__device__ __forceinline__ int seq_of_block(const AttArgs& a, int blk)
+{
+    int b = 0;
+    while (b + 1 < a.n_seq && blk >= a.s[b + 1].blk0) ++b;
+    return b;
+}
+__device__ __forceinline__ int seq_of_query(const AttArgs& a, int qp)
+{
+    int b = 0;
+    while (b + 1 < a.n_seq && qp >= a.s[b + 1].qp0) ++b;
+    return b;
+}
+// Tiles of `tile` keys that queries at [lo, hi] may see: `sinks` tiles from the first on, then those from `first` on, `count` in all.
+// Where the positions are data every tile of the sequence is named, and looked at when it comes up.
+struct TileRange {
+    int sinks, first, count;
+    __device__ __forceinline__ int tile(int t) const { return t < sinks ? t : first + t - sinks; }
+};
+__device__ __forceinline__ TileRange tile_range(const AttArgs& a, int len, int lo, int hi, int tile)
+{
+    TileRange r = {0, 0, 0};
+    const int end = a.kv_pos ? len : min(len, max(hi, -1) + 1);
+    const int n = (end + tile - 1) / tile;
+    const int from = a.kv_pos || a.window > lo ? 0 : lo - a.window + 1;
+    r.first = min(from / tile, n);
+    r.sinks = min(static_cast<int>((static_cast<int64_t>(a.n_sink) + tile - 1) / tile), r.first);
+    r.count = r.sinks + n - r.first;
+    return r;
+}
+
+}  // namespace mvla

@@ -1,0 +1,83 @@
+// Host arithmetic of a windowed-attention call: its blocks, how the visible keys are split, and where its workspace lies.
+#pragma once
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "mvla_prune.h"
+
+namespace mvla {
+
+// What the plans and checks of a call go by in its context.
+struct ServeShape {
+    int dtype, hidden_dtype;            // MVLA_DTYPE_* of q / k / v and of the rows beside them (bf16 where q / k / v are e4m3)
+    int n_heads, kv_heads, head_dim, max_batch, sm_count;
+    size_t elem, wide;                  // bytes per element of q / k / v, and of the rows beside them
+};
+
+// What a call reads of a sequence at most, by its descriptor (positions that are data may leave anything visible).
+inline int64_t visible_keys(const mvla_seq& s, bool counted, int32_t window, int32_t n_sink)
+{
+    if (!counted) return s.n_kv;
+    const int64_t all = static_cast<int64_t>(window) + s.n_q - 1 + n_sink;
+    return all < s.n_kv ? all : s.n_kv;
+}
+
+struct Workspace {
+    int64_t bytes = 0;
+    int64_t take(int64_t n)
+    {
+        const int64_t at = bytes;
+        bytes += (n + 255) / 256 * 256;
+        return at;
+    }
+};
+
+struct AttendPlan {
+    int32_t rows = 32;           // query rows of a block (a block shares a key head: queries x heads of a group)
+    int32_t splits = 1;
+    int64_t total_q = 0, total_kv = 0, blocks = 0;
+    // offsets in the workspace, -1: not used
+    int64_t part_o = -1, part_ml = -1, lse2 = -1, part_mass = -1, bytes = 0;
+};
+
+inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, bool mass)
+{
+    AttendPlan p;
+    const int group = c.n_heads / c.kv_heads;
+    int64_t longest = 0, most_rows = 0;
+    for (int b = 0; b < batch; ++b) {
+        const mvla_seq& s = seqs[b];
+        p.total_q += s.n_q;
+        p.total_kv += s.n_kv;
+        if (s.n_q == 0) continue;
+        const int64_t keys = visible_keys(s, counted, window, n_sink), rows = static_cast<int64_t>(s.n_q) * group;
+        longest = keys > longest ? keys : longest;
+        most_rows = rows > most_rows ? rows : most_rows;
+    }
+    p.rows = most_rows <= 8 ? 8 : 32;
+    for (int b = 0; b < batch; ++b) p.blocks += (static_cast<int64_t>(seqs[b].n_q) * group + p.rows - 1) / p.rows;
+    if (p.blocks > 0) {
+        // enough CTAs for every multiprocessor twice, of at least four tiles of 64 keys
+        const int64_t ctas = p.blocks * c.kv_heads;
+        int64_t n = (2 * static_cast<int64_t>(c.sm_count) + ctas - 1) / ctas;
+        const int64_t most = longest / 256;
+        n = n > most ? most : n;
+        n = n > 64 ? 64 : n;
+        p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
+    }
+    Workspace w;
+    const int64_t qh = p.total_q * c.n_heads;
+    if (p.splits > 1) {
+        p.part_o = w.take(p.splits * qh * c.head_dim * static_cast<int64_t>(sizeof(float)));
+        p.part_ml = w.take(p.splits * qh * 2 * static_cast<int64_t>(sizeof(float)));
+    }
+    if (mass) {
+        p.lse2 = w.take(qh * static_cast<int64_t>(sizeof(float)));
+        p.part_mass = w.take(c.kv_heads * p.total_kv * static_cast<int64_t>(sizeof(float)));
+    }
+    p.bytes = w.bytes;
+    return p;
+}
+
+}  // namespace mvla

@@ -6,6 +6,7 @@
 // of interpreter work per call, here about 1 us.
 #include <torch/csrc/autograd/python_variable.h>
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 
 #include <cstring>
@@ -366,6 +367,260 @@ PyObject* py_patch_select(PyObject*, PyObject* const* a, Py_ssize_t n)
     MVLA_CATCH
 }
 
+// ---- calls around the prune point.  Tensors are looked at here for what the library cannot see: their type, device and rows.
+
+bool expect(bool ok, const char* what)
+{
+    if (!ok) PyErr_SetString(PyExc_AssertionError, what);
+    return ok;
+}
+// The device of a call: every tensor of it lies there.
+bool on_device(const at::Tensor& t, const char* name, int64_t device)
+{
+    if (t.device().index() == device) return true;
+    PyErr_Format(PyExc_AssertionError, "%s: not on the context's device", name);
+    return false;
+}
+// Pointer and tensor of an optional argument of a given type; `dims`: how many it must have.
+bool typed(PyObject* o, const char* name, at::ScalarType type, int dims, int64_t device, void** p, const at::Tensor** t)
+{
+    *t = nullptr;
+    if (!tensor_ptr(o, p, t)) return false;
+    if (!*t) return true;
+    if ((*t)->scalar_type() != type || (*t)->dim() != dims) {
+        PyErr_Format(PyExc_AssertionError, "%s: wrong type or number of dimensions", name);
+        return false;
+    }
+    return on_device(**t, name, device);
+}
+// Sequence descriptors: an array of them as it lies in memory.
+struct Seqs {
+    const mvla_seq* ptr = nullptr;
+    int n = 0;
+    Py_buffer view;
+    bool viewed = false;
+    ~Seqs() { if (viewed) PyBuffer_Release(&view); }
+    bool take(PyObject* o)
+    {
+        if (PyObject_GetBuffer(o, &view, PyBUF_SIMPLE) != 0) return false;
+        viewed = true;
+        if (!expect(view.len % static_cast<Py_ssize_t>(sizeof(mvla_seq)) == 0, "seqs: not an array of sequence descriptors")) return false;
+        ptr = static_cast<const mvla_seq*>(view.buf);
+        n = static_cast<int>(view.len / static_cast<Py_ssize_t>(sizeof(mvla_seq)));
+        return true;
+    }
+};
+// The stream of a call on `device`: the given one, or the device's current one.
+bool stream_on(PyObject* o, int64_t device, void** st)
+{
+    if (o != Py_None) return stream_of(o, st);
+    *st = c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(device)).stream();
+    return true;
+}
+// Memory for the time that the stream takes to run the call (torch's allocator keeps it apart from what other streams use, and inside
+// a graph capture in the graph's pool).
+at::Tensor scratch(int64_t bytes, int64_t device, void* st)
+{
+    const auto index = static_cast<c10::DeviceIndex>(device);
+    const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(st), index));
+    return at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, index));
+}
+at::ScalarType scalar_of(int64_t dtype)
+{
+    return dtype == MVLA_DTYPE_FP32 ? at::kFloat : dtype == MVLA_DTYPE_BF16 ? at::kBFloat16 : at::kFloat8_e4m3fn;
+}
+// What a context is, as PruneContext hands it over with every call: (dtype, heads, kv_heads, head_dim, device) from a[1] on.
+struct Shape {
+    int64_t dtype, heads, kv_heads, dim, device;
+    at::ScalarType kept, wide;
+    bool take(PyObject* const* a)
+    {
+        if (!int_of(a[1], &dtype) || !int_of(a[2], &heads) || !int_of(a[3], &kv_heads) || !int_of(a[4], &dim) || !int_of(a[5], &device)) return false;
+        kept = scalar_of(dtype);
+        wide = dtype == MVLA_DTYPE_FP32 ? at::kFloat : at::kBFloat16;
+        return true;
+    }
+    bool rows_of_keys(const at::Tensor* t) const { return !t || (t->size(1) == kv_heads && t->size(2) == dim); }
+};
+bool entries(const at::Tensor* t, int64_t n) { return !t || t->size(0) == n; }
+
+// Rows of [heads, head_dim] with a stride of their own: pointer, stride, rows.
+bool strided_rows(PyObject* o, const char* name, const Shape& c, int64_t heads, const void** p, int64_t* stride, int64_t* rows)
+{
+    *p = nullptr;
+    *stride = 0;
+    if (o == Py_None) return true;
+    if (!expect(THPVariable_Check(o), "expected a torch.Tensor or None")) return false;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.scalar_type() != c.wide || t.dim() != 3 || t.size(1) != heads || t.size(2) != c.dim ||
+        (t.numel() && (t.stride(2) != 1 || (heads > 1 && t.stride(1) != c.dim)))) {
+        PyErr_Format(PyExc_AssertionError, "%s: device tensor [rows, heads, head_dim] of the context's row type with contiguous rows", name);
+        return false;
+    }
+    if (!expect(*rows < 0 || *rows == t.size(0), "q, k and v: as many rows of one as of another")) return false;
+    *rows = t.size(0);
+    *p = t.data_ptr();
+    *stride = t.size(0) > 1 ? t.stride(0) : heads * c.dim;
+    return on_device(t, name, c.device);
+}
+
+// qk_norm_rope(ctx, dtype, heads, kv_heads, dim, device, q, k, v, pos, inv_freq, q_weight, k_weight, flags, eps, q_out, k_out, v_out,
+//   out_rows, stream) -> status
+PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    MVLA_TRY
+    if (!arg_count(n, 20)) return nullptr;
+    Shape c;
+    int64_t flags;
+    if (!c.take(a) || !int_of(a[13], &flags)) return nullptr;
+    mvla_qk_rope r;
+    std::memset(&r, 0, sizeof r);
+    r.eps = PyFloat_AsDouble(a[14]);
+    if (r.eps == -1.0 && PyErr_Occurred()) return nullptr;
+    int64_t rows = -1;
+    if (!strided_rows(a[6], "q", c, c.heads, &r.q, &r.q_stride, &rows) || !strided_rows(a[7], "k", c, c.kv_heads, &r.k, &r.k_stride, &rows) ||
+        !strided_rows(a[8], "v", c, c.kv_heads, &r.v, &r.v_stride, &rows))
+        return nullptr;
+    if (!expect(rows >= 0, "qk_norm_rope: none of q, k, v is given")) return nullptr;
+    void *pos, *freq, *wq, *wk, *qo, *ko, *vo, *to, *st;
+    const at::Tensor *tp, *tf, *twq, *twk, *tqo, *tko, *tvo, *tto;
+    if (!typed(a[9], "pos", at::kInt, 1, c.device, &pos, &tp) || !typed(a[10], "inv_freq", at::kDouble, 1, c.device, &freq, &tf) ||
+        !typed(a[11], "q_weight", c.wide, 1, c.device, &wq, &twq) || !typed(a[12], "k_weight", c.wide, 1, c.device, &wk, &twk) ||
+        !typed(a[15], "q_out", c.kept, 3, c.device, &qo, &tqo) || !typed(a[16], "k_out", c.kept, 3, c.device, &ko, &tko) ||
+        !typed(a[17], "v_out", c.kept, 3, c.device, &vo, &tvo) || !typed(a[18], "out_rows", at::kInt, 1, c.device, &to, &tto) ||
+        !stream_on(a[19], c.device, &st))
+        return nullptr;
+    if (!expect(entries(tp, rows) && entries(tto, rows), "pos, out_rows: one entry per row") ||
+        !expect(entries(twq, c.dim) && entries(twk, c.dim), "weights: one entry per element of a head") ||
+        !expect(!tqo || (tqo->size(0) == rows && tqo->size(1) == c.heads && tqo->size(2) == c.dim), "q_out: [rows, heads, head_dim]") ||
+        !expect(c.rows_of_keys(tko) && c.rows_of_keys(tvo), "k_out, v_out: [rows, heads, head_dim]") ||
+        !expect(!tko || !tvo || tko->size(0) == tvo->size(0), "k_out, v_out: as many rows of one as of the other") ||
+        !expect(!tf || tf->size(0) <= c.dim, "inv_freq: one entry per pair of a head"))
+        return nullptr;
+    r.n_rows = rows;
+    r.q_weight = wq; r.k_weight = wk;
+    r.pos = static_cast<const int32_t*>(pos);
+    r.inv_freq = static_cast<const double*>(freq);
+    r.rot_dim = tf ? static_cast<int32_t>(2 * tf->size(0)) : 0;
+    r.flags = static_cast<uint32_t>(flags);
+    r.q_out = qo; r.k_out = ko; r.v_out = vo;
+    r.out_rows = static_cast<const int32_t*>(to);
+    r.kv_rows = tko ? tko->size(0) : tvo ? tvo->size(0) : 0;
+    mvla_ctx* ctx = ctx_of(a[0]);
+    return PyLong_FromLong(unlocked([&] { return mvla_qk_norm_rope(ctx, &r, st); }));
+    MVLA_CATCH
+}
+
+// window_attention(ctx, dtype, heads, kv_heads, dim, device, seqs, q, k, v, window, sinks, scale, q_pos, kv_pos, kv_len, out, lse, mass,
+//   stream) -> (status, out); a missing `out` is allocated
+PyObject* py_window_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    MVLA_TRY
+    if (!arg_count(n, 20)) return nullptr;
+    Shape c;
+    int64_t window, sinks;
+    if (!c.take(a) || !int_of(a[10], &window) || !int_of(a[11], &sinks)) return nullptr;
+    mvla_attention r;
+    std::memset(&r, 0, sizeof r);
+    r.scale = PyFloat_AsDouble(a[12]);
+    if (r.scale == -1.0 && PyErr_Occurred()) return nullptr;
+    Seqs s;
+    void *q, *k, *v, *qp, *kp, *kl, *out, *lse, *mass, *st;
+    const at::Tensor *tq, *tk, *tv, *tqp, *tkp, *tkl, *to, *tl, *tm;
+    if (!s.take(a[6]) || !typed(a[7], "q", c.kept, 3, c.device, &q, &tq) || !typed(a[8], "k", c.kept, 3, c.device, &k, &tk) ||
+        !typed(a[9], "v", c.kept, 3, c.device, &v, &tv) || !typed(a[13], "q_pos", at::kInt, 1, c.device, &qp, &tqp) ||
+        !typed(a[14], "kv_pos", at::kInt, 1, c.device, &kp, &tkp) || !typed(a[15], "kv_len", at::kInt, 1, c.device, &kl, &tkl) ||
+        !typed(a[16], "out", c.wide, 3, c.device, &out, &to) || !typed(a[17], "lse", at::kFloat, 2, c.device, &lse, &tl) ||
+        !typed(a[18], "mass", at::kFloat, 1, c.device, &mass, &tm) || !stream_on(a[19], c.device, &st))
+        return nullptr;
+    if (!expect(tq && tk && tv, "q, k and v are needed")) return nullptr;
+    const int64_t rows = tq->size(0), kv_rows = tk->size(0);
+    if (!expect(tq->size(1) == c.heads && tq->size(2) == c.dim, "q: [rows, heads, head_dim]") ||
+        !expect(c.rows_of_keys(tk) && tv->sizes() == tk->sizes(), "k, v: [rows, heads, head_dim], alike") ||
+        !expect(entries(tqp, rows) && entries(tkp, kv_rows), "q_pos, kv_pos: one entry per row") ||
+        !expect(entries(tkl, s.n), "kv_len: one entry per sequence") || !expect(!to || to->sizes() == tq->sizes(), "out: as q") ||
+        !expect(!tl || (tl->size(0) == rows && tl->size(1) == c.heads), "lse: [rows, heads]") || !expect(entries(tm, kv_rows), "mass: one entry per cached row") ||
+        !expect(window >= 1 && window <= MVLA_WINDOW_ALL && sinks >= 0 && sinks <= MVLA_WINDOW_ALL, "window, n_sink: out of range"))
+        return nullptr;
+    r.q = q; r.k = k; r.v = v; r.q_rows = rows; r.kv_rows = kv_rows;
+    r.q_pos = static_cast<const int32_t*>(qp);
+    r.kv_pos = static_cast<const int32_t*>(kp);
+    r.kv_len = static_cast<const int32_t*>(kl);
+    r.window = static_cast<int32_t>(window);
+    r.n_sink = static_cast<int32_t>(sinks);
+    r.lse = static_cast<float*>(lse);
+    r.mass = static_cast<float*>(mass);
+    mvla_ctx* ctx = ctx_of(a[0]);
+    int64_t bytes = 0;
+    int32_t rc = mvla_window_attention_workspace(ctx, s.n, s.ptr, &r, &bytes);
+    if (rc != MVLA_OK) return Py_BuildValue("(iO)", rc, Py_None);
+    at::Tensor ws, fresh;
+    if (bytes > 0) ws = scratch(bytes, c.device, st);
+    if (!to) {
+        fresh = scratch(tq->numel() * (c.wide == at::kFloat ? 4 : 2), c.device, st).view(c.wide).view(tq->sizes());
+        out = fresh.data_ptr();
+    }
+    r.out = out;
+    r.workspace = bytes > 0 ? ws.data_ptr() : nullptr;
+    r.workspace_bytes = bytes;
+    rc = unlocked([&] { return mvla_window_attention(ctx, s.n, s.ptr, &r, st); });
+    if (to) return Py_BuildValue("(iO)", rc, a[16]);
+    PyObject* o = THPVariable_Wrap(fresh);
+    PyObject* ret = o ? Py_BuildValue("(iO)", rc, o) : nullptr;
+    Py_XDECREF(o);
+    return ret;
+    MVLA_CATCH
+}
+
+// cache_evict(ctx, dtype, heads, kv_heads, dim, device, seqs, k, v, pos, mass, pos_out, mass_out, kept_idx, kv_len, kv_len_out, sinks,
+//   recent, stream) -> status
+PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    MVLA_TRY
+    if (!arg_count(n, 19)) return nullptr;
+    Shape c;
+    int64_t sinks, recent;
+    if (!c.take(a) || !int_of(a[16], &sinks) || !int_of(a[17], &recent)) return nullptr;
+    Seqs s;
+    void *k, *v, *pos, *mass, *po, *mo, *idx, *kl, *klo, *st;
+    const at::Tensor *tk, *tv, *tp, *tm, *tpo, *tmo, *ti, *tkl, *tklo;
+    if (!s.take(a[6]) || !typed(a[7], "k", c.kept, 3, c.device, &k, &tk) || !typed(a[8], "v", c.kept, 3, c.device, &v, &tv) ||
+        !typed(a[9], "pos", at::kInt, 1, c.device, &pos, &tp) || !typed(a[10], "mass", at::kFloat, 1, c.device, &mass, &tm) ||
+        !typed(a[11], "pos_out", at::kInt, 1, c.device, &po, &tpo) || !typed(a[12], "mass_out", at::kFloat, 1, c.device, &mo, &tmo) ||
+        !typed(a[13], "kept_idx", at::kInt, 1, c.device, &idx, &ti) || !typed(a[14], "kv_len", at::kInt, 1, c.device, &kl, &tkl) ||
+        !typed(a[15], "kv_len_out", at::kInt, 1, c.device, &klo, &tklo) || !stream_on(a[18], c.device, &st))
+        return nullptr;
+    if (!expect(tk && tv && tp && tm && tpo && tmo, "k, v, pos and mass are needed")) return nullptr;
+    const int64_t rows = tk->size(0);
+    if (!expect(c.rows_of_keys(tk) && tv->sizes() == tk->sizes(), "k, v: [rows, heads, head_dim], alike") ||
+        !expect(entries(tp, rows) && entries(tm, rows) && entries(tpo, rows) && entries(tmo, rows) && entries(ti, rows),
+                "pos, mass, kept_idx: one entry per cached row") ||
+        !expect(entries(tkl, s.n) && entries(tklo, s.n), "kv_len: one entry per sequence") ||
+        !expect(sinks >= 0 && sinks <= MVLA_WINDOW_ALL && recent >= 0 && recent <= MVLA_WINDOW_ALL, "n_sink, n_recent: out of range"))
+        return nullptr;
+    mvla_eviction r;
+    std::memset(&r, 0, sizeof r);
+    r.k = k; r.v = v; r.kv_rows = rows;
+    r.pos = static_cast<const int32_t*>(pos);
+    r.mass = static_cast<const float*>(mass);
+    r.pos_out = static_cast<int32_t*>(po);
+    r.mass_out = static_cast<float*>(mo);
+    r.kept_idx = static_cast<int32_t*>(idx);
+    r.kv_len = static_cast<const int32_t*>(kl);
+    r.kv_len_out = static_cast<int32_t*>(klo);
+    r.n_sink = static_cast<int32_t>(sinks);
+    r.n_recent = static_cast<int32_t>(recent);
+    mvla_ctx* ctx = ctx_of(a[0]);
+    int64_t bytes = 0;
+    const int32_t rc = mvla_cache_evict_workspace(ctx, s.n, s.ptr, &r, &bytes);
+    if (rc != MVLA_OK) return PyLong_FromLong(rc);
+    const at::Tensor ws = scratch(bytes, c.device, st);
+    r.workspace = ws.data_ptr();
+    r.workspace_bytes = bytes;
+    return PyLong_FromLong(unlocked([&] { return mvla_cache_evict(ctx, s.n, s.ptr, &r, st); }));
+    MVLA_CATCH
+}
+
 // fill_samples(array, sequence): descriptors from objects with the descriptor's field names, into a ctypes array
 PyObject* py_fill_samples(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -395,6 +650,8 @@ PyObject* py_fill_samples(PyObject*, PyObject* const* a, Py_ssize_t n)
 PyMethodDef kMethods[] = {MVLA_FAST("prune_step", py_prune_step), MVLA_FAST("salience", py_salience),
                           MVLA_FAST("select", py_select), MVLA_FAST("compact", py_compact),
                           MVLA_FAST("patch_indicators", py_patch_indicators), MVLA_FAST("patch_select", py_patch_select),
+                          MVLA_FAST("qk_norm_rope", py_qk_norm_rope), MVLA_FAST("window_attention", py_window_attention),
+                          MVLA_FAST("cache_evict", py_cache_evict),
                           MVLA_FAST("fill_samples", py_fill_samples), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of libmvla_prune.so", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};

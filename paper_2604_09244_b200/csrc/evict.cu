@@ -1,0 +1,269 @@
+// Eviction from a cache by accumulated attention weight: which rows stay, and the moves that leave them in front.
+//
+// Kept rows that lie below the new length stay where they are; those behind it move into the holes.  Sources and
+// destinations are then different rows by construction, so all moves may run at once and in place, and a decode step that is one row
+// over its budget moves one row instead of the cache.
+//
+// evict_select_kernel: one CTA a sequence.  Every row has a 32-bit key (its weight's bits in order of size; protected rows above all,
+// hidden rows below all); four rounds of 256-bin counts over the keys, most significant byte first, give the key of the
+// last row that stays and how many of its equals do; then every warp walks a run of rows in ascending order and counts, and once
+// more to write.  Keys are kept in shared memory where they fit.  Bound by the latency of its passes.
+// evict_move_kernel: one warp a 2 KB piece of a moved row.  Bound by bytes.
+#include "device_utils.cuh"
+#include "serve.h"
+
+#include <algorithm>
+
+namespace mvla {
+namespace {
+
+constexpr int kThreads = 1024;
+constexpr int kWarps = kThreads / 32;
+constexpr int kKeysInSmem = 49152;           // 192 KB
+constexpr int kMoveThreads = 256;
+constexpr int kPiece = 2048;
+constexpr int kMovesInSelect = 4;            // rows that the selecting CTA moves itself
+
+__device__ __forceinline__ int seq_rows(const EvictArgs& a, const EvictSeq& s)
+{
+    return a.kv_len ? min(max(a.kv_len[s.index], 0), s.n_kv) : s.n_kv;
+}
+__device__ __forceinline__ uint32_t key_of(const EvictArgs& a, const EvictSeq& s, int j, int last)
+{
+    const int c = a.pos[s.kv_row + j];
+    if (c < 0) return 0u;
+    if (c < a.n_sink || last - c < a.n_recent) return 0xFFFFFFFFu;
+    const float w = a.mass[s.kv_row + j];
+    if (w != w) return 1u;                                    // NaN: below every number
+    const uint32_t u = __float_as_uint(w + 0.f);              // (-0 is 0)
+    return u & 0x80000000u ? ~u : u | 0x80000000u;            // (from 0x007FFFFF, -infinity, to 0xFF800000, +infinity)
+}
+// A 2 KB piece of a row, or what is left of it (16-byte steps).
+__device__ __forceinline__ void move_piece(char* dst, const char* src, int bytes, int lane)
+{
+    uint4 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((i * 32 + lane) * 16 < bytes) x[i] = *reinterpret_cast<const uint4*>(src + (i * 32 + lane) * 16);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if ((i * 32 + lane) * 16 < bytes) *reinterpret_cast<uint4*>(dst + (i * 32 + lane) * 16) = x[i];
+}
+// Largest over the block, in every thread.
+__device__ __forceinline__ int block_max(int v, int* red)
+{
+    v = __reduce_max_sync(0xffffffffu, v);
+    __syncthreads();
+    if ((threadIdx.x & 31) == 0) red[threadIdx.x >> 5] = v;
+    __syncthreads();
+    return __reduce_max_sync(0xffffffffu, red[threadIdx.x & 31]);
+}
+// Exclusive sum over the warps of one value per warp (the same in all its lanes), and the total.
+__device__ __forceinline__ int warps_before(int v, int* red, int* total)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __syncthreads();
+    if (lane == 0) red[warp] = v;
+    __syncthreads();
+    int x = red[lane];
+    const int mine = x;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    *total = __shfl_sync(0xffffffffu, x, 31);
+    return __shfl_sync(0xffffffffu, x - mine, warp);
+}
+
+__global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_constant__ EvictArgs a)
+{
+    extern __shared__ uint32_t cached[];
+    __shared__ int hist[256];
+    __shared__ int red[kWarps];
+    __shared__ int found[2];
+    const EvictSeq& s = a.s[blockIdx.x];
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
+    pdl_wait();
+    const int n = seq_rows(a, s), m = min(n, s.budget);
+    const int64_t row = s.kv_row;
+    __syncthreads();                                          // (kv_len_out may be kv_len: everybody has read it)
+    if (m == n || m == 0) {                                   // everything stays, or nothing
+        if (a.pos_out != a.pos) for (int j = t; j < m; j += kThreads) a.pos_out[row + j] = a.pos[row + j];
+        if (a.mass_out != a.mass) for (int j = t; j < m; j += kThreads) a.mass_out[row + j] = a.mass[row + j];
+        if (a.kept_idx) for (int j = t; j < m; j += kThreads) a.kept_idx[row + j] = j;
+        if (t == 0) {
+            a.n_moves[blockIdx.x] = 0;
+            if (a.kv_len_out) a.kv_len_out[s.index] = m;
+        }
+        return;
+    }
+    int last = -1;
+    for (int j = t; j < n; j += kThreads) last = max(last, a.pos[row + j]);
+    last = block_max(last, red);
+    const bool fits = n <= kKeysInSmem;
+    const auto key_at = [&](int j) { return fits ? cached[j] : key_of(a, s, j, last); };
+    if (fits) for (int j = t; j < n; j += kThreads) cached[j] = key_of(a, s, j, last);
+    // The key of the m-th row in descending order, byte by byte; `left`: rows still to be found among those with the bytes so far.
+    uint32_t prefix = 0;
+    int left = m;
+    for (int shift = 24; shift >= 0; shift -= 8) {
+        if (t < 256) hist[t] = 0;
+        __syncthreads();
+        const uint32_t above = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
+        for (int j0 = 0; j0 < n; j0 += kThreads) {
+            const int j = j0 + t;
+            const uint32_t k = j < n ? key_at(j) : 0u;
+            const bool counts = j < n && (k & above) == prefix;
+            const uint32_t bin = counts ? (k >> shift) & 255u : 256u;
+            const unsigned same = __match_any_sync(0xffffffffu, bin);      // (weights crowd in few bins: one add for all lanes of a bin)
+            if (counts && lane == __ffs(same) - 1) atomicAdd(&hist[bin], __popc(same));
+        }
+        __syncthreads();
+        if (warp == 0) {                                      // eight bins a lane, from the top
+            int c[8], sum = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += c[i] = hist[255 - (lane * 8 + i)];
+            int upto = sum;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) {
+                const int y = __shfl_up_sync(0xffffffffu, upto, o);
+                if (lane >= o) upto += y;
+            }
+            int before = upto - sum;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (before < left && left <= before + c[i]) {
+                    found[0] = 255 - (lane * 8 + i);
+                    found[1] = left - before;
+                }
+                before += c[i];
+            }
+        }
+        __syncthreads();
+        prefix |= static_cast<uint32_t>(found[0]) << shift;
+        left = found[1];
+        __syncthreads();
+    }
+    // Rows with a larger key stay, and the first `left` of those with this one.  A warp has a run of rows.
+    const int run = (n + kThreads - 1) / kThreads * 32, first = min(warp * run, n), end = min(first + run, n);
+    int total, equal = 0;
+    for (int j0 = first; j0 < end; j0 += 32) equal += __popc(__ballot_sync(0xffffffffu, j0 + lane < end && key_at(j0 + lane) == prefix));
+    const int equal_before = warps_before(equal, red, &total);
+    const auto kept_of = [&](int j0, int& seen) {             // which of 32 rows stay; `seen`: equals so far
+        const uint32_t k = j0 + lane < end ? key_at(j0 + lane) : 0u;
+        const unsigned eq = __ballot_sync(0xffffffffu, j0 + lane < end && k == prefix);
+        const bool stays = j0 + lane < end && (k > prefix || (k == prefix && seen + __popc(eq & ((1u << lane) - 1u)) < left));
+        seen += __popc(eq);
+        return __ballot_sync(0xffffffffu, stays);
+    };
+    // holes: rows below m that go; moved: rows from m on that stay.  There are as many of one as of the other.
+    int holes = 0, moved = 0;
+    for (int j0 = first, seen = equal_before; j0 < end; j0 += 32) {
+        const unsigned stay = kept_of(j0, seen);
+        const unsigned below = j0 >= m ? 0u : j0 + 32 <= m ? 0xffffffffu : (1u << (m - j0)) - 1u;
+        const unsigned there = end - j0 >= 32 ? 0xffffffffu : (1u << (end - j0)) - 1u;
+        holes += __popc(~stay & below & there);
+        moved += __popc(stay & ~below);
+    }
+    int n_moves;
+    int hole_at = warps_before(holes, red, &total), moved_at = warps_before(moved, red, &n_moves);
+    int2* const moves = a.moves + s.move0;
+    for (int j0 = first, seen = equal_before; j0 < end; j0 += 32) {
+        const unsigned stay = kept_of(j0, seen);
+        const int j = j0 + lane;
+        const unsigned below = j0 >= m ? 0u : j0 + 32 <= m ? 0xffffffffu : (1u << (m - j0)) - 1u;
+        const unsigned there = end - j0 >= 32 ? 0xffffffffu : (1u << (end - j0)) - 1u;
+        const unsigned hole = ~stay & below & there, from = stay & ~below, bit = 1u << lane, lower = bit - 1u;
+        if (hole & bit) moves[hole_at + __popc(hole & lower)].y = j;
+        if (from & bit) moves[moved_at + __popc(from & lower)].x = j;
+        if (stay & below & bit) {
+            if (a.pos_out != a.pos) a.pos_out[row + j] = a.pos[row + j];
+            if (a.mass_out != a.mass) a.mass_out[row + j] = a.mass[row + j];
+            if (a.kept_idx) a.kept_idx[row + j] = j;
+        }
+        hole_at += __popc(hole);
+        moved_at += __popc(from);
+    }
+    __syncthreads();                                          // the block's writes to `moves` are visible to it
+    for (int i = t; i < n_moves; i += kThreads) {
+        const int2 mv = moves[i];
+        a.pos_out[row + mv.y] = a.pos[row + mv.x];
+        a.mass_out[row + mv.y] = a.mass[row + mv.x];
+        if (a.kept_idx) a.kept_idx[row + mv.y] = mv.x;
+    }
+    if (t == 0) {
+        a.n_moves[blockIdx.x] = n_moves;
+        if (a.kv_len_out) a.kv_len_out[s.index] = m;
+    }
+    if (a.max_moves <= kMovesInSelect) {                      // (then no other kernel moves rows)
+        const int pieces = static_cast<int>((a.row_bytes + kPiece - 1) / kPiece);
+        for (int u = warp; u < n_moves * pieces * 2; u += kWarps) {
+            const int2 mv = moves[u / (2 * pieces)];
+            const int64_t off = static_cast<int64_t>(u / 2 % pieces) * kPiece;
+            char* const base = static_cast<char*>(u & 1 ? a.v : a.k) + row * a.row_bytes + off;
+            move_piece(base + mv.y * a.row_bytes, base + mv.x * a.row_bytes, static_cast<int>(min(static_cast<int64_t>(kPiece), a.row_bytes - off)), lane);
+        }
+    }
+}
+
+__global__ void __launch_bounds__(kMoveThreads) evict_move_kernel(const __grid_constant__ EvictArgs a)
+{
+    __shared__ int64_t before[kMaxBatch + 1];
+    pdl_wait();
+    if (threadIdx.x == 0) {
+        int64_t sum = 0;
+        for (int b = 0; b < a.n_seq; ++b) {
+            before[b] = sum;
+            sum += a.n_moves[b];
+        }
+        before[a.n_seq] = sum;
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 31, pieces = static_cast<int>((a.row_bytes + kPiece - 1) / kPiece);
+    const int64_t units = before[a.n_seq] * pieces * 2, step = static_cast<int64_t>(gridDim.x) * (kMoveThreads / 32);
+    for (int64_t u = static_cast<int64_t>(blockIdx.x) * (kMoveThreads / 32) + (threadIdx.x >> 5); u < units; u += step) {
+        const int64_t i = u / (2 * pieces);
+        const int w = static_cast<int>(u - i * 2 * pieces);
+        int b = 0;
+        while (i >= before[b + 1]) ++b;
+        const EvictSeq& s = a.s[b];
+        const int2 mv = a.moves[s.move0 + i - before[b]];
+        const int64_t off = static_cast<int64_t>(w >> 1) * kPiece;
+        char* const base = static_cast<char*>(w & 1 ? a.v : a.k) + s.kv_row * a.row_bytes + off;
+        move_piece(base + mv.y * a.row_bytes, base + mv.x * a.row_bytes, static_cast<int>(min(static_cast<int64_t>(kPiece), a.row_bytes - off)), lane);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_cache_evict(const EvictArgs& a, cudaStream_t stream)
+{
+    static KernelSetup setup;
+    int longest = 0;
+    int64_t most = 0;
+    for (int b = 0; b < a.n_seq; ++b) {
+        longest = std::max(longest, a.s[b].n_kv);
+        most += std::min(a.s[b].budget, std::max(0, a.s[b].n_kv - a.s[b].budget));
+    }
+    const size_t smem = sizeof(uint32_t) * static_cast<size_t>(std::min(longest, kKeysInSmem));
+    cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(evict_select_kernel), smem, 0);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.n_seq));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, evict_select_kernel, a);
+    if (e != cudaSuccess || a.max_moves <= kMovesInSelect) return e;
+    const int64_t units = most * 2 * ((a.row_bytes + kPiece - 1) / kPiece);
+    cfg.gridDim = dim3(static_cast<unsigned>(std::min<int64_t>((units + kMoveThreads / 32 - 1) / (kMoveThreads / 32), 8 * sm_count_of_current_device())));
+    cfg.blockDim = dim3(kMoveThreads);
+    cfg.dynamicSmemBytes = 0;
+    return cudaLaunchKernelEx(&cfg, evict_move_kernel, a);
+}
+
+}  // namespace mvla

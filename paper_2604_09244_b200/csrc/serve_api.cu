@@ -1,0 +1,178 @@
+// C-ABI layer of the calls around the prune point: argument validation, plans and workspaces, launch sequencing.  No stream
+// synchronisation anywhere.
+#include "serve.h"
+#include "serve_checks.h"
+
+#include <cmath>
+#include <cstring>
+
+using namespace mvla;
+
+namespace {
+
+int32_t rope_impl(mvla_ctx* ctx, const mvla_qk_rope* r, void* stream)
+{
+    if (!ctx || !r) return MVLA_ERR_INVALID_ARG;
+    CtxView v;
+    int32_t rc = open_call(ctx, true, &v);
+    if (rc == MVLA_OK) rc = check_rope(v, r);
+    if (rc != MVLA_OK) return rc;
+    if (r->n_rows == 0 || (!r->q && !r->k && !r->v)) return MVLA_OK;
+    DeviceGuard guard(v.device);
+    if (!guard.ok) return MVLA_ERR_CUDA;
+    RopeJob job;
+    std::memset(&job, 0, sizeof job);
+    job.q = r->q; job.k = r->k; job.v = r->v; job.q_weight = r->q_weight; job.k_weight = r->k_weight;
+    job.n_rows = r->n_rows; job.q_stride = r->q_stride; job.k_stride = r->k_stride; job.v_stride = r->v_stride; job.kv_rows = r->kv_rows;
+    job.pos = r->pos; job.inv_freq = r->inv_freq; job.out_rows = r->out_rows;
+    job.q_out = r->q_out; job.k_out = r->k_out; job.v_out = r->v_out;
+    job.n_heads = v.n_heads; job.kv_heads = v.kv_heads; job.head_dim = v.head_dim; job.rot_dim = r->rot_dim;
+    job.eps = static_cast<float>(r->eps);
+    job.norm = (r->flags & MVLA_ROPE_NORM) != 0;
+    job.interleaved = (r->flags & MVLA_ROPE_INTERLEAVED) != 0;
+    return close_call(ctx, launch_qk_norm_rope(v.dtype, job, static_cast<cudaStream_t>(stream)));
+}
+
+int32_t workspace_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, int64_t* bytes)
+{
+    if (!ctx || !a || !bytes) return MVLA_ERR_INVALID_ARG;
+    CtxView v;
+    int32_t rc = open_call(ctx, false, &v);
+    if (rc == MVLA_OK) rc = check_attention(v, batch, seqs, a);
+    if (rc != MVLA_OK) return rc;
+    *bytes = plan_of(v, batch, seqs, a).bytes;
+    return MVLA_OK;
+}
+
+int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, void* stream)
+{
+    if (!ctx || !a) return MVLA_ERR_INVALID_ARG;
+    CtxView v;
+    int32_t rc = open_call(ctx, true, &v);
+    if (rc == MVLA_OK) rc = check_attention(v, batch, seqs, a);
+    if (rc != MVLA_OK) return rc;
+    const AttendPlan plan = plan_of(v, batch, seqs, a);
+    if (plan.total_q == 0) return MVLA_OK;
+    rc = check_attention_memory(v, batch, a, plan);
+    if (rc != MVLA_OK) return rc;
+    DeviceGuard guard(v.device);
+    if (!guard.ok) return MVLA_ERR_CUDA;
+    AttArgs k;
+    std::memset(&k, 0, sizeof k);
+    k.q = a->q; k.k = a->k; k.v = a->v; k.out = a->out; k.lse = a->lse; k.mass = a->mass;
+    k.q_pos = a->q_pos; k.kv_pos = a->kv_pos; k.kv_len = a->kv_len;
+    k.n_heads = v.n_heads; k.kv_heads = v.kv_heads; k.head_dim = v.head_dim; k.window = a->window; k.n_sink = a->n_sink;
+    k.scale_log2 = static_cast<float>((a->scale > 0.0 ? a->scale : 1.0 / std::sqrt(static_cast<double>(v.head_dim))) * 1.4426950408889634);   // log2 e
+    k.n_seq = batch; k.n_blocks = static_cast<int32_t>(plan.blocks);
+    k.total_q = static_cast<int32_t>(plan.total_q); k.total_kv = static_cast<int32_t>(plan.total_kv);
+    k.splits = plan.splits;
+    char* const ws = static_cast<char*>(a->workspace);
+    const auto at = [&](int64_t off) { return off < 0 ? nullptr : ws + off; };
+    k.part_o = reinterpret_cast<float*>(at(plan.part_o));
+    k.part_ml = reinterpret_cast<float2*>(at(plan.part_ml));
+    k.lse2 = reinterpret_cast<float*>(at(plan.lse2));
+    k.part_mass = reinterpret_cast<float*>(at(plan.part_mass));
+    const int group = v.n_heads / v.kv_heads;
+    int32_t blk = 0, qp = 0, kvp = 0;
+    for (int b = 0; b < batch; ++b) {
+        const mvla_seq& s = seqs[b];
+        k.s[b] = AttSeq{s.q_row, s.kv_row, s.n_q, s.n_kv, blk, qp, kvp, b};
+        blk += static_cast<int32_t>((static_cast<int64_t>(s.n_q) * group + plan.rows - 1) / plan.rows);
+        qp += s.n_q;
+        kvp += s.n_kv;
+    }
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = launch_attend_fma(v.dtype, k, plan.rows, st);
+    if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);
+    if (e == cudaSuccess && a->mass) e = launch_mass_fma(v.dtype, k, st);
+    if (e == cudaSuccess && a->mass) e = launch_mass_add(k, st);
+    return close_call(ctx, e);
+}
+
+int32_t evict_workspace_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_eviction* a, int64_t* bytes)
+{
+    if (!ctx || !a || !bytes) return MVLA_ERR_INVALID_ARG;
+    CtxView v;
+    int32_t rc = open_call(ctx, false, &v);
+    if (rc == MVLA_OK) rc = check_eviction(v, batch, seqs, a);
+    if (rc != MVLA_OK) return rc;
+    *bytes = plan_evict(batch, seqs).bytes;
+    return MVLA_OK;
+}
+
+int32_t evict_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_eviction* a, void* stream)
+{
+    if (!ctx || !a) return MVLA_ERR_INVALID_ARG;
+    CtxView v;
+    int32_t rc = open_call(ctx, true, &v);
+    if (rc == MVLA_OK) rc = check_eviction(v, batch, seqs, a);
+    if (rc != MVLA_OK) return rc;
+    const EvictPlan plan = plan_evict(batch, seqs);
+    rc = check_eviction_memory(v, batch, a, plan);
+    if (rc != MVLA_OK) return rc;
+    DeviceGuard guard(v.device);
+    if (!guard.ok) return MVLA_ERR_CUDA;
+    EvictArgs k;
+    std::memset(&k, 0, sizeof k);
+    k.k = a->k; k.v = a->v;
+    k.row_bytes = static_cast<int64_t>(v.kv_heads) * v.head_dim * static_cast<int64_t>(v.elem);
+    k.pos = a->pos; k.kv_len = a->kv_len; k.mass = a->mass;
+    k.pos_out = a->pos_out; k.kept_idx = a->kept_idx; k.kv_len_out = a->kv_len_out; k.mass_out = a->mass_out;
+    k.n_sink = a->n_sink; k.n_recent = a->n_recent; k.n_seq = batch; k.max_moves = plan.most;
+    k.moves = static_cast<int2*>(a->workspace);
+    k.n_moves = reinterpret_cast<int32_t*>(static_cast<char*>(a->workspace) + plan.count_at);
+    int64_t at = 0;
+    for (int b = 0; b < batch; ++b) {
+        k.s[b] = EvictSeq{seqs[b].kv_row, at, seqs[b].n_kv, seqs[b].budget, b};
+        at += moves_of(seqs[b]);
+    }
+    return close_call(ctx, launch_cache_evict(k, static_cast<cudaStream_t>(stream)));
+}
+
+long long ll(int64_t x) { return static_cast<long long>(x); }
+
+}  // namespace
+
+extern "C" {
+
+int32_t mvla_qk_norm_rope(mvla_ctx* ctx, const mvla_qk_rope* args, void* stream)
+{
+    ApiRange range("mvla_qk_norm_rope");
+    const int32_t rc = rope_impl(ctx, args, stream);
+    if (log_enabled()) std::fprintf(stderr, "[mvla] mvla_qk_norm_rope(rows %lld, rot_dim %lld, flags %lld) -> %d\n", ll(args ? args->n_rows : -1), ll(args ? args->rot_dim : -1), ll(args ? args->flags : 0), rc);
+    return rc;
+}
+
+int32_t mvla_window_attention(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_attention* args, void* stream)
+{
+    ApiRange range("mvla_window_attention");
+    const int32_t rc = attention_impl(ctx, batch, seqs, args, stream);
+    if (log_enabled()) std::fprintf(stderr, "[mvla] mvla_window_attention(batch %lld, window %lld, sinks %lld) -> %d\n", ll(batch), ll(args ? args->window : -1), ll(args ? args->n_sink : -1), rc);
+    return rc;
+}
+
+int32_t mvla_window_attention_workspace(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_attention* args, int64_t* bytes)
+{
+    ApiRange range("mvla_window_attention_workspace");
+    const int32_t rc = workspace_impl(ctx, batch, seqs, args, bytes);
+    if (log_enabled()) std::fprintf(stderr, "[mvla] mvla_window_attention_workspace(batch %lld) -> %d\n", ll(batch), rc);
+    return rc;
+}
+
+int32_t mvla_cache_evict(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_eviction* args, void* stream)
+{
+    ApiRange range("mvla_cache_evict");
+    const int32_t rc = evict_impl(ctx, batch, seqs, args, stream);
+    if (log_enabled()) std::fprintf(stderr, "[mvla] mvla_cache_evict(batch %lld, sinks %lld, recent %lld) -> %d\n", ll(batch), ll(args ? args->n_sink : -1), ll(args ? args->n_recent : -1), rc);
+    return rc;
+}
+
+int32_t mvla_cache_evict_workspace(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_eviction* args, int64_t* bytes)
+{
+    ApiRange range("mvla_cache_evict_workspace");
+    const int32_t rc = evict_workspace_impl(ctx, batch, seqs, args, bytes);
+    if (log_enabled()) std::fprintf(stderr, "[mvla] mvla_cache_evict_workspace(batch %lld) -> %d\n", ll(batch), rc);
+    return rc;
+}
+
+}  // extern "C"

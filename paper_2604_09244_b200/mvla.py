@@ -30,11 +30,14 @@ LABEL_BG, LABEL_ROB, LABEL_OBJ = 0, 1, 2
 FLAG_RESET_STATE, FLAG_NO_STATE_UPDATE, FLAG_INPUTS_STABLE = 1, 2, 4
 SALIENCE_AUTO, SALIENCE_FMA = 0, 1
 SET_2D, SET_3D = 1, 2
+ROPE_NORM, ROPE_INTERLEAVED = 1, 2
+WINDOW_ALL = 0x7FFFFFFF
 
 EXPORTS = ("mvla_prune_create", "mvla_salience", "mvla_select", "mvla_compact",
            "mvla_prune_step", "mvla_prune_destroy", "mvla_patch_indicators", "mvla_patch_select",
            "mvla_salience_noalloc", "mvla_selftest_wait_timeout", "mvla_set_stage_event", "mvla_set_kernel_stamps",
-           "mvla_logit_cache_stats")
+           "mvla_logit_cache_stats", "mvla_qk_norm_rope", "mvla_window_attention", "mvla_window_attention_workspace",
+           "mvla_cache_evict", "mvla_cache_evict_workspace")
 
 
 class MvlaError(RuntimeError):
@@ -88,6 +91,34 @@ class CPatchDiag(C.Structure):
                 ("mu_3d", C.c_float), ("reserved", C.c_float * 3)]
 
 
+class CSeq(C.Structure):
+    _fields_ = [("q_row", C.c_int64), ("kv_row", C.c_int64), ("n_q", C.c_int32), ("n_kv", C.c_int32),
+                ("budget", C.c_int32), ("reserved0", C.c_int32)]
+
+
+class CQkRope(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("n_rows", C.c_int64),
+                ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("q_weight", C.c_void_p), ("k_weight", C.c_void_p), ("pos", C.c_void_p), ("inv_freq", C.c_void_p),
+                ("rot_dim", C.c_int32), ("flags", C.c_uint32), ("eps", C.c_double),
+                ("q_out", C.c_void_p), ("k_out", C.c_void_p), ("v_out", C.c_void_p), ("out_rows", C.c_void_p),
+                ("kv_rows", C.c_int64)]
+
+
+class CAttention(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_rows", C.c_int64), ("kv_rows", C.c_int64),
+                ("q_pos", C.c_void_p), ("kv_pos", C.c_void_p), ("kv_len", C.c_void_p), ("window", C.c_int32),
+                ("n_sink", C.c_int32), ("scale", C.c_double), ("out", C.c_void_p), ("lse", C.c_void_p),
+                ("mass", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
+class CEviction(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("kv_rows", C.c_int64), ("pos", C.c_void_p), ("mass", C.c_void_p),
+                ("pos_out", C.c_void_p), ("mass_out", C.c_void_p), ("kept_idx", C.c_void_p), ("kv_len", C.c_void_p),
+                ("kv_len_out", C.c_void_p), ("n_sink", C.c_int32), ("n_recent", C.c_int32), ("workspace", C.c_void_p),
+                ("workspace_bytes", C.c_int64)]
+
+
 def load_library(path: str = LIB_PATH) -> C.CDLL:
     if not os.path.exists(path):
         raise OSError(f"{path} is missing: build it with `python -m paper_2604_09244_b200.build` "
@@ -120,6 +151,15 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.mvla_set_stage_event.restype = i32
     lib.mvla_selftest_wait_timeout.argtypes = [vp, u32, vp]
     lib.mvla_selftest_wait_timeout.restype = i32
+    sq = C.POINTER(CSeq)
+    lib.mvla_qk_norm_rope.argtypes = [vp, C.POINTER(CQkRope), vp]
+    lib.mvla_window_attention.argtypes = [vp, i32, sq, C.POINTER(CAttention), vp]
+    lib.mvla_window_attention_workspace.argtypes = [vp, i32, sq, C.POINTER(CAttention), C.POINTER(i64)]
+    lib.mvla_cache_evict.argtypes = [vp, i32, sq, C.POINTER(CEviction), vp]
+    lib.mvla_cache_evict_workspace.argtypes = [vp, i32, sq, C.POINTER(CEviction), C.POINTER(i64)]
+    for fn in ("mvla_qk_norm_rope", "mvla_window_attention", "mvla_window_attention_workspace", "mvla_cache_evict",
+               "mvla_cache_evict_workspace"):
+        getattr(lib, fn).restype = i32
     return lib
 
 
@@ -154,6 +194,22 @@ def c_samples(samples: Sequence) -> "C.Array[CSample]":
     arr = (CSample * len(samples))()
     native().fill_samples(arr, samples)
     return arr
+
+
+@dataclass
+class Seq:
+    """One sequence of a cache call (``mvla_seq``): its queries, its run of cached rows, and how many may stay."""
+    q_row: int = 0
+    n_q: int = 0
+    kv_row: int = 0
+    n_kv: int = 0
+    budget: int = 0
+
+
+def c_seqs(seqs: Sequence[Seq]) -> "C.Array[CSeq]":
+    """The descriptors as the library takes them.  A program whose caches keep their places makes this array once and writes
+    its fields."""
+    return (CSeq * len(seqs))(*[CSeq(s.q_row, s.kv_row, s.n_q, s.n_kv, s.budget, 0) for s in seqs])
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -349,6 +405,57 @@ class PruneContext:
             raise MvlaError(rc, "mvla_prune_step")
         out.total_kept = rc
         return out
+
+    # -- around the prune point (`seqs`: a ctypes array from c_seqs, or Seq objects) ------------------------------------------
+    def _shape(self):
+        c = self.cfg
+        return c.dtype, c.n_heads, c.n_kv_heads or c.n_heads, c.head_dim, c.device
+
+    def qk_norm_rope(self, q, k, pos, inv_freq, *, v=None, q_weight=None, k_weight=None, norm=True, eps=1e-6, interleaved=False,
+                     q_out=None, k_out=None, v_out=None, out_rows=None, stream=None):
+        """Norms of queries and keys for each head and the position rotation (``mvla_qk_norm_rope``); `v` rows are copied along.
+
+        q, k, v: [rows, heads, head_dim] of the hidden type; slices of a fused projection need no copy.  pos: int32 [rows];
+        inv_freq: float64 [rot_dim / 2] (None: no rotation).  k_out / v_out: packed rows, or a cache of which row i of the call
+        becomes row out_rows[i] (a row outside the cache is dropped).  Outputs that are not given are allocated; returned as
+        (q_out, k_out, v_out)."""
+        def out(src, dst):
+            if src is None or dst is not None:
+                return dst
+            if src is not q and out_rows is not None:
+                raise ValueError("out_rows: rows of a k_out / v_out that is given")
+            with torch.cuda.stream(stream):
+                return torch.empty(src.shape, dtype=self.torch_dtype, device=self.device)
+        q_out, k_out, v_out = out(q, q_out), out(k, k_out), out(v, v_out)
+        flags = (ROPE_NORM if norm else 0) | (ROPE_INTERLEAVED if interleaved else 0)
+        rc = self._nat.qk_norm_rope(self._h.value or 0, *self._shape(), q, k, v, pos, inv_freq, q_weight, k_weight, flags, eps,
+                                    q_out, k_out, v_out, out_rows, stream)
+        if rc != OK:
+            raise MvlaError(rc, "mvla_qk_norm_rope")
+        return q_out, k_out, v_out
+
+    def window_attention(self, seqs, q, k, v, *, window=None, n_sink=0, scale=0.0, q_pos=None, kv_pos=None, kv_len=None, out=None,
+                         lse=None, mass=None, stream=None):
+        """Causal attention with a sliding window (None: everything before a query) and `n_sink` first positions that stay
+        visible, over packed rows or a cache (``mvla_window_attention``).  `mass` (float32 [cached rows]) is added to, `lse`
+        (float32 [rows, heads]) written.  Returns `out` (allocated where it is not given: rows outside the sequences then
+        hold anything)."""
+        cs = seqs if isinstance(seqs, C.Array) else c_seqs(seqs)
+        rc, out = self._nat.window_attention(self._h.value or 0, *self._shape(), cs, q, k, v, WINDOW_ALL if window is None else window,
+                                             n_sink, scale, q_pos, kv_pos, kv_len, out, lse, mass, stream)
+        if rc != OK:
+            raise MvlaError(rc, "mvla_window_attention")
+        return out
+
+    def cache_evict(self, seqs, k, v, pos, mass, *, n_sink=0, n_recent=0, pos_out=None, mass_out=None, kept_idx=None, kv_len=None,
+                    kv_len_out=None, stream=None) -> None:
+        """Keeps the `budget` rows of every sequence that matter most by accumulated attention weight, in front of its run, in
+        place (``mvla_cache_evict``).  pos and mass are rewritten too unless pos_out / mass_out are given."""
+        cs = seqs if isinstance(seqs, C.Array) else c_seqs(seqs)
+        rc = self._nat.cache_evict(self._h.value or 0, *self._shape(), cs, k, v, pos, mass, pos if pos_out is None else pos_out,
+                                   mass if mass_out is None else mass_out, kept_idx, kv_len, kv_len_out, n_sink, n_recent, stream)
+        if rc != OK:
+            raise MvlaError(rc, "mvla_cache_evict")
 
 
 def context_for(wl, *, max_batch=None, n_prune_points=1, n_state_slots=0, salience_path=SALIENCE_AUTO,
