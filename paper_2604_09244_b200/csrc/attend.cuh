@@ -12,9 +12,10 @@ __device__ __forceinline__ int seq_len(const AttArgs& a, const AttSeq& s)
 {
     return a.kv_len ? min(max(a.kv_len[s.index], 0), s.n_kv) : s.n_kv;
 }
+// (all negative positions see the same, nothing: one of them will do)
 __device__ __forceinline__ int query_pos(const AttArgs& a, const AttSeq& s, int len, int i)
 {
-    return a.q_pos ? a.q_pos[s.q_row + i] : len - s.n_q + i;
+    return max(a.q_pos ? a.q_pos[s.q_row + i] : len - s.n_q + i, -1);
 }
 // Position of row j of a sequence, -1 where nobody sees it.
 __device__ __forceinline__ int key_pos(const AttArgs& a, const AttSeq& s, int len, int j)

@@ -1,4 +1,4 @@
-// What follows the attention kernels: parts of a split key range joined, and the weights of the key heads added into the
+// What follows the attention kernels: parts of a split key range joined, and the weights of the heads added into the
 // accumulated weight of every cached row.
 #include "attend.cuh"
 
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_cons
     }
 }
 
-// One thread adds the key heads' weights of one cached row, in their order.
+// One thread adds the parts' weights of one cached row, in their order.
 __global__ void __launch_bounds__(kThreads) mass_add_kernel(const __grid_constant__ AttArgs a)
 {
     pdl_wait();
@@ -61,7 +61,7 @@ __global__ void __launch_bounds__(kThreads) mass_add_kernel(const __grid_constan
     const int j = static_cast<int>(at) - s.kvp0;
     if (s.n_q == 0 || j >= seq_len(a, s)) return;
     float sum = 0.f;
-    for (int h = 0; h < a.kv_heads; ++h) sum += a.part_mass[static_cast<int64_t>(h) * a.total_kv + at];
+    for (int h = 0; h < a.mass_parts; ++h) sum += a.part_mass[static_cast<int64_t>(h) * a.total_kv + at];
     if (sum != 0.f) a.mass[s.kv_row + j] += sum / static_cast<float>(a.n_heads);
 }
 

@@ -33,19 +33,35 @@ struct Workspace {
     }
 };
 
+constexpr int kMaxTiles = 2048;          // tiles of keys that a CTA of the tile kernels walks (its list of them: 11 bits an entry)
+
+// kFormFma: by FMAs.  kFormTile: by tiles of 128 query rows on the tensor cores (e4m3: after widening to fp16).
+enum AttendForm { kFormFma, kFormTile };
+
 struct AttendPlan {
+    AttendForm form = kFormFma;
     int32_t rows = 32;           // query rows of a block (a block shares a key head: queries x heads of a group)
-    int32_t splits = 1;
+    int32_t pack = 1;            // heads side by side in a tile of rows
+    int32_t queries = 0;         // queries of a block of the tile form
+    int32_t splits = 1, mass_parts = 1;
     int64_t total_q = 0, total_kv = 0, blocks = 0;
     // offsets in the workspace, -1: not used
-    int64_t part_o = -1, part_ml = -1, lse2 = -1, part_mass = -1, bytes = 0;
+    int64_t part_o = -1, part_ml = -1, lse2 = -1, part_mass = -1, wide_q = -1, wide_k = -1, wide_v = -1, bytes = 0;
 };
+
+// Heads of a group that share a tile of 128 rows: as many as divide the group, 32 at most.
+inline int pack_of(int group)
+{
+    int p = group < 32 ? group : 32;
+    while (group % p) --p;
+    return p;
+}
 
 inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, bool mass)
 {
     AttendPlan p;
     const int group = c.n_heads / c.kv_heads;
-    int64_t longest = 0, most_rows = 0;
+    int64_t longest = 0, longest_kv = 0, most_rows = 0;
     for (int b = 0; b < batch; ++b) {
         const mvla_seq& s = seqs[b];
         p.total_q += s.n_q;
@@ -53,18 +69,47 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
         if (s.n_q == 0) continue;
         const int64_t keys = visible_keys(s, counted, window, n_sink), rows = static_cast<int64_t>(s.n_q) * group;
         longest = keys > longest ? keys : longest;
+        longest_kv = s.n_kv > longest_kv ? s.n_kv : longest_kv;
         most_rows = rows > most_rows ? rows : most_rows;
     }
-    p.rows = most_rows <= 8 ? 8 : 32;
-    for (int b = 0; b < batch; ++b) p.blocks += (static_cast<int64_t>(seqs[b].n_q) * group + p.rows - 1) / p.rows;
-    if (p.blocks > 0) {
-        // enough CTAs for every multiprocessor twice, of at least four tiles of 64 keys
-        const int64_t ctas = p.blocks * c.kv_heads;
-        int64_t n = (2 * static_cast<int64_t>(c.sm_count) + ctas - 1) / ctas;
-        const int64_t most = longest / 256;
-        n = n > most ? most : n;
-        n = n > 64 ? 64 : n;
-        p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
+    if (c.dtype == MVLA_DTYPE_FP32) {
+        p.rows = most_rows <= 8 ? 8 : 32;
+        p.mass_parts = c.kv_heads;
+        for (int b = 0; b < batch; ++b) p.blocks += (static_cast<int64_t>(seqs[b].n_q) * group + p.rows - 1) / p.rows;
+        if (p.blocks > 0) {
+            // enough CTAs for every multiprocessor twice, of at least four tiles of 64 keys
+            const int64_t ctas = p.blocks * c.kv_heads;
+            int64_t n = (2 * static_cast<int64_t>(c.sm_count) + ctas - 1) / ctas;
+            const int64_t most = longest / 256;
+            n = n > most ? most : n;
+            n = n > 64 ? 64 : n;
+            p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
+        }
+    } else {
+        p.form = kFormTile;
+        p.pack = pack_of(group);
+        const int per = 128 / p.pack;
+        const bool two = c.head_dim <= 128;                  // tiles of rows in a CTA, and the keys of a tile (attend_tile.cu)
+        const int64_t tile = two ? 128 : 64;
+        p.queries = two ? 2 * per : per;
+        int64_t most_q = 0;
+        for (int b = 0; b < batch; ++b) {
+            p.blocks += (static_cast<int64_t>(seqs[b].n_q) + p.queries - 1) / p.queries;
+            most_q = seqs[b].n_q > most_q ? seqs[b].n_q : most_q;
+        }
+        const int64_t packs = c.n_heads / p.pack;
+        if (p.blocks > 0) {
+            // one CTA to a multiprocessor; parts of at least four tiles; and no more tiles than a CTA's list holds
+            const int64_t ctas = p.blocks * packs, tiles = (longest + tile - 1) / tile;
+            int64_t n = c.sm_count / ctas;
+            const int64_t most = tiles / 4, least = ((longest_kv + tile - 1) / tile + kMaxTiles - 1) / kMaxTiles;
+            n = n > most ? most : n;
+            n = n > 64 ? 64 : n;
+            n = n < least ? least : n;
+            p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
+        }
+        const int64_t runs = ((most_q + per - 1) / per + kMaxTiles - 1) / kMaxTiles;
+        p.mass_parts = static_cast<int32_t>(packs * (runs < 1 ? 1 : runs));
     }
     Workspace w;
     const int64_t qh = p.total_q * c.n_heads;
@@ -74,7 +119,12 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
     }
     if (mass) {
         p.lse2 = w.take(qh * static_cast<int64_t>(sizeof(float)));
-        p.part_mass = w.take(c.kv_heads * p.total_kv * static_cast<int64_t>(sizeof(float)));
+        p.part_mass = w.take(p.mass_parts * p.total_kv * static_cast<int64_t>(sizeof(float)));
+    }
+    if (p.form == kFormTile && c.dtype == MVLA_DTYPE_FP8_E4M3) {
+        p.wide_q = w.take(qh * c.head_dim * 2);
+        p.wide_k = w.take(p.total_kv * c.kv_heads * c.head_dim * 2);
+        p.wide_v = w.take(p.total_kv * c.kv_heads * c.head_dim * 2);
     }
     p.bytes = w.bytes;
     return p;

@@ -27,6 +27,7 @@ struct AttSeq {
     int32_t n_q, n_kv;
     int32_t blk0;                // first of its blocks of query rows in the launch (a block: rows of one key head)
     int32_t qp0, kvp0;           // its first query / cached row among those of the batch, packed
+    int32_t qm_row, km_row;      // where its queries and cached rows begin in the tensor maps (kernels by tiles)
     int32_t index;               // its place in the caller's batch (kv_len)
 };
 struct AttArgs {
@@ -42,7 +43,10 @@ struct AttArgs {
     float* part_o;               // [splits][total_q][n_heads][head_dim] sums against the part's own maximum   (splits > 1)
     float2* part_ml;             // [splits][total_q][n_heads] (maximum, sum of exponentials), powers of two
     float* lse2;                 // [total_q][n_heads] logarithm to base 2 of the sum of exponentials          (with mass)
-    float* part_mass;            // [kv_heads][total_kv]                                                       (with mass)
+    float* part_mass;            // [mass_parts][total_kv]                                                     (with mass)
+    int32_t mass_parts;
+    int32_t pack;                // heads of a group side by side in a tile of rows (kernels by tiles)
+    int* status;                 // word that receives MVLA_ERR_TIMEOUT when a bounded wait gives up
     AttSeq s[kMaxBatch];
 };
 
@@ -50,9 +54,18 @@ struct AttArgs {
 cudaError_t launch_attend_fma(int dtype, const AttArgs& a, int rows, cudaStream_t stream);
 // The weights of every cached row over the queries of its sequence, by key head, into part_mass (by FMAs in 32 bits).
 cudaError_t launch_mass_fma(int dtype, const AttArgs& a, cudaStream_t stream);
+// bf16 (f16: what launch_widen made) by tiles of 128 rows on the tensor cores; at most kMaxTiles tiles of keys to a split.
+struct AttMaps {
+    CUtensorMap q, k, v;
+};
+cudaError_t launch_attend_tile(bool f16, const AttArgs& a, const AttMaps& maps, cudaStream_t stream);
+// The weights as above, by tiles of 128 keys.  (mass_parts: packs of heads, times runs of kMaxTiles tiles of queries)
+cudaError_t launch_attend_weights(bool f16, const AttArgs& a, const AttMaps& maps, cudaStream_t stream);
+// The sequences' e4m3 rows as packed fp16 rows.
+cudaError_t launch_widen(const AttArgs& a, void* wide_q, void* wide_k, void* wide_v, cudaStream_t stream);
 // part_o / part_ml -> out, lse, lse2.
 cudaError_t launch_attend_join(int dtype, const AttArgs& a, cudaStream_t stream);
-// mass += part_mass over the key heads.
+// mass += part_mass over its parts.
 cudaError_t launch_mass_add(const AttArgs& a, cudaStream_t stream);
 
 // ---- eviction by accumulated weight

@@ -44,6 +44,47 @@ int32_t workspace_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     return MVLA_OK;
 }
 
+// (head_dim, heads, rows) of a token-major tensor, in boxes of 64 elements x `box_heads` x `box_rows`: rows of 128 bytes in shared memory,
+// 128-byte swizzle, heads of a token next to one another.
+bool row_map(const CtxView& v, CUtensorMap* m, const void* p, int heads, int64_t rows, int box_heads, int box_rows)
+{
+    const cuuint64_t dims[3] = {static_cast<cuuint64_t>(v.head_dim), static_cast<cuuint64_t>(heads), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[2] = {static_cast<cuuint64_t>(v.head_dim) * 2, static_cast<cuuint64_t>(v.head_dim) * 2 * heads};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(box_heads), static_cast<cuuint32_t>(box_rows)}, step[3] = {1, 1, 1};
+    return v.encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(p), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                    CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// The tile form: tensor maps over the caller's bf16 rows, or over their widened copies.
+int32_t attend_by_tiles(const CtxView& v, AttArgs& k, const mvla_attention* a, const AttendPlan& plan, cudaError_t* e, cudaStream_t st)
+{
+    const bool widen = plan.wide_q >= 0;
+    char* const ws = static_cast<char*>(a->workspace);
+    const void* const q = widen ? ws + plan.wide_q : a->q;
+    const void* const kk = widen ? ws + plan.wide_k : a->k;
+    const void* const vv = widen ? ws + plan.wide_v : a->v;
+    const int64_t q_rows = widen ? plan.total_q : a->q_rows, kv_rows = widen ? plan.total_kv : a->kv_rows;
+    for (int b = 0; b < k.n_seq; ++b) {
+        AttSeq& s = k.s[b];
+        s.qm_row = widen ? s.qp0 : static_cast<int32_t>(s.q_row);
+        s.km_row = widen ? s.kvp0 : static_cast<int32_t>(s.kv_row);
+    }
+    AttMaps maps;
+    std::memset(&maps, 0, sizeof maps);
+    const int tile = v.head_dim <= 128 ? 128 : 64;
+    if (!row_map(v, &maps.q, q, v.n_heads, q_rows, plan.pack, 128 / plan.pack)) return MVLA_ERR_CUDA;
+    // (no cached rows: no key tile is ever asked for)
+    if (plan.total_kv > 0 && (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, tile) || !row_map(v, &maps.v, vv, v.kv_heads, kv_rows, 1, tile))) return MVLA_ERR_CUDA;
+    *e = widen ? launch_widen(k, ws + plan.wide_q, ws + plan.wide_k, ws + plan.wide_v, st) : cudaSuccess;
+    if (*e == cudaSuccess) *e = launch_attend_tile(widen, k, maps, st);
+    if (*e == cudaSuccess && plan.splits > 1) *e = launch_attend_join(v.dtype, k, st);
+    if (*e == cudaSuccess && a->mass && plan.total_kv > 0) {
+        if (tile != 128 && !row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, 128)) return MVLA_ERR_CUDA;
+        *e = launch_attend_weights(widen, k, maps, st);
+    }
+    return MVLA_OK;
+}
+
 int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, void* stream)
 {
     if (!ctx || !a) return MVLA_ERR_INVALID_ARG;
@@ -65,7 +106,7 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     k.scale_log2 = static_cast<float>((a->scale > 0.0 ? a->scale : 1.0 / std::sqrt(static_cast<double>(v.head_dim))) * 1.4426950408889634);   // log2 e
     k.n_seq = batch; k.n_blocks = static_cast<int32_t>(plan.blocks);
     k.total_q = static_cast<int32_t>(plan.total_q); k.total_kv = static_cast<int32_t>(plan.total_kv);
-    k.splits = plan.splits;
+    k.splits = plan.splits; k.mass_parts = plan.mass_parts; k.pack = plan.pack; k.status = v.status_dev;
     char* const ws = static_cast<char*>(a->workspace);
     const auto at = [&](int64_t off) { return off < 0 ? nullptr : ws + off; };
     k.part_o = reinterpret_cast<float*>(at(plan.part_o));
@@ -76,15 +117,22 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     int32_t blk = 0, qp = 0, kvp = 0;
     for (int b = 0; b < batch; ++b) {
         const mvla_seq& s = seqs[b];
-        k.s[b] = AttSeq{s.q_row, s.kv_row, s.n_q, s.n_kv, blk, qp, kvp, b};
-        blk += static_cast<int32_t>((static_cast<int64_t>(s.n_q) * group + plan.rows - 1) / plan.rows);
+        k.s[b] = AttSeq{s.q_row, s.kv_row, s.n_q, s.n_kv, blk, qp, kvp, 0, 0, b};
+        blk += static_cast<int32_t>(plan.form == kFormTile ? (static_cast<int64_t>(s.n_q) + plan.queries - 1) / plan.queries
+                                                           : (static_cast<int64_t>(s.n_q) * group + plan.rows - 1) / plan.rows);
         qp += s.n_q;
         kvp += s.n_kv;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    cudaError_t e = launch_attend_fma(v.dtype, k, plan.rows, st);
-    if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);
-    if (e == cudaSuccess && a->mass) e = launch_mass_fma(v.dtype, k, st);
+    cudaError_t e = cudaSuccess;
+    if (plan.form == kFormTile) {
+        rc = attend_by_tiles(v, k, a, plan, &e, st);
+        if (rc != MVLA_OK) return rc;
+    } else {
+        e = launch_attend_fma(v.dtype, k, plan.rows, st);
+        if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);
+        if (e == cudaSuccess && a->mass) e = launch_mass_fma(v.dtype, k, st);
+    }
     if (e == cudaSuccess && a->mass) e = launch_mass_add(k, st);
     return close_call(ctx, e);
 }

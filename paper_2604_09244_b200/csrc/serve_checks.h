@@ -118,6 +118,7 @@ inline int32_t check_attention(const ServeShape& v, int32_t batch, const mvla_se
         total_q += s.n_q;
         total_kv += s.n_kv;
     }
+    if (v.dtype != MVLA_DTYPE_FP32 && (a->q_rows > 0x7FFFFFFF || a->kv_rows > 0x7FFFFFFF)) return MVLA_ERR_UNSUPPORTED;   // (rows of a tensor map are counted in 32 bits)
     if (total_q * v.n_heads / v.kv_heads > kMaxRows || total_kv > 0x7FFFFFFF) return MVLA_ERR_UNSUPPORTED;
     if (shared_rows(batch, seqs, [](const mvla_seq& s) { return s.q_row; }, [](const mvla_seq& s) { return s.n_q; })) return MVLA_ERR_INVALID_ARG;
     if (a->mass && shared_rows(batch, seqs, [](const mvla_seq& s) { return s.kv_row; }, [](const mvla_seq& s) { return s.n_kv; }))
