@@ -114,7 +114,7 @@ __device__ __forceinline__ int compact_entries(uint16_t* list, int n, int lane)
     return count;
 }
 
-// Bounded waits of a CTA: the first that runs out makes all others give up.
+// Bounded waits of a CTA: when one runs out, the others end without waiting for long.
 struct Guard {
     int* dead;
     int* status;
@@ -124,7 +124,12 @@ struct Guard {
     {
         if (mbar_try_wait<false>(bar, parity)) return true;
         if (*reinterpret_cast<volatile int*>(dead)) return false;
-        if (mbar_wait(bar, parity)) return true;
+        // (the clock of the multiprocessor, about a second of it; the global timer takes a microsecond to read)
+        const long long t0 = clock64();
+        for (uint32_t it = 1; it < kSpinLimit; ++it) {
+            if (mbar_try_wait<false>(bar, parity)) return true;
+            if ((it & 63u) == 0 && clock64() - t0 > 2000000000ll) break;
+        }
         *reinterpret_cast<volatile int*>(dead) = 1;
         *reinterpret_cast<volatile int*>(status) = MVLA_ERR_TIMEOUT;
         return false;
@@ -333,25 +338,26 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             if (!ok) break;
             tc_fence_after();
             const uint32_t s_col = tmem + buf * Sh::kS + lanes;
-            float x[BN];
-#pragma unroll
-            for (int c = 0; c < BN; c += 32) tmem_ld_cols<32>(s_col + c, *reinterpret_cast<float(*)[32]>(x + c));
-            if (e >> tile & kMask) {
+            if (e >> tile & kMask) {                         // (in place, in small pieces: the registers are for the scores)
                 const int j0 = range.tile(v0 + (e >> kEntryShift)) * BN;
-                if (a.kv_pos) {
-                    const int* const pos = a.kv_pos + s.kv_row + j0;
-                    const int there = len - j0;
+                const int last = min(p, len - 1) - j0, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
+#pragma unroll 1
+                for (int c0 = 0; c0 < BN; c0 += 16) {
+                    float y[16];
+                    uint32_t w[16];
+                    tmem_ld_cols<16>(s_col + c0, y);
 #pragma unroll
-                    for (int c = 0; c < BN; ++c) {
-                        const int k = c < there ? pos[c] : -1;
-                        x[c] = sees(p, k, a.window, a.n_sink) ? x[c] : -CUDART_INF_F;
+                    for (int c = 0; c < 16; ++c) {
+                        const int at = c0 + c;
+                        const bool seen_by = a.kv_pos ? sees(p, key_pos(a, s, len, j0 + at), a.window, a.n_sink) : at <= last && (at >= first || at < sink);
+                        w[c] = seen_by ? __float_as_uint(y[c]) : 0xFF800000u;      // -infinity
                     }
-                } else {
-                    const int last = min(p, len - 1) - j0, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
-#pragma unroll
-                    for (int c = 0; c < BN; ++c) x[c] = c <= last && (c >= first || c < sink) ? x[c] : -CUDART_INF_F;
+                    tmem_st_cols<16>(s_col + c0, w);
                 }
+                tmem_st_wait();
             }
+            float x[BN];
+            tmem_ld_cols<BN>(s_col, x);
             float tops[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
             for (int c = 4; c < BN; ++c) tops[c & 3] = fmaxf(tops[c & 3], x[c]);
@@ -363,13 +369,14 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                 if (!ok) break;
                 tc_fence_after();
                 const float f = move ? ex2_approx(m - top) : 1.f;
-                for (int c = 0; c < a.head_dim; c += 32) {
-                    float o[32];
-                    uint32_t w[32];
-                    tmem_ld_cols<32>(o_col + c, o);
+#pragma unroll 1
+                for (int c = 0; c < a.head_dim; c += 16) {
+                    float o[16];
+                    uint32_t w[16];
+                    tmem_ld_cols<16>(o_col + c, o);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(o[k] * f);
-                    tmem_st_cols<32>(o_col + c, w);
+                    for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(o[k] * f);
+                    tmem_st_cols<16>(o_col + c, w);
                 }
                 l *= f;
             }
@@ -377,16 +384,16 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             const float ref = m == -CUDART_INF_F ? 0.f : m;
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c0 = 0; c0 < BN; c0 += 64) {
-                uint32_t w[32];
+            for (int c0 = 0; c0 < BN; c0 += 32) {
+                uint32_t w[16];
 #pragma unroll
-                for (int c = 0; c < 64; c += 2) {
+                for (int c = 0; c < 32; c += 2) {
                     const float y = ex2_approx(fmaf(x[c0 + c], scale, -ref)), z = ex2_approx(fmaf(x[c0 + c + 1], scale, -ref));
                     sum[c & 2] += y;
                     sum[(c & 2) + 1] += z;
                     w[c / 2] = F16 ? two_f16(y, z) : two_bf16(y, z);
                 }
-                tmem_st_cols<32>(s_col + c0 / 2, w);
+                tmem_st_cols<16>(s_col + c0 / 2, w);
             }
             l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
             tmem_st_wait();
