@@ -32,19 +32,22 @@ __device__ __forceinline__ bool some_sees(int lo, int hi, int c, int window, int
 {
     return c >= 0 && c <= hi && (c >= lo || lo - c < window || c < n_sink);
 }
+// The last sequence whose field (ascending over the batch) is not above x: by halves, since every look costs a constant load's latency.
+template <class Field>
+__device__ __forceinline__ int seq_at(const AttArgs& a, int x, Field field)
+{
+    int lo = 0, n = a.n_seq;
+    while (n > 1) {
+        const int half = n >> 1;
+        if (field(a.s[lo + half]) <= x) lo += half;
+        n -= half;
+    }
+    return lo;
+}
 // The block of the launch's grid that `blk` is: its sequence.
-__device__ __forceinline__ int seq_of_block(const AttArgs& a, int blk)
-{
-    int b = 0;
-    while (b + 1 < a.n_seq && blk >= a.s[b + 1].blk0) ++b;
-    return b;
-}
-__device__ __forceinline__ int seq_of_query(const AttArgs& a, int qp)
-{
-    int b = 0;
-    while (b + 1 < a.n_seq && qp >= a.s[b + 1].qp0) ++b;
-    return b;
-}
+__device__ __forceinline__ int seq_of_block(const AttArgs& a, int blk) { return seq_at(a, blk, [](const AttSeq& s) { return s.blk0; }); }
+__device__ __forceinline__ int seq_of_query(const AttArgs& a, int qp) { return seq_at(a, qp, [](const AttSeq& s) { return s.qp0; }); }
+__device__ __forceinline__ int seq_of_key(const AttArgs& a, int kvp) { return seq_at(a, kvp, [](const AttSeq& s) { return s.kvp0; }); }
 // Tiles of `tile` keys that queries at [lo, hi] may see: `sinks` tiles from the first on, then those from `first` on, `count` in all.
 // Where the positions are data every tile of the sequence is named, and looked at when it comes up.
 struct TileRange {

@@ -210,7 +210,7 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
             const float l = row_l[r], f = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
             const float4 x = make_float4(o[n][0] * f, o[n][1] * f, o[n][2] * f, o[n][3] * f);
             if (whole) store4(static_cast<typename OutOf<T>::type*>(a.out) + ((s.q_row + i) * a.n_heads + h) * d + ocol, x);
-            else store4(a.part_o + ((static_cast<int64_t>(blockIdx.z) * a.total_q + s.qp0 + i) * a.n_heads + h) * d + ocol, x);
+            else store4(a.part_o + ((s.part0 + static_cast<int64_t>(blockIdx.z) * s.n_q + i) * a.n_heads + h) * d + ocol, x);
         }
     }
     if (t < n_rows) {
@@ -220,7 +220,7 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
             if (a.lse) a.lse[(s.q_row + i) * a.n_heads + h] = z * 0.69314718055994531f;      // ln 2
             if (a.mass) a.lse2[static_cast<int64_t>(s.qp0 + i) * a.n_heads + h] = z;
         } else {
-            a.part_ml[(static_cast<int64_t>(blockIdx.z) * a.total_q + s.qp0 + i) * a.n_heads + h] = make_float2(row_m[t], row_l[t]);
+            a.part_ml[(s.part0 + static_cast<int64_t>(blockIdx.z) * s.n_q + i) * a.n_heads + h] = make_float2(row_m[t], row_l[t]);
         }
     }
 }

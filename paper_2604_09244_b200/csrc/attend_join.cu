@@ -21,21 +21,23 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_cons
     if (unit >= static_cast<int64_t>(a.total_q) * a.n_heads) return;
     const int qp = static_cast<int>(unit / a.n_heads), h = static_cast<int>(unit % a.n_heads);
     const AttSeq& s = a.s[seq_of_query(a, qp)];
-    const int64_t row = s.q_row + (qp - s.qp0), step = static_cast<int64_t>(a.total_q) * a.n_heads;
+    const int64_t row = s.q_row + (qp - s.qp0), step = static_cast<int64_t>(s.n_q) * a.n_heads;
+    const int64_t first = (s.part0 + (qp - s.qp0)) * a.n_heads + h;
+    if (a.skip_whole && s.parts == 1) return;                // (written already)
     float m = -CUDART_INF_F;
-    for (int p = 0; p < a.splits; ++p) m = fmaxf(m, a.part_ml[p * step + unit].x);
+    for (int p = 0; p < s.parts; ++p) m = fmaxf(m, a.part_ml[first + p * step].x);
     const float ref = m == -CUDART_INF_F ? 0.f : m;
     float l = 0.f;
-    for (int p = 0; p < a.splits; ++p) {
-        const float2 ml = a.part_ml[p * step + unit];
+    for (int p = 0; p < s.parts; ++p) {
+        const float2 ml = a.part_ml[first + p * step];
         l += ml.y * exp2f(ml.x - ref);
     }
     const float inv = l > 0.f ? 1.f / l : 0.f;
     for (int c = 2 * lane; c < a.head_dim; c += 64) {
         float x = 0.f, y = 0.f;
-        for (int p = 0; p < a.splits; ++p) {
-            const float f = exp2f(a.part_ml[p * step + unit].x - ref);
-            const float2 o = *reinterpret_cast<const float2*>(a.part_o + (p * step + unit) * a.head_dim + c);
+        for (int p = 0; p < s.parts; ++p) {
+            const float f = exp2f(a.part_ml[first + p * step].x - ref);
+            const float2 o = *reinterpret_cast<const float2*>(a.part_o + (first + p * step) * a.head_dim + c);
             x = fmaf(o.x, f, x);
             y = fmaf(o.y, f, y);
         }
@@ -55,9 +57,7 @@ __global__ void __launch_bounds__(kThreads) mass_add_kernel(const __grid_constan
     pdl_trigger();
     const int64_t at = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
     if (at >= a.total_kv) return;
-    int b = 0;
-    while (b + 1 < a.n_seq && at >= a.s[b + 1].kvp0) ++b;
-    const AttSeq& s = a.s[b];
+    const AttSeq& s = a.s[seq_of_key(a, static_cast<int>(at))];
     const int j = static_cast<int>(at) - s.kvp0;
     if (s.n_q == 0 || j >= seq_len(a, s)) return;
     float sum = 0.f;

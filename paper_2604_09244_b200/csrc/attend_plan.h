@@ -36,7 +36,8 @@ struct Workspace {
 constexpr int kMaxTiles = 2048;          // tiles of keys that a CTA of the tile kernels walks (its list of them: 11 bits an entry)
 
 // kFormFma: by FMAs.  kFormTile: by tiles of 128 query rows on the tensor cores (e4m3: after widening to fp16).
-enum AttendForm { kFormFma, kFormTile };
+// kFormToken: at most 16 query rows to a key head, straight from global memory.
+enum AttendForm { kFormFma, kFormTile, kFormToken };
 
 struct AttendPlan {
     AttendForm form = kFormFma;
@@ -46,8 +47,19 @@ struct AttendPlan {
     int32_t splits = 1, mass_parts = 1;
     int64_t total_q = 0, total_kv = 0, blocks = 0;
     // offsets in the workspace, -1: not used
-    int64_t part_o = -1, part_ml = -1, lse2 = -1, part_mass = -1, wide_q = -1, wide_k = -1, wide_v = -1, bytes = 0;
+    int64_t part_o = -1, part_ml = -1, lse2 = -1, part_mass = -1, wide_q = -1, wide_k = -1, wide_v = -1, logits = -1, bytes = 0;
+    int64_t part_keys = 0;       // single tokens: keys of a part
+    int64_t logit_floats = 0;
 };
+
+// Parts that a sequence's visible keys are cut into.
+inline int32_t parts_of(const AttendPlan& p, const mvla_seq& s, bool counted, int32_t window, int32_t n_sink)
+{
+    if (s.n_q == 0) return 0;
+    if (p.form != kFormToken) return p.splits;
+    const int64_t n = (visible_keys(s, counted, window, n_sink) + p.part_keys - 1) / p.part_keys;
+    return n < 1 ? 1 : static_cast<int32_t>(n);
+}
 
 // Heads of a group that share a tile of 128 rows: as many as divide the group, 32 at most.
 inline int pack_of(int group)
@@ -85,6 +97,28 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
             n = n > 64 ? 64 : n;
             p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
         }
+    } else if (most_rows <= 16) {
+        // Parts of equal length over the whole batch: about two rounds of the CTAs that fit, of 64 keys at least (a tile for each warp)
+        // and a multiple of that, and 256 parts to a sequence at most (the join reads them all).
+        p.form = kFormToken;
+        p.rows = static_cast<int32_t>(most_rows);
+        int64_t keys = 0, scores = 0;
+        for (int b = 0; b < batch; ++b) {
+            if (seqs[b].n_q == 0) continue;
+            keys += visible_keys(seqs[b], counted, window, n_sink);
+            scores += static_cast<int64_t>(seqs[b].n_q) * c.n_heads * seqs[b].n_kv;
+        }
+        const int64_t ctas = 2 * static_cast<int64_t>(c.sm_count) * (c.head_dim <= 128 ? 3 : 2);
+        int64_t part = (keys * c.kv_heads + ctas - 1) / ctas;
+        part = part < (longest + 255) / 256 ? (longest + 255) / 256 : part;
+        p.part_keys = (part + 63) / 64 * 64;
+        if (p.part_keys < 64) p.part_keys = 64;
+        for (int b = 0; b < batch; ++b) {
+            const int32_t n = parts_of(p, seqs[b], counted, window, n_sink);
+            p.blocks += n;
+            p.splits = n > p.splits ? n : p.splits;
+        }
+        p.logit_floats = mass ? scores : 0;
     } else {
         p.form = kFormTile;
         p.pack = pack_of(group);
@@ -114,12 +148,15 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
     Workspace w;
     const int64_t qh = p.total_q * c.n_heads;
     if (p.splits > 1) {
-        p.part_o = w.take(p.splits * qh * c.head_dim * static_cast<int64_t>(sizeof(float)));
-        p.part_ml = w.take(p.splits * qh * 2 * static_cast<int64_t>(sizeof(float)));
+        int64_t part_q = 0;
+        for (int b = 0; b < batch; ++b) part_q += static_cast<int64_t>(parts_of(p, seqs[b], counted, window, n_sink)) * seqs[b].n_q;
+        p.part_o = w.take(part_q * c.n_heads * c.head_dim * static_cast<int64_t>(sizeof(float)));
+        p.part_ml = w.take(part_q * c.n_heads * 2 * static_cast<int64_t>(sizeof(float)));
     }
     if (mass) {
         p.lse2 = w.take(qh * static_cast<int64_t>(sizeof(float)));
-        p.part_mass = w.take(p.mass_parts * p.total_kv * static_cast<int64_t>(sizeof(float)));
+        if (p.form == kFormToken) p.logits = w.take(p.logit_floats * static_cast<int64_t>(sizeof(float)));
+        else p.part_mass = w.take(p.mass_parts * p.total_kv * static_cast<int64_t>(sizeof(float)));
     }
     if (p.form == kFormTile && c.dtype == MVLA_DTYPE_FP8_E4M3) {
         p.wide_q = w.take(qh * c.head_dim * 2);

@@ -68,6 +68,9 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x)
     *reinterpret_cast<uint4*>(p) = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
 }
 
+// The lowest n of 32 bits (all of them from 32 on, none below 1).
+__device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
+
 // An entry of the list of key (or query) tiles that a CTA walks: which of the range, and what has to be done with it.
 constexpr int kNeed = 1, kMask = 4, kHidden = 16, kEntryShift = 5;      // kNeed, kMask: shifted by the tile of rows
 __device__ __forceinline__ int entry_of(int rel, int flags) { return rel << kEntryShift | flags; }
@@ -158,6 +161,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[2 * kMaxStages + 8];
     __shared__ uint16_t list[kMaxTiles];
+    __shared__ __align__(16) int key_at[NT][2][BN];
     __shared__ int range_lo[2], range_hi[2], n_list, dead;
     __shared__ uint32_t tmem_base;
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -334,30 +338,36 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             const int e = list[i];
             if (!(e >> tile & kNeed)) continue;
             const int buf = NT == 2 ? tile : seen & 1, turn = NT == 2 ? seen : seen >> 1;
+            uint32_t visible[BN / 32];                       // a bit for every key of the tile that the row sees
+            if (e >> tile & kMask) {
+                const int j0 = range.tile(v0 + (e >> kEntryShift)) * BN;
+                if (a.kv_pos) {                              // the positions for the four warps (two buffers: one barrier a tile is enough)
+                    int* const at = key_at[tile][seen & 1];
+                    if (r < BN) at[r] = key_pos(a, s, len, j0 + r);
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + tile) : "memory");
+#pragma unroll
+                    for (int w = 0; w < BN / 32; ++w) {
+                        uint32_t bits = 0;
+#pragma unroll 8
+                        for (int c = 0; c < 32; ++c) bits |= sees(p, at[32 * w + c], a.window, a.n_sink) ? 1u << c : 0u;
+                        visible[w] = bits;
+                    }
+                } else {
+                    const int past = min(p, len - 1) - j0 + 1, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
+#pragma unroll
+                    for (int w = 0; w < BN / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
+                }
+            }
             ok = guard.wait_all(s_full + 8 * buf, turn & 1);
             if (!ok) break;
             tc_fence_after();
             const uint32_t s_col = tmem + buf * Sh::kS + lanes;
-            if (e >> tile & kMask) {                         // (in place, in small pieces: the registers are for the scores)
-                const int j0 = range.tile(v0 + (e >> kEntryShift)) * BN;
-                const int last = min(p, len - 1) - j0, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
-#pragma unroll 1
-                for (int c0 = 0; c0 < BN; c0 += 16) {
-                    float y[16];
-                    uint32_t w[16];
-                    tmem_ld_cols<16>(s_col + c0, y);
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) {
-                        const int at = c0 + c;
-                        const bool seen_by = a.kv_pos ? sees(p, key_pos(a, s, len, j0 + at), a.window, a.n_sink) : at <= last && (at >= first || at < sink);
-                        w[c] = seen_by ? __float_as_uint(y[c]) : 0xFF800000u;      // -infinity
-                    }
-                    tmem_st_cols<16>(s_col + c0, w);
-                }
-                tmem_st_wait();
-            }
             float x[BN];
             tmem_ld_cols<BN>(s_col, x);
+            if (e >> tile & kMask) {
+#pragma unroll
+                for (int c = 0; c < BN; ++c) x[c] = visible[c / 32] >> (c & 31) & 1u ? x[c] : -CUDART_INF_F;
+            }
             float tops[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
             for (int c = 4; c < BN; ++c) tops[c & 3] = fmaxf(tops[c & 3], x[c]);
@@ -404,7 +414,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         // ---- the tile's rows
         if (ok && seen > 0) ok = guard.wait_all(o_full + 8 * (NT == 2 ? tile : 1), 0);
         tc_fence_after();
-        const int64_t part = static_cast<int64_t>(blockIdx.y) * a.total_q + s.qp0 + i_row;
+        const int64_t part = s.part0 + static_cast<int64_t>(blockIdx.y) * s.n_q + i_row;
         const float inv = l > 0.f ? 1.f / l : 0.f;
         for (int c = 0; c < a.head_dim && ok; c += 32) {
             float o[32];

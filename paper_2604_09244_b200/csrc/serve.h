@@ -27,6 +27,9 @@ struct AttSeq {
     int32_t n_q, n_kv;
     int32_t blk0;                // first of its blocks of query rows in the launch (a block: rows of one key head)
     int32_t qp0, kvp0;           // its first query / cached row among those of the batch, packed
+    int32_t parts;               // parts that its visible keys are cut into
+    int64_t part0;               // first of its queries among the parts' results: [parts][n_q] of them
+    int64_t logit0;              // first of its scores (single tokens with mass): [n_q][n_heads][n_kv]
     int32_t qm_row, km_row;      // where its queries and cached rows begin in the tensor maps (kernels by tiles)
     int32_t index;               // its place in the caller's batch (kv_len)
 };
@@ -38,13 +41,15 @@ struct AttArgs {
     int32_t n_heads, kv_heads, head_dim, window, n_sink;
     float scale_log2;            // scale of the dot products, in powers of two
     int32_t n_seq, n_blocks, total_q, total_kv;
-    int32_t splits;              // parts that the visible keys are cut into
+    int32_t splits;              // the most parts that the visible keys of a sequence are cut into
     // workspace
-    float* part_o;               // [splits][total_q][n_heads][head_dim] sums against the part's own maximum   (splits > 1)
-    float2* part_ml;             // [splits][total_q][n_heads] (maximum, sum of exponentials), powers of two
+    float* part_o;               // [parts' queries][n_heads][head_dim] sums against the part's own reference      (splits > 1)
+    float2* part_ml;             // [parts' queries][n_heads] (reference, sum of exponentials), powers of two
     float* lse2;                 // [total_q][n_heads] logarithm to base 2 of the sum of exponentials          (with mass)
     float* part_mass;            // [mass_parts][total_kv]                                                     (with mass)
     int32_t mass_parts;
+    int32_t skip_whole;          // sequences of one part have written their output themselves (single tokens)
+    float* logits;               // scores in powers of two, -infinity where a row is not seen                (single tokens with mass)
     int32_t pack;                // heads of a group side by side in a tile of rows (kernels by tiles)
     int* status;                 // word that receives MVLA_ERR_TIMEOUT when a bounded wait gives up
     AttSeq s[kMaxBatch];
@@ -63,6 +68,11 @@ cudaError_t launch_attend_tile(bool f16, const AttArgs& a, const AttMaps& maps, 
 cudaError_t launch_attend_weights(bool f16, const AttArgs& a, const AttMaps& maps, cudaStream_t stream);
 // The sequences' e4m3 rows as packed fp16 rows.
 cudaError_t launch_widen(const AttArgs& a, void* wide_q, void* wide_k, void* wide_v, cudaStream_t stream);
+// bf16 / e4m3, at most 16 query rows (queries x heads of a group) to a sequence and key head; `rows`: the most there are.  A block: a
+// part of a sequence's keys.
+cudaError_t launch_attend_token(int dtype, const AttArgs& a, int rows, cudaStream_t stream);
+// mass += the weights that the kept scores stand for.
+cudaError_t launch_mass_of_scores(const AttArgs& a, cudaStream_t stream);
 // part_o / part_ml -> out, lse, lse2.
 cudaError_t launch_attend_join(int dtype, const AttArgs& a, cudaStream_t stream);
 // mass += part_mass over its parts.

@@ -113,21 +113,34 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     k.part_ml = reinterpret_cast<float2*>(at(plan.part_ml));
     k.lse2 = reinterpret_cast<float*>(at(plan.lse2));
     k.part_mass = reinterpret_cast<float*>(at(plan.part_mass));
+    k.logits = reinterpret_cast<float*>(at(plan.logits));
+    k.skip_whole = plan.form == kFormToken;
     const int group = v.n_heads / v.kv_heads;
+    const bool counted = all_counted(a);
     int32_t blk = 0, qp = 0, kvp = 0;
+    int64_t part = 0, logit = 0;
     for (int b = 0; b < batch; ++b) {
         const mvla_seq& s = seqs[b];
-        k.s[b] = AttSeq{s.q_row, s.kv_row, s.n_q, s.n_kv, blk, qp, kvp, 0, 0, b};
-        blk += static_cast<int32_t>(plan.form == kFormTile ? (static_cast<int64_t>(s.n_q) + plan.queries - 1) / plan.queries
+        const int32_t parts = parts_of(plan, s, counted, a->window, a->n_sink);
+        k.s[b] = AttSeq{s.q_row, s.kv_row, s.n_q, s.n_kv, blk, qp, kvp, parts, part, logit, 0, 0, b};
+        blk += plan.form == kFormToken ? parts
+             : static_cast<int32_t>(plan.form == kFormTile ? (static_cast<int64_t>(s.n_q) + plan.queries - 1) / plan.queries
                                                            : (static_cast<int64_t>(s.n_q) * group + plan.rows - 1) / plan.rows);
         qp += s.n_q;
         kvp += s.n_kv;
+        part += static_cast<int64_t>(parts) * s.n_q;
+        logit += static_cast<int64_t>(s.n_q) * v.n_heads * s.n_kv;
     }
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaSuccess;
     if (plan.form == kFormTile) {
         rc = attend_by_tiles(v, k, a, plan, &e, st);
         if (rc != MVLA_OK) return rc;
+    } else if (plan.form == kFormToken) {
+        e = launch_attend_token(v.dtype, k, plan.rows, st);
+        if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);
+        if (e == cudaSuccess && a->mass) e = launch_mass_of_scores(k, st);
+        return close_call(ctx, e);
     } else {
         e = launch_attend_fma(v.dtype, k, plan.rows, st);
         if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);

@@ -126,9 +126,11 @@ inline int32_t check_attention(const ServeShape& v, int32_t batch, const mvla_se
     return MVLA_OK;
 }
 
+// Whether every position is known to the host.
+inline bool all_counted(const mvla_attention* a) { return !a->q_pos && !a->kv_pos && !a->kv_len; }
 inline AttendPlan plan_of(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a)
 {
-    return plan_attend(v, batch, seqs, !a->q_pos && !a->kv_pos && !a->kv_len, a->window, a->n_sink, a->mass != nullptr);
+    return plan_attend(v, batch, seqs, all_counted(a), a->window, a->n_sink, a->mass != nullptr);
 }
 
 // Pointers of a call that has queries.
