@@ -123,9 +123,8 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
         p.form = kFormTile;
         p.pack = pack_of(group);
         const int per = 128 / p.pack;
-        const bool two = c.head_dim <= 128;                  // tiles of rows in a CTA, and the keys of a tile (attend_tile.cu)
-        const int64_t tile = two ? 128 : 64;
-        p.queries = two ? 2 * per : per;
+        const int64_t tile = 64;                             // keys (attend_tile.cu)
+        p.queries = per;
         int64_t most_q = 0;
         for (int b = 0; b < batch; ++b) {
             p.blocks += (static_cast<int64_t>(seqs[b].n_q) + p.queries - 1) / p.queries;
@@ -133,9 +132,9 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
         }
         const int64_t packs = c.n_heads / p.pack;
         if (p.blocks > 0) {
-            // one CTA to a multiprocessor; parts of at least four tiles; and no more tiles than a CTA's list holds
+            // one round of the CTAs that fit; parts of at least four tiles; and no more tiles than a CTA's list holds
             const int64_t ctas = p.blocks * packs, tiles = (longest + tile - 1) / tile;
-            int64_t n = c.sm_count / ctas;
+            int64_t n = (c.head_dim <= 128 ? 2 : 1) * static_cast<int64_t>(c.sm_count) / ctas;
             const int64_t most = tiles / 4, least = ((longest_kv + tile - 1) / tile + kMaxTiles - 1) / kMaxTiles;
             n = n > most ? most : n;
             n = n > 64 ? 64 : n;

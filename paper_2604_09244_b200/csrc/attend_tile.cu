@@ -1,15 +1,17 @@
 // Windowed attention of blocks of queries on the tensor cores (bf16; e4m3 widened to fp16), and the weights that it gives to the cached rows.
 //
-// attend_tile_kernel.  A CTA has NT tiles of 128 query rows that share a key head (row r of a tile: query r / g, head r % g of the g heads
-// packed side by side, one TMA box) and walks the tiles of BN keys that some of its rows may see:
+// attend_tile_kernel.  A CTA has a tile of 128 query rows that share a key head (row r: query r / g, head r % g of the g heads
+// packed side by side, one TMA box) and walks the tiles of 64 keys that some of its rows may see:
 //     S = Q K^T (tcgen05, both from shared memory)  ->  P = 2^(S - reference), rounded to 16 bits, back into the columns of S
 //     ->  O += P V (tcgen05, P from tensor memory, V as it lies in the cache: its rows are the contraction).
-// Warps 0-3 and 4-7: the softmax of one tile each, a thread per row: maximum and sum without a shuffle.  The sums in O are taken
-// against a reference that is moved only when a row's maximum grows past it by 2^8 (the result is the same; moving it is a pass over O).
-// Warp 8 loads, warp 9 issues the MMAs.  Two tiles keep the tensor cores and the exponentials busy in turn; heads above 128 elements
-// leave tensor memory for one tile, whose S is double-buffered instead.
-// Which key tiles, which of them some row of a tile sees, and which need their mask element by element, is settled before
-// the walk, from the positions; rows that nobody may look at have their values set to zero in shared memory (0 times NaN is NaN).
+// Warps 0-3: the softmax, a thread per row: maximum and sum without a shuffle.  The sums in O are taken against a reference that is
+// moved only when a row's maximum grows past it by 2^8 (the result is the same; moving it is a pass over O).  Warp 4 loads, warp 5
+// issues the MMAs; S is double-buffered, so that the next scores are there when the softmax of the last ones ends.
+// Heads of up to 128 elements leave room for two CTAs to a multiprocessor (256 columns of tensor memory, 97 KB of shared memory each):
+// one's exponentials, prologue and epilogue lie beside the other's MMAs.  Measured on 8192 queries, 16 heads of 128 in groups of 4, and on
+// 16 x 808 queries of 32 heads, window 512: two tiles of rows in one CTA with tiles of 128 keys 295 / 250 us, this 291 / 189.
+// Positions that are counted tell every warp which tiles to visit and which need their mask; where they are data, a list of the
+// tiles is made first.  Rows that nobody may look at have their values set to zero in shared memory (0 times NaN is NaN).
 #include "attend.cuh"
 #include "tmem_ld.cuh"
 #include "tmem_plan.h"
@@ -22,8 +24,9 @@
 namespace mvla {
 namespace {
 
-constexpr int kThreads = 320;
+constexpr int kThreads = 320;                // attend_weights_kernel
 constexpr int kRows = 128;                   // query rows of a tile
+constexpr int kKeys = 64;                    // keys of a tile
 constexpr int kMaxStages = 6;
 constexpr float kMoveAt = 8.f;               // a row's maximum may lie this far (powers of two) above its reference
 
@@ -71,10 +74,8 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x)
 // The lowest n of 32 bits (all of them from 32 on, none below 1).
 __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// An entry of the list of key (or query) tiles that a CTA walks: which of the range, and what has to be done with it.
-constexpr int kNeed = 1, kMask = 4, kHidden = 16, kEntryShift = 5;      // kNeed, kMask: shifted by the tile of rows
-__device__ __forceinline__ int entry_of(int rel, int flags) { return rel << kEntryShift | flags; }
-
+// What a tile of keys (or queries) is to a CTA: some row sees some key, not every row sees every key, some keys nobody may look at.
+constexpr int kNeed = 1, kMask = 2, kHidden = 4, kEntryShift = 3;       // an entry of a list: the tile's place in the range above the flags
 // Positions of `n` keys from row j0 on, by one warp: smallest and largest of those somebody may see, and whether there are others.
 struct Span {
     int lo, hi;
@@ -108,9 +109,9 @@ __device__ __forceinline__ int compact_entries(uint16_t* list, int n, int lane)
     int count = 0;
     for (int i0 = 0; i0 < n; i0 += 32) {
         const int f = i0 + lane < n ? list[i0 + lane] : 0;
-        const unsigned on = __ballot_sync(0xffffffffu, (f & 3) != 0);
+        const unsigned on = __ballot_sync(0xffffffffu, (f & kNeed) != 0);
         __syncwarp();
-        if (f & 3) list[count + __popc(on & ((1u << lane) - 1u))] = static_cast<uint16_t>(entry_of(i0 + lane, f));
+        if (f & kNeed) list[count + __popc(on & ((1u << lane) - 1u))] = static_cast<uint16_t>((i0 + lane) << kEntryShift | f);
         __syncwarp();
         count += __popc(on);
     }
@@ -139,254 +140,254 @@ struct Guard {
     }
 };
 
-template <int DB, int NT, int BN>
+// Smallest and largest position of queries [i0, i1) of a sequence, by one warp.
+__device__ __forceinline__ void query_span(const AttArgs& a, const AttSeq& s, int len, int i0, int i1, int lane, int* lo, int* hi)
+{
+    if (!a.q_pos) {
+        *lo = query_pos(a, s, len, i0);
+        *hi = query_pos(a, s, len, i1 - 1);
+        return;
+    }
+    int l = 0x7FFFFFFF, h = -1;
+    for (int i = i0 + lane; i < i1; i += 32) {
+        const int p = query_pos(a, s, len, i);
+        l = min(l, p);
+        h = max(h, p);
+    }
+    *lo = __reduce_min_sync(0xffffffffu, l);
+    *hi = __reduce_max_sync(0xffffffffu, h);
+}
+
+template <int DB>
 struct TileShape {
-    static constexpr int kQBytes = DB * kRows * 128;         // one tile of query rows
-    static constexpr int kStage = DB * BN * 128;             // one tile of keys or values
-    static constexpr int kRoom = (kSmemMaxPerCta - 8 * 1024 - NT * kQBytes) / kStage;
-    static constexpr int kStages = kRoom > kMaxStages ? kMaxStages : kRoom;
-    static constexpr int kSmem = 1024 + NT * kQBytes + kStages * kStage;
+    static constexpr int kWarps = 6, kLoads = 4, kIssues = 5;
     // columns of tensor memory: S (two buffers, P in the same columns), then O
-    static constexpr int kS = BN, kO = 2 * BN, kOStride = DB * 64;
-    static_assert(kStages >= 3 && 2 * BN + NT * DB * 64 <= kTmemColsPerSm, "shape");
+    static constexpr int kO = 2 * kKeys, kColumns = kO + DB * 64 <= 256 ? 256 : 512;
+    static constexpr int kCtas = kTmemColsPerSm / kColumns;  // to a multiprocessor
+    static constexpr int kQBytes = DB * kRows * 128;
+    static constexpr int kStage = DB * kKeys * 128;          // one tile of keys or values
+    static constexpr int kRoom = ((kCtas == 2 ? kSmemPerSm / 2 - kSmemReservedPerCta : kSmemMaxPerCta) - 8 * 1024 - kQBytes) / kStage;
+    static constexpr int kStages = kRoom > kMaxStages ? kMaxStages : kRoom;
+    static constexpr int kSmem = 1024 + kQBytes + kStages * kStage;
+    static_assert(kStages >= 4, "shape");
 };
 
-template <bool F16, int DB, int NT, int BN>
-__global__ void __launch_bounds__(kThreads, 1)
+template <bool F16, int DB>
+__global__ void __launch_bounds__(TileShape<DB>::kWarps * 32, TileShape<DB>::kCtas)
 attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v)
 {
-    using Sh = TileShape<DB, NT, BN>;
+    using Sh = TileShape<DB>;
     constexpr int ST = Sh::kStages;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[2 * kMaxStages + 8];
+    __shared__ uint64_t bars[2 * kMaxStages + 7];
     __shared__ uint16_t list[kMaxTiles];
-    __shared__ __align__(16) int key_at[NT][2][BN];
-    __shared__ int range_lo[2], range_hi[2], n_list, dead;
+    __shared__ int key_at[kKeys];
+    __shared__ int n_list, dead;
     __shared__ uint32_t tmem_base;
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    const uint32_t q_at = base, kv_at = base + NT * Sh::kQBytes;
+    const uint32_t q_at = base, kv_at = base + Sh::kQBytes;
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int i) { return bar0 + 8u * i; };
     const auto empty = [&](int i) { return bar0 + 8u * (kMaxStages + i); };
-    const uint32_t q_full = bar0 + 8u * (2 * kMaxStages), s_full = q_full + 8, p_full = q_full + 24, o_full = q_full + 40;      // two of each
+    // s_full, p_full: of each S buffer; o_step: a step's values are in O; o_full: all are
+    const uint32_t q_full = bar0 + 8u * (2 * kMaxStages), s_full = q_full + 8, p_full = q_full + 24, o_step = q_full + 40, o_full = q_full + 48;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
 
-    if (t == 0) {
+    if (warp == Sh::kLoads && lane == 0) {
         for (int i = 0; i < ST; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
         mbar_init(q_full, 1);
-        for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_full + 8 * i, 128); mbar_init(o_full + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_full + 8 * i, 128); }
+        mbar_init(o_step, 1);
+        mbar_init(o_full, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        for (int i = 0; i < 2; ++i) { range_lo[i] = 0x7FFFFFFF; range_hi[i] = -1; }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         dead = 0;
+        prefetch_tensormap(&map_q);
+        prefetch_tensormap(&map_k);
+        prefetch_tensormap(&map_v);
     }
-    if (warp == 9 && elect_one()) { prefetch_tensormap(&map_q); prefetch_tensormap(&map_k); prefetch_tensormap(&map_v); }
+    __syncwarp();
     pdl_wait();
     // (only now: what holds tensor memory ahead of this kernel in the stream is complete, and nothing that holds some waits for this CTA)
-    if (warp == 9) tmem_alloc(smem_u32(&tmem_base), kTmemColsPerSm);
+    if (warp == Sh::kIssues) tmem_alloc(smem_u32(&tmem_base), Sh::kColumns);
     // the block: the last ones, which see most keys, first
     const int heads = a.n_heads / a.pack, blk = a.n_blocks - 1 - static_cast<int>(blockIdx.x) / heads, head0 = static_cast<int>(blockIdx.x) % heads * a.pack;
     const AttSeq& s = a.s[seq_of_block(a, blk)];
-    const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack;      // queries of a tile
-    const int q0 = (blk - s.blk0) * NT * per, len = seq_len(a, s);
+    const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack;      // queries of the tile
+    const int q0 = (blk - s.blk0) * per, len = seq_len(a, s);
+    int lo, hi;
+    query_span(a, s, len, q0, min(q0 + per, s.n_q), lane, &lo, &hi);
+    const TileRange range = tile_range(a, len, lo, hi, kKeys);
+    const int per_split = (range.count + a.splits - 1) / a.splits, v0 = static_cast<int>(blockIdx.y) * per_split;
+    int n = max(0, min(range.count - v0, per_split));
+    if (a.kv_pos) {
+        for (int v = warp; v < n; v += Sh::kWarps) {
+            const Span k = key_span(a, s, len, range.tile(v0 + v) * kKeys, kKeys, lane);
+            if (lane == 0) list[v] = static_cast<uint16_t>(span_flags(a, lo, hi, k) | (k.hidden ? kHidden : 0));
+        }
+        __syncthreads();
+        if (warp == 0) {
+            const int c = compact_entries(list, n, lane);
+            if (lane == 0) n_list = c;
+        }
+        __syncthreads();
+        n = n_list;
+    }
+    // the i-th tile: where its keys begin, and what it is (counted positions: all tiles of the range are visited)
+    const auto first_key = [&](int i) { return range.tile(v0 + (a.kv_pos ? list[i] >> kEntryShift : i)) * kKeys; };
+    const auto flags_of = [&](int i, int j0) {
+        if (a.kv_pos) return static_cast<int>(list[i]);
+        const Span k = counted_span(len, j0, kKeys);
+        const int f = span_flags(a, lo, hi, k);              // (queries far apart may leave out a tile between them: then no row sees a key)
+        return (f ? f : kMask) | (k.hidden ? kHidden : 0);
+    };
+    Guard guard = {&dead, a.status};
+
+    // ---- loads (one lane of a warp): the first ones before the CTA meets
+    const auto load = [&](int c) {                           // tiles of keys and values in turn
+        const int st = c % ST, row = s.km_row + first_key(c / 2);
+        mbar_expect_tx(full(st), Sh::kStage);
+        for (int b = 0; b < DB; ++b) tma_load_3d(kv_at + st * Sh::kStage + b * kKeys * 128, c & 1 ? &map_v : &map_k, b * 64, hk, row, full(st));
+    };
+    const int at_once = min(ST, 2 * n);
+    if (warp == Sh::kLoads && lane == 0 && n > 0) {
+        mbar_expect_tx(q_full, DB * per * a.pack * 128);
+        for (int b = 0; b < DB; ++b) tma_load_3d(q_at + b * kRows * 128, &map_q, b * 64, head0, s.qm_row + q0, q_full);
+        for (int c = 0; c < at_once; ++c) load(c);
+    }
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     pdl_trigger();
-    // this thread's row (softmax warps)
-    const int tile = warp / 4, r = t & 127, i_row = q0 + tile * per + r / a.pack, head = head0 + r % a.pack;
-    const bool mine = warp < 4 * NT && r < per * a.pack && i_row < s.n_q;
-    const int p = mine ? query_pos(a, s, len, i_row) : -1;
-    if (warp < 4 * NT) {
-        const int lo = __reduce_min_sync(0xffffffffu, mine ? p : 0x7FFFFFFF), hi = __reduce_max_sync(0xffffffffu, p);
-        if (lane == 0) { atomicMin(&range_lo[tile], lo); atomicMax(&range_hi[tile], hi); }
-    }
-    __syncthreads();
-    const int lo0 = range_lo[0], hi0 = range_hi[0], lo1 = NT > 1 ? range_lo[1] : 0x7FFFFFFF, hi1 = NT > 1 ? range_hi[1] : -1;
-    const TileRange range = tile_range(a, len, min(lo0, lo1), max(hi0, hi1), BN);
-    const int per_split = (range.count + a.splits - 1) / a.splits, v0 = static_cast<int>(blockIdx.y) * per_split;
-    const int n_range = max(0, min(range.count - v0, per_split));
-    if (a.kv_pos) {
-        for (int v = warp; v < n_range; v += kThreads / 32) {
-            const Span k = key_span(a, s, len, range.tile(v0 + v) * BN, BN, lane);
-            const int f = span_flags(a, lo0, hi0, k) | (NT > 1 ? span_flags(a, lo1, hi1, k) << 1 : 0);
-            if (lane == 0) list[v] = static_cast<uint16_t>(f | (k.hidden ? kHidden : 0));
-        }
-    } else {
-        for (int v = t; v < n_range; v += kThreads) {
-            const Span k = counted_span(len, range.tile(v0 + v) * BN, BN);
-            list[v] = static_cast<uint16_t>(span_flags(a, lo0, hi0, k) | (NT > 1 ? span_flags(a, lo1, hi1, k) << 1 : 0) | (k.hidden ? kHidden : 0));
-        }
-    }
-    __syncthreads();
-    if (warp == 0) {
-        const int n = compact_entries(list, n_range, lane);
-        if (lane == 0) n_list = n;
-    }
-    __syncthreads();
-    const int n = n_list;
     const uint32_t tmem = tmem_base;
-    Guard guard = {&dead, a.status};
 
-    if (warp == 8) {
-        if (n > 0 && elect_one()) {
-            const int tiles = NT > 1 && q0 + per < s.n_q ? 2 : 1;
-            mbar_expect_tx(q_full, tiles * DB * per * a.pack * 128);
-            for (int i = 0; i < tiles; ++i)
-                for (int b = 0; b < DB; ++b) tma_load_3d(q_at + i * Sh::kQBytes + b * kRows * 128, &map_q, b * 64, head0, s.qm_row + q0 + i * per, q_full);
-            int c = 0;                                       // tiles of keys and values in turn
+    if (warp == Sh::kLoads) {
+        if (lane == 0 && n > 0) {
+            int c = at_once;
             for (; c < 2 * n; ++c) {
-                const int st = c % ST;
-                if (c >= ST && !guard.wait(empty(st), (c / ST - 1) & 1)) break;
-                const int row = s.km_row + range.tile(v0 + (list[c / 2] >> kEntryShift)) * BN;
-                mbar_expect_tx(full(st), Sh::kStage);
-                for (int b = 0; b < DB; ++b) tma_load_3d(kv_at + st * Sh::kStage + b * BN * 128, c & 1 ? &map_v : &map_k, b * 64, hk, row, full(st));
+                if (!guard.wait(empty(c % ST), (c / ST - 1) & 1)) break;
+                load(c);
             }
             if (c < 2 * n) {                                 // given up: what is under way has to land before the CTA may end
                 mbar_wait(q_full, 0);
                 for (int i = max(0, c - ST); i < c; ++i) mbar_wait(full(i % ST), i / ST & 1);
             }
         }
-    } else if (warp == 9 && n > 0) {
-        const uint32_t idesc_s = idesc_16<F16>(BN), idesc_o = idesc_16<F16>(a.head_dim) | kRowsAreContraction;
+    } else if (warp == Sh::kIssues && n > 0) {
+        const uint32_t idesc_s = idesc_16<F16>(kKeys), idesc_o = idesc_16<F16>(a.head_dim) | kRowsAreContraction;
         const int steps = a.head_dim / 16;                   // of the contraction over the head
-        const auto scores = [&](int i, int tl, int buf) {    // S of list entry i
+        const bool one = elect_one();
+        const auto scores = [&](int i) {                     // S of tile i; its keys' stage is free when it is there
             const int st = 2 * i % ST;
             for (int b = 0; b < DB; ++b)
-                umma_box(2, tmem + buf * Sh::kS, smem_desc_sw128(q_at + tl * Sh::kQBytes + b * kRows * 128), smem_desc_sw128(kv_at + st * Sh::kStage + b * BN * 128),
-                         idesc_s, min(4, steps - 4 * b), b > 0);
-            umma_commit(s_full + 8 * buf);
+                umma_box(2, tmem + (i & 1) * kKeys, smem_desc_sw128(q_at + b * kRows * 128), smem_desc_sw128(kv_at + st * Sh::kStage + b * kKeys * 128), idesc_s,
+                         min(4, steps - 4 * b), b > 0);
+            umma_commit(s_full + 8 * (i & 1));
+            umma_commit(empty(st));
         };
-        const auto values = [&](int i, int tl, int buf, bool more) {
-            const int st = (2 * i + 1) % ST;
-            for (int k = 0; k < BN / 16; ++k)
-                umma_bf16_ts(tmem + Sh::kO + tl * Sh::kOStride, tmem + buf * Sh::kS + 8 * k, smem_desc_rows_sw128(kv_at + st * Sh::kStage + k * 2048, BN * 128), idesc_o, more || k > 0);
-        };
-        const bool one = elect_one();
-        int done[2] = {0, 0};                                // tiles whose P was taken, by tile of rows (NT = 2) or S buffer (NT = 1)
-        bool any[2] = {false, false};
         bool ok = guard.wait_all(q_full, 0) && guard.wait_all(full(0), 0);
         if (ok && one) {
             tc_fence_after();
-            for (int tl = 0; tl < NT; ++tl)
-                if (list[0] >> tl & kNeed) scores(0, tl, tl);
-            umma_commit(empty(0));
+            scores(0);
         }
         for (int i = 0; i < n && ok; ++i) {
-            const int e = list[i], next = i + 1 < n ? list[i + 1] : 0;
-            if (NT == 1 && i + 1 < n) {
+            if (i + 1 < n) {
                 ok = guard.wait_all(full((2 * i + 2) % ST), (2 * i + 2) / ST & 1);
-                if (!ok) break;
-                if (one) {
+                if (ok && one) {
                     tc_fence_after();
-                    scores(i + 1, 0, (i + 1) & 1);
-                    umma_commit(empty((2 * i + 2) % ST));
+                    scores(i + 1);
                 }
+                __syncwarp();
             }
-            const int st = (2 * i + 1) % ST;
-            ok = guard.wait_all(full(st), (2 * i + 1) / ST & 1);
+            const int c = 2 * i + 1, st = c % ST;
+            ok = ok && guard.wait_all(full(st), c / ST & 1);
             if (!ok) break;
-            if (e & kHidden) {                               // values that nobody may look at become zero
-                const int j0 = range.tile(v0 + (e >> kEntryShift)) * BN;
-                for (int k = lane; k < BN; k += 32) {
+            const int j0 = first_key(i);
+            if (flags_of(i, j0) & kHidden) {                 // values that nobody may look at become zero
+                for (int k = lane; k < kKeys; k += 32) {
                     if (key_pos(a, s, len, j0 + k) >= 0) continue;
                     for (int b = 0; b < DB; ++b)
-                        for (int c = 0; c < 8; ++c)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(kv_at + st * Sh::kStage + b * BN * 128 + k * 128 + c * 16), "r"(0) : "memory");
+                        for (int x = 0; x < 8; ++x)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(kv_at + st * Sh::kStage + b * kKeys * 128 + k * 128 + x * 16), "r"(0) : "memory");
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
             }
-            if (NT == 2 && i + 1 < n) {
-                ok = guard.wait_all(full((2 * i + 2) % ST), (2 * i + 2) / ST & 1);
-                if (!ok) break;
-            }
-            for (int tl = 0; tl < NT && ok; ++tl) {
-                const int buf = NT == 2 ? tl : i & 1;
-                if (e >> tl & kNeed) {
-                    ok = guard.wait_all(p_full + 8 * buf, done[buf]++ & 1);
-                    if (!ok) break;
-                    if (one) {
-                        tc_fence_after();
-                        values(i, tl, buf, any[tl]);
-                        if (NT == 1) umma_commit(o_full);    // (every step: the softmax warps look at it when they move the reference)
-                    }
-                    any[tl] = true;
-                }
-                if (NT == 2 && one && (next >> tl & kNeed)) scores(i + 1, tl, tl);
-            }
+            ok = guard.wait_all(p_full + 8 * (i & 1), i / 2 & 1);
             if (ok && one) {
+                tc_fence_after();
+                for (int k = 0; k < kKeys / 16; ++k)
+                    umma_bf16_ts(tmem + Sh::kO, tmem + (i & 1) * kKeys + 8 * k, smem_desc_rows_sw128(kv_at + st * Sh::kStage + k * 2048, kKeys * 128), idesc_o, i > 0 || k > 0);
+                umma_commit(o_step);
                 umma_commit(empty(st));
-                if (NT == 2 && i + 1 < n) umma_commit(empty((2 * i + 2) % ST));
             }
             __syncwarp();
         }
-        if (ok && one) {                                     // everything is in O (NT = 1: on the second barrier, the first one counts steps)
-            if (NT == 2) umma_commit(o_full);
-            umma_commit(o_full + 8);
-        }
+        if (ok && one) umma_commit(o_full);
         __syncwarp();
-    } else if (warp < 4 * NT) {
-        // ---- softmax of a tile of rows, a thread per row
-        const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;        // this warp's 32 lanes
-        const uint32_t o_col = tmem + Sh::kO + tile * Sh::kOStride + lanes;
+    } else if (warp < 4) {
+        // ---- softmax, a thread per row
+        const int i_row = q0 + t / a.pack, head = head0 + t % a.pack;
+        const bool mine = t < per * a.pack && i_row < s.n_q;
+        const int p = mine ? query_pos(a, s, len, i_row) : -1;
+        const uint32_t lanes = static_cast<uint32_t>(warp) << 21;            // this warp's 32 lanes
+        const uint32_t o_col = tmem + Sh::kO + lanes;
         const float scale = a.scale_log2;
         float m = -CUDART_INF_F, l = 0.f;                    // reference (scaled), sum
-        int seen = 0;                                        // tiles so far
         bool ok = true;
         for (int i = 0; i < n; ++i) {
-            const int e = list[i];
-            if (!(e >> tile & kNeed)) continue;
-            const int buf = NT == 2 ? tile : seen & 1, turn = NT == 2 ? seen : seen >> 1;
-            uint32_t visible[BN / 32];                       // a bit for every key of the tile that the row sees
-            if (e >> tile & kMask) {
-                const int j0 = range.tile(v0 + (e >> kEntryShift)) * BN;
-                if (a.kv_pos) {                              // the positions for the four warps (two buffers: one barrier a tile is enough)
-                    int* const at = key_at[tile][seen & 1];
-                    if (r < BN) at[r] = key_pos(a, s, len, j0 + r);
-                    asm volatile("bar.sync %0, 128;" ::"r"(1 + tile) : "memory");
+            const int buf = i & 1, j0 = first_key(i);
+            const bool masked = (flags_of(i, j0) & kMask) != 0;
+            uint32_t visible[kKeys / 32];                    // a bit for every key of the tile that the row sees
+            if (masked) {
+                if (a.kv_pos) {                              // the positions, for the four warps
+                    asm volatile("bar.sync 1, 128;" ::: "memory");       // (nobody reads the last ones any more)
+                    if (t < kKeys) key_at[t] = key_pos(a, s, len, j0 + t);
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
 #pragma unroll
-                    for (int w = 0; w < BN / 32; ++w) {
+                    for (int w = 0; w < kKeys / 32; ++w) {
                         uint32_t bits = 0;
 #pragma unroll 8
-                        for (int c = 0; c < 32; ++c) bits |= sees(p, at[32 * w + c], a.window, a.n_sink) ? 1u << c : 0u;
+                        for (int c = 0; c < 32; ++c) bits |= sees(p, key_at[32 * w + c], a.window, a.n_sink) ? 1u << c : 0u;
                         visible[w] = bits;
                     }
                 } else {
                     const int past = min(p, len - 1) - j0 + 1, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
 #pragma unroll
-                    for (int w = 0; w < BN / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
+                    for (int w = 0; w < kKeys / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
                 }
             }
-            ok = guard.wait_all(s_full + 8 * buf, turn & 1);
+            ok = guard.wait_all(s_full + 8 * buf, i / 2 & 1);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t s_col = tmem + buf * Sh::kS + lanes;
-            float x[BN];
-            tmem_ld_cols<BN>(s_col, x);
-            if (e >> tile & kMask) {
+            const uint32_t s_col = tmem + buf * kKeys + lanes;
+            float x[kKeys];
+            tmem_ld_cols<kKeys>(s_col, x);
+            if (masked) {
 #pragma unroll
-                for (int c = 0; c < BN; ++c) x[c] = visible[c / 32] >> (c & 31) & 1u ? x[c] : -CUDART_INF_F;
+                for (int c = 0; c < kKeys; ++c) x[c] = visible[c / 32] >> (c & 31) & 1u ? x[c] : -CUDART_INF_F;
             }
             float tops[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-            for (int c = 4; c < BN; ++c) tops[c & 3] = fmaxf(tops[c & 3], x[c]);
+            for (int c = 4; c < kKeys; ++c) tops[c & 3] = fmaxf(tops[c & 3], x[c]);
             const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;      // (scale is positive)
             const bool move = top > m + kMoveAt;
-            if (seen > 0 && __any_sync(0xffffffffu, move)) {
-                // (one tile of rows: the step before may still be adding; the one before that was complete before this S was)
-                if (NT == 1) ok = guard.wait_all(o_full, (seen - 1) & 1);
+            if (i > 0 && __any_sync(0xffffffffu, move)) {
+                // (the step before may still be adding; the one before that was complete before this S was)
+                ok = guard.wait_all(o_step, (i - 1) & 1);
                 if (!ok) break;
                 tc_fence_after();
                 const float f = move ? ex2_approx(m - top) : 1.f;
 #pragma unroll 1
-                for (int c = 0; c < a.head_dim; c += 16) {
-                    float o[16];
-                    uint32_t w[16];
-                    tmem_ld_cols<16>(o_col + c, o);
+                for (int c = 0; c < a.head_dim; c += 32) {
+                    float o[32];
+                    uint32_t w[32];
+                    tmem_ld_cols<32>(o_col + c, o);
 #pragma unroll
-                    for (int k = 0; k < 16; ++k) w[k] = __float_as_uint(o[k] * f);
-                    tmem_st_cols<16>(o_col + c, w);
+                    for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(o[k] * f);
+                    tmem_st_cols<32>(o_col + c, w);
                 }
                 l *= f;
             }
@@ -394,7 +395,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             const float ref = m == -CUDART_INF_F ? 0.f : m;
             float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c0 = 0; c0 < BN; c0 += 32) {
+            for (int c0 = 0; c0 < kKeys; c0 += 32) {
                 uint32_t w[16];
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
@@ -409,16 +410,15 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             tmem_st_wait();
             tc_fence_before();
             mbar_arrive(p_full + 8 * buf);
-            ++seen;
         }
-        // ---- the tile's rows
-        if (ok && seen > 0) ok = guard.wait_all(o_full + 8 * (NT == 2 ? tile : 1), 0);
+        // ---- the rows
+        if (ok && n > 0) ok = guard.wait_all(o_full, 0);
         tc_fence_after();
         const int64_t part = s.part0 + static_cast<int64_t>(blockIdx.y) * s.n_q + i_row;
         const float inv = l > 0.f ? 1.f / l : 0.f;
         for (int c = 0; c < a.head_dim && ok; c += 32) {
             float o[32];
-            if (seen > 0) tmem_ld_cols<32>(o_col + c, o);
+            if (n > 0) tmem_ld_cols<32>(o_col + c, o);
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? (a.splits > 1 ? o[k] : o[k] * inv) : 0.f;
             if (!mine) continue;
@@ -444,40 +444,38 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         tc_fence_before();
     }
     __syncthreads();
-    if (warp == 9) {
+    if (warp == Sh::kIssues) {
         tc_fence_after();
-        tmem_dealloc(tmem, kTmemColsPerSm);
+        tmem_dealloc(tmem, Sh::kColumns);
     }
 }
 
 // attend_weights_kernel: mass of 128 cached rows over the queries of their sequence, for the heads packed together.  Keys on the lanes
 // of tensor memory, queries on its columns: S^T = K Q^T, and a thread adds up 2^(S - lse) over the columns of its key, so that
-// no sum crosses threads.  Tiles of queries go to the two groups of four warps in turn; four buffers of S.
-constexpr int kQStages = 4;
+// no sum crosses threads.  Tiles of 128 query rows go to the two groups of four warps in turn, each with an S of its own; two CTAs to a
+// multiprocessor (heads of up to 128 elements).  Bound by the exponentials.
+constexpr int kWeightStages = 2;
 
 template <int DB>
 struct WeightShape {
     static constexpr int kTileBytes = DB * kRows * 128;
-    static constexpr int kRoom = (kSmemMaxPerCta - 16 * 1024 - kTileBytes) / kTileBytes;
-    static constexpr int kStages = kRoom > kQStages ? kQStages : kRoom;
-    // (at least what keeps a second CTA, which would find no tensor memory, off the multiprocessor)
-    static constexpr int kUsed = 1024 + (1 + kStages) * kTileBytes;
-    static constexpr int kSmem = kUsed > 120 * 1024 ? kUsed : 120 * 1024;
-    static_assert(kStages >= 2, "shape");
+    static constexpr int kColumns = 2 * kRows;
+    static constexpr int kSmem = 1024 + (1 + kWeightStages) * kTileBytes;
+    static constexpr int kCtas = 2 * (kSmem + 6 * 1024 + kSmemReservedPerCta) <= kSmemPerSm ? 2 : 1;
 };
 
 template <bool F16, int DB>
-__global__ void __launch_bounds__(kThreads, 1)
+__global__ void __launch_bounds__(kThreads, WeightShape<DB>::kCtas)
 attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                       const __grid_constant__ CUtensorMap)
 {
     using Sh = WeightShape<DB>;
-    constexpr int ST = Sh::kStages;
+    constexpr int ST = kWeightStages;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[2 * kQStages + 9];
+    __shared__ uint64_t bars[2 * ST + 5];
     __shared__ uint16_t list[kMaxTiles];
-    __shared__ __align__(16) float row_z[4][kRows];
-    __shared__ int row_p[4][kRows];
+    __shared__ __align__(16) float row_z[2][kRows];
+    __shared__ int row_p[2][kRows];
     __shared__ float half[kRows];
     __shared__ int n_list, dead;
     __shared__ uint32_t tmem_base;
@@ -485,72 +483,85 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
     const uint32_t k_at = base, q_at = base + Sh::kTileBytes;
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int i) { return bar0 + 8u * i; };
-    const auto empty = [&](int i) { return bar0 + 8u * (kQStages + i); };
-    const uint32_t s_full = bar0 + 8u * (2 * kQStages), s_empty = s_full + 32, k_full = s_full + 64;      // four of each S buffer's
+    const auto empty = [&](int i) { return bar0 + 8u * (ST + i); };
+    const uint32_t s_full = bar0 + 8u * (2 * ST), s_empty = s_full + 16, k_full = s_full + 32;      // two of each group's S
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
-    if (t == 0) {
+    if (warp == 8 && lane == 0) {
         for (int i = 0; i < ST; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
-        for (int i = 0; i < 4; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_empty + 8 * i, 128); }
+        for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_empty + 8 * i, 128); }
         mbar_init(k_full, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         dead = 0;
+        prefetch_tensormap(&map_q);
+        prefetch_tensormap(&map_k);
     }
-    if (warp == 9 && elect_one()) { prefetch_tensormap(&map_q); prefetch_tensormap(&map_k); }
+    __syncwarp();
     pdl_wait();
-    if (warp == 9) tmem_alloc(smem_u32(&tmem_base), kTmemColsPerSm);
+    if (warp == 9) tmem_alloc(smem_u32(&tmem_base), Sh::kColumns);
     const int packs = a.n_heads / a.pack, pk = static_cast<int>(blockIdx.x) % packs, head0 = pk * a.pack;
-    int b = 0, tile = static_cast<int>(blockIdx.x) / packs;
-    while (b + 1 < a.n_seq && tile >= (a.s[b].n_kv + kRows - 1) / kRows) tile -= (a.s[b++].n_kv + kRows - 1) / kRows;
-    const AttSeq& s = a.s[b];
-    const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack, len = seq_len(a, s), j0 = tile * kRows;
-    const int q_tiles = (s.n_q + per - 1) / per, v0 = static_cast<int>(blockIdx.y) * kMaxTiles, n_range = max(0, min(q_tiles - v0, kMaxTiles));
-    // the tiles of queries some of which see some of these keys
+    const int blk = static_cast<int>(blockIdx.x) / packs;
+    const AttSeq& s = a.s[seq_at(a, blk, [](const AttSeq& x) { return x.tile0; })];
+    const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack, len = seq_len(a, s), j0 = (blk - s.tile0) * kRows;
+    const int q_tiles = (s.n_q + per - 1) / per;
+    // the tiles of queries some of which see some of these keys: counted positions name them, else a list is made
     const Span k = a.kv_pos ? key_span(a, s, len, j0, kRows, lane) : counted_span(len, j0, kRows);
-    const auto tile_flags = [&](int v, int lo, int hi) {
-        const bool whole = (v + 1) * per <= s.n_q && per * a.pack == kRows;
+    const bool listed = a.kv_pos || a.q_pos;
+    int v0 = static_cast<int>(blockIdx.y) * kMaxTiles, n = max(0, min(q_tiles - v0, kMaxTiles));
+    const auto tile_flags = [&](int v) {
+        int lo, hi;
+        query_span(a, s, len, v * per, min((v + 1) * per, s.n_q), lane, &lo, &hi);
         const int f = span_flags(a, lo, hi, k);
-        return f && !whole ? f | kMask : f;
+        return f && ((v + 1) * per > s.n_q || per * a.pack < kRows) ? f | kMask : f;
     };
-    if (a.q_pos) {
-        for (int v = warp; v < n_range; v += kThreads / 32) {
-            int lo = 0x7FFFFFFF, hi = -1;
-            for (int i = (v0 + v) * per + lane; i < min((v0 + v + 1) * per, s.n_q); i += 32) {
-                const int p = query_pos(a, s, len, i);
-                lo = min(lo, p);
-                hi = max(hi, p);
-            }
-            lo = __reduce_min_sync(0xffffffffu, lo);
-            hi = __reduce_max_sync(0xffffffffu, hi);
-            if (lane == 0) list[v] = static_cast<uint16_t>(tile_flags(v0 + v, lo, hi));
+    if (listed) {
+        for (int v = warp; v < n; v += kThreads / 32) {
+            const int f = tile_flags(v0 + v);
+            if (lane == 0) list[v] = static_cast<uint16_t>(f);
         }
+        __syncthreads();
+        if (warp == 0) {
+            const int c = compact_entries(list, n, lane);
+            if (lane == 0) n_list = c;
+        }
+        __syncthreads();
+        n = n_list;
     } else {
-        for (int v = t; v < n_range; v += kThreads)
-            list[v] = static_cast<uint16_t>(tile_flags(v0 + v, query_pos(a, s, len, (v0 + v) * per), query_pos(a, s, len, min((v0 + v + 1) * per, s.n_q) - 1)));
+        // queries from the first key's position on, up to the last one whose window reaches the last key (any, where a sink is among them)
+        const int p0 = len - s.n_q, last = v0 + n;
+        const int from = max(k.lo - p0, 0) / per;
+        const int64_t reach = k.lo < a.n_sink ? s.n_q : min(static_cast<int64_t>(k.hi) - p0 + a.window, static_cast<int64_t>(s.n_q));
+        const int to = k.hi < 0 || reach <= 0 ? 0 : static_cast<int>((reach + per - 1) / per);
+        const int first = max(v0, min(from, last));
+        n = max(0, min(to, last) - first);
+        v0 = first;
     }
+    const auto tile_at = [&](int i) { return v0 + (listed ? list[i] >> kEntryShift : i); };
+    Guard guard = {&dead, a.status};
+    const auto load = [&](int c) {
+        const int st = c % ST, row = s.qm_row + tile_at(c) * per;
+        mbar_expect_tx(full(st), DB * per * a.pack * 128);
+        for (int i = 0; i < DB; ++i) tma_load_3d(q_at + st * Sh::kTileBytes + i * kRows * 128, &map_q, i * 64, head0, row, full(st));
+    };
+    const int at_once = min(ST, n);
+    if (warp == 8 && lane == 0 && n > 0) {
+        mbar_expect_tx(k_full, Sh::kTileBytes);
+        for (int i = 0; i < DB; ++i) tma_load_3d(k_at + i * kRows * 128, &map_k, i * 64, hk, s.km_row + j0, k_full);
+        for (int c = 0; c < at_once; ++c) load(c);
+    }
+    __syncwarp();
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
     pdl_trigger();
-    if (warp == 0) {
-        const int c = compact_entries(list, n_range, lane);
-        if (lane == 0) n_list = c;
-    }
-    __syncthreads();
-    const int n = n_list;
     const uint32_t tmem = tmem_base;
-    Guard guard = {&dead, a.status};
-    const int row_bytes = per * a.pack * 128;
 
     if (warp == 8) {
-        if (n > 0 && elect_one()) {
-            mbar_expect_tx(k_full, Sh::kTileBytes);
-            for (int i = 0; i < DB; ++i) tma_load_3d(k_at + i * kRows * 128, &map_k, i * 64, hk, s.km_row + j0, k_full);
-            int c = 0;
+        if (n > 0 && lane == 0) {
+            int c = at_once;
             for (; c < n; ++c) {
-                const int st = c % ST;
-                if (c >= ST && !guard.wait(empty(st), (c / ST - 1) & 1)) break;
-                mbar_expect_tx(full(st), DB * row_bytes);
-                for (int i = 0; i < DB; ++i) tma_load_3d(q_at + st * Sh::kTileBytes + i * kRows * 128, &map_q, i * 64, head0, s.qm_row + (v0 + (list[c] >> kEntryShift)) * per, full(st));
+                if (!guard.wait(empty(c % ST), (c / ST - 1) & 1)) break;
+                load(c);
             }
             if (c < n) {
                 mbar_wait(k_full, 0);
@@ -563,8 +574,8 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
         const bool one = elect_one();
         bool ok = n == 0 || guard.wait_all(k_full, 0);
         for (int i = 0; i < n && ok; ++i) {
-            const int st = i % ST, buf = i & 3;
-            ok = guard.wait_all(full(st), i / ST & 1) && (i < 4 || guard.wait_all(s_empty + 8 * buf, (i / 4 - 1) & 1));
+            const int st = i % ST, buf = i & 1;
+            ok = guard.wait_all(full(st), i / ST & 1) && (i < 2 || guard.wait_all(s_empty + 8 * buf, (i / 2 - 1) & 1));
             if (ok && one) {
                 tc_fence_after();
                 for (int c = 0; c < DB; ++c)
@@ -577,49 +588,74 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
         }
     } else {
         const int group = warp / 4, r = t & 127, j = j0 + r;
-        const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;
+        const uint32_t s_col = tmem + group * kRows + (static_cast<uint32_t>(warp & 3) << 21);
         const int c_pos = key_pos(a, s, len, j);
         const float scale = a.scale_log2;
         float sum = 0.f;
         bool ok = true;
-        for (int i = group; i < n && ok; i += 2) {
-            const int buf = i & 3, e = list[i];
-            {                                                // this thread's query row: for all keys of the group
-                const int iq = (v0 + (e >> kEntryShift)) * per + r / a.pack;
-                const bool there = r < per * a.pack && iq < s.n_q;
-                row_p[buf][r] = there ? query_pos(a, s, len, iq) : -1;
-                row_z[buf][r] = there ? a.lse2[static_cast<int64_t>(s.qp0 + iq) * a.n_heads + head0 + r % a.pack] : 0.f;
-            }
+        // this thread's query row of a tile, for all keys of the group: logarithm of its sum, position
+        float z = 0.f;
+        int p = -1;
+        const auto fetch = [&](int i) {
+            const int iq = i < n ? tile_at(i) * per + r / a.pack : s.n_q;
+            const bool there = r < per * a.pack && iq < s.n_q;
+            z = there ? a.lse2[static_cast<int64_t>(s.qp0 + iq) * a.n_heads + head0 + r % a.pack] : 0.f;
+            p = there ? query_pos(a, s, len, iq) : -1;
+        };
+        fetch(group);
+        for (int i = group; i < n; i += 2) {
+            asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");       // (nobody reads the last tile's any more)
+            row_z[group][r] = z;
+            row_p[group][r] = p;
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
-            ok = guard.wait_all(s_full + 8 * buf, i / 4 & 1);
+            fetch(i + 2);
+            const int v = tile_at(i);
+            uint32_t visible[kRows / 32];                    // a bit for every query row that sees this thread's key
+            const bool masked = listed ? (list[i] & kMask) != 0 : tile_flags(v) != kNeed;
+            if (masked) {
+                if (listed) {
+#pragma unroll
+                    for (int w = 0; w < kRows / 32; ++w) {
+                        uint32_t bits = 0;
+#pragma unroll 8
+                        for (int c = 0; c < 32; ++c) bits |= sees(row_p[group][32 * w + c], c_pos, a.window, a.n_sink) ? 1u << c : 0u;
+                        visible[w] = bits;
+                    }
+                } else {
+                    const int q0 = len - s.n_q + v * per, there = min(per, s.n_q - v * per);      // position of the tile's first query, and how many
+                    const int first = max(c_pos - q0, 0), past = c_pos < 0 ? 0 : c_pos < a.n_sink ? there : static_cast<int>(min(static_cast<int64_t>(c_pos) - q0 + a.window, static_cast<int64_t>(there)));
+#pragma unroll
+                    for (int w = 0; w < kRows / 32; ++w)
+                        visible[w] = below(max(past, 0) * a.pack - 32 * w) & ~below(min(first, per) * a.pack - 32 * w);
+                }
+            }
+            ok = guard.wait_all(s_full + 8 * group, i / 2 & 1);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t s_col = tmem + buf * kRows + lanes;
             float part[4] = {0.f, 0.f, 0.f, 0.f};
-            const bool masked = (e & kMask) != 0;
 #pragma unroll
             for (int c0 = 0; c0 < kRows; c0 += 32) {
                 float x[32];
                 tmem_ld_cols<32>(s_col + c0, x);
+                if (c0 + 32 == kRows) {                      // S is read: the next one may come
+                    tc_fence_before();
+                    mbar_arrive(s_empty + 8 * group);
+                }
+#pragma unroll
+                for (int c = 0; c < 32; c += 4) {
+                    const float4 y = *reinterpret_cast<const float4*>(&row_z[group][c0 + c]);
+                    x[c] = ex2_approx(fmaf(x[c], scale, -y.x));
+                    x[c + 1] = ex2_approx(fmaf(x[c + 1], scale, -y.y));
+                    x[c + 2] = ex2_approx(fmaf(x[c + 2], scale, -y.z));
+                    x[c + 3] = ex2_approx(fmaf(x[c + 3], scale, -y.w));
+                }
                 if (masked) {
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) {
-                        const float y = ex2_approx(fmaf(x[c], scale, -row_z[buf][c0 + c]));
-                        part[c & 3] += sees(row_p[buf][c0 + c], c_pos, a.window, a.n_sink) ? y : 0.f;
-                    }
-                } else {
-#pragma unroll
-                    for (int c = 0; c < 32; c += 4) {
-                        const float4 z = *reinterpret_cast<const float4*>(&row_z[buf][c0 + c]);
-                        part[0] += ex2_approx(fmaf(x[c], scale, -z.x));
-                        part[1] += ex2_approx(fmaf(x[c + 1], scale, -z.y));
-                        part[2] += ex2_approx(fmaf(x[c + 2], scale, -z.z));
-                        part[3] += ex2_approx(fmaf(x[c + 3], scale, -z.w));
-                    }
+                    for (int c = 0; c < 32; ++c) x[c] = visible[c0 / 32] >> c & 1u ? x[c] : 0.f;
                 }
+#pragma unroll
+                for (int c = 0; c < 32; ++c) part[c & 3] += x[c];
             }
-            tc_fence_before();
-            mbar_arrive(s_empty + 8 * buf);
             sum += (part[0] + part[1]) + (part[2] + part[3]);
         }
         if (group == 1) half[r] = sum;
@@ -631,18 +667,19 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
     __syncthreads();
     if (warp == 9) {
         tc_fence_after();
-        tmem_dealloc(tmem, kTmemColsPerSm);
+        tmem_dealloc(tmem, Sh::kColumns);
     }
 }
 
 template <class K>
-cudaError_t launch(KernelSetup& setup, K kernel, dim3 grid, size_t smem, const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
+cudaError_t launch(KernelSetup& setup, K kernel, dim3 grid, int threads, int columns, size_t smem, const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
-    const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(kernel), smem, kTmemColsPerSm);
+    smem = smem_for_tmem(smem, columns);                     // (no CTA more than there is tensor memory for)
+    const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(kernel), smem, columns);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(static_cast<unsigned>(threads));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1] = {pdl_attribute()};
@@ -651,23 +688,25 @@ cudaError_t launch(KernelSetup& setup, K kernel, dim3 grid, size_t smem, const A
     return cudaLaunchKernelEx(&cfg, kernel, a, maps.q, maps.k, maps.v);
 }
 
-template <bool F16, int DB, int NT, int BN>
+template <bool F16, int DB>
 cudaError_t attend(const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
     static KernelSetup setup;
     const dim3 grid(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack), static_cast<unsigned>(a.splits));
-    return launch(setup, attend_tile_kernel<F16, DB, NT, BN>, grid, TileShape<DB, NT, BN>::kSmem, a, maps, stream);
+    using Sh = TileShape<DB>;
+    return launch(setup, attend_tile_kernel<F16, DB>, grid, Sh::kWarps * 32, Sh::kColumns, Sh::kSmem, a, maps, stream);
 }
 
 template <bool F16, int DB>
 cudaError_t weights(const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
     static KernelSetup setup;
-    int64_t tiles = 0;
-    for (int b = 0; b < a.n_seq; ++b) tiles += (a.s[b].n_kv + kRows - 1) / kRows;
+    const AttSeq& last = a.s[a.n_seq - 1];
+    const int64_t tiles = last.tile0 + (last.n_kv + kRows - 1) / kRows;
     if (tiles == 0) return cudaSuccess;
     const int packs = a.n_heads / a.pack;
-    return launch(setup, attend_weights_kernel<F16, DB>, dim3(static_cast<unsigned>(tiles * packs), static_cast<unsigned>(a.mass_parts / packs)), WeightShape<DB>::kSmem, a, maps, stream);
+    return launch(setup, attend_weights_kernel<F16, DB>, dim3(static_cast<unsigned>(tiles * packs), static_cast<unsigned>(a.mass_parts / packs)), kThreads,
+                  WeightShape<DB>::kColumns, WeightShape<DB>::kSmem, a, maps, stream);
 }
 
 // e4m3 rows of the sequences as fp16 rows, packed (exact).  A thread converts 16 elements at a time.
@@ -731,10 +770,10 @@ template <bool F16>
 cudaError_t attend_by_dim(const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
     switch ((a.head_dim + 63) / 64) {
-    case 1: return attend<F16, 1, 2, 128>(a, maps, stream);
-    case 2: return attend<F16, 2, 2, 128>(a, maps, stream);
-    case 3: return attend<F16, 3, 1, 64>(a, maps, stream);
-    default: return attend<F16, 4, 1, 64>(a, maps, stream);
+    case 1: return attend<F16, 1>(a, maps, stream);
+    case 2: return attend<F16, 2>(a, maps, stream);
+    case 3: return attend<F16, 3>(a, maps, stream);
+    default: return attend<F16, 4>(a, maps, stream);
     }
 }
 }  // namespace

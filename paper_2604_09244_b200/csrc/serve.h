@@ -27,6 +27,7 @@ struct AttSeq {
     int32_t n_q, n_kv;
     int32_t blk0;                // first of its blocks of query rows in the launch (a block: rows of one key head)
     int32_t qp0, kvp0;           // its first query / cached row among those of the batch, packed
+    int32_t tile0;               // first of its tiles of 128 cached rows
     int32_t parts;               // parts that its visible keys are cut into
     int64_t part0;               // first of its queries among the parts' results: [parts][n_q] of them
     int64_t logit0;              // first of its scores (single tokens with mass): [n_q][n_heads][n_kv]

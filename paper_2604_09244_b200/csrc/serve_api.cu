@@ -71,15 +71,15 @@ int32_t attend_by_tiles(const CtxView& v, AttArgs& k, const mvla_attention* a, c
     }
     AttMaps maps;
     std::memset(&maps, 0, sizeof maps);
-    const int tile = v.head_dim <= 128 ? 128 : 64;
+    constexpr int kKeys = 64;              // of a tile (attend_tile.cu)
     if (!row_map(v, &maps.q, q, v.n_heads, q_rows, plan.pack, 128 / plan.pack)) return MVLA_ERR_CUDA;
     // (no cached rows: no key tile is ever asked for)
-    if (plan.total_kv > 0 && (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, tile) || !row_map(v, &maps.v, vv, v.kv_heads, kv_rows, 1, tile))) return MVLA_ERR_CUDA;
+    if (plan.total_kv > 0 && (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, kKeys) || !row_map(v, &maps.v, vv, v.kv_heads, kv_rows, 1, kKeys))) return MVLA_ERR_CUDA;
     *e = widen ? launch_widen(k, ws + plan.wide_q, ws + plan.wide_k, ws + plan.wide_v, st) : cudaSuccess;
     if (*e == cudaSuccess) *e = launch_attend_tile(widen, k, maps, st);
     if (*e == cudaSuccess && plan.splits > 1) *e = launch_attend_join(v.dtype, k, st);
     if (*e == cudaSuccess && a->mass && plan.total_kv > 0) {
-        if (tile != 128 && !row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, 128)) return MVLA_ERR_CUDA;
+        if (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, 128)) return MVLA_ERR_CUDA;
         *e = launch_attend_weights(widen, k, maps, st);
     }
     return MVLA_OK;
@@ -117,17 +117,18 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     k.skip_whole = plan.form == kFormToken;
     const int group = v.n_heads / v.kv_heads;
     const bool counted = all_counted(a);
-    int32_t blk = 0, qp = 0, kvp = 0;
+    int32_t blk = 0, qp = 0, kvp = 0, tile = 0;
     int64_t part = 0, logit = 0;
     for (int b = 0; b < batch; ++b) {
         const mvla_seq& s = seqs[b];
         const int32_t parts = parts_of(plan, s, counted, a->window, a->n_sink);
-        k.s[b] = AttSeq{s.q_row, s.kv_row, s.n_q, s.n_kv, blk, qp, kvp, parts, part, logit, 0, 0, b};
+        k.s[b] = AttSeq{s.q_row, s.kv_row, s.n_q, s.n_kv, blk, qp, kvp, tile, parts, part, logit, 0, 0, b};
         blk += plan.form == kFormToken ? parts
              : static_cast<int32_t>(plan.form == kFormTile ? (static_cast<int64_t>(s.n_q) + plan.queries - 1) / plan.queries
                                                            : (static_cast<int64_t>(s.n_q) * group + plan.rows - 1) / plan.rows);
         qp += s.n_q;
         kvp += s.n_kv;
+        tile += static_cast<int32_t>((static_cast<int64_t>(s.n_kv) + 127) / 128);
         part += static_cast<int64_t>(parts) * s.n_q;
         logit += static_cast<int64_t>(s.n_q) * v.n_heads * s.n_kv;
     }
