@@ -33,7 +33,7 @@ struct Workspace {
     }
 };
 
-constexpr int kMaxTiles = 1024;          // tiles of 128 keys that a CTA of the tile kernels walks (its list of them: 10 bits an entry)
+constexpr int kMaxTiles = 2048;          // tiles of keys that a CTA of the tile kernels walks (its list of them: 11 bits an entry)
 
 // kFormFma: by FMAs.  kFormTile: by tiles of 128 query rows on the tensor cores (e4m3: after widening to fp16).
 // kFormToken: at most 16 query rows to a key head, straight from global memory.
@@ -123,7 +123,7 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
         p.form = kFormTile;
         p.pack = pack_of(group);
         const int per = 128 / p.pack;
-        const int64_t tile = 128;                            // keys (attend_tile.cu)
+        const int64_t tile = 64;                             // keys (attend_tile.cu)
         p.queries = per;
         int64_t most_q = 0;
         for (int b = 0; b < batch; ++b) {
@@ -132,10 +132,10 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
         }
         const int64_t packs = c.n_heads / p.pack;
         if (p.blocks > 0) {
-            // one round of the CTAs that fit; parts of at least two tiles; and no more tiles than a CTA's list holds
+            // one round of the CTAs that fit; parts of at least four tiles; and no more tiles than a CTA's list holds
             const int64_t ctas = p.blocks * packs, tiles = (longest + tile - 1) / tile;
             int64_t n = (c.head_dim <= 128 ? 2 : 1) * static_cast<int64_t>(c.sm_count) / ctas;
-            const int64_t most = tiles / 2, least = ((longest_kv + tile - 1) / tile + kMaxTiles - 1) / kMaxTiles;
+            const int64_t most = tiles / 4, least = ((longest_kv + tile - 1) / tile + kMaxTiles - 1) / kMaxTiles;
             n = n > most ? most : n;
             n = n > 64 ? 64 : n;
             n = n < least ? least : n;

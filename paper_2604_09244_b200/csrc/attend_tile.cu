@@ -1,13 +1,12 @@
 // Windowed attention of blocks of queries on the tensor cores (bf16; e4m3 widened to fp16), and the weights that it gives to the cached rows.
 //
 // attend_tile_kernel.  A CTA has a tile of 128 query rows that share a key head (row r: query r / g, head r % g of the g heads
-// packed side by side, one TMA box) and walks the tiles of 128 keys that some of its rows may see:
+// packed side by side, one TMA box) and walks the tiles of 64 keys that some of its rows may see:
 //     S = Q K^T (tcgen05, both from shared memory)  ->  P = 2^(S - reference), rounded to 16 bits, back into the columns of S
 //     ->  O += P V (tcgen05, P from tensor memory, V as it lies in the cache: its rows are the contraction).
 // Warps 0-3: the softmax, a thread per row: maximum and sum without a shuffle.  The sums in O are taken against a reference that is
 // moved only when a row's maximum grows past it by 2^8 (the result is the same; moving it is a pass over O).  Warp 4 loads, warp 5
-// issues the MMAs.  Weights are made and meet their values in two halves of 64 keys; the scores come for 128 keys at once, since an MMA of
-// 64 columns takes as long as one of 96.
+// issues the MMAs; S is double-buffered, so that the next scores are there when the softmax of the last ones ends.
 // Heads of up to 128 elements leave room for two CTAs to a multiprocessor (256 columns of tensor memory, 97 KB of shared memory each):
 // one's exponentials, prologue and epilogue lie beside the other's MMAs.  Measured on 8192 queries, 16 heads of 128 in groups of 4, and on
 // 16 x 808 queries of 32 heads, window 512: two tiles of rows in one CTA with tiles of 128 keys 295 / 250 us, this 291 / 189.
@@ -27,8 +26,8 @@ namespace {
 
 constexpr int kThreads = 320;                // attend_weights_kernel
 constexpr int kRows = 128;                   // query rows of a tile
-constexpr int kKeys = 128;                   // keys of a tile
-constexpr int kHalf = 64;                    // ... and of the steps in which its weights are made and meet their values
+constexpr int kKeys = 64;                    // keys of a tile
+constexpr int kMaxStages = 6;
 constexpr float kMoveAt = 8.f;               // a row's maximum may lie this far (powers of two) above its reference
 
 // D[tmem] (+)= A[tmem] * B[smem], bf16, fp32 accumulate; issued by one thread.
@@ -72,33 +71,11 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x)
     *reinterpret_cast<uint4*>(p) = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
 }
 
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ uint64_t two_f32(float lo, float hi)
-{
-    uint64_t v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
-    return v;
-}
-__device__ __forceinline__ void split_f32(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
-}
-
 // The lowest n of 32 bits (all of them from 32 on, none below 1).
 __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// What keys (or queries) are to a CTA: some row sees some key, not every row sees every key, some keys nobody may look at.  An entry of a
-// list: a tile's place in the range above the flags of its halves.
-constexpr int kNeed = 1, kMask = 2, kHidden = 4, kHalfShift = 3, kEntryShift = 6;
+// What a tile of keys (or queries) is to a CTA: some row sees some key, not every row sees every key, some keys nobody may look at.
+constexpr int kNeed = 1, kMask = 2, kHidden = 4, kEntryShift = 3;       // an entry of a list: the tile's place in the range above the flags
 // Positions of `n` keys from row j0 on, by one warp: smallest and largest of those somebody may see, and whether there are others.
 struct Span {
     int lo, hi;
@@ -132,9 +109,9 @@ __device__ __forceinline__ int compact_entries(uint16_t* list, int n, int lane)
     int count = 0;
     for (int i0 = 0; i0 < n; i0 += 32) {
         const int f = i0 + lane < n ? list[i0 + lane] : 0;
-        const unsigned on = __ballot_sync(0xffffffffu, (f & (kNeed | kNeed << kHalfShift)) != 0);
+        const unsigned on = __ballot_sync(0xffffffffu, (f & kNeed) != 0);
         __syncwarp();
-        if (on >> lane & 1u) list[count + __popc(on & ((1u << lane) - 1u))] = static_cast<uint16_t>((i0 + lane) << kEntryShift | f);
+        if (f & kNeed) list[count + __popc(on & ((1u << lane) - 1u))] = static_cast<uint16_t>((i0 + lane) << kEntryShift | f);
         __syncwarp();
         count += __popc(on);
     }
@@ -184,13 +161,15 @@ __device__ __forceinline__ void query_span(const AttArgs& a, const AttSeq& s, in
 template <int DB>
 struct TileShape {
     static constexpr int kWarps = 6, kLoads = 4, kIssues = 5;
-    // columns of tensor memory: S (P in the same columns), then O.  Heads that leave room for one CTA only have two buffers of S.
-    static constexpr int kBufs = DB <= 2 ? 1 : 2;
-    static constexpr int kO = kBufs * kKeys, kColumns = DB <= 2 ? 256 : 512;
+    // columns of tensor memory: S (two buffers, P in the same columns), then O
+    static constexpr int kO = 2 * kKeys, kColumns = kO + DB * 64 <= 256 ? 256 : 512;
     static constexpr int kCtas = kTmemColsPerSm / kColumns;  // to a multiprocessor
-    static constexpr int kBytes = DB * 128 * 128;            // 128 rows of queries, keys or values
-    static constexpr int kSmem = 1024 + 3 * kBytes;
-    static_assert(kO + DB * 64 <= kColumns, "shape");
+    static constexpr int kQBytes = DB * kRows * 128;
+    static constexpr int kStage = DB * kKeys * 128;          // one tile of keys or values
+    static constexpr int kRoom = ((kCtas == 2 ? kSmemPerSm / 2 - kSmemReservedPerCta : kSmemMaxPerCta) - 8 * 1024 - kQBytes) / kStage;
+    static constexpr int kStages = kRoom > kMaxStages ? kMaxStages : kRoom;
+    static constexpr int kSmem = 1024 + kQBytes + kStages * kStage;
+    static_assert(kStages >= 4, "shape");
 };
 
 template <bool F16, int DB>
@@ -199,23 +178,28 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                    const __grid_constant__ CUtensorMap map_v)
 {
     using Sh = TileShape<DB>;
-    constexpr int kBufs = Sh::kBufs;
+    constexpr int ST = Sh::kStages;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[18];
+    __shared__ uint64_t bars[2 * kMaxStages + 7];
     __shared__ uint16_t list[kMaxTiles];
-    __shared__ int key_at[kHalf];
+    __shared__ int key_at[kKeys];
     __shared__ int n_list, dead;
     __shared__ uint32_t tmem_base;
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
-    const uint32_t q_at = base, k_at = base + Sh::kBytes, v_at = base + 2 * Sh::kBytes;      // v_at: the halves one after another
+    const uint32_t q_at = base, kv_at = base + Sh::kQBytes;
     const uint32_t bar0 = smem_u32(bars);
-    // s_full: of each S buffer; p_full: of each of its halves; v_full, v_empty: of each half; o_step: the values of every fourth half are in O; o_full: all are
-    const uint32_t q_full = bar0, k_full = bar0 + 8, k_empty = bar0 + 16, v_full = bar0 + 24, v_empty = bar0 + 40, s_full = bar0 + 56, p_full = bar0 + 72,
-                   o_step = bar0 + 104, o_full = bar0 + 136;
+    const auto full = [&](int i) { return bar0 + 8u * i; };
+    const auto empty = [&](int i) { return bar0 + 8u * (kMaxStages + i); };
+    // s_full, p_full: of each S buffer; o_step: a step's values are in O; o_full: all are
+    const uint32_t q_full = bar0 + 8u * (2 * kMaxStages), s_full = q_full + 8, p_full = q_full + 24, o_step = q_full + 40, o_full = q_full + 48;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
 
     if (warp == Sh::kLoads && lane == 0) {
-        for (int i = 0; i < 18; ++i) mbar_init(bar0 + 8 * i, i >= 9 && i <= 12 ? 128 : 1);      // (p_full: the softmax's threads)
+        for (int i = 0; i < ST; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
+        mbar_init(q_full, 1);
+        for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_full + 8 * i, 128); }
+        mbar_init(o_step, 1);
+        mbar_init(o_full, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         dead = 0;
@@ -237,15 +221,10 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     const TileRange range = tile_range(a, len, lo, hi, kKeys);
     const int per_split = (range.count + a.splits - 1) / a.splits, v0 = static_cast<int>(blockIdx.y) * per_split;
     int n = max(0, min(range.count - v0, per_split));
-    // flags of the halves of a tile, side by side
-    const auto both = [&](const Span& x, const Span& y) {
-        return span_flags(a, lo, hi, x) | (x.hidden ? kHidden : 0) | (span_flags(a, lo, hi, y) | (y.hidden ? kHidden : 0)) << kHalfShift;
-    };
     if (a.kv_pos) {
         for (int v = warp; v < n; v += Sh::kWarps) {
-            const int j0 = range.tile(v0 + v) * kKeys;
-            const Span x = key_span(a, s, len, j0, kHalf, lane), y = key_span(a, s, len, j0 + kHalf, kHalf, lane);
-            if (lane == 0) list[v] = static_cast<uint16_t>(both(x, y));
+            const Span k = key_span(a, s, len, range.tile(v0 + v) * kKeys, kKeys, lane);
+            if (lane == 0) list[v] = static_cast<uint16_t>(span_flags(a, lo, hi, k) | (k.hidden ? kHidden : 0));
         }
         __syncthreads();
         if (warp == 0) {
@@ -255,29 +234,27 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         __syncthreads();
         n = n_list;
     }
-    // the i-th tile: where its keys begin, and what it is.  (Counted positions: all tiles of the range are visited.  Queries far apart may
-    // leave out one between them: then there is nothing to add.)
+    // the i-th tile: where its keys begin, and what it is (counted positions: all tiles of the range are visited)
     const auto first_key = [&](int i) { return range.tile(v0 + (a.kv_pos ? list[i] >> kEntryShift : i)) * kKeys; };
-    const auto flags_of = [&](int i, int j0) { return a.kv_pos ? static_cast<int>(list[i]) : both(counted_span(len, j0, kHalf), counted_span(len, j0 + kHalf, kHalf)); };
+    const auto flags_of = [&](int i, int j0) {
+        if (a.kv_pos) return static_cast<int>(list[i]);
+        const Span k = counted_span(len, j0, kKeys);
+        const int f = span_flags(a, lo, hi, k);              // (queries far apart may leave out a tile between them: then no row sees a key)
+        return (f ? f : kMask) | (k.hidden ? kHidden : 0);
+    };
     Guard guard = {&dead, a.status};
 
-    const auto load_keys = [&](int j0) {
-        mbar_expect_tx(k_full, Sh::kBytes);
-        for (int b = 0; b < DB; ++b) tma_load_3d(k_at + b * kKeys * 128, &map_k, b * 64, hk, s.km_row + j0, k_full);
+    // ---- loads (one lane of a warp): the first ones before the CTA meets
+    const auto load = [&](int c) {                           // tiles of keys and values in turn
+        const int st = c % ST, row = s.km_row + first_key(c / 2);
+        mbar_expect_tx(full(st), Sh::kStage);
+        for (int b = 0; b < DB; ++b) tma_load_3d(kv_at + st * Sh::kStage + b * kKeys * 128, c & 1 ? &map_v : &map_k, b * 64, hk, row, full(st));
     };
-    const auto load_values = [&](int h, int j0) {
-        mbar_expect_tx(v_full + 8 * h, Sh::kBytes / 2);
-        for (int b = 0; b < DB; ++b) tma_load_3d(v_at + h * (Sh::kBytes / 2) + b * kHalf * 128, &map_v, b * 64, hk, s.km_row + j0 + h * kHalf, v_full + 8 * h);
-    };
-    // loads, by one lane of a warp: the first ones before the CTA meets
-    int v_loads[2] = {0, 0};
+    const int at_once = min(ST, 2 * n);
     if (warp == Sh::kLoads && lane == 0 && n > 0) {
         mbar_expect_tx(q_full, DB * per * a.pack * 128);
         for (int b = 0; b < DB; ++b) tma_load_3d(q_at + b * kRows * 128, &map_q, b * 64, head0, s.qm_row + q0, q_full);
-        const int j0 = first_key(0), f = flags_of(0, j0);
-        load_keys(j0);
-        for (int h = 0; h < 2; ++h)
-            if (f >> (h * kHalfShift) & kNeed) { load_values(h, j0); ++v_loads[h]; }
+        for (int c = 0; c < at_once; ++c) load(c);
     }
     __syncwarp();
     tc_fence_before();
@@ -288,87 +265,65 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
 
     if (warp == Sh::kLoads) {
         if (lane == 0 && n > 0) {
-            int i = 1;
-            bool ok = true;
-            for (; i < n && ok; ++i) {
-                const int j0 = first_key(i), f = flags_of(i, j0);
-                ok = guard.wait(k_empty, (i - 1) & 1);
-                if (!ok) break;
-                load_keys(j0);
-                for (int h = 0; h < 2 && ok; ++h) {
-                    if (!(f >> (h * kHalfShift) & kNeed)) continue;
-                    ok = v_loads[h] == 0 || guard.wait(v_empty + 8 * h, (v_loads[h] - 1) & 1);
-                    if (ok) { load_values(h, j0); ++v_loads[h]; }
-                }
+            int c = at_once;
+            for (; c < 2 * n; ++c) {
+                if (!guard.wait(empty(c % ST), (c / ST - 1) & 1)) break;
+                load(c);
             }
-            if (!ok) {                                       // given up: what is under way has to land before the CTA may end
+            if (c < 2 * n) {                                 // given up: what is under way has to land before the CTA may end
                 mbar_wait(q_full, 0);
-                mbar_wait(k_full, (i - 1) & 1);
-                for (int h = 0; h < 2; ++h)
-                    if (v_loads[h]) mbar_wait(v_full + 8 * h, (v_loads[h] - 1) & 1);
+                for (int i = max(0, c - ST); i < c; ++i) mbar_wait(full(i % ST), i / ST & 1);
             }
         }
     } else if (warp == Sh::kIssues && n > 0) {
         const uint32_t idesc_s = idesc_16<F16>(kKeys), idesc_o = idesc_16<F16>(a.head_dim) | kRowsAreContraction;
         const int steps = a.head_dim / 16;                   // of the contraction over the head
         const bool one = elect_one();
-        const auto scores = [&](int i) {                     // S of tile i; its keys' place is free when it is there
+        const auto scores = [&](int i) {                     // S of tile i; its keys' stage is free when it is there
+            const int st = 2 * i % ST;
             for (int b = 0; b < DB; ++b)
-                umma_box(2, tmem + i % kBufs * kKeys, smem_desc_sw128(q_at + b * kRows * 128), smem_desc_sw128(k_at + b * kKeys * 128), idesc_s,
+                umma_box(2, tmem + (i & 1) * kKeys, smem_desc_sw128(q_at + b * kRows * 128), smem_desc_sw128(kv_at + st * Sh::kStage + b * kKeys * 128), idesc_s,
                          min(4, steps - 4 * b), b > 0);
-            umma_commit(s_full + 8 * (i % kBufs));
-            umma_commit(k_empty);
+            umma_commit(s_full + 8 * (i & 1));
+            umma_commit(empty(st));
         };
-        bool ok = guard.wait_all(q_full, 0) && guard.wait_all(k_full, 0);
+        bool ok = guard.wait_all(q_full, 0) && guard.wait_all(full(0), 0);
         if (ok && one) {
             tc_fence_after();
             scores(0);
         }
-        int taken[2] = {0, 0}, p_turn = 0;                   // halves so far; a bit for every p_full: the phase that comes
-        const auto next_scores = [&](int i) {
-            if (i >= n || !ok) return;
-            ok = guard.wait_all(k_full, i & 1);
-            if (ok && one) {
-                tc_fence_after();
-                scores(i);
-            }
-            __syncwarp();
-        };
         for (int i = 0; i < n && ok; ++i) {
-            if (kBufs == 2) next_scores(i + 1);
-            const int j0 = first_key(i), f = flags_of(i, j0);
-            for (int h = 0; h < 2 && ok; ++h) {
-                const int fh = f >> (h * kHalfShift);
-                if (!(fh & kNeed)) continue;
-                ok = guard.wait_all(v_full + 8 * h, taken[h] & 1);
-                if (!ok) break;
-                const uint32_t place = v_at + h * (Sh::kBytes / 2);
-                if (fh & kHidden) {                          // values that nobody may look at become zero
-                    for (int k = lane; k < kHalf; k += 32) {
-                        if (key_pos(a, s, len, j0 + h * kHalf + k) >= 0) continue;
-                        for (int b = 0; b < DB; ++b)
-                            for (int x = 0; x < 8; ++x)
-                                asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(place + b * kHalf * 128 + k * 128 + x * 16), "r"(0) : "memory");
-                    }
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                }
-                const int place_p = i % kBufs * 2 + h;
-                ok = guard.wait_all(p_full + 8 * place_p, p_turn >> place_p & 1);
-                if (!ok) break;
-                p_turn ^= 1 << place_p;
-                const int step = taken[0] + taken[1];
-                if (one) {
+            if (i + 1 < n) {
+                ok = guard.wait_all(full((2 * i + 2) % ST), (2 * i + 2) / ST & 1);
+                if (ok && one) {
                     tc_fence_after();
-                    for (int k = 0; k < kHalf / 16; ++k)
-                        umma_bf16_ts(tmem + Sh::kO, tmem + i % kBufs * kKeys + h * kHalf + 8 * k, smem_desc_rows_sw128(place + k * 2048, kHalf * 128), idesc_o, step > 0 || k > 0);
-                    umma_commit(o_step + 8 * (step & 3));
-                    umma_commit(v_empty + 8 * h);
+                    scores(i + 1);
                 }
                 __syncwarp();
-                ++taken[h];
             }
-            if (kBufs == 1) next_scores(i + 1);
+            const int c = 2 * i + 1, st = c % ST;
+            ok = ok && guard.wait_all(full(st), c / ST & 1);
+            if (!ok) break;
+            const int j0 = first_key(i);
+            if (flags_of(i, j0) & kHidden) {                 // values that nobody may look at become zero
+                for (int k = lane; k < kKeys; k += 32) {
+                    if (key_pos(a, s, len, j0 + k) >= 0) continue;
+                    for (int b = 0; b < DB; ++b)
+                        for (int x = 0; x < 8; ++x)
+                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(kv_at + st * Sh::kStage + b * kKeys * 128 + k * 128 + x * 16), "r"(0) : "memory");
+                }
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+            }
+            ok = guard.wait_all(p_full + 8 * (i & 1), i / 2 & 1);
+            if (ok && one) {
+                tc_fence_after();
+                for (int k = 0; k < kKeys / 16; ++k)
+                    umma_bf16_ts(tmem + Sh::kO, tmem + (i & 1) * kKeys + 8 * k, smem_desc_rows_sw128(kv_at + st * Sh::kStage + k * 2048, kKeys * 128), idesc_o, i > 0 || k > 0);
+                umma_commit(o_step);
+                umma_commit(empty(st));
+            }
+            __syncwarp();
         }
         if (ok && one) umma_commit(o_full);
         __syncwarp();
@@ -380,95 +335,81 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         const uint32_t lanes = static_cast<uint32_t>(warp) << 21;            // this warp's 32 lanes
         const uint32_t o_col = tmem + Sh::kO + lanes;
         const float scale = a.scale_log2;
-        const uint64_t scale2 = two_f32(scale, scale);
         float m = -CUDART_INF_F, l = 0.f;                    // reference (scaled), sum
-        int step = 0;                                        // halves so far
         bool ok = true;
-        for (int i = 0; i < n && ok; ++i) {
-            const int j0 = first_key(i), f = flags_of(i, j0);
-            ok = guard.wait_all(s_full + 8 * (i % kBufs), i / kBufs & 1);
+        for (int i = 0; i < n; ++i) {
+            const int buf = i & 1, j0 = first_key(i);
+            const bool masked = (flags_of(i, j0) & kMask) != 0;
+            uint32_t visible[kKeys / 32];                    // a bit for every key of the tile that the row sees
+            if (masked) {
+                if (a.kv_pos) {                              // the positions, for the four warps
+                    asm volatile("bar.sync 1, 128;" ::: "memory");       // (nobody reads the last ones any more)
+                    if (t < kKeys) key_at[t] = key_pos(a, s, len, j0 + t);
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+                    for (int w = 0; w < kKeys / 32; ++w) {
+                        uint32_t bits = 0;
+#pragma unroll 8
+                        for (int c = 0; c < 32; ++c) bits |= sees(p, key_at[32 * w + c], a.window, a.n_sink) ? 1u << c : 0u;
+                        visible[w] = bits;
+                    }
+                } else {
+                    const int past = min(p, len - 1) - j0 + 1, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
+#pragma unroll
+                    for (int w = 0; w < kKeys / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
+                }
+            }
+            ok = guard.wait_all(s_full + 8 * buf, i / 2 & 1);
             if (!ok) break;
             tc_fence_after();
-#pragma unroll 1
-            for (int h = 0; h < 2; ++h) {
-                const int fh = f >> (h * kHalfShift);
-                if (!(fh & kNeed)) continue;
-                const uint32_t s_col = tmem + i % kBufs * kKeys + h * kHalf + lanes;
-                float x[kHalf];
-                tmem_ld_cols<kHalf>(s_col, x);
-                if (fh & kMask) {
-                    const int jh = j0 + h * kHalf;
-                    uint32_t visible[kHalf / 32];            // a bit for every key that the row sees
-                    if (a.kv_pos) {                          // the positions, for the four warps
-                        asm volatile("bar.sync 1, 128;" ::: "memory");       // (nobody reads the last ones any more)
-                        if (t < kHalf) key_at[t] = key_pos(a, s, len, jh + t);
-                        asm volatile("bar.sync 1, 128;" ::: "memory");
+            const uint32_t s_col = tmem + buf * kKeys + lanes;
+            float x[kKeys];
+            tmem_ld_cols<kKeys>(s_col, x);
+            if (masked) {
 #pragma unroll
-                        for (int w = 0; w < kHalf / 32; ++w) {
-                            uint32_t bits = 0;
-#pragma unroll 8
-                            for (int c = 0; c < 32; ++c) bits |= sees(p, key_at[32 * w + c], a.window, a.n_sink) ? 1u << c : 0u;
-                            visible[w] = bits;
-                        }
-                    } else {
-                        const int past = min(p, len - 1) - jh + 1, first = max(p - a.window + 1, 0) - jh, sink = a.n_sink - jh;
-#pragma unroll
-                        for (int w = 0; w < kHalf / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
-                    }
-#pragma unroll
-                    for (int c = 0; c < kHalf; ++c) x[c] = visible[c / 32] >> (c & 31) & 1u ? x[c] : -CUDART_INF_F;
-                }
-                float tops[4] = {x[0], x[1], x[2], x[3]};
-#pragma unroll
-                for (int c = 4; c < kHalf; c += 8) {         // (three at a time)
-#pragma unroll
-                    for (int b = 0; b < 4; ++b) tops[b] = c + 4 + b < kHalf ? fmaxf(fmaxf(tops[b], x[c + b]), x[c + 4 + b]) : fmaxf(tops[b], x[c + b]);
-                }
-                const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;      // (scale is positive)
-                const bool move = top > m + kMoveAt;
-                if (step > 0 && __any_sync(0xffffffffu, move)) {
-                    // (what the last half adds has to be there.  Four barriers: the one before on this barrier was complete before this S was)
-                    ok = guard.wait_all(o_step + 8 * ((step - 1) & 3), (step - 1) / 4 & 1);
-                    if (!ok) break;
-                    tc_fence_after();
-                    const float g = move ? ex2_approx(m - top) : 1.f;
-#pragma unroll 1
-                    for (int c = 0; c < a.head_dim; c += 32) {
-                        float o[32];
-                        uint32_t w[32];
-                        tmem_ld_cols<32>(o_col + c, o);
-#pragma unroll
-                        for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(o[k] * g);
-                        tmem_st_cols<32>(o_col + c, w);
-                    }
-                    l *= g;
-                }
-                if (move) m = top;
-                const float ref = m == -CUDART_INF_F ? 0.f : m;
-                const uint64_t ref2 = two_f32(-ref, -ref);
-                uint64_t sums[2] = {0, 0};
-#pragma unroll
-                for (int c0 = 0; c0 < kHalf; c0 += 32) {
-                    uint32_t w[16];
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) {
-                        float y, z;
-                        split_f32(fma_f32x2(two_f32(x[c0 + c], x[c0 + c + 1]), scale2, ref2), y, z);
-                        y = ex2_approx(y);
-                        z = ex2_approx(z);
-                        sums[c / 2 & 1] = add_f32x2(sums[c / 2 & 1], two_f32(y, z));
-                        w[c / 2] = F16 ? two_f16(y, z) : two_bf16(y, z);
-                    }
-                    tmem_st_cols<16>(s_col + c0 / 2, w);
-                }
-                float even, odd;
-                split_f32(add_f32x2(sums[0], sums[1]), even, odd);
-                l += even + odd;
-                tmem_st_wait();
-                tc_fence_before();
-                mbar_arrive(p_full + 8 * (i % kBufs * 2 + h));
-                ++step;
+                for (int c = 0; c < kKeys; ++c) x[c] = visible[c / 32] >> (c & 31) & 1u ? x[c] : -CUDART_INF_F;
             }
+            float tops[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+            for (int c = 4; c < kKeys; ++c) tops[c & 3] = fmaxf(tops[c & 3], x[c]);
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;      // (scale is positive)
+            const bool move = top > m + kMoveAt;
+            if (i > 0 && __any_sync(0xffffffffu, move)) {
+                // (the step before may still be adding; the one before that was complete before this S was)
+                ok = guard.wait_all(o_step, (i - 1) & 1);
+                if (!ok) break;
+                tc_fence_after();
+                const float f = move ? ex2_approx(m - top) : 1.f;
+#pragma unroll 1
+                for (int c = 0; c < a.head_dim; c += 32) {
+                    float o[32];
+                    uint32_t w[32];
+                    tmem_ld_cols<32>(o_col + c, o);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(o[k] * f);
+                    tmem_st_cols<32>(o_col + c, w);
+                }
+                l *= f;
+            }
+            if (move) m = top;
+            const float ref = m == -CUDART_INF_F ? 0.f : m;
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int c0 = 0; c0 < kKeys; c0 += 32) {
+                uint32_t w[16];
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    const float y = ex2_approx(fmaf(x[c0 + c], scale, -ref)), z = ex2_approx(fmaf(x[c0 + c + 1], scale, -ref));
+                    sum[c & 2] += y;
+                    sum[(c & 2) + 1] += z;
+                    w[c / 2] = F16 ? two_f16(y, z) : two_bf16(y, z);
+                }
+                tmem_st_cols<16>(s_col + c0 / 2, w);
+            }
+            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(p_full + 8 * buf);
         }
         // ---- the rows
         if (ok && n > 0) ok = guard.wait_all(o_full, 0);
@@ -477,7 +418,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         const float inv = l > 0.f ? 1.f / l : 0.f;
         for (int c = 0; c < a.head_dim && ok; c += 32) {
             float o[32];
-            if (step > 0) tmem_ld_cols<32>(o_col + c, o);
+            if (n > 0) tmem_ld_cols<32>(o_col + c, o);
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? (a.splits > 1 ? o[k] : o[k] * inv) : 0.f;
             if (!mine) continue;
@@ -649,7 +590,7 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
         const int group = warp / 4, r = t & 127, j = j0 + r;
         const uint32_t s_col = tmem + group * kRows + (static_cast<uint32_t>(warp & 3) << 21);
         const int c_pos = key_pos(a, s, len, j);
-        const uint64_t scale2 = two_f32(a.scale_log2, a.scale_log2);
+        const float scale = a.scale_log2;
         float sum = 0.f;
         bool ok = true;
         // this thread's query row of a tile, for all keys of the group: logarithm of its sum, position
@@ -664,7 +605,7 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
         fetch(group);
         for (int i = group; i < n; i += 2) {
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");       // (nobody reads the last tile's any more)
-            row_z[group][r] = -z;
+            row_z[group][r] = z;
             row_p[group][r] = p;
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
             fetch(i + 2);
@@ -691,7 +632,7 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
             ok = guard.wait_all(s_full + 8 * group, i / 2 & 1);
             if (!ok) break;
             tc_fence_after();
-            uint64_t part[2] = {0, 0};
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int c0 = 0; c0 < kRows; c0 += 32) {
                 float x[32];
@@ -701,23 +642,21 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
                     mbar_arrive(s_empty + 8 * group);
                 }
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {            // (row_z: what the logarithms of the sums take off)
-                    const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(&row_z[group][c0 + c]);
-                    split_f32(fma_f32x2(two_f32(x[c], x[c + 1]), scale2, y.x), x[c], x[c + 1]);
-                    split_f32(fma_f32x2(two_f32(x[c + 2], x[c + 3]), scale2, y.y), x[c + 2], x[c + 3]);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) x[c + e] = ex2_approx(x[c + e]);
+                for (int c = 0; c < 32; c += 4) {
+                    const float4 y = *reinterpret_cast<const float4*>(&row_z[group][c0 + c]);
+                    x[c] = ex2_approx(fmaf(x[c], scale, -y.x));
+                    x[c + 1] = ex2_approx(fmaf(x[c + 1], scale, -y.y));
+                    x[c + 2] = ex2_approx(fmaf(x[c + 2], scale, -y.z));
+                    x[c + 3] = ex2_approx(fmaf(x[c + 3], scale, -y.w));
                 }
                 if (masked) {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) x[c] = visible[c0 / 32] >> c & 1u ? x[c] : 0.f;
                 }
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) part[c / 2 & 1] = add_f32x2(part[c / 2 & 1], two_f32(x[c], x[c + 1]));
+                for (int c = 0; c < 32; ++c) part[c & 3] += x[c];
             }
-            float even, odd;
-            split_f32(add_f32x2(part[0], part[1]), even, odd);
-            sum += even + odd;
+            sum += (part[0] + part[1]) + (part[2] + part[3]);
         }
         if (group == 1) half[r] = sum;
         asm volatile("bar.sync 3, 256;" ::: "memory");

@@ -71,14 +71,17 @@ int32_t attend_by_tiles(const CtxView& v, AttArgs& k, const mvla_attention* a, c
     }
     AttMaps maps;
     std::memset(&maps, 0, sizeof maps);
-    constexpr int kKeys = 128, kHalf = 64; // (attend_tile.cu)
+    constexpr int kKeys = 64;              // of a tile (attend_tile.cu)
     if (!row_map(v, &maps.q, q, v.n_heads, q_rows, plan.pack, 128 / plan.pack)) return MVLA_ERR_CUDA;
     // (no cached rows: no key tile is ever asked for)
-    if (plan.total_kv > 0 && (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, kKeys) || !row_map(v, &maps.v, vv, v.kv_heads, kv_rows, 1, kHalf))) return MVLA_ERR_CUDA;
+    if (plan.total_kv > 0 && (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, kKeys) || !row_map(v, &maps.v, vv, v.kv_heads, kv_rows, 1, kKeys))) return MVLA_ERR_CUDA;
     *e = widen ? launch_widen(k, ws + plan.wide_q, ws + plan.wide_k, ws + plan.wide_v, st) : cudaSuccess;
     if (*e == cudaSuccess) *e = launch_attend_tile(widen, k, maps, st);
     if (*e == cudaSuccess && plan.splits > 1) *e = launch_attend_join(v.dtype, k, st);
-    if (*e == cudaSuccess && a->mass && plan.total_kv > 0) *e = launch_attend_weights(widen, k, maps, st);
+    if (*e == cudaSuccess && a->mass && plan.total_kv > 0) {
+        if (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, 128)) return MVLA_ERR_CUDA;
+        *e = launch_attend_weights(widen, k, maps, st);
+    }
     return MVLA_OK;
 }
 
