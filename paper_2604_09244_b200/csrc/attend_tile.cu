@@ -71,6 +71,27 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x)
     *reinterpret_cast<uint4*>(p) = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
 }
 
+// Two fp32 operations in one instruction.
+__device__ __forceinline__ uint64_t two_f32(float lo, float hi)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+__device__ __forceinline__ void split_f32(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b)
+{
+    uint64_t d;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+
 // The lowest n of 32 bits (all of them from 32 on, none below 1).
 __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
 
@@ -335,6 +356,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         const uint32_t lanes = static_cast<uint32_t>(warp) << 21;            // this warp's 32 lanes
         const uint32_t o_col = tmem + Sh::kO + lanes;
         const float scale = a.scale_log2;
+        const uint64_t scale2 = two_f32(scale, scale);
         float m = -CUDART_INF_F, l = 0.f;                    // reference (scaled), sum
         bool ok = true;
         for (int i = 0; i < n; ++i) {
@@ -371,7 +393,10 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             }
             float tops[4] = {x[0], x[1], x[2], x[3]};
 #pragma unroll
-            for (int c = 4; c < kKeys; ++c) tops[c & 3] = fmaxf(tops[c & 3], x[c]);
+            for (int c = 4; c < kKeys; c += 8) {             // (three at a time)
+#pragma unroll
+                for (int b = 0; b < 4; ++b) tops[b] = c + 4 + b < kKeys ? fmaxf(fmaxf(tops[b], x[c + b]), x[c + 4 + b]) : fmaxf(tops[b], x[c + b]);
+            }
             const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;      // (scale is positive)
             const bool move = top > m + kMoveAt;
             if (i > 0 && __any_sync(0xffffffffu, move)) {
@@ -393,20 +418,25 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             }
             if (move) m = top;
             const float ref = m == -CUDART_INF_F ? 0.f : m;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
+            const uint64_t ref2 = two_f32(-ref, -ref);
+            uint64_t sums[2] = {0, 0};
 #pragma unroll
             for (int c0 = 0; c0 < kKeys; c0 += 32) {
                 uint32_t w[16];
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
-                    const float y = ex2_approx(fmaf(x[c0 + c], scale, -ref)), z = ex2_approx(fmaf(x[c0 + c + 1], scale, -ref));
-                    sum[c & 2] += y;
-                    sum[(c & 2) + 1] += z;
+                    float y, z;
+                    split_f32(fma_f32x2(two_f32(x[c0 + c], x[c0 + c + 1]), scale2, ref2), y, z);
+                    y = ex2_approx(y);
+                    z = ex2_approx(z);
+                    sums[c / 2 & 1] = add_f32x2(sums[c / 2 & 1], two_f32(y, z));
                     w[c / 2] = F16 ? two_f16(y, z) : two_bf16(y, z);
                 }
                 tmem_st_cols<16>(s_col + c0 / 2, w);
             }
-            l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+            float even, odd;
+            split_f32(add_f32x2(sums[0], sums[1]), even, odd);
+            l += even + odd;
             tmem_st_wait();
             tc_fence_before();
             mbar_arrive(p_full + 8 * buf);
@@ -590,7 +620,7 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
         const int group = warp / 4, r = t & 127, j = j0 + r;
         const uint32_t s_col = tmem + group * kRows + (static_cast<uint32_t>(warp & 3) << 21);
         const int c_pos = key_pos(a, s, len, j);
-        const float scale = a.scale_log2;
+        const uint64_t scale2 = two_f32(a.scale_log2, a.scale_log2);
         float sum = 0.f;
         bool ok = true;
         // this thread's query row of a tile, for all keys of the group: logarithm of its sum, position
@@ -605,7 +635,7 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
         fetch(group);
         for (int i = group; i < n; i += 2) {
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");       // (nobody reads the last tile's any more)
-            row_z[group][r] = z;
+            row_z[group][r] = -z;
             row_p[group][r] = p;
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
             fetch(i + 2);
@@ -632,7 +662,7 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
             ok = guard.wait_all(s_full + 8 * group, i / 2 & 1);
             if (!ok) break;
             tc_fence_after();
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
+            uint64_t part[2] = {0, 0};
 #pragma unroll
             for (int c0 = 0; c0 < kRows; c0 += 32) {
                 float x[32];
@@ -642,21 +672,23 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
                     mbar_arrive(s_empty + 8 * group);
                 }
 #pragma unroll
-                for (int c = 0; c < 32; c += 4) {
-                    const float4 y = *reinterpret_cast<const float4*>(&row_z[group][c0 + c]);
-                    x[c] = ex2_approx(fmaf(x[c], scale, -y.x));
-                    x[c + 1] = ex2_approx(fmaf(x[c + 1], scale, -y.y));
-                    x[c + 2] = ex2_approx(fmaf(x[c + 2], scale, -y.z));
-                    x[c + 3] = ex2_approx(fmaf(x[c + 3], scale, -y.w));
+                for (int c = 0; c < 32; c += 4) {            // (row_z: what the logarithms of the sums take off)
+                    const ulonglong2 y = *reinterpret_cast<const ulonglong2*>(&row_z[group][c0 + c]);
+                    split_f32(fma_f32x2(two_f32(x[c], x[c + 1]), scale2, y.x), x[c], x[c + 1]);
+                    split_f32(fma_f32x2(two_f32(x[c + 2], x[c + 3]), scale2, y.y), x[c + 2], x[c + 3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[c + e] = ex2_approx(x[c + e]);
                 }
                 if (masked) {
 #pragma unroll
                     for (int c = 0; c < 32; ++c) x[c] = visible[c0 / 32] >> c & 1u ? x[c] : 0.f;
                 }
 #pragma unroll
-                for (int c = 0; c < 32; ++c) part[c & 3] += x[c];
+                for (int c = 0; c < 32; c += 2) part[c / 2 & 1] = add_f32x2(part[c / 2 & 1], two_f32(x[c], x[c + 1]));
             }
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
+            float even, odd;
+            split_f32(add_f32x2(part[0], part[1]), even, odd);
+            sum += even + odd;
         }
         if (group == 1) half[r] = sum;
         asm volatile("bar.sync 3, 256;" ::: "memory");
