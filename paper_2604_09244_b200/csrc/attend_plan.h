@@ -98,7 +98,7 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
             p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
         }
     } else if (most_rows <= 16) {
-        // Parts of equal length over the whole batch: about two rounds of the CTAs that fit, of 64 keys at least (a tile for each warp)
+        // Parts of equal length over the whole batch: one round of the CTAs that fit, of 64 keys at least (a tile for each warp)
         // and a multiple of that, and 256 parts to a sequence at most (the join reads them all).
         p.form = kFormToken;
         p.rows = static_cast<int32_t>(most_rows);
@@ -108,7 +108,7 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
             keys += visible_keys(seqs[b], counted, window, n_sink);
             scores += static_cast<int64_t>(seqs[b].n_q) * c.n_heads * seqs[b].n_kv;
         }
-        const int64_t ctas = 2 * static_cast<int64_t>(c.sm_count) * (c.head_dim <= 128 ? 3 : 2);
+        const int64_t ctas = static_cast<int64_t>(c.sm_count) * (c.head_dim <= 128 ? 3 : 2);
         int64_t part = (keys * c.kv_heads + ctas - 1) / ctas;
         part = part < (longest + 255) / 256 ? (longest + 255) / 256 : part;
         p.part_keys = (part + 63) / 64 * 64;
@@ -146,14 +146,14 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
     }
     Workspace w;
     const int64_t qh = p.total_q * c.n_heads;
-    if (p.splits > 1) {
+    if (p.splits > 1 || (mass && p.form == kFormToken)) {
         int64_t part_q = 0;
         for (int b = 0; b < batch; ++b) part_q += static_cast<int64_t>(parts_of(p, seqs[b], counted, window, n_sink)) * seqs[b].n_q;
-        p.part_o = w.take(part_q * c.n_heads * c.head_dim * static_cast<int64_t>(sizeof(float)));
+        if (p.splits > 1) p.part_o = w.take(part_q * c.n_heads * c.head_dim * static_cast<int64_t>(sizeof(float)));
         p.part_ml = w.take(part_q * c.n_heads * 2 * static_cast<int64_t>(sizeof(float)));
     }
     if (mass) {
-        p.lse2 = w.take(qh * static_cast<int64_t>(sizeof(float)));
+        if (p.form != kFormToken) p.lse2 = w.take(qh * static_cast<int64_t>(sizeof(float)));
         if (p.form == kFormToken) p.logits = w.take(p.logit_floats * static_cast<int64_t>(sizeof(float)));
         else p.part_mass = w.take(p.mass_parts * p.total_kv * static_cast<int64_t>(sizeof(float)));
     }

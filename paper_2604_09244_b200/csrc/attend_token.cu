@@ -302,44 +302,10 @@ __global__ void __launch_bounds__(kWarps * 32, D32 <= 4 ? 3 : 2) attend_token_ke
             if (whole) {
                 const float z = l > 0.f ? m + log2f(l) : -CUDART_INF_F;
                 if (a.lse) a.lse[(s.q_row + i) * a.n_heads + head] = z * 0.69314718055994531f;      // ln 2
-                if (a.mass) a.lse2[static_cast<int64_t>(s.qp0 + i) * a.n_heads + head] = z;
-            } else {
-                a.part_ml[at] = make_float2(m, l);
             }
+            if (a.part_ml) a.part_ml[at] = make_float2(m, l);
         }
     }
-}
-
-// mass[j] += 1 / n_heads * the weights of row j, from the scores: a thread has a key and goes over queries and heads in their order.
-__global__ void __launch_bounds__(128) mass_of_scores_kernel(const __grid_constant__ AttArgs a)
-{
-    pdl_wait();
-    pdl_trigger();
-    const int64_t at = static_cast<int64_t>(blockIdx.x) * 128 + threadIdx.x;
-    if (at >= a.total_kv) return;
-    const AttSeq& s = a.s[seq_of_key(a, static_cast<int>(at))];
-    const int j = static_cast<int>(at) - s.kvp0, len = seq_len(a, s);
-    if (s.n_q == 0 || j >= len) return;
-    // (counted positions: keys outside the window were not looked at and have no score)
-    if (!a.kv_pos) {
-        int lo = 0x7FFFFFFF, hi = -1;
-        for (int i = 0; i < s.n_q; ++i) {
-            const int p = query_pos(a, s, len, i);
-            lo = min(lo, p);
-            hi = max(hi, p);
-        }
-        if (!some_sees(lo, hi, j, a.window, a.n_sink)) return;
-    }
-    const float* const x = a.logits + s.logit0 + j;
-    const float* const z = a.lse2 + static_cast<int64_t>(s.qp0) * a.n_heads;
-    const int rows = s.n_q * a.n_heads;
-    float sum = 0.f;
-#pragma unroll 8
-    for (int r = 0; r < rows; ++r) {
-        const float y = x[static_cast<int64_t>(r) * s.n_kv], b = z[r];
-        sum += y == -CUDART_INF_F ? 0.f : exp2f(y - b);
-    }
-    if (sum != 0.f) a.mass[s.kv_row + j] += sum / static_cast<float>(a.n_heads);
 }
 
 template <class T, int D32, bool BOTH>
@@ -378,19 +344,6 @@ cudaError_t by_dim(const AttArgs& a, int rows, cudaStream_t stream)
 cudaError_t launch_attend_token(int dtype, const AttArgs& a, int rows, cudaStream_t stream)
 {
     return dtype == MVLA_DTYPE_BF16 ? by_dim<__nv_bfloat16>(a, rows, stream) : by_dim<__nv_fp8_e4m3>(a, rows, stream);
-}
-
-cudaError_t launch_mass_of_scores(const AttArgs& a, cudaStream_t stream)
-{
-    if (a.total_kv == 0) return cudaSuccess;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>((static_cast<int64_t>(a.total_kv) + 127) / 128));
-    cfg.blockDim = dim3(128);
-    cfg.stream = stream;
-    cudaLaunchAttribute attr[1] = {pdl_attribute()};
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, mass_of_scores_kernel, a);
 }
 
 }  // namespace mvla

@@ -72,8 +72,8 @@ cudaError_t launch_widen(const AttArgs& a, void* wide_q, void* wide_k, void* wid
 // bf16 / e4m3, at most 16 query rows (queries x heads of a group) to a sequence and key head; `rows`: the most there are.  A block: a
 // part of a sequence's keys.
 cudaError_t launch_attend_token(int dtype, const AttArgs& a, int rows, cudaStream_t stream);
-// mass += the weights that the kept scores stand for.
-cudaError_t launch_mass_of_scores(const AttArgs& a, cudaStream_t stream);
+// Behind it: the parts joined, and mass += the weights that the kept scores stand for.
+cudaError_t launch_attend_finish(const AttArgs& a, cudaStream_t stream);
 // part_o / part_ml -> out, lse, lse2.
 cudaError_t launch_attend_join(int dtype, const AttArgs& a, cudaStream_t stream);
 // mass += part_mass over its parts.

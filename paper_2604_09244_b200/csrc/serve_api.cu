@@ -139,8 +139,7 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
         if (rc != MVLA_OK) return rc;
     } else if (plan.form == kFormToken) {
         e = launch_attend_token(v.dtype, k, plan.rows, st);
-        if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);
-        if (e == cudaSuccess && a->mass) e = launch_mass_of_scores(k, st);
+        if (e == cudaSuccess && (plan.splits > 1 || a->mass)) e = launch_attend_finish(k, st);
         return close_call(ctx, e);
     } else {
         e = launch_attend_fma(v.dtype, k, plan.rows, st);
