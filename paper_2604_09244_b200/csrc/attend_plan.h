@@ -8,6 +8,15 @@
 
 namespace mvla {
 
+// Shared memory of a CTA of the token form (attend_token.cu): four warps with three tiles of 16 keys and values each, in whole groups of 64
+// columns of the values; and the CTAs that fit on a multiprocessor (four at most: by registers).
+constexpr int token_smem(int pieces_of_32, int elem) { return 4 * 3 * (2 * pieces_of_32 + 4 * ((pieces_of_32 + 1) / 2)) * 32 * 8 * elem; }
+constexpr int token_ctas(int pieces_of_32, int elem)
+{
+    const int n = 220 * 1024 / (token_smem(pieces_of_32, elem) + 8 * 1024);
+    return n > 4 ? 4 : n < 1 ? 1 : n;
+}
+
 // What the plans and checks of a call go by in its context.
 struct ServeShape {
     int dtype, hidden_dtype;            // MVLA_DTYPE_* of q / k / v and of the rows beside them (bf16 where q / k / v are e4m3)
@@ -108,7 +117,7 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
             keys += visible_keys(seqs[b], counted, window, n_sink);
             scores += static_cast<int64_t>(seqs[b].n_q) * c.n_heads * seqs[b].n_kv;
         }
-        const int64_t ctas = static_cast<int64_t>(c.sm_count) * (c.head_dim <= 128 ? 3 : 2);
+        const int64_t ctas = static_cast<int64_t>(c.sm_count) * token_ctas(c.head_dim / 32, static_cast<int>(c.elem));
         int64_t part = (keys * c.kv_heads + ctas - 1) / ctas;
         part = part < (longest + 255) / 256 ? (longest + 255) / 256 : part;
         p.part_keys = (part + 63) / 64 * 64;

@@ -1,9 +1,10 @@
 // Windowed attention of single tokens over a cache: at most 16 query rows of a sequence share a key head (bf16, e4m3).
 //
-// Bound by the bytes of the keys and values.  A warp takes tiles of 16 keys straight from global memory into the registers that the
-// tensor cores read (m16n8k16, rows x keys x head), with no shared memory and no barrier between: which element of the head meets which
-// is free as long as queries and keys agree, so a lane's 16 bytes of a key row are two steps' operands as they come, and the
-// same holds for the columns of the values.  The scores' registers are the weights' registers of the second product.
+// Bound by the bytes of the keys and values.  A warp takes tiles of 16 keys as the registers that the tensor cores read (m16n8k16, rows x
+// keys x head): which element of the head meets which is free as long as queries and keys agree, so a lane's 16 bytes of a key row are two
+// steps' operands as they come, and the same holds for the columns of the values.  So every lane copies its own bytes, three tiles
+// ahead, into places of its own in shared memory (asynchronously), and no lane reads another's: no barrier between the warps, and none
+// between the lanes.  The scores' registers are the weights' registers of the second product.
 // The sums are taken against a reference per row that is moved when some score lies 2^8 above it: one vote a tile, and no shuffle
 // between rows and lanes but then and at the end.  Weights meet the values in two parts, what the 16-bit type holds and what it leaves
 // (the tensor cores have nothing else to do), so that rounding them costs nothing.
@@ -20,6 +21,17 @@ namespace mvla {
 namespace {
 
 constexpr int kWarps = 4;
+constexpr int kStages = 3;                   // tiles of a warp in shared memory
+
+// `BYTES` (8 or 16) from global memory to this lane's place, asynchronously; and waits for all groups of copies but the last N.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src)
+{
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi)
 {
@@ -69,13 +81,25 @@ template <> struct Kind<__nv_fp8_e4m3> {         // widened to fp16, which holds
     }
 };
 
+// Pieces of a lane in a tile: its chunks of two key rows and of four value rows.
+template <class T, int D32>
+struct TokenShape {
+    static constexpr int kM64 = (D32 + 1) / 2, kPieces = 2 * D32 + 4 * kM64, kPiece = 8 * sizeof(T);
+    static constexpr int kTile = kPieces * 32 * kPiece;      // of a warp
+    static constexpr int kSmem = kWarps * kStages * kTile, kCtas = token_ctas(D32, sizeof(T));
+    static_assert(kSmem == token_smem(D32, sizeof(T)), "the plan's size");
+};
+
 // D32: pieces of 32 elements in a head.  BOTH: more than eight query rows.
 template <class T, int D32, bool BOTH>
-__global__ void __launch_bounds__(kWarps * 32, D32 <= 4 ? 3 : 2) attend_token_kernel(const __grid_constant__ AttArgs a)
+__global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend_token_kernel(const __grid_constant__ AttArgs a)
 {
     using K = Kind<T>;
     constexpr int D = D32 * 32, M64 = (D32 + 1) / 2;         // M64: groups of 64 columns of the values
     constexpr int kHalves = BOTH ? 2 : 1;                    // rows g and g + 8 of a lane
+    using Sh = TokenShape<T, D32>;
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ int pos_ring[kWarps][kStages][32];
     __shared__ uint4 q_frag[D32][kHalves][32];
     __shared__ float merge_o[kWarps][D];
     __shared__ float merge_m[kWarps][16], merge_l[kWarps][16];
@@ -116,38 +140,58 @@ __global__ void __launch_bounds__(kWarps * 32, D32 <= 4 ? 3 : 2) attend_token_ke
 #pragma unroll
     for (int h = 0; h < kHalves; ++h) { ref[h] = -CUDART_INF_F; sum[h] = 0.f; }
 
-    // position of key (lane & 15) of a tile
-    const auto pos_of = [&](int it) { return it < t1 ? key_pos(a, s, len, range.tile(it) * 16 + (lane & 15)) : -1; };
-    int ahead = pos_of(t0 + warp);
-    for (int it = t0 + warp; it < t1; it += kWarps) {
-        const int pos = ahead, j0 = range.tile(it) * 16;
-        ahead = pos_of(it + kWarps);
+    // Tile t0 + warp + kWarps u is this warp's u-th, in stage u % kStages.  Position of its key (lane & 15):
+    const int mine = t1 > t0 + warp ? (t1 - t0 - warp + kWarps - 1) / kWarps : 0;
+    const auto first_key = [&](int u) { return range.tile(t0 + warp + kWarps * u) * 16; };
+    const auto pos_of = [&](int u) { return u < mine ? key_pos(a, s, len, first_key(u) + (lane & 15)) : -1; };
+    const uint32_t lane_at = smem_u32(ring) + warp * kStages * Sh::kTile + lane * Sh::kPiece;
+    // starts the copies of a tile that some row sees (always a group of copies, an empty one too)
+    const auto fetch = [&](int u, int pos) {
+        if (u < mine) {
+            pos_ring[warp][u % kStages][lane] = pos;
+            if (__any_sync(0xffffffffu, some_sees(lo, hi, pos, a.window, a.n_sink))) {
+                const int j0 = first_key(u);
+                uint32_t dst = lane_at + u % kStages * Sh::kTile;
+#pragma unroll
+                for (int n = 0; n < 2; ++n) {
+                    const T* const row = kb + static_cast<int64_t>(min(j0 + 8 * n + g, len - 1)) * stride;
+#pragma unroll
+                    for (int i = 0; i < D32; ++i, dst += 32 * Sh::kPiece) copy_async<Sh::kPiece>(dst, row + 32 * i);
+                }
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    const T* const row = vb + static_cast<int64_t>(min(j0 + 2 * c + (n & 1) + 8 * (n >> 1), len - 1)) * stride;
+#pragma unroll
+                    for (int m = 0; m < M64; ++m, dst += 32 * Sh::kPiece)
+                        if (m < D32 / 2 || g < 4) copy_async<Sh::kPiece>(dst, row + 64 * m);
+                }
+            }
+        }
+        copies_done();
+    };
+    int ahead[kStages - 1];
+#pragma unroll
+    for (int u = 0; u < kStages - 1; ++u) ahead[u] = pos_of(u);
+#pragma unroll
+    for (int u = 0; u < kStages - 1; ++u) fetch(u, ahead[u]);
+    int next = pos_of(kStages - 1);
+    for (int u = 0; u < mine; ++u) {
+        const int then = pos_of(u + kStages);
+        fetch(u + kStages - 1, next);                        // (into the stage that the last tile was read from)
+        next = then;
+        wait_copies<kStages - 1>();
+        const int pos = pos_ring[warp][u % kStages][lane], j0 = first_key(u);
         if (!__any_sync(0xffffffffu, some_sees(lo, hi, pos, a.window, a.n_sink))) {
             if (a.logits) {                                  // (rows that nobody sees: their weight is nothing)
-                const int r = lane >> 1;
-                for (int rr = r; rr < n_rows; rr += 16)
+                for (int rr = lane >> 1; rr < n_rows; rr += 16)
                     for (int j = j0 + 8 * (lane & 1); j < min(j0 + 8 * (lane & 1) + 8, len); ++j)
                         a.logits[s.logit0 + (static_cast<int64_t>(rr / group) * a.n_heads + hk * group + rr % group) * s.n_kv + j] = -CUDART_INF_F;
             }
             continue;
         }
         const bool all = __all_sync(0xffffffffu, pos >= 0 && pos <= lo && (hi - pos < a.window || pos < a.n_sink));
-        typename K::Raw kr[2][D32], vr[4][M64];
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-            const T* const row = kb + static_cast<int64_t>(min(j0 + 8 * n + g, len - 1)) * stride;
-#pragma unroll
-            for (int i = 0; i < D32; ++i) kr[n][i] = K::load(row + 32 * i);
-        }
-#pragma unroll
-        for (int n = 0; n < 4; ++n) {
-            const T* const row = vb + static_cast<int64_t>(min(j0 + 2 * c + (n & 1) + 8 * (n >> 1), len - 1)) * stride;
-#pragma unroll
-            for (int m = 0; m < M64; ++m) {
-                if (m < D32 / 2 || g < 4) vr[n][m] = K::load(row + 64 * m);
-                else vr[n][m] = typename K::Raw{};
-            }
-        }
+        const uint8_t* const tile = ring + (warp * kStages + u % kStages) * Sh::kTile + lane * Sh::kPiece;
+        const auto piece = [&](int i) { return *reinterpret_cast<const typename K::Raw*>(tile + i * 32 * Sh::kPiece); };
         float x[2][4] = {};
 #pragma unroll
         for (int i = 0; i < D32; ++i) {
@@ -156,7 +200,7 @@ __global__ void __launch_bounds__(kWarps * 32, D32 <= 4 ? 3 : 2) attend_token_ke
 #pragma unroll
             for (int n = 0; n < 2; ++n) {
                 uint32_t w[4];
-                K::words(kr[n][i], w);
+                K::words(piece(n * D32 + i), w);
                 K::mma(x[n], qa.x, qb.x, qa.y, qb.y, w[0], w[1]);
                 K::mma(x[n], qa.z, qb.z, qa.w, qb.w, w[2], w[3]);
             }
@@ -229,20 +273,20 @@ __global__ void __launch_bounds__(kWarps * 32, D32 <= 4 ? 3 : 2) attend_token_ke
                 w_lo[2 * n + h] = K::pack(y - v.x, z - v.y);
             }
         }
-        if (!all) {                                          // values that nobody may look at (0 times NaN is NaN)
+        bool hidden[4] = {};                                 // values that nobody may look at (0 times NaN is NaN)
+        if (!all) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                const bool hidden = __shfl_sync(0xffffffffu, pos, 2 * c + (n & 1) + 8 * (n >> 1)) < 0;
-#pragma unroll
-                for (int m = 0; m < M64; ++m)
-                    if (hidden) vr[n][m] = typename K::Raw{};
-            }
+            for (int n = 0; n < 4; ++n) hidden[n] = __shfl_sync(0xffffffffu, pos, 2 * c + (n & 1) + 8 * (n >> 1)) < 0;
         }
 #pragma unroll
         for (int m = 0; m < M64; ++m) {
             uint32_t w[4][4];
 #pragma unroll
-            for (int n = 0; n < 4; ++n) K::words(vr[n][m], w[n]);
+            for (int n = 0; n < 4; ++n) {
+                typename K::Raw v = {};
+                if (!hidden[n] && (m < D32 / 2 || g < 4)) v = piece(2 * D32 + n * M64 + m);
+                K::words(v, w[n]);
+            }
 #pragma unroll
             for (int i = 0; i < 8; ++i) {                    // column 8 g + i of the group, keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
                 const uint32_t sel = i & 1 ? 0x7632u : 0x5410u;
@@ -311,9 +355,13 @@ __global__ void __launch_bounds__(kWarps * 32, D32 <= 4 ? 3 : 2) attend_token_ke
 template <class T, int D32, bool BOTH>
 cudaError_t attend(const AttArgs& a, cudaStream_t stream)
 {
+    static KernelSetup setup;
+    const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(attend_token_kernel<T, D32, BOTH>), TokenShape<T, D32>::kSmem, 0);
+    if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(a.n_blocks), static_cast<unsigned>(a.kv_heads));
     cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = TokenShape<T, D32>::kSmem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1] = {pdl_attribute()};
     cfg.attrs = attr;
