@@ -107,27 +107,43 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
             p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
         }
     } else if (most_rows <= 16) {
-        // Parts of equal length over the whole batch: one round of the CTAs that fit, of 64 keys at least (a tile for each warp)
-        // and a multiple of that, and 256 parts to a sequence at most (the join reads them all).
+        // Parts of equal length over the whole batch, a multiple of 64 keys (a tile for each warp), so that their CTAs fill whole rounds of
+        // those that fit: of one to four rounds the ones that end first, by the keys of a round's longest part and 128 for its start
+        // and end.  256 parts to a sequence at most (the join reads them all).
         p.form = kFormToken;
         p.rows = static_cast<int32_t>(most_rows);
-        int64_t keys = 0, scores = 0;
+        int64_t keys = 0;
         for (int b = 0; b < batch; ++b) {
             if (seqs[b].n_q == 0) continue;
             keys += visible_keys(seqs[b], counted, window, n_sink);
-            scores += static_cast<int64_t>(seqs[b].n_q) * c.n_heads * seqs[b].n_kv;
+            p.logit_floats += mass ? static_cast<int64_t>(seqs[b].n_q) * c.n_heads * seqs[b].n_kv : 0;
         }
-        const int64_t ctas = static_cast<int64_t>(c.sm_count) * token_ctas(c.head_dim / 32, static_cast<int>(c.elem));
-        int64_t part = (keys * c.kv_heads + ctas - 1) / ctas;
-        part = part < (longest + 255) / 256 ? (longest + 255) / 256 : part;
-        p.part_keys = (part + 63) / 64 * 64;
-        if (p.part_keys < 64) p.part_keys = 64;
+        const int64_t fit = static_cast<int64_t>(c.sm_count) * token_ctas(c.head_dim / 32, static_cast<int>(c.elem));
+        const auto ctas_of = [&](int64_t part) {
+            int64_t n = 0;
+            p.part_keys = part;
+            for (int b = 0; b < batch; ++b) n += parts_of(p, seqs[b], counted, window, n_sink);
+            return n * c.kv_heads;
+        };
+        int64_t best = 0, best_cost = 0;
+        for (int rounds = 1; rounds <= 4; ++rounds) {
+            int64_t part = (keys * c.kv_heads + rounds * fit - 1) / (rounds * fit);
+            part = part < (longest + 255) / 256 ? (longest + 255) / 256 : part;
+            part = part < 64 ? 64 : (part + 63) / 64 * 64;
+            int64_t n = ctas_of(part);
+            for (int tries = 0; n > rounds * fit && tries < 8; ++tries) {
+                part += (part / 16 + 63) / 64 * 64;
+                n = ctas_of(part);
+            }
+            const int64_t cost = (n + fit - 1) / fit * ((part < longest ? part : longest) + 128);
+            if (!best || cost < best_cost) { best = part; best_cost = cost; }
+        }
+        p.part_keys = best;
         for (int b = 0; b < batch; ++b) {
             const int32_t n = parts_of(p, seqs[b], counted, window, n_sink);
             p.blocks += n;
             p.splits = n > p.splits ? n : p.splits;
         }
-        p.logit_floats = mass ? scores : 0;
     } else {
         p.form = kFormTile;
         p.pack = pack_of(group);
