@@ -1,13 +1,14 @@
 // Windowed attention of single tokens over a cache: at most 16 query rows of a sequence share a key head (bf16, e4m3).
 //
-// Bound by the bytes of the keys and values.  A warp takes tiles of 16 keys as the registers that the tensor cores read (m16n8k16, rows x
-// keys x head): which element of the head meets which is free as long as queries and keys agree, so a lane's 16 bytes of a key row are two
-// steps' operands as they come, and the same holds for the columns of the values.  So every lane copies its own bytes, three tiles
-// ahead, into places of its own in shared memory (asynchronously), and no lane reads another's: no barrier between the warps, and none
-// between the lanes.  The scores' registers are the weights' registers of the second product.
+// Bound by the bytes of the keys and values.  A warp takes tiles of 16 keys as the registers that the tensor cores read (m16n8k16): keys
+// are the 16 rows of the first product and columns of the values those of the second, query rows the 8 columns of both, so that a single
+// token wastes as little as can be.  Which element of the head meets which is free as long as queries and keys agree, so a lane's 16 bytes
+// of a key row are two steps' operands as they come, and the same holds for the columns of the values.  So every lane copies its own bytes,
+// three tiles ahead, into places of its own in shared memory (asynchronously), and no lane reads another's: no barrier between the
+// warps, and none between the lanes.  The scores become the second product's operand by transposing 8 x 8 blocks between the lanes.
 // The sums are taken against a reference per row that is moved when some score lies 2^8 above it: one vote a tile, and no shuffle
-// between rows and lanes but then and at the end.  Weights meet the values in two parts, what the 16-bit type holds and what it leaves
-// (the tensor cores have nothing else to do), so that rounding them costs nothing.
+// but then and at the end.  bf16 weights meet the values in two parts, what the type holds and what it leaves (the tensor cores have
+// nothing else to do), so that rounding them costs nothing; fp16 is fine enough.
 // A sequence's visible keys are cut into parts of about the same length over the whole batch; a CTA is four warps that take the part's
 // tiles in turn.  With accumulated weights the scores are kept (a fraction 2 / head_dim of the keys' and values' bytes and one more for
 // every query row) and become weights once all parts are joined.
@@ -46,6 +47,7 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 template <class T> struct Kind;
 template <> struct Kind<__nv_bfloat16> {
     using Raw = uint4;                           // eight elements as they lie in memory
+    static constexpr bool kTwoParts = true;
     static __device__ __forceinline__ Raw load(const __nv_bfloat16* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
     static __device__ __forceinline__ void words(const Raw& r, uint32_t (&w)[4]) { w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w; }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16(lo, hi); }
@@ -58,6 +60,7 @@ template <> struct Kind<__nv_bfloat16> {
 };
 template <> struct Kind<__nv_fp8_e4m3> {         // widened to fp16, which holds every e4m3 number
     using Raw = uint2;
+    static constexpr bool kTwoParts = false;
     static __device__ __forceinline__ Raw load(const __nv_fp8_e4m3* p) { return __ldg(reinterpret_cast<const uint2*>(p)); }
     static __device__ __forceinline__ uint32_t two(uint32_t x)
     {
@@ -90,38 +93,47 @@ struct TokenShape {
     static_assert(kSmem == token_smem(D32, sizeof(T)), "the plan's size");
 };
 
-// D32: pieces of 32 elements in a head.  BOTH: more than eight query rows.
-template <class T, int D32, bool BOTH>
+// The transpose of an 8 x 8 block of 16-bit values, a pair of neighbours in every lane.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+
+// D32: pieces of 32 elements in a head.  NR: groups of eight query rows.
+template <class T, int D32, int NR>
 __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend_token_kernel(const __grid_constant__ AttArgs a)
 {
     using K = Kind<T>;
-    constexpr int D = D32 * 32, M64 = (D32 + 1) / 2;         // M64: groups of 64 columns of the values
-    constexpr int kHalves = BOTH ? 2 : 1;                    // rows g and g + 8 of a lane
     using Sh = TokenShape<T, D32>;
+    constexpr int D = D32 * 32, M64 = Sh::kM64;              // M64: groups of 64 columns of the values
     extern __shared__ __align__(16) uint8_t ring[];
-    __shared__ int pos_ring[kWarps][kStages][32];
-    __shared__ uint4 q_frag[D32][kHalves][32];
+    __shared__ uint4 q_frag[D32][NR][32];
     __shared__ float merge_o[kWarps][D];
     __shared__ float merge_m[kWarps][16], merge_l[kWarps][16];
+    __shared__ int pos_ring[kWarps][kStages][32];
     pdl_wait();
     pdl_trigger();
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5, g = lane >> 2, c = lane & 3;
     const AttSeq& s = a.s[seq_of_block(a, blockIdx.x)];
     const int hk = blockIdx.y, group = a.n_heads / a.kv_heads, n_rows = s.n_q * group, len = seq_len(a, s);
     const T* const q = static_cast<const T*>(a.q);
-    for (int u = t; u < D32 * kHalves * 32; u += kWarps * 32) {
-        const int piece = u / (kHalves * 32), h = u / 32 % kHalves, l = u & 31, r = (l >> 2) + 8 * h;
+    for (int u = t; u < D32 * NR * 32; u += kWarps * 32) {
+        const int piece = u / (NR * 32), n = u / 32 % NR, l = u & 31, r = (l >> 2) + 8 * n;
         uint32_t w[4] = {0, 0, 0, 0};
         if (r < n_rows) K::words(K::load(q + ((s.q_row + r / group) * a.n_heads + hk * group + r % group) * D + 32 * piece + 8 * (l & 3)), w);
-        q_frag[piece][h][l] = make_uint4(w[0], w[1], w[2], w[3]);
+        q_frag[piece][n][l] = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    int p[kHalves], lo = 0x7FFFFFFF, hi = -1;                // this lane's rows, and the span of all rows
+    int p[NR][2], lo = 0x7FFFFFFF, hi = -1;                  // positions of this lane's rows 8 n + 2 c + e, and the span of all rows
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) {
-        const int r = g + 8 * h;
-        p[h] = r < n_rows ? query_pos(a, s, len, r / group) : -1;
-        if (r < n_rows) { lo = min(lo, p[h]); hi = max(hi, p[h]); }
-    }
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = 8 * n + 2 * c + e;
+            p[n][e] = r < n_rows ? query_pos(a, s, len, r / group) : -1;
+            if (r < n_rows) { lo = min(lo, p[n][e]); hi = max(hi, p[n][e]); }
+        }
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
     __syncthreads();
@@ -131,14 +143,17 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
     const int64_t stride = static_cast<int64_t>(a.kv_heads) * D;
     const T* const kb = static_cast<const T*>(a.k) + s.kv_row * stride + static_cast<int64_t>(hk) * D + 8 * c;
     const T* const vb = static_cast<const T*>(a.v) + s.kv_row * stride + static_cast<int64_t>(hk) * D + 8 * g;
-    float o[M64][8][4];
+    // o[m][i][n]: columns 64 m + 8 g + 2 i and + 1 (values 0, 1 and 2, 3), rows 8 n + 2 c and + 1
+    float o[M64][4][NR][4];
 #pragma unroll
     for (int m = 0; m < M64; ++m)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[m][i][0] = o[m][i][1] = o[m][i][2] = o[m][i][3] = 0.f;
-    float ref[kHalves], sum[kHalves];
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) { ref[h] = -CUDART_INF_F; sum[h] = 0.f; }
+            for (int n = 0; n < NR; ++n) o[m][i][n][0] = o[m][i][n][1] = o[m][i][n][2] = o[m][i][n][3] = 0.f;
+    float ref[NR][2], sum[NR][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) { ref[n][0] = ref[n][1] = -CUDART_INF_F; sum[n][0] = sum[n][1] = 0.f; }
 
     // Tile t0 + warp + kWarps u is this warp's u-th, in stage u % kStages.  Position of its key (lane & 15):
     const int mine = t1 > t0 + warp ? (t1 - t0 - warp + kWarps - 1) / kWarps : 0;
@@ -192,85 +207,87 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
         const bool all = __all_sync(0xffffffffu, pos >= 0 && pos <= lo && (hi - pos < a.window || pos < a.n_sink));
         const uint8_t* const tile = ring + (warp * kStages + u % kStages) * Sh::kTile + lane * Sh::kPiece;
         const auto piece = [&](int i) { return *reinterpret_cast<const typename K::Raw*>(tile + i * 32 * Sh::kPiece); };
-        float x[2][4] = {};
+        // x[n][2 k + e]: key g + 8 k, row 8 n + 2 c + e
+        float x[NR][4] = {};
 #pragma unroll
         for (int i = 0; i < D32; ++i) {
-            const uint4 qa = q_frag[i][0][lane];
-            const uint4 qb = BOTH ? q_frag[i][kHalves - 1][lane] : make_uint4(0, 0, 0, 0);
+            uint32_t w0[4], w1[4];
+            K::words(piece(i), w0);
+            K::words(piece(D32 + i), w1);
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                uint32_t w[4];
-                K::words(piece(n * D32 + i), w);
-                K::mma(x[n], qa.x, qb.x, qa.y, qb.y, w[0], w[1]);
-                K::mma(x[n], qa.z, qb.z, qa.w, qb.w, w[2], w[3]);
+            for (int n = 0; n < NR; ++n) {
+                const uint4 y = q_frag[i][n][lane];
+                K::mma(x[n], w0[0], w1[0], w0[1], w1[1], y.x, y.y);
+                K::mma(x[n], w0[2], w1[2], w0[3], w1[3], y.z, y.w);
             }
         }
-        // x[n][2 h + e]: row g + 8 h, key 8 n + 2 c + e
 #pragma unroll
-        for (int n = 0; n < 2; ++n)
+        for (int n = 0; n < NR; ++n)
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[n][i] *= a.scale_log2;
         if (!all) {
 #pragma unroll
-            for (int n = 0; n < 2; ++n)
+            for (int k = 0; k < 2; ++k) {
+                const int at = __shfl_sync(0xffffffffu, pos, g + 8 * k);
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const int k = __shfl_sync(0xffffffffu, pos, 8 * n + 2 * c + e);
+                for (int n = 0; n < NR; ++n)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        if (h >= kHalves || !sees(p[h < kHalves ? h : 0], k, a.window, a.n_sink)) x[n][2 * h + e] = -CUDART_INF_F;
-                }
+                    for (int e = 0; e < 2; ++e)
+                        if (!sees(p[n][e], at, a.window, a.n_sink)) x[n][2 * k + e] = -CUDART_INF_F;
+            }
         }
         if (a.logits) {
 #pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                const int r = g + 8 * h;
-                if (r >= n_rows) continue;
-                float* const dst = a.logits + s.logit0 + (static_cast<int64_t>(r / group) * a.n_heads + hk * group + r % group) * s.n_kv;
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int e = 0; e < 2; ++e) {
+                    const int r = 8 * n + 2 * c + e;
+                    if (r >= n_rows) continue;
+                    float* const dst = a.logits + s.logit0 + (static_cast<int64_t>(r / group) * a.n_heads + hk * group + r % group) * s.n_kv;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int j = j0 + 8 * n + 2 * c + e;
-                        if (j < len) dst[j] = x[n][2 * h + e];
-                    }
-            }
+                    for (int k = 0; k < 2; ++k)
+                        if (j0 + g + 8 * k < len) dst[j0 + g + 8 * k] = x[n][2 * k + e];
+                }
         }
         // references
         bool move = false;
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) {
-            const float top = fmaxf(fmaxf(x[0][2 * h], x[0][2 * h + 1]), fmaxf(x[1][2 * h], x[1][2 * h + 1]));
-            move |= top > ref[h] + 8.f;
-        }
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) move |= fmaxf(x[n][e], x[n][2 + e]) > ref[n][e] + 8.f;
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
-            for (int h = 0; h < kHalves; ++h) {
-                float top = fmaxf(fmaxf(x[0][2 * h], x[0][2 * h + 1]), fmaxf(x[1][2 * h], x[1][2 * h + 1]));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
-                top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
-                const float m = fmaxf(ref[h], top);
-                const float f = m == ref[h] ? 1.f : exp2f(ref[h] - m);
-                ref[h] = m;
-                sum[h] *= f;
+            for (int n = 0; n < NR; ++n)
 #pragma unroll
-                for (int mm = 0; mm < M64; ++mm)
+                for (int e = 0; e < 2; ++e) {
+                    float top = fmaxf(x[n][e], x[n][2 + e]);
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) { o[mm][i][2 * h] *= f; o[mm][i][2 * h + 1] *= f; }
-            }
+                    for (int w = 4; w < 32; w *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+                    const float m = fmaxf(ref[n][e], top), f = m == ref[n][e] ? 1.f : exp2f(ref[n][e] - m);
+                    ref[n][e] = m;
+                    sum[n][e] *= f;
+#pragma unroll
+                    for (int mm = 0; mm < M64; ++mm)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { o[mm][i][n][e] *= f; o[mm][i][n][2 + e] *= f; }
+                }
         }
-        uint32_t w_hi[4] = {0, 0, 0, 0}, w_lo[4] = {0, 0, 0, 0};
+        // weights, as the second product's operand: keys 2 c, 2 c + 1 (+ 8) of row 8 n + g
+        uint32_t w_hi[NR][2], w_lo[NR][2];
 #pragma unroll
-        for (int h = 0; h < kHalves; ++h) {
-            const float base = ref[h] == -CUDART_INF_F ? 0.f : ref[h];
+        for (int n = 0; n < NR; ++n) {
+            const float b0 = ref[n][0] == -CUDART_INF_F ? 0.f : ref[n][0], b1 = ref[n][1] == -CUDART_INF_F ? 0.f : ref[n][1];
 #pragma unroll
-            for (int n = 0; n < 2; ++n) {
-                const float y = ex2_approx(x[n][2 * h] - base), z = ex2_approx(x[n][2 * h + 1] - base);
-                sum[h] += y + z;
+            for (int k = 0; k < 2; ++k) {
+                const float y = ex2_approx(x[n][2 * k] - b0), z = ex2_approx(x[n][2 * k + 1] - b1);
+                sum[n][0] += y;
+                sum[n][1] += z;
                 const uint32_t w = K::pack(y, z);
-                const float2 v = K::value(w);
-                w_hi[2 * n + h] = w;
-                w_lo[2 * n + h] = K::pack(y - v.x, z - v.y);
+                w_hi[n][k] = transpose8(w);
+                if (K::kTwoParts) {
+                    const float2 v = K::value(w);
+                    w_lo[n][k] = transpose8(K::pack(y - v.x, z - v.y));
+                }
             }
         }
         bool hidden[4] = {};                                 // values that nobody may look at (0 times NaN is NaN)
@@ -288,35 +305,38 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
                 K::words(v, w[n]);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {                    // column 8 g + i of the group, keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
-                const uint32_t sel = i & 1 ? 0x7632u : 0x5410u;
-                const uint32_t b0 = __byte_perm(w[0][i / 2], w[1][i / 2], sel), b1 = __byte_perm(w[2][i / 2], w[3][i / 2], sel);
-                K::mma(o[m][i], w_hi[0], w_hi[1], w_hi[2], w_hi[3], b0, b1);
-                K::mma(o[m][i], w_lo[0], w_lo[1], w_lo[2], w_lo[3], b0, b1);
+            for (int i = 0; i < 4; ++i) {                    // columns 8 g + 2 i and + 1 of the group, keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+                const uint32_t a0 = __byte_perm(w[0][i], w[1][i], 0x5410), a1 = __byte_perm(w[0][i], w[1][i], 0x7632);
+                const uint32_t a2 = __byte_perm(w[2][i], w[3][i], 0x5410), a3 = __byte_perm(w[2][i], w[3][i], 0x7632);
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    K::mma(o[m][i][n], a0, a1, a2, a3, w_hi[n][0], w_hi[n][1]);
+                    if (K::kTwoParts) K::mma(o[m][i][n], a0, a1, a2, a3, w_lo[n][0], w_lo[n][1]);
+                }
             }
         }
     }
     // ---- the warps' sums, row by row
 #pragma unroll
-    for (int h = 0; h < kHalves; ++h) {
-        sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 1);
-        sum[h] += __shfl_xor_sync(0xffffffffu, sum[h], 2);
-        if (c == 0) { merge_m[warp][g + 8 * h] = ref[h]; merge_l[warp][g + 8 * h] = sum[h]; }
-    }
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int w = 4; w < 32; w *= 2) sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], w);
+            if (g == 0) { merge_m[warp][8 * n + 2 * c + e] = ref[n][e]; merge_l[warp][8 * n + 2 * c + e] = sum[n][e]; }
+        }
     const bool whole = s.parts == 1;
-    for (int r = 0; r < n_rows; ++r) {
+#pragma unroll
+    for (int r = 0; r < 8 * NR; ++r) {
+        if (r >= n_rows) break;
         __syncthreads();
-        if (g == (r & 7)) {
+        if (c == (r & 7) >> 1) {
 #pragma unroll
             for (int m = 0; m < M64; ++m)
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        const int col = 64 * m + 16 * c + 8 * e + i;
-                        const float v = BOTH && r >= 8 ? o[m][i][2 + e] : o[m][i][e];
-                        if (col < D) merge_o[warp][col] = v;
-                    }
+                for (int i = 0; i < 4; ++i)
+                    if (m < D32 / 2 || g < 4)
+                        *reinterpret_cast<float2*>(&merge_o[warp][64 * m + 8 * g + 2 * i]) = make_float2(o[m][i][r / 8][r & 1], o[m][i][r / 8][2 + (r & 1)]);
         }
         __syncthreads();
         float m = merge_m[0][r];
@@ -343,20 +363,17 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
             else *reinterpret_cast<float2*>(a.part_o + at * D + col) = make_float2(x, y);
         }
         if (t == 0) {
-            if (whole) {
-                const float z = l > 0.f ? m + log2f(l) : -CUDART_INF_F;
-                if (a.lse) a.lse[(s.q_row + i) * a.n_heads + head] = z * 0.69314718055994531f;      // ln 2
-            }
+            if (whole && a.lse) a.lse[(s.q_row + i) * a.n_heads + head] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
             if (a.part_ml) a.part_ml[at] = make_float2(m, l);
         }
     }
 }
 
-template <class T, int D32, bool BOTH>
+template <class T, int D32, int NR>
 cudaError_t attend(const AttArgs& a, cudaStream_t stream)
 {
     static KernelSetup setup;
-    const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(attend_token_kernel<T, D32, BOTH>), TokenShape<T, D32>::kSmem, 0);
+    const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(attend_token_kernel<T, D32, NR>), TokenShape<T, D32>::kSmem, 0);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(a.n_blocks), static_cast<unsigned>(a.kv_heads));
@@ -366,12 +383,12 @@ cudaError_t attend(const AttArgs& a, cudaStream_t stream)
     cudaLaunchAttribute attr[1] = {pdl_attribute()};
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, attend_token_kernel<T, D32, BOTH>, a);
+    return cudaLaunchKernelEx(&cfg, attend_token_kernel<T, D32, NR>, a);
 }
 template <class T, int D32>
 cudaError_t by_rows(const AttArgs& a, int rows, cudaStream_t stream)
 {
-    return rows <= 8 ? attend<T, D32, false>(a, stream) : attend<T, D32, true>(a, stream);
+    return rows <= 8 ? attend<T, D32, 1>(a, stream) : attend<T, D32, 2>(a, stream);
 }
 template <class T>
 cudaError_t by_dim(const AttArgs& a, int rows, cudaStream_t stream)
