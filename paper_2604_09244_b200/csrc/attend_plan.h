@@ -8,9 +8,13 @@
 
 namespace mvla {
 
-// Shared memory of a CTA of the token form (attend_token.cu): four warps with three tiles of 16 keys and values each, in whole groups of 64
+// Token form (attend_token.cu): subtiles of 16 keys in a warp's tile; shared memory of a CTA, four warps with three tiles each, in whole groups of 64
 // columns of the values; and the CTAs that fit on a multiprocessor (four at most: by registers).
-constexpr int token_smem(int pieces_of_32, int elem) { return 4 * 3 * (2 * pieces_of_32 + 4 * ((pieces_of_32 + 1) / 2)) * 32 * 8 * elem; }
+constexpr int token_sub(int pieces_of_32) { return pieces_of_32 <= 2 ? 2 : 1; }
+constexpr int token_smem(int pieces_of_32, int elem)
+{
+    return 4 * 3 * token_sub(pieces_of_32) * (2 * pieces_of_32 + 4 * ((pieces_of_32 + 1) / 2)) * 32 * 8 * elem;
+}
 constexpr int token_ctas(int pieces_of_32, int elem)
 {
     const int n = 220 * 1024 / (token_smem(pieces_of_32, elem) + 8 * 1024);

@@ -46,10 +46,21 @@ __device__ __forceinline__ uint32_t pack_f16(float lo, float hi)
 }
 template <class T> struct Kind;
 template <> struct Kind<__nv_bfloat16> {
-    using Raw = uint4;                           // eight elements as they lie in memory
+    using Run = uint4;                           // eight elements as they lie in memory
+    // 32 elements of 16 keys (rows g and g + 8 of a lane) with those of eight query rows
+    static __device__ __forceinline__ void scores(float (&x)[4], const Run& k0, const Run& k1, const Run& y)
+    {
+        mma(x, k0.x, k1.x, k0.y, k1.y, y.x, y.y);
+        mma(x, k0.z, k1.z, k0.w, k1.w, y.z, y.w);
+    }
     static constexpr bool kTwoParts = true;
-    static __device__ __forceinline__ Raw load(const __nv_bfloat16* p) { return __ldg(reinterpret_cast<const uint4*>(p)); }
-    static __device__ __forceinline__ void words(const Raw& r, uint32_t (&w)[4]) { w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w; }
+    static constexpr bool kPairs = false;        // eight elements are what a lane copies at once
+    // eight elements as the products' 16-bit pairs
+    static __device__ __forceinline__ void words(const void* p, uint32_t (&w)[4])
+    {
+        const uint4 r = *static_cast<const uint4*>(p);
+        w[0] = r.x; w[1] = r.y; w[2] = r.z; w[3] = r.w;
+    }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_bf16(lo, hi); }
     static __device__ __forceinline__ float2 value(uint32_t w) { return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)); }
     static __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
@@ -58,17 +69,23 @@ template <> struct Kind<__nv_bfloat16> {
                      : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
     }
 };
-template <> struct Kind<__nv_fp8_e4m3> {         // widened to fp16, which holds every e4m3 number
-    using Raw = uint2;
+template <> struct Kind<__nv_fp8_e4m3> {         // scores from the 8-bit operands; values widened to fp16, which holds every e4m3 number
+    using Run = uint2;
+    static __device__ __forceinline__ void scores(float (&x)[4], const Run& k0, const Run& k1, const Run& y)
+    {
+        asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]) : "r"(k0.x), "r"(k1.x), "r"(k0.y), "r"(k1.y), "r"(y.x), "r"(y.y));
+    }
     static constexpr bool kTwoParts = false;
-    static __device__ __forceinline__ Raw load(const __nv_fp8_e4m3* p) { return __ldg(reinterpret_cast<const uint2*>(p)); }
+    static constexpr bool kPairs = true;         // sixteen, where a head has them
     static __device__ __forceinline__ uint32_t two(uint32_t x)
     {
         const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(x), __NV_E4M3);
         return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16;
     }
-    static __device__ __forceinline__ void words(const Raw& r, uint32_t (&w)[4])
+    static __device__ __forceinline__ void words(const void* p, uint32_t (&w)[4])
     {
+        const uint2 r = *static_cast<const uint2*>(p);
         w[0] = two(r.x & 0xFFFFu); w[1] = two(r.x >> 16); w[2] = two(r.y & 0xFFFFu); w[3] = two(r.y >> 16);
     }
     static __device__ __forceinline__ uint32_t pack(float lo, float hi) { return pack_f16(lo, hi); }
@@ -84,13 +101,24 @@ template <> struct Kind<__nv_fp8_e4m3> {         // widened to fp16, which holds
     }
 };
 
-// Pieces of a lane in a tile: its chunks of two key rows and of four value rows.
+// A warp's tile of kKeys keys in shared memory: runs of 8 or 16 bytes of every lane, side by side.  A row of keys is cut into runs of eight
+// elements (32 elements a step of four lanes), or of sixteen (64) where two steps make a pair; a row of values into runs of eight
+// columns (64 a group of eight lanes) or sixteen (128).
 template <class T, int D32>
 struct TokenShape {
-    static constexpr int kM64 = (D32 + 1) / 2, kPieces = 2 * D32 + 4 * kM64, kPiece = 8 * sizeof(T);
-    static constexpr int kTile = kPieces * 32 * kPiece;      // of a warp
+    static constexpr int kM64 = (D32 + 1) / 2, kSub = token_sub(D32), kKeys = 16 * kSub;
+    static constexpr int kRun = 8 * sizeof(T);
+    static constexpr int kKPairs = Kind<T>::kPairs ? D32 / 2 : 0, kVPairs = Kind<T>::kPairs ? D32 / 4 : 0;     // pairs of steps, of groups
+    static constexpr int kKRow = D32 * 32 * kRun, kVRow = kM64 * 32 * kRun;       // of a lane's row of keys, of values, for the whole warp
+    static constexpr int kTile = kSub * (2 * kKRow + 4 * kVRow);
     static constexpr int kSmem = kWarps * kStages * kTile, kCtas = token_ctas(D32, sizeof(T));
     static_assert(kSmem == token_smem(D32, sizeof(T)), "the plan's size");
+    // element of the head at which lane c's run of step i begins; column at which lane g's of group m does
+    static __device__ __forceinline__ int element(int i, int c) { return i < 2 * kKPairs ? 64 * (i / 2) + 16 * c + 8 * (i & 1) : 32 * i + 8 * c; }
+    static __device__ __forceinline__ int column(int m, int g) { return m < 2 * kVPairs ? 128 * (m / 2) + 16 * g + 8 * (m & 1) : 64 * m + 8 * g; }
+    // where they lie in a row of the tile
+    static __device__ __forceinline__ int key_at(int i, int lane) { return i < 2 * kKPairs ? (i / 2) * 64 * kRun + lane * 2 * kRun + (i & 1) * kRun : i * 32 * kRun + lane * kRun; }
+    static __device__ __forceinline__ int value_at(int m, int lane) { return m < 2 * kVPairs ? (m / 2) * 64 * kRun + lane * 2 * kRun + (m & 1) * kRun : m * 32 * kRun + lane * kRun; }
 };
 
 // The transpose of an 8 x 8 block of 16-bit values, a pair of neighbours in every lane.
@@ -107,9 +135,9 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
 {
     using K = Kind<T>;
     using Sh = TokenShape<T, D32>;
-    constexpr int D = D32 * 32, M64 = Sh::kM64;              // M64: groups of 64 columns of the values
+    constexpr int D = D32 * 32, M64 = Sh::kM64, U = Sh::kSub;
     extern __shared__ __align__(16) uint8_t ring[];
-    __shared__ uint4 q_frag[D32][NR][32];
+    __shared__ typename K::Run q_frag[D32][NR][32];
     __shared__ float merge_o[kWarps][D];
     __shared__ float merge_m[kWarps][16], merge_l[kWarps][16];
     __shared__ int pos_ring[kWarps][kStages][32];
@@ -121,9 +149,9 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
     const T* const q = static_cast<const T*>(a.q);
     for (int u = t; u < D32 * NR * 32; u += kWarps * 32) {
         const int piece = u / (NR * 32), n = u / 32 % NR, l = u & 31, r = (l >> 2) + 8 * n;
-        uint32_t w[4] = {0, 0, 0, 0};
-        if (r < n_rows) K::words(K::load(q + ((s.q_row + r / group) * a.n_heads + hk * group + r % group) * D + 32 * piece + 8 * (l & 3)), w);
-        q_frag[piece][n][l] = make_uint4(w[0], w[1], w[2], w[3]);
+        typename K::Run w = {};
+        if (r < n_rows) w = *reinterpret_cast<const typename K::Run*>(q + ((s.q_row + r / group) * a.n_heads + hk * group + r % group) * D + Sh::element(piece, l & 3));
+        q_frag[piece][n][l] = w;
     }
     int p[NR][2], lo = 0x7FFFFFFF, hi = -1;                  // positions of this lane's rows 8 n + 2 c + e, and the span of all rows
 #pragma unroll
@@ -137,13 +165,13 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
     __syncthreads();
-    const TileRange range = tile_range(a, len, lo, hi, 16);
+    const TileRange range = tile_range(a, len, lo, hi, Sh::kKeys);
     const int part = static_cast<int>(blockIdx.x) - s.blk0, per_part = (range.count + s.parts - 1) / s.parts;
     const int t0 = part * per_part, t1 = min(range.count, t0 + per_part);
     const int64_t stride = static_cast<int64_t>(a.kv_heads) * D;
-    const T* const kb = static_cast<const T*>(a.k) + s.kv_row * stride + static_cast<int64_t>(hk) * D + 8 * c;
-    const T* const vb = static_cast<const T*>(a.v) + s.kv_row * stride + static_cast<int64_t>(hk) * D + 8 * g;
-    // o[m][i][n]: columns 64 m + 8 g + 2 i and + 1 (values 0, 1 and 2, 3), rows 8 n + 2 c and + 1
+    const T* const kb = static_cast<const T*>(a.k) + s.kv_row * stride + static_cast<int64_t>(hk) * D;
+    const T* const vb = static_cast<const T*>(a.v) + s.kv_row * stride + static_cast<int64_t>(hk) * D;
+    // o[m][i][n]: columns column(m, g) + 2 i and + 1 (values 0, 1 and 2, 3), rows 8 n + 2 c and + 1
     float o[M64][4][NR][4];
 #pragma unroll
     for (int m = 0; m < M64; ++m)
@@ -155,30 +183,38 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
 #pragma unroll
     for (int n = 0; n < NR; ++n) { ref[n][0] = ref[n][1] = -CUDART_INF_F; sum[n][0] = sum[n][1] = 0.f; }
 
-    // Tile t0 + warp + kWarps u is this warp's u-th, in stage u % kStages.  Position of its key (lane & 15):
+    // Tile t0 + warp + kWarps u is this warp's u-th.  Position of its key (lane % kKeys):
     const int mine = t1 > t0 + warp ? (t1 - t0 - warp + kWarps - 1) / kWarps : 0;
-    const auto first_key = [&](int u) { return range.tile(t0 + warp + kWarps * u) * 16; };
-    const auto pos_of = [&](int u) { return u < mine ? key_pos(a, s, len, first_key(u) + (lane & 15)) : -1; };
-    const uint32_t lane_at = smem_u32(ring) + warp * kStages * Sh::kTile + lane * Sh::kPiece;
+    const auto first_key = [&](int u) { return range.tile(t0 + warp + kWarps * u) * Sh::kKeys; };
+    const auto pos_of = [&](int u) { return u < mine ? key_pos(a, s, len, first_key(u) + lane % Sh::kKeys) : -1; };
+    uint8_t* const stages = ring + warp * kStages * Sh::kTile;
+    const uint32_t stages_at = smem_u32(stages);
     // starts the copies of a tile that some row sees (always a group of copies, an empty one too)
-    const auto fetch = [&](int u, int pos) {
+    const auto fetch = [&](int u, int stage, int pos) {
         if (u < mine) {
-            pos_ring[warp][u % kStages][lane] = pos;
+            pos_ring[warp][stage][lane] = pos;
             if (__any_sync(0xffffffffu, some_sees(lo, hi, pos, a.window, a.n_sink))) {
                 const int j0 = first_key(u);
-                uint32_t dst = lane_at + u % kStages * Sh::kTile;
+                uint32_t dst = stages_at + stage * Sh::kTile;
 #pragma unroll
-                for (int n = 0; n < 2; ++n) {
+                for (int n = 0; n < 2 * U; ++n, dst += Sh::kKRow) {
                     const T* const row = kb + static_cast<int64_t>(min(j0 + 8 * n + g, len - 1)) * stride;
 #pragma unroll
-                    for (int i = 0; i < D32; ++i, dst += 32 * Sh::kPiece) copy_async<Sh::kPiece>(dst, row + 32 * i);
+                    for (int i = 0; i < D32; ++i) {
+                        if (i < 2 * Sh::kKPairs && (i & 1)) continue;
+                        if (i < 2 * Sh::kKPairs) copy_async<2 * Sh::kRun>(dst + Sh::key_at(i, lane), row + Sh::element(i, c));
+                        else copy_async<Sh::kRun>(dst + Sh::key_at(i, lane), row + Sh::element(i, c));
+                    }
                 }
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    const T* const row = vb + static_cast<int64_t>(min(j0 + 2 * c + (n & 1) + 8 * (n >> 1), len - 1)) * stride;
+                for (int n = 0; n < 4 * U; ++n, dst += Sh::kVRow) {
+                    const T* const row = vb + static_cast<int64_t>(min(j0 + 16 * (n / 4) + 2 * c + (n & 1) + 8 * (n >> 1 & 1), len - 1)) * stride;
 #pragma unroll
-                    for (int m = 0; m < M64; ++m, dst += 32 * Sh::kPiece)
-                        if (m < D32 / 2 || g < 4) copy_async<Sh::kPiece>(dst, row + 64 * m);
+                    for (int m = 0; m < M64; ++m) {
+                        if (m < 2 * Sh::kVPairs && (m & 1)) continue;
+                        if (m < 2 * Sh::kVPairs) copy_async<2 * Sh::kRun>(dst + Sh::value_at(m, lane), row + Sh::column(m, g));
+                        else if (m < D32 / 2 || g < 4) copy_async<Sh::kRun>(dst + Sh::value_at(m, lane), row + Sh::column(m, g));
+                    }
                 }
             }
         }
@@ -188,53 +224,57 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
 #pragma unroll
     for (int u = 0; u < kStages - 1; ++u) ahead[u] = pos_of(u);
 #pragma unroll
-    for (int u = 0; u < kStages - 1; ++u) fetch(u, ahead[u]);
-    int next = pos_of(kStages - 1);
-    for (int u = 0; u < mine; ++u) {
+    for (int u = 0; u < kStages - 1; ++u) fetch(u, u, ahead[u]);
+    int next = pos_of(kStages - 1), stage = 0;
+    for (int u = 0; u < mine; ++u, stage = stage + 1 < kStages ? stage + 1 : 0) {
         const int then = pos_of(u + kStages);
-        fetch(u + kStages - 1, next);                        // (into the stage that the last tile was read from)
+        fetch(u + kStages - 1, stage > 0 ? stage - 1 : kStages - 1, next);       // (into the stage that the last tile was read from)
         next = then;
         wait_copies<kStages - 1>();
-        const int pos = pos_ring[warp][u % kStages][lane], j0 = first_key(u);
+        const int pos = pos_ring[warp][stage][lane], j0 = first_key(u);
         if (!__any_sync(0xffffffffu, some_sees(lo, hi, pos, a.window, a.n_sink))) {
             if (a.logits) {                                  // (rows that nobody sees: their weight is nothing)
-                for (int rr = lane >> 1; rr < n_rows; rr += 16)
-                    for (int j = j0 + 8 * (lane & 1); j < min(j0 + 8 * (lane & 1) + 8, len); ++j)
-                        a.logits[s.logit0 + (static_cast<int64_t>(rr / group) * a.n_heads + hk * group + rr % group) * s.n_kv + j] = -CUDART_INF_F;
+                for (int r = 0; r < n_rows; ++r)
+                    if (lane < Sh::kKeys && j0 + lane < len)
+                        a.logits[s.logit0 + (static_cast<int64_t>(r / group) * a.n_heads + hk * group + r % group) * s.n_kv + j0 + lane] = -CUDART_INF_F;
             }
             continue;
         }
         const bool all = __all_sync(0xffffffffu, pos >= 0 && pos <= lo && (hi - pos < a.window || pos < a.n_sink));
-        const uint8_t* const tile = ring + (warp * kStages + u % kStages) * Sh::kTile + lane * Sh::kPiece;
-        const auto piece = [&](int i) { return *reinterpret_cast<const typename K::Raw*>(tile + i * 32 * Sh::kPiece); };
-        // x[n][2 k + e]: key g + 8 k, row 8 n + 2 c + e
-        float x[NR][4] = {};
+        const uint8_t* const tile = stages + stage * Sh::kTile;
+        // x[v][n][2 k + e]: key 16 v + g + 8 k, row 8 n + 2 c + e
+        float x[U][NR][4] = {};
 #pragma unroll
         for (int i = 0; i < D32; ++i) {
-            uint32_t w0[4], w1[4];
-            K::words(piece(i), w0);
-            K::words(piece(D32 + i), w1);
+            typename K::Run y[NR];
 #pragma unroll
-            for (int n = 0; n < NR; ++n) {
-                const uint4 y = q_frag[i][n][lane];
-                K::mma(x[n], w0[0], w1[0], w0[1], w1[1], y.x, y.y);
-                K::mma(x[n], w0[2], w1[2], w0[3], w1[3], y.z, y.w);
+            for (int n = 0; n < NR; ++n) y[n] = q_frag[i][n][lane];
+#pragma unroll
+            for (int v = 0; v < U; ++v) {
+                const auto k0 = *reinterpret_cast<const typename K::Run*>(tile + 2 * v * Sh::kKRow + Sh::key_at(i, lane));
+                const auto k1 = *reinterpret_cast<const typename K::Run*>(tile + (2 * v + 1) * Sh::kKRow + Sh::key_at(i, lane));
+#pragma unroll
+                for (int n = 0; n < NR; ++n) K::scores(x[v][n], k0, k1, y[n]);
             }
         }
 #pragma unroll
-        for (int n = 0; n < NR; ++n)
+        for (int v = 0; v < U; ++v)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[n][i] *= a.scale_log2;
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[v][n][i] *= a.scale_log2;
         if (!all) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const int at = __shfl_sync(0xffffffffu, pos, g + 8 * k);
+            for (int v = 0; v < U; ++v)
 #pragma unroll
-                for (int n = 0; n < NR; ++n)
+                for (int k = 0; k < 2; ++k) {
+                    const int at = __shfl_sync(0xffffffffu, pos, 16 * v + g + 8 * k);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        if (!sees(p[n][e], at, a.window, a.n_sink)) x[n][2 * k + e] = -CUDART_INF_F;
-            }
+                    for (int n = 0; n < NR; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            if (!sees(p[n][e], at, a.window, a.n_sink)) x[v][n][2 * k + e] = -CUDART_INF_F;
+                }
         }
         if (a.logits) {
 #pragma unroll
@@ -245,25 +285,31 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
                     if (r >= n_rows) continue;
                     float* const dst = a.logits + s.logit0 + (static_cast<int64_t>(r / group) * a.n_heads + hk * group + r % group) * s.n_kv;
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        if (j0 + g + 8 * k < len) dst[j0 + g + 8 * k] = x[n][2 * k + e];
+                    for (int k = 0; k < 2 * U; ++k)
+                        if (j0 + g + 8 * k < len) dst[j0 + g + 8 * k] = x[k / 2][n][2 * (k & 1) + e];
                 }
         }
         // references
+        float top[NR][2];
         bool move = false;
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
-            for (int e = 0; e < 2; ++e) move |= fmaxf(x[n][e], x[n][2 + e]) > ref[n][e] + 8.f;
+            for (int e = 0; e < 2; ++e) {
+                top[n][e] = fmaxf(x[0][n][e], x[0][n][2 + e]);
+                if (U > 1) top[n][e] = fmaxf(top[n][e], fmaxf(x[U - 1][n][e], x[U - 1][n][2 + e]));
+                move |= top[n][e] > ref[n][e] + 8.f;
+            }
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float top = fmaxf(x[n][e], x[n][2 + e]);
+                    float m = top[n][e];
 #pragma unroll
-                    for (int w = 4; w < 32; w *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
-                    const float m = fmaxf(ref[n][e], top), f = m == ref[n][e] ? 1.f : exp2f(ref[n][e] - m);
+                    for (int w = 4; w < 32; w *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, w));
+                    m = fmaxf(ref[n][e], m);
+                    const float f = m == ref[n][e] ? 1.f : exp2f(ref[n][e] - m);
                     ref[n][e] = m;
                     sum[n][e] *= f;
 #pragma unroll
@@ -272,46 +318,48 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
                         for (int i = 0; i < 4; ++i) { o[mm][i][n][e] *= f; o[mm][i][n][2 + e] *= f; }
                 }
         }
-        // weights, as the second product's operand: keys 2 c, 2 c + 1 (+ 8) of row 8 n + g
-        uint32_t w_hi[NR][2], w_lo[NR][2];
 #pragma unroll
-        for (int n = 0; n < NR; ++n) {
-            const float b0 = ref[n][0] == -CUDART_INF_F ? 0.f : ref[n][0], b1 = ref[n][1] == -CUDART_INF_F ? 0.f : ref[n][1];
+        for (int v = 0; v < U; ++v) {
+            // weights, as the second product's operand: keys 2 c, 2 c + 1 (+ 8) of row 8 n + g
+            uint32_t w_hi[NR][2], w_lo[NR][2];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float y = ex2_approx(x[n][2 * k] - b0), z = ex2_approx(x[n][2 * k + 1] - b1);
-                sum[n][0] += y;
-                sum[n][1] += z;
-                const uint32_t w = K::pack(y, z);
-                w_hi[n][k] = transpose8(w);
-                if (K::kTwoParts) {
-                    const float2 v = K::value(w);
-                    w_lo[n][k] = transpose8(K::pack(y - v.x, z - v.y));
+            for (int n = 0; n < NR; ++n) {
+                const float b0 = ref[n][0] == -CUDART_INF_F ? 0.f : ref[n][0], b1 = ref[n][1] == -CUDART_INF_F ? 0.f : ref[n][1];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float y = ex2_approx(x[v][n][2 * k] - b0), z = ex2_approx(x[v][n][2 * k + 1] - b1);
+                    sum[n][0] += y;
+                    sum[n][1] += z;
+                    const uint32_t w = K::pack(y, z);
+                    w_hi[n][k] = transpose8(w);
+                    if (K::kTwoParts) {
+                        const float2 back = K::value(w);
+                        w_lo[n][k] = transpose8(K::pack(y - back.x, z - back.y));
+                    }
                 }
             }
-        }
-        bool hidden[4] = {};                                 // values that nobody may look at (0 times NaN is NaN)
-        if (!all) {
+            bool hidden[4] = {};                             // values that nobody may look at (0 times NaN is NaN)
+            if (!all) {
 #pragma unroll
-            for (int n = 0; n < 4; ++n) hidden[n] = __shfl_sync(0xffffffffu, pos, 2 * c + (n & 1) + 8 * (n >> 1)) < 0;
-        }
-#pragma unroll
-        for (int m = 0; m < M64; ++m) {
-            uint32_t w[4][4];
-#pragma unroll
-            for (int n = 0; n < 4; ++n) {
-                typename K::Raw v = {};
-                if (!hidden[n] && (m < D32 / 2 || g < 4)) v = piece(2 * D32 + n * M64 + m);
-                K::words(v, w[n]);
+                for (int n = 0; n < 4; ++n) hidden[n] = __shfl_sync(0xffffffffu, pos, 16 * v + 2 * c + (n & 1) + 8 * (n >> 1)) < 0;
             }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {                    // columns 8 g + 2 i and + 1 of the group, keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
-                const uint32_t a0 = __byte_perm(w[0][i], w[1][i], 0x5410), a1 = __byte_perm(w[0][i], w[1][i], 0x7632);
-                const uint32_t a2 = __byte_perm(w[2][i], w[3][i], 0x5410), a3 = __byte_perm(w[2][i], w[3][i], 0x7632);
+            for (int m = 0; m < M64; ++m) {
+                uint32_t w[4][4];
 #pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    K::mma(o[m][i][n], a0, a1, a2, a3, w_hi[n][0], w_hi[n][1]);
-                    if (K::kTwoParts) K::mma(o[m][i][n], a0, a1, a2, a3, w_lo[n][0], w_lo[n][1]);
+                for (int n = 0; n < 4; ++n) {
+                    w[n][0] = w[n][1] = w[n][2] = w[n][3] = 0;
+                    if (!hidden[n] && (m < D32 / 2 || g < 4)) K::words(tile + 2 * U * Sh::kKRow + (4 * v + n) * Sh::kVRow + Sh::value_at(m, lane), w[n]);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {                // columns 2 i and 2 i + 1 of the lane's run, keys 2 c, 2 c + 1, 2 c + 8, 2 c + 9
+                    const uint32_t a0 = __byte_perm(w[0][i], w[1][i], 0x5410), a1 = __byte_perm(w[0][i], w[1][i], 0x7632);
+                    const uint32_t a2 = __byte_perm(w[2][i], w[3][i], 0x5410), a3 = __byte_perm(w[2][i], w[3][i], 0x7632);
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) {
+                        K::mma(o[m][i][n], a0, a1, a2, a3, w_hi[n][0], w_hi[n][1]);
+                        if (K::kTwoParts) K::mma(o[m][i][n], a0, a1, a2, a3, w_lo[n][0], w_lo[n][1]);
+                    }
                 }
             }
         }
@@ -336,7 +384,7 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     if (m < D32 / 2 || g < 4)
-                        *reinterpret_cast<float2*>(&merge_o[warp][64 * m + 8 * g + 2 * i]) = make_float2(o[m][i][r / 8][r & 1], o[m][i][r / 8][2 + (r & 1)]);
+                        *reinterpret_cast<float2*>(&merge_o[warp][Sh::column(m, g) + 2 * i]) = make_float2(o[m][i][r / 8][r & 1], o[m][i][r / 8][2 + (r & 1)]);
         }
         __syncthreads();
         float m = merge_m[0][r];
