@@ -4,10 +4,11 @@
 // destinations are then different rows by construction, so all moves may run at once and in place, and a decode step that is one row
 // over its budget moves one row instead of the cache.
 //
-// evict_select_kernel: one CTA a sequence.  Every row has a 32-bit key (its weight's bits in order of size; protected rows above all,
-// hidden rows below all); four rounds of 256-bin counts over the keys, most significant byte first, give the key of the
-// last row that stays and how many of its equals do; then every warp walks a run of rows in ascending order and counts, and once
-// more to write.  Keys are kept in shared memory where they fit.  Bound by the latency of its passes.
+// evict_select_kernel: a cluster of one to eight CTAs a sequence, by its length; a CTA has a run of its rows.  Every row has a 32-bit key
+// (its weight's bits in order of size; protected rows above all, hidden rows below all); four rounds of 256-bin counts over the keys, most
+// significant byte first, give the key of the last row that stays and how many of its equals do: every CTA adds up the cluster's counts for
+// itself, out of the others' shared memory.  Then every warp walks a run of rows in ascending order and counts, and once more to write.
+// Keys are kept in shared memory where they fit.  Bound by the latency of its passes.
 // evict_move_kernel: one warp a 2 KB piece of a moved row.  Bound by bytes.
 #include "device_utils.cuh"
 #include "serve.h"
@@ -20,6 +21,7 @@ namespace {
 constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kKeysInSmem = 49152;           // 192 KB
+constexpr int kRowsPerCta = 4096;            // from here on a sequence gets another CTA, up to kMaxCluster
 constexpr int kMoveThreads = 256;
 constexpr int kPiece = 2048;
 constexpr int kMovesInSelect = 4;            // rows that the selecting CTA moves itself
@@ -58,8 +60,22 @@ __device__ __forceinline__ int block_max(int v, int* red)
     __syncthreads();
     return __reduce_max_sync(0xffffffffu, red[threadIdx.x & 31]);
 }
-// Exclusive sum over the warps of one value per warp (the same in all its lanes), and the total.
-__device__ __forceinline__ int warps_before(int v, int* red, int* total)
+__device__ __forceinline__ int ld_peer(const int* p, uint32_t rank)
+{
+    uint32_t at;
+    int v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    cluster_arrive_release();
+    cluster_wait_acquire();
+}
+// Exclusive sum over the cluster's warps of one value per warp (the same in all its lanes), and the total.  `slot`: a word of its own for every
+// use in a kernel, so that no barrier is needed behind the reading.
+__device__ __forceinline__ int warps_before(int v, int* red, int* slot, uint32_t rank, uint32_t n_ranks, int* total)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __syncthreads();
@@ -72,58 +88,95 @@ __device__ __forceinline__ int warps_before(int v, int* red, int* total)
         const int y = __shfl_up_sync(0xffffffffu, x, o);
         if (lane >= o) x += y;
     }
-    *total = __shfl_sync(0xffffffffu, x, 31);
-    return __shfl_sync(0xffffffffu, x - mine, warp);
+    const int own = __shfl_sync(0xffffffffu, x, 31);
+    int before = __shfl_sync(0xffffffffu, x - mine, warp);
+    *total = own;
+    if (n_ranks > 1) {
+        if (threadIdx.x == 0) *slot = own;
+        cluster_sync();
+        *total = 0;
+        for (uint32_t r = 0; r < n_ranks; ++r) {
+            const int y = ld_peer(slot, r);
+            *total += y;
+            if (r < rank) before += y;
+        }
+    }
+    return before;
 }
 
 __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_constant__ EvictArgs a)
 {
     extern __shared__ uint32_t cached[];
-    __shared__ int hist[256];
+    __shared__ int hist[2][256];
     __shared__ int red[kWarps];
-    __shared__ int found[2];
-    const EvictSeq& s = a.s[blockIdx.x];
+    __shared__ int found[2], slots[4];
+    uint32_t n_ranks;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ranks));
+    const uint32_t rank = cluster_ctarank();
+    const int seq = static_cast<int>(blockIdx.x / n_ranks);
+    const EvictSeq& s = a.s[seq];
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
     pdl_wait();
     const int n = seq_rows(a, s), m = min(n, s.budget);
     const int64_t row = s.kv_row;
-    __syncthreads();                                          // (kv_len_out may be kv_len: everybody has read it)
+    __syncthreads();                                          // (kv_len_out may be kv_len: everybody of the CTA has read it)
+    // this CTA's rows: whole runs of 1024
+    const int per_rank = ((n + static_cast<int>(n_ranks) - 1) / static_cast<int>(n_ranks) + kThreads - 1) / kThreads * kThreads;
+    const int r0 = min(static_cast<int>(rank) * per_rank, n), r1 = min(r0 + per_rank, n);
     if (m == n || m == 0) {                                   // everything stays, or nothing
-        if (a.pos_out != a.pos) for (int j = t; j < m; j += kThreads) a.pos_out[row + j] = a.pos[row + j];
-        if (a.mass_out != a.mass) for (int j = t; j < m; j += kThreads) a.mass_out[row + j] = a.mass[row + j];
-        if (a.kept_idx) for (int j = t; j < m; j += kThreads) a.kept_idx[row + j] = j;
-        if (t == 0) {
-            a.n_moves[blockIdx.x] = 0;
-            if (a.kv_len_out) a.kv_len_out[s.index] = m;
+        const int end = min(r1, m);
+        if (a.pos_out != a.pos) for (int j = r0 + t; j < end; j += kThreads) a.pos_out[row + j] = a.pos[row + j];
+        if (a.mass_out != a.mass) for (int j = r0 + t; j < end; j += kThreads) a.mass_out[row + j] = a.mass[row + j];
+        if (a.kept_idx) for (int j = r0 + t; j < end; j += kThreads) a.kept_idx[row + j] = j;
+        if (t == 0 && rank == 0) {
+            a.n_moves[seq] = 0;
+            if (a.kv_len_out) a.kv_len_out[s.index] = m;      // (another CTA of the cluster that reads it now ends here just the same)
         }
         return;
     }
     int last = -1;
-    for (int j = t; j < n; j += kThreads) last = max(last, a.pos[row + j]);
+    for (int j = r0 + t; j < r1; j += kThreads) last = max(last, a.pos[row + j]);
     last = block_max(last, red);
-    const bool fits = n <= kKeysInSmem;
-    const auto key_at = [&](int j) { return fits ? cached[j] : key_of(a, s, j, last); };
-    if (fits) for (int j = t; j < n; j += kThreads) cached[j] = key_of(a, s, j, last);
+    if (t < 256) hist[0][t] = 0;
+    if (n_ranks > 1) {
+        if (t == 0) slots[3] = last;
+        cluster_sync();
+        for (uint32_t r = 0; r < n_ranks; ++r) last = max(last, ld_peer(&slots[3], r));
+    }
+    const bool fits = r1 - r0 <= kKeysInSmem;
+    const auto key_at = [&](int j) { return fits ? cached[j - r0] : key_of(a, s, j, last); };
+    if (fits) for (int j = r0 + t; j < r1; j += kThreads) cached[j - r0] = key_of(a, s, j, last);
     // The key of the m-th row in descending order, byte by byte; `left`: rows still to be found among those with the bytes so far.
     uint32_t prefix = 0;
     int left = m;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-        if (t < 256) hist[t] = 0;
+#pragma unroll 1
+    for (int round = 0; round < 4; ++round) {
+        const int shift = 24 - 8 * round;
+        int* const mine = hist[round & 1];
+        const uint32_t above = round == 0 ? 0u : 0xFFFFFFFFu << (shift + 8);
         __syncthreads();
-        const uint32_t above = shift == 24 ? 0u : 0xFFFFFFFFu << (shift + 8);
-        for (int j0 = 0; j0 < n; j0 += kThreads) {
+        for (int j0 = r0; j0 < r1; j0 += kThreads) {
             const int j = j0 + t;
-            const uint32_t k = j < n ? key_at(j) : 0u;
-            const bool counts = j < n && (k & above) == prefix;
+            const uint32_t k = j < r1 ? key_at(j) : 0u;
+            const bool counts = j < r1 && (k & above) == prefix;
             const uint32_t bin = counts ? (k >> shift) & 255u : 256u;
             const unsigned same = __match_any_sync(0xffffffffu, bin);      // (weights crowd in few bins: one add for all lanes of a bin)
-            if (counts && lane == __ffs(same) - 1) atomicAdd(&hist[bin], __popc(same));
+            if (counts && lane == __ffs(same) - 1) atomicAdd(&mine[bin], __popc(same));
         }
         __syncthreads();
+        if (n_ranks > 1) cluster_sync();
+        // (the other buffer was read by everybody before this barrier)
+        if (t < 256) hist[(round + 1) & 1][t] = 0;
         if (warp == 0) {                                      // eight bins a lane, from the top
             int c[8], sum = 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sum += c[i] = hist[255 - (lane * 8 + i)];
+            for (int i = 0; i < 8; ++i) {
+                int* const bin = &mine[255 - (lane * 8 + i)];
+                c[i] = 0;
+                if (n_ranks == 1) c[i] = *bin;
+                else for (uint32_t r = 0; r < n_ranks; ++r) c[i] += ld_peer(bin, r);
+                sum += c[i];
+            }
             int upto = sum;
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) {
@@ -143,13 +196,12 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
         __syncthreads();
         prefix |= static_cast<uint32_t>(found[0]) << shift;
         left = found[1];
-        __syncthreads();
     }
     // Rows with a larger key stay, and the first `left` of those with this one.  A warp has a run of rows.
-    const int run = (n + kThreads - 1) / kThreads * 32, first = min(warp * run, n), end = min(first + run, n);
+    const int run = (r1 - r0 + kThreads - 1) / kThreads * 32, first = min(r0 + warp * run, r1), end = min(first + run, r1);
     int total, equal = 0;
     for (int j0 = first; j0 < end; j0 += 32) equal += __popc(__ballot_sync(0xffffffffu, j0 + lane < end && key_at(j0 + lane) == prefix));
-    const int equal_before = warps_before(equal, red, &total);
+    const int equal_before = warps_before(equal, red, &slots[0], rank, n_ranks, &total);
     const auto kept_of = [&](int j0, int& seen) {             // which of 32 rows stay; `seen`: equals so far
         const uint32_t k = j0 + lane < end ? key_at(j0 + lane) : 0u;
         const unsigned eq = __ballot_sync(0xffffffffu, j0 + lane < end && k == prefix);
@@ -167,7 +219,7 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
         moved += __popc(stay & ~below);
     }
     int n_moves;
-    int hole_at = warps_before(holes, red, &total), moved_at = warps_before(moved, red, &n_moves);
+    int hole_at = warps_before(holes, red, &slots[1], rank, n_ranks, &total), moved_at = warps_before(moved, red, &slots[2], rank, n_ranks, &n_moves);
     int2* const moves = a.moves + s.move0;
     for (int j0 = first, seen = equal_before; j0 < end; j0 += 32) {
         const unsigned stay = kept_of(j0, seen);
@@ -185,18 +237,20 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
         hole_at += __popc(hole);
         moved_at += __popc(from);
     }
-    __syncthreads();                                          // the block's writes to `moves` are visible to it
-    for (int i = t; i < n_moves; i += kThreads) {
+    // (the writes to `moves` are visible to the CTA, to the cluster; and nobody reads another's shared memory any more)
+    if (n_ranks > 1) cluster_sync();
+    else __syncthreads();
+    for (int i = static_cast<int>(rank) * kThreads + t; i < n_moves; i += static_cast<int>(n_ranks) * kThreads) {
         const int2 mv = moves[i];
         a.pos_out[row + mv.y] = a.pos[row + mv.x];
         a.mass_out[row + mv.y] = a.mass[row + mv.x];
         if (a.kept_idx) a.kept_idx[row + mv.y] = mv.x;
     }
-    if (t == 0) {
-        a.n_moves[blockIdx.x] = n_moves;
+    if (t == 0 && rank == 0) {
+        a.n_moves[seq] = n_moves;
         if (a.kv_len_out) a.kv_len_out[s.index] = m;
     }
-    if (a.max_moves <= kMovesInSelect) {                      // (then no other kernel moves rows)
+    if (a.max_moves <= kMovesInSelect && rank == 0) {         // (then no other kernel moves rows)
         const int pieces = static_cast<int>((a.row_bytes + kPiece - 1) / kPiece);
         for (int u = warp; u < n_moves * pieces * 2; u += kWarps) {
             const int2 mv = moves[u / (2 * pieces)];
@@ -246,19 +300,27 @@ cudaError_t launch_cache_evict(const EvictArgs& a, cudaStream_t stream)
         longest = std::max(longest, a.s[b].n_kv);
         most += std::min(a.s[b].budget, std::max(0, a.s[b].n_kv - a.s[b].budget));
     }
-    const size_t smem = sizeof(uint32_t) * static_cast<size_t>(std::min(longest, kKeysInSmem));
+    int cluster = 1;
+    while (cluster < kMaxCluster && longest > cluster * kRowsPerCta) cluster *= 2;
+    const int per_cta = (longest / cluster + 1 + kThreads - 1) / kThreads * kThreads;
+    const size_t smem = sizeof(uint32_t) * static_cast<size_t>(std::min(per_cta, kKeysInSmem));
     cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(evict_select_kernel), smem, 0);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(a.n_seq));
+    cfg.gridDim = dim3(static_cast<unsigned>(a.n_seq * cluster));
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cudaLaunchAttribute attr[2] = {pdl_attribute(), {}};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     e = cudaLaunchKernelEx(&cfg, evict_select_kernel, a);
     if (e != cudaSuccess || a.max_moves <= kMovesInSelect) return e;
+    cfg.numAttrs = 1;
     const int64_t units = most * 2 * ((a.row_bytes + kPiece - 1) / kPiece);
     cfg.gridDim = dim3(static_cast<unsigned>(std::min<int64_t>((units + kMoveThreads / 32 - 1) / (kMoveThreads / 32), 8 * sm_count_of_current_device())));
     cfg.blockDim = dim3(kMoveThreads);
