@@ -5,9 +5,9 @@
 // over its budget moves one row instead of the cache.
 //
 // evict_select_kernel: a cluster of one to eight CTAs a sequence, by its length; a CTA has a run of its rows.  Every row has a 32-bit key
-// (its weight's bits in order of size; protected rows above all, hidden rows below all); four rounds of 256-bin counts over the keys, most
-// significant byte first, give the key of the last row that stays and how many of its equals do: every CTA adds up the cluster's counts for
-// itself, out of the others' shared memory.  Then every warp walks a run of rows in ascending order and counts, and once more to write.
+// (its weight's bits in order of size; protected rows above all, hidden rows below all); three rounds of 2048-bin counts over the keys, most
+// significant bits first (sign, exponent and two bits of the fraction, so that weights of one size spread over bins), give the key of the
+// last row that stays and how many of its equals do: every CTA adds up the cluster's counts for itself, out of the others' shared memory.  Then every warp walks a run of rows in ascending order and counts, and once more to write.
 // Keys are kept in shared memory where they fit.  Bound by the latency of its passes.
 // evict_move_kernel: one warp a 2 KB piece of a moved row.  Bound by bytes.
 #include "device_utils.cuh"
@@ -22,6 +22,7 @@ constexpr int kThreads = 1024;
 constexpr int kWarps = kThreads / 32;
 constexpr int kKeysInSmem = 49152;           // 192 KB
 constexpr int kRowsPerCta = 4096;            // from here on a sequence gets another CTA, up to kMaxCluster
+constexpr int kBins = 2 * kThreads;          // of a round: eleven bits of the key
 constexpr int kMoveThreads = 256;
 constexpr int kPiece = 2048;
 constexpr int kMovesInSelect = 4;            // rows that the selecting CTA moves itself
@@ -73,9 +74,8 @@ __device__ __forceinline__ void cluster_sync()
     cluster_arrive_release();
     cluster_wait_acquire();
 }
-// Exclusive sum over the cluster's warps of one value per warp (the same in all its lanes), and the total.  `slot`: a word of its own for every
-// use in a kernel, so that no barrier is needed behind the reading.
-__device__ __forceinline__ int warps_before(int v, int* red, int* slot, uint32_t rank, uint32_t n_ranks, int* total)
+// Exclusive sum over the CTA's warps of one value per warp (the same in all its lanes), and the total.
+__device__ __forceinline__ int warps_before(int v, int* red, int* total)
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     __syncthreads();
@@ -88,28 +88,16 @@ __device__ __forceinline__ int warps_before(int v, int* red, int* slot, uint32_t
         const int y = __shfl_up_sync(0xffffffffu, x, o);
         if (lane >= o) x += y;
     }
-    const int own = __shfl_sync(0xffffffffu, x, 31);
-    int before = __shfl_sync(0xffffffffu, x - mine, warp);
-    *total = own;
-    if (n_ranks > 1) {
-        if (threadIdx.x == 0) *slot = own;
-        cluster_sync();
-        *total = 0;
-        for (uint32_t r = 0; r < n_ranks; ++r) {
-            const int y = ld_peer(slot, r);
-            *total += y;
-            if (r < rank) before += y;
-        }
-    }
-    return before;
+    *total = __shfl_sync(0xffffffffu, x, 31);
+    return __shfl_sync(0xffffffffu, x - mine, warp);
 }
 
 __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_constant__ EvictArgs a)
 {
     extern __shared__ uint32_t cached[];
-    __shared__ int hist[2][256];
+    __shared__ int hist[2][kBins];
     __shared__ int red[kWarps];
-    __shared__ int found[2], slots[4];
+    __shared__ int found[2], slots[3];
     uint32_t n_ranks;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ranks));
     const uint32_t rank = cluster_ctarank();
@@ -135,73 +123,77 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
         return;
     }
     int last = -1;
+#pragma unroll 4
     for (int j = r0 + t; j < r1; j += kThreads) last = max(last, a.pos[row + j]);
     last = block_max(last, red);
-    if (t < 256) hist[0][t] = 0;
+    hist[0][t] = hist[0][t + kThreads] = 0;
     if (n_ranks > 1) {
-        if (t == 0) slots[3] = last;
+        if (t == 0) slots[0] = last;
         cluster_sync();
-        for (uint32_t r = 0; r < n_ranks; ++r) last = max(last, ld_peer(&slots[3], r));
+        for (uint32_t r = 0; r < n_ranks; ++r) last = max(last, ld_peer(&slots[0], r));
     }
     const bool fits = r1 - r0 <= kKeysInSmem;
     const auto key_at = [&](int j) { return fits ? cached[j - r0] : key_of(a, s, j, last); };
-    if (fits) for (int j = r0 + t; j < r1; j += kThreads) cached[j - r0] = key_of(a, s, j, last);
-    // The key of the m-th row in descending order, byte by byte; `left`: rows still to be found among those with the bytes so far.
+    if (fits) {
+#pragma unroll 4
+        for (int j = r0 + t; j < r1; j += kThreads) cached[j - r0] = key_of(a, s, j, last);
+    }
+    // The key of the m-th row in descending order, eleven, eleven and ten bits; `left`: rows still to be found among those with the bits so far.
     uint32_t prefix = 0;
-    int left = m;
+    int left = m, equal_here = 0, equal_before = 0;          // rows with that key: in this CTA, in the CTAs before it
 #pragma unroll 1
-    for (int round = 0; round < 4; ++round) {
-        const int shift = 24 - 8 * round;
+    for (int round = 0; round < 3; ++round) {
+        const int shift = round == 0 ? 21 : round == 1 ? 10 : 0;
         int* const mine = hist[round & 1];
-        const uint32_t above = round == 0 ? 0u : 0xFFFFFFFFu << (shift + 8);
+        const uint32_t above = round == 0 ? 0u : round == 1 ? 0xFFE00000u : 0xFFFFFC00u, bins = round < 2 ? 2047u : 1023u;
         __syncthreads();
-        for (int j0 = r0; j0 < r1; j0 += kThreads) {
-            const int j = j0 + t;
-            const uint32_t k = j < r1 ? key_at(j) : 0u;
-            const bool counts = j < r1 && (k & above) == prefix;
-            const uint32_t bin = counts ? (k >> shift) & 255u : 256u;
-            const unsigned same = __match_any_sync(0xffffffffu, bin);      // (weights crowd in few bins: one add for all lanes of a bin)
-            if (counts && lane == __ffs(same) - 1) atomicAdd(&mine[bin], __popc(same));
+#pragma unroll 2
+        for (int j = r0 + t; j < r1; j += kThreads) {
+            const uint32_t k = key_at(j);
+            if ((k & above) == prefix) atomicAdd(&mine[(k >> shift) & bins], 1);
         }
         __syncthreads();
         if (n_ranks > 1) cluster_sync();
         // (the other buffer was read by everybody before this barrier)
-        if (t < 256) hist[(round + 1) & 1][t] = 0;
-        if (warp == 0) {                                      // eight bins a lane, from the top
-            int c[8], sum = 0;
+        hist[(round + 1) & 1][t] = hist[(round + 1) & 1][t + kThreads] = 0;
+        // two bins a thread, from the top
+        const int top = kBins - 1 - 2 * t;
+        int c0 = 0, c1 = 0;
+        if (n_ranks == 1) {
+            c0 = mine[top];
+            c1 = mine[top - 1];
+        } else {
+            for (uint32_t r = 0; r < n_ranks; ++r) { c0 += ld_peer(&mine[top], r); c1 += ld_peer(&mine[top - 1], r); }
+        }
+        int upto = c0 + c1;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                int* const bin = &mine[255 - (lane * 8 + i)];
-                c[i] = 0;
-                if (n_ranks == 1) c[i] = *bin;
-                else for (uint32_t r = 0; r < n_ranks; ++r) c[i] += ld_peer(bin, r);
-                sum += c[i];
-            }
-            int upto = sum;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) {
-                const int y = __shfl_up_sync(0xffffffffu, upto, o);
-                if (lane >= o) upto += y;
-            }
-            int before = upto - sum;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (before < left && left <= before + c[i]) {
-                    found[0] = 255 - (lane * 8 + i);
-                    found[1] = left - before;
-                }
-                before += c[i];
-            }
+        for (int o = 1; o < 32; o *= 2) {
+            const int y = __shfl_up_sync(0xffffffffu, upto, o);
+            if (lane >= o) upto += y;
+        }
+        int all;
+        const int before = warps_before(__shfl_sync(0xffffffffu, upto, 31), red, &all) + upto - c0 - c1;
+        if (before < left && left <= before + c0 + c1) {      // (one thread of the CTA)
+            const bool second = left > before + c0;
+            found[0] = second ? top - 1 : top;
+            found[1] = left - before - (second ? c0 : 0);
         }
         __syncthreads();
         prefix |= static_cast<uint32_t>(found[0]) << shift;
         left = found[1];
+        if (round == 2) {
+            equal_here = mine[found[0]];
+            for (uint32_t r = 0; r < rank; ++r) equal_before += ld_peer(&mine[found[0]], r);
+        }
     }
     // Rows with a larger key stay, and the first `left` of those with this one.  A warp has a run of rows.
     const int run = (r1 - r0 + kThreads - 1) / kThreads * 32, first = min(r0 + warp * run, r1), end = min(first + run, r1);
-    int total, equal = 0;
-    for (int j0 = first; j0 < end; j0 += 32) equal += __popc(__ballot_sync(0xffffffffu, j0 + lane < end && key_at(j0 + lane) == prefix));
-    const int equal_before = warps_before(equal, red, &slots[0], rank, n_ranks, &total);
+    int total;
+    if (equal_here > 1) {                                     // (of one it does not matter which warp has it)
+        int equal = 0;
+        for (int j0 = first; j0 < end; j0 += 32) equal += __popc(__ballot_sync(0xffffffffu, j0 + lane < end && key_at(j0 + lane) == prefix));
+        equal_before += warps_before(equal, red, &total);
+    }
     const auto kept_of = [&](int j0, int& seen) {             // which of 32 rows stay; `seen`: equals so far
         const uint32_t k = j0 + lane < end ? key_at(j0 + lane) : 0u;
         const unsigned eq = __ballot_sync(0xffffffffu, j0 + lane < end && k == prefix);
@@ -218,8 +210,18 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
         holes += __popc(~stay & below & there);
         moved += __popc(stay & ~below);
     }
-    int n_moves;
-    int hole_at = warps_before(holes, red, &slots[1], rank, n_ranks, &total), moved_at = warps_before(moved, red, &slots[2], rank, n_ranks, &n_moves);
+    int holes_here, n_moves;
+    int hole_at = warps_before(holes, red, &holes_here), moved_at = warps_before(moved, red, &n_moves);
+    if (n_ranks > 1) {
+        if (t == 0) { slots[1] = holes_here; slots[2] = n_moves; }
+        cluster_sync();
+        n_moves = 0;
+        for (uint32_t r = 0; r < n_ranks; ++r) {
+            const int moved_there = ld_peer(&slots[2], r);
+            n_moves += moved_there;
+            if (r < rank) { hole_at += ld_peer(&slots[1], r); moved_at += moved_there; }
+        }
+    }
     int2* const moves = a.moves + s.move0;
     for (int j0 = first, seen = equal_before; j0 < end; j0 += 32) {
         const unsigned stay = kept_of(j0, seen);
