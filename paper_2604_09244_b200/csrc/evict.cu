@@ -69,6 +69,14 @@ __device__ __forceinline__ int ld_peer(const int* p, uint32_t rank)
     asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
     return v;
 }
+__device__ __forceinline__ int2 ld_peer2(const int* p, uint32_t rank)
+{
+    uint32_t at;
+    int2 v;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(smem_u32(p)), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.s32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+    return v;
+}
 __device__ __forceinline__ void cluster_sync()
 {
     cluster_arrive_release();
@@ -95,7 +103,7 @@ __device__ __forceinline__ int warps_before(int v, int* red, int* total)
 __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_constant__ EvictArgs a)
 {
     extern __shared__ uint32_t cached[];
-    __shared__ int hist[2][kBins];
+    __shared__ __align__(8) int hist[2][kBins];
     __shared__ int red[kWarps];
     __shared__ int found[2], slots[3];
     uint32_t n_ranks;
@@ -163,7 +171,11 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
             c0 = mine[top];
             c1 = mine[top - 1];
         } else {
-            for (uint32_t r = 0; r < n_ranks; ++r) { c0 += ld_peer(&mine[top], r); c1 += ld_peer(&mine[top - 1], r); }
+            int2 c[kMaxCluster];                              // (all on their way at once, each CTA beginning with another)
+#pragma unroll
+            for (uint32_t i = 0; i < kMaxCluster; ++i) c[i] = i < n_ranks ? ld_peer2(&mine[top - 1], (i + rank) & (n_ranks - 1)) : make_int2(0, 0);
+#pragma unroll
+            for (uint32_t i = 0; i < kMaxCluster; ++i) { c0 += c[i].y; c1 += c[i].x; }
         }
         int upto = c0 + c1;
 #pragma unroll
