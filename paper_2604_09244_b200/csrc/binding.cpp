@@ -419,11 +419,13 @@ bool stream_on(PyObject* o, int64_t device, void** st)
 }
 // Memory for the time that the stream takes to run the call (torch's allocator keeps it apart from what other streams use, and inside
 // a graph capture in the graph's pool).
-at::Tensor scratch(int64_t bytes, int64_t device, void* st)
+at::Tensor fresh_on(at::IntArrayRef sizes, at::ScalarType type, int64_t device, PyObject* stream, void* st)
 {
     const auto index = static_cast<c10::DeviceIndex>(device);
+    const auto options = at::TensorOptions().dtype(type).device(at::kCUDA, index);
+    if (stream == Py_None) return at::empty(sizes, options);              // (the device's current stream)
     const c10::cuda::CUDAStreamGuard guard(c10::cuda::getStreamFromExternal(static_cast<cudaStream_t>(st), index));
-    return at::empty({bytes}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, index));
+    return at::empty(sizes, options);
 }
 at::ScalarType scalar_of(int64_t dtype)
 {
@@ -465,7 +467,7 @@ bool strided_rows(PyObject* o, const char* name, const Shape& c, int64_t heads, 
 }
 
 // qk_norm_rope(ctx, dtype, heads, kv_heads, dim, device, q, k, v, pos, inv_freq, q_weight, k_weight, flags, eps, q_out, k_out, v_out,
-//   out_rows, stream) -> status
+//   out_rows, stream) -> (status, q_out, k_out, v_out); an output that is missing beside its input is allocated
 PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
     MVLA_TRY
@@ -497,17 +499,37 @@ PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
         !expect(!tko || !tvo || tko->size(0) == tvo->size(0), "k_out, v_out: as many rows of one as of the other") ||
         !expect(!tf || tf->size(0) <= c.dim, "inv_freq: one entry per pair of a head"))
         return nullptr;
+    if (!expect(!tto || ((a[7] == Py_None || tko) && (a[8] == Py_None || tvo)), "out_rows: rows of a k_out / v_out that is given")) return nullptr;
     r.n_rows = rows;
     r.q_weight = wq; r.k_weight = wk;
     r.pos = static_cast<const int32_t*>(pos);
     r.inv_freq = static_cast<const double*>(freq);
     r.rot_dim = tf ? static_cast<int32_t>(2 * tf->size(0)) : 0;
     r.flags = static_cast<uint32_t>(flags);
-    r.q_out = qo; r.k_out = ko; r.v_out = vo;
     r.out_rows = static_cast<const int32_t*>(to);
-    r.kv_rows = tko ? tko->size(0) : tvo ? tvo->size(0) : 0;
-    mvla_ctx* ctx = ctx_of(a[0]);
-    return PyLong_FromLong(unlocked([&] { return mvla_qk_norm_rope(ctx, &r, st); }));
+    PyObject* outs[3] = {a[15], a[16], a[17]};
+    for (int i = 0; i < 3; ++i) Py_INCREF(outs[i]);
+    const at::Tensor* const given[3] = {tqo, tko, tvo};
+    void* ptr[3] = {qo, ko, vo};
+    int64_t kv_rows = tko ? tko->size(0) : tvo ? tvo->size(0) : rows;
+    bool ok = true;
+    for (int i = 0; i < 3 && ok; ++i) {
+        if (given[i] || a[6 + i] == Py_None) continue;
+        const at::Tensor t = fresh_on({i ? kv_rows : rows, i ? c.kv_heads : c.heads, c.dim}, c.kept, c.device, a[19], st);
+        ptr[i] = t.data_ptr();
+        Py_DECREF(outs[i]);
+        ok = (outs[i] = THPVariable_Wrap(t)) != nullptr;
+    }
+    PyObject* ret = nullptr;
+    if (ok) {
+        r.q_out = ptr[0]; r.k_out = ptr[1]; r.v_out = ptr[2];
+        r.kv_rows = kv_rows;
+        mvla_ctx* ctx = ctx_of(a[0]);
+        const int32_t rc = unlocked([&] { return mvla_qk_norm_rope(ctx, &r, st); });
+        ret = Py_BuildValue("(iOOO)", rc, outs[0], outs[1], outs[2]);
+    }
+    for (int i = 0; i < 3; ++i) Py_XDECREF(outs[i]);
+    return ret;
     MVLA_CATCH
 }
 
@@ -555,9 +577,9 @@ PyObject* py_window_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
     int32_t rc = mvla_window_attention_workspace(ctx, s.n, s.ptr, &r, &bytes);
     if (rc != MVLA_OK) return Py_BuildValue("(iO)", rc, Py_None);
     at::Tensor ws, fresh;
-    if (bytes > 0) ws = scratch(bytes, c.device, st);
+    if (bytes > 0) ws = fresh_on({bytes}, at::kByte, c.device, a[19], st);
     if (!to) {
-        fresh = scratch(tq->numel() * (c.wide == at::kFloat ? 4 : 2), c.device, st).view(c.wide).view(tq->sizes());
+        fresh = fresh_on(tq->sizes(), c.wide, c.device, a[19], st);
         out = fresh.data_ptr();
     }
     r.out = out;
@@ -614,7 +636,7 @@ PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n)
     int64_t bytes = 0;
     const int32_t rc = mvla_cache_evict_workspace(ctx, s.n, s.ptr, &r, &bytes);
     if (rc != MVLA_OK) return PyLong_FromLong(rc);
-    const at::Tensor ws = scratch(bytes, c.device, st);
+    const at::Tensor ws = fresh_on({bytes}, at::kByte, c.device, a[18], st);
     r.workspace = ws.data_ptr();
     r.workspace_bytes = bytes;
     return PyLong_FromLong(unlocked([&] { return mvla_cache_evict(ctx, s.n, s.ptr, &r, st); }));

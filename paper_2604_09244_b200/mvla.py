@@ -267,6 +267,7 @@ class PruneContext:
                           max_3d, n_prune_points, n_state_slots, window_k, cold_start_full_keep,
                           salience_path, tau_2d, tau_3d, beta, eps_3d, floor_ratio, obj_2d_min, patch_path,
                           kmeans_max_iter, n_kv_heads, logit_cache, 0)
+        self._shape = (code, n_heads, n_kv_heads or n_heads, head_dim, int(device))      # what the calls around the prune point check by
         rc = self._lib.mvla_prune_create(C.byref(self.cfg), C.byref(self._h))
         if rc != OK:
             self._h = C.c_void_p()
@@ -407,10 +408,6 @@ class PruneContext:
         return out
 
     # -- around the prune point (`seqs`: a ctypes array from c_seqs, or Seq objects) ------------------------------------------
-    def _shape(self):
-        c = self.cfg
-        return c.dtype, c.n_heads, c.n_kv_heads or c.n_heads, c.head_dim, c.device
-
     def qk_norm_rope(self, q, k, pos, inv_freq, *, v=None, q_weight=None, k_weight=None, norm=True, eps=1e-6, interleaved=False,
                      q_out=None, k_out=None, v_out=None, out_rows=None, stream=None):
         """Norms of queries and keys for each head and the position rotation (``mvla_qk_norm_rope``); `v` rows are copied along.
@@ -419,17 +416,9 @@ class PruneContext:
         inv_freq: float64 [rot_dim / 2] (None: no rotation).  k_out / v_out: packed rows, or a cache of which row i of the call
         becomes row out_rows[i] (a row outside the cache is dropped).  Outputs that are not given are allocated; returned as
         (q_out, k_out, v_out)."""
-        def out(src, dst):
-            if src is None or dst is not None:
-                return dst
-            if src is not q and out_rows is not None:
-                raise ValueError("out_rows: rows of a k_out / v_out that is given")
-            with torch.cuda.stream(stream):
-                return torch.empty(src.shape, dtype=self.torch_dtype, device=self.device)
-        q_out, k_out, v_out = out(q, q_out), out(k, k_out), out(v, v_out)
         flags = (ROPE_NORM if norm else 0) | (ROPE_INTERLEAVED if interleaved else 0)
-        rc = self._nat.qk_norm_rope(self._h.value or 0, *self._shape(), q, k, v, pos, inv_freq, q_weight, k_weight, flags, eps,
-                                    q_out, k_out, v_out, out_rows, stream)
+        rc, q_out, k_out, v_out = self._nat.qk_norm_rope(self._h.value or 0, *self._shape, q, k, v, pos, inv_freq, q_weight, k_weight, flags,
+                                                         eps, q_out, k_out, v_out, out_rows, stream)
         if rc != OK:
             raise MvlaError(rc, "mvla_qk_norm_rope")
         return q_out, k_out, v_out
@@ -441,7 +430,7 @@ class PruneContext:
         (float32 [rows, heads]) written.  Returns `out` (allocated where it is not given: rows outside the sequences then
         hold anything)."""
         cs = seqs if isinstance(seqs, C.Array) else c_seqs(seqs)
-        rc, out = self._nat.window_attention(self._h.value or 0, *self._shape(), cs, q, k, v, WINDOW_ALL if window is None else window,
+        rc, out = self._nat.window_attention(self._h.value or 0, *self._shape, cs, q, k, v, WINDOW_ALL if window is None else window,
                                              n_sink, scale, q_pos, kv_pos, kv_len, out, lse, mass, stream)
         if rc != OK:
             raise MvlaError(rc, "mvla_window_attention")
@@ -452,7 +441,7 @@ class PruneContext:
         """Keeps the `budget` rows of every sequence that matter most by accumulated attention weight, in front of its run, in
         place (``mvla_cache_evict``).  pos and mass are rewritten too unless pos_out / mass_out are given."""
         cs = seqs if isinstance(seqs, C.Array) else c_seqs(seqs)
-        rc = self._nat.cache_evict(self._h.value or 0, *self._shape(), cs, k, v, pos, mass, pos if pos_out is None else pos_out,
+        rc = self._nat.cache_evict(self._h.value or 0, *self._shape, cs, k, v, pos, mass, pos if pos_out is None else pos_out,
                                    mass if mass_out is None else mass_out, kept_idx, kv_len, kv_len_out, n_sink, n_recent, stream)
         if rc != OK:
             raise MvlaError(rc, "mvla_cache_evict")
