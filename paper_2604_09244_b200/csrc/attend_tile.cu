@@ -13,6 +13,7 @@
 // Positions that are counted tell every warp which tiles to visit and which need their mask; where they are data, a list of the
 // tiles is made first.  Rows that nobody may look at have their values set to zero in shared memory (0 times NaN is NaN).
 #include "attend.cuh"
+#include "f32x2.cuh"
 #include "tmem_ld.cuh"
 #include "tmem_plan.h"
 #include "tmem_st.cuh"
@@ -69,27 +70,6 @@ __device__ __forceinline__ uint32_t two_bf16(float lo, float hi)
 __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x)
 {
     *reinterpret_cast<uint4*>(p) = make_uint4(two_bf16(x[0], x[1]), two_bf16(x[2], x[3]), two_bf16(x[4], x[5]), two_bf16(x[6], x[7]));
-}
-
-// Two fp32 operations in one instruction.
-__device__ __forceinline__ uint64_t two_f32(float lo, float hi)
-{
-    uint64_t v;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
-    return v;
-}
-__device__ __forceinline__ void split_f32(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
-__device__ __forceinline__ uint64_t fma_f32x2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t d;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
-    return d;
-}
-__device__ __forceinline__ uint64_t add_f32x2(uint64_t a, uint64_t b)
-{
-    uint64_t d;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
-    return d;
 }
 
 // The lowest n of 32 bits (all of them from 32 on, none below 1).
