@@ -99,8 +99,17 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
     }
     if (c.dtype == MVLA_DTYPE_FP32) {
         p.rows = most_rows <= 8 ? 8 : 32;
-        p.mass_parts = c.kv_heads;
-        for (int b = 0; b < batch; ++b) p.blocks += (static_cast<int64_t>(seqs[b].n_q) * group + p.rows - 1) / p.rows;
+        int64_t row_blocks = 0, key_tiles = 0;
+        for (int b = 0; b < batch; ++b) {
+            p.blocks += (static_cast<int64_t>(seqs[b].n_q) * group + p.rows - 1) / p.rows;
+            row_blocks += (static_cast<int64_t>(seqs[b].n_q) * group + 31) / 32;
+            key_tiles += (static_cast<int64_t>(seqs[b].n_kv) + 63) / 64;
+        }
+        // weights: enough CTAs (64 keys of a head each) for every multiprocessor eight times, since the first keys have the most rows to
+        // go through, of at least two blocks of 32 rows on average
+        int64_t runs = key_tiles == 0 ? 1 : 8 * static_cast<int64_t>(c.sm_count) / (key_tiles * c.kv_heads);
+        runs = runs > row_blocks / 2 ? row_blocks / 2 : runs;
+        p.mass_parts = static_cast<int32_t>(c.kv_heads * (runs < 1 ? 1 : runs));
         if (p.blocks > 0) {
             // enough CTAs for every multiprocessor twice, of at least four tiles of 64 keys
             const int64_t ctas = p.blocks * c.kv_heads;

@@ -56,10 +56,10 @@ struct AttArgs {
     AttSeq s[kMaxBatch];
 };
 
-// By FMAs in 32 bits: any shape, in blocks of `rows` (8 or 32) query rows.
-cudaError_t launch_attend_fma(int dtype, const AttArgs& a, int rows, cudaStream_t stream);
+// fp32, by FMAs: any shape, in blocks of `rows` (8 or 32) query rows.
+cudaError_t launch_attend_fma(const AttArgs& a, int rows, cudaStream_t stream);
 // The weights of every cached row over the queries of its sequence, by key head, into part_mass (by FMAs in 32 bits).
-cudaError_t launch_mass_fma(int dtype, const AttArgs& a, cudaStream_t stream);
+cudaError_t launch_mass_fma(const AttArgs& a, cudaStream_t stream);
 // bf16 (f16: what launch_widen made) by tiles of 128 rows on the tensor cores; at most kMaxTiles tiles of keys to a split.
 struct AttMaps {
     CUtensorMap q, k, v;

@@ -142,9 +142,9 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
         if (e == cudaSuccess && (plan.splits > 1 || a->mass)) e = launch_attend_finish(k, st);
         return close_call(ctx, e);
     } else {
-        e = launch_attend_fma(v.dtype, k, plan.rows, st);
+        e = launch_attend_fma(k, plan.rows, st);
         if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);
-        if (e == cudaSuccess && a->mass) e = launch_mass_fma(v.dtype, k, st);
+        if (e == cudaSuccess && a->mass) e = launch_mass_fma(k, st);
     }
     if (e == cudaSuccess && a->mass) e = launch_mass_add(k, st);
     return close_call(ctx, e);
