@@ -7,9 +7,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-constexpr int kFewParts = 8;                 // up to here a warp joins the parts of a (query, head), beyond a CTA does
+// Up to so many parts a warp joins those of a (query, head), beyond a CTA does.  Tokens of 16 requests over 500 to 4000 e4m3 rows, 1 to 8 parts:
+// 31.5 us so, 35.4 with CTAs; one token over 800 rows of 32 heads 11.6, with CTAs 11.1; 131072 rows, a hundred parts and more: CTAs.
+constexpr int kFewParts = 8;
 constexpr int kMassKeys = 128;               // keys of a CTA (AttSeq::tile0 counts such tiles)
 constexpr int kRowGroups = kThreads / kMassKeys;
+constexpr int kFinishRows = 4 * kWarps;      // rows (queries and heads) whose scores are added up at a time: eight lanes to a row's parts
 
 __device__ __forceinline__ void store_two(float* p, float x, float y) { *reinterpret_cast<float2*>(p) = make_float2(x, y); }
 __device__ __forceinline__ void store_two(__nv_bfloat16* p, float x, float y) { *reinterpret_cast<__nv_bfloat162*>(p) = __floats2bfloat162_rn(x, y); }
@@ -41,14 +44,22 @@ __device__ __forceinline__ void write_sums(const AttArgs& a, int64_t row, int64_
     if (a.lse2) a.lse2[unit] = z;
 }
 
-// Few parts: a warp joins those of one (query, head), two neighbouring elements of the head to a lane at a time.  Bound by the parts' bytes.
-template <class TOut>
-__global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_constant__ AttArgs a)
+// x += elements c .. c + 3 of a part's sums, taken to the common reference.
+__device__ __forceinline__ void add_part(const AttArgs& a, int64_t part, int c, float ref, float4& x)
 {
-    pdl_wait();
-    pdl_trigger();
+    const float f = exp2f(a.part_ml[part].x - ref);
+    const float4 o = *reinterpret_cast<const float4*>(a.part_o + part * a.head_dim + c);
+    x.x = fmaf(o.x, f, x.x);
+    x.y = fmaf(o.y, f, x.y);
+    x.z = fmaf(o.z, f, x.z);
+    x.w = fmaf(o.w, f, x.w);
+}
+
+// Few parts: a warp joins those of one (query, head), four neighbouring elements of the head to a lane at a time.  Bound by the parts' bytes.
+template <class TOut>
+__device__ __forceinline__ void join_by_warp(const AttArgs& a, int64_t unit)
+{
     const int lane = threadIdx.x & 31;
-    const int64_t unit = static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5);
     if (unit >= static_cast<int64_t>(a.total_q) * a.n_heads) return;
     const int qp = static_cast<int>(unit / a.n_heads), h = static_cast<int>(unit % a.n_heads);
     const AttSeq& s = a.s[seq_of_query(a, qp)];
@@ -56,15 +67,13 @@ __global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_cons
     const int64_t row = s.q_row + (qp - s.qp0), step = static_cast<int64_t>(s.n_q) * a.n_heads, first = (s.part0 + (qp - s.qp0)) * a.n_heads + h;
     const float2 ml = parts_sum<32>(a, first, step, s.parts, lane);
     const float ref = ml.x == -CUDART_INF_F ? 0.f : ml.x, inv = ml.y > 0.f ? 1.f / ml.y : 0.f;
-    for (int c = 2 * lane; c < a.head_dim; c += 64) {
-        float x = 0.f, y = 0.f;
-        for (int p = 0; p < s.parts; ++p) {
-            const float f = exp2f(a.part_ml[first + p * step].x - ref);
-            const float2 o = *reinterpret_cast<const float2*>(a.part_o + (first + p * step) * a.head_dim + c);
-            x = fmaf(o.x, f, x);
-            y = fmaf(o.y, f, y);
-        }
-        store_two(static_cast<TOut*>(a.out) + (row * a.n_heads + h) * a.head_dim + c, x * inv, y * inv);
+    for (int c = 4 * lane; c < a.head_dim; c += 128) {
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
+        for (int p = 0; p < s.parts; ++p) add_part(a, first + p * step, c, ref, x);
+        TOut* const out = static_cast<TOut*>(a.out) + (row * a.n_heads + h) * a.head_dim + c;
+        store_two(out, x.x * inv, x.y * inv);
+        store_two(out + 2, x.z * inv, x.w * inv);
     }
     if (lane == 0) write_sums(a, row, unit, h, ml);
 }
@@ -84,14 +93,7 @@ __device__ __forceinline__ void join_by_cta(const AttArgs& a, int64_t unit)
     for (int c = 4 * lane; c < a.head_dim; c += 128) {
         float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-        for (int p = warp; p < s.parts; p += kWarps) {
-            const float f = exp2f(a.part_ml[first + p * step].x - ref);
-            const float4 o = *reinterpret_cast<const float4*>(a.part_o + (first + p * step) * a.head_dim + c);
-            x.x = fmaf(o.x, f, x.x);
-            x.y = fmaf(o.y, f, x.y);
-            x.z = fmaf(o.z, f, x.z);
-            x.w = fmaf(o.w, f, x.w);
-        }
+        for (int p = warp; p < s.parts; p += kWarps) add_part(a, first + p * step, c, ref, x);
         *reinterpret_cast<float4*>(&sums[warp][c]) = x;
     }
     __syncthreads();
@@ -102,6 +104,14 @@ __device__ __forceinline__ void join_by_cta(const AttArgs& a, int64_t unit)
         store_two(static_cast<TOut*>(a.out) + (row * a.n_heads + h) * a.head_dim + c, x * inv, y * inv);
     }
     if (threadIdx.x == 0) write_sums(a, row, unit, h, ml);
+}
+
+template <class TOut>
+__global__ void __launch_bounds__(kThreads) attend_join_kernel(const __grid_constant__ AttArgs a)
+{
+    pdl_wait();
+    pdl_trigger();
+    join_by_warp<TOut>(a, static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5));
 }
 
 template <class TOut>
@@ -116,11 +126,12 @@ __global__ void __launch_bounds__(kThreads) attend_join_cta_kernel(const __grid_
 // weights and add them up, queries and heads in their order (two threads to a key, every second row each).
 __global__ void __launch_bounds__(kThreads) attend_finish_kernel(const __grid_constant__ AttArgs a, int joins)
 {
-    __shared__ float row_z[kThreads], half[kMassKeys];
+    __shared__ float row_z[2][kFinishRows], half[kMassKeys];
     pdl_wait();
     pdl_trigger();
     if (static_cast<int>(blockIdx.x) < joins) {
-        join_by_cta<__nv_bfloat16>(a, blockIdx.x);
+        if (a.splits > kFewParts) join_by_cta<__nv_bfloat16>(a, blockIdx.x);
+        else join_by_warp<__nv_bfloat16>(a, static_cast<int64_t>(blockIdx.x) * kWarps + (threadIdx.x >> 5));
         return;
     }
     const int tile = static_cast<int>(blockIdx.x) - joins, t = threadIdx.x, lane = t & 31, warp = t >> 5;
@@ -141,19 +152,21 @@ __global__ void __launch_bounds__(kThreads) attend_finish_kernel(const __grid_co
     const int rows = s.n_q * a.n_heads;
     const float* const x = a.logits + s.logit0 + j;
     float sum = 0.f;
-    for (int r0 = 0; r0 < rows; r0 += kThreads) {
-        const int n = min(kThreads, rows - r0);
-        __syncthreads();
-        for (int r = warp * 4; r < n; r += kWarps * 4) {     // the logarithm of a row's sum by eight lanes
-            const int mine = r0 + min(r + (lane >> 3), n - 1);
+    for (int r0 = 0, buf = 0; r0 < rows; r0 += kFinishRows, buf ^= 1) {
+        float y[kFinishRows / kRowGroups];                   // the scores, on their way with the parts' sums
+#pragma unroll
+        for (int i = 0; i < kFinishRows / kRowGroups; ++i) {
+            const int r = r0 + group + i * kRowGroups;
+            y[i] = seen && r < rows ? x[static_cast<int64_t>(r) * s.n_kv] : -CUDART_INF_F;
+        }
+        {                                                    // the logarithm of a row's sum by eight lanes
+            const int r = warp * 4 + (lane >> 3), mine = min(r0 + r, rows - 1);
             const float2 ml = parts_sum<8>(a, s.part0 * a.n_heads + mine, rows, s.parts, lane & 7);
-            if ((lane & 7) == 0 && r + (lane >> 3) < n) row_z[r + (lane >> 3)] = ml.y > 0.f ? ml.x + log2f(ml.y) : 0.f;
+            if ((lane & 7) == 0) row_z[buf][r] = ml.y > 0.f ? ml.x + log2f(ml.y) : 0.f;
         }
-        __syncthreads();
-        if (seen) {
-#pragma unroll 8
-            for (int r = group; r < n; r += kRowGroups) sum += exp2f(x[static_cast<int64_t>(r0 + r) * s.n_kv] - row_z[r]);      // (2^-inf is 0)
-        }
+        __syncthreads();                                     // (and nobody is with the buffer that is written next)
+#pragma unroll
+        for (int i = 0; i < kFinishRows / kRowGroups; ++i) sum += exp2f(y[i] - row_z[buf][group + i * kRowGroups]);      // (2^-inf is 0)
     }
     if (group == 1) half[t % kMassKeys] = sum;
     __syncthreads();
@@ -205,7 +218,8 @@ cudaError_t launch_attend_join(int dtype, const AttArgs& a, cudaStream_t stream)
 
 cudaError_t launch_attend_finish(const AttArgs& a, cudaStream_t stream)
 {
-    const int64_t joins = a.splits > 1 ? static_cast<int64_t>(a.total_q) * a.n_heads : 0;
+    const int64_t units = a.splits > 1 ? static_cast<int64_t>(a.total_q) * a.n_heads : 0;
+    const int64_t joins = a.splits > kFewParts ? units : (units + kWarps - 1) / kWarps;
     const AttSeq& last = a.s[a.n_seq - 1];
     const int64_t tiles = a.mass ? last.tile0 + (last.n_kv + kMassKeys - 1) / kMassKeys : 0;
     return launch(attend_finish_kernel, joins + tiles, stream, a, static_cast<int>(joins));

@@ -146,13 +146,6 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
     const int t = threadIdx.x, lane = t & 31, warp = t >> 5, g = lane >> 2, c = lane & 3;
     const AttSeq& s = a.s[seq_of_block(a, blockIdx.x)];
     const int hk = blockIdx.y, group = a.n_heads / a.kv_heads, n_rows = s.n_q * group, len = seq_len(a, s);
-    const T* const q = static_cast<const T*>(a.q);
-    for (int u = t; u < D32 * NR * 32; u += kWarps * 32) {
-        const int piece = u / (NR * 32), n = u / 32 % NR, l = u & 31, r = (l >> 2) + 8 * n;
-        typename K::Run w = {};
-        if (r < n_rows) w = *reinterpret_cast<const typename K::Run*>(q + ((s.q_row + r / group) * a.n_heads + hk * group + r % group) * D + Sh::element(piece, l & 3));
-        q_frag[piece][n][l] = w;
-    }
     int p[NR][2], lo = 0x7FFFFFFF, hi = -1;                  // positions of this lane's rows 8 n + 2 c + e, and the span of all rows
 #pragma unroll
     for (int n = 0; n < NR; ++n)
@@ -164,7 +157,6 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
         }
     lo = __reduce_min_sync(0xffffffffu, lo);
     hi = __reduce_max_sync(0xffffffffu, hi);
-    __syncthreads();
     const TileRange range = tile_range(a, len, lo, hi, Sh::kKeys);
     const int part = static_cast<int>(blockIdx.x) - s.blk0, per_part = (range.count + s.parts - 1) / s.parts;
     const int t0 = part * per_part, t1 = min(range.count, t0 + per_part);
@@ -225,6 +217,14 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
     for (int u = 0; u < kStages - 1; ++u) ahead[u] = pos_of(u);
 #pragma unroll
     for (int u = 0; u < kStages - 1; ++u) fetch(u, u, ahead[u]);
+    const T* const q = static_cast<const T*>(a.q);
+    for (int u = t; u < D32 * NR * 32; u += kWarps * 32) {
+        const int piece = u / (NR * 32), n = u / 32 % NR, l = u & 31, r = (l >> 2) + 8 * n;
+        typename K::Run w = {};
+        if (r < n_rows) w = *reinterpret_cast<const typename K::Run*>(q + ((s.q_row + r / group) * a.n_heads + hk * group + r % group) * D + Sh::element(piece, l & 3));
+        q_frag[piece][n][l] = w;
+    }
+    __syncthreads();
     int next = pos_of(kStages - 1), stage = 0;
     for (int u = 0; u < mine; ++u, stage = stage + 1 < kStages ? stage + 1 : 0) {
         const int then = pos_of(u + kStages);
