@@ -7,9 +7,15 @@
 // evict_select_kernel: a cluster of one to eight CTAs a sequence, by its length; a CTA has a run of its rows.  Every row has a 32-bit key
 // (its weight's bits in order of size; protected rows above all, hidden rows below all); three rounds of 2048-bin counts over the keys, most
 // significant bits first (sign, exponent and two bits of the fraction, so that weights of one size spread over bins), give the key of the
-// last row that stays and how many of its equals do: every CTA adds up the cluster's counts for itself, out of the others' shared memory.  Then every warp walks a run of rows in ascending order and counts, and once more to write.
-// Keys are kept in shared memory where they fit.  Bound by the latency of its passes.
+// last row that stays and how many of its equals do.  A round looks for its bin in two steps, sums of 64 bins and then the 64 of one sum, so
+// that little is read out of the other CTAs' shared memory; every CTA does so for itself.  Then every warp walks a run of rows in
+// ascending order and counts, keeps a bit for each row that stays, and goes over the bits once more to write.
+// Keys are kept in shared memory where they fit.  Bound by the latency of its passes: a barrier of the cluster is about 0.8 us.
 // evict_move_kernel: one warp a 2 KB piece of a moved row.  Bound by bytes.
+//
+// B200: 16 sequences one row over their budgets (one kernel) 8.3 us; 16 of 784 to 832 rows of 32 + 32 heads of 128 cut to three tenths 25 us, of it
+// 16 the move's 88 MB; 65537 rows of 8 + 8 heads cut to an eighth 37 us, of it 11 the move (with one CTA 300; reading all bins of all
+// CTAs, and taking the keys apart again for the second walk, 46).  Equal bins of a warp counted together: 54 (the atomics are not what it waits for).
 #include "device_utils.cuh"
 #include "serve.h"
 
@@ -31,12 +37,11 @@ __device__ __forceinline__ int seq_rows(const EvictArgs& a, const EvictSeq& s)
 {
     return a.kv_len ? min(max(a.kv_len[s.index], 0), s.n_kv) : s.n_kv;
 }
-__device__ __forceinline__ uint32_t key_of(const EvictArgs& a, const EvictSeq& s, int j, int last)
+// Key of a row at position c whose weight is w; `last`: the largest position of its sequence.
+__device__ __forceinline__ uint32_t key_of(const EvictArgs& a, int c, float w, int last)
 {
-    const int c = a.pos[s.kv_row + j];
     if (c < 0) return 0u;
     if (c < a.n_sink || last - c < a.n_recent) return 0xFFFFFFFFu;
-    const float w = a.mass[s.kv_row + j];
     if (w != w) return 1u;                                    // NaN: below every number
     const uint32_t u = __float_as_uint(w + 0.f);              // (-0 is 0)
     return u & 0x80000000u ? ~u : u | 0x80000000u;            // (from 0x007FFFFF, -infinity, to 0xFF800000, +infinity)
@@ -82,6 +87,17 @@ __device__ __forceinline__ void cluster_sync()
     cluster_arrive_release();
     cluster_wait_acquire();
 }
+// Inclusive sum over the lanes.
+__device__ __forceinline__ int sum_upto(int x)
+{
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) {
+        const int y = __shfl_up_sync(0xffffffffu, x, o);
+        if (lane >= o) x += y;
+    }
+    return x;
+}
 // Exclusive sum over the CTA's warps of one value per warp (the same in all its lanes), and the total.
 __device__ __forceinline__ int warps_before(int v, int* red, int* total)
 {
@@ -89,13 +105,7 @@ __device__ __forceinline__ int warps_before(int v, int* red, int* total)
     __syncthreads();
     if (lane == 0) red[warp] = v;
     __syncthreads();
-    int x = red[lane];
-    const int mine = x;
-#pragma unroll
-    for (int o = 1; o < 32; o *= 2) {
-        const int y = __shfl_up_sync(0xffffffffu, x, o);
-        if (lane >= o) x += y;
-    }
+    const int mine = red[lane], x = sum_upto(mine);
     *total = __shfl_sync(0xffffffffu, x, 31);
     return __shfl_sync(0xffffffffu, x - mine, warp);
 }
@@ -105,7 +115,8 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
     extern __shared__ uint32_t cached[];
     __shared__ __align__(8) int hist[2][kBins];
     __shared__ int red[kWarps];
-    __shared__ int found[2], slots[3];
+    __shared__ __align__(8) int slots[4];
+    __shared__ int coarse[2][kWarps], found[2];
     uint32_t n_ranks;
     asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(n_ranks));
     const uint32_t rank = cluster_ctarank();
@@ -130,21 +141,24 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
         }
         return;
     }
+    const bool fits = r1 - r0 <= kKeysInSmem;
     int last = -1;
 #pragma unroll 4
-    for (int j = r0 + t; j < r1; j += kThreads) last = max(last, a.pos[row + j]);
+    for (int j = r0 + t; j < r1; j += kThreads) {             // (the weights on their way together with the positions)
+        last = max(last, a.pos[row + j]);
+        if (fits) cached[j - r0] = __float_as_uint(a.mass[row + j]);
+    }
     last = block_max(last, red);
     hist[0][t] = hist[0][t + kThreads] = 0;
     if (n_ranks > 1) {
         if (t == 0) slots[0] = last;
         cluster_sync();
-        for (uint32_t r = 0; r < n_ranks; ++r) last = max(last, ld_peer(&slots[0], r));
+        last = __reduce_max_sync(0xffffffffu, lane < static_cast<int>(n_ranks) ? ld_peer(&slots[0], lane) : -1);
     }
-    const bool fits = r1 - r0 <= kKeysInSmem;
-    const auto key_at = [&](int j) { return fits ? cached[j - r0] : key_of(a, s, j, last); };
+    const auto key_at = [&](int j) { return fits ? cached[j - r0] : key_of(a, a.pos[row + j], a.mass[row + j], last); };
     if (fits) {
 #pragma unroll 4
-        for (int j = r0 + t; j < r1; j += kThreads) cached[j - r0] = key_of(a, s, j, last);
+        for (int j = r0 + t; j < r1; j += kThreads) cached[j - r0] = key_of(a, a.pos[row + j], __uint_as_float(cached[j - r0]), last);
     }
     // The key of the m-th row in descending order, eleven, eleven and ten bits; `left`: rows still to be found among those with the bits so far.
     uint32_t prefix = 0;
@@ -161,41 +175,46 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
             if ((k & above) == prefix) atomicAdd(&mine[(k >> shift) & bins], 1);
         }
         __syncthreads();
+        {                                                     // 64 bins a warp
+            const int2 c = *reinterpret_cast<const int2*>(&mine[64 * warp + 2 * lane]);
+            const int sum = __reduce_add_sync(0xffffffffu, c.x + c.y);
+            if (lane == 0) coarse[round & 1][warp] = sum;
+        }
         if (n_ranks > 1) cluster_sync();
+        else __syncthreads();
         // (the other buffer was read by everybody before this barrier)
         hist[(round + 1) & 1][t] = hist[(round + 1) & 1][t + kThreads] = 0;
-        // two bins a thread, from the top
-        const int top = kBins - 1 - 2 * t;
-        int c0 = 0, c1 = 0;
-        if (n_ranks == 1) {
-            c0 = mine[top];
-            c1 = mine[top - 1];
-        } else {
-            int2 c[kMaxCluster];                              // (all on their way at once, each CTA beginning with another)
+        if (warp == 0) {
+            // from the top: the 64 bins among which the row is found, then the bin; the cluster's counts all on their way at once
+            int c = 0;
 #pragma unroll
-            for (uint32_t i = 0; i < kMaxCluster; ++i) c[i] = i < n_ranks ? ld_peer2(&mine[top - 1], (i + rank) & (n_ranks - 1)) : make_int2(0, 0);
+            for (uint32_t i = 0; i < kMaxCluster; ++i) c += i < n_ranks ? ld_peer(&coarse[round & 1][31 - lane], (i + rank) & (n_ranks - 1)) : 0;
+            int upto = sum_upto(c);
+            unsigned hit = __ballot_sync(0xffffffffu, upto >= left) | 1u << 31;
+            const int at = __ffs(hit) - 1, base = 64 * (31 - at);
+            left -= __shfl_sync(0xffffffffu, upto - c, at);
+            int c0 = 0, c1 = 0;
 #pragma unroll
-            for (uint32_t i = 0; i < kMaxCluster; ++i) { c0 += c[i].y; c1 += c[i].x; }
-        }
-        int upto = c0 + c1;
-#pragma unroll
-        for (int o = 1; o < 32; o *= 2) {
-            const int y = __shfl_up_sync(0xffffffffu, upto, o);
-            if (lane >= o) upto += y;
-        }
-        int all;
-        const int before = warps_before(__shfl_sync(0xffffffffu, upto, 31), red, &all) + upto - c0 - c1;
-        if (before < left && left <= before + c0 + c1) {      // (one thread of the CTA)
-            const bool second = left > before + c0;
-            found[0] = second ? top - 1 : top;
-            found[1] = left - before - (second ? c0 : 0);
+            for (uint32_t i = 0; i < kMaxCluster; ++i) {
+                const int2 x = i < n_ranks ? ld_peer2(&mine[base + 62 - 2 * lane], (i + rank) & (n_ranks - 1)) : make_int2(0, 0);
+                c0 += x.y;
+                c1 += x.x;
+            }
+            upto = sum_upto(c0 + c1);
+            hit = __ballot_sync(0xffffffffu, upto >= left) | 1u << 31;
+            if (lane == __ffs(hit) - 1) {
+                const int rest = left - (upto - c0 - c1);
+                const bool second = rest > c0;
+                found[0] = base + 63 - 2 * lane - (second ? 1 : 0);
+                found[1] = rest - (second ? c0 : 0);
+            }
         }
         __syncthreads();
         prefix |= static_cast<uint32_t>(found[0]) << shift;
         left = found[1];
         if (round == 2) {
             equal_here = mine[found[0]];
-            for (uint32_t r = 0; r < rank; ++r) equal_before += ld_peer(&mine[found[0]], r);
+            equal_before = __reduce_add_sync(0xffffffffu, lane < static_cast<int>(rank) ? ld_peer(&mine[found[0]], lane) : 0);
         }
     }
     // Rows with a larger key stay, and the first `left` of those with this one.  A warp has a run of rows.
@@ -207,16 +226,24 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
         equal_before += warps_before(equal, red, &total);
     }
     const auto kept_of = [&](int j0, int& seen) {             // which of 32 rows stay; `seen`: equals so far
-        const uint32_t k = j0 + lane < end ? key_at(j0 + lane) : 0u;
-        const unsigned eq = __ballot_sync(0xffffffffu, j0 + lane < end && k == prefix);
-        const bool stays = j0 + lane < end && (k > prefix || (k == prefix && seen + __popc(eq & ((1u << lane) - 1u)) < left));
-        seen += __popc(eq);
-        return __ballot_sync(0xffffffffu, stays);
+        const bool there = j0 + lane < end;
+        const uint32_t k = there ? key_at(j0 + lane) : 0u;
+        const unsigned eq = __ballot_sync(0xffffffffu, there && k == prefix);
+        unsigned stay = __ballot_sync(0xffffffffu, there && k > prefix);
+        if (eq) {
+            stay |= __ballot_sync(0xffffffffu, there && k == prefix && seen + __popc(eq & ((1u << lane) - 1u)) < left);
+            seen += __popc(eq);
+        }
+        return stay;
     };
+    // (kept for the second walk where the keys are kept too: the bins of the second round are read by nobody any more)
+    uint32_t* const staying = reinterpret_cast<uint32_t*>(hist[1]);
+    static_assert(kKeysInSmem / 32 <= kBins, "a bit for every key");
     // holes: rows below m that go; moved: rows from m on that stay.  There are as many of one as of the other.
     int holes = 0, moved = 0;
     for (int j0 = first, seen = equal_before; j0 < end; j0 += 32) {
         const unsigned stay = kept_of(j0, seen);
+        if (fits && lane == 0) staying[(j0 - r0) / 32] = stay;
         const unsigned below = j0 >= m ? 0u : j0 + 32 <= m ? 0xffffffffu : (1u << (m - j0)) - 1u;
         const unsigned there = end - j0 >= 32 ? 0xffffffffu : (1u << (end - j0)) - 1u;
         holes += __popc(~stay & below & there);
@@ -225,25 +252,24 @@ __global__ void __launch_bounds__(kThreads) evict_select_kernel(const __grid_con
     int holes_here, n_moves;
     int hole_at = warps_before(holes, red, &holes_here), moved_at = warps_before(moved, red, &n_moves);
     if (n_ranks > 1) {
-        if (t == 0) { slots[1] = holes_here; slots[2] = n_moves; }
+        if (t == 0) { slots[2] = holes_here; slots[3] = n_moves; }
         cluster_sync();
-        n_moves = 0;
-        for (uint32_t r = 0; r < n_ranks; ++r) {
-            const int moved_there = ld_peer(&slots[2], r);
-            n_moves += moved_there;
-            if (r < rank) { hole_at += ld_peer(&slots[1], r); moved_at += moved_there; }
-        }
+        const int2 x = lane < static_cast<int>(n_ranks) ? ld_peer2(&slots[2], lane) : make_int2(0, 0);
+        n_moves = __reduce_add_sync(0xffffffffu, x.y);
+        hole_at += __reduce_add_sync(0xffffffffu, lane < static_cast<int>(rank) ? x.x : 0);
+        moved_at += __reduce_add_sync(0xffffffffu, lane < static_cast<int>(rank) ? x.y : 0);
     }
     int2* const moves = a.moves + s.move0;
+    const bool copies = a.pos_out != a.pos || a.mass_out != a.mass || a.kept_idx;
     for (int j0 = first, seen = equal_before; j0 < end; j0 += 32) {
-        const unsigned stay = kept_of(j0, seen);
+        const unsigned stay = fits ? staying[(j0 - r0) / 32] : kept_of(j0, seen);
         const int j = j0 + lane;
         const unsigned below = j0 >= m ? 0u : j0 + 32 <= m ? 0xffffffffu : (1u << (m - j0)) - 1u;
         const unsigned there = end - j0 >= 32 ? 0xffffffffu : (1u << (end - j0)) - 1u;
         const unsigned hole = ~stay & below & there, from = stay & ~below, bit = 1u << lane, lower = bit - 1u;
         if (hole & bit) moves[hole_at + __popc(hole & lower)].y = j;
         if (from & bit) moves[moved_at + __popc(from & lower)].x = j;
-        if (stay & below & bit) {
+        if (copies && (stay & below & bit)) {
             if (a.pos_out != a.pos) a.pos_out[row + j] = a.pos[row + j];
             if (a.mass_out != a.mass) a.mass_out[row + j] = a.mass[row + j];
             if (a.kept_idx) a.kept_idx[row + j] = j;
