@@ -466,8 +466,8 @@ typedef struct mvla_attention {
  * exponentials in 32 bits (16-bit types: weights are rounded to bf16 for their product with the values, e4m3: to fp16).  A query
  * that sees nothing: out 0, lse -infinity.  mass[j] += 1 / n_heads * sum over heads and queries of the weight of row j, in an order
  * that does not change from run to run.
- * What q, k and v hold must be finite in rows that some query of the sequence sees; rows behind a sequence's length and rows of
- * negative position may hold anything.  Rows of q, out and lse outside the sequences are left as they are.  Sequences must not
+ * What q, k and v hold must be finite in rows that some query of the sequence sees; cached rows that none sees (behind a sequence's
+ * length, of negative position, outside every window) may hold anything.  Rows of q, out and lse outside the sequences are left as they are.  Sequences must not
  * share query rows, nor cache rows where `mass` is given (INVALID_ARG); without it they may (a common prefix).  out, lse, mass and
  * the workspace must not overlap the inputs.  The workspace holds nothing between calls, but calls that may run at the same time
  * (two streams, two graphs) need one each.  Batches of up to max_batch sequences (CAPACITY).

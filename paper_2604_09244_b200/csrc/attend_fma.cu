@@ -113,12 +113,18 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
     const float* const k = static_cast<const float*>(a.k) + s.kv_row * stride + static_cast<int64_t>(hk) * d;
     const float* const v = static_cast<const float*>(a.v) + s.kv_row * stride + static_cast<int64_t>(hk) * d;
 
-    // The first tile from `it` on with a key that some row may see (t1: none), its positions in pos[buf]; a barrier of the CTA at least once.
+    // The first tile from `it` on with a key that some row sees (t1: none), its positions in pos[buf], -1 for keys that no row sees (what they hold
+    // is left out then); a barrier of the CTA at least once.
     const auto look = [&](int it) { return t < kTile && it < t1 ? key_pos(a, s, len, range.tile(it) * kTile + t) : -1; };
     const auto find = [&](int it, int c, int buf) {
         while (true) {
-            if (t < kTile) pos[buf][t] = c;
-            if (__syncthreads_or(some_sees(lo, hi, c, a.window, a.n_sink))) return it;
+            bool seen = some_sees(lo, hi, c, a.window, a.n_sink);
+            if (seen && a.q_pos) {                           // (queries may lie far apart)
+                seen = false;
+                for (int r = 0; r < n_rows && !seen; ++r) seen = sees(row_p[r], c, a.window, a.n_sink);
+            }
+            if (t < kTile) pos[buf][t] = seen ? c : -1;
+            if (__syncthreads_or(seen)) return it;
             if (it >= t1) return t1;
             c = look(++it);
         }

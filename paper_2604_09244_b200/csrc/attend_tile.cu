@@ -11,7 +11,7 @@
 // one's exponentials, prologue and epilogue lie beside the other's MMAs.  Measured on 8192 queries, 16 heads of 128 in groups of 4, and on
 // 16 x 808 queries of 32 heads, window 512: two tiles of rows in one CTA with tiles of 128 keys 295 / 250 us, this 291 / 189.
 // Positions that are counted tell every warp which tiles to visit and which need their mask; where they are data, a list of the
-// tiles is made first.  Rows that nobody may look at have their values set to zero in shared memory (0 times NaN is NaN).
+// tiles is made first.  Keys that no row of the tile sees have their values set to zero in shared memory (0 times NaN is NaN).
 #include "attend.cuh"
 #include "f32x2.cuh"
 #include "tmem_ld.cuh"
@@ -75,8 +75,8 @@ __device__ __forceinline__ void store8(__nv_bfloat16* p, const float* x)
 // The lowest n of 32 bits (all of them from 32 on, none below 1).
 __device__ __forceinline__ uint32_t below(int n) { return n >= 32 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << n) - 1u; }
 
-// What a tile of keys (or queries) is to a CTA: some row sees some key, not every row sees every key, some keys nobody may look at.
-constexpr int kNeed = 1, kMask = 2, kHidden = 4, kEntryShift = 3;       // an entry of a list: the tile's place in the range above the flags
+// What a tile of keys (or queries) is to a CTA: some row sees some key, not every row sees every key.
+constexpr int kNeed = 1, kMask = 2, kEntryShift = 2;         // an entry of a list: the tile's place in the range above the flags
 // Positions of `n` keys from row j0 on, by one warp: smallest and largest of those somebody may see, and whether there are others.
 struct Span {
     int lo, hi;
@@ -184,6 +184,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     __shared__ uint64_t bars[2 * kMaxStages + 7];
     __shared__ uint16_t list[kMaxTiles];
     __shared__ int key_at[kKeys];
+    __shared__ uint32_t seen_by[4][4][kKeys / 32];           // of the last tiles: the keys that some row of a warp sees
     __shared__ int n_list, dead;
     __shared__ uint32_t tmem_base;
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
@@ -225,7 +226,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     if (a.kv_pos) {
         for (int v = warp; v < n; v += Sh::kWarps) {
             const Span k = key_span(a, s, len, range.tile(v0 + v) * kKeys, kKeys, lane);
-            if (lane == 0) list[v] = static_cast<uint16_t>(span_flags(a, lo, hi, k) | (k.hidden ? kHidden : 0));
+            if (lane == 0) list[v] = static_cast<uint16_t>(span_flags(a, lo, hi, k));
         }
         __syncthreads();
         if (warp == 0) {
@@ -241,7 +242,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         if (a.kv_pos) return static_cast<int>(list[i]);
         const Span k = counted_span(len, j0, kKeys);
         const int f = span_flags(a, lo, hi, k);              // (queries far apart may leave out a tile between them: then no row sees a key)
-        return (f ? f : kMask) | (k.hidden ? kHidden : 0);
+        return f ? f : kMask;
     };
     Guard guard = {&dead, a.status};
 
@@ -306,17 +307,28 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             ok = ok && guard.wait_all(full(st), c / ST & 1);
             if (!ok) break;
             const int j0 = first_key(i);
-            if (flags_of(i, j0) & kHidden) {                 // values that nobody may look at become zero
-                for (int k = lane; k < kKeys; k += 32) {
-                    if (key_pos(a, s, len, j0 + k) >= 0) continue;
-                    for (int b = 0; b < DB; ++b)
-                        for (int x = 0; x < 8; ++x)
-                            asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(kv_at + st * Sh::kStage + b * kKeys * 128 + k * 128 + x * 16), "r"(0) : "memory");
+            if (flags_of(i, j0) & kMask) {
+                // values that no row sees become zero: counted queries lie side by side, so that their span says it, others have to be asked
+                uint32_t by[kKeys / 32] = {};
+                if (a.q_pos) {
+                    ok = guard.wait_all(p_full + 8 * (i & 1), i / 2 & 1);
+                    for (int w = 0; w < 4; ++w)
+#pragma unroll
+                        for (int x = 0; x < kKeys / 32; ++x) by[x] |= seen_by[i & 3][w][x];
                 }
-                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                bool some = false;
+#pragma unroll
+                for (int x = 0; x < kKeys / 32; ++x) {
+                    const int k = 32 * x + lane;
+                    if (a.q_pos ? by[x] >> lane & 1u : j0 + k < len && some_sees(lo, hi, j0 + k, a.window, a.n_sink)) continue;
+                    some = true;
+                    for (int c16 = 0; c16 < DB * 8; ++c16)
+                        asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(kv_at + st * Sh::kStage + c16 / 8 * kKeys * 128 + k * 128 + c16 % 8 * 16), "r"(0) : "memory");
+                }
+                if (some) asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
             }
-            ok = guard.wait_all(p_full + 8 * (i & 1), i / 2 & 1);
+            ok = ok && guard.wait_all(p_full + 8 * (i & 1), i / 2 & 1);
             if (ok && one) {
                 tc_fence_after();
                 for (int k = 0; k < kKeys / 16; ++k)
@@ -359,6 +371,13 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                     const int past = min(p, len - 1) - j0 + 1, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
 #pragma unroll
                     for (int w = 0; w < kKeys / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
+                }
+                if (a.q_pos) {                               // (those of three tiles ago were read before the last S was made)
+#pragma unroll
+                    for (int w = 0; w < kKeys / 32; ++w) {
+                        const uint32_t any = __reduce_or_sync(0xffffffffu, visible[w]);
+                        if (lane == 0) seen_by[i & 3][warp][w] = any;
+                    }
                 }
             }
             ok = guard.wait_all(s_full + 8 * buf, i / 2 & 1);

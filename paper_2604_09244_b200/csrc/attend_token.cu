@@ -263,17 +263,23 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
             for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[v][n][i] *= a.scale_log2;
+        uint32_t seen[U][2] = {};                            // four bits for every key g + 8 k: which lanes have a row that sees it
         if (!all) {
 #pragma unroll
             for (int v = 0; v < U; ++v)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const int at = __shfl_sync(0xffffffffu, pos, 16 * v + g + 8 * k);
+                    bool some = false;
 #pragma unroll
                     for (int n = 0; n < NR; ++n)
 #pragma unroll
-                        for (int e = 0; e < 2; ++e)
-                            if (!sees(p[n][e], at, a.window, a.n_sink)) x[v][n][2 * k + e] = -CUDART_INF_F;
+                        for (int e = 0; e < 2; ++e) {
+                            const bool on = sees(p[n][e], at, a.window, a.n_sink);
+                            some |= on;
+                            if (!on) x[v][n][2 * k + e] = -CUDART_INF_F;
+                        }
+                    seen[v][k] = __ballot_sync(0xffffffffu, some);
                 }
         }
         if (a.logits) {
@@ -338,11 +344,9 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
                     }
                 }
             }
-            bool hidden[4] = {};                             // values that nobody may look at (0 times NaN is NaN)
-            if (!all) {
+            bool hidden[4];                                  // values of keys that no row sees (0 times NaN is NaN)
 #pragma unroll
-                for (int n = 0; n < 4; ++n) hidden[n] = __shfl_sync(0xffffffffu, pos, 16 * v + 2 * c + (n & 1) + 8 * (n >> 1)) < 0;
-            }
+            for (int n = 0; n < 4; ++n) hidden[n] = !all && (seen[v][n >> 1] >> (4 * (2 * c + (n & 1))) & 0xFu) == 0;
 #pragma unroll
             for (int m = 0; m < M64; ++m) {
                 uint32_t w[4][4];

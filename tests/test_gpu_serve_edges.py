@@ -133,3 +133,30 @@ def test_full_batches():
         ctx.close()
     with pytest.raises(mvla.MvlaError):
         context("bf16", 4, 2, 64, batch=100000)
+
+
+@pytest.mark.parametrize("pos", ["count", "kept", "filled"])
+@pytest.mark.parametrize("n_q", [1, 3, 50, 300])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32", "fp8"])
+def test_attention_beside_rows_that_no_query_sees(dtype, n_q, pos):
+    """Cached rows outside every window, behind every query or between the windows of queries far apart may hold NaN and infinities."""
+    ctx = context(dtype, 4, 2, 64)
+    for window, sinks in ((20, 3), (100, 0), (1, 1)):
+        args, mass, kept = attend_case(dtype, 4, 2, 64, [n_q, n_q], [n_q + 333, n_q + 70], window, sinks, pos, seed=n_q)
+        if pos == "filled":                              # queries far apart, and rows behind all of them
+            for s in args["seqs"]:
+                args["q_pos"][s.q_row:s.q_row + s.n_q] = torch.linspace(0, 1.5 * s.n_kv, s.n_q, device="cuda").to(torch.int32)
+        some = 0
+        for b, s in enumerate(args["seqs"]):
+            c = args["kv_pos"][s.kv_row:s.kv_row + s.n_kv] if args["kv_pos"] is not None else torch.arange(s.n_kv, device="cuda")
+            p = args["q_pos"][s.q_row:s.q_row + s.n_q] if args["q_pos"] is not None else torch.arange(s.n_kv - s.n_q, s.n_kv, device="cuda")
+            seen = (c[None] >= 0) & (c[None] <= p[:, None]) & ((p[:, None] - c[None] < window) | (c[None] < sinks))
+            unseen = s.kv_row + torch.nonzero(~seen.any(0)).flatten()
+            some += unseen.numel()
+            for x in (args["k"], args["v"]):
+                x[unseen] = float("nan")
+                if dtype != "fp8":
+                    x[unseen[::3]] = float("inf")
+        assert some > 0
+        check_attention(ctx, args, mass, kept)
+    ctx.close()
