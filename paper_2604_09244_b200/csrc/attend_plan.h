@@ -52,6 +52,16 @@ constexpr int kMaxTiles = 2048;          // tiles of keys that a CTA of the tile
 // kFormToken: at most 16 query rows to a key head, straight from global memory.
 enum AttendForm { kFormFma, kFormTile, kFormToken };
 
+// Few query rows to a key head: the token form reads e4m3 rows as they are and keeps scores for the weights, where the tile form widens all rows and
+// goes over the keys a second time; heads of 64 are tiles too small for it.  Else the tile form's larger copies win although its rows are mostly
+// empty.  us, token / tile form, one token: 60000 rows of 8 e4m3 heads of 128 44 / 129; 800 rows with weights 11.7 / 22.6; 60000 rows of 8 bf16
+// heads of 64 35.4 / 37.0; of 8 heads of 128 58 / 48, of 32 185 / 149, of 16 of 256 183 / 166, of 32 of 96 143 / 131; 131072 rows of 8 of 128
+// 108 / 97; 16 ragged caches 45.9 / 45.9; 800 rows of 32 heads 12.0 / 12.7; 2 to 4 tokens over 200 rows 10.4 to 14.5 / 9.2.
+inline bool by_tokens(int dtype, int head_dim, int64_t rows, bool mass)
+{
+    return rows <= 16 && (dtype == MVLA_DTYPE_FP8_E4M3 || mass || head_dim <= 64);
+}
+
 struct AttendPlan {
     AttendForm form = kFormFma;
     int32_t rows = 32;           // query rows of a block (a block shares a key head: queries x heads of a group)
@@ -98,6 +108,7 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
         most_rows = rows > most_rows ? rows : most_rows;
     }
     if (c.dtype == MVLA_DTYPE_FP32) {
+        // (four tokens over 200 to 900 rows 20.6 us with blocks of 8 rows, 28.7 with 32; 30000 rows of 8 heads 81 and 94)
         p.rows = most_rows <= 8 ? 8 : 32;
         int64_t row_blocks = 0, key_tiles = 0;
         for (int b = 0; b < batch; ++b) {
@@ -119,7 +130,7 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
             n = n > 64 ? 64 : n;
             p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
         }
-    } else if (most_rows <= 16) {
+    } else if (by_tokens(c.dtype, c.head_dim, most_rows, mass)) {
         // Parts of equal length over the whole batch, a multiple of 64 keys (a tile for each warp), so that their CTAs fill whole rounds of
         // those that fit: of one to four rounds the ones that end first, by the keys of a round's longest part and 128 for its start
         // and end.  256 parts to a sequence at most (the join reads them all).
