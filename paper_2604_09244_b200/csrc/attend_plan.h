@@ -56,10 +56,12 @@ enum AttendForm { kFormFma, kFormTile, kFormToken };
 // goes over the keys a second time; heads of 64 are tiles too small for it.  Else the tile form's larger copies win although its rows are mostly
 // empty.  us, token / tile form, one token: 60000 rows of 8 e4m3 heads of 128 44 / 129; 800 rows with weights 11.7 / 22.6; 60000 rows of 8 bf16
 // heads of 64 35.4 / 37.0; of 8 heads of 128 58 / 48, of 32 185 / 149, of 16 of 256 183 / 166, of 32 of 96 143 / 131; 131072 rows of 8 of 128
-// 108 / 97; 16 ragged caches 45.9 / 45.9; 800 rows of 32 heads 12.0 / 12.7; 2 to 4 tokens over 200 rows 10.4 to 14.5 / 9.2.
-inline bool by_tokens(int dtype, int head_dim, int64_t rows, bool mass)
+// 108 / 97; 16 ragged caches 45.9 / 45.9; 800 rows of 32 heads 12.0 / 12.7; 2 to 4 tokens over 200 rows 10.4 to 14.5 / 9.2.  The tile form cuts all
+// sequences into as many parts, so lengths have to be alike, the longest half as long again as the average at most (16 requests over 8 heads, token /
+// tile form: 1500 to 3000 rows 45.4 / 39.0, 500 to 4000 46.1 / 45.4, 500 to 60000 381 / 505, 100 to 131071 794 / 1095).
+inline bool by_tokens(int dtype, int head_dim, int64_t rows, bool mass, bool alike)
 {
-    return rows <= 16 && (dtype == MVLA_DTYPE_FP8_E4M3 || mass || head_dim <= 64);
+    return rows <= 16 && (dtype == MVLA_DTYPE_FP8_E4M3 || mass || head_dim <= 64 || !alike);
 }
 
 struct AttendPlan {
@@ -96,7 +98,7 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
 {
     AttendPlan p;
     const int group = c.n_heads / c.kv_heads;
-    int64_t longest = 0, longest_kv = 0, most_rows = 0;
+    int64_t longest = 0, longest_kv = 0, most_rows = 0, all_keys = 0, active = 0;
     for (int b = 0; b < batch; ++b) {
         const mvla_seq& s = seqs[b];
         p.total_q += s.n_q;
@@ -104,6 +106,8 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
         if (s.n_q == 0) continue;
         const int64_t keys = visible_keys(s, counted, window, n_sink), rows = static_cast<int64_t>(s.n_q) * group;
         longest = keys > longest ? keys : longest;
+        all_keys += keys;
+        ++active;
         longest_kv = s.n_kv > longest_kv ? s.n_kv : longest_kv;
         most_rows = rows > most_rows ? rows : most_rows;
     }
@@ -130,7 +134,7 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
             n = n > 64 ? 64 : n;
             p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
         }
-    } else if (by_tokens(c.dtype, c.head_dim, most_rows, mass)) {
+    } else if (by_tokens(c.dtype, c.head_dim, most_rows, mass, 2 * longest * active <= 3 * all_keys)) {
         // Parts of equal length over the whole batch, a multiple of 64 keys (a tile for each warp), so that their CTAs fill whole rounds of
         // those that fit: of one to four rounds the ones that end first, by the keys of a round's longest part and 128 for its start
         // and end.  256 parts to a sequence at most (the join reads them all).

@@ -7,7 +7,7 @@
 // once, in 64 bits, and serve its q and k heads; a group of lanes has one head, with both elements of every pair in the lane that rotates
 // them, so that nothing but the sum of squares crosses lanes.  A row's first heads of q, k and v are on their way together.
 //
-// B200, bf16, 12800 rows of 32 + 8 + 8 heads of 128, rows gathered: 116 us (5.4 TB/s read and written; the bytes alone take 96 us).
+// B200, bf16, 12800 rows of 32 + 32 + 32 heads of 128: 115 us (5.5 TB/s read and written; the bytes alone take 97 us).
 // Arithmetic in pairs of fp32 and angles one row ahead brought it from 133 us; what is left waits for the row's loads.  Held to
 // 80 registers for a third CTA on each SM it spills (144 us).
 #include "device_utils.cuh"
