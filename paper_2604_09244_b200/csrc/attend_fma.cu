@@ -1,6 +1,6 @@
 // Windowed attention of fp32 rows by FMAs, and the weights that it gives to the cached rows.
 //
-// Flash form: one pass over the keys in tiles of 64, running maximum and sum per query row, exponentials in powers of two.  A CTA has a
+// One pass over the keys in tiles of 64, running maximum and sum per query row, exponentials in powers of two.  A CTA has a
 // block of 32 (8) query rows that share a key head: row r of a block is query r / group, head r % group of the group.  A half warp has 4 (1)
 // of them for the whole pass, in the scores and in the output, so that a row's statistics stay in its registers and its weights
 // cross only the half warp; a thread works out 4 x 4 scores from 8 loads of four elements, and 4 x 4 outputs likewise, which is where the
