@@ -57,7 +57,7 @@ struct TileRange {
 __device__ __forceinline__ TileRange tile_range(const AttArgs& a, int len, int lo, int hi, int tile)
 {
     TileRange r = {0, 0, 0};
-    const int end = a.kv_pos ? len : min(len, max(hi, -1) + 1);
+    const int end = a.kv_pos ? len : min(len - 1, max(hi, -1)) + 1;      // (hi may be the last position of its type)
     const int n = (end + tile - 1) / tile;
     const int from = a.kv_pos || a.window > lo ? 0 : lo - a.window + 1;
     r.first = min(from / tile, n);
