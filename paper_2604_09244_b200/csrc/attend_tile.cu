@@ -15,6 +15,7 @@
 // Positions that are counted tell every warp which tiles to visit and which need their mask; where they are data, a list of the
 // tiles is made first.  Keys that no row of the tile sees have their values set to zero in shared memory (0 times NaN is NaN).
 #include "attend.cuh"
+#include "attend_walk.h"
 #include "f32x2.cuh"
 #include "tmem_ld.cuh"
 #include "tmem_plan.h"
@@ -121,7 +122,8 @@ __device__ __forceinline__ int compact_entries(uint16_t* list, int n, int lane)
     return count;
 }
 
-// Bounded waits of a CTA: when one runs out, the others end without waiting for long.
+// Bounded waits of a CTA: when one runs out, the others end without waiting for long, and warps that meet one another go on meeting
+// (attend_walk.h).  Before the CTA ends, the loads and the MMAs that are under way do: also with a limit.
 struct Guard {
     int* dead;
     int* status;
@@ -130,7 +132,15 @@ struct Guard {
     __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity)
     {
         if (mbar_try_wait<false>(bar, parity)) return true;
-        if (*reinterpret_cast<volatile int*>(dead)) return false;
+        return !*reinterpret_cast<volatile int*>(dead) && spin(bar, parity);
+    }
+    // of what is under way, whoever gave up
+    __device__ __forceinline__ void settle(uint32_t bar, uint32_t parity)
+    {
+        if (!mbar_try_wait<false>(bar, parity)) spin(bar, parity);
+    }
+    __device__ __forceinline__ bool spin(uint32_t bar, uint32_t parity)
+    {
         // (the clock of the multiprocessor, about a second of it; the global timer takes a microsecond to read)
         const long long t0 = clock64();
         for (uint32_t it = 1; it < kSpinLimit; ++it) {
@@ -183,7 +193,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     using Sh = TileShape<DB>;
     constexpr int ST = Sh::kStages;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[2 * kMaxStages + 7];
+    __shared__ uint64_t bars[2 * kMaxStages + 8];
     __shared__ uint16_t list[kMaxTiles];
     __shared__ int key_at[kKeys];
     __shared__ uint32_t seen_by[4][4][kKeys / 32];           // of the last tiles: the keys that some row of a warp sees
@@ -194,8 +204,9 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int i) { return bar0 + 8u * i; };
     const auto empty = [&](int i) { return bar0 + 8u * (kMaxStages + i); };
-    // s_full, p_full: of each S buffer; o_step: a step's values are in O; o_full: all are
-    const uint32_t q_full = bar0 + 8u * (2 * kMaxStages), s_full = q_full + 8, p_full = q_full + 24, o_step = q_full + 40, o_full = q_full + 48;
+    // s_full, p_full: of each S buffer; o_step: a step's values are in O; o_full: all are; ended: the MMAs of a CTA that gave up
+    const uint32_t q_full = bar0 + 8u * (2 * kMaxStages), s_full = q_full + 8, p_full = q_full + 24, o_step = q_full + 40, o_full = q_full + 48,
+                   ended = q_full + 56;
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
 
     if (warp == Sh::kLoads && lane == 0) {
@@ -204,6 +215,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_full + 8 * i, 128); }
         mbar_init(o_step, 1);
         mbar_init(o_full, 1);
+        mbar_init(ended, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         dead = 0;
@@ -274,10 +286,8 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                 if (!guard.wait(empty(c % ST), (c / ST - 1) & 1)) break;
                 load(c);
             }
-            if (c < 2 * n) {                                 // given up: what is under way has to land before the CTA may end
-                mbar_wait(q_full, 0);
-                for (int i = max(0, c - ST); i < c; ++i) mbar_wait(full(i % ST), i / ST & 1);
-            }
+            guard.settle(q_full, 0);                         // (whoever gave up, what is under way lands before the CTA ends)
+            for (int i = max(0, c - ST); i < c; ++i) guard.settle(full(i % ST), i / ST & 1);
         }
     } else if (warp == Sh::kIssues && n > 0) {
         const uint32_t idesc_s = idesc_16<F16>(kKeys), idesc_o = idesc_16<F16>(a.head_dim) | kRowsAreContraction;
@@ -340,8 +350,9 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             }
             __syncwarp();
         }
-        if (ok && one) umma_commit(o_full);
+        if (one) umma_commit(ok ? o_full : ended);
         __syncwarp();
+        guard.settle(ok ? o_full : ended, 0);                   // (whoever else gave up, the tensor memory is not given back under an MMA)
     } else if (warp < 4) {
         // ---- softmax, a thread per row
         const int i_row = q0 + t / a.pack, head = head0 + t % a.pack;
@@ -352,38 +363,39 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         const float scale = a.scale_log2;
         const uint64_t scale2 = two_f32(scale, scale);
         float m = -CUDART_INF_F, l = 0.f;                    // reference (scaled), sum
-        bool ok = true;
-        for (int i = 0; i < n; ++i) {
-            const int buf = i & 1, j0 = first_key(i);
-            const bool masked = (flags_of(i, j0) & kMask) != 0;
-            uint32_t visible[kKeys / 32];                    // a bit for every key of the tile that the row sees
-            if (masked) {
-                if (a.kv_pos) {                              // the positions, for the four warps
-                    asm volatile("bar.sync 1, 128;" ::: "memory");       // (nobody reads the last ones any more)
-                    if (t < kKeys) key_at[t] = key_pos(a, s, len, j0 + t);
-                    asm volatile("bar.sync 1, 128;" ::: "memory");
+        bool masked = false;
+        uint32_t visible[kKeys / 32];                        // a bit for every key of the tile that the row sees
+        const auto look = [&](int i) {
+            const int j0 = first_key(i);
+            masked = (flags_of(i, j0) & kMask) != 0;
+            if (!masked) return;
+            if (a.kv_pos) {                                  // the positions, for the four warps
+                asm volatile("bar.sync 1, 128;" ::: "memory");       // (nobody reads the last ones any more)
+                if (t < kKeys) key_at[t] = key_pos(a, s, len, j0 + t);
+                asm volatile("bar.sync 1, 128;" ::: "memory");
 #pragma unroll
-                    for (int w = 0; w < kKeys / 32; ++w) {
-                        uint32_t bits = 0;
+                for (int w = 0; w < kKeys / 32; ++w) {
+                    uint32_t bits = 0;
 #pragma unroll 8
-                        for (int c = 0; c < 32; ++c) bits |= sees(p, key_at[32 * w + c], a.window, a.n_sink) ? 1u << c : 0u;
-                        visible[w] = bits;
-                    }
-                } else {
-                    const int past = min(p, len - 1) - j0 + 1, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
-#pragma unroll
-                    for (int w = 0; w < kKeys / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
+                    for (int c = 0; c < 32; ++c) bits |= sees(p, key_at[32 * w + c], a.window, a.n_sink) ? 1u << c : 0u;
+                    visible[w] = bits;
                 }
-                if (a.q_pos) {                               // (those of three tiles ago were read before the last S was made)
+            } else {
+                const int past = min(p, len - 1) - j0 + 1, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
 #pragma unroll
-                    for (int w = 0; w < kKeys / 32; ++w) {
-                        const uint32_t any = __reduce_or_sync(0xffffffffu, visible[w]);
-                        if (lane == 0) seen_by[i & 3][warp][w] = any;
-                    }
+                for (int w = 0; w < kKeys / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
+            }
+            if (a.q_pos) {                                   // (those of three tiles ago were read before the last S was made)
+#pragma unroll
+                for (int w = 0; w < kKeys / 32; ++w) {
+                    const uint32_t any = __reduce_or_sync(0xffffffffu, visible[w]);
+                    if (lane == 0) seen_by[i & 3][warp][w] = any;
                 }
             }
-            ok = guard.wait_all(s_full + 8 * buf, i / 2 & 1);
-            if (!ok) break;
+        };
+        const auto scores_there = [&](int i) { return guard.wait_all(s_full + 8 * (i & 1), i / 2 & 1); };
+        const auto weigh = [&](int i) {
+            const int buf = i & 1;
             tc_fence_after();
             const uint32_t s_col = tmem + buf * kKeys + lanes;
             float x[kKeys];
@@ -402,8 +414,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             const bool move = top > m + kMoveAt;
             if (i > 0 && __any_sync(0xffffffffu, move)) {
                 // (the step before may still be adding; the one before that was complete before this S was)
-                ok = guard.wait_all(o_step, (i - 1) & 1);
-                if (!ok) break;
+                if (!guard.wait_all(o_step, (i - 1) & 1)) return false;
                 tc_fence_after();
                 const float f = move ? ex2_approx(m - top) : 1.f;
 #pragma unroll 1
@@ -441,7 +452,9 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             tmem_st_wait();
             tc_fence_before();
             mbar_arrive(p_full + 8 * buf);
-        }
+            return true;
+        };
+        bool ok = walk_tiles(0, n, 1, look, scores_there, weigh);
         // ---- the rows
         if (ok && n > 0) ok = guard.wait_all(o_full, 0);
         tc_fence_after();
@@ -503,7 +516,7 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
     using Sh = WeightShape<DB>;
     constexpr int ST = kWeightStages;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[2 * ST + 5];
+    __shared__ uint64_t bars[2 * ST + 6];
     __shared__ uint16_t list[kMaxTiles];
     __shared__ __align__(16) float row_z[2][kRows];
     __shared__ int row_p[2][kRows];
@@ -515,12 +528,13 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int i) { return bar0 + 8u * i; };
     const auto empty = [&](int i) { return bar0 + 8u * (ST + i); };
-    const uint32_t s_full = bar0 + 8u * (2 * ST), s_empty = s_full + 16, k_full = s_full + 32;      // two of each group's S
+    const uint32_t s_full = bar0 + 8u * (2 * ST), s_empty = s_full + 16, k_full = s_full + 32, ended = s_full + 40;      // two of each group's S
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
     if (warp == 8 && lane == 0) {
         for (int i = 0; i < ST; ++i) { mbar_init(full(i), 1); mbar_init(empty(i), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(s_empty + 8 * i, 128); }
         mbar_init(k_full, 1);
+        mbar_init(ended, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         dead = 0;
@@ -594,10 +608,8 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
                 if (!guard.wait(empty(c % ST), (c / ST - 1) & 1)) break;
                 load(c);
             }
-            if (c < n) {
-                mbar_wait(k_full, 0);
-                for (int i = max(0, c - ST); i < c; ++i) mbar_wait(full(i % ST), i / ST & 1);
-            }
+            guard.settle(k_full, 0);
+            for (int i = max(0, c - ST); i < c; ++i) guard.settle(full(i % ST), i / ST & 1);
         }
     } else if (warp == 9) {
         const uint32_t idesc = idesc_16<F16>(kRows);
@@ -617,13 +629,15 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
             }
             __syncwarp();
         }
+        if (one) umma_commit(ended);
+        __syncwarp();
+        guard.settle(ended, 0);
     } else {
         const int group = warp / 4, r = t & 127, j = j0 + r;
         const uint32_t s_col = tmem + group * kRows + (static_cast<uint32_t>(warp & 3) << 21);
         const int c_pos = key_pos(a, s, len, j);
         const uint64_t scale2 = two_f32(a.scale_log2, a.scale_log2);
         float sum = 0.f;
-        bool ok = true;
         // this thread's query row of a tile, for all keys of the group: logarithm of its sum, position
         float z = 0.f;
         int p = -1;
@@ -634,15 +648,16 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
             p = there ? query_pos(a, s, len, iq) : -1;
         };
         fetch(group);
-        for (int i = group; i < n; i += 2) {
+        bool masked = false;
+        uint32_t visible[kRows / 32];                        // a bit for every query row that sees this thread's key
+        const auto look = [&](int i) {
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");       // (nobody reads the last tile's any more)
             row_z[group][r] = -z;
             row_p[group][r] = p;
             asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
             fetch(i + 2);
             const int v = tile_at(i);
-            uint32_t visible[kRows / 32];                    // a bit for every query row that sees this thread's key
-            const bool masked = listed ? (list[i] & kMask) != 0 : tile_flags(v) != kNeed;
+            masked = listed ? (list[i] & kMask) != 0 : tile_flags(v) != kNeed;
             if (masked) {
                 if (listed) {
 #pragma unroll
@@ -660,8 +675,9 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
                         visible[w] = below(max(past, 0) * a.pack - 32 * w) & ~below(min(first, per) * a.pack - 32 * w);
                 }
             }
-            ok = guard.wait_all(s_full + 8 * group, i / 2 & 1);
-            if (!ok) break;
+        };
+        const auto scores_there = [&](int i) { return guard.wait_all(s_full + 8 * group, i / 2 & 1); };
+        const auto add_up = [&](int) {
             tc_fence_after();
             uint64_t part[2] = {0, 0};
 #pragma unroll
@@ -690,7 +706,9 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
             float even, odd;
             split_f32(add_f32x2(part[0], part[1]), even, odd);
             sum += even + odd;
-        }
+            return true;
+        };
+        walk_tiles(group, n, 2, look, scores_there, add_up);
         if (group == 1) half[r] = sum;
         asm volatile("bar.sync 3, 256;" ::: "memory");
         if (group == 0 && j < s.n_kv)
