@@ -220,8 +220,10 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         dead = 0;
         prefetch_tensormap(&map_q);
-        prefetch_tensormap(&map_k);
-        prefetch_tensormap(&map_v);
+        if (a.total_kv > 0) {                                // (else these two are no tensor maps)
+            prefetch_tensormap(&map_k);
+            prefetch_tensormap(&map_v);
+        }
     }
     __syncwarp();
     pdl_wait();

@@ -1,5 +1,5 @@
 """Arguments of the calls around the prune point that are used together: lengths on the device and positions that are data, caches that grow between the
-replays of a graph, cached rows that sequences share."""
+replays of a graph, cached rows that sequences share, caches without rows."""
 import pytest
 import torch
 
@@ -90,4 +90,17 @@ def test_eviction_with_lengths_and_long_caches():
         seqs, k, v, pos, mass = evict_case("bf16", 1, 64, [n, 33], [budget, 20], 3)
         kv_len = torch.tensor([lens, 33], dtype=torch.int32, device="cuda")
         check_evict(ctx, seqs, k, v, pos, mass, 0, 1, kv_len=kv_len, in_place=lens % 2 == 1)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32", "fp8"])
+@pytest.mark.parametrize("n_q", [1, 40, 300])
+def test_a_batch_without_cached_rows(dtype, n_q):
+    """Queries before anything is cached: they see nothing, whether the cache has rows of nobody's or none at all."""
+    ctx = context(dtype, 4, 2, 128)
+    for mass in (True, False):
+        args, weights, kept = attend_case(dtype, 4, 2, 128, [n_q, 1], [0, 0], None, 0, "count", seed=1, mass=mass)
+        check_attention(ctx, args, weights, kept)
+        none = dict(args, k=args["k"][:0], v=args["v"][:0], seqs=[Seq(q_row=s.q_row, n_q=s.n_q) for s in args["seqs"]])
+        check_attention(ctx, none, None if weights is None else weights[:0], kept)
     ctx.close()
