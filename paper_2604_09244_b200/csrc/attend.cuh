@@ -8,6 +8,11 @@
 
 namespace mvla {
 
+// Weights that meet the values in fp16 are counted in units of 2^-kF16Lift of their row's reference: none lies more than 2^8 above the reference, so that
+// the largest is 2^15 and fits, and one stays a normal number (11 bits) down to 2^-21 of the reference instead of 2^-14, and is nothing below 2^-32
+// instead of 2^-25.  The sum that divides them is taken of the same units, and the reference that is handed on is less by as much.
+constexpr float kF16Lift = 7.f;
+
 __device__ __forceinline__ int seq_len(const AttArgs& a, const AttSeq& s)
 {
     return a.kv_len ? min(max(a.kv_len[s.index], 0), s.n_kv) : s.n_kv;

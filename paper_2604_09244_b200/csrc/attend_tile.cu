@@ -4,6 +4,7 @@
 // packed side by side, one TMA box) and walks the tiles of 64 keys that some of its rows may see:
 //     S = Q K^T (tcgen05, both from shared memory)  ->  P = 2^(S - reference), rounded to 16 bits, back into the columns of S
 //     ->  O += P V (tcgen05, P from tensor memory, V as it lies in the cache: its rows are the contraction).
+// fp16 weights (e4m3 rows) are counted in units of 2^-kF16Lift of the reference, so that faint ones stay normal numbers as long as can be.
 // Warps 0-3: the softmax, a thread per row: maximum and sum without a shuffle.  The sums in O are taken against a reference that is
 // moved only when a row's maximum grows past it by 2^8 (the result is the same; moving it is a pass over O).  Warp 4 loads, warp 5
 // issues the MMAs; S is double-buffered, so that the next scores are there when the softmax of the last ones ends.
@@ -364,7 +365,8 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         const uint32_t o_col = tmem + Sh::kO + lanes;
         const float scale = a.scale_log2;
         const uint64_t scale2 = two_f32(scale, scale);
-        float m = -CUDART_INF_F, l = 0.f;                    // reference (scaled), sum
+        constexpr float kLift = F16 ? kF16Lift : 0.f;
+        float m = -CUDART_INF_F, l = 0.f;                    // reference (scaled), sum (of weights against the reference less kLift)
         bool masked = false;
         uint32_t visible[kKeys / 32];                        // a bit for every key of the tile that the row sees
         const auto look = [&](int i) {
@@ -431,7 +433,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                 l *= f;
             }
             if (move) m = top;
-            const float ref = m == -CUDART_INF_F ? 0.f : m;
+            const float ref = m == -CUDART_INF_F ? 0.f : m - kLift;
             const uint64_t ref2 = two_f32(-ref, -ref);
             uint64_t sums[2] = {0, 0};
 #pragma unroll
@@ -462,6 +464,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         tc_fence_after();
         const int64_t part = s.part0 + static_cast<int64_t>(blockIdx.y) * s.n_q + i_row;
         const float inv = l > 0.f ? 1.f / l : 0.f;
+        m -= kLift;
         for (int c = 0; c < a.head_dim && ok; c += 32) {
             float o[32];
             if (n > 0) tmem_ld_cols<32>(o_col + c, o);

@@ -9,7 +9,7 @@
 // warps, and none between the lanes.  The scores become the second product's operand by transposing 8 x 8 blocks between the lanes.
 // The sums are taken against a reference per row that is moved when some score lies 2^8 above it: one vote a tile, and no shuffle
 // but then and at the end.  bf16 weights meet the values in two parts, what the type holds and what it leaves (the tensor cores have
-// nothing else to do), so that rounding them costs nothing; fp16 is fine enough.
+// nothing else to do), so that rounding them costs nothing; fp16 weights (e4m3 rows) are one part, lifted (kF16Lift).
 // A sequence's visible keys are cut into parts of about the same length over the whole batch; a CTA is four warps that take the part's
 // tiles in turn.  With accumulated weights the scores are kept (a fraction 2 / head_dim of the keys' and values' bytes and one more for
 // every query row) and become weights once all parts are joined.
@@ -60,6 +60,7 @@ template <> struct Kind<__nv_bfloat16> {
         mma(x, k0.z, k1.z, k0.w, k1.w, y.z, y.w);
     }
     static constexpr bool kTwoParts = true;
+    static constexpr float kLift = 0.f;
     static constexpr bool kPairs = false;        // eight elements are what a lane copies at once
     // eight elements as the products' 16-bit pairs
     static __device__ __forceinline__ void words(const void* p, uint32_t (&w)[4])
@@ -83,6 +84,7 @@ template <> struct Kind<__nv_fp8_e4m3> {         // scores from the 8-bit operan
                      : "+f"(x[0]), "+f"(x[1]), "+f"(x[2]), "+f"(x[3]) : "r"(k0.x), "r"(k1.x), "r"(k0.y), "r"(k1.y), "r"(y.x), "r"(y.y));
     }
     static constexpr bool kTwoParts = false;
+    static constexpr float kLift = kF16Lift;
     static constexpr bool kPairs = true;         // sixteen, where a head has them
     static __device__ __forceinline__ uint32_t two(uint32_t x)
     {
@@ -336,7 +338,7 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
             uint32_t w_hi[NR][2], w_lo[NR][2];
 #pragma unroll
             for (int n = 0; n < NR; ++n) {
-                const float b0 = ref[n][0] == -CUDART_INF_F ? 0.f : ref[n][0], b1 = ref[n][1] == -CUDART_INF_F ? 0.f : ref[n][1];
+                const float b0 = ref[n][0] == -CUDART_INF_F ? 0.f : ref[n][0] - K::kLift, b1 = ref[n][1] == -CUDART_INF_F ? 0.f : ref[n][1] - K::kLift;
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const float y = ex2_approx(x[v][n][2 * k] - b0), z = ex2_approx(x[v][n][2 * k + 1] - b1);
@@ -381,7 +383,7 @@ __global__ void __launch_bounds__(kWarps * 32, TokenShape<T, D32>::kCtas) attend
         for (int e = 0; e < 2; ++e) {
 #pragma unroll
             for (int w = 4; w < 32; w *= 2) sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], w);
-            if (g == 0) { merge_m[warp][8 * n + 2 * c + e] = ref[n][e]; merge_l[warp][8 * n + 2 * c + e] = sum[n][e]; }
+            if (g == 0) { merge_m[warp][8 * n + 2 * c + e] = ref[n][e] - K::kLift; merge_l[warp][8 * n + 2 * c + e] = sum[n][e]; }
         }
     const bool whole = s.parts == 1;
 #pragma unroll
