@@ -463,8 +463,9 @@ typedef struct mvla_attention {
  * Causal attention with a sliding window and sinks.  Query i (position p_i) sees cached row j (position c_j) of its sequence where
  *   0 <= c_j <= p_i  and  (p_i - c_j < window  or  c_j < n_sink);
  * query head h reads key head h / (n_heads / n_kv_heads).  out = softmax over the visible rows, times their values; sums and
- * exponentials in 32 bits (16-bit types: weights are rounded to bf16 for their product with the values, e4m3: to fp16).  A query
- * that sees nothing: out 0, lse -infinity.  mass[j] += 1 / n_heads * sum over heads and queries of the weight of row j, in an order
+ * exponentials in 32 bits.  For their product with the values weights are rounded: bf16 rows' to bf16 (2^-8 of a weight at most), but to
+ * 16 bits (2^-16) where a sequence has at most 16 query rows to a key head (single tokens), with `mass` or without it, whatever else is in
+ * the batch; e4m3 rows' to fp16 in units of 2^-7 of the row's largest (or less).  A query that sees nothing: out 0, lse -infinity.  mass[j] += 1 / n_heads * sum over heads and queries of the weight of row j, in an order
  * that does not change from run to run.
  * What q, k and v hold must be finite in rows that some query of the sequence sees; cached rows that none sees (behind a sequence's
  * length, of negative position, outside every window) may hold anything.  Rows of q, out and lse outside the sequences are left as they are.  Sequences must not

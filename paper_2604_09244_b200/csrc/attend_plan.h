@@ -52,16 +52,23 @@ constexpr int kMaxTiles = 2048;          // tiles of keys that a CTA of the tile
 // kFormToken: at most 16 query rows to a key head, straight from global memory.
 enum AttendForm { kFormFma, kFormTile, kFormToken };
 
+// A sequence of at most so many query rows to a key head counts as single tokens: its bf16 weights keep what rounding leaves of them, in the token form and
+// in the tile form, so that the form that its batch is given costs no bits.
+constexpr int kTokenRows = 16;
+
 // Few query rows to a key head: the token form reads e4m3 rows as they are and keeps scores for the weights, where the tile form widens all rows and
 // goes over the keys a second time; heads of 64 are tiles too small for it.  Else the tile form's larger copies win although its rows are mostly
-// empty.  us, token / tile form, one token: 60000 rows of 8 e4m3 heads of 128 44 / 129; 800 rows with weights 11.7 / 22.6; 60000 rows of 8 bf16
-// heads of 64 35.4 / 37.0; of 8 heads of 128 58 / 48, of 32 185 / 149, of 16 of 256 183 / 166, of 32 of 96 143 / 131; 131072 rows of 8 of 128
-// 108 / 97; 16 ragged caches 45.9 / 45.9; 800 rows of 32 heads 12.0 / 12.7; 2 to 4 tokens over 200 rows 10.4 to 14.5 / 9.2.  The tile form cuts all
-// sequences into as many parts, so lengths have to be alike, the longest half as long again as the average at most (16 requests over 8 heads, token /
-// tile form: 1500 to 3000 rows 45.4 / 39.0, 500 to 4000 46.1 / 45.4, 500 to 60000 381 / 505, 100 to 131071 794 / 1095).
+// empty.
+// us, token / tile form, one token where nothing else is said: e4m3, 60000 rows of 8 heads of 128 44 / 129; with weights, 800 rows 11.7 / 22.6; heads of
+// 64, 60000 rows of 8 35.4 / 37.0.  bf16 without weights, 4 query heads to each of 8 heads of 128, 800 / 4000 / 16000 / 131071 rows 8.5 / 12.8,
+// 12.4 / 14.2, 23.4 / 21.4, 107 / 89; 32 heads of 128 with a query head each 11.0 / 15.2, 20.7 / 24.8, 57 / 53, 394 / 331; 32 of 96 10.3 / 13.8, 18.0 / 19.9,
+// 46 / 46, 310 / 287; 16 of 256 12.9 / 17.5, 23.1 / 25.3, 58 / 57, 399 / 357; 2, 3 and 4 tokens (8, 12, 16 rows) over 200 rows 9.7 / 9.8, 12.1 / 9.8, 14.5 / 9.8,
+// over 30000 36 / 31, 41 / 31, 43 / 31; 32 requests over 700 to 800 rows 28.2 / 26.5.  The tile form cuts all sequences into as many parts, so lengths
+// have to be alike, the longest half as long again as the average at most (16 requests over 8 heads: 1500 to 3000 rows 45.1 / 40.0, 500 to 4000 46.1 / 45.4,
+// 500 to 60000 381 / 505, 100 to 131071 794 / 1095).
 inline bool by_tokens(int dtype, int head_dim, int64_t rows, bool mass, bool alike)
 {
-    return rows <= 16 && (dtype == MVLA_DTYPE_FP8_E4M3 || mass || head_dim <= 64 || !alike);
+    return rows <= kTokenRows && (dtype == MVLA_DTYPE_FP8_E4M3 || mass || head_dim <= 64 || !alike);
 }
 
 struct AttendPlan {

@@ -12,7 +12,7 @@
 // one's exponentials, prologue and epilogue lie beside the other's MMAs.  Measured on 8192 queries, 16 heads of 128 in groups of 4, and on
 // 16 x 808 queries of 32 heads, window 512: two tiles of rows in one CTA with tiles of 128 keys 295 / 250 us, this 291 / 189.
 // Now 306 us (900 TFLOP/s; the MMAs alone 235, without the exponentials 286: reads of shared memory by 64-key MMAs, and the chain from scores to
-// weights) and 195 + 135 for the weights.  Single tokens without weights come here too: 131072 rows of 8 heads of 128 101 us, 5.3 TB/s.
+// weights) and 195 + 135 for the weights.  Single tokens without weights come here too: 131072 rows of 8 heads of 128 99.9 us, 5.4 TB/s.
 // Positions that are counted tell every warp which tiles to visit and which need their mask; where they are data, a list of the
 // tiles is made first.  Keys that no row of the tile sees have their values set to zero in shared memory (0 times NaN is NaN).
 #include "attend.cuh"
@@ -186,7 +186,13 @@ struct TileShape {
     static_assert(kStages >= 4, "shape");
 };
 
-template <bool F16, int DB>
+// TOKENS: bf16 weights of sequences that count as single tokens meet the values in two parts, what the type holds and what it leaves.  Such a sequence
+// has kTokenRows of the tile's 128 rows at most, so its query rows are there twice, kTwin rows apart: the first ones' row of P takes the one part, their
+// twin's the other, and the rows of O are added up at the end.  No MMA more, and none of the other rows' exponentials.
+constexpr int kTwin = 32;                    // (a warp's lanes)
+static_assert(kTokenRows <= kTwin, "the rows of a warp");
+
+template <bool F16, int DB, bool TOKENS>
 __global__ void __launch_bounds__(TileShape<DB>::kWarps * 32, TileShape<DB>::kCtas)
 attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v)
@@ -235,6 +241,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     const AttSeq& s = a.s[seq_of_block(a, blk)];
     const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack;      // queries of the tile
     const int q0 = (blk - s.blk0) * per, len = seq_len(a, s);
+    const bool twins = TOKENS && static_cast<int64_t>(s.n_q) * (a.n_heads / a.kv_heads) <= kTokenRows;
     int lo, hi;
     query_span(a, s, len, q0, min(q0 + per, s.n_q), lane, &lo, &hi);
     const TileRange range = tile_range(a, len, lo, hi, kKeys);
@@ -304,7 +311,22 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             umma_commit(s_full + 8 * (i & 1));
             umma_commit(empty(st));
         };
-        bool ok = guard.wait_all(q_full, 0) && guard.wait_all(full(0), 0);
+        bool ok = guard.wait_all(q_full, 0);
+        if (TOKENS && twins && ok) {                         // (whole swizzled groups of eight rows: they lie alike kTwin rows on)
+            constexpr int kPer = kTokenRows * 8 / 32;        // 16-byte pieces of a lane in a box
+            uint32_t w[DB * kPer][4];
+#pragma unroll
+            for (int u = 0; u < DB * kPer; ++u)
+                asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(w[u][0]), "=r"(w[u][1]), "=r"(w[u][2]), "=r"(w[u][3])
+                             : "r"(q_at + u / kPer * kRows * 128 + (u % kPer * 32 + lane) * 16) : "memory");
+#pragma unroll
+            for (int u = 0; u < DB * kPer; ++u)
+                asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(q_at + u / kPer * kRows * 128 + kTwin * 128 + (u % kPer * 32 + lane) * 16),
+                             "r"(w[u][0]), "r"(w[u][1]), "r"(w[u][2]), "r"(w[u][3]) : "memory");
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+        }
+        ok = ok && guard.wait_all(full(0), 0);
         if (ok && one) {
             tc_fence_after();
             scores(0);
@@ -358,8 +380,10 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         guard.settle(ok ? o_full : ended, 0);                   // (whoever else gave up, the tensor memory is not given back under an MMA)
     } else if (warp < 4) {
         // ---- softmax, a thread per row
-        const int i_row = q0 + t / a.pack, head = head0 + t % a.pack;
-        const bool mine = t < per * a.pack && i_row < s.n_q;
+        const int r = TOKENS && twins ? t % kTwin : t;       // row of the tile
+        const bool twin = TOKENS && twins && t >= kTwin;     // (the rows from 2 kTwin on are nobody's)
+        const int i_row = q0 + r / a.pack, head = head0 + r % a.pack;
+        const bool mine = r < per * a.pack && i_row < s.n_q && !(TOKENS && twins && t >= 2 * kTwin);
         const int p = mine ? query_pos(a, s, len, i_row) : -1;
         const uint32_t lanes = static_cast<uint32_t>(warp) << 21;            // this warp's 32 lanes
         const uint32_t o_col = tmem + Sh::kO + lanes;
@@ -400,6 +424,10 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         const auto scores_there = [&](int i) { return guard.wait_all(s_full + 8 * (i & 1), i / 2 & 1); };
         const auto weigh = [&](int i) {
             const int buf = i & 1;
+            if (TOKENS && twins && t >= 2 * kTwin) {
+                mbar_arrive(p_full + 8 * buf);
+                return true;
+            }
             tc_fence_after();
             const uint32_t s_col = tmem + buf * kKeys + lanes;
             float x[kKeys];
@@ -447,6 +475,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                     z = ex2_approx(z);
                     sums[c / 2 & 1] = add_f32x2(sums[c / 2 & 1], two_f32(y, z));
                     w[c / 2] = F16 ? two_f16(y, z) : two_bf16(y, z);
+                    if (TOKENS && twin) w[c / 2] = two_bf16(y - __uint_as_float(w[c / 2] << 16), z - __uint_as_float(w[c / 2] & 0xFFFF0000u));
                 }
                 tmem_st_cols<16>(s_col + c0 / 2, w);
             }
@@ -465,9 +494,26 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         const int64_t part = s.part0 + static_cast<int64_t>(blockIdx.y) * s.n_q + i_row;
         const float inv = l > 0.f ? 1.f / l : 0.f;
         m -= kLift;
-        for (int c = 0; c < a.head_dim && ok; c += 32) {
+        // the twins' rows of O, for the others (the keys and values have been read): element by element, the rows side by side
+        float* const beside = reinterpret_cast<float*>(raw + (kv_at - smem_u32(raw)));
+        if (TOKENS && twins && t < 2 * kTwin) {
+            if (twin && ok && n > 0) {
+                for (int c = 0; c < a.head_dim; c += 32) {
+                    float o[32];
+                    tmem_ld_cols<32>(o_col + c, o);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) beside[(c + k) * kTwin + r] = o[k];
+                }
+            }
+            asm volatile("bar.sync 2, 64;" ::: "memory");    // (reached by both warps, whoever gave up)
+        }
+        for (int c = 0; c < a.head_dim && ok && !(TOKENS && twins && t >= kTwin); c += 32) {
             float o[32];
             if (n > 0) tmem_ld_cols<32>(o_col + c, o);
+            if (TOKENS && twins && n > 0) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) o[k] += beside[(c + k) * kTwin + r];
+            }
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? (a.splits > 1 ? o[k] : o[k] * inv) : 0.f;
             if (!mine) continue;
@@ -481,7 +527,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                 for (int k = 0; k < 32; k += 8) store8(dst + k, o + k);
             }
         }
-        if (mine && ok) {
+        if (mine && ok && !twin) {
             if (a.splits > 1) {
                 a.part_ml[part * a.n_heads + head] = make_float2(m, l);
             } else {
@@ -744,13 +790,13 @@ cudaError_t launch(KernelSetup& setup, K kernel, dim3 grid, int threads, int col
     return cudaLaunchKernelEx(&cfg, kernel, a, maps.q, maps.k, maps.v);
 }
 
-template <bool F16, int DB>
+template <bool F16, int DB, bool TOKENS>
 cudaError_t attend(const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
     static KernelSetup setup;
     const dim3 grid(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack), static_cast<unsigned>(a.splits));
     using Sh = TileShape<DB>;
-    return launch(setup, attend_tile_kernel<F16, DB>, grid, Sh::kWarps * 32, Sh::kColumns, Sh::kSmem, a, maps, stream);
+    return launch(setup, attend_tile_kernel<F16, DB, TOKENS>, grid, Sh::kWarps * 32, Sh::kColumns, Sh::kSmem, a, maps, stream);
 }
 
 template <bool F16, int DB>
@@ -822,14 +868,14 @@ cudaError_t weights_by_dim(const AttArgs& a, const AttMaps& maps, cudaStream_t s
     default: return weights<F16, 4>(a, maps, stream);
     }
 }
-template <bool F16>
+template <bool F16, bool TOKENS>
 cudaError_t attend_by_dim(const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
     switch ((a.head_dim + 63) / 64) {
-    case 1: return attend<F16, 1>(a, maps, stream);
-    case 2: return attend<F16, 2>(a, maps, stream);
-    case 3: return attend<F16, 3>(a, maps, stream);
-    default: return attend<F16, 4>(a, maps, stream);
+    case 1: return attend<F16, 1, TOKENS>(a, maps, stream);
+    case 2: return attend<F16, 2, TOKENS>(a, maps, stream);
+    case 3: return attend<F16, 3, TOKENS>(a, maps, stream);
+    default: return attend<F16, 4, TOKENS>(a, maps, stream);
     }
 }
 }  // namespace
@@ -839,9 +885,10 @@ cudaError_t launch_attend_weights(bool f16, const AttArgs& a, const AttMaps& map
     return f16 ? weights_by_dim<true>(a, maps, stream) : weights_by_dim<false>(a, maps, stream);
 }
 
-cudaError_t launch_attend_tile(bool f16, const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
+cudaError_t launch_attend_tile(bool f16, bool tokens, const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
-    return f16 ? attend_by_dim<true>(a, maps, stream) : attend_by_dim<false>(a, maps, stream);
+    if (f16) return attend_by_dim<true, false>(a, maps, stream);
+    return tokens ? attend_by_dim<false, true>(a, maps, stream) : attend_by_dim<false, false>(a, maps, stream);
 }
 
 }  // namespace mvla

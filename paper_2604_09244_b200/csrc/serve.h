@@ -64,7 +64,8 @@ cudaError_t launch_mass_fma(const AttArgs& a, cudaStream_t stream);
 struct AttMaps {
     CUtensorMap q, k, v;
 };
-cudaError_t launch_attend_tile(bool f16, const AttArgs& a, const AttMaps& maps, cudaStream_t stream);
+// `tokens`: bf16, and some sequence counts as single tokens (kTokenRows).
+cudaError_t launch_attend_tile(bool f16, bool tokens, const AttArgs& a, const AttMaps& maps, cudaStream_t stream);
 // The weights as above, by tiles of 128 keys.  (mass_parts: packs of heads, times runs of kMaxTiles tiles of queries)
 cudaError_t launch_attend_weights(bool f16, const AttArgs& a, const AttMaps& maps, cudaStream_t stream);
 // The sequences' e4m3 rows as packed fp16 rows.

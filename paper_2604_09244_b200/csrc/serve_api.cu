@@ -64,8 +64,10 @@ int32_t attend_by_tiles(const CtxView& v, AttArgs& k, const mvla_attention* a, c
     const void* const kk = widen ? ws + plan.wide_k : a->k;
     const void* const vv = widen ? ws + plan.wide_v : a->v;
     const int64_t q_rows = widen ? plan.total_q : a->q_rows, kv_rows = widen ? plan.total_kv : a->kv_rows;
+    bool tokens = false;
     for (int b = 0; b < k.n_seq; ++b) {
         AttSeq& s = k.s[b];
+        tokens |= !widen && s.n_q > 0 && static_cast<int64_t>(s.n_q) * (v.n_heads / v.kv_heads) <= kTokenRows;
         s.qm_row = widen ? s.qp0 : static_cast<int32_t>(s.q_row);
         s.km_row = widen ? s.kvp0 : static_cast<int32_t>(s.kv_row);
     }
@@ -76,7 +78,7 @@ int32_t attend_by_tiles(const CtxView& v, AttArgs& k, const mvla_attention* a, c
     // (no cached rows: no key tile is ever asked for)
     if (plan.total_kv > 0 && (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, kKeys) || !row_map(v, &maps.v, vv, v.kv_heads, kv_rows, 1, kKeys))) return MVLA_ERR_CUDA;
     *e = widen ? launch_widen(k, ws + plan.wide_q, ws + plan.wide_k, ws + plan.wide_v, st) : cudaSuccess;
-    if (*e == cudaSuccess) *e = launch_attend_tile(widen, k, maps, st);
+    if (*e == cudaSuccess) *e = launch_attend_tile(widen, tokens, k, maps, st);
     if (*e == cudaSuccess && plan.splits > 1) *e = launch_attend_join(v.dtype, k, st);
     if (*e == cudaSuccess && a->mass && plan.total_kv > 0) {
         if (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, 128)) return MVLA_ERR_CUDA;
