@@ -58,7 +58,7 @@ constexpr int kTokenRows = 16;
 
 // Few query rows to a key head: the token form reads e4m3 rows as they are and keeps scores for the weights, where the tile form widens all rows and
 // goes over the keys a second time; heads of 64 are tiles too small for it.  Else the tile form's larger copies win although its rows are mostly
-// empty.
+// empty, but for calls too short to fill the device with its parts of four tiles and more, of up to eight rows (beyond, the token form does all twice).
 // us, token / tile form, one token where nothing else is said: e4m3, 60000 rows of 8 heads of 128 44 / 129; with weights, 800 rows 11.7 / 22.6; heads of
 // 64, 60000 rows of 8 35.4 / 37.0.  bf16 without weights, 4 query heads to each of 8 heads of 128, 800 / 4000 / 16000 / 131071 rows 8.5 / 12.8,
 // 12.4 / 14.2, 23.4 / 21.4, 107 / 89; 32 heads of 128 with a query head each 11.0 / 15.2, 20.7 / 24.8, 57 / 53, 394 / 331; 32 of 96 10.3 / 13.8, 18.0 / 19.9,
@@ -66,9 +66,9 @@ constexpr int kTokenRows = 16;
 // over 30000 36 / 31, 41 / 31, 43 / 31; 32 requests over 700 to 800 rows 28.2 / 26.5.  The tile form cuts all sequences into as many parts, so lengths
 // have to be alike, the longest half as long again as the average at most (16 requests over 8 heads: 1500 to 3000 rows 45.1 / 40.0, 500 to 4000 46.1 / 45.4,
 // 500 to 60000 381 / 505, 100 to 131071 794 / 1095).
-inline bool by_tokens(int dtype, int head_dim, int64_t rows, bool mass, bool alike)
+inline bool by_tokens(int dtype, int head_dim, int64_t rows, bool mass, bool alike, int64_t all_keys)
 {
-    return rows <= kTokenRows && (dtype == MVLA_DTYPE_FP8_E4M3 || mass || head_dim <= 64 || !alike);
+    return rows <= kTokenRows && (dtype == MVLA_DTYPE_FP8_E4M3 || mass || head_dim <= 64 || !alike || (rows <= 8 && all_keys < 8192));
 }
 
 struct AttendPlan {
@@ -141,7 +141,7 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
             n = n > 64 ? 64 : n;
             p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
         }
-    } else if (by_tokens(c.dtype, c.head_dim, most_rows, mass, 2 * longest * active <= 3 * all_keys)) {
+    } else if (by_tokens(c.dtype, c.head_dim, most_rows, mass, 2 * longest * active <= 3 * all_keys, all_keys)) {
         // Parts of equal length over the whole batch, a multiple of 64 keys (a tile for each warp), so that their CTAs fill whole rounds of
         // those that fit: of one to four rounds the ones that end first, by the keys of a round's longest part and 128 for its start
         // and end.  256 parts to a sequence at most (the join reads them all).

@@ -1,5 +1,5 @@
-// Windowed attention of single tokens over a cache: at most 16 query rows of a sequence share a key head (e4m3; bf16 where weights are added up
-// or heads have 64 elements).
+// Windowed attention of single tokens over a cache: at most 16 query rows of a sequence share a key head (e4m3; bf16 where weights are added up,
+// heads have 64 elements, lengths are unlike or the call is short: by_tokens in attend_plan.h).
 //
 // Bound by the bytes of the keys and values.  A warp takes tiles of 16 keys as the registers that the tensor cores read (m16n8k16): keys
 // are the 16 rows of the first product and columns of the values those of the second, query rows the 8 columns of both, so that a single
