@@ -64,7 +64,8 @@ inline int32_t check_rope(const ServeShape& v, const mvla_qk_rope* r)
         return MVLA_ERR_INVALID_ARG;
     if (r->rot_dim < 0 || r->rot_dim > v.head_dim || !(r->eps >= 0.0) || !std::isfinite(r->eps)) return MVLA_ERR_INVALID_ARG;
     if (r->rot_dim % 16 != 0) return MVLA_ERR_UNSUPPORTED;
-    if (r->rot_dim > 0 && r->n_rows > 0 && (!r->pos || !r->inv_freq)) return MVLA_ERR_INVALID_ARG;
+    if (r->n_rows == 0) return MVLA_OK;                    // (tensors without rows may have no address where their outputs, a cache, have one)
+    if (r->rot_dim > 0 && (!r->pos || !r->inv_freq)) return MVLA_ERR_INVALID_ARG;
     if (!aligned(r->pos, 4) || !aligned(r->out_rows, 4) || !aligned(r->inv_freq, 8)) return MVLA_ERR_INVALID_ARG;
     if (!(r->flags & MVLA_ROPE_NORM) && (r->q_weight || r->k_weight)) return MVLA_ERR_INVALID_ARG;
     if (!aligned(r->q_weight, 16) || !aligned(r->k_weight, 16)) return MVLA_ERR_INVALID_ARG;
@@ -82,7 +83,7 @@ inline int32_t check_rope(const ServeShape& v, const mvla_qk_rope* r)
         const int64_t width = static_cast<int64_t>(i ? v.kv_heads : v.n_heads) * v.head_dim;
         if ((in[i] == nullptr) != (out[i] == nullptr)) return MVLA_ERR_INVALID_ARG;
         ri[i] = ro[i] = Range{nullptr, nullptr};
-        if (!in[i] || r->n_rows == 0) continue;
+        if (!in[i]) continue;
         if (!aligned(in[i], 16) || !aligned(out[i], 16) || stride[i] < 0 || stride[i] > kMaxStride || (r->n_rows > 1 && stride[i] < width) ||
             stride[i] * wide % 16 != 0)
             return MVLA_ERR_INVALID_ARG;

@@ -1,0 +1,28 @@
+"""The calls around the prune point at the ends of what they accept, as a program makes them."""
+import pytest
+import torch
+
+from test_gpu_serve import TYPES, bits, context, randn
+import serve_util as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32", "fp8"])
+def test_rows_of_an_empty_batch_into_a_cache(dtype):
+    """A batch without tokens goes the way of every other one: nothing is written."""
+    H, G, d = 8, 2, 64
+    ctx = context(dtype, H, G, d)
+    gen = torch.Generator("cuda").manual_seed(1)
+    wide = R.WIDE[TYPES[dtype]]
+    qkv = randn(gen, 0, (H + 2 * G) * d, dtype=wide)
+    q, k, v = (x.unflatten(1, (-1, d)) for x in qkv.split([H * d, G * d, G * d], 1))
+    kc, vc = (randn(gen, 50, G, d, dtype=TYPES[dtype]) for _ in range(2))
+    k0, v0 = kc.clone(), vc.clone()
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    freq = torch.ones(d // 2, dtype=torch.float64, device="cuda")
+    q_out, ko, vo = ctx.qk_norm_rope(q, k, none, freq, v=v, k_out=kc, v_out=vc, out_rows=none)
+    assert q_out.shape == (0, H, d) and ko is kc and vo is vc
+    torch.cuda.synchronize()
+    assert torch.equal(bits(kc), bits(k0)) and torch.equal(bits(vc), bits(v0))
+    ctx.close()
