@@ -451,7 +451,7 @@ typedef struct mvla_attention {
                                       between replays; values are taken into [0, n_kv] */
     int32_t window;                /* >= 1; MVLA_WINDOW_ALL: everything before a query is visible */
     int32_t n_sink;                /* >= 0: positions below it stay visible outside the window */
-    double scale;                  /* of the dot products; 0: 1 / sqrt(head_dim) */
+    double scale;                  /* of the dot products; 0: 1 / sqrt(head_dim).  1e-38 to 2e38; products have to stay within 32 bits with it */
     void *out;                     /* [q_rows, n_heads, head_dim], hidden type */
     float *lse;                    /* [q_rows, n_heads] natural logarithm of the sum of exponentials, nullable */
     float *mass;                   /* [kv_rows] accumulated attention weights, nullable: added to */

@@ -3,7 +3,6 @@
 #include "serve.h"
 #include "serve_checks.h"
 
-#include <cmath>
 #include <cstring>
 
 using namespace mvla;
@@ -107,7 +106,7 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     k.n_heads = v.n_heads; k.kv_heads = v.kv_heads; k.head_dim = v.head_dim; k.window = a->window;
     // (no window: the one distance that is not below MVLA_WINDOW_ALL, from the last position that there is to the first, is a sink's)
     k.n_sink = a->window == MVLA_WINDOW_ALL && a->n_sink == 0 ? 1 : a->n_sink;
-    k.scale_log2 = static_cast<float>((a->scale > 0.0 ? a->scale : 1.0 / std::sqrt(static_cast<double>(v.head_dim))) * 1.4426950408889634);   // log2 e
+    k.scale_log2 = static_cast<float>(scale_log2(v, a));
     k.n_seq = batch; k.n_blocks = static_cast<int32_t>(plan.blocks);
     k.total_q = static_cast<int32_t>(plan.total_q); k.total_kv = static_cast<int32_t>(plan.total_kv);
     k.splits = plan.splits; k.mass_parts = plan.mass_parts; k.pack = plan.pack; k.status = v.status_dev;

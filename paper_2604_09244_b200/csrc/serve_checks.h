@@ -4,6 +4,7 @@
 #include "attend_plan.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 
 namespace mvla {
@@ -104,11 +105,19 @@ inline int32_t check_rope(const ServeShape& v, const mvla_qk_rope* r)
 
 // ---- windowed attention
 
+// The scale of the dot products in powers of two, as the kernels take it.
+inline double scale_log2(const ServeShape& v, const mvla_attention* a)
+{
+    return (a->scale > 0.0 ? a->scale : 1.0 / std::sqrt(static_cast<double>(v.head_dim))) * 1.4426950408889634;       // log2 e
+}
+
 inline int32_t check_attention(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a)
 {
     const int32_t rc = check_batch(v, batch, seqs);
     if (rc != MVLA_OK) return rc;
-    if (a->window < 1 || a->n_sink < 0 || !(a->scale >= 0.0) || !std::isfinite(a->scale)) return MVLA_ERR_INVALID_ARG;
+    if (a->window < 1 || a->n_sink < 0 || !(a->scale >= 0.0)) return MVLA_ERR_INVALID_ARG;
+    // (a normal number of 32 bits: zero times the -infinity of a row that is not seen is no number)
+    if (!(scale_log2(v, a) >= FLT_MIN && scale_log2(v, a) <= FLT_MAX)) return MVLA_ERR_INVALID_ARG;
     if (a->kv_pos && !a->q_pos) return MVLA_ERR_INVALID_ARG;
     if (a->q_rows < 0 || a->kv_rows < 0 || a->q_rows > kMaxTensorRows || a->kv_rows > kMaxTensorRows) return MVLA_ERR_INVALID_ARG;
     if (v.kv_heads > 65535) return MVLA_ERR_UNSUPPORTED;

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from test_gpu_serve import TYPES, bits, context, randn
+from test_gpu_serve import TYPES, attend_case, bits, check_attention, context, randn
 import serve_util as R
 
 pytestmark = pytest.mark.gpu
@@ -25,4 +25,14 @@ def test_rows_of_an_empty_batch_into_a_cache(dtype):
     assert q_out.shape == (0, H, d) and ko is kc and vo is vc
     torch.cuda.synchronize()
     assert torch.equal(bits(kc), bits(k0)) and torch.equal(bits(vc), bits(v0))
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype,n_q", [("bf16", 1), ("bf16", 40), ("fp32", 1), ("fp32", 40), ("fp8", 1), ("fp8", 40)])
+def test_attention_with_the_smallest_scale(dtype, n_q):
+    """All logits are nothing: the mean of the visible values, and rows that are not seen stay out of it."""
+    ctx = context(dtype, 4, 2, 128)
+    for scale in (1e-38, 1e-30):
+        args, mass, kept = attend_case(dtype, 4, 2, 128, [n_q, n_q], [n_q + 100, n_q], 60, 2, "filled", seed=1, scale=scale)
+        check_attention(ctx, args, mass, kept)
     ctx.close()

@@ -14,3 +14,10 @@ def test_no_rows_are_nothing_to_do_whatever_the_outputs_are(shim, dtype):  # noq
         assert shim.rope(dtype, 8, 4, 64, C.byref(rope_args(n_rows=0, **kw))) == OK
     for kw in (dict(rot_dim=80), dict(flags=4), dict(eps=-1.0), dict(kv_rows=-1)):       # (the numbers are looked at all the same)
         assert shim.rope(dtype, 8, 4, 64, C.byref(rope_args(n_rows=0, q=None, **kw))) == BAD
+
+
+@pytest.mark.parametrize("want,scale", [(OK, 1e-38), (OK, 1.0), (OK, 2e38), (BAD, 1e-39), (BAD, 1e-300), (BAD, 3e38), (BAD, 1e300), (BAD, float("inf")),
+                                        (BAD, float("nan"))])
+def test_scales_that_32_bits_do_not_hold(shim, want, scale):  # noqa: F811
+    for dtype in (BF16, FP32, FP8):
+        assert attention_call(shim, ONE, dtype, scale=scale)[0] == want
