@@ -480,7 +480,8 @@ int32_t mvla_window_attention_workspace(mvla_ctx *ctx, int32_t batch, const mvla
                                         int64_t *bytes);
 
 typedef struct mvla_eviction {
-    void *k, *v;                   /* device, context type, 16-byte aligned: rows move in place */
+    void *k, *v;                   /* device, context type, 16-byte aligned: rows move in place.  (These and the four arrays below are
+                                      nullable where kv_rows is 0) */
     int64_t kv_rows;
     const int32_t *pos;            /* [kv_rows] positions, negative: a row that nobody sees */
     const float *mass;             /* [kv_rows] accumulated weights (mvla_window_attention) */

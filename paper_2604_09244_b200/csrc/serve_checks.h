@@ -200,7 +200,8 @@ inline int32_t check_eviction(const ServeShape& v, int32_t batch, const mvla_seq
 
 inline int32_t check_eviction_memory(const ServeShape& v, int32_t batch, const mvla_eviction* a, const EvictPlan& plan)
 {
-    if (!a->k || !a->v || !a->pos || !a->mass || !a->pos_out || !a->mass_out) return MVLA_ERR_INVALID_ARG;
+    // (a cache without rows may have no address: then only its lengths, which are zero, are written)
+    if (a->kv_rows > 0 && (!a->k || !a->v || !a->pos || !a->mass || !a->pos_out || !a->mass_out)) return MVLA_ERR_INVALID_ARG;
     if (!aligned(a->k, 16) || !aligned(a->v, 16) || !aligned(a->pos, 4) || !aligned(a->mass, 4) || !aligned(a->pos_out, 4) || !aligned(a->mass_out, 4) ||
         !aligned(a->kept_idx, 4) || !aligned(a->kv_len, 4) || !aligned(a->kv_len_out, 4) || !aligned(a->workspace, 256))
         return MVLA_ERR_INVALID_ARG;

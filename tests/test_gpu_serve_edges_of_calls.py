@@ -4,6 +4,7 @@ import torch
 
 from test_gpu_serve import TYPES, attend_case, bits, check_attention, context, randn
 import serve_util as R
+from paper_2604_09244_b200.mvla import Seq
 
 pytestmark = pytest.mark.gpu
 
@@ -35,4 +36,17 @@ def test_attention_with_the_smallest_scale(dtype, n_q):
     for scale in (1e-38, 1e-30):
         args, mass, kept = attend_case(dtype, 4, 2, 128, [n_q, n_q], [n_q + 100, n_q], 60, 2, "filled", seed=1, scale=scale)
         check_attention(ctx, args, mass, kept)
+    ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32", "fp8"])
+def test_eviction_from_a_cache_without_rows(dtype):
+    """Nothing is cached yet: nothing moves, and no rows stay."""
+    ctx = context(dtype, 2, 2, 64)
+    k, v = (torch.zeros(0, 2, 64, device="cuda").to(TYPES[dtype]) for _ in range(2))
+    pos, mass = torch.zeros(0, dtype=torch.int32, device="cuda"), torch.zeros(0, device="cuda")
+    left = torch.full((2,), 7, dtype=torch.int32, device="cuda")
+    for kv_len in (None, torch.tensor([3, -1], dtype=torch.int32, device="cuda")):
+        ctx.cache_evict([Seq(budget=5), Seq(budget=9)], k, v, pos, mass, n_sink=1, n_recent=4, kv_len=kv_len, kv_len_out=left.fill_(7))
+        assert left.tolist() == [0, 0]
     ctx.close()

@@ -21,3 +21,12 @@ def test_no_rows_are_nothing_to_do_whatever_the_outputs_are(shim, dtype):  # noq
 def test_scales_that_32_bits_do_not_hold(shim, want, scale):  # noqa: F811
     for dtype in (BF16, FP32, FP8):
         assert attention_call(shim, ONE, dtype, scale=scale)[0] == want
+
+
+def test_eviction_from_a_cache_without_rows(shim):  # noqa: F811
+    none = dict(k=None, v=None, pos=None, mass=None, pos_out=None, mass_out=None)
+    assert eviction_call(shim, [dict(n_kv=0, budget=5)], kv_rows=0, **none) == OK
+    assert eviction_call(shim, [dict(n_kv=0, budget=5)] * 2, kv_rows=0, kv_len=6 * MB, kv_len_out=6 * MB, **none) == OK
+    assert eviction_call(shim, [dict(n_kv=1, budget=5)], kv_rows=0, **none) == BAD
+    for name in none:                                        # of a cache with rows everything is needed, whether the sequences have any or not
+        assert eviction_call(shim, [dict(n_kv=0, budget=5)], **{name: None}) == BAD
