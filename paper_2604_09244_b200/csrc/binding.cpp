@@ -466,6 +466,20 @@ bool strided_rows(PyObject* o, const char* name, const Shape& c, int64_t heads, 
     return on_device(t, name, c.device);
 }
 
+// An object that is held until the scope ends, by an exception too (memory for an output may run out).
+struct Held {
+    PyObject* o;
+    explicit Held(PyObject* held) : o(held) { Py_XINCREF(o); }
+    ~Held() { Py_XDECREF(o); }
+    Held(const Held&) = delete;
+    Held& operator=(const Held&) = delete;
+    void take(PyObject* fresh)                               // instead of what it holds; a reference of the caller's
+    {
+        Py_XDECREF(o);
+        o = fresh;
+    }
+};
+
 // qk_norm_rope(ctx, dtype, heads, kv_heads, dim, device, q, k, v, pos, inv_freq, q_weight, k_weight, flags, eps, q_out, k_out, v_out,
 //   out_rows, stream) -> (status, q_out, k_out, v_out); an output that is missing beside its input is allocated
 PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
@@ -507,29 +521,22 @@ PyObject* py_qk_norm_rope(PyObject*, PyObject* const* a, Py_ssize_t n)
     r.rot_dim = tf ? static_cast<int32_t>(2 * tf->size(0)) : 0;
     r.flags = static_cast<uint32_t>(flags);
     r.out_rows = static_cast<const int32_t*>(to);
-    PyObject* outs[3] = {a[15], a[16], a[17]};
-    for (int i = 0; i < 3; ++i) Py_INCREF(outs[i]);
+    Held outs[3] = {Held(a[15]), Held(a[16]), Held(a[17])};
     const at::Tensor* const given[3] = {tqo, tko, tvo};
     void* ptr[3] = {qo, ko, vo};
     int64_t kv_rows = tko ? tko->size(0) : tvo ? tvo->size(0) : rows;
-    bool ok = true;
-    for (int i = 0; i < 3 && ok; ++i) {
+    for (int i = 0; i < 3; ++i) {
         if (given[i] || a[6 + i] == Py_None) continue;
         const at::Tensor t = fresh_on({i ? kv_rows : rows, i ? c.kv_heads : c.heads, c.dim}, c.kept, c.device, a[19], st);
         ptr[i] = t.data_ptr();
-        Py_DECREF(outs[i]);
-        ok = (outs[i] = THPVariable_Wrap(t)) != nullptr;
+        outs[i].take(THPVariable_Wrap(t));
+        if (!outs[i].o) return nullptr;
     }
-    PyObject* ret = nullptr;
-    if (ok) {
-        r.q_out = ptr[0]; r.k_out = ptr[1]; r.v_out = ptr[2];
-        r.kv_rows = kv_rows;
-        mvla_ctx* ctx = ctx_of(a[0]);
-        const int32_t rc = unlocked([&] { return mvla_qk_norm_rope(ctx, &r, st); });
-        ret = Py_BuildValue("(iOOO)", rc, outs[0], outs[1], outs[2]);
-    }
-    for (int i = 0; i < 3; ++i) Py_XDECREF(outs[i]);
-    return ret;
+    r.q_out = ptr[0]; r.k_out = ptr[1]; r.v_out = ptr[2];
+    r.kv_rows = kv_rows;
+    mvla_ctx* ctx = ctx_of(a[0]);
+    const int32_t rc = unlocked([&] { return mvla_qk_norm_rope(ctx, &r, st); });
+    return Py_BuildValue("(iOOO)", rc, outs[0].o, outs[1].o, outs[2].o);
     MVLA_CATCH
 }
 

@@ -50,3 +50,28 @@ def test_eviction_from_a_cache_without_rows(dtype):
         ctx.cache_evict([Seq(budget=5), Seq(budget=9)], k, v, pos, mass, n_sink=1, n_recent=4, kv_len=kv_len, kv_len_out=left.fill_(7))
         assert left.tolist() == [0, 0]
     ctx.close()
+
+
+def test_memory_that_runs_out_between_two_outputs():
+    """The first output, and what the caller gave, are let go when there is no memory for the next one."""
+    ctx = context("bf16", 32, 32, 128)
+    rows = 16384                                             # 128 MB to an output
+    q, k = (torch.zeros(rows, 32, 128, device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    pos = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    freq = torch.ones(64, dtype=torch.float64, device="cuda")
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    total = torch.cuda.mem_get_info()[1]
+    before = torch.cuda.memory_allocated()
+    try:
+        torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (192 << 20)) / total)
+        for _ in range(2):
+            with pytest.raises(RuntimeError):
+                ctx.qk_norm_rope(q, k, pos, freq)
+            assert torch.cuda.memory_allocated() == before
+        ctx.qk_norm_rope(q, None, pos, freq)                 # one output fits
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert torch.cuda.memory_allocated() == before
+    ctx.qk_norm_rope(q, k, pos, freq)
+    ctx.close()
