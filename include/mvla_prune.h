@@ -422,7 +422,8 @@ typedef struct mvla_qk_rope {
     const double *inv_freq;        /* [rot_dim / 2] radians per position, 64 bits: angles of far positions lose their meaning in 32 */
     int32_t rot_dim;               /* leading elements of a head that are rotated: a multiple of 16, at most head_dim; 0: none */
     uint32_t flags;                /* MVLA_ROPE_* */
-    double eps;                    /* of the norm, >= 0 */
+    double eps;                    /* of the norm, >= 0; added in 32 bits, at least 1.2e-38 where it is not zero.  Sums of squares are taken in
+                                      32 bits: elements up to 1e18 */
     void *q_out;                   /* [n_rows, n_heads, head_dim], context type; nullable with q */
     void *k_out, *v_out;           /* [kv_rows, n_kv_heads, head_dim], context type: a cache, or packed rows; nullable with k, v */
     const int32_t *out_rows;       /* [n_rows] row of k_out / v_out that row i goes to, nullable (row i).  A row outside

@@ -26,7 +26,7 @@ int32_t rope_impl(mvla_ctx* ctx, const mvla_qk_rope* r, void* stream)
     job.pos = r->pos; job.inv_freq = r->inv_freq; job.out_rows = r->out_rows;
     job.q_out = r->q_out; job.k_out = r->k_out; job.v_out = r->v_out;
     job.n_heads = v.n_heads; job.kv_heads = v.kv_heads; job.head_dim = v.head_dim; job.rot_dim = r->rot_dim;
-    job.eps = static_cast<float>(r->eps);
+    job.eps = norm_eps(r->eps);
     job.norm = (r->flags & MVLA_ROPE_NORM) != 0;
     job.interleaved = (r->flags & MVLA_ROPE_INTERLEAVED) != 0;
     return close_call(ctx, launch_qk_norm_rope(v.dtype, job, static_cast<cudaStream_t>(stream)));

@@ -58,6 +58,14 @@ inline int32_t check_batch(const ServeShape& v, int32_t batch, const mvla_seq* s
 
 // ---- norms and rotation
 
+// The norm's constant as the kernel takes it: where it is not zero, no smaller than the normal numbers of 32 bits (a row of zeros stays zeros), and infinite
+// above them (all that is normed is nothing then).
+inline float norm_eps(double eps)
+{
+    if (eps > FLT_MAX) return HUGE_VALF;
+    return eps > 0.0 ? std::max(static_cast<float>(eps), FLT_MIN) : 0.f;
+}
+
 inline int32_t check_rope(const ServeShape& v, const mvla_qk_rope* r)
 {
     if (r->n_rows < 0 || r->n_rows > 0x7FFFFFFF || r->kv_rows < 0 || r->kv_rows > kMaxTensorRows ||

@@ -75,3 +75,21 @@ def test_memory_that_runs_out_between_two_outputs():
     assert torch.cuda.memory_allocated() == before
     ctx.qk_norm_rope(q, k, pos, freq)
     ctx.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32", "fp8"])
+def test_norms_of_rows_of_zeros(dtype):
+    """However small the constant is, a row of zeros stays one; the others are normed as if it were not there."""
+    ctx = context(dtype, 4, 2, 64)
+    gen = torch.Generator("cuda").manual_seed(2)
+    wide = R.WIDE[TYPES[dtype]]
+    q, k = randn(gen, 20, 4, 64, dtype=wide), randn(gen, 20, 2, 64, dtype=wide)
+    q[3], k[7], q[5, 1] = 0, 0, 0
+    pos = torch.arange(20, dtype=torch.int32, device="cuda")
+    freq = 10000.0 ** (-torch.arange(0, 64, 2, device="cuda", dtype=torch.float64) / 64)
+    for eps in (1e-300, 1e-45, 1e-39, 1e-6, 1e30, 1e300):
+        qo, ko, _ = ctx.qk_norm_rope(q, k, pos, freq, eps=eps)
+        for x, got in ((q, qo), (k, ko)):
+            z, size = R.rope(x, pos, freq, None, True, eps, False)
+            assert bool(((got.double() - z).abs() <= R.rope_tolerance(z, size, TYPES[dtype], 20)).all()), eps
+    ctx.close()
