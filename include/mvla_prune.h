@@ -393,9 +393,11 @@ int32_t mvla_patch_select(mvla_ctx *ctx, int32_t prune_point, int32_t batch, con
 /*
  * ---- Around the prune point: what makes the rows that pruning scores, attends over the rows that survive, and keeps the cache
  * small while action tokens are decoded.  (The paper has no counterpart: its host model does these.)  The calls use the context's
- * device, type, heads and head_dim; they are stateless and touch no prune state.  q is [rows, n_heads, head_dim], keys and values
- * are [rows, n_kv_heads, head_dim] as above.  A cache is such a pair of tensors; a sequence owns a run of its rows.  Rows of hidden
- * states and of attention outputs have the context's hidden type (fp32 contexts: fp32, else bf16).
+ * device, type, heads and head_dim; they are stateless and touch no prune state.  (Like a stage call, one that enqueues work ends the
+ * overlap of MVLA_FLAG_INPUTS_STABLE: the next prune step is ordered after everything enqueued so far, those behind it overlap again.)
+ * q is [rows, n_heads, head_dim], keys and values are [rows, n_kv_heads, head_dim] as above.  A cache is such a pair of tensors; a
+ * sequence owns a run of its rows.  Rows of hidden states and of attention outputs have the context's hidden type (fp32 contexts:
+ * fp32, else bf16).
  */
 
 /* One sequence of a batch (host array). */

@@ -786,16 +786,16 @@ int32_t prune_step_patch(mvla_ctx* ctx, int32_t prune_point, int32_t batch, cons
 }  // namespace
 
 namespace mvla {
-int32_t open_call(mvla_ctx* ctx, bool enqueues, CtxView* view)
+int32_t open_call(mvla_ctx* ctx, CtxView* view)
 {
     const int32_t rc = check_sticky(ctx);
     if (rc != MVLA_OK) return rc;
-    if (enqueues) ctx->hist_unknown = true;          // what the stream ran last is no longer a known prune step
     const mvla_config& c = ctx->cfg;
     *view = CtxView{{c.dtype, ctx->hidden_dtype, c.n_heads, ctx->kv_heads, c.head_dim, c.max_batch, ctx->sm_count, ctx->qk_elem, ctx->elem},
                     c.device, ctx->status_dev, ctx->encode};
     return MVLA_OK;
 }
+void note_work(mvla_ctx* ctx) { ctx->hist_unknown = true; }
 int32_t close_call(mvla_ctx* ctx, cudaError_t e) { return e == cudaSuccess ? MVLA_OK : fail_cuda(ctx, e); }
 }  // namespace mvla
 

@@ -56,9 +56,11 @@ struct CtxView : ServeShape {
     int* status_dev;                    // word that a kernel whose bounded wait gave up writes
     PFN_cuTensorMapEncodeTiled_v12000 encode;
 };
-// Opens such a call: the sticky status, and the note that the stream now runs other work than prune steps (`enqueues`: false for
-// a call that only looks at sizes).
-int32_t open_call(mvla_ctx* ctx, bool enqueues, CtxView* view);
+// Opens such a call: the sticky status.
+int32_t open_call(mvla_ctx* ctx, CtxView* view);
+// The call enqueues work: what the stream ran last is no longer a known prune step, and the next one with stable inputs is ordered after all of it.  (Not
+// for a call that is refused or has nothing to do: the overlap of the prune steps around it stays.)
+void note_work(mvla_ctx* ctx);
 int32_t close_call(mvla_ctx* ctx, cudaError_t e);      // status of the call's launches
 
 }  // namespace mvla

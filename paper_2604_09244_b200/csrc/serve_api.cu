@@ -13,12 +13,13 @@ int32_t rope_impl(mvla_ctx* ctx, const mvla_qk_rope* r, void* stream)
 {
     if (!ctx || !r) return MVLA_ERR_INVALID_ARG;
     CtxView v;
-    int32_t rc = open_call(ctx, true, &v);
+    int32_t rc = open_call(ctx, &v);
     if (rc == MVLA_OK) rc = check_rope(v, r);
     if (rc != MVLA_OK) return rc;
     if (r->n_rows == 0 || (!r->q && !r->k && !r->v)) return MVLA_OK;
     DeviceGuard guard(v.device);
     if (!guard.ok) return MVLA_ERR_CUDA;
+    note_work(ctx);
     RopeJob job;
     std::memset(&job, 0, sizeof job);
     job.q = r->q; job.k = r->k; job.v = r->v; job.q_weight = r->q_weight; job.k_weight = r->k_weight;
@@ -36,7 +37,7 @@ int32_t workspace_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
 {
     if (!ctx || !a || !bytes) return MVLA_ERR_INVALID_ARG;
     CtxView v;
-    int32_t rc = open_call(ctx, false, &v);
+    int32_t rc = open_call(ctx, &v);
     if (rc == MVLA_OK) rc = check_attention(v, batch, seqs, a);
     if (rc != MVLA_OK) return rc;
     *bytes = plan_of(v, batch, seqs, a).bytes;
@@ -90,7 +91,7 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
 {
     if (!ctx || !a) return MVLA_ERR_INVALID_ARG;
     CtxView v;
-    int32_t rc = open_call(ctx, true, &v);
+    int32_t rc = open_call(ctx, &v);
     if (rc == MVLA_OK) rc = check_attention(v, batch, seqs, a);
     if (rc != MVLA_OK) return rc;
     const AttendPlan plan = plan_of(v, batch, seqs, a);
@@ -99,6 +100,7 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     if (rc != MVLA_OK) return rc;
     DeviceGuard guard(v.device);
     if (!guard.ok) return MVLA_ERR_CUDA;
+    note_work(ctx);
     AttArgs k;
     std::memset(&k, 0, sizeof k);
     k.q = a->q; k.k = a->k; k.v = a->v; k.out = a->out; k.lse = a->lse; k.mass = a->mass;
@@ -157,7 +159,7 @@ int32_t evict_workspace_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs,
 {
     if (!ctx || !a || !bytes) return MVLA_ERR_INVALID_ARG;
     CtxView v;
-    int32_t rc = open_call(ctx, false, &v);
+    int32_t rc = open_call(ctx, &v);
     if (rc == MVLA_OK) rc = check_eviction(v, batch, seqs, a);
     if (rc != MVLA_OK) return rc;
     *bytes = plan_evict(batch, seqs).bytes;
@@ -168,7 +170,7 @@ int32_t evict_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvl
 {
     if (!ctx || !a) return MVLA_ERR_INVALID_ARG;
     CtxView v;
-    int32_t rc = open_call(ctx, true, &v);
+    int32_t rc = open_call(ctx, &v);
     if (rc == MVLA_OK) rc = check_eviction(v, batch, seqs, a);
     if (rc != MVLA_OK) return rc;
     const EvictPlan plan = plan_evict(batch, seqs);
@@ -176,6 +178,7 @@ int32_t evict_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvl
     if (rc != MVLA_OK) return rc;
     DeviceGuard guard(v.device);
     if (!guard.ok) return MVLA_ERR_CUDA;
+    note_work(ctx);
     EvictArgs k;
     std::memset(&k, 0, sizeof k);
     k.k = a->k; k.v = a->v;

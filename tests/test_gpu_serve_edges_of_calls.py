@@ -4,7 +4,11 @@ import torch
 
 from test_gpu_serve import TYPES, attend_case, bits, check_attention, context, randn
 import serve_util as R
+from cuda.bindings import runtime as cudart
+from paper_2604_09244_b200 import mvla
+from paper_2604_09244_b200 import workloads as W
 from paper_2604_09244_b200.mvla import Seq
+from parity_util import device_tensors
 
 pytestmark = pytest.mark.gpu
 
@@ -93,3 +97,57 @@ def test_norms_of_rows_of_zeros(dtype):
             z, size = R.rope(x, pos, freq, None, True, eps, False)
             assert bool(((got.double() - z).abs() <= R.rope_tolerance(z, size, TYPES[dtype], 20)).all()), eps
     ctx.close()
+
+
+def test_calls_that_enqueue_nothing_leave_the_overlap_of_prune_steps():
+    """Steps with the promise of stable inputs are ordered by events of their own; after other work of the context they wait for all of it once more.
+    A call that is refused or has nothing to do is no such work: the captured steps depend on one another as if it had not been made."""
+    wl = W.small_workload(7, batch=2, D=256, H=4, d=64, dtype="bf16", n_txt=(9, 17), n_2d=(90, 130), n_3d=(80, 60), cold_start=0)
+    dev = device_tensors(wl)
+    rows = dev["hidden"].shape[0]
+    q, k, v = dev["q"], dev["k"], dev["v"]
+    pos = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    freq = torch.ones(32, dtype=torch.float64, device="cuda")
+    weights = torch.zeros(rows, device="cuda")
+
+    def refused(ctx):
+        with pytest.raises(mvla.MvlaError):
+            ctx.window_attention([Seq(n_q=rows + 1, n_kv=rows)], q, k, v)
+        with pytest.raises(mvla.MvlaError):
+            ctx.qk_norm_rope(q, None, pos, freq[:5])
+        with pytest.raises(mvla.MvlaError):
+            ctx.cache_evict([Seq(n_kv=10, budget=5)], k, v, pos, weights, n_sink=4, n_recent=4)
+
+    def empty(ctx):
+        ctx.qk_norm_rope(q[:0], None, pos[:0], freq)
+        ctx.window_attention([Seq(n_kv=rows)], q, k, v)
+
+    def work(ctx):
+        ctx.qk_norm_rope(q, None, pos, freq, q_out=torch.empty_like(q))
+
+    def dependencies(between):
+        ctx = mvla.context_for(wl)
+        outs = [ctx.alloc_outputs(wl.samples, extras=True) for _ in range(11)]      # (a step in flight that writes the same buffers would be waited for)
+
+        def step(i):
+            ctx.prune_step(0, wl.samples, wl.mode, q, k, v, dev["hidden"], flags=mvla.FLAG_INPUTS_STABLE, out=outs[i])
+        for i in range(8):
+            step(i)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph(keep_graph=True)
+        with torch.cuda.graph(graph):
+            for i in range(8):
+                step(i)
+            between(ctx)
+            for i in range(8, 11):
+                step(i)
+        raw = graph.raw_cuda_graph()
+        rc, _, n = cudart.cudaGraphGetNodes(raw)
+        rc, nodes, n = cudart.cudaGraphGetNodes(raw, n)
+        place = {int(x): i for i, x in enumerate(nodes)}
+        edges = cudart.cudaGraphGetEdges_v2(raw, cudart.cudaGraphGetEdges_v2(raw)[-1])
+        ctx.close()
+        return n, sorted((place[int(a)], place[int(b)]) for a, b in zip(edges[1], edges[2]))
+    plain = dependencies(lambda ctx: None)
+    assert plain[0] >= 22 and dependencies(refused) == plain and dependencies(empty) == plain
+    assert dependencies(work) != plain
