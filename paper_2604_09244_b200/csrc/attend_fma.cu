@@ -10,6 +10,7 @@
 // B200: 208 rows of 8 heads of 64, window 64: 18 us (of it about 9 the launch and three tiles' latencies).  1500 rows of 32 + 8 heads of
 // 128, everything before a row visible: 720 us, 26 TFLOP/s, bound by the FMAs and the reads of shared memory beside them.  One token
 // over 30000 rows of 32 heads of 128: 252 us, 3.9 TB/s.  The weights of the 1500 rows: 400 us more, 1340 when every key's rows were one CTA's.
+// (Blocks of 8 rows of heads above 192 elements spill 24 bytes.)
 #include "attend.cuh"
 #include "f32x2.cuh"
 

@@ -11,8 +11,8 @@
 // Heads of up to 128 elements leave room for two CTAs to a multiprocessor (256 columns of tensor memory, 97 KB of shared memory each):
 // one's exponentials, prologue and epilogue lie beside the other's MMAs.  Measured on 8192 queries, 16 heads of 128 in groups of 4, and on
 // 16 x 808 queries of 32 heads, window 512: two tiles of rows in one CTA with tiles of 128 keys 295 / 250 us, this 291 / 189.
-// Now 306 us (900 TFLOP/s; the MMAs alone 235, without the exponentials 286: reads of shared memory by 64-key MMAs, and the chain from scores to
-// weights) and 195 + 135 for the weights.  Single tokens without weights come here too: 131072 rows of 8 heads of 128 99.9 us, 5.4 TB/s.
+// Now 305 us (900 TFLOP/s; copies of the kernel without all but the MMAs 235, without the exponentials 286: reads of shared memory by 64-key MMAs, and
+// the chain from scores to weights; the tensor cores are busy half of the time, and so are the pipes of the exponentials) and 195 + 135 for the weights.  Single tokens without weights come here too: 131072 rows of 8 heads of 128 99.9 us, 5.4 TB/s.
 // Positions that are counted tell every warp which tiles to visit and which need their mask; where they are data, a list of the
 // tiles is made first.  Keys that no row of the tile sees have their values set to zero in shared memory (0 times NaN is NaN).
 #include "attend.cuh"
@@ -474,6 +474,8 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                     y = ex2_approx(y);
                     z = ex2_approx(z);
                     sums[c / 2 & 1] = add_f32x2(sums[c / 2 & 1], two_f32(y, z));
+                    // (rounded for the product alone: the sum, which the logarithm is taken of too, is of the weights as they are.  Against 64 bits
+                    // 8192 x 8192 causal is off by 2.17e-3, of which the rounding of the output to bf16 is 1.65e-3)
                     w[c / 2] = F16 ? two_f16(y, z) : two_bf16(y, z);
                     if (TOKENS && twin) w[c / 2] = two_bf16(y - __uint_as_float(w[c / 2] << 16), z - __uint_as_float(w[c / 2] & 0xFFFF0000u));
                 }
@@ -548,7 +550,8 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
 // attend_weights_kernel: mass of 128 cached rows over the queries of their sequence, for the heads packed together.  Keys on the lanes
 // of tensor memory, queries on its columns: S^T = K Q^T, and a thread adds up 2^(S - lse) over the columns of its key, so that
 // no sum crosses threads.  Tiles of 128 query rows go to the two groups of four warps in turn, each with an S of its own; two CTAs to a
-// multiprocessor (heads of up to 128 elements).  Bound by the exponentials.
+// multiprocessor (heads of up to 128 elements; the 96 registers that leaves spill 16 bytes: 16 frames with weights 336 us, with one CTA and no spills 378).
+// Bound by the exponentials, whose pipe is busy half of the time (the tensor cores a fifth), and by the barriers between tiles.
 constexpr int kWeightStages = 2;
 
 template <int DB>

@@ -17,7 +17,8 @@
 // B200, one token each, with what follows the kernel: 16 requests over 500 to 4000 e4m3 rows of 8 heads of 128, window 2048, weights added up 43 us
 // (74 MB that have to be looked at; 680 instructions of a warp to 16 keys, of which the schedulers issue 0.42 a cycle: bound by their latency, 2.7
 // warps a scheduler); 60000 e4m3 rows of 32 heads 127 us, 3.9 TB/s; 16 requests over bf16 rows of 32 heads with weights 144 us, 4.1 TB/s.  Tiles of 32
-// e4m3 keys halve the CTAs that fit: 47 us instead of 44 (16 requests), 133 instead of 126 (60000 rows).
+// e4m3 keys halve the CTAs that fit: 47 us instead of 44 (16 requests), 133 instead of 126 (60000 rows).  (e4m3 heads of 96 with more than eight rows:
+// 20 bytes spill for the fourth CTA; nowhere else.)
 #include "attend.cuh"
 
 #include <cuda_fp16.h>

@@ -16,6 +16,7 @@
 // B200: 16 sequences one row over their budgets (one kernel) 8.3 us; 16 of 784 to 832 rows of 32 + 32 heads of 128 cut to three tenths 25 us, of it
 // 16 the move's 88 MB; 65537 rows of 8 + 8 heads cut to an eighth 37 us, of it 11 the move (with one CTA 300; reading all bins of all
 // CTAs, and taking the keys apart again for the second walk, 46).  Equal bins of a warp counted together: 54 (the atomics are not what it waits for).
+// The selection's 25 us of the last: seven barriers of the cluster are a quarter, the rest is eight multiprocessors going over 8192 rows each six times.
 #include "device_utils.cuh"
 #include "serve.h"
 
