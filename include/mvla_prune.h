@@ -402,9 +402,9 @@ int32_t mvla_patch_select(mvla_ctx *ctx, int32_t prune_point, int32_t batch, con
 
 /* One sequence of a batch (host array). */
 typedef struct mvla_seq {
-    int64_t q_row;             /* mvla_window_attention: first row of the sequence's queries in q, out, lse, q_pos */
-    int64_t kv_row;            /* first row of the sequence in the cache */
-    int32_t n_q;               /* mvla_window_attention: queries of this call; 0: none */
+    int64_t q_row;             /* mvla_window_attention, mvla_page_*: first row of the sequence's queries (new rows) in q, out, lse, q_pos, k, v */
+    int64_t kv_row;            /* first row of the sequence in the cache (not of mvla_page_*) */
+    int32_t n_q;               /* mvla_window_attention, mvla_page_*: queries (new rows) of this call; 0: none */
     int32_t n_kv;              /* cached rows, those of this call's queries among them; with kv_len the most there can be */
     int32_t budget;            /* mvla_cache_evict: rows that may stay */
     int32_t reserved0;
@@ -510,6 +510,87 @@ int32_t mvla_cache_evict(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, con
 
 /* Workspace bytes of a call with these arguments (pointers are not looked at). */
 int32_t mvla_cache_evict_workspace(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, const mvla_eviction *args, int64_t *bytes);
+
+/*
+ * ---- A cache in pages.  Sequences that grow beside one another own no run of rows: their rows lie in pages of a pool, named by a
+ * table, and may be kept in 8 or 4 bits.  Row j of sequence b (its cached rows are counted from 0) is row j % page_rows of page
+ * table[b][j / page_rows].  A page number outside the pool stands for a page of zeros; what is written there is dropped.  Rows beside the
+ * cache (queries, new keys and values, outputs) have the context's hidden type (fp32 contexts: fp32, else bf16).  Like the calls above
+ * these are stateless; they allocate nothing and may be captured.
+ */
+#define MVLA_PAGE_ROWS 0      /* elements of the hidden type */
+#define MVLA_PAGE_E4M3 1      /* e4m3, one scale for a row of a head */
+#define MVLA_PAGE_E2M1 2      /* e2m1, two to a byte (the even element in the low half), one scale for 32 elements */
+
+typedef struct mvla_pages {
+    void *k, *v;               /* device, 16-byte aligned: [n_pages, n_kv_heads, page_rows, head_dim] elements */
+    uint8_t *k_scale, *v_scale;    /* device, 16-byte aligned: a scale is 2^(byte - 127), 255: not a number.  E4M3: [n_pages, n_kv_heads, page_rows],
+                                  E2M1: [n_pages, n_kv_heads, page_rows, head_dim / 32], ROWS: null */
+    int64_t n_pages;           /* n_pages n_kv_heads below 2^31 */
+    int32_t page_rows;         /* 16, 32, 64, 128 or 256 */
+    int32_t kind;              /* MVLA_PAGE_* */
+} mvla_pages;
+
+typedef struct mvla_page_rows {
+    mvla_pages pages;
+    const int32_t *table;      /* DEVICE [batch][table_stride]: pages of every sequence, as many as its n_kv rows need (those behind are not read) */
+    int64_t table_stride;
+    const int32_t *kv_len;     /* DEVICE [batch], nullable: cached rows of every sequence, for captured calls whose caches grow between
+                                  replays; values are taken into [0, n_kv].  Null: n_kv */
+    void *k, *v;               /* device, hidden type, each nullable: rows [n_kv_heads, head_dim] contiguous, k_stride ... elements from one
+                                  row to the next; bases and strides multiples of 16 bytes */
+    int64_t rows;              /* rows of k and v */
+    int64_t k_stride, v_stride;
+} mvla_page_rows;
+
+/*
+ * Rows into pages.  Of every sequence (n_q, n_kv, q_row of its descriptor) row q_row + i of k / v becomes cached row n - n_q + i, i < n_q, n = n_kv or
+ * kv_len: the sequence's last rows, those of this call counted in n already.  (Rows before cached row 0 are dropped.)  Quantised pages:
+ *   scale = the least 2^e, -117 <= e, with max |x| <= 448 2^e (E4M3) or 6 2^e (E2M1);  element = x / scale, rounded to the nearest (ties to even)
+ * over the row of the head, or over each 32 elements.  (Above 2.5e38 elements are brought down to what the type holds with the
+ * largest scale, 2^119 or 2^125.)  What shares a scale with an element that is not finite becomes not a number.  No cached row may be written
+ * twice by a call.
+ */
+int32_t mvla_page_write(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, const mvla_page_rows *args, void *stream);
+
+/*
+ * The same rows out of the pages: cached row n - n_q + i becomes row q_row + i of k / v, in the hidden type (exact: element times scale; in bf16
+ * too).  To read rows [a, b) of a sequence give n_kv = b and n_q = b - a.  Rows before cached row 0 are zeros.  Sequences must not
+ * share rows of k / v (INVALID_ARG); other rows are left as they are.
+ */
+int32_t mvla_page_read(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, const mvla_page_rows *args, void *stream);
+
+typedef struct mvla_paged_attention {
+    mvla_pages pages;
+    const int32_t *table;      /* as above */
+    int64_t table_stride;
+    const int32_t *kv_len;     /* as above */
+    const void *q;             /* device, hidden type, 16-byte aligned: [q_rows, n_heads, head_dim] */
+    int64_t q_rows;
+    int32_t window;            /* >= 1; MVLA_WINDOW_ALL: everything before a query is visible */
+    int32_t n_sink;            /* >= 0: the first rows stay visible outside the window */
+    double scale;              /* of the dot products; 0: 1 / sqrt(head_dim) */
+    void *out;                 /* [q_rows, n_heads, head_dim], hidden type */
+    float *lse;                /* [q_rows, n_heads] natural logarithm of the sum of exponentials, nullable */
+    void *workspace;           /* device, 256-byte aligned; nullable where mvla_page_attention_workspace says 0 */
+    int64_t workspace_bytes;
+} mvla_paged_attention;
+
+/*
+ * Causal attention of the last n_q rows of every sequence over its pages, those rows' own keys and values among them (write them first).
+ * Positions are counted: query i has position p = n - n_q + i and sees row j where j <= p and (p - j < window or j < n_sink); query head h reads
+ * key head h / (n_heads / n_kv_heads).  out = softmax over the visible rows, times their values; scores, exponentials and sums in 32 bits, cached
+ * elements exact.  Weights are rounded for their product with the values as by mvla_window_attention for bf16 rows; sequences of at
+ * most 16 query rows to a key head over quantised pages: to fp16 in units of 2^-7 of the row's largest product of weight and scale (or less), and
+ * there groups of 32 e2m1 elements below 2^-27 of the largest scale of their row and head count as nothing.
+ * A query that sees nothing: out 0, lse -infinity.  What is cached must be finite in rows that some query of the sequence sees; other rows, the
+ * rest of the last page among them, may hold anything.  Rows of out and lse outside the sequences are left as they are; sequences must not share
+ * query rows, and may share pages.  Batches of up to max_batch sequences (CAPACITY).  The workspace: as by mvla_window_attention.
+ */
+int32_t mvla_page_attention(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, const mvla_paged_attention *args, void *stream);
+
+/* Workspace bytes of a call with these arguments (pointers are looked at only for being null). */
+int32_t mvla_page_attention_workspace(mvla_ctx *ctx, int32_t batch, const mvla_seq *seqs, const mvla_paged_attention *args, int64_t *bytes);
 
 /* Free everything the context owns.  NULL is accepted.  The caller must have
  * synchronised any stream that still runs work enqueued through the context. */

@@ -650,6 +650,148 @@ PyObject* py_cache_evict(PyObject*, PyObject* const* a, Py_ssize_t n)
     MVLA_CATCH
 }
 
+// A pool of pages as its four tensors (PagePool): keys, values, their scales.  The type of the elements says which kind it is.
+struct Pool {
+    mvla_pages p;
+    bool take(PyObject* const* a, const Shape& c)
+    {
+        std::memset(&p, 0, sizeof p);
+        const at::Tensor* t[4] = {};
+        void* ptr[4] = {};
+        for (int i = 0; i < 4; ++i)
+            if (!tensor_ptr(a[i], &ptr[i], &t[i]) || (t[i] && !on_device(*t[i], "pool", c.device))) return false;
+        if (!expect(t[0] && t[1], "pool: k and v are needed")) return false;
+        const at::ScalarType type = t[0]->scalar_type();
+        p.kind = type == at::kByte ? MVLA_PAGE_E2M1 : type == at::kFloat8_e4m3fn ? MVLA_PAGE_E4M3 : MVLA_PAGE_ROWS;
+        if (!expect(p.kind != MVLA_PAGE_ROWS || type == c.wide, "pool: elements of the context's row type, e4m3, or bytes of two e2m1") ||
+            !expect(t[0]->dim() == 4 && t[0]->size(1) == c.kv_heads && t[0]->size(3) == (p.kind == MVLA_PAGE_E2M1 ? c.dim / 2 : c.dim) &&
+                        t[1]->scalar_type() == type && t[1]->sizes() == t[0]->sizes(),
+                    "pool: k, v: [pages, heads, page rows, head_dim] (e2m1: head_dim / 2 bytes), alike") ||
+            !expect((p.kind == MVLA_PAGE_ROWS) == !t[2] && !t[2] == !t[3], "pool: scales beside quantised pages, and only there"))
+            return false;
+        for (int i = 2; i < 4; ++i)
+            if (t[i] && !expect(t[i]->scalar_type() == at::kByte && t[i]->dim() == (p.kind == MVLA_PAGE_E4M3 ? 3 : 4) && t[i]->size(0) == t[0]->size(0) &&
+                                    t[i]->size(1) == c.kv_heads && t[i]->size(2) == t[0]->size(2) && (p.kind == MVLA_PAGE_E4M3 || t[i]->size(3) == c.dim / 32),
+                                "pool: scales: bytes [pages, heads, page rows] (e2m1: and head_dim / 32)"))
+                return false;
+        if (!expect(t[0]->size(2) <= 0x7FFFFFFF, "pool: page rows out of range")) return false;
+        p.k = ptr[0];
+        p.v = ptr[1];
+        p.k_scale = static_cast<uint8_t*>(ptr[2]);
+        p.v_scale = static_cast<uint8_t*>(ptr[3]);
+        p.n_pages = t[0]->size(0);
+        p.page_rows = static_cast<int32_t>(t[0]->size(2));
+        return true;
+    }
+};
+// The table of a call: [sequences, pages].
+bool table_of(PyObject* o, const Shape& c, int n, const int32_t** p, int64_t* stride)
+{
+    void* ptr;
+    const at::Tensor* t;
+    if (!typed(o, "table", at::kInt, 2, c.device, &ptr, &t) || !expect(t && t->size(0) == n, "table: [sequences, pages]")) return false;
+    *p = static_cast<const int32_t*>(ptr);
+    *stride = t->size(1);
+    return true;
+}
+
+// page_rows(ctx, dtype, heads, kv_heads, dim, device, write, seqs, pool k, v, k_scale, v_scale, table, k, v, kv_len, stream) ->
+//   (status, k, v); a read that is given neither allocates both
+PyObject* py_page_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    MVLA_TRY
+    if (!arg_count(n, 17)) return nullptr;
+    Shape c;
+    int64_t write;
+    if (!c.take(a) || !int_of(a[6], &write)) return nullptr;
+    Seqs s;
+    Pool pool;
+    mvla_page_rows r;
+    std::memset(&r, 0, sizeof r);
+    void *kl, *st;
+    const at::Tensor* tkl;
+    if (!s.take(a[7]) || !pool.take(a + 8, c) || !table_of(a[12], c, s.n, &r.table, &r.table_stride) || !typed(a[15], "kv_len", at::kInt, 1, c.device, &kl, &tkl) ||
+        !stream_on(a[16], c.device, &st) || !expect(entries(tkl, s.n), "kv_len: one entry per sequence"))
+        return nullptr;
+    r.pages = pool.p;
+    r.kv_len = static_cast<const int32_t*>(kl);
+    Held rows[2] = {Held(a[13]), Held(a[14])};
+    if (a[13] == Py_None && a[14] == Py_None) {
+        if (!expect(!write, "k or v is needed")) return nullptr;
+        int64_t end = 0;
+        for (int i = 0; i < s.n; ++i)
+            if (s.ptr[i].n_q > 0 && s.ptr[i].q_row >= 0 && s.ptr[i].q_row <= 0x7FFFFFFF) end = std::max<int64_t>(end, s.ptr[i].q_row + s.ptr[i].n_q);
+        for (Held& h : rows) {
+            h.take(THPVariable_Wrap(fresh_on({end, c.kv_heads, c.dim}, c.wide, c.device, a[16], st)));
+            if (!h.o) return nullptr;
+        }
+    }
+    const void *k, *v;
+    int64_t count = -1;
+    if (!strided_rows(rows[0].o, "k", c, c.kv_heads, &k, &r.k_stride, &count) || !strided_rows(rows[1].o, "v", c, c.kv_heads, &v, &r.v_stride, &count)) return nullptr;
+    r.k = const_cast<void*>(k);
+    r.v = const_cast<void*>(v);
+    r.rows = count;
+    mvla_ctx* ctx = ctx_of(a[0]);
+    const int32_t rc = unlocked([&] { return write ? mvla_page_write(ctx, s.n, s.ptr, &r, st) : mvla_page_read(ctx, s.n, s.ptr, &r, st); });
+    return Py_BuildValue("(iOO)", rc, rows[0].o, rows[1].o);
+    MVLA_CATCH
+}
+
+// page_attention(ctx, dtype, heads, kv_heads, dim, device, seqs, pool k, v, k_scale, v_scale, table, q, window, sinks, scale, kv_len, out, lse,
+//   stream) -> (status, out); a missing `out` is allocated
+PyObject* py_page_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    MVLA_TRY
+    if (!arg_count(n, 20)) return nullptr;
+    Shape c;
+    int64_t window, sinks;
+    if (!c.take(a) || !int_of(a[13], &window) || !int_of(a[14], &sinks)) return nullptr;
+    mvla_paged_attention r;
+    std::memset(&r, 0, sizeof r);
+    r.scale = PyFloat_AsDouble(a[15]);
+    if (r.scale == -1.0 && PyErr_Occurred()) return nullptr;
+    Seqs s;
+    Pool pool;
+    void *q, *kl, *out, *lse, *st;
+    const at::Tensor *tq, *tkl, *to, *tl;
+    if (!s.take(a[6]) || !pool.take(a + 7, c) || !table_of(a[11], c, s.n, &r.table, &r.table_stride) || !typed(a[12], "q", c.wide, 3, c.device, &q, &tq) ||
+        !typed(a[16], "kv_len", at::kInt, 1, c.device, &kl, &tkl) || !typed(a[17], "out", c.wide, 3, c.device, &out, &to) ||
+        !typed(a[18], "lse", at::kFloat, 2, c.device, &lse, &tl) || !stream_on(a[19], c.device, &st))
+        return nullptr;
+    if (!expect(tq && tq->size(1) == c.heads && tq->size(2) == c.dim, "q: [rows, heads, head_dim]") || !expect(entries(tkl, s.n), "kv_len: one entry per sequence") ||
+        !expect(!to || to->sizes() == tq->sizes(), "out: as q") || !expect(!tl || (tl->size(0) == tq->size(0) && tl->size(1) == c.heads), "lse: [rows, heads]") ||
+        !expect(window >= 1 && window <= MVLA_WINDOW_ALL && sinks >= 0 && sinks <= MVLA_WINDOW_ALL, "window, n_sink: out of range"))
+        return nullptr;
+    r.pages = pool.p;
+    r.kv_len = static_cast<const int32_t*>(kl);
+    r.q = q;
+    r.q_rows = tq->size(0);
+    r.window = static_cast<int32_t>(window);
+    r.n_sink = static_cast<int32_t>(sinks);
+    r.lse = static_cast<float*>(lse);
+    mvla_ctx* ctx = ctx_of(a[0]);
+    int64_t bytes = 0;
+    int32_t rc = mvla_page_attention_workspace(ctx, s.n, s.ptr, &r, &bytes);
+    if (rc != MVLA_OK) return Py_BuildValue("(iO)", rc, Py_None);
+    at::Tensor ws, fresh;
+    if (bytes > 0) ws = fresh_on({bytes}, at::kByte, c.device, a[19], st);
+    if (!to) {
+        fresh = fresh_on(tq->sizes(), c.wide, c.device, a[19], st);
+        out = fresh.data_ptr();
+    }
+    r.out = out;
+    r.workspace = bytes > 0 ? ws.data_ptr() : nullptr;
+    r.workspace_bytes = bytes;
+    rc = unlocked([&] { return mvla_page_attention(ctx, s.n, s.ptr, &r, st); });
+    if (to) return Py_BuildValue("(iO)", rc, a[17]);
+    PyObject* o = THPVariable_Wrap(fresh);
+    PyObject* ret = o ? Py_BuildValue("(iO)", rc, o) : nullptr;
+    Py_XDECREF(o);
+    return ret;
+    MVLA_CATCH
+}
+
 // fill_samples(array, sequence): descriptors from objects with the descriptor's field names, into a ctypes array
 PyObject* py_fill_samples(PyObject*, PyObject* const* a, Py_ssize_t n)
 {
@@ -680,7 +822,8 @@ PyMethodDef kMethods[] = {MVLA_FAST("prune_step", py_prune_step), MVLA_FAST("sal
                           MVLA_FAST("select", py_select), MVLA_FAST("compact", py_compact),
                           MVLA_FAST("patch_indicators", py_patch_indicators), MVLA_FAST("patch_select", py_patch_select),
                           MVLA_FAST("qk_norm_rope", py_qk_norm_rope), MVLA_FAST("window_attention", py_window_attention),
-                          MVLA_FAST("cache_evict", py_cache_evict),
+                          MVLA_FAST("cache_evict", py_cache_evict), MVLA_FAST("page_rows", py_page_rows),
+                          MVLA_FAST("page_attention", py_page_attention),
                           MVLA_FAST("fill_samples", py_fill_samples), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_native", "Argument marshalling of libmvla_prune.so", -1, kMethods,
                        nullptr, nullptr, nullptr, nullptr};

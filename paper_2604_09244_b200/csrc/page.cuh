@@ -1,0 +1,58 @@
+// Device side of a cache in pages that its kernels share: where a cached row lies, and what codes and scales stand for.
+#pragma once
+
+#include "device_utils.cuh"
+#include "page.h"
+
+#include <cuda_fp4.h>
+#include <cuda_fp8.h>
+
+namespace mvla {
+
+// Page of cached row j of the batch's sequence `index`, -1 where it is none of the pool's.
+__device__ __forceinline__ int page_of(const PagePool& p, int index, int j)
+{
+    const int page = p.table[index * p.table_stride + (j >> p.page_shift)];
+    return page >= 0 && page < p.n_pages ? page : -1;
+}
+// Row of head h's rows [n_pages, kv_heads, page_rows] that row j of a sequence is, on its page.
+__device__ __forceinline__ int64_t page_row(const PagePool& p, int page, int h, int j)
+{
+    return ((static_cast<int64_t>(page) * p.kv_heads + h) << p.page_shift) + (j & ((1 << p.page_shift) - 1));
+}
+
+// The least exponent e, not below kScaleLeast, with |x| <= M 2^e for the largest |x| of a group, whose bits in 32 bits these are (finite).
+template <int KIND>
+__device__ __forceinline__ int scale_exponent(uint32_t big)
+{
+    constexpr bool kE4m3 = KIND == MVLA_PAGE_E4M3;           // M = 448 = 1.75 2^8, or 6 = 1.5 2^2
+    const int e = static_cast<int>(big >> 23) - 127 - (kE4m3 ? 8 : 2) + ((big & 0x7FFFFFu) > (kE4m3 ? 0x600000u : 0x400000u) ? 1 : 0);
+    return min(max(e, kScaleLeast), kE4m3 ? kScaleMostE4m3 : kScaleMostE2m1);
+}
+// 2^e for a normal number's e.
+__device__ __forceinline__ float two_to(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
+// What a scale's byte stands for.
+__device__ __forceinline__ float scale_value(uint32_t byte) { return byte == 255u ? CUDART_NAN_F : byte == 0u ? 0x1p-127f : __uint_as_float(byte << 23); }
+
+// Eight codes as numbers.
+__device__ __forceinline__ void code_values(uint2 codes, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = (i < 2 ? codes.x : codes.y) >> (16 * (i & 1)) & 0xFFFFu;
+        const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w), __NV_E4M3)));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+__device__ __forceinline__ void code_values(uint32_t codes, float (&x)[8])
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(codes >> (8 * i) & 0xFFu), __NV_E2M1)));
+        x[2 * i] = f.x;
+        x[2 * i + 1] = f.y;
+    }
+}
+
+}  // namespace mvla

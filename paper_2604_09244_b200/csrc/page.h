@@ -1,0 +1,49 @@
+// Launchers of the calls on a cache in pages (page_*.cu) and what they are given.
+#pragma once
+
+#include "serve.h"
+
+namespace mvla {
+
+constexpr int kPageGroup = 32;               // elements that share a scale in e2m1 pages
+// Exponents of the scales: from 2^-117 on every element that the codes can stand for is a normal number of 32 bits and of bf16; up to 2^119 (e4m3) and 2^125
+// (e2m1) it is a finite one.
+constexpr int kScaleLeast = -117, kScaleMostE4m3 = 119, kScaleMostE2m1 = 125;
+
+// Bytes of a cached row of one head, and of its scales.
+__host__ __device__ inline int page_row_bytes(int kind, int d, int wide) { return kind == MVLA_PAGE_ROWS ? d * wide : kind == MVLA_PAGE_E4M3 ? d : d / 2; }
+__host__ __device__ inline int page_row_scales(int kind, int d) { return kind == MVLA_PAGE_ROWS ? 0 : kind == MVLA_PAGE_E4M3 ? 1 : d / kPageGroup; }
+
+struct PagePool {
+    void *k, *v;
+    uint8_t *k_scale, *v_scale;
+    const int32_t* table;
+    int64_t table_stride;
+    int64_t n_pages;
+    int32_t page_shift;                      // page_rows = 1 << page_shift
+    int32_t kv_heads, head_dim;
+};
+
+// ---- rows into pages and out of them
+
+struct PageSeq {
+    int64_t q_row;
+    int32_t n_q, n_kv;
+    int32_t row0;                            // its first row among those of the batch, packed
+    int32_t index;                           // its place in the caller's batch
+};
+struct PageRowsArgs {
+    PagePool pool;
+    const int32_t* kv_len;
+    void *k, *v;                             // each null: left alone
+    int64_t k_stride, v_stride;
+    int32_t n_seq, total;                    // rows of the batch
+    int32_t block_rows;                      // rows of a CTA
+    int32_t from_start;                      // read rows 0 .. n_q - 1 of a sequence instead of its last ones
+    int64_t packed_row;                      // >= 0: row r of the batch, packed, is row packed_row + r of k / v (instead of q_row + i)
+    PageSeq s[kMaxBatch];
+};
+cudaError_t launch_page_write(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream);
+cudaError_t launch_page_read(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream);
+
+}  // namespace mvla

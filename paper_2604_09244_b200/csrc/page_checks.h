@@ -1,0 +1,183 @@
+// Host-side checks and plans of the calls on a cache in pages: arithmetic on descriptors and addresses, without a device.
+#pragma once
+
+#include "serve_checks.h"
+
+namespace mvla {
+
+inline int64_t page_data_bytes(const ServeShape& v, const mvla_pages& p)
+{
+    const int64_t row = p.kind == MVLA_PAGE_ROWS ? v.head_dim * static_cast<int64_t>(v.wide) : p.kind == MVLA_PAGE_E4M3 ? v.head_dim : v.head_dim / 2;
+    return p.n_pages * v.kv_heads * p.page_rows * row;
+}
+inline int64_t page_scale_bytes(const ServeShape& v, const mvla_pages& p)
+{
+    const int64_t row = p.kind == MVLA_PAGE_ROWS ? 0 : p.kind == MVLA_PAGE_E4M3 ? 1 : v.head_dim / 32;
+    return p.n_pages * v.kv_heads * p.page_rows * row;
+}
+
+// The sequences of a call, and the table that has to name their pages.
+inline int32_t check_page_batch(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_pages& p, int64_t table_stride)
+{
+    const int32_t rc = check_batch(v, batch, seqs);
+    if (rc != MVLA_OK) return rc;
+    if (p.kind < MVLA_PAGE_ROWS || p.kind > MVLA_PAGE_E2M1 || p.n_pages < 0 || table_stride < 0 || table_stride > kMaxTensorRows) return MVLA_ERR_INVALID_ARG;
+    if (p.page_rows < 16 || p.page_rows > 256 || (p.page_rows & (p.page_rows - 1))) return MVLA_ERR_UNSUPPORTED;
+    if (p.n_pages > 0x7FFFFFFF || p.n_pages * v.kv_heads > 0x7FFFFFFF || v.kv_heads > 65535) return MVLA_ERR_UNSUPPORTED;
+    int64_t rows = 0, cached = 0;
+    for (int b = 0; b < batch; ++b) {
+        const mvla_seq& s = seqs[b];
+        if ((static_cast<int64_t>(s.n_kv) + p.page_rows - 1) / p.page_rows > table_stride) return MVLA_ERR_INVALID_ARG;
+        rows += s.n_q;
+        cached += s.n_kv;
+    }
+    if (rows > kMaxRows || cached > 0x7FFFFFFF) return MVLA_ERR_UNSUPPORTED;
+    return MVLA_OK;
+}
+
+// The pool's own memory: there, aligned, its parts apart.  `parts` receives their ranges.
+inline int32_t check_pool(const ServeShape& v, const mvla_pages& p, Range (&parts)[4])
+{
+    const bool scaled = p.kind != MVLA_PAGE_ROWS;
+    if ((p.n_pages > 0 && (!p.k || !p.v || (scaled && (!p.k_scale || !p.v_scale)))) || (!scaled && (p.k_scale || p.v_scale))) return MVLA_ERR_INVALID_ARG;
+    if (!aligned(p.k, 16) || !aligned(p.v, 16) || !aligned(p.k_scale, 16) || !aligned(p.v_scale, 16)) return MVLA_ERR_INVALID_ARG;
+    const int64_t data = page_data_bytes(v, p), scale = page_scale_bytes(v, p);
+    parts[0] = range_of(p.k, data);
+    parts[1] = range_of(p.v, data);
+    parts[2] = range_of(p.k_scale, scale);
+    parts[3] = range_of(p.v_scale, scale);
+    for (int i = 0; i < 4; ++i)
+        for (int j = i + 1; j < 4; ++j) if (meet(parts[i], parts[j])) return MVLA_ERR_INVALID_ARG;
+    return MVLA_OK;
+}
+inline Range table_range(int32_t batch, const int32_t* table, int64_t stride) { return range_of(stride > 0 ? table : nullptr, batch * stride * 4); }
+
+// mvla_page_write (`write`) and mvla_page_read.
+inline int32_t check_page_rows(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_page_rows* a, bool write)
+{
+    int32_t rc = check_page_batch(v, batch, seqs, a->pages, a->table_stride);
+    if (rc != MVLA_OK) return rc;
+    if (a->rows < 0 || a->rows > kMaxTensorRows) return MVLA_ERR_INVALID_ARG;
+    int64_t total = 0, cached = 0;
+    for (int b = 0; b < batch; ++b) {
+        if (seqs[b].q_row > a->rows - seqs[b].n_q) return MVLA_ERR_INVALID_ARG;
+        total += seqs[b].n_q;
+        cached += seqs[b].n_kv;
+    }
+    if (!write && shared_rows(batch, seqs, [](const mvla_seq& s) { return s.q_row; }, [](const mvla_seq& s) { return s.n_q; })) return MVLA_ERR_INVALID_ARG;
+    if (total == 0) return MVLA_OK;                        // (nothing to do: whatever the pointers are)
+    Range pool[4];
+    rc = check_pool(v, a->pages, pool);
+    if (rc != MVLA_OK) return rc;
+    if ((cached > 0 && !a->table) || !aligned(a->table, 4) || !aligned(a->kv_len, 4)) return MVLA_ERR_INVALID_ARG;
+    const int64_t width = static_cast<int64_t>(v.kv_heads) * v.head_dim, wide = static_cast<int64_t>(v.wide);
+    const void* const p[2] = {a->k, a->v};
+    const int64_t stride[2] = {a->k_stride, a->v_stride};
+    Range rows[2];
+    for (int i = 0; i < 2; ++i) {
+        rows[i] = Range{nullptr, nullptr};
+        if (!p[i]) continue;
+        if (!aligned(p[i], 16) || stride[i] < 0 || stride[i] > kMaxStride || (a->rows > 1 && stride[i] < width) || stride[i] * wide % 16 != 0) return MVLA_ERR_INVALID_ARG;
+        rows[i] = range_of(p[i], ((a->rows - 1) * stride[i] + width) * wide);
+    }
+    // slices of a fused tensor interleave: of two outputs that do, rows must have room for one another
+    const Range side[2] = {table_range(batch, a->table, a->table_stride), range_of(a->kv_len, batch * 4)};
+    for (const Range& r : rows) {
+        for (const Range& q : pool) if (meet(r, q)) return MVLA_ERR_INVALID_ARG;
+        if (!write) for (const Range& q : side) if (meet(r, q)) return MVLA_ERR_INVALID_ARG;
+    }
+    if (write) {
+        for (const Range& r : pool) for (const Range& q : side) if (meet(r, q)) return MVLA_ERR_INVALID_ARG;
+    } else if (meet(rows[0], rows[1])) {
+        const char* lo = rows[0].lo < rows[1].lo ? rows[0].lo : rows[1].lo;
+        const int64_t apart = (rows[0].lo < rows[1].lo ? rows[1].lo : rows[0].lo) - lo;
+        if (stride[0] != stride[1] || apart < width * wide || apart + width * wide > stride[0] * wide) return MVLA_ERR_INVALID_ARG;
+    }
+    return MVLA_OK;
+}
+
+// ---- attention over pages: rows taken out of the pages into the workspace, then attended over as packed rows
+
+struct PageAttendPlan {
+    AttendPlan attend;
+    int64_t dense_k = -1, dense_v = -1, bytes = 0;
+};
+
+inline ServeShape hidden_shape(const ServeShape& v)
+{
+    ServeShape h = v;
+    h.dtype = v.hidden_dtype;
+    h.elem = v.wide;
+    return h;
+}
+
+// The call as mvla_window_attention would be given it.
+inline mvla_attention as_window(const mvla_paged_attention* a)
+{
+    mvla_attention w = {};
+    w.q = a->q;
+    w.q_rows = a->q_rows;
+    w.kv_len = a->kv_len;
+    w.window = a->window;
+    w.n_sink = a->n_sink;
+    w.scale = a->scale;
+    w.out = a->out;
+    w.lse = a->lse;
+    return w;
+}
+
+inline int32_t check_page_attention(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_paged_attention* a)
+{
+    int32_t rc = check_page_batch(v, batch, seqs, a->pages, a->table_stride);
+    if (rc != MVLA_OK) return rc;
+    const ServeShape h = hidden_shape(v);
+    const mvla_attention w = as_window(a);
+    if (w.window < 1 || w.n_sink < 0 || !(w.scale >= 0.0)) return MVLA_ERR_INVALID_ARG;
+    if (!(scale_log2(h, &w) >= FLT_MIN && scale_log2(h, &w) <= FLT_MAX)) return MVLA_ERR_INVALID_ARG;
+    if (a->q_rows < 0 || a->q_rows > kMaxTensorRows) return MVLA_ERR_INVALID_ARG;
+    int64_t total_q = 0;
+    for (int b = 0; b < batch; ++b) {
+        if (seqs[b].q_row > a->q_rows - seqs[b].n_q) return MVLA_ERR_INVALID_ARG;
+        total_q += seqs[b].n_q;
+    }
+    if (h.dtype != MVLA_DTYPE_FP32 && a->q_rows > 0x7FFFFFFF) return MVLA_ERR_UNSUPPORTED;      // (rows of a tensor map are counted in 32 bits)
+    if (total_q * v.n_heads / v.kv_heads > kMaxRows) return MVLA_ERR_UNSUPPORTED;
+    if (shared_rows(batch, seqs, [](const mvla_seq& s) { return s.q_row; }, [](const mvla_seq& s) { return s.n_q; })) return MVLA_ERR_INVALID_ARG;
+    return MVLA_OK;
+}
+
+inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_paged_attention* a)
+{
+    PageAttendPlan p;
+    const ServeShape h = hidden_shape(v);
+    p.attend = plan_attend(h, batch, seqs, !a->kv_len, a->window, a->n_sink, false);
+    Workspace w;
+    w.take(p.attend.bytes);
+    const int64_t rows = p.attend.total_kv * v.kv_heads * v.head_dim * static_cast<int64_t>(v.wide);
+    p.dense_k = w.take(rows);
+    p.dense_v = w.take(rows);
+    p.bytes = w.bytes;
+    return p;
+}
+
+// Pointers of a call that has queries.
+inline int32_t check_page_attention_memory(const ServeShape& v, int32_t batch, const mvla_paged_attention* a, const PageAttendPlan& plan)
+{
+    Range pool[4];
+    const int32_t rc = check_pool(v, a->pages, pool);
+    if (rc != MVLA_OK) return rc;
+    if (!a->q || !a->out || (plan.attend.total_kv > 0 && !a->table)) return MVLA_ERR_INVALID_ARG;
+    if (!aligned(a->q, 16) || !aligned(a->out, 16) || !aligned(a->lse, 4) || !aligned(a->table, 4) || !aligned(a->kv_len, 4) || !aligned(a->workspace, 256))
+        return MVLA_ERR_INVALID_ARG;
+    if (plan.bytes > 0 && (!a->workspace || a->workspace_bytes < plan.bytes)) return MVLA_ERR_INVALID_ARG;
+    const int64_t qw = static_cast<int64_t>(v.n_heads) * v.head_dim * static_cast<int64_t>(v.wide);
+    const Range in[7] = {range_of(a->q, a->q_rows * qw), table_range(batch, a->table, a->table_stride), range_of(a->kv_len, batch * 4), pool[0], pool[1], pool[2], pool[3]};
+    const Range out[3] = {range_of(a->out, a->q_rows * qw), range_of(a->lse, a->q_rows * v.n_heads * 4), range_of(plan.bytes ? a->workspace : nullptr, plan.bytes)};
+    for (int i = 0; i < 3; ++i) {
+        for (const Range& r : in) if (meet(out[i], r)) return MVLA_ERR_INVALID_ARG;
+        for (int j = i + 1; j < 3; ++j) if (meet(out[i], out[j])) return MVLA_ERR_INVALID_ARG;
+    }
+    return MVLA_OK;
+}
+
+}  // namespace mvla

@@ -80,6 +80,10 @@ cudaError_t launch_attend_join(int dtype, const AttArgs& a, cudaStream_t stream)
 // mass += part_mass over its parts.
 cudaError_t launch_mass_add(const AttArgs& a, cudaStream_t stream);
 
+// What a checked call enqueues, and its status.
+int32_t enqueue_attention(mvla_ctx* ctx, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan,
+                          cudaStream_t stream);
+
 // ---- eviction by accumulated weight
 
 struct EvictSeq {

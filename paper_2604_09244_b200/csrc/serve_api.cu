@@ -87,20 +87,12 @@ int32_t attend_by_tiles(const CtxView& v, AttArgs& k, const mvla_attention* a, c
     return MVLA_OK;
 }
 
-int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, void* stream)
+}  // namespace
+
+namespace mvla {
+
+int32_t enqueue_attention(mvla_ctx* ctx, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan, cudaStream_t st)
 {
-    if (!ctx || !a) return MVLA_ERR_INVALID_ARG;
-    CtxView v;
-    int32_t rc = open_call(ctx, &v);
-    if (rc == MVLA_OK) rc = check_attention(v, batch, seqs, a);
-    if (rc != MVLA_OK) return rc;
-    const AttendPlan plan = plan_of(v, batch, seqs, a);
-    if (plan.total_q == 0) return MVLA_OK;
-    rc = check_attention_memory(v, batch, a, plan);
-    if (rc != MVLA_OK) return rc;
-    DeviceGuard guard(v.device);
-    if (!guard.ok) return MVLA_ERR_CUDA;
-    note_work(ctx);
     AttArgs k;
     std::memset(&k, 0, sizeof k);
     k.q = a->q; k.k = a->k; k.v = a->v; k.out = a->out; k.lse = a->lse; k.mass = a->mass;
@@ -137,10 +129,9 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
         part += static_cast<int64_t>(parts) * s.n_q;
         logit += static_cast<int64_t>(s.n_q) * v.n_heads * s.n_kv;
     }
-    cudaStream_t st = static_cast<cudaStream_t>(stream);
     cudaError_t e = cudaSuccess;
     if (plan.form == kFormTile) {
-        rc = attend_by_tiles(v, k, a, plan, &e, st);
+        const int32_t rc = attend_by_tiles(v, k, a, plan, &e, st);
         if (rc != MVLA_OK) return rc;
     } else if (plan.form == kFormToken) {
         e = launch_attend_token(v.dtype, k, plan.rows, st);
@@ -153,6 +144,27 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     }
     if (e == cudaSuccess && a->mass) e = launch_mass_add(k, st);
     return close_call(ctx, e);
+}
+
+}  // namespace mvla
+
+namespace {
+
+int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, void* stream)
+{
+    if (!ctx || !a) return MVLA_ERR_INVALID_ARG;
+    CtxView v;
+    int32_t rc = open_call(ctx, &v);
+    if (rc == MVLA_OK) rc = check_attention(v, batch, seqs, a);
+    if (rc != MVLA_OK) return rc;
+    const AttendPlan plan = plan_of(v, batch, seqs, a);
+    if (plan.total_q == 0) return MVLA_OK;
+    rc = check_attention_memory(v, batch, a, plan);
+    if (rc != MVLA_OK) return rc;
+    DeviceGuard guard(v.device);
+    if (!guard.ok) return MVLA_ERR_CUDA;
+    note_work(ctx);
+    return enqueue_attention(ctx, v, batch, seqs, a, plan, static_cast<cudaStream_t>(stream));
 }
 
 int32_t evict_workspace_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_eviction* a, int64_t* bytes)

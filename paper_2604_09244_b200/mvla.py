@@ -32,12 +32,14 @@ SALIENCE_AUTO, SALIENCE_FMA = 0, 1
 SET_2D, SET_3D = 1, 2
 ROPE_NORM, ROPE_INTERLEAVED = 1, 2
 WINDOW_ALL = 0x7FFFFFFF
+PAGE_ROWS, PAGE_E4M3, PAGE_E2M1 = 0, 1, 2
 
 EXPORTS = ("mvla_prune_create", "mvla_salience", "mvla_select", "mvla_compact",
            "mvla_prune_step", "mvla_prune_destroy", "mvla_patch_indicators", "mvla_patch_select",
            "mvla_salience_noalloc", "mvla_selftest_wait_timeout", "mvla_set_stage_event", "mvla_set_kernel_stamps",
            "mvla_logit_cache_stats", "mvla_qk_norm_rope", "mvla_window_attention", "mvla_window_attention_workspace",
-           "mvla_cache_evict", "mvla_cache_evict_workspace")
+           "mvla_cache_evict", "mvla_cache_evict_workspace", "mvla_page_write", "mvla_page_read", "mvla_page_attention",
+           "mvla_page_attention_workspace")
 
 
 class MvlaError(RuntimeError):
@@ -119,6 +121,22 @@ class CEviction(C.Structure):
                 ("workspace_bytes", C.c_int64)]
 
 
+class CPages(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("n_pages", C.c_int64),
+                ("page_rows", C.c_int32), ("kind", C.c_int32)]
+
+
+class CPageRows(C.Structure):
+    _fields_ = [("pages", CPages), ("table", C.c_void_p), ("table_stride", C.c_int64), ("kv_len", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("rows", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64)]
+
+
+class CPagedAttention(C.Structure):
+    _fields_ = [("pages", CPages), ("table", C.c_void_p), ("table_stride", C.c_int64), ("kv_len", C.c_void_p), ("q", C.c_void_p),
+                ("q_rows", C.c_int64), ("window", C.c_int32), ("n_sink", C.c_int32), ("scale", C.c_double), ("out", C.c_void_p),
+                ("lse", C.c_void_p), ("workspace", C.c_void_p), ("workspace_bytes", C.c_int64)]
+
+
 def load_library(path: str = LIB_PATH) -> C.CDLL:
     if not os.path.exists(path):
         raise OSError(f"{path} is missing: build it with `python -m paper_2604_09244_b200.build` "
@@ -157,8 +175,12 @@ def load_library(path: str = LIB_PATH) -> C.CDLL:
     lib.mvla_window_attention_workspace.argtypes = [vp, i32, sq, C.POINTER(CAttention), C.POINTER(i64)]
     lib.mvla_cache_evict.argtypes = [vp, i32, sq, C.POINTER(CEviction), vp]
     lib.mvla_cache_evict_workspace.argtypes = [vp, i32, sq, C.POINTER(CEviction), C.POINTER(i64)]
+    lib.mvla_page_write.argtypes = [vp, i32, sq, C.POINTER(CPageRows), vp]
+    lib.mvla_page_read.argtypes = [vp, i32, sq, C.POINTER(CPageRows), vp]
+    lib.mvla_page_attention.argtypes = [vp, i32, sq, C.POINTER(CPagedAttention), vp]
+    lib.mvla_page_attention_workspace.argtypes = [vp, i32, sq, C.POINTER(CPagedAttention), C.POINTER(i64)]
     for fn in ("mvla_qk_norm_rope", "mvla_window_attention", "mvla_window_attention_workspace", "mvla_cache_evict",
-               "mvla_cache_evict_workspace"):
+               "mvla_cache_evict_workspace", "mvla_page_write", "mvla_page_read", "mvla_page_attention", "mvla_page_attention_workspace"):
         getattr(lib, fn).restype = i32
     return lib
 
@@ -210,6 +232,17 @@ def c_seqs(seqs: Sequence[Seq]) -> "C.Array[CSeq]":
     """The descriptors as the library takes them.  A program whose caches keep their places makes this array once and writes
     its fields."""
     return (CSeq * len(seqs))(*[CSeq(s.q_row, s.kv_row, s.n_q, s.n_kv, s.budget, 0) for s in seqs])
+
+
+@dataclass
+class PagePool:
+    """A cache in pages (``mvla_pages``): k, v [pages, kv_heads, page rows, head_dim] of the context's hidden type, of e4m3, or bytes of
+    two e2m1 elements each (head_dim / 2); quantised pages with scale bytes, 2^(byte - 127): [pages, kv_heads, page rows], e2m1 one for
+    32 elements: [pages, kv_heads, page rows, head_dim / 32]."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: Optional[torch.Tensor] = None
+    v_scale: Optional[torch.Tensor] = None
 
 
 def _ptr(t: Optional[torch.Tensor]) -> Optional[int]:
@@ -445,6 +478,51 @@ class PruneContext:
                                    mass if mass_out is None else mass_out, kept_idx, kv_len, kv_len_out, n_sink, n_recent, stream)
         if rc != OK:
             raise MvlaError(rc, "mvla_cache_evict")
+
+
+    # -- a cache in pages (`table`: int32 [sequences, pages]; `seqs` as above, without kv_row) --------------------------------------------
+    def alloc_pages(self, n_pages: int, *, page_rows: int = 64, kind: int = PAGE_ROWS) -> PagePool:
+        """Pages of zeros (``PAGE_ROWS``: the hidden type; ``PAGE_E4M3``: 8 bits; ``PAGE_E2M1``: 4 bits)."""
+        heads, d = self.cfg.n_kv_heads or self.cfg.n_heads, self.cfg.head_dim
+        dt = {PAGE_ROWS: self.hidden_dtype, PAGE_E4M3: torch.float8_e4m3fn, PAGE_E2M1: torch.uint8}[kind]
+        shape = (n_pages, heads, page_rows)
+        mk = lambda *last, dtype: torch.zeros(*shape, *last, dtype=dtype, device=self.device)
+        scales = {PAGE_ROWS: None, PAGE_E4M3: (), PAGE_E2M1: (d // 32,)}[kind]
+        width = d // 2 if kind == PAGE_E2M1 else d
+        ks, vs = (None, None) if scales is None else (mk(*scales, dtype=torch.uint8), mk(*scales, dtype=torch.uint8))
+        return PagePool(mk(width, dtype=dt), mk(width, dtype=dt), ks, vs)
+
+    def page_write(self, pool, seqs, table, k, v, *, kv_len=None, stream=None) -> None:
+        """The sequences' last rows into their pages, quantised where the pool is (``mvla_page_write``): row q_row + i of k / v ([rows,
+        kv_heads, head_dim] of the hidden type, slices of a fused projection need no copy; either may be None) becomes cached row
+        n_kv - n_q + i."""
+        cs = seqs if isinstance(seqs, C.Array) else c_seqs(seqs)
+        rc, _, _ = self._nat.page_rows(self._h.value or 0, *self._shape, 1, cs, pool.k, pool.v, pool.k_scale, pool.v_scale, table, k, v, kv_len, stream)
+        if rc != OK:
+            raise MvlaError(rc, "mvla_page_write")
+
+    def page_read(self, pool, seqs, table, *, k_out=None, v_out=None, kv_len=None, stream=None):
+        """The sequences' last rows out of their pages, dense, in the hidden type (``mvla_page_read``): cached row n_kv - n_q + i becomes row
+        q_row + i of (k_out, v_out), which is returned.  Given one of them only that one is read; given none both are allocated (rows that
+        belong to no sequence then hold anything)."""
+        cs = seqs if isinstance(seqs, C.Array) else c_seqs(seqs)
+        rc, k_out, v_out = self._nat.page_rows(self._h.value or 0, *self._shape, 0, cs, pool.k, pool.v, pool.k_scale, pool.v_scale, table, k_out, v_out,
+                                               kv_len, stream)
+        if rc != OK:
+            raise MvlaError(rc, "mvla_page_read")
+        return k_out, v_out
+
+    def page_attention(self, pool, seqs, table, q, *, window=None, n_sink=0, scale=0.0, kv_len=None, out=None, lse=None, stream=None):
+        """Causal attention of the sequences' last rows over their pages (``mvla_page_attention``), with a sliding window (None: everything
+        before a query) and `n_sink` first rows that stay visible; positions are counted.  q: [rows, heads, head_dim] of the hidden
+        type; `lse` (float32 [rows, heads]) is written.  Returns `out` (allocated where it is not given: rows outside the sequences then
+        hold anything)."""
+        cs = seqs if isinstance(seqs, C.Array) else c_seqs(seqs)
+        rc, out = self._nat.page_attention(self._h.value or 0, *self._shape, cs, pool.k, pool.v, pool.k_scale, pool.v_scale, table, q,
+                                           WINDOW_ALL if window is None else window, n_sink, scale, kv_len, out, lse, stream)
+        if rc != OK:
+            raise MvlaError(rc, "mvla_page_attention")
+        return out
 
 
 def context_for(wl, *, max_batch=None, n_prune_points=1, n_state_slots=0, salience_path=SALIENCE_AUTO,
