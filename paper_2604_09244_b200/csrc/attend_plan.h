@@ -101,6 +101,45 @@ inline int pack_of(int group)
     return p;
 }
 
+// Parts of single tokens: of equal length over the whole batch, a multiple of 64 keys (a tile for each warp), so that their CTAs fill whole rounds of
+// those that fit: of one to four rounds the ones that end first, by the keys of a round's longest part and 128 for its start and end.  256
+// parts to a sequence at most (the join reads them all).
+inline void cut_for_tokens(AttendPlan& p, int64_t fit, int kv_heads, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink)
+{
+    int64_t keys = 0, longest = 0;
+    for (int b = 0; b < batch; ++b) {
+        if (seqs[b].n_q == 0) continue;
+        const int64_t n = visible_keys(seqs[b], counted, window, n_sink);
+        keys += n;
+        longest = n > longest ? n : longest;
+    }
+    const auto ctas_of = [&](int64_t part) {
+        int64_t n = 0;
+        p.part_keys = part;
+        for (int b = 0; b < batch; ++b) n += parts_of(p, seqs[b], counted, window, n_sink);
+        return n * kv_heads;
+    };
+    int64_t best = 0, best_cost = 0;
+    for (int rounds = 1; rounds <= 4; ++rounds) {
+        int64_t part = (keys * kv_heads + rounds * fit - 1) / (rounds * fit);
+        part = part < (longest + 255) / 256 ? (longest + 255) / 256 : part;
+        part = part < 64 ? 64 : (part + 63) / 64 * 64;
+        int64_t n = ctas_of(part);
+        for (int tries = 0; n > rounds * fit && tries < 8; ++tries) {
+            part += (part / 16 + 63) / 64 * 64;
+            n = ctas_of(part);
+        }
+        const int64_t cost = (n + fit - 1) / fit * ((part < longest ? part : longest) + 128);
+        if (!best || cost < best_cost) { best = part; best_cost = cost; }
+    }
+    p.part_keys = best;
+    for (int b = 0; b < batch; ++b) {
+        const int32_t n = parts_of(p, seqs[b], counted, window, n_sink);
+        p.blocks += n;
+        p.splits = n > p.splits ? n : p.splits;
+    }
+}
+
 inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, bool mass)
 {
     AttendPlan p;
@@ -142,43 +181,11 @@ inline AttendPlan plan_attend(const ServeShape& c, int32_t batch, const mvla_seq
             p.splits = n < 1 ? 1 : static_cast<int32_t>(n);
         }
     } else if (by_tokens(c.dtype, c.head_dim, most_rows, mass, 2 * longest * active <= 3 * all_keys, all_keys)) {
-        // Parts of equal length over the whole batch, a multiple of 64 keys (a tile for each warp), so that their CTAs fill whole rounds of
-        // those that fit: of one to four rounds the ones that end first, by the keys of a round's longest part and 128 for its start
-        // and end.  256 parts to a sequence at most (the join reads them all).
         p.form = kFormToken;
         p.rows = static_cast<int32_t>(most_rows);
-        int64_t keys = 0;
-        for (int b = 0; b < batch; ++b) {
-            if (seqs[b].n_q == 0) continue;
-            keys += visible_keys(seqs[b], counted, window, n_sink);
-            p.logit_floats += mass ? static_cast<int64_t>(seqs[b].n_q) * c.n_heads * seqs[b].n_kv : 0;
-        }
-        const int64_t fit = static_cast<int64_t>(c.sm_count) * token_ctas(c.head_dim / 32, static_cast<int>(c.elem));
-        const auto ctas_of = [&](int64_t part) {
-            int64_t n = 0;
-            p.part_keys = part;
-            for (int b = 0; b < batch; ++b) n += parts_of(p, seqs[b], counted, window, n_sink);
-            return n * c.kv_heads;
-        };
-        int64_t best = 0, best_cost = 0;
-        for (int rounds = 1; rounds <= 4; ++rounds) {
-            int64_t part = (keys * c.kv_heads + rounds * fit - 1) / (rounds * fit);
-            part = part < (longest + 255) / 256 ? (longest + 255) / 256 : part;
-            part = part < 64 ? 64 : (part + 63) / 64 * 64;
-            int64_t n = ctas_of(part);
-            for (int tries = 0; n > rounds * fit && tries < 8; ++tries) {
-                part += (part / 16 + 63) / 64 * 64;
-                n = ctas_of(part);
-            }
-            const int64_t cost = (n + fit - 1) / fit * ((part < longest ? part : longest) + 128);
-            if (!best || cost < best_cost) { best = part; best_cost = cost; }
-        }
-        p.part_keys = best;
-        for (int b = 0; b < batch; ++b) {
-            const int32_t n = parts_of(p, seqs[b], counted, window, n_sink);
-            p.blocks += n;
-            p.splits = n > p.splits ? n : p.splits;
-        }
+        for (int b = 0; b < batch; ++b)
+            if (mass) p.logit_floats += static_cast<int64_t>(seqs[b].n_q) * c.n_heads * seqs[b].n_kv;
+        cut_for_tokens(p, static_cast<int64_t>(c.sm_count) * token_ctas(c.head_dim / 32, static_cast<int>(c.elem)), c.kv_heads, batch, seqs, counted, window, n_sink);
     } else {
         p.form = kFormTile;
         p.pack = pack_of(group);

@@ -1,18 +1,10 @@
 // Launchers of the calls on a cache in pages (page_*.cu) and what they are given.
 #pragma once
 
+#include "page_plan.h"
 #include "serve.h"
 
 namespace mvla {
-
-constexpr int kPageGroup = 32;               // elements that share a scale in e2m1 pages
-// Exponents of the scales: from 2^-117 on every element that the codes can stand for is a normal number of 32 bits and of bf16; up to 2^119 (e4m3) and 2^125
-// (e2m1) it is a finite one.
-constexpr int kScaleLeast = -117, kScaleMostE4m3 = 119, kScaleMostE2m1 = 125;
-
-// Bytes of a cached row of one head, and of its scales.
-__host__ __device__ inline int page_row_bytes(int kind, int d, int wide) { return kind == MVLA_PAGE_ROWS ? d * wide : kind == MVLA_PAGE_E4M3 ? d : d / 2; }
-__host__ __device__ inline int page_row_scales(int kind, int d) { return kind == MVLA_PAGE_ROWS ? 0 : kind == MVLA_PAGE_E4M3 ? 1 : d / kPageGroup; }
 
 struct PagePool {
     void *k, *v;
@@ -45,5 +37,10 @@ struct PageRowsArgs {
 };
 cudaError_t launch_page_write(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream);
 cudaError_t launch_page_read(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream);
+
+// ---- attention
+
+// Single tokens (launch_attend_token's), over pages; q and out bf16.  Behind it: launch_attend_finish.
+cudaError_t launch_page_token(int kind, const AttArgs& a, const PagePool& pool, int rows, cudaStream_t stream);
 
 }  // namespace mvla

@@ -82,8 +82,20 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     if (!guard.ok) return MVLA_ERR_CUDA;
     note_work(ctx);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    // the sequences' rows, packed one after another
     char* const ws = static_cast<char*>(a->workspace);
+    mvla_attention w = as_window(a);
+    w.workspace = a->workspace;
+    w.workspace_bytes = plan.attend.bytes;
+    CtxView h = v;
+    static_cast<ServeShape&>(h) = hidden_shape(v);
+    if (plan.attend.form == kFormToken && plan.dense_k < 0) {
+        AttArgs t;
+        fill_attention(t, h, batch, seqs, &w, plan.attend);
+        cudaError_t e = launch_page_token(a->pages.kind, t, pool_of(v, a->pages, a->table, a->table_stride), plan.attend.rows, st);
+        if (e == cudaSuccess && plan.attend.splits > 1) e = launch_attend_finish(t, st);
+        return close_call(ctx, e);
+    }
+    // the sequences' rows, packed one after another
     mvla_seq dense[kMaxBatch];
     PageRowsArgs k;
     std::memset(&k, 0, sizeof k);
@@ -94,12 +106,9 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
         k.s[b] = PageSeq{0, seqs[b].n_kv, seqs[b].n_kv, row, b};
         row += seqs[b].n_kv;
     }
-    mvla_attention w = as_window(a);
     w.k = k.k = ws + plan.dense_k;
     w.v = k.v = ws + plan.dense_v;
     w.kv_rows = row;
-    w.workspace = a->workspace;
-    w.workspace_bytes = plan.attend.bytes;
     k.pool = pool_of(v, a->pages, a->table, a->table_stride);
     k.kv_len = a->kv_len;
     k.k_stride = k.v_stride = static_cast<int64_t>(v.kv_heads) * v.head_dim;
@@ -108,8 +117,6 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     k.from_start = 1;
     const cudaError_t e = row > 0 ? launch_page_read(v.hidden_dtype, a->pages.kind, k, st) : cudaSuccess;
     if (e != cudaSuccess) return close_call(ctx, e);
-    CtxView h = v;
-    static_cast<ServeShape&>(h) = hidden_shape(v);
     return enqueue_attention(ctx, h, batch, dense, &w, plan.attend, st);
 }
 

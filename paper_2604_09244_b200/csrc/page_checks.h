@@ -1,19 +1,18 @@
 // Host-side checks and plans of the calls on a cache in pages: arithmetic on descriptors and addresses, without a device.
 #pragma once
 
+#include "page_plan.h"
 #include "serve_checks.h"
 
 namespace mvla {
 
 inline int64_t page_data_bytes(const ServeShape& v, const mvla_pages& p)
 {
-    const int64_t row = p.kind == MVLA_PAGE_ROWS ? v.head_dim * static_cast<int64_t>(v.wide) : p.kind == MVLA_PAGE_E4M3 ? v.head_dim : v.head_dim / 2;
-    return p.n_pages * v.kv_heads * p.page_rows * row;
+    return p.n_pages * v.kv_heads * p.page_rows * page_row_bytes(p.kind, v.head_dim, static_cast<int>(v.wide));
 }
 inline int64_t page_scale_bytes(const ServeShape& v, const mvla_pages& p)
 {
-    const int64_t row = p.kind == MVLA_PAGE_ROWS ? 0 : p.kind == MVLA_PAGE_E4M3 ? 1 : v.head_dim / 32;
-    return p.n_pages * v.kv_heads * p.page_rows * row;
+    return p.n_pages * v.kv_heads * p.page_rows * page_row_scales(p.kind, v.head_dim);
 }
 
 // The sequences of a call, and the table that has to name their pages.
@@ -96,10 +95,11 @@ inline int32_t check_page_rows(const ServeShape& v, int32_t batch, const mvla_se
     return MVLA_OK;
 }
 
-// ---- attention over pages: rows taken out of the pages into the workspace, then attended over as packed rows
+// ---- attention over pages
 
 struct PageAttendPlan {
     AttendPlan attend;
+    // where rows are taken out of the pages first and attended over as packed rows (-1: they are not)
     int64_t dense_k = -1, dense_v = -1, bytes = 0;
 };
 
@@ -146,10 +146,41 @@ inline int32_t check_page_attention(const ServeShape& v, int32_t batch, const mv
     return MVLA_OK;
 }
 
+// Single tokens, of whose CTAs `ctas` fit on a multiprocessor.
+inline AttendPlan plan_tokens(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, int ctas)
+{
+    AttendPlan p;
+    p.form = kFormToken;
+    p.rows = 0;
+    for (int b = 0; b < batch; ++b) {
+        p.total_q += seqs[b].n_q;
+        p.total_kv += seqs[b].n_kv;
+        p.rows = std::max(p.rows, static_cast<int32_t>(seqs[b].n_q * static_cast<int64_t>(c.n_heads / c.kv_heads)));
+    }
+    cut_for_tokens(p, static_cast<int64_t>(c.sm_count) * ctas, c.kv_heads, batch, seqs, counted, window, n_sink);
+    if (p.splits > 1) {
+        int64_t part_q = 0;
+        for (int b = 0; b < batch; ++b) part_q += static_cast<int64_t>(parts_of(p, seqs[b], counted, window, n_sink)) * seqs[b].n_q;
+        Workspace w;
+        p.part_o = w.take(part_q * c.n_heads * c.head_dim * static_cast<int64_t>(sizeof(float)));
+        p.part_ml = w.take(part_q * c.n_heads * 2 * static_cast<int64_t>(sizeof(float)));
+        p.bytes = w.bytes;
+    }
+    return p;
+}
+
 inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_paged_attention* a)
 {
     PageAttendPlan p;
     const ServeShape h = hidden_shape(v);
+    const int64_t group = v.n_heads / v.kv_heads;
+    int64_t most_rows = 0;
+    for (int b = 0; b < batch; ++b) most_rows = std::max(most_rows, seqs[b].n_q * group);
+    if (h.dtype != MVLA_DTYPE_FP32 && most_rows <= kTokenRows) {
+        p.attend = plan_tokens(h, batch, seqs, !a->kv_len, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32));
+        p.bytes = p.attend.bytes;
+        return p;
+    }
     p.attend = plan_attend(h, batch, seqs, !a->kv_len, a->window, a->n_sink, false);
     Workspace w;
     w.take(p.attend.bytes);

@@ -1,0 +1,40 @@
+// Sizes of a cache in pages that plans and kernels go by.
+#pragma once
+
+#include "mvla_prune.h"
+
+#ifdef __CUDACC__
+#define MVLA_BOTH __host__ __device__
+#else
+#define MVLA_BOTH
+#endif
+
+namespace mvla {
+
+constexpr int kPageGroup = 32;               // elements that share a scale in e2m1 pages
+// Exponents of the scales: from 2^-117 on every element that the codes can stand for is a normal number of 32 bits and of bf16; up to 2^119 (e4m3) and 2^125
+// (e2m1) it is a finite one.
+constexpr int kScaleLeast = -117, kScaleMostE4m3 = 119, kScaleMostE2m1 = 125;
+
+// Bytes of a cached row of one head, and of its scales.
+MVLA_BOTH constexpr int page_row_bytes(int kind, int d, int wide) { return kind == MVLA_PAGE_ROWS ? d * wide : kind == MVLA_PAGE_E4M3 ? d : d / 2; }
+MVLA_BOTH constexpr int page_row_scales(int kind, int d) { return kind == MVLA_PAGE_ROWS ? 0 : kind == MVLA_PAGE_E4M3 ? 1 : d / kPageGroup; }
+
+// Single tokens (page_token.cu): subtiles of 16 keys in a warp's tile, bytes of a tile in shared memory (in whole groups of 64 columns of the values),
+// tiles of a warp, and the CTAs that fit on a multiprocessor (four at most: by registers).
+constexpr int kPageTokenStages = 3;
+MVLA_BOTH constexpr int page_token_sub(int kind, int pieces_of_32) { return pieces_of_32 <= 2 || (kind == MVLA_PAGE_E2M1 && pieces_of_32 <= 4) ? 2 : 1; }
+MVLA_BOTH constexpr int page_token_tile(int kind, int pieces_of_32)
+{
+    const int run = kind == MVLA_PAGE_ROWS ? 16 : kind == MVLA_PAGE_E4M3 ? 8 : 4, scales = kind == MVLA_PAGE_ROWS ? 0 : kind == MVLA_PAGE_E4M3 ? 1 : pieces_of_32;
+    return page_token_sub(kind, pieces_of_32) * ((2 * pieces_of_32 + 4 * ((pieces_of_32 + 1) / 2)) * 32 * run + 32 * scales);
+}
+MVLA_BOTH constexpr int page_token_ctas(int kind, int pieces_of_32)
+{
+    // (queries of 16 rows, factors of the scales, and what the system takes)
+    const int fixed = 1024 * pieces_of_32 + (kind == MVLA_PAGE_E2M1 ? 256 * page_token_sub(kind, pieces_of_32) * pieces_of_32 : 0) + 2048;
+    const int n = 227 * 1024 / (4 * kPageTokenStages * page_token_tile(kind, pieces_of_32) + fixed);
+    return n > 4 ? 4 : n < 1 ? 1 : n;
+}
+
+}  // namespace mvla

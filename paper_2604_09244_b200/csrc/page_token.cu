@@ -1,0 +1,603 @@
+// Attention of single tokens over a cache in pages: at most 16 query rows of a sequence share a key head.  The rows' own type (bf16), e4m3 or e2m1.
+//
+// Bound by the bytes of the pages, and by unpacking them.  A warp takes tiles of 16 or 32 keys as the registers that the tensor cores read (m16n8k16):
+// keys are the 16 rows of the first product, columns of the values those of the second, query rows the 8 columns of both.  Which element of the
+// head meets which is free as long as queries and keys agree, so a lane copies runs of its own, two tiles ahead, asynchronously, and no lane waits for
+// another's but for the scales, which all of them read.  16 rows of a tile never cross a page, so that a page number is looked up once for 16 keys, a tile before its copies begin.
+//   Quantised keys and values become fp16 in registers, which holds every code; values of two keys are interleaved before that, in their 8 or 4 bits,
+// which makes them the second product's operand.  Scales are powers of two.  One a row (e4m3): a key's multiplies its scores; a value's is added to
+// the exponent of its weight, w = 2^(x + e - reference).  So there are two references and two exponentials: those of the weights that meet the values, and those
+// of the sum that divides them.  One for 32 elements (e2m1): the row's largest is taken as above, the rest of it multiplies the codes (2^13 times
+// the quotient of the scales: 6 2^13 is a number of fp16, and a group 2^-27 of the largest one is nothing).  Queries are fp16 too, every row
+// times a power of two that puts its largest element between 2^14 and 2^15.  bf16 weights (unquantised pages) meet the values in two
+// parts, what the type holds and what it leaves; fp16 ones are one part, in units of 2^-kF16Lift of their reference.
+//   A sequence's visible keys are cut into parts of about the same length over the whole batch; a CTA is four warps that take the part's tiles in turn.
+#include "attend.cuh"
+#include "page.cuh"
+
+#include <cuda_fp16.h>
+
+namespace mvla {
+namespace {
+
+constexpr int kWarps = 4;
+constexpr int kStages = kPageTokenStages;
+
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int there)
+{
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(there ? 16 : 0) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(there ? BYTES : 0) : "memory");
+}
+__device__ __forceinline__ void copies_done() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ uint32_t bits_of(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ __forceinline__ uint32_t bits_of(__nv_bfloat162 h) { return *reinterpret_cast<const uint32_t*>(&h); }
+__device__ __forceinline__ uint32_t bits_of(__half2_raw h) { return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16; }
+__device__ __forceinline__ uint32_t from_e4m3(uint32_t two) { return bits_of(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3)); }
+__device__ __forceinline__ uint32_t from_e2m1(uint32_t two) { return bits_of(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(two), __NV_E2M1)); }
+__device__ __forceinline__ uint32_t times(uint32_t x, uint32_t f)
+{
+    return bits_of(__hmul2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&f)));
+}
+// The transpose of an 8 x 8 block of 16-bit values, a pair of neighbours in every lane.
+__device__ __forceinline__ uint32_t transpose8(uint32_t x)
+{
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+template <bool F16>
+__device__ __forceinline__ void mma16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1)
+{
+    if constexpr (F16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                     : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// Eight codes as they lie in memory, and how many runs of eight a lane copies at once at most: of a key's row, of a value's.
+template <int KIND> struct Run;
+template <> struct Run<MVLA_PAGE_ROWS> { using Word = uint4; static constexpr int kKeyRuns = 1, kValueRuns = 1; };
+template <> struct Run<MVLA_PAGE_E4M3> { using Word = uint2; static constexpr int kKeyRuns = 2, kValueRuns = 2; };
+template <> struct Run<MVLA_PAGE_E2M1> { using Word = uint32_t; static constexpr int kKeyRuns = 4, kValueRuns = 2; };
+
+// A warp's tile in shared memory: every lane's runs of its rows of keys (g, g + 8 of 16), of values (2 c, 2 c + 1, 2 c + 8, 2 c + 9), and the scales of keys
+// and values.  Runs of a key's row: D32, four lanes side by side; in lots of kKeyRuns, then halves of those, that one lane has next to one another.  Runs of
+// a value's row: M64, eight lanes side by side, likewise.
+template <int KIND, int D32>
+struct Tile {
+    static constexpr int kM64 = (D32 + 1) / 2, kSub = page_token_sub(KIND, D32), kKeys = 16 * kSub;
+    static constexpr int kRun = static_cast<int>(sizeof(typename Run<KIND>::Word));
+    static constexpr int kKeyRow = D32 * 32 * kRun, kValueRow = kM64 * 32 * kRun;       // of a lane's row, for the whole warp
+    static constexpr int kGroups = page_row_scales(KIND, D32 * 32);
+    static constexpr int kRows = kSub * (2 * kKeyRow + 4 * kValueRow), kScales = kSub * 2 * 16 * kGroups;
+    static constexpr int kBytes = kRows + kScales;
+    static_assert(kBytes == page_token_tile(KIND, D32), "the plan's size");
+    // runs i .. i + n - 1 of a lane lie together: how many, and the first
+    static __device__ __forceinline__ constexpr int lot(int i, int all, int most)
+    {
+        int n = most;
+        while (i / n * n + n > all) n /= 2;
+        return n;
+    }
+    // first element of run i of lane c's keys, first column of run m of lane g's values
+    static __device__ __forceinline__ constexpr int element(int i, int c)
+    {
+        const int n = lot(i, D32, Run<KIND>::kKeyRuns);
+        return i / n * n * 32 + 8 * n * c + 8 * (i % n);
+    }
+    static __device__ __forceinline__ constexpr int column(int m, int g)
+    {
+        const int n = lot(m, D32 / 2, Run<KIND>::kValueRuns);
+        return m < D32 / 2 ? m / n * n * 64 + 8 * n * g + 8 * (m % n) : 64 * m + 8 * g;
+    }
+    // where run i of a lane lies in its row of the tile
+    static __device__ __forceinline__ constexpr int key_at(int i, int lane)
+    {
+        const int n = lot(i, D32, Run<KIND>::kKeyRuns);
+        return (i / n * n * 32 + lane * n + i % n) * kRun;
+    }
+    static __device__ __forceinline__ constexpr int value_at(int m, int lane)
+    {
+        const int n = m < D32 / 2 ? lot(m, D32 / 2, Run<KIND>::kValueRuns) : 1;
+        return (m / n * n * 32 + lane * n + m % n) * kRun;
+    }
+};
+
+template <int KIND, int D32, int NR>
+__global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_token_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ PagePool pool)
+{
+    using Sh = Tile<KIND, D32>;
+    using Word = typename Run<KIND>::Word;
+    constexpr bool kScaled = KIND != MVLA_PAGE_ROWS, kE2m1 = KIND == MVLA_PAGE_E2M1;
+    constexpr int D = D32 * 32, M64 = Sh::kM64, U = Sh::kSub, G = Sh::kGroups;
+    constexpr float kLift = kScaled ? kF16Lift : 0.f;
+    constexpr int kCodeLift = kE2m1 ? 13 : 0;
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ uint4 q_frag[D32][NR][32];
+    __shared__ float merge_m[kWarps][16], merge_f[kWarps][16], merge_l[kWarps][16];
+    __shared__ float q_lift[16], q_scale[16];                // what a row's queries are multiplied by; what that makes of the scores' scale
+    __shared__ __align__(4) uint16_t factors[kE2m1 ? kWarps : 1][kE2m1 ? U : 1][2][kE2m1 ? D32 : 1][16];      // of the groups of a tile's rows, fp16
+    pdl_wait();
+    pdl_trigger();
+    const int t = threadIdx.x, lane = t & 31, warp = t >> 5, g = lane >> 2, c = lane & 3;
+    const AttSeq& s = a.s[seq_of_block(a, blockIdx.x)];
+    const int hk = blockIdx.y, group = a.n_heads / a.kv_heads, n_rows = s.n_q * group, len = seq_len(a, s);
+    int p[NR][2];                                            // positions of this lane's rows 8 n + 2 c + e
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const int r = 8 * n + 2 * c + e;
+            p[n][e] = r < n_rows ? query_pos(a, s, len, r / group) : -1;
+        }
+    const int lo = query_pos(a, s, len, 0), hi = query_pos(a, s, len, s.n_q - 1);
+    const TileRange range = tile_range(a, len, lo, hi, Sh::kKeys);
+    const int part = static_cast<int>(blockIdx.x) - s.blk0, per_part = (range.count + s.parts - 1) / s.parts;
+    const int t0 = part * per_part, t1 = min(range.count, t0 + per_part);
+    // o[m][i][n]: columns column(m, g) + 2 i and + 1 (values 0, 1 and 2, 3), rows 8 n + 2 c and + 1
+    float o[M64][4][NR][4];
+#pragma unroll
+    for (int m = 0; m < M64; ++m)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int n = 0; n < NR; ++n) o[m][i][n][0] = o[m][i][n][1] = o[m][i][n][2] = o[m][i][n][3] = 0.f;
+    // references of the sum, and of the weights as they meet the values (the same where there are no scales)
+    float ref[NR][2], ref_w[NR][2], sum[NR][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { ref[n][e] = ref_w[n][e] = -CUDART_INF_F; sum[n][e] = 0.f; }
+
+    // Tile t0 + warp + kWarps u is this warp's u-th.  Page of its keys 16 (lane / 16) ... (of the first sixteen, where a tile has no more):
+    const int mine = t1 > t0 + warp ? (t1 - t0 - warp + kWarps - 1) / kWarps : 0;
+    const auto first_key = [&](int u) { return range.tile(t0 + warp + kWarps * u) * Sh::kKeys; };
+    const auto look_up = [&](int u) {
+        if (u >= mine) return -1;
+        const int j = first_key(u) + (U > 1 ? lane & 16 : 0);
+        return j < len ? page_of(pool, s.index, j) : -1;
+    };
+    uint8_t* const stages = ring + warp * kStages * Sh::kBytes;
+    const uint32_t stages_at = smem_u32(stages);
+    const int row_bytes = page_row_bytes(KIND, D, 2);
+    const uint8_t* const kb = static_cast<const uint8_t*>(pool.k);
+    const uint8_t* const vb = static_cast<const uint8_t*>(pool.v);
+    // starts the copies of a tile (always a group of copies, an empty one too)
+    const auto fetch = [&](int u, int stage, int page) {
+        if (u < mine) {
+            const int j0 = first_key(u);
+            uint32_t dst = stages_at + stage * Sh::kBytes;
+#pragma unroll
+            for (int v = 0; v < U; ++v, dst += 2 * Sh::kKeyRow + 4 * Sh::kValueRow) {
+                const int pg = __shfl_sync(0xffffffffu, page, 16 * v);
+                const bool there = pg >= 0;
+                const int64_t row0 = there ? page_row(pool, pg, hk, j0 + 16 * v) : 0;
+                const uint8_t* const k0 = kb + row0 * row_bytes;
+                const uint8_t* const v0 = vb + row0 * row_bytes;
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+#pragma unroll
+                    for (int i = 0; i < D32; ++i) {
+                        constexpr int most = Run<KIND>::kKeyRuns;
+                        const int lot = Sh::lot(i, D32, most);
+                        if (i % lot) continue;
+                        const uint32_t to = dst + n * Sh::kKeyRow + Sh::key_at(i, lane);
+                        const uint8_t* const from = k0 + (g + 8 * n) * row_bytes + Sh::element(i, c) / 8 * Sh::kRun;
+                        if (lot == 4) copy_async<(4 * Sh::kRun > 16 ? 16 : 4 * Sh::kRun)>(to, from, there);
+                        else if (lot == 2) copy_async<(2 * Sh::kRun > 16 ? 16 : 2 * Sh::kRun)>(to, from, there);
+                        else copy_async<Sh::kRun>(to, from, there);
+                    }
+#pragma unroll
+                for (int n = 0; n < 4; ++n)
+#pragma unroll
+                    for (int m = 0; m < M64; ++m) {
+                        const int lot = m < D32 / 2 ? Sh::lot(m, D32 / 2, Run<KIND>::kValueRuns) : 1;
+                        if (m % lot) continue;
+                        if (m >= D32 / 2 && g >= 4) continue;
+                        const uint32_t to = dst + 2 * Sh::kKeyRow + n * Sh::kValueRow + Sh::value_at(m, lane);
+                        const uint8_t* const from = v0 + (2 * c + (n & 1) + 8 * (n >> 1)) * row_bytes + Sh::column(m, g) / 8 * Sh::kRun;
+                        if (lot == 2) copy_async<(2 * Sh::kRun > 16 ? 16 : 2 * Sh::kRun)>(to, from, there);
+                        else copy_async<Sh::kRun>(to, from, there);
+                    }
+                if constexpr (kScaled) {                     // (16 rows' scales lie side by side: 16 bytes a lane)
+                    if (lane < 2 * G) {
+                        const uint8_t* const from = (lane < G ? pool.k_scale : pool.v_scale) + row0 * G + lane % G * 16;
+                        copy_async<16>(stages_at + stage * Sh::kBytes + Sh::kRows + (v * 2 * G + lane) * 16, from, there);
+                    }
+                }
+            }
+        }
+        copies_done();
+    };
+    int ahead[kStages - 1];
+#pragma unroll
+    for (int u = 0; u < kStages - 1; ++u) ahead[u] = look_up(u);
+#pragma unroll
+    for (int u = 0; u < kStages - 1; ++u) fetch(u, u, ahead[u]);
+    int next = look_up(kStages - 1);
+    // ---- queries: the first product's operand
+    const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.q);
+    const auto query = [&](int r) { return q + ((s.q_row + r / group) * a.n_heads + hk * group + r % group) * D; };
+    for (int r = warp; r < 8 * NR; r += kWarps) {
+        uint32_t top = 0;
+        if (kScaled && r < n_rows)
+            for (int i = 2 * lane; i < D; i += 64) top = __vmaxu2(top, *reinterpret_cast<const uint32_t*>(query(r) + i) & 0x7FFF7FFFu);
+        top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16));
+        if (lane == 0) {
+            const int e = kScaled && top ? max(14 - (static_cast<int>(top >> 7) - 127), -113) : 0;       // (2^126 times the smallest ones at most)
+            q_lift[r] = two_to(min(e, 126));
+            q_scale[r] = a.scale_log2 * two_to(-min(e, 126));
+        }
+    }
+    __syncthreads();
+    for (int u = t; u < D32 * NR * 32; u += kWarps * 32) {
+        const int piece = u / (NR * 32), n = u / 32 % NR, l = u & 31, r = (l >> 2) + 8 * n;
+        uint4 w = make_uint4(0, 0, 0, 0);
+        if (r < n_rows) w = *reinterpret_cast<const uint4*>(query(r) + Sh::element(piece, l & 3));
+        if constexpr (kScaled) {
+            const float f = q_lift[r];
+            uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = bits_of(__floats2half2_rn(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xFFFF0000u) * f));
+            w = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+        q_frag[piece][n][l] = w;
+    }
+    __syncthreads();
+    float q_by[NR][2];
+#pragma unroll
+    for (int n = 0; n < NR; ++n) { q_by[n][0] = q_scale[8 * n + 2 * c]; q_by[n][1] = q_scale[8 * n + 2 * c + 1]; }
+
+    int stage = 0;
+    for (int u = 0; u < mine; ++u, stage = stage + 1 < kStages ? stage + 1 : 0) {
+        const int then = look_up(u + kStages);
+        wait_copies<kStages - 2>();
+        __syncwarp();                                        // (every lane's copies are there; nobody reads the last tile any more)
+        fetch(u + kStages - 1, stage > 0 ? stage - 1 : kStages - 1, next);
+        next = then;
+        const int j0 = first_key(u);
+        const bool all = j0 + Sh::kKeys - 1 <= lo && (hi - j0 < a.window || j0 + Sh::kKeys - 1 < a.n_sink);      // (lo is below the length)
+        const uint8_t* const tile = stages + stage * Sh::kBytes;
+        int largest[U];                                      // e2m1: byte of the largest scale of key lane % 16, or of its values (lanes 16 ...)
+        if constexpr (kE2m1) {
+#pragma unroll
+            for (int v = 0; v < U; ++v) {
+                const uint8_t* const bytes = tile + Sh::kRows + v * 2 * G * 16 + lane * G;
+                int b[D32], top = 0;
+                if constexpr (D32 % 4 == 0) {
+#pragma unroll
+                    for (int i = 0; i < D32; i += 4) {
+                        const uint32_t w = *reinterpret_cast<const uint32_t*>(bytes + i);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k) b[i + k] = w >> (8 * k) & 0xFFu;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < D32; ++i) b[i] = bytes[i];
+                }
+#pragma unroll
+                for (int i = 0; i < D32; ++i) top = max(top, b[i]);
+                largest[v] = top;
+                // 2^(13 + difference) in fp16, nothing below its normal numbers
+#pragma unroll
+                for (int i = 0; i < D32; ++i) factors[warp][v][lane >> 4][i][lane & 15] = static_cast<uint16_t>(max(b[i] - top + 15 + kCodeLift, 0) << 10);
+            }
+            __syncwarp();
+        }
+        // x[v][n][2 k + e]: key 16 v + g + 8 k, row 8 n + 2 c + e
+        float x[U][NR][4] = {};
+#pragma unroll
+        for (int i = 0; i < D32; ++i) {
+            uint4 y[NR];
+#pragma unroll
+            for (int n = 0; n < NR; ++n) y[n] = q_frag[i][n][lane];
+#pragma unroll
+            for (int v = 0; v < U; ++v) {
+                const uint8_t* const rows = tile + v * (2 * Sh::kKeyRow + 4 * Sh::kValueRow) + Sh::key_at(i, lane);
+                const Word k0 = *reinterpret_cast<const Word*>(rows), k1 = *reinterpret_cast<const Word*>(rows + Sh::kKeyRow);
+                uint32_t w0[4], w1[4];
+                if constexpr (KIND == MVLA_PAGE_ROWS) {
+                    w0[0] = k0.x; w0[1] = k0.y; w0[2] = k0.z; w0[3] = k0.w;
+                    w1[0] = k1.x; w1[1] = k1.y; w1[2] = k1.z; w1[3] = k1.w;
+                } else if constexpr (KIND == MVLA_PAGE_E4M3) {
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        w0[h] = from_e4m3((h < 2 ? k0.x : k0.y) >> (16 * (h & 1)) & 0xFFFFu);
+                        w1[h] = from_e4m3((h < 2 ? k1.x : k1.y) >> (16 * (h & 1)) & 0xFFFFu);
+                    }
+                } else {
+                    const int gr = Sh::element(i, c) / kPageGroup;
+                    const uint32_t f0 = factors[warp][v][0][gr][g] * 0x10001u, f1 = factors[warp][v][0][gr][g + 8] * 0x10001u;
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        w0[h] = times(from_e2m1(k0 >> (8 * h) & 0xFFu), f0);
+                        w1[h] = times(from_e2m1(k1 >> (8 * h) & 0xFFu), f1);
+                    }
+                }
+#pragma unroll
+                for (int n = 0; n < NR; ++n) {
+                    mma16<kScaled>(x[v][n], w0[0], w1[0], w0[1], w1[1], y[n].x, y[n].y);
+                    mma16<kScaled>(x[v][n], w0[2], w1[2], w0[3], w1[3], y[n].z, y[n].w);
+                }
+            }
+        }
+        float of_value[U][2];                                // exponent of the scale of key g + 8 k's values
+#pragma unroll
+        for (int v = 0; v < U; ++v) {
+            uint32_t kbyte[2] = {127, 127};
+            of_value[v][0] = of_value[v][1] = 0.f;
+            if constexpr (KIND == MVLA_PAGE_E4M3) {
+                const uint8_t* const bytes = tile + Sh::kRows + v * 32;
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    kbyte[k] = bytes[g + 8 * k];
+                    of_value[v][k] = static_cast<float>(static_cast<int>(bytes[16 + g + 8 * k]) - 127);
+                }
+            } else if constexpr (kE2m1) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    kbyte[k] = static_cast<uint32_t>(__shfl_sync(0xffffffffu, largest[v], g + 8 * k));
+                    of_value[v][k] = static_cast<float>(__shfl_sync(0xffffffffu, largest[v], 16 + g + 8 * k) - 127 - kCodeLift);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const float by = __uint_as_float(kbyte[k] << 23) * (kE2m1 ? 0x1p-13f : 1.f);     // (without the codes' lift)
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) x[v][n][2 * k + e] *= kScaled ? q_by[n][e] * by : q_by[n][e];
+                }
+        }
+        uint32_t seen[U][2] = {};                            // four bits for every key g + 8 k: which lanes have a row that sees it
+        if (!all) {
+#pragma unroll
+            for (int v = 0; v < U; ++v)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const int j = j0 + 16 * v + g + 8 * k, at = j < len ? j : -1;
+                    bool some = false;
+#pragma unroll
+                    for (int n = 0; n < NR; ++n)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            const bool on = sees(p[n][e], at, a.window, a.n_sink);
+                            some |= on;
+                            if (!on) x[v][n][2 * k + e] = -CUDART_INF_F;
+                        }
+                    seen[v][k] = __ballot_sync(0xffffffffu, some);
+                }
+        }
+        // references
+        float top[NR][2], top_w[NR][2];
+        bool move = false;
+#pragma unroll
+        for (int n = 0; n < NR; ++n)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                top[n][e] = fmaxf(x[0][n][e], x[0][n][2 + e]);
+                top_w[n][e] = fmaxf(x[0][n][e] + of_value[0][0], x[0][n][2 + e] + of_value[0][1]);
+                if (U > 1) {
+                    top[n][e] = fmaxf(top[n][e], fmaxf(x[U - 1][n][e], x[U - 1][n][2 + e]));
+                    top_w[n][e] = fmaxf(top_w[n][e], fmaxf(x[U - 1][n][e] + of_value[U - 1][0], x[U - 1][n][2 + e] + of_value[U - 1][1]));
+                }
+                move |= top[n][e] > ref[n][e] + 8.f;
+                if (kScaled) move |= top_w[n][e] > ref_w[n][e] + 8.f;
+            }
+        if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+            for (int n = 0; n < NR; ++n)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float m = top[n][e], w = top_w[n][e];
+#pragma unroll
+                    for (int k = 4; k < 32; k *= 2) {
+                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
+                        w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, k));
+                    }
+                    m = fmaxf(ref[n][e], m);
+                    w = kScaled ? fmaxf(ref_w[n][e], w) : m;
+                    sum[n][e] *= m == ref[n][e] ? 1.f : exp2f(ref[n][e] - m);
+                    const float f = w == ref_w[n][e] ? 1.f : exp2f(ref_w[n][e] - w);
+                    ref[n][e] = m;
+                    ref_w[n][e] = w;
+#pragma unroll
+                    for (int mm = 0; mm < M64; ++mm)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) { o[mm][i][n][e] *= f; o[mm][i][n][2 + e] *= f; }
+                }
+        }
+#pragma unroll
+        for (int v = 0; v < U; ++v) {
+            // weights, as the second product's operand: keys 2 c, 2 c + 1 (+ 8) of row 8 n + g
+            uint32_t w_hi[NR][2], w_lo[NR][2];
+#pragma unroll
+            for (int n = 0; n < NR; ++n) {
+                float y[2][2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const float b = ref[n][e] == -CUDART_INF_F ? 0.f : ref[n][e], b_w = ref_w[n][e] == -CUDART_INF_F ? 0.f : ref_w[n][e] - kLift;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+                        const float z = ex2_approx(x[v][n][2 * k + e] - b);
+                        sum[n][e] += z;
+                        y[k][e] = kScaled ? ex2_approx(x[v][n][2 * k + e] + of_value[v][k] - b_w) : z;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    if constexpr (kScaled) {
+                        w_hi[n][k] = transpose8(bits_of(__floats2half2_rn(y[k][0], y[k][1])));
+                    } else {
+                        const uint32_t w = bits_of(__floats2bfloat162_rn(y[k][0], y[k][1]));
+                        w_hi[n][k] = transpose8(w);
+                        w_lo[n][k] = transpose8(bits_of(__floats2bfloat162_rn(y[k][0] - __uint_as_float(w << 16), y[k][1] - __uint_as_float(w & 0xFFFF0000u))));
+                    }
+                }
+            }
+            bool hidden[4];                                  // values of keys that no row sees (0 times NaN is NaN)
+#pragma unroll
+            for (int n = 0; n < 4; ++n) hidden[n] = !kE2m1 && !all && (seen[v][n >> 1] >> (4 * (2 * c + (n & 1))) & 0xFu) == 0;
+#pragma unroll
+            for (int m = 0; m < M64; ++m) {
+                Word w[4];
+#pragma unroll
+                for (int n = 0; n < 4; ++n) {
+                    w[n] = Word{};
+                    if (!hidden[n] && (m < D32 / 2 || g < 4))
+                        w[n] = *reinterpret_cast<const Word*>(tile + v * (2 * Sh::kKeyRow + 4 * Sh::kValueRow) + 2 * Sh::kKeyRow + n * Sh::kValueRow + Sh::value_at(m, lane));
+                }
+                // op[i][h]: columns 2 i (h = 0, 2) and 2 i + 1 of the lane's run, keys 2 c, 2 c + 1 (h < 2) and 2 c + 8, 2 c + 9
+                uint32_t op[4][4];
+                if constexpr (KIND == MVLA_PAGE_ROWS) {
+                    const uint32_t x4[4][4] = {{w[0].x, w[0].y, w[0].z, w[0].w}, {w[1].x, w[1].y, w[1].z, w[1].w}, {w[2].x, w[2].y, w[2].z, w[2].w}, {w[3].x, w[3].y, w[3].z, w[3].w}};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            op[i][2 * h] = __byte_perm(x4[2 * h][i], x4[2 * h + 1][i], 0x5410);
+                            op[i][2 * h + 1] = __byte_perm(x4[2 * h][i], x4[2 * h + 1][i], 0x7632);
+                        }
+                } else if constexpr (KIND == MVLA_PAGE_E4M3) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {        // (the two keys' bytes of two columns)
+                            const uint32_t two = __byte_perm(i < 2 ? w[2 * h].x : w[2 * h].y, i < 2 ? w[2 * h + 1].x : w[2 * h + 1].y, i & 1 ? 0x7362 : 0x5140);
+                            op[i][2 * h] = from_e4m3(two & 0xFFFFu);
+                            op[i][2 * h + 1] = from_e4m3(two >> 16);
+                        }
+                } else {
+                    const int gr = min(Sh::column(m, g) / kPageGroup, D32 - 1);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {            // (the two keys' halves of a byte, of even and of odd columns)
+                        const uint32_t f = *reinterpret_cast<const uint32_t*>(&factors[warp][v][1][gr][2 * c + 8 * h]);
+                        const uint32_t even = (w[2 * h] & 0x0F0F0F0Fu) | (w[2 * h + 1] << 4 & 0xF0F0F0F0u);
+                        const uint32_t odd = (w[2 * h] >> 4 & 0x0F0F0F0Fu) | (w[2 * h + 1] & 0xF0F0F0F0u);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            op[i][2 * h] = times(from_e2m1(even >> (8 * i) & 0xFFu), f);
+                            op[i][2 * h + 1] = times(from_e2m1(odd >> (8 * i) & 0xFFu), f);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) {
+                        mma16<kScaled>(o[m][i][n], op[i][0], op[i][1], op[i][2], op[i][3], w_hi[n][0], w_hi[n][1]);
+                        if constexpr (!kScaled) mma16<false>(o[m][i][n], op[i][0], op[i][1], op[i][2], op[i][3], w_lo[n][0], w_lo[n][1]);
+                    }
+            }
+        }
+        if constexpr (kE2m1) __syncwarp();                   // (the factors are read)
+    }
+    // ---- the warps' sums, row by row (where the tiles were: their copies have all been waited for)
+    float (*const merge_o)[D] = reinterpret_cast<float (*)[D]>(ring);
+#pragma unroll
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+            for (int w = 4; w < 32; w *= 2) sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], w);
+            if (g == 0) {
+                merge_m[warp][8 * n + 2 * c + e] = ref[n][e];
+                merge_f[warp][8 * n + 2 * c + e] = ref_w[n][e] - kLift;
+                merge_l[warp][8 * n + 2 * c + e] = sum[n][e];
+            }
+        }
+    const bool whole = s.parts == 1;
+#pragma unroll
+    for (int r = 0; r < 8 * NR; ++r) {
+        if (r >= n_rows) break;
+        __syncthreads();
+        if (c == (r & 7) >> 1) {
+#pragma unroll
+            for (int m = 0; m < M64; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (m < D32 / 2 || g < 4)
+                        *reinterpret_cast<float2*>(&merge_o[warp][Sh::column(m, g) + 2 * i]) = make_float2(o[m][i][r / 8][r & 1], o[m][i][r / 8][2 + (r & 1)]);
+        }
+        __syncthreads();
+        float m = merge_m[0][r];
+#pragma unroll
+        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, merge_m[w][r]);
+        const float base = m == -CUDART_INF_F ? 0.f : m;
+        float l = 0.f, f[kWarps];
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            f[w] = exp2f(merge_f[w][r] - base);
+            l += merge_l[w][r] * exp2f(merge_m[w][r] - base);
+        }
+        const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+        const int i = r / group, head = hk * group + r % group;
+        const int64_t at = (s.part0 + static_cast<int64_t>(part) * s.n_q + i) * a.n_heads + head;
+        for (int col = 2 * t; col < D; col += 2 * kWarps * 32) {
+            float y = 0.f, z = 0.f;
+#pragma unroll
+            for (int w = 0; w < kWarps; ++w) {
+                y = fmaf(merge_o[w][col], f[w], y);
+                z = fmaf(merge_o[w][col + 1], f[w], z);
+            }
+            if (whole) reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(a.out) + ((s.q_row + i) * a.n_heads + head) * D)[col / 2] = __floats2bfloat162_rn(y * inv, z * inv);
+            else *reinterpret_cast<float2*>(a.part_o + at * D + col) = make_float2(y, z);
+        }
+        if (t == 0) {
+            if (whole && a.lse) a.lse[(s.q_row + i) * a.n_heads + head] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
+            if (a.part_ml) a.part_ml[at] = make_float2(m, l);
+        }
+    }
+}
+
+template <int KIND, int D32, int NR>
+cudaError_t attend(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
+{
+    static KernelSetup setup;
+    constexpr int smem = kWarps * kStages * Tile<KIND, D32>::kBytes;
+    const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(page_token_kernel<KIND, D32, NR>), smem, 0);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.n_blocks), static_cast<unsigned>(a.kv_heads));
+    cfg.blockDim = dim3(kWarps * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, page_token_kernel<KIND, D32, NR>, a, pool);
+}
+template <int KIND, int D32>
+cudaError_t by_rows(const AttArgs& a, const PagePool& pool, int rows, cudaStream_t stream)
+{
+    return rows <= 8 ? attend<KIND, D32, 1>(a, pool, stream) : attend<KIND, D32, 2>(a, pool, stream);
+}
+template <int KIND>
+cudaError_t by_dim(const AttArgs& a, const PagePool& pool, int rows, cudaStream_t stream)
+{
+    switch (a.head_dim / 32) {
+    case 2: return by_rows<KIND, 2>(a, pool, rows, stream);
+    case 3: return by_rows<KIND, 3>(a, pool, rows, stream);
+    case 4: return by_rows<KIND, 4>(a, pool, rows, stream);
+    case 5: return by_rows<KIND, 5>(a, pool, rows, stream);
+    case 6: return by_rows<KIND, 6>(a, pool, rows, stream);
+    case 7: return by_rows<KIND, 7>(a, pool, rows, stream);
+    default: return by_rows<KIND, 8>(a, pool, rows, stream);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_page_token(int kind, const AttArgs& a, const PagePool& pool, int rows, cudaStream_t stream)
+{
+    return kind == MVLA_PAGE_ROWS ? by_dim<MVLA_PAGE_ROWS>(a, pool, rows, stream)
+         : kind == MVLA_PAGE_E4M3 ? by_dim<MVLA_PAGE_E4M3>(a, pool, rows, stream)
+                                  : by_dim<MVLA_PAGE_E2M1>(a, pool, rows, stream);
+}
+
+}  // namespace mvla

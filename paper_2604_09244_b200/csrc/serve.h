@@ -80,7 +80,8 @@ cudaError_t launch_attend_join(int dtype, const AttArgs& a, cudaStream_t stream)
 // mass += part_mass over its parts.
 cudaError_t launch_mass_add(const AttArgs& a, cudaStream_t stream);
 
-// What a checked call enqueues, and its status.
+// What the kernels of a checked call are given; what it enqueues, and its status.
+void fill_attention(AttArgs& k, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan);
 int32_t enqueue_attention(mvla_ctx* ctx, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan,
                           cudaStream_t stream);
 

@@ -91,9 +91,8 @@ int32_t attend_by_tiles(const CtxView& v, AttArgs& k, const mvla_attention* a, c
 
 namespace mvla {
 
-int32_t enqueue_attention(mvla_ctx* ctx, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan, cudaStream_t st)
+void fill_attention(AttArgs& k, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan)
 {
-    AttArgs k;
     std::memset(&k, 0, sizeof k);
     k.q = a->q; k.k = a->k; k.v = a->v; k.out = a->out; k.lse = a->lse; k.mass = a->mass;
     k.q_pos = a->q_pos; k.kv_pos = a->kv_pos; k.kv_len = a->kv_len;
@@ -129,6 +128,12 @@ int32_t enqueue_attention(mvla_ctx* ctx, const CtxView& v, int32_t batch, const 
         part += static_cast<int64_t>(parts) * s.n_q;
         logit += static_cast<int64_t>(s.n_q) * v.n_heads * s.n_kv;
     }
+}
+
+int32_t enqueue_attention(mvla_ctx* ctx, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan, cudaStream_t st)
+{
+    AttArgs k;
+    fill_attention(k, v, batch, seqs, a, plan);
     cudaError_t e = cudaSuccess;
     if (plan.form == kFormTile) {
         const int32_t rc = attend_by_tiles(v, k, a, plan, &e, st);
