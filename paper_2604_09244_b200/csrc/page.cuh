@@ -4,8 +4,7 @@
 #include "device_utils.cuh"
 #include "page.h"
 
-#include <cuda_fp4.h>
-#include <cuda_fp8.h>
+#include <cuda_fp16.h>
 
 namespace mvla {
 
@@ -34,25 +33,46 @@ __device__ __forceinline__ float two_to(int e) { return __uint_as_float(static_c
 // What a scale's byte stands for.
 __device__ __forceinline__ float scale_value(uint32_t byte) { return byte == 255u ? CUDART_NAN_F : byte == 0u ? 0x1p-127f : __uint_as_float(byte << 23); }
 
+// The codes of a register as fp16 pairs: one instruction to a pair.  (The conversions of the headers take a pair as a number of its own and hand back two halves: 7
+// cycles of a warp to a pair of e4m3, 10 to one of e2m1, instead of 2.)
+__device__ __forceinline__ void from_e4m3(uint32_t four, uint32_t& lo, uint32_t& hi)
+{
+    asm("{\n\t.reg .b16 a, b;\n\t"
+        "mov.b32 {a, b}, %2;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(lo), "=r"(hi) : "r"(four));
+}
+__device__ __forceinline__ void from_e2m1(uint32_t eight, uint32_t (&x)[4])
+{
+    asm("{\n\t.reg .b8 a, b, c, d;\n\t"
+        "mov.b32 {a, b, c, d}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, a;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, d;\n\t}" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(eight));
+}
 // Eight codes as numbers.
-__device__ __forceinline__ void code_values(uint2 codes, float (&x)[8])
+__device__ __forceinline__ void code_values(const uint32_t (&h)[4], float (&x)[8])
 {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const uint32_t w = (i < 2 ? codes.x : codes.y) >> (16 * (i & 1)) & 0xFFFFu;
-        const float2 f = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(w), __NV_E4M3)));
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&h[i]));
         x[2 * i] = f.x;
         x[2 * i + 1] = f.y;
     }
 }
+__device__ __forceinline__ void code_values(uint2 codes, float (&x)[8])
+{
+    uint32_t h[4];
+    from_e4m3(codes.x, h[0], h[1]);
+    from_e4m3(codes.y, h[2], h[3]);
+    code_values(h, x);
+}
 __device__ __forceinline__ void code_values(uint32_t codes, float (&x)[8])
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float2 f = __half22float2(__half2(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(codes >> (8 * i) & 0xFFu), __NV_E2M1)));
-        x[2 * i] = f.x;
-        x[2 * i + 1] = f.y;
-    }
+    uint32_t h[4];
+    from_e2m1(codes, h);
+    code_values(h, x);
 }
 
 }  // namespace mvla

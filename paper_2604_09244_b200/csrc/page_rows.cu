@@ -9,6 +9,9 @@
 // keeps its head and elements from row to row, four rows on their way at a time.
 #include "page.cuh"
 
+#include <cuda_fp4.h>
+#include <cuda_fp8.h>
+
 #include <algorithm>
 
 namespace mvla {

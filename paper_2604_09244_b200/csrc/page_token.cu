@@ -15,8 +15,6 @@
 #include "attend.cuh"
 #include "page.cuh"
 
-#include <cuda_fp16.h>
-
 namespace mvla {
 namespace {
 
@@ -34,9 +32,6 @@ template <int N> __device__ __forceinline__ void wait_copies() { asm volatile("c
 
 __device__ __forceinline__ uint32_t bits_of(__half2 h) { return *reinterpret_cast<const uint32_t*>(&h); }
 __device__ __forceinline__ uint32_t bits_of(__nv_bfloat162 h) { return *reinterpret_cast<const uint32_t*>(&h); }
-__device__ __forceinline__ uint32_t bits_of(__half2_raw h) { return static_cast<uint32_t>(h.x) | static_cast<uint32_t>(h.y) << 16; }
-__device__ __forceinline__ uint32_t from_e4m3(uint32_t two) { return bits_of(__nv_cvt_fp8x2_to_halfraw2(static_cast<__nv_fp8x2_storage_t>(two), __NV_E4M3)); }
-__device__ __forceinline__ uint32_t from_e2m1(uint32_t two) { return bits_of(__nv_cvt_fp4x2_to_halfraw2(static_cast<__nv_fp4x2_storage_t>(two), __NV_E2M1)); }
 __device__ __forceinline__ uint32_t times(uint32_t x, uint32_t f)
 {
     return bits_of(__hmul2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&f)));
@@ -305,19 +300,17 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
                     w0[0] = k0.x; w0[1] = k0.y; w0[2] = k0.z; w0[3] = k0.w;
                     w1[0] = k1.x; w1[1] = k1.y; w1[2] = k1.z; w1[3] = k1.w;
                 } else if constexpr (KIND == MVLA_PAGE_E4M3) {
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        w0[h] = from_e4m3((h < 2 ? k0.x : k0.y) >> (16 * (h & 1)) & 0xFFFFu);
-                        w1[h] = from_e4m3((h < 2 ? k1.x : k1.y) >> (16 * (h & 1)) & 0xFFFFu);
-                    }
+                    from_e4m3(k0.x, w0[0], w0[1]);
+                    from_e4m3(k0.y, w0[2], w0[3]);
+                    from_e4m3(k1.x, w1[0], w1[1]);
+                    from_e4m3(k1.y, w1[2], w1[3]);
                 } else {
                     const int gr = Sh::element(i, c) / kPageGroup;
                     const uint32_t f0 = factors[warp][v][0][gr][g] * 0x10001u, f1 = factors[warp][v][0][gr][g + 8] * 0x10001u;
+                    from_e2m1(k0, w0);
+                    from_e2m1(k1, w1);
 #pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        w0[h] = times(from_e2m1(k0 >> (8 * h) & 0xFFu), f0);
-                        w1[h] = times(from_e2m1(k1 >> (8 * h) & 0xFFu), f1);
-                    }
+                    for (int h = 0; h < 4; ++h) { w0[h] = times(w0[h], f0); w1[h] = times(w1[h], f1); }
                 }
 #pragma unroll
                 for (int n = 0; n < NR; ++n) {
@@ -469,8 +462,7 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {        // (the two keys' bytes of two columns)
                             const uint32_t two = __byte_perm(i < 2 ? w[2 * h].x : w[2 * h].y, i < 2 ? w[2 * h + 1].x : w[2 * h + 1].y, i & 1 ? 0x7362 : 0x5140);
-                            op[i][2 * h] = from_e4m3(two & 0xFFFFu);
-                            op[i][2 * h + 1] = from_e4m3(two >> 16);
+                            from_e4m3(two, op[i][2 * h], op[i][2 * h + 1]);
                         }
                 } else {
                     const int gr = min(Sh::column(m, g) / kPageGroup, D32 - 1);
@@ -479,11 +471,11 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
                         const uint32_t f = *reinterpret_cast<const uint32_t*>(&factors[warp][v][1][gr][2 * c + 8 * h]);
                         const uint32_t even = (w[2 * h] & 0x0F0F0F0Fu) | (w[2 * h + 1] << 4 & 0xF0F0F0F0u);
                         const uint32_t odd = (w[2 * h] >> 4 & 0x0F0F0F0Fu) | (w[2 * h + 1] & 0xF0F0F0F0u);
+                        uint32_t lo[4], hi[4];
+                        from_e2m1(even, lo);
+                        from_e2m1(odd, hi);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            op[i][2 * h] = times(from_e2m1(even >> (8 * i) & 0xFFu), f);
-                            op[i][2 * h + 1] = times(from_e2m1(odd >> (8 * i) & 0xFFu), f);
-                        }
+                        for (int i = 0; i < 4; ++i) { op[i][2 * h] = times(lo[i], f); op[i][2 * h + 1] = times(hi[i], f); }
                     }
                 }
 #pragma unroll
