@@ -59,16 +59,20 @@ struct TileRange {
     int sinks, first, count;
     __device__ __forceinline__ int tile(int t) const { return t < sinks ? t : first + t - sinks; }
 };
-__device__ __forceinline__ TileRange tile_range(const AttArgs& a, int len, int lo, int hi, int tile)
+__device__ __forceinline__ TileRange counted_tiles(int len, int lo, int hi, int tile, int window, int n_sink)
 {
     TileRange r = {0, 0, 0};
-    const int end = a.kv_pos ? len : min(len - 1, max(hi, -1)) + 1;      // (hi may be the last position of its type)
-    const int n = (end + tile - 1) / tile;
-    const int from = a.kv_pos || a.window > lo ? 0 : lo - a.window + 1;
-    r.first = min(from / tile, n);
-    r.sinks = min(static_cast<int>((static_cast<int64_t>(a.n_sink) + tile - 1) / tile), r.first);
+    const int n = (min(len - 1, max(hi, -1)) + 1 + tile - 1) / tile;     // (hi may be the last position of its type)
+    r.first = min((window > lo ? 0 : lo - window + 1) / tile, n);
+    r.sinks = min(static_cast<int>((static_cast<int64_t>(n_sink) + tile - 1) / tile), r.first);
     r.count = r.sinks + n - r.first;
     return r;
+}
+__device__ __forceinline__ TileRange tile_range(const AttArgs& a, int len, int lo, int hi, int tile)
+{
+    if (!a.kv_pos) return counted_tiles(len, lo, hi, tile, a.window, a.n_sink);
+    const int n = (len + tile - 1) / tile;
+    return {0, 0, n};
 }
 
 }  // namespace mvla

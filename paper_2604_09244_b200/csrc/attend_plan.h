@@ -49,8 +49,8 @@ struct Workspace {
 constexpr int kMaxTiles = 2048;          // tiles of keys that a CTA of the tile kernels walks (its list of them: 11 bits an entry)
 
 // kFormFma: by FMAs.  kFormTile: by tiles of 128 query rows on the tensor cores (e4m3: after widening to fp16).
-// kFormToken: at most 16 query rows to a key head, straight from global memory.
-enum AttendForm { kFormFma, kFormTile, kFormToken };
+// kFormToken: at most 16 query rows to a key head, straight from global memory.  kFormPageTile: by tiles, over pages.
+enum AttendForm { kFormFma, kFormTile, kFormToken, kFormPageTile };
 
 // A sequence of at most so many query rows to a key head counts as single tokens: its bf16 weights keep what rounding leaves of them, in the token form and
 // in the tile form, so that the form that its batch is given costs no bits.
@@ -80,7 +80,7 @@ struct AttendPlan {
     int64_t total_q = 0, total_kv = 0, blocks = 0;
     // offsets in the workspace, -1: not used
     int64_t part_o = -1, part_ml = -1, lse2 = -1, part_mass = -1, wide_q = -1, wide_k = -1, wide_v = -1, logits = -1, bytes = 0;
-    int64_t part_keys = 0;       // single tokens: keys of a part
+    int64_t part_keys = 0;       // single tokens, tiles over pages: keys of a part
     int64_t logit_floats = 0;
 };
 
@@ -88,7 +88,7 @@ struct AttendPlan {
 inline int32_t parts_of(const AttendPlan& p, const mvla_seq& s, bool counted, int32_t window, int32_t n_sink)
 {
     if (s.n_q == 0) return 0;
-    if (p.form != kFormToken) return p.splits;
+    if (p.form != kFormToken && p.form != kFormPageTile) return p.splits;
     const int64_t n = (visible_keys(s, counted, window, n_sink) + p.part_keys - 1) / p.part_keys;
     return n < 1 ? 1 : static_cast<int32_t>(n);
 }

@@ -192,7 +192,9 @@ struct TileShape {
 constexpr int kTwin = 32;                    // (a warp's lanes)
 static_assert(kTokenRows <= kTwin, "the rows of a warp");
 
-template <bool F16, int DB, bool TOKENS>
+// PAGED: keys and values lie in pages (a tile is the rows of one, or of several side by side), positions are counted, and every sequence is cut into parts
+// of its own number: a.n_blocks counts its blocks of queries times its parts.
+template <bool F16, int DB, bool TOKENS, bool PAGED>
 __global__ void __launch_bounds__(TileShape<DB>::kWarps * 32, TileShape<DB>::kCtas)
 attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
                    const __grid_constant__ CUtensorMap map_v)
@@ -240,14 +242,15 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     const int heads = a.n_heads / a.pack, blk = a.n_blocks - 1 - static_cast<int>(blockIdx.x) / heads, head0 = static_cast<int>(blockIdx.x) % heads * a.pack;
     const AttSeq& s = a.s[seq_of_block(a, blk)];
     const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack;      // queries of the tile
-    const int q0 = (blk - s.blk0) * per, len = seq_len(a, s);
+    const int parts = PAGED ? s.parts : a.splits, piece = PAGED ? (blk - s.blk0) % s.parts : static_cast<int>(blockIdx.y);
+    const int q0 = (PAGED ? (blk - s.blk0) / s.parts : blk - s.blk0) * per, len = seq_len(a, s);
     const bool twins = TOKENS && static_cast<int64_t>(s.n_q) * (a.n_heads / a.kv_heads) <= kTokenRows;
     int lo, hi;
     query_span(a, s, len, q0, min(q0 + per, s.n_q), lane, &lo, &hi);
     const TileRange range = tile_range(a, len, lo, hi, kKeys);
-    const int per_split = (range.count + a.splits - 1) / a.splits, v0 = static_cast<int>(blockIdx.y) * per_split;
+    const int per_split = (range.count + parts - 1) / parts, v0 = piece * per_split;
     int n = max(0, min(range.count - v0, per_split));
-    if (a.kv_pos) {
+    if (!PAGED && a.kv_pos) {
         for (int v = warp; v < n; v += Sh::kWarps) {
             const Span k = key_span(a, s, len, range.tile(v0 + v) * kKeys, kKeys, lane);
             if (lane == 0) list[v] = static_cast<uint16_t>(span_flags(a, lo, hi, k));
@@ -261,25 +264,53 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         n = n_list;
     }
     // the i-th tile: where its keys begin, and what it is (counted positions: all tiles of the range are visited)
-    const auto first_key = [&](int i) { return range.tile(v0 + (a.kv_pos ? list[i] >> kEntryShift : i)) * kKeys; };
+    const auto first_key = [&](int i) { return range.tile(v0 + (!PAGED && a.kv_pos ? list[i] >> kEntryShift : i)) * kKeys; };
     const auto flags_of = [&](int i, int j0) {
-        if (a.kv_pos) return static_cast<int>(list[i]);
+        if (!PAGED && a.kv_pos) return static_cast<int>(list[i]);
         const Span k = counted_span(len, j0, kKeys);
         const int f = span_flags(a, lo, hi, k);              // (queries far apart may leave out a tile between them: then no row sees a key)
         return f ? f : kMask;
     };
     Guard guard = {&dead, a.status};
 
-    // ---- loads (one lane of a warp): the first ones before the CTA meets
+    // ---- loads (one lane of a warp; with pages the warp looks numbers up, 32 at a time): the first ones before the CTA meets
+    int page = 0, page0 = -64;                               // this lane's: of rows (page0 + lane) << page_shift on
+    const TileRange whole = PAGED && !a.table ? tile_range(a, len, query_pos(a, s, len, 0), query_pos(a, s, len, s.n_q - 1), kKeys) : TileRange{0, 0, 0};
     const auto load = [&](int c) {                           // tiles of keys and values in turn
-        const int st = c % ST, row = s.km_row + first_key(c / 2);
-        mbar_expect_tx(full(st), Sh::kStage);
-        for (int b = 0; b < DB; ++b) tma_load_3d(kv_at + st * Sh::kStage + b * kKeys * 128, c & 1 ? &map_v : &map_k, b * 64, hk, row, full(st));
+        const int st = c % ST, j0 = first_key(c / 2);
+        const CUtensorMap* const map = c & 1 ? &map_v : &map_k;
+        if constexpr (!PAGED) {
+            mbar_expect_tx(full(st), Sh::kStage);
+            for (int b = 0; b < DB; ++b) tma_load_3d(kv_at + st * Sh::kStage + b * kKeys * 128, map, b * 64, hk, s.km_row + j0, full(st));
+        } else {
+            if (lane == 0) mbar_expect_tx(full(st), Sh::kStage);
+            const int rows = min(kKeys, 1 << a.page_shift);
+            for (int r = 0; r < kKeys; r += rows) {
+                int z;
+                if (!a.table) {                              // (the sequence's tiles that are seen, one after another)
+                    const int tile = j0 / kKeys;
+                    z = (s.km_row + (tile < whole.sinks ? tile : tile - whole.first + whole.sinks)) * a.kv_heads + hk;
+                } else {
+                    const int at = (j0 + r) >> a.page_shift;
+                    if (at < page0 || at >= page0 + 32) {
+                        page0 = at;
+                        page = static_cast<int64_t>(at + lane) << a.page_shift < len ? a.table[s.index * a.table_stride + at + lane] : -1;
+                    }
+                    const int pg = __shfl_sync(0xffffffffu, page, at - page0);
+                    z = pg >= 0 && pg < a.n_pages ? pg * a.kv_heads + hk : -1;       // (outside the map: zeros)
+                }
+                if (lane == 0)
+                    for (int b = 0; b < DB; ++b)
+                        tma_load_3d(kv_at + st * Sh::kStage + b * kKeys * 128 + r * 128, map, b * 64, (j0 + r) & ((1 << a.page_shift) - 1), z, full(st));
+            }
+        }
     };
     const int at_once = min(ST, 2 * n);
-    if (warp == Sh::kLoads && lane == 0 && n > 0) {
-        mbar_expect_tx(q_full, DB * per * a.pack * 128);
-        for (int b = 0; b < DB; ++b) tma_load_3d(q_at + b * kRows * 128, &map_q, b * 64, head0, s.qm_row + q0, q_full);
+    if (warp == Sh::kLoads && (PAGED || lane == 0) && n > 0) {
+        if (lane == 0) {
+            mbar_expect_tx(q_full, DB * per * a.pack * 128);
+            for (int b = 0; b < DB; ++b) tma_load_3d(q_at + b * kRows * 128, &map_q, b * 64, head0, s.qm_row + q0, q_full);
+        }
         for (int c = 0; c < at_once; ++c) load(c);
     }
     __syncwarp();
@@ -290,11 +321,19 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     const uint32_t tmem = tmem_base;
 
     if (warp == Sh::kLoads) {
-        if (lane == 0 && n > 0) {
-            int c = at_once;
+        int c = at_once;
+        if (PAGED && n > 0) {
             for (; c < 2 * n; ++c) {
-                if (!guard.wait(empty(c % ST), (c / ST - 1) & 1)) break;
+                if (!guard.wait_all(empty(c % ST), (c / ST - 1) & 1)) break;
                 load(c);
+            }
+        }
+        if (lane == 0 && n > 0) {
+            if (!PAGED) {
+                for (; c < 2 * n; ++c) {
+                    if (!guard.wait(empty(c % ST), (c / ST - 1) & 1)) break;
+                    load(c);
+                }
             }
             guard.settle(q_full, 0);                         // (whoever gave up, what is under way lands before the CTA ends)
             for (int i = max(0, c - ST); i < c; ++i) guard.settle(full(i % ST), i / ST & 1);
@@ -347,7 +386,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             if (flags_of(i, j0) & kMask) {
                 // values that no row sees become zero: counted queries lie side by side, so that their span says it, others have to be asked
                 uint32_t by[kKeys / 32] = {};
-                if (a.q_pos) {
+                if (!PAGED && a.q_pos) {
                     ok = guard.wait_all(p_full + 8 * (i & 1), i / 2 & 1);
                     for (int w = 0; w < 4; ++w)
 #pragma unroll
@@ -357,7 +396,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
 #pragma unroll
                 for (int x = 0; x < kKeys / 32; ++x) {
                     const int k = 32 * x + lane;
-                    if (a.q_pos ? by[x] >> lane & 1u : j0 + k < len && some_sees(lo, hi, j0 + k, a.window, a.n_sink)) continue;
+                    if (!PAGED && a.q_pos ? by[x] >> lane & 1u : j0 + k < len && some_sees(lo, hi, j0 + k, a.window, a.n_sink)) continue;
                     some = true;
                     for (int c16 = 0; c16 < DB * 8; ++c16)
                         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};" ::"r"(kv_at + st * Sh::kStage + c16 / 8 * kKeys * 128 + k * 128 + c16 % 8 * 16), "r"(0) : "memory");
@@ -397,7 +436,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             const int j0 = first_key(i);
             masked = (flags_of(i, j0) & kMask) != 0;
             if (!masked) return;
-            if (a.kv_pos) {                                  // the positions, for the four warps
+            if (!PAGED && a.kv_pos) {                        // the positions, for the four warps
                 asm volatile("bar.sync 1, 128;" ::: "memory");       // (nobody reads the last ones any more)
                 if (t < kKeys) key_at[t] = key_pos(a, s, len, j0 + t);
                 asm volatile("bar.sync 1, 128;" ::: "memory");
@@ -413,7 +452,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
 #pragma unroll
                 for (int w = 0; w < kKeys / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
             }
-            if (a.q_pos) {                                   // (those of three tiles ago were read before the last S was made)
+            if (!PAGED && a.q_pos) {                         // (those of three tiles ago were read before the last S was made)
 #pragma unroll
                 for (int w = 0; w < kKeys / 32; ++w) {
                     const uint32_t any = __reduce_or_sync(0xffffffffu, visible[w]);
@@ -493,7 +532,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         // ---- the rows
         if (ok && n > 0) ok = guard.wait_all(o_full, 0);
         tc_fence_after();
-        const int64_t part = s.part0 + static_cast<int64_t>(blockIdx.y) * s.n_q + i_row;
+        const int64_t part = s.part0 + static_cast<int64_t>(piece) * s.n_q + i_row;
         const float inv = l > 0.f ? 1.f / l : 0.f;
         m -= kLift;
         // the twins' rows of O, for the others (the keys and values have been read): element by element, the rows side by side
@@ -517,9 +556,9 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                 for (int k = 0; k < 32; ++k) o[k] += beside[(c + k) * kTwin + r];
             }
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? (a.splits > 1 ? o[k] : o[k] * inv) : 0.f;
+            for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? (parts > 1 ? o[k] : o[k] * inv) : 0.f;
             if (!mine) continue;
-            if (a.splits > 1) {
+            if (parts > 1) {
                 float* const dst = a.part_o + (part * a.n_heads + head) * a.head_dim + c;
 #pragma unroll
                 for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(dst + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
@@ -530,12 +569,12 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             }
         }
         if (mine && ok && !twin) {
-            if (a.splits > 1) {
+            if (parts > 1) {
                 a.part_ml[part * a.n_heads + head] = make_float2(m, l);
             } else {
                 const float z = l > 0.f ? m + log2f(l) : -CUDART_INF_F;
                 if (a.lse) a.lse[(s.q_row + i_row) * a.n_heads + head] = z * 0.69314718055994531f;      // ln 2
-                if (a.mass) a.lse2[static_cast<int64_t>(s.qp0 + i_row) * a.n_heads + head] = z;
+                if (!PAGED && a.mass) a.lse2[static_cast<int64_t>(s.qp0 + i_row) * a.n_heads + head] = z;
             }
         }
         tc_fence_before();
@@ -793,13 +832,13 @@ cudaError_t launch(KernelSetup& setup, K kernel, dim3 grid, int threads, int col
     return cudaLaunchKernelEx(&cfg, kernel, a, maps.q, maps.k, maps.v);
 }
 
-template <bool F16, int DB, bool TOKENS>
+template <bool F16, int DB, bool TOKENS, bool PAGED>
 cudaError_t attend(const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
     static KernelSetup setup;
-    const dim3 grid(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack), static_cast<unsigned>(a.splits));
+    const dim3 grid(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack), PAGED ? 1u : static_cast<unsigned>(a.splits));
     using Sh = TileShape<DB>;
-    return launch(setup, attend_tile_kernel<F16, DB, TOKENS>, grid, Sh::kWarps * 32, Sh::kColumns, Sh::kSmem, a, maps, stream);
+    return launch(setup, attend_tile_kernel<F16, DB, TOKENS, PAGED>, grid, Sh::kWarps * 32, Sh::kColumns, Sh::kSmem, a, maps, stream);
 }
 
 template <bool F16, int DB>
@@ -871,14 +910,14 @@ cudaError_t weights_by_dim(const AttArgs& a, const AttMaps& maps, cudaStream_t s
     default: return weights<F16, 4>(a, maps, stream);
     }
 }
-template <bool F16, bool TOKENS>
+template <bool F16, bool TOKENS, bool PAGED>
 cudaError_t attend_by_dim(const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
     switch ((a.head_dim + 63) / 64) {
-    case 1: return attend<F16, 1, TOKENS>(a, maps, stream);
-    case 2: return attend<F16, 2, TOKENS>(a, maps, stream);
-    case 3: return attend<F16, 3, TOKENS>(a, maps, stream);
-    default: return attend<F16, 4, TOKENS>(a, maps, stream);
+    case 1: return attend<F16, 1, TOKENS, PAGED>(a, maps, stream);
+    case 2: return attend<F16, 2, TOKENS, PAGED>(a, maps, stream);
+    case 3: return attend<F16, 3, TOKENS, PAGED>(a, maps, stream);
+    default: return attend<F16, 4, TOKENS, PAGED>(a, maps, stream);
     }
 }
 }  // namespace
@@ -890,8 +929,13 @@ cudaError_t launch_attend_weights(bool f16, const AttArgs& a, const AttMaps& map
 
 cudaError_t launch_attend_tile(bool f16, bool tokens, const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
-    if (f16) return attend_by_dim<true, false>(a, maps, stream);
-    return tokens ? attend_by_dim<false, true>(a, maps, stream) : attend_by_dim<false, false>(a, maps, stream);
+    if (f16) return attend_by_dim<true, false, false>(a, maps, stream);
+    return tokens ? attend_by_dim<false, true, false>(a, maps, stream) : attend_by_dim<false, false, false>(a, maps, stream);
+}
+
+cudaError_t launch_page_tile(bool tokens, const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
+{
+    return tokens ? attend_by_dim<false, true, true>(a, maps, stream) : attend_by_dim<false, false, true>(a, maps, stream);
 }
 
 }  // namespace mvla

@@ -31,12 +31,15 @@ struct PageRowsArgs {
     int64_t k_stride, v_stride;
     int32_t n_seq, total;                    // rows of the batch
     int32_t block_rows;                      // rows of a CTA
-    int32_t from_start;                      // read rows 0 .. n_q - 1 of a sequence instead of its last ones
-    int64_t packed_row;                      // >= 0: row r of the batch, packed, is row packed_row + r of k / v (instead of q_row + i)
+    int64_t k_head, v_head;                  // elements from one head of a row to the next
+    // launch_page_tiles: the rows of the tiles of 64 that a sequence's queries see, tile after tile, of every tile head after head.  Of s: n_q, n_kv, and as
+    // row0 64 times the sequence's first tile
+    int32_t window, n_sink;
     PageSeq s[kMaxBatch];
 };
 cudaError_t launch_page_write(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream);
 cudaError_t launch_page_read(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream);
+cudaError_t launch_page_tiles(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream);
 
 // ---- attention
 

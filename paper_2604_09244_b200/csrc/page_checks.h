@@ -97,11 +97,22 @@ inline int32_t check_page_rows(const ServeShape& v, int32_t batch, const mvla_se
 
 // ---- attention over pages
 
+constexpr int kPageTile = 64;                // keys of a tile (attend_tile.cu, attend_fma.cu)
+
 struct PageAttendPlan {
     AttendPlan attend;
-    // where rows are taken out of the pages first and attended over as packed rows (-1: they are not)
-    int64_t dense_k = -1, dense_v = -1, bytes = 0;
+    // quantised pages that are no single tokens': the tiles that some query sees, as elements of the hidden type (-1: there are none)
+    int64_t dense_k = -1, dense_v = -1, dense_tiles = 0, bytes = 0;
 };
+
+// Tiles that a sequence's queries see, at most.
+inline int64_t seen_tiles(const mvla_seq& s, int32_t window, int32_t n_sink)
+{
+    if (s.n_q == 0) return 0;
+    const int64_t all = (static_cast<int64_t>(s.n_kv) + kPageTile - 1) / kPageTile;
+    const int64_t near = (static_cast<int64_t>(window) + s.n_q - 1 + kPageTile - 1) / kPageTile + 1, sinks = (static_cast<int64_t>(n_sink) + kPageTile - 1) / kPageTile;
+    return std::min(all, near + sinks);
+}
 
 inline ServeShape hidden_shape(const ServeShape& v)
 {
@@ -169,24 +180,80 @@ inline AttendPlan plan_tokens(const ServeShape& c, int32_t batch, const mvla_seq
     return p;
 }
 
+// Blocks of queries by tiles of 128 rows, every sequence's keys cut into parts of about the same length over the whole batch (a multiple of 64, at least
+// 256 keys), so that their CTAs fill whole rounds of those that fit: of one to four rounds, or no cut at all, what ends first.  In tiles of a CTA (1.3 us with
+// another one beside it): its longest part and 4 for its start and end; 4 for the join, and what the parts' sums, written and read, take at 6 TB/s.
+inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink)
+{
+    AttendPlan p;
+    p.form = kFormPageTile;
+    p.pack = pack_of(c.n_heads / c.kv_heads);
+    p.queries = 128 / p.pack;
+    const int64_t packs = c.n_heads / p.pack, slots = (c.head_dim <= 128 ? 2 : 1) * static_cast<int64_t>(c.sm_count);
+    int64_t work = 0, longest = 1;
+    const auto blocks_of = [&](const mvla_seq& s) { return (static_cast<int64_t>(s.n_q) + p.queries - 1) / p.queries; };
+    for (int b = 0; b < batch; ++b) {
+        p.total_q += seqs[b].n_q;
+        p.total_kv += seqs[b].n_kv;
+        if (seqs[b].n_q == 0) continue;
+        const int64_t keys = visible_keys(seqs[b], counted, window, n_sink);
+        work += blocks_of(seqs[b]) * packs * keys;
+        longest = std::max(longest, keys);
+    }
+    int64_t ctas = 0, part_q = 0;
+    const auto cut = [&](int64_t part) {
+        p.part_keys = part;
+        ctas = part_q = 0;
+        p.splits = 1;
+        for (int b = 0; b < batch; ++b) {
+            const int32_t n = parts_of(p, seqs[b], counted, window, n_sink);
+            ctas += blocks_of(seqs[b]) * n * packs;
+            part_q += static_cast<int64_t>(seqs[b].n_q) * n;
+            p.splits = std::max(p.splits, n);
+        }
+    };
+    int64_t best = 0;
+    double best_cost = 0;
+    for (int rounds = 0; rounds <= 4; ++rounds) {
+        int64_t part = rounds ? (work + rounds * slots - 1) / (rounds * slots) : longest;
+        part = std::max<int64_t>({part, 256, (longest + 63) / 64});
+        part = (part + 63) / 64 * 64;
+        cut(part);
+        for (int tries = 0; rounds && ctas > rounds * slots && part < longest && tries < 16; ++tries) cut(part += std::max<int64_t>(64, part / 16 / 64 * 64));
+        const double join = p.splits > 1 ? 4.0 + static_cast<double>(part_q) * c.n_heads * c.head_dim * 8 / 8e6 : 0.0;
+        const double cost = static_cast<double>((ctas + slots - 1) / slots) * (static_cast<double>(std::min(part, longest)) / 64 + 4) + join;
+        if (!best || cost < best_cost) { best = part; best_cost = cost; }
+    }
+    cut(best);
+    for (int b = 0; b < batch; ++b) p.blocks += blocks_of(seqs[b]) * parts_of(p, seqs[b], counted, window, n_sink);
+    if (p.splits > 1) {
+        Workspace w;
+        p.part_o = w.take(part_q * c.n_heads * c.head_dim * static_cast<int64_t>(sizeof(float)));
+        p.part_ml = w.take(part_q * c.n_heads * 2 * static_cast<int64_t>(sizeof(float)));
+        p.bytes = w.bytes;
+    }
+    return p;
+}
+
 inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_paged_attention* a)
 {
     PageAttendPlan p;
     const ServeShape h = hidden_shape(v);
-    const int64_t group = v.n_heads / v.kv_heads;
+    const bool counted = !a->kv_len;
     int64_t most_rows = 0;
-    for (int b = 0; b < batch; ++b) most_rows = std::max(most_rows, seqs[b].n_q * group);
-    if (h.dtype != MVLA_DTYPE_FP32 && most_rows <= kTokenRows) {
-        p.attend = plan_tokens(h, batch, seqs, !a->kv_len, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32));
-        p.bytes = p.attend.bytes;
-        return p;
-    }
-    p.attend = plan_attend(h, batch, seqs, !a->kv_len, a->window, a->n_sink, false);
+    for (int b = 0; b < batch; ++b) most_rows = std::max(most_rows, seqs[b].n_q * static_cast<int64_t>(v.n_heads / v.kv_heads));
+    const bool tokens = h.dtype != MVLA_DTYPE_FP32 && most_rows <= kTokenRows;
+    p.attend = h.dtype == MVLA_DTYPE_FP32 ? plan_attend(h, batch, seqs, counted, a->window, a->n_sink, false)
+             : tokens ? plan_tokens(h, batch, seqs, counted, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32))
+                      : plan_page_tiles(h, batch, seqs, counted, a->window, a->n_sink);
+    p.bytes = p.attend.bytes;
+    if (a->pages.kind == MVLA_PAGE_ROWS || tokens) return p;
     Workspace w;
     w.take(p.attend.bytes);
-    const int64_t rows = p.attend.total_kv * v.kv_heads * v.head_dim * static_cast<int64_t>(v.wide);
-    p.dense_k = w.take(rows);
-    p.dense_v = w.take(rows);
+    for (int b = 0; b < batch; ++b) p.dense_tiles += seen_tiles(seqs[b], a->window, a->n_sink);
+    const int64_t bytes = p.dense_tiles * kPageTile * v.kv_heads * v.head_dim * static_cast<int64_t>(v.wide);
+    p.dense_k = w.take(bytes);
+    p.dense_v = w.take(bytes);
     p.bytes = w.bytes;
     return p;
 }

@@ -7,6 +7,7 @@
 // largest element crosses them by shuffles, of bf16 as pairs of 16-bit patterns, whose order is that of the numbers and leaves what is not
 // finite on top.  A CTA has a block of rows; where each of them lies is looked up once, by a thread, and a thread
 // keeps its head and elements from row to row, four rows on their way at a time.
+#include "attend.cuh"
 #include "page.cuh"
 
 #include <cuda_fp4.h>
@@ -86,7 +87,11 @@ template <> struct Eight<float> {
     }
 };
 
-// Row r of the batch, packed: its row of k / v, and its row of head 0 in the pool, -1 where there is none.
+constexpr int64_t kZeros = -1, kNobodys = -2;                // rows of the pool: none; and one that is left alone
+constexpr int kTile = 64;
+
+// Row r of the batch, packed: its row of k / v, and its row of head 0 in the pool, or one of the above.
+template <bool TILES>
 __device__ __forceinline__ void locate(const PageRowsArgs& a, int r, int64_t* row, int64_t* at)
 {
     int b = 0, n = a.n_seq;
@@ -96,10 +101,20 @@ __device__ __forceinline__ void locate(const PageRowsArgs& a, int r, int64_t* ro
         n -= half;
     }
     const PageSeq& s = a.s[b];
-    const int len = a.kv_len ? min(max(a.kv_len[s.index], 0), s.n_kv) : s.n_kv;
-    const int i = r - s.row0, j = a.from_start ? i : len - s.n_q + i;
-    *row = a.packed_row >= 0 ? a.packed_row + r : s.q_row + i;
-    *at = -1;
+    const int len = a.kv_len ? min(max(a.kv_len[s.index], 0), s.n_kv) : s.n_kv, i = r - s.row0;
+    int j;
+    if constexpr (TILES) {
+        const int lo = max(len - s.n_q, -1), hi = max(len - 1, -1);
+        const TileRange range = counted_tiles(len, lo, hi, kTile, a.window, a.n_sink);
+        j = i / kTile < range.count ? range.tile(i / kTile) * kTile + i % kTile : -1;
+        *row = static_cast<int64_t>(r / kTile) * kTile * a.pool.kv_heads + r % kTile;
+        *at = kNobodys;
+        if (j < 0 || j >= len) return;
+    } else {
+        j = len - s.n_q + i;
+        *row = s.q_row + i;
+    }
+    *at = kZeros;
     if (j < 0 || j >= len) return;
     const int page = page_of(a.pool, s.index, j);
     if (page >= 0) *at = page_row(a.pool, page, 0, j);
@@ -142,11 +157,11 @@ __global__ void __launch_bounds__(kThreads) page_write_kernel(const __grid_const
     pdl_wait();
     pdl_trigger();
     const int r0 = static_cast<int>(blockIdx.x) * a.block_rows, n = min(a.block_rows, a.total - r0);
-    if (static_cast<int>(threadIdx.x) < n) locate(a, r0 + threadIdx.x, &rows[threadIdx.x], &ats[threadIdx.x]);
+    if (static_cast<int>(threadIdx.x) < n) locate<false>(a, r0 + threadIdx.x, &rows[threadIdx.x], &ats[threadIdx.x]);
     __syncthreads();
     const Slot s = slot_of<LANES>(a);
     const int d = a.pool.head_dim, c = s.sub * 8;
-    const char* const src = static_cast<const char*>(s.values ? a.v : a.k) + (static_cast<int64_t>(s.head) * d + c) * static_cast<int64_t>(sizeof(T));
+    const char* const src = static_cast<const char*>(s.values ? a.v : a.k) + (s.head * (s.values ? a.v_head : a.k_head) + c) * static_cast<int64_t>(sizeof(T));
     const int64_t stride = (s.values ? a.v_stride : a.k_stride) * static_cast<int64_t>(sizeof(T));
     uint8_t* const data = static_cast<uint8_t*>(s.values ? a.pool.v : a.pool.k);
     uint8_t* const scales = s.values ? a.pool.v_scale : a.pool.k_scale;
@@ -200,7 +215,8 @@ __global__ void __launch_bounds__(kThreads) page_write_kernel(const __grid_const
     }
 }
 
-template <class T, int KIND, int LANES>
+// TILES: for launch_page_tile; rows that no query sees are left out.
+template <class T, int KIND, int LANES, bool TILES>
 __global__ void __launch_bounds__(kThreads) page_read_kernel(const __grid_constant__ PageRowsArgs a)
 {
     using Codes = std::conditional_t<KIND == MVLA_PAGE_ROWS, Eight<T>, std::conditional_t<KIND == MVLA_PAGE_E4M3, uint2, uint32_t>>;
@@ -208,12 +224,12 @@ __global__ void __launch_bounds__(kThreads) page_read_kernel(const __grid_consta
     pdl_wait();
     pdl_trigger();
     const int r0 = static_cast<int>(blockIdx.x) * a.block_rows, n = min(a.block_rows, a.total - r0);
-    if (static_cast<int>(threadIdx.x) < n) locate(a, r0 + threadIdx.x, &rows[threadIdx.x], &ats[threadIdx.x]);
+    if (static_cast<int>(threadIdx.x) < n) locate<TILES>(a, r0 + threadIdx.x, &rows[threadIdx.x], &ats[threadIdx.x]);
     __syncthreads();
     const Slot s = slot_of<LANES>(a);
     if (!s.on) return;
     const int d = a.pool.head_dim, c = s.sub * 8;
-    char* const dst = static_cast<char*>(s.values ? a.v : a.k) + (static_cast<int64_t>(s.head) * d + c) * static_cast<int64_t>(sizeof(T));
+    char* const dst = static_cast<char*>(s.values ? a.v : a.k) + (s.head * (s.values ? a.v_head : a.k_head) + c) * static_cast<int64_t>(sizeof(T));
     const int64_t stride = (s.values ? a.v_stride : a.k_stride) * static_cast<int64_t>(sizeof(T));
     const uint8_t* const data = static_cast<const uint8_t*>(s.values ? a.pool.v : a.pool.k);
     const uint8_t* const scales = s.values ? a.pool.v_scale : a.pool.k_scale;
@@ -239,6 +255,7 @@ __global__ void __launch_bounds__(kThreads) page_read_kernel(const __grid_consta
         for (int u = 0; u < kAhead; ++u) {
             const int r = b0 + u * s.step;
             if (r >= n) break;
+            if (TILES && ats[r] == kNobodys) continue;
             Eight<T> y;
             y.clear();
             if (there[u]) {
@@ -260,7 +277,8 @@ __global__ void __launch_bounds__(kThreads) page_read_kernel(const __grid_consta
 
 int lanes_of(int d) { return d <= 64 ? 8 : d <= 128 ? 16 : 32; }
 
-template <bool WRITE, class T, int KIND, int LANES>
+enum Way { kWrite, kRead, kTiles };
+template <Way WAY, class T, int KIND, int LANES>
 cudaError_t launch(PageRowsArgs& a, cudaStream_t stream)
 {
     const int heads = (a.k ? a.pool.kv_heads : 0) + (a.v ? a.pool.kv_heads : 0);
@@ -278,25 +296,25 @@ cudaError_t launch(PageRowsArgs& a, cudaStream_t stream)
     cudaLaunchAttribute attr[1] = {pdl_attribute()};
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if constexpr (WRITE) return cudaLaunchKernelEx(&cfg, page_write_kernel<T, KIND, LANES>, a);
-    else return cudaLaunchKernelEx(&cfg, page_read_kernel<T, KIND, LANES>, a);
+    if constexpr (WAY == kWrite) return cudaLaunchKernelEx(&cfg, page_write_kernel<T, KIND, LANES>, a);
+    else return cudaLaunchKernelEx(&cfg, page_read_kernel<T, KIND, LANES, WAY == kTiles>, a);
 }
-template <bool WRITE, class T, int KIND>
+template <Way WAY, class T, int KIND>
 cudaError_t by_lanes(PageRowsArgs& a, cudaStream_t stream)
 {
     switch (lanes_of(a.pool.head_dim)) {
-    case 8: return launch<WRITE, T, KIND, 8>(a, stream);
-    case 16: return launch<WRITE, T, KIND, 16>(a, stream);
-    default: return launch<WRITE, T, KIND, 32>(a, stream);
+    case 8: return launch<WAY, T, KIND, 8>(a, stream);
+    case 16: return launch<WAY, T, KIND, 16>(a, stream);
+    default: return launch<WAY, T, KIND, 32>(a, stream);
     }
 }
-template <bool WRITE, class T>
+template <Way WAY, class T>
 cudaError_t by_kind(int kind, PageRowsArgs& a, cudaStream_t stream)
 {
     switch (kind) {
-    case MVLA_PAGE_ROWS: return by_lanes<WRITE, T, MVLA_PAGE_ROWS>(a, stream);
-    case MVLA_PAGE_E4M3: return by_lanes<WRITE, T, MVLA_PAGE_E4M3>(a, stream);
-    default: return by_lanes<WRITE, T, MVLA_PAGE_E2M1>(a, stream);
+    case MVLA_PAGE_ROWS: return by_lanes<WAY, T, MVLA_PAGE_ROWS>(a, stream);
+    case MVLA_PAGE_E4M3: return by_lanes<WAY, T, MVLA_PAGE_E4M3>(a, stream);
+    default: return by_lanes<WAY, T, MVLA_PAGE_E2M1>(a, stream);
     }
 }
 
@@ -304,11 +322,15 @@ cudaError_t by_kind(int kind, PageRowsArgs& a, cudaStream_t stream)
 
 cudaError_t launch_page_write(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream)
 {
-    return hidden_dtype == MVLA_DTYPE_FP32 ? by_kind<true, float>(kind, a, stream) : by_kind<true, __nv_bfloat16>(kind, a, stream);
+    return hidden_dtype == MVLA_DTYPE_FP32 ? by_kind<kWrite, float>(kind, a, stream) : by_kind<kWrite, __nv_bfloat16>(kind, a, stream);
 }
 cudaError_t launch_page_read(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream)
 {
-    return hidden_dtype == MVLA_DTYPE_FP32 ? by_kind<false, float>(kind, a, stream) : by_kind<false, __nv_bfloat16>(kind, a, stream);
+    return hidden_dtype == MVLA_DTYPE_FP32 ? by_kind<kRead, float>(kind, a, stream) : by_kind<kRead, __nv_bfloat16>(kind, a, stream);
+}
+cudaError_t launch_page_tiles(int hidden_dtype, int kind, PageRowsArgs& a, cudaStream_t stream)
+{
+    return hidden_dtype == MVLA_DTYPE_FP32 ? by_kind<kTiles, float>(kind, a, stream) : by_kind<kTiles, __nv_bfloat16>(kind, a, stream);
 }
 
 }  // namespace mvla

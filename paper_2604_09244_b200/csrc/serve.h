@@ -53,11 +53,17 @@ struct AttArgs {
     float* logits;               // scores in powers of two, -infinity where a row is not seen                (single tokens with mass)
     int32_t pack;                // heads of a group side by side in a tile of rows (kernels by tiles)
     int* status;                 // word that receives MVLA_ERR_TIMEOUT when a bounded wait gives up
+    // pages (launch_page_tile, launch_page_fma)
+    const int32_t* table;        // null: the tiles that a sequence's queries see lie one after another, from tile km_row on
+    int64_t table_stride;
+    int32_t n_pages, page_shift; // page_rows = 1 << page_shift
     AttSeq s[kMaxBatch];
 };
 
 // fp32, by FMAs: any shape, in blocks of `rows` (8 or 32) query rows.
 cudaError_t launch_attend_fma(const AttArgs& a, int rows, cudaStream_t stream);
+// The same over pages.
+cudaError_t launch_page_fma(const AttArgs& a, int rows, cudaStream_t stream);
 // The weights of every cached row over the queries of its sequence, by key head, into part_mass (by FMAs in 32 bits).
 cudaError_t launch_mass_fma(const AttArgs& a, cudaStream_t stream);
 // bf16 (f16: what launch_widen made) by tiles of 128 rows on the tensor cores; at most kMaxTiles tiles of keys to a split.
@@ -66,6 +72,8 @@ struct AttMaps {
 };
 // `tokens`: bf16, and some sequence counts as single tokens (kTokenRows).
 cudaError_t launch_attend_tile(bool f16, bool tokens, const AttArgs& a, const AttMaps& maps, cudaStream_t stream);
+// The same over pages: maps.k and maps.v of (head_dim, rows of a page, pages x key heads), boxes of as many rows as a page has, 64 at most.
+cudaError_t launch_page_tile(bool tokens, const AttArgs& a, const AttMaps& maps, cudaStream_t stream);
 // The weights as above, by tiles of 128 keys.  (mass_parts: packs of heads, times runs of kMaxTiles tiles of queries)
 cudaError_t launch_attend_weights(bool f16, const AttArgs& a, const AttMaps& maps, cudaStream_t stream);
 // The sequences' e4m3 rows as packed fp16 rows.
