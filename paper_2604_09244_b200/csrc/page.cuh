@@ -20,13 +20,14 @@ __device__ __forceinline__ int64_t page_row(const PagePool& p, int page, int h, 
     return ((static_cast<int64_t>(page) * p.kv_heads + h) << p.page_shift) + (j & ((1 << p.page_shift) - 1));
 }
 
-// The least exponent e, not below kScaleLeast, with |x| <= M 2^e for the largest |x| of a group, whose bits in 32 bits these are (finite).
+// The byte of the least scale 2^e, e not below kScaleLeast, with |x| <= M 2^e for the largest |x| of a group, whose bits in 32 bits these are (finite): M = 448 = 1.75
+// 2^8 or 6 = 1.5 2^2, and a larger fraction than M's carries into the exponent.
 template <int KIND>
-__device__ __forceinline__ int scale_exponent(uint32_t big)
+__device__ __forceinline__ uint32_t scale_byte(uint32_t big)
 {
-    constexpr bool kE4m3 = KIND == MVLA_PAGE_E4M3;           // M = 448 = 1.75 2^8, or 6 = 1.5 2^2
-    const int e = static_cast<int>(big >> 23) - 127 - (kE4m3 ? 8 : 2) + ((big & 0x7FFFFFu) > (kE4m3 ? 0x600000u : 0x400000u) ? 1 : 0);
-    return min(max(e, kScaleLeast), kE4m3 ? kScaleMostE4m3 : kScaleMostE2m1);
+    constexpr bool kE4m3 = KIND == MVLA_PAGE_E4M3;
+    const int e = static_cast<int>((big + (kE4m3 ? 0x1FFFFFu : 0x3FFFFFu)) >> 23) - (kE4m3 ? 8 : 2);
+    return static_cast<uint32_t>(min(max(e, kScaleLeast + 127), (kE4m3 ? kScaleMostE4m3 : kScaleMostE2m1) + 127));
 }
 // 2^e for a normal number's e.
 __device__ __forceinline__ float two_to(int e) { return __uint_as_float(static_cast<uint32_t>(e + 127) << 23); }
