@@ -273,9 +273,18 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     };
     Guard guard = {&dead, a.status};
 
-    // ---- loads (one lane of a warp; with pages the warp looks numbers up, 32 at a time): the first ones before the CTA meets
-    int page = 0, page0 = -64;                               // this lane's: of rows (page0 + lane) << page_shift on
+    // ---- loads (one lane of a warp; with pages a lane to every box, which looks its page up a tile ahead): the first ones before the CTA meets
+    const int box_rows = PAGED ? min(kKeys, 1 << a.page_shift) : kKeys, boxes = DB * (kKeys / box_rows);
+    const int row_of_box = lane / DB * box_rows, piece_of_box = lane % DB;
     const TileRange whole = PAGED && !a.table ? tile_range(a, len, query_pos(a, s, len, 0), query_pos(a, s, len, s.n_q - 1), kKeys) : TileRange{0, 0, 0};
+    const auto look_up = [&](int i) {                        // where this lane's box of tile i lies: outside the map where there is nothing (zeros)
+        if (!PAGED || lane >= boxes || i >= n) return -1;
+        const int j = first_key(i) + row_of_box, tile = j / kKeys;
+        if (!a.table) return (s.km_row + (tile < whole.sinks ? tile : tile - whole.first + whole.sinks)) * a.kv_heads + hk;      // (seen tiles, one after another)
+        const int page = j < len ? a.table[s.index * a.table_stride + (j >> a.page_shift)] : -1;
+        return page >= 0 && page < a.n_pages ? page * a.kv_heads + hk : -1;
+    };
+    int here = 0, ahead = 0;
     const auto load = [&](int c) {                           // tiles of keys and values in turn
         const int st = c % ST, j0 = first_key(c / 2);
         const CUtensorMap* const map = c & 1 ? &map_v : &map_k;
@@ -283,26 +292,15 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             mbar_expect_tx(full(st), Sh::kStage);
             for (int b = 0; b < DB; ++b) tma_load_3d(kv_at + st * Sh::kStage + b * kKeys * 128, map, b * 64, hk, s.km_row + j0, full(st));
         } else {
-            if (lane == 0) mbar_expect_tx(full(st), Sh::kStage);
-            const int rows = min(kKeys, 1 << a.page_shift);
-            for (int r = 0; r < kKeys; r += rows) {
-                int z;
-                if (!a.table) {                              // (the sequence's tiles that are seen, one after another)
-                    const int tile = j0 / kKeys;
-                    z = (s.km_row + (tile < whole.sinks ? tile : tile - whole.first + whole.sinks)) * a.kv_heads + hk;
-                } else {
-                    const int at = (j0 + r) >> a.page_shift;
-                    if (at < page0 || at >= page0 + 32) {
-                        page0 = at;
-                        page = static_cast<int64_t>(at + lane) << a.page_shift < len ? a.table[s.index * a.table_stride + at + lane] : -1;
-                    }
-                    const int pg = __shfl_sync(0xffffffffu, page, at - page0);
-                    z = pg >= 0 && pg < a.n_pages ? pg * a.kv_heads + hk : -1;       // (outside the map: zeros)
-                }
-                if (lane == 0)
-                    for (int b = 0; b < DB; ++b)
-                        tma_load_3d(kv_at + st * Sh::kStage + b * kKeys * 128 + r * 128, map, b * 64, (j0 + r) & ((1 << a.page_shift) - 1), z, full(st));
+            if (!(c & 1)) {
+                here = ahead;
+                ahead = look_up(c / 2 + 1);
             }
+            if (lane == 0) mbar_expect_tx(full(st), Sh::kStage);
+            __syncwarp();
+            if (lane < boxes)
+                tma_load_3d(kv_at + st * Sh::kStage + piece_of_box * kKeys * 128 + row_of_box * 128, map, piece_of_box * 64,
+                            (j0 + row_of_box) & ((1 << a.page_shift) - 1), here, full(st));
         }
     };
     const int at_once = min(ST, 2 * n);
@@ -311,6 +309,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             mbar_expect_tx(q_full, DB * per * a.pack * 128);
             for (int b = 0; b < DB; ++b) tma_load_3d(q_at + b * kRows * 128, &map_q, b * 64, head0, s.qm_row + q0, q_full);
         }
+        ahead = look_up(0);
         for (int c = 0; c < at_once; ++c) load(c);
     }
     __syncwarp();

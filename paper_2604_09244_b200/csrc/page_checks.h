@@ -235,6 +235,15 @@ inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla
     return p;
 }
 
+// Few query rows to a key head: the token form unpacks quantised rows as it reads them, where the tile form has them unpacked first.  Rows of their own type
+// go to the tile form, whose larger copies win although its rows are mostly empty, but for the shortest calls (us, token / tile form, one token of 32 heads
+// over 8 heads of 128: 800 rows 13.3 / 17.4, 4000 19.5 / 19.5, 16000 35.8 / 29.7, 131071 138 / 112; over 32 heads: 800 rows 17.4 / 19.5, 4000 31.7 / 29.7; four tokens
+// over 200 rows 25.6 / 15.4; 16 tokens over 500 to 4000 rows 60 / 50).
+inline bool page_by_tokens(int kind, int64_t rows, int64_t keys_and_heads)
+{
+    return rows <= kTokenRows && (kind != MVLA_PAGE_ROWS || (rows <= 8 && keys_and_heads < 32768));
+}
+
 inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_paged_attention* a)
 {
     PageAttendPlan p;
@@ -242,7 +251,9 @@ inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, co
     const bool counted = !a->kv_len;
     int64_t most_rows = 0;
     for (int b = 0; b < batch; ++b) most_rows = std::max(most_rows, seqs[b].n_q * static_cast<int64_t>(v.n_heads / v.kv_heads));
-    const bool tokens = h.dtype != MVLA_DTYPE_FP32 && most_rows <= kTokenRows;
+    int64_t keys = 0;
+    for (int b = 0; b < batch; ++b) keys += seqs[b].n_q ? visible_keys(seqs[b], counted, a->window, a->n_sink) : 0;
+    const bool tokens = h.dtype != MVLA_DTYPE_FP32 && page_by_tokens(a->pages.kind, most_rows, keys * v.kv_heads);
     p.attend = h.dtype == MVLA_DTYPE_FP32 ? plan_attend(h, batch, seqs, counted, a->window, a->n_sink, false)
              : tokens ? plan_tokens(h, batch, seqs, counted, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32))
                       : plan_page_tiles(h, batch, seqs, counted, a->window, a->n_sink);
