@@ -157,6 +157,50 @@ inline int32_t check_page_attention(const ServeShape& v, int32_t batch, const mv
     return MVLA_OK;
 }
 
+// Parts (clusters of 1, 2, 4 or 8 CTAs) of about the same length over the whole batch, a multiple of 64 keys to a CTA, so that their CTAs fill whole rounds
+// of those that fit, or a cluster to a sequence: what ends first, in keys of a CTA (about 30 a microsecond): its keys and 256 for its start and end in every round, and where a
+// sequence has several clusters 128 for the kernel that joins them and 4 for every one of the most there are (one token over 131072 e4m3 rows: the join 7.3 us
+// of 68 with 74 parts).  256 parts to a sequence at most.
+inline void cut_page_tokens(AttendPlan& p, int64_t fit, int kv_heads, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink)
+{
+    int64_t keys = 0, longest = 1;
+    for (int b = 0; b < batch; ++b) {
+        if (seqs[b].n_q == 0) continue;
+        const int64_t n = visible_keys(seqs[b], counted, window, n_sink);
+        keys += n;
+        longest = n > longest ? n : longest;
+    }
+    int64_t ctas = 0;
+    const auto cut = [&](int cluster, int64_t part) {        // `part` keys to a CTA
+        p.cluster = cluster;
+        p.part_keys = part * cluster;
+        p.splits = 1;
+        p.blocks = 0;
+        for (int b = 0; b < batch; ++b) {
+            const int32_t n = parts_of(p, seqs[b], counted, window, n_sink);
+            p.blocks += static_cast<int64_t>(n) * cluster;
+            p.splits = n > p.splits ? n : p.splits;
+        }
+        ctas = p.blocks * kv_heads;
+    };
+    int64_t best = 0, best_cost = 0;
+    int best_cluster = 1;
+    for (int cluster = 1; cluster <= 8; cluster *= 2)
+        for (int rounds = 0; rounds <= 4; ++rounds) {
+            // (a cluster lies inside a group of multiprocessors, whose number need not divide)
+            const int64_t at_once = fit - fit * (cluster == 1 ? 0 : cluster == 2 ? 3 : cluster == 4 ? 6 : 10) / 100;
+            int64_t part = rounds ? (keys * kv_heads + rounds * at_once - 1) / (rounds * at_once) : (longest + cluster - 1) / cluster;
+            part = std::max<int64_t>(part, (longest + 256 * cluster - 1) / (256 * cluster));
+            part = std::max<int64_t>(64, (part + 63) / 64 * 64);
+            cut(cluster, part);
+            for (int tries = 0; rounds && ctas > rounds * at_once && part * cluster < longest && tries < 8; ++tries) cut(cluster, part += (part / 16 + 63) / 64 * 64);
+            const int64_t mine = std::min(part, (longest + cluster - 1) / cluster);
+            const int64_t cost = (ctas + at_once - 1) / at_once * (mine + 256) + (p.splits > 1 ? 128 + 4 * p.splits : 0);
+            if (!best || cost < best_cost) { best = part; best_cost = cost; best_cluster = cluster; }
+        }
+    cut(best_cluster, best);
+}
+
 // Single tokens, of whose CTAs `ctas` fit on a multiprocessor.
 inline AttendPlan plan_tokens(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, int ctas)
 {
@@ -168,7 +212,7 @@ inline AttendPlan plan_tokens(const ServeShape& c, int32_t batch, const mvla_seq
         p.total_kv += seqs[b].n_kv;
         p.rows = std::max(p.rows, static_cast<int32_t>(seqs[b].n_q * static_cast<int64_t>(c.n_heads / c.kv_heads)));
     }
-    cut_for_tokens(p, static_cast<int64_t>(c.sm_count) * ctas, c.kv_heads, batch, seqs, counted, window, n_sink);
+    cut_page_tokens(p, static_cast<int64_t>(c.sm_count) * ctas, c.kv_heads, batch, seqs, counted, window, n_sink);
     if (p.splits > 1) {
         int64_t part_q = 0;
         for (int b = 0; b < batch; ++b) part_q += static_cast<int64_t>(parts_of(p, seqs[b], counted, window, n_sink)) * seqs[b].n_q;

@@ -22,8 +22,8 @@ MVLA_BOTH constexpr int page_row_scales(int kind, int d) { return kind == MVLA_P
 
 // Single tokens (page_token.cu): subtiles of 16 keys in a warp's tile, bytes of a tile in shared memory (in whole groups of 64 columns of the values),
 // tiles of a warp, and the CTAs that fit on a multiprocessor (four at most: by registers).
-constexpr int kPageTokenStages = 3;
-MVLA_BOTH constexpr int page_token_sub(int kind, int pieces_of_32) { return pieces_of_32 <= 2 || (kind == MVLA_PAGE_E2M1 && pieces_of_32 <= 4) ? 2 : 1; }
+constexpr int kPageTokenStages = 2;
+MVLA_BOTH constexpr int page_token_sub(int kind, int pieces_of_32) { return pieces_of_32 <= 2 || (kind != MVLA_PAGE_ROWS && pieces_of_32 <= 4) ? 2 : 1; }
 MVLA_BOTH constexpr int page_token_tile(int kind, int pieces_of_32)
 {
     const int run = kind == MVLA_PAGE_ROWS ? 16 : kind == MVLA_PAGE_E4M3 ? 8 : 4, scales = kind == MVLA_PAGE_ROWS ? 0 : kind == MVLA_PAGE_E4M3 ? 1 : pieces_of_32;

@@ -11,7 +11,8 @@
 // the quotient of the scales: 6 2^13 is a number of fp16, and a group 2^-27 of the largest one is nothing).  Queries are fp16 too, every row
 // times a power of two that puts its largest element between 2^14 and 2^15.  bf16 weights (unquantised pages) meet the values in two
 // parts, what the type holds and what it leaves; fp16 ones are one part, in units of 2^-kF16Lift of their reference.
-//   A sequence's visible keys are cut into parts of about the same length over the whole batch; a CTA is four warps that take the part's tiles in turn.
+//   A sequence's visible keys are cut into parts of about the same length over the whole batch; a CTA is four warps that take the part's tiles in turn.  The
+// parts of a cluster are joined through its shared memory, and clusters (where a sequence has more than one) by a kernel behind.
 #include "attend.cuh"
 #include "page.cuh"
 
@@ -103,6 +104,39 @@ struct Tile {
     }
 };
 
+// CTAs of this cluster; two words of the shared memory of one of them, at the offset of `addr`.
+__device__ __forceinline__ int cluster_ctas()
+{
+    int n;
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+    return n;
+}
+__device__ __forceinline__ float2 ld_peer(uint32_t addr, int rank)
+{
+    uint32_t remote;
+    float2 x;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(remote) : "memory");
+    return x;
+}
+// N runs that lie next to one another (16 bytes at most).
+template <int N, class W>
+__device__ __forceinline__ void load_runs(const uint8_t* p, W* w)
+{
+    if constexpr (N * sizeof(W) == 16) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p);
+        memcpy(w, &x, 16);
+    } else if constexpr (N * sizeof(W) == 8) {
+        const uint2 x = *reinterpret_cast<const uint2*>(p);
+        memcpy(w, &x, 8);
+    } else {
+        static_assert(N == 1, "runs");
+        w[0] = *reinterpret_cast<const W*>(p);
+    }
+}
+// The number that eight bits stand for, less `off`, without the conversion's pipe.
+__device__ __forceinline__ float byte_float(uint32_t byte, int off) { return __uint_as_float(0x4B000000u + byte) - static_cast<float>(8388608 + off); }
+
 template <int KIND, int D32, int NR>
 __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_token_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ PagePool pool)
 {
@@ -115,6 +149,7 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ uint4 q_frag[D32][NR][32];
     __shared__ float merge_m[kWarps][16], merge_f[kWarps][16], merge_l[kWarps][16];
+    __shared__ float2 cta_ml[16], peer_ml[kMaxCluster][8];
     __shared__ float q_lift[16], q_scale[16];                // what a row's queries are multiplied by; what that makes of the scores' scale
     __shared__ __align__(4) uint16_t factors[kE2m1 ? kWarps : 1][kE2m1 ? U : 1][2][kE2m1 ? D32 : 1][16];      // of the groups of a tile's rows, fp16
     pdl_wait();
@@ -132,7 +167,9 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
         }
     const int lo = query_pos(a, s, len, 0), hi = query_pos(a, s, len, s.n_q - 1);
     const TileRange range = tile_range(a, len, lo, hi, Sh::kKeys);
-    const int part = static_cast<int>(blockIdx.x) - s.blk0, per_part = (range.count + s.parts - 1) / s.parts;
+    // (s.parts: clusters; each CTA of one takes a part)
+    const int ranks = cluster_ctas(), rank = ranks > 1 ? static_cast<int>(cluster_ctarank()) : 0;
+    const int part = static_cast<int>(blockIdx.x) - s.blk0, parts = s.parts * ranks, per_part = (range.count + parts - 1) / parts;
     const int t0 = part * per_part, t1 = min(range.count, t0 + per_part);
     // o[m][i][n]: columns column(m, g) + 2 i and + 1 (values 0, 1 and 2, 3), rows 8 n + 2 c and + 1
     float o[M64][4][NR][4];
@@ -287,35 +324,56 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
         // x[v][n][2 k + e]: key 16 v + g + 8 k, row 8 n + 2 c + e
         float x[U][NR][4] = {};
 #pragma unroll
-        for (int i = 0; i < D32; ++i) {
-            uint4 y[NR];
+        for (int i0 = 0; i0 < D32; ++i0) {
+            const int lot = Sh::lot(i0, D32, Run<KIND>::kKeyRuns);
+            if (i0 % lot) continue;
+            uint4 y[4][NR];
 #pragma unroll
-            for (int n = 0; n < NR; ++n) y[n] = q_frag[i][n][lane];
+            for (int i = 0; i < lot; ++i)
+#pragma unroll
+                for (int n = 0; n < NR; ++n) y[i][n] = q_frag[i0 + i][n][lane];
 #pragma unroll
             for (int v = 0; v < U; ++v) {
-                const uint8_t* const rows = tile + v * (2 * Sh::kKeyRow + 4 * Sh::kValueRow) + Sh::key_at(i, lane);
-                const Word k0 = *reinterpret_cast<const Word*>(rows), k1 = *reinterpret_cast<const Word*>(rows + Sh::kKeyRow);
-                uint32_t w0[4], w1[4];
-                if constexpr (KIND == MVLA_PAGE_ROWS) {
-                    w0[0] = k0.x; w0[1] = k0.y; w0[2] = k0.z; w0[3] = k0.w;
-                    w1[0] = k1.x; w1[1] = k1.y; w1[2] = k1.z; w1[3] = k1.w;
-                } else if constexpr (KIND == MVLA_PAGE_E4M3) {
-                    from_e4m3(k0.x, w0[0], w0[1]);
-                    from_e4m3(k0.y, w0[2], w0[3]);
-                    from_e4m3(k1.x, w1[0], w1[1]);
-                    from_e4m3(k1.y, w1[2], w1[3]);
+                const uint8_t* const rows = tile + v * (2 * Sh::kKeyRow + 4 * Sh::kValueRow) + Sh::key_at(i0, lane);
+                Word k0[4], k1[4];
+                if (lot == 4 && kE2m1) {
+                    load_runs<kE2m1 ? 4 : 1>(rows, k0);
+                    load_runs<kE2m1 ? 4 : 1>(rows + Sh::kKeyRow, k1);
+                } else if (lot == 2 && kScaled) {
+                    load_runs<kScaled ? 2 : 1>(rows, k0);
+                    load_runs<kScaled ? 2 : 1>(rows + Sh::kKeyRow, k1);
                 } else {
-                    const int gr = Sh::element(i, c) / kPageGroup;
-                    const uint32_t f0 = factors[warp][v][0][gr][g] * 0x10001u, f1 = factors[warp][v][0][gr][g + 8] * 0x10001u;
-                    from_e2m1(k0, w0);
-                    from_e2m1(k1, w1);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) { w0[h] = times(w0[h], f0); w1[h] = times(w1[h], f1); }
+                    load_runs<1>(rows, k0);
+                    load_runs<1>(rows + Sh::kKeyRow, k1);
+                }
+                uint32_t f0 = 0, f1 = 0;
+                if constexpr (kE2m1) {
+                    const int gr = i0 + (lot == 4 ? c : lot == 2 ? c >> 1 : 0);
+                    f0 = factors[warp][v][0][gr][g] * 0x10001u;
+                    f1 = factors[warp][v][0][gr][g + 8] * 0x10001u;
                 }
 #pragma unroll
-                for (int n = 0; n < NR; ++n) {
-                    mma16<kScaled>(x[v][n], w0[0], w1[0], w0[1], w1[1], y[n].x, y[n].y);
-                    mma16<kScaled>(x[v][n], w0[2], w1[2], w0[3], w1[3], y[n].z, y[n].w);
+                for (int i = 0; i < lot; ++i) {
+                    uint32_t w0[4], w1[4];
+                    if constexpr (KIND == MVLA_PAGE_ROWS) {
+                        w0[0] = k0[i].x; w0[1] = k0[i].y; w0[2] = k0[i].z; w0[3] = k0[i].w;
+                        w1[0] = k1[i].x; w1[1] = k1[i].y; w1[2] = k1[i].z; w1[3] = k1[i].w;
+                    } else if constexpr (KIND == MVLA_PAGE_E4M3) {
+                        from_e4m3(k0[i].x, w0[0], w0[1]);
+                        from_e4m3(k0[i].y, w0[2], w0[3]);
+                        from_e4m3(k1[i].x, w1[0], w1[1]);
+                        from_e4m3(k1[i].y, w1[2], w1[3]);
+                    } else {
+                        from_e2m1(k0[i], w0);
+                        from_e2m1(k1[i], w1);
+#pragma unroll
+                        for (int h = 0; h < 4; ++h) { w0[h] = times(w0[h], f0); w1[h] = times(w1[h], f1); }
+                    }
+#pragma unroll
+                    for (int n = 0; n < NR; ++n) {
+                        mma16<kScaled>(x[v][n], w0[0], w1[0], w0[1], w1[1], y[i][n].x, y[i][n].y);
+                        mma16<kScaled>(x[v][n], w0[2], w1[2], w0[3], w1[3], y[i][n].z, y[i][n].w);
+                    }
                 }
             }
         }
@@ -329,13 +387,13 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     kbyte[k] = bytes[g + 8 * k];
-                    of_value[v][k] = static_cast<float>(static_cast<int>(bytes[16 + g + 8 * k]) - 127);
+                    of_value[v][k] = byte_float(bytes[16 + g + 8 * k], 127);
                 }
             } else if constexpr (kE2m1) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     kbyte[k] = static_cast<uint32_t>(__shfl_sync(0xffffffffu, largest[v], g + 8 * k));
-                    of_value[v][k] = static_cast<float>(__shfl_sync(0xffffffffu, largest[v], 16 + g + 8 * k) - 127 - kCodeLift);
+                    of_value[v][k] = byte_float(static_cast<uint32_t>(__shfl_sync(0xffffffffu, largest[v], 16 + g + 8 * k)), 127 + kCodeLift);
                 }
             }
 #pragma unroll
@@ -437,60 +495,74 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
 #pragma unroll
             for (int n = 0; n < 4; ++n) hidden[n] = !kE2m1 && !all && (seen[v][n >> 1] >> (4 * (2 * c + (n & 1))) & 0xFu) == 0;
 #pragma unroll
-            for (int m = 0; m < M64; ++m) {
-                Word w[4];
+            for (int m0 = 0; m0 < M64; ++m0) {
+                const int lot = m0 < D32 / 2 ? Sh::lot(m0, D32 / 2, Run<KIND>::kValueRuns) : 1;
+                if (m0 % lot) continue;
+                Word w[4][2];
 #pragma unroll
-                for (int n = 0; n < 4; ++n) {
-                    w[n] = Word{};
-                    if (!hidden[n] && (m < D32 / 2 || g < 4))
-                        w[n] = *reinterpret_cast<const Word*>(tile + v * (2 * Sh::kKeyRow + 4 * Sh::kValueRow) + 2 * Sh::kKeyRow + n * Sh::kValueRow + Sh::value_at(m, lane));
+                for (int n = 0; n < 4; ++n) {               // (a half group: what its other lanes find goes into columns that nobody reads)
+                    const uint8_t* const row = tile + v * (2 * Sh::kKeyRow + 4 * Sh::kValueRow) + 2 * Sh::kKeyRow + n * Sh::kValueRow + Sh::value_at(m0, lane);
+                    if (lot == 2 && kScaled) load_runs<kScaled ? 2 : 1>(row, w[n]);
+                    else load_runs<1>(row, w[n]);
                 }
-                // op[i][h]: columns 2 i (h = 0, 2) and 2 i + 1 of the lane's run, keys 2 c, 2 c + 1 (h < 2) and 2 c + 8, 2 c + 9
-                uint32_t op[4][4];
-                if constexpr (KIND == MVLA_PAGE_ROWS) {
-                    const uint32_t x4[4][4] = {{w[0].x, w[0].y, w[0].z, w[0].w}, {w[1].x, w[1].y, w[1].z, w[1].w}, {w[2].x, w[2].y, w[2].z, w[2].w}, {w[3].x, w[3].y, w[3].z, w[3].w}};
+                if (!kE2m1 && !all) {
+#pragma unroll
+                    for (int n = 0; n < 4; ++n)
+                        if (hidden[n]) w[n][0] = w[n][1] = Word{};
+                }
+                uint32_t f[2] = {0, 0};
+                if constexpr (kE2m1) {
+                    const int gr = min(2 * m0 + (lot == 2 ? g >> 1 : g >> 2), D32 - 1);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) f[h] = *reinterpret_cast<const uint32_t*>(&factors[warp][v][1][gr][2 * c + 8 * h]);
+                }
+#pragma unroll
+                for (int mm = 0; mm < lot; ++mm) {
+                    // op[i][h]: columns 2 i (h = 0, 2) and 2 i + 1 of the lane's run, keys 2 c, 2 c + 1 (h < 2) and 2 c + 8, 2 c + 9
+                    uint32_t op[4][4];
+                    if constexpr (KIND == MVLA_PAGE_ROWS) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const uint4 p0 = w[2 * h][mm], p1 = w[2 * h + 1][mm];
+                            const uint32_t x0[4] = {p0.x, p0.y, p0.z, p0.w}, x1[4] = {p1.x, p1.y, p1.z, p1.w};
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                op[i][2 * h] = __byte_perm(x0[i], x1[i], 0x5410);
+                                op[i][2 * h + 1] = __byte_perm(x0[i], x1[i], 0x7632);
+                            }
+                        }
+                    } else if constexpr (KIND == MVLA_PAGE_E4M3) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {    // (the two keys' bytes of two columns)
+                                const uint2 p0 = w[2 * h][mm], p1 = w[2 * h + 1][mm];
+                                from_e4m3(__byte_perm(i < 2 ? p0.x : p0.y, i < 2 ? p1.x : p1.y, i & 1 ? 0x7362 : 0x5140), op[i][2 * h], op[i][2 * h + 1]);
+                            }
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {        // (the two keys' halves of a byte, of even and of odd columns)
+                            const uint32_t p0 = w[2 * h][mm], p1 = w[2 * h + 1][mm];
+                            uint32_t lo[4], hi[4];
+                            from_e2m1((p0 & 0x0F0F0F0Fu) | (p1 << 4 & 0xF0F0F0F0u), lo);
+                            from_e2m1((p0 >> 4 & 0x0F0F0F0Fu) | (p1 & 0xF0F0F0F0u), hi);
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) { op[i][2 * h] = times(lo[i], f[h]); op[i][2 * h + 1] = times(hi[i], f[h]); }
+                        }
+                    }
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            op[i][2 * h] = __byte_perm(x4[2 * h][i], x4[2 * h + 1][i], 0x5410);
-                            op[i][2 * h + 1] = __byte_perm(x4[2 * h][i], x4[2 * h + 1][i], 0x7632);
+                        for (int n = 0; n < NR; ++n) {
+                            mma16<kScaled>(o[m0 + mm][i][n], op[i][0], op[i][1], op[i][2], op[i][3], w_hi[n][0], w_hi[n][1]);
+                            if constexpr (!kScaled) mma16<false>(o[m0 + mm][i][n], op[i][0], op[i][1], op[i][2], op[i][3], w_lo[n][0], w_lo[n][1]);
                         }
-                } else if constexpr (KIND == MVLA_PAGE_E4M3) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {        // (the two keys' bytes of two columns)
-                            const uint32_t two = __byte_perm(i < 2 ? w[2 * h].x : w[2 * h].y, i < 2 ? w[2 * h + 1].x : w[2 * h + 1].y, i & 1 ? 0x7362 : 0x5140);
-                            from_e4m3(two, op[i][2 * h], op[i][2 * h + 1]);
-                        }
-                } else {
-                    const int gr = min(Sh::column(m, g) / kPageGroup, D32 - 1);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {            // (the two keys' halves of a byte, of even and of odd columns)
-                        const uint32_t f = *reinterpret_cast<const uint32_t*>(&factors[warp][v][1][gr][2 * c + 8 * h]);
-                        const uint32_t even = (w[2 * h] & 0x0F0F0F0Fu) | (w[2 * h + 1] << 4 & 0xF0F0F0F0u);
-                        const uint32_t odd = (w[2 * h] >> 4 & 0x0F0F0F0Fu) | (w[2 * h + 1] & 0xF0F0F0F0u);
-                        uint32_t lo[4], hi[4];
-                        from_e2m1(even, lo);
-                        from_e2m1(odd, hi);
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) { op[i][2 * h] = times(lo[i], f); op[i][2 * h + 1] = times(hi[i], f); }
-                    }
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-#pragma unroll
-                    for (int n = 0; n < NR; ++n) {
-                        mma16<kScaled>(o[m][i][n], op[i][0], op[i][1], op[i][2], op[i][3], w_hi[n][0], w_hi[n][1]);
-                        if constexpr (!kScaled) mma16<false>(o[m][i][n], op[i][0], op[i][1], op[i][2], op[i][3], w_lo[n][0], w_lo[n][1]);
-                    }
             }
         }
         if constexpr (kE2m1) __syncwarp();                   // (the factors are read)
     }
-    // ---- the warps' sums, row by row (where the tiles were: their copies have all been waited for)
-    float (*const merge_o)[D] = reinterpret_cast<float (*)[D]>(ring);
+    // ---- the warps' sums, eight rows at a time (where the tiles were: their copies have all been waited for), then the cluster's
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -503,47 +575,87 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
                 merge_l[warp][8 * n + 2 * c + e] = sum[n][e];
             }
         }
-    const bool whole = s.parts == 1;
+    __syncthreads();
+    if (t < 8 * NR) {
+        float m = merge_m[0][t], l = 0.f;
 #pragma unroll
-    for (int r = 0; r < 8 * NR; ++r) {
-        if (r >= n_rows) break;
-        __syncthreads();
-        if (c == (r & 7) >> 1) {
-#pragma unroll
-            for (int m = 0; m < M64; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (m < D32 / 2 || g < 4)
-                        *reinterpret_cast<float2*>(&merge_o[warp][Sh::column(m, g) + 2 * i]) = make_float2(o[m][i][r / 8][r & 1], o[m][i][r / 8][2 + (r & 1)]);
-        }
-        __syncthreads();
-        float m = merge_m[0][r];
-#pragma unroll
-        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, merge_m[w][r]);
+        for (int w = 1; w < kWarps; ++w) m = fmaxf(m, merge_m[w][t]);
         const float base = m == -CUDART_INF_F ? 0.f : m;
-        float l = 0.f, f[kWarps];
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
-            f[w] = exp2f(merge_f[w][r] - base);
-            l += merge_l[w][r] * exp2f(merge_m[w][r] - base);
+            l += merge_l[w][t] * exp2f(merge_m[w][t] - base);
+            merge_f[w][t] = exp2f(merge_f[w][t] - base);
         }
-        const float inv = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
-        const int i = r / group, head = hk * group + r % group;
-        const int64_t at = (s.part0 + static_cast<int64_t>(part) * s.n_q + i) * a.n_heads + head;
-        for (int col = 2 * t; col < D; col += 2 * kWarps * 32) {
+        cta_ml[t] = make_float2(m, l);
+    }
+    const bool whole = s.parts == 1;
+    // elements col, col + 1 of row r's sums against reference m, whose exponentials have the sum l
+    const auto give = [&](int r, int col, float y, float z, float m, float l) {
+        const int i = r / group, head = hk * group + r - i * group;
+        if (whole) {
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const int64_t at = (s.q_row + i) * a.n_heads + head;
+            *reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(a.out) + at * D + col) = __floats2bfloat162_rn(y * inv, z * inv);
+            if (a.lse && col == 0) a.lse[at] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
+        } else {
+            const int64_t at = (s.part0 + static_cast<int64_t>(part / ranks) * s.n_q + i) * a.n_heads + head;
+            *reinterpret_cast<float2*>(a.part_o + at * D + col) = make_float2(y, z);
+            if (col == 0) a.part_ml[at] = make_float2(m, l);
+        }
+    };
+    float (*const merge_o)[8][D] = reinterpret_cast<float (*)[8][D]>(ring);
+#pragma unroll
+    for (int n = 0; n < NR; ++n) {
+        if (8 * n >= n_rows) break;                          // (in all CTAs of a cluster: they share the sequence)
+        if (n > 0) __syncthreads();
+#pragma unroll
+        for (int m = 0; m < M64; ++m)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (m < D32 / 2 || g < 4) {
+                    *reinterpret_cast<float2*>(&merge_o[warp][2 * c][Sh::column(m, g) + 2 * i]) = make_float2(o[m][i][n][0], o[m][i][n][2]);
+                    *reinterpret_cast<float2*>(&merge_o[warp][2 * c + 1][Sh::column(m, g) + 2 * i]) = make_float2(o[m][i][n][1], o[m][i][n][3]);
+                }
+        __syncthreads();
+        const int pairs = min(8, n_rows - 8 * n) * (D / 2);
+        for (int u = t; u < pairs; u += kWarps * 32) {
+            const int r = u / (D / 2), col = u % (D / 2) * 2;
             float y = 0.f, z = 0.f;
 #pragma unroll
             for (int w = 0; w < kWarps; ++w) {
-                y = fmaf(merge_o[w][col], f[w], y);
-                z = fmaf(merge_o[w][col + 1], f[w], z);
+                const float2 x2 = *reinterpret_cast<const float2*>(&merge_o[w][r][col]);
+                y = fmaf(x2.x, merge_f[w][8 * n + r], y);
+                z = fmaf(x2.y, merge_f[w][8 * n + r], z);
             }
-            if (whole) reinterpret_cast<__nv_bfloat162*>(static_cast<__nv_bfloat16*>(a.out) + ((s.q_row + i) * a.n_heads + head) * D)[col / 2] = __floats2bfloat162_rn(y * inv, z * inv);
-            else *reinterpret_cast<float2*>(a.part_o + at * D + col) = make_float2(y, z);
+            if (ranks == 1) give(8 * n + r, col, y, z, cta_ml[8 * n + r].x, cta_ml[8 * n + r].y);
+            else *reinterpret_cast<float2*>(&merge_o[0][r][col]) = make_float2(y, z);
         }
-        if (t == 0) {
-            if (whole && a.lse) a.lse[(s.q_row + i) * a.n_heads + head] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
-            if (a.part_ml) a.part_ml[at] = make_float2(m, l);
+        if (ranks == 1) continue;
+        cluster_arrive_release();
+        cluster_wait_acquire();
+        if (t < 8 * ranks) peer_ml[t >> 3][t & 7] = ld_peer(smem_u32(&cta_ml[8 * n + (t & 7)]), t >> 3);
+        __syncthreads();
+        for (int u = rank * kWarps * 32 + t; u < pairs; u += ranks * kWarps * 32) {
+            const int r = u / (D / 2), col = u % (D / 2) * 2;
+            float2 x2[kMaxCluster];
+#pragma unroll
+            for (int k = 0; k < kMaxCluster; ++k)
+                if (k < ranks) x2[k] = ld_peer(smem_u32(&merge_o[0][r][col]), k);
+            float m = -CUDART_INF_F, l = 0.f, y = 0.f, z = 0.f;
+            for (int k = 0; k < ranks; ++k) m = fmaxf(m, peer_ml[k][r].x);
+            const float base = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+            for (int k = 0; k < kMaxCluster; ++k)
+                if (k < ranks) {
+                    const float f = exp2f(peer_ml[k][r].x - base);
+                    l = fmaf(peer_ml[k][r].y, f, l);
+                    y = fmaf(x2[k].x, f, y);
+                    z = fmaf(x2[k].y, f, z);
+                }
+            give(8 * n + r, col, y, z, m, l);
         }
+        cluster_arrive_release();                            // (nobody's sums are written over, or gone, while another reads them)
+        cluster_wait_acquire();
     }
 }
 
@@ -559,9 +671,12 @@ cudaError_t attend(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
     cfg.blockDim = dim3(kWarps * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cudaLaunchAttribute attr[2] = {pdl_attribute(), {}};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(a.cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = a.cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, page_token_kernel<KIND, D32, NR>, a, pool);
 }
 template <int KIND, int D32>

@@ -110,6 +110,7 @@ void fill_attention(AttArgs& k, const CtxView& v, int32_t batch, const mvla_seq*
     k.lse2 = reinterpret_cast<float*>(at(plan.lse2));
     k.part_mass = reinterpret_cast<float*>(at(plan.part_mass));
     k.logits = reinterpret_cast<float*>(at(plan.logits));
+    k.cluster = plan.cluster;
     k.skip_whole = plan.form == kFormToken || plan.form == kFormPageTile;
     const int group = v.n_heads / v.kv_heads;
     const bool counted = all_counted(a);
@@ -119,7 +120,7 @@ void fill_attention(AttArgs& k, const CtxView& v, int32_t batch, const mvla_seq*
         const mvla_seq& s = seqs[b];
         const int32_t parts = parts_of(plan, s, counted, a->window, a->n_sink);
         k.s[b] = AttSeq{s.q_row, s.kv_row, s.n_q, s.n_kv, blk, qp, kvp, tile, parts, part, logit, 0, 0, b};
-        blk += plan.form == kFormToken ? parts
+        blk += plan.form == kFormToken ? parts * plan.cluster
              : plan.form == kFormPageTile ? static_cast<int32_t>((static_cast<int64_t>(s.n_q) + plan.queries - 1) / plan.queries * parts)
              : static_cast<int32_t>(plan.form == kFormTile ? (static_cast<int64_t>(s.n_q) + plan.queries - 1) / plan.queries
                                                            : (static_cast<int64_t>(s.n_q) * group + plan.rows - 1) / plan.rows);
