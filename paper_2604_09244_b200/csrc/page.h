@@ -46,4 +46,7 @@ cudaError_t launch_page_tiles(int hidden_dtype, int kind, PageRowsArgs& a, cudaS
 // Single tokens (launch_attend_token's), over pages; q and out bf16.  Behind it: launch_attend_finish.
 cudaError_t launch_page_token(int kind, const AttArgs& a, const PagePool& pool, int rows, cudaStream_t stream);
 
+// Blocks of query rows over quantised pages, unpacked on the way (launch_page_tile's blocks and parts); q and out bf16.  Behind it: launch_attend_join.
+cudaError_t launch_page_decode(int kind, const AttArgs& a, const PagePool& pool, cudaStream_t stream);
+
 }  // namespace mvla

@@ -152,7 +152,9 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
         t.page_shift = __builtin_ctz(kPageTile);
     }
     cudaError_t e;
-    if (plan.attend.form == kFormFma) {
+    if (plan.unpack) {
+        e = launch_page_decode(a->pages.kind, t, pool, st);
+    } else if (plan.attend.form == kFormFma) {
         e = launch_page_fma(t, plan.attend.rows, st);
     } else {
         bool tokens = false;

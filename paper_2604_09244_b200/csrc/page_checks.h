@@ -103,6 +103,7 @@ struct PageAttendPlan {
     AttendPlan attend;
     // quantised pages that are no single tokens': the tiles that some query sees, as elements of the hidden type (-1: there are none)
     int64_t dense_k = -1, dense_v = -1, dense_tiles = 0, bytes = 0;
+    bool unpack = false;         // ... or the tile form unpacks them on the way
 };
 
 // Tiles that a sequence's queries see, at most.
@@ -288,6 +289,33 @@ inline bool page_by_tokens(int kind, int64_t rows, int64_t keys_and_heads)
     return rows <= kTokenRows && (kind != MVLA_PAGE_ROWS || (rows <= 8 && keys_and_heads < 32768));
 }
 
+// Whether so few blocks of queries go over a sequence's pages that each had better unpack them for itself: unpacking first costs 0.15 us for 1000 rows of a head (their
+// bytes, twice), on the way 0.06 us for every block that does.  us, on the way / first, 32 heads in groups of 4, e4m3: 5 tokens over 60000 rows (a block) 61 / 121;
+// 4 chunks of 56 over 2000 to 6000 (two) 52 / 57, of 33 over 4000 (two) 48 / 51; 100 over 4096 (four) 36 / 31; 512 over 8192 (16) 141 / 98.
+inline bool unpacks_on_the_way(const AttendPlan& p, int32_t batch, const mvla_seq* seqs)
+{
+    int64_t most = 0;
+    for (int b = 0; b < batch; ++b) most = std::max(most, (static_cast<int64_t>(seqs[b].n_q) + p.queries - 1) / p.queries);
+    return most <= 2;
+}
+
+// fp32: as packed rows, but in blocks of 8 query rows where the call is so short that the CTAs of those run at once and a block's keys are few (208 rows of 8 heads of 64,
+// window 64, 16.6 us instead of 22.4; 64 queries of 32 heads of 128 over 564 rows would take 82 instead of 44: a block copies all keys).
+inline AttendPlan plan_page_fma(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink)
+{
+    AttendPlan p = plan_attend(c, batch, seqs, counted, window, n_sink, false);
+    int64_t blocks = 0, longest = 0;
+    for (int b = 0; b < batch; ++b) {
+        blocks += (static_cast<int64_t>(seqs[b].n_q) * (c.n_heads / c.kv_heads) + 7) / 8;
+        if (seqs[b].n_q) longest = std::max(longest, visible_keys(seqs[b], counted, window, n_sink));
+    }
+    if (p.splits == 1 && blocks * c.kv_heads <= 2 * static_cast<int64_t>(c.sm_count) && longest * c.head_dim <= 16384) {
+        p.rows = 8;
+        p.blocks = blocks;
+    }
+    return p;
+}
+
 inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, const mvla_seq* seqs, const mvla_paged_attention* a)
 {
     PageAttendPlan p;
@@ -298,11 +326,15 @@ inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, co
     int64_t keys = 0;
     for (int b = 0; b < batch; ++b) keys += seqs[b].n_q ? visible_keys(seqs[b], counted, a->window, a->n_sink) : 0;
     const bool tokens = h.dtype != MVLA_DTYPE_FP32 && page_by_tokens(a->pages.kind, most_rows, keys * v.kv_heads);
-    p.attend = h.dtype == MVLA_DTYPE_FP32 ? plan_attend(h, batch, seqs, counted, a->window, a->n_sink, false)
+    p.attend = h.dtype == MVLA_DTYPE_FP32 ? plan_page_fma(h, batch, seqs, counted, a->window, a->n_sink)
              : tokens ? plan_tokens(h, batch, seqs, counted, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32))
                       : plan_page_tiles(h, batch, seqs, counted, a->window, a->n_sink);
     p.bytes = p.attend.bytes;
     if (a->pages.kind == MVLA_PAGE_ROWS || tokens) return p;
+    if (p.attend.form == kFormPageTile && unpacks_on_the_way(p.attend, batch, seqs)) {
+        p.unpack = true;
+        return p;
+    }
     Workspace w;
     w.take(p.attend.bytes);
     for (int b = 0; b < batch; ++b) p.dense_tiles += seen_tiles(seqs[b], a->window, a->n_sink);

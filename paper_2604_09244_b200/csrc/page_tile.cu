@@ -1,0 +1,474 @@
+// Attention of chunks of new tokens over quantised pages on the tensor cores: keys and values are unpacked to fp16 on their way into shared memory.
+//
+// As attend_tile.cu: a CTA has a tile of 128 query rows that share a key head and walks the tiles of 64 keys of its part,
+//     S = Q K^T  ->  P = 2^(S - reference) in fp16, back into the columns of S  ->  O += P V,
+// a thread to a row in the softmax (warps 0-3), S double-buffered, one warp that issues the MMAs.  A warp copies codes and scales into a ring, 16 rows of a page at
+// a time; four warps turn them into fp16 and store them as the MMAs read them (128-byte swizzle).
+// Scales are powers of two.  A tile's largest scale of its keys becomes a factor of its scores and the largest one of its values a factor of its weights (both the same
+// for the whole tile); what a row, or 32 elements, have less is multiplied into the codes, which have as much room above in fp16 (2^7 for e4m3, 2^13 for e2m1): rows or
+// groups below 2^-21 (2^-27) of their tile's largest scale count as nothing.  Outputs are summed in units of the largest values so far (and four
+// times more); where a tile's are larger still, the sums are taken down, as they are when a row's reference moves.  Queries are fp16 too, every row times a
+// power of two that puts its largest element between 2^14 and 2^15.
+#include "attend_tile.cuh"
+#include "attend_walk.h"
+#include "page.cuh"
+
+#include <algorithm>
+
+namespace mvla {
+namespace {
+
+template <int KIND> struct Codes;
+template <> struct Codes<MVLA_PAGE_E4M3> { using Word = uint2; static constexpr int kLift = 7; };       // eight elements; room above the codes in fp16
+template <> struct Codes<MVLA_PAGE_E2M1> { using Word = uint32_t; static constexpr int kLift = 13; };
+
+template <int KIND, int D32>
+struct PageTileShape {
+    static constexpr int kDB = (D32 + 1) / 2;                // boxes of 64 elements
+    static constexpr int kIssues = 4, kLoads = 5, kDecodes = 6, kDecoders = 4, kWarps = kDecodes + kDecoders;
+    static constexpr int kO = 2 * kKeys, kColumns = kO + kDB * 64 <= 256 ? 256 : 512;       // of tensor memory: S (two buffers, P in the same columns), then O
+    static constexpr int kCtas = kTmemColsPerSm / kColumns;
+    static constexpr int kQBytes = kDB * kRows * 128, kStage = kDB * kKeys * 128;
+    // the ring: codes of a tile's keys, with the scales of its keys and values, or codes of its values
+    static constexpr int kRowBytes = page_row_bytes(KIND, D32 * 32, 2), kGroups = page_row_scales(KIND, D32 * 32);
+    static constexpr int kCodes = kKeys * kRowBytes, kSlot = kCodes + 2 * kKeys * kGroups, kSlots = 3;
+    static constexpr int kRoom = ((kCtas == 2 ? kSmemPerSm / 2 - kSmemReservedPerCta : kSmemMaxPerCta) - 6 * 1024 - kQBytes - kSlots * kSlot) / kStage;
+    static constexpr int kStages = kRoom > kMaxStages ? kMaxStages : kRoom;
+    static constexpr int kSmem = 1024 + kQBytes + kStages * kStage + kSlots * kSlot;
+    static constexpr int kPieces = 2 * D32;                  // of eight elements, of a decoding thread, in a tile of keys or of values
+    static_assert(kStages >= 3 && kSlot % 16 == 0, "shape");
+};
+constexpr int kTileRefs = 8;                 // tiles whose references are kept
+
+__device__ __forceinline__ void codes_f16(uint2 w, uint32_t (&h)[4])
+{
+    from_e4m3(w.x, h[0], h[1]);
+    from_e4m3(w.y, h[2], h[3]);
+}
+__device__ __forceinline__ void codes_f16(uint32_t w, uint32_t (&h)[4]) { from_e2m1(w, h); }
+__device__ __forceinline__ uint32_t times2(uint32_t x, uint32_t f)
+{
+    const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&f));
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+__device__ __forceinline__ void store16(uint32_t at, const uint32_t (&w)[4])
+{
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+}
+// Where eight elements of a row lie in a tile of such rows, in boxes of 64 elements of `rows` rows.
+__device__ __forceinline__ uint32_t swizzled(int row, int piece, int rows) { return piece / 8 * rows * 128 + row * 128 + ((piece & 7) ^ (row & 7)) * 16; }
+
+template <int KIND, int D32>
+__global__ void __launch_bounds__(PageTileShape<KIND, D32>::kWarps * 32, PageTileShape<KIND, D32>::kCtas)
+page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ PagePool pool)
+{
+    using Sh = PageTileShape<KIND, D32>;
+    using Word = typename Codes<KIND>::Word;
+    constexpr bool kE2m1 = KIND == MVLA_PAGE_E2M1;
+    constexpr int D = D32 * 32, ST = Sh::kStages, P = Sh::kPieces, G = kE2m1 ? D32 : 1, kCodeLift = Codes<KIND>::kLift, kRowBytes = Sh::kRowBytes;
+    extern __shared__ uint8_t raw[];
+    __shared__ uint64_t bars[2 * kMaxStages + 8 + 2 * Sh::kSlots];
+    __shared__ unsigned groups_there[Sh::kSlots];            // of a slot: a bit to every 16 rows that have a page
+    __shared__ uint32_t factors[2][kKeys][G];                // of a tile's keys and values: fp16, twice
+    __shared__ uint32_t warp_top[Sh::kDecoders];
+    __shared__ int2 refs[kTileRefs];                         // bytes of the largest scales of a tile's keys and values
+    __shared__ int dead;
+    __shared__ uint32_t tmem_base;
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t q_at = base, kv_at = base + Sh::kQBytes;
+    const uint32_t bar0 = smem_u32(bars);
+    const auto full = [&](int i) { return bar0 + 8u * i; };
+    const auto empty = [&](int i) { return bar0 + 8u * (kMaxStages + i); };
+    const uint32_t q_full = bar0 + 8u * (2 * kMaxStages), s_full = q_full + 8, p_full = q_full + 24, o_step = q_full + 40, o_full = q_full + 48, ended = q_full + 56;
+    const uint32_t ring_at = kv_at + ST * Sh::kStage;
+    const uint8_t* const ring = raw + (ring_at - smem_u32(raw));
+    const auto raw_full = [&](int i) { return ended + 8u * (1 + i); };
+    const auto raw_empty = [&](int i) { return ended + 8u * (1 + Sh::kSlots + i); };
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
+
+    if (warp == Sh::kIssues && lane == 0) {
+        for (int i = 0; i < ST; ++i) { mbar_init(full(i), Sh::kDecoders); mbar_init(empty(i), 1); }
+        mbar_init(q_full, 4);
+        for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_full + 8 * i, 128); }
+        mbar_init(o_step, 1);
+        mbar_init(o_full, 1);
+        mbar_init(ended, 1);
+        for (int i = 0; i < Sh::kSlots; ++i) { mbar_init(raw_full(i), 1); mbar_init(raw_empty(i), Sh::kDecoders); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        dead = 0;
+    }
+    __syncwarp();
+    pdl_wait();
+    // (only now: what holds tensor memory ahead of this kernel in the stream is complete, and nothing that holds some waits for this CTA)
+    if (warp == Sh::kIssues) tmem_alloc(smem_u32(&tmem_base), Sh::kColumns);
+    const int heads = a.n_heads / a.pack, blk = a.n_blocks - 1 - static_cast<int>(blockIdx.x) / heads, head0 = static_cast<int>(blockIdx.x) % heads * a.pack;
+    const AttSeq& s = a.s[seq_of_block(a, blk)];
+    const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack;      // queries of the tile
+    const int piece_of_seq = (blk - s.blk0) % s.parts, q0 = (blk - s.blk0) / s.parts * per, len = seq_len(a, s);
+    const int lo = query_pos(a, s, len, q0), hi = query_pos(a, s, len, min(q0 + per, s.n_q) - 1);
+    const TileRange range = tile_range(a, len, lo, hi, kKeys);
+    const int per_part = (range.count + s.parts - 1) / s.parts, v0 = piece_of_seq * per_part, n = max(0, min(range.count - v0, per_part));
+    const auto first_key = [&](int i) { return range.tile(v0 + i) * kKeys; };
+    const auto masks = [&](int j0) {                         // whether some row does not see some key of a tile
+        return span_flags(a, lo, hi, counted_span(len, j0, kKeys)) != kNeed;
+    };
+    Guard guard = {&dead, a.status};
+
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    pdl_trigger();
+    const uint32_t tmem = tmem_base;
+
+    if (warp == Sh::kLoads) {
+        // ---- codes and scales: chunk 2 i the keys of tile i and both scales, chunk 2 i + 1 its values; a lane to every 16 rows
+        const auto look_up = [&](int i) {
+            if (i >= n || lane >= 4) return -1;
+            const int j = first_key(i) + 16 * lane;
+            return j < len ? page_of(pool, s.index, j) : -1;
+        };
+        int page = -1, ahead = look_up(0), c = 0;
+        for (; c < 2 * n; ++c) {
+            const int slot = c % Sh::kSlots;
+            if (!(c & 1)) {
+                page = ahead;
+                ahead = look_up(c / 2 + 1);
+            }
+            if (c >= Sh::kSlots && !guard.wait_all(raw_empty(slot), (c / Sh::kSlots - 1) & 1)) break;
+            const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
+            if (lane == 0) {
+                groups_there[slot] = there;
+                mbar_expect_tx(raw_full(slot), __popc(there) * (16 * kRowBytes + (c & 1 ? 0 : 2 * 16 * G)));
+            }
+            __syncwarp();
+            if (page >= 0) {
+                const int64_t row = page_row(pool, page, hk, first_key(c / 2) + 16 * lane);
+                const uint32_t to = ring_at + slot * Sh::kSlot;
+                bulk_load(to + 16 * lane * kRowBytes, static_cast<const uint8_t*>(c & 1 ? pool.v : pool.k) + row * kRowBytes, 16 * kRowBytes, raw_full(slot));
+                if (!(c & 1)) {
+                    bulk_load(to + Sh::kCodes + 16 * lane * G, pool.k_scale + row * G, 16 * G, raw_full(slot));
+                    bulk_load(to + Sh::kCodes + (kKeys + 16 * lane) * G, pool.v_scale + row * G, 16 * G, raw_full(slot));
+                }
+            }
+        }
+        for (int i = max(0, c - Sh::kSlots); i < c; ++i) guard.settle(raw_full(i % Sh::kSlots), i / Sh::kSlots & 1);      // (whoever gave up, what is under way lands)
+    } else if (warp >= Sh::kDecodes) {
+        // ---- codes into fp16
+        const int dt = t - Sh::kDecodes * 32, side = dt >> 6, own_row = dt & 63;
+        bool ok = true;
+        const auto meet = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+        uint8_t* const stages = raw + (kv_at - smem_u32(raw));
+        const auto one_piece = [&](uint8_t* stage, int u, Word w, uint32_t f, bool out) {
+            uint32_t h[4];
+            codes_f16(w, h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) h[i] = out ? 0u : times2(h[i], f);       // (0 times NaN is NaN)
+            *reinterpret_cast<uint4*>(stage + swizzled(u / (4 * D32), u % (4 * D32), kKeys)) = make_uint4(h[0], h[1], h[2], h[3]);
+        };
+        const auto decode = [&](int c, bool masked, int j0, unsigned there) {
+            uint8_t* const stage = stages + c % ST * Sh::kStage;
+            const Word* const codes = reinterpret_cast<const Word*>(ring + c % Sh::kSlots * Sh::kSlot);
+            const auto factor = [&](int u) { return factors[c & 1][u / (4 * D32)][kE2m1 ? u % (4 * D32) / 4 : 0]; };
+            if (!masked && there == 0xFu) {
+                Word w[P];
+                uint32_t f[P];
+#pragma unroll
+                for (int k = 0; k < P; ++k) {
+                    w[k] = codes[dt + 128 * k];
+                    f[k] = factor(dt + 128 * k);
+                }
+#pragma unroll
+                for (int k = 0; k < P; ++k) one_piece(stage, dt + 128 * k, w[k], f[k], false);
+            } else {
+#pragma unroll 1
+                for (int u = dt; u < 128 * P; u += 128) {
+                    const int row = u / (4 * D32);
+                    one_piece(stage, u, codes[u], factor(u), !(there >> (row >> 4) & 1u) || !(j0 + row < len && some_sees(lo, hi, j0 + row, a.window, a.n_sink)));
+                }
+            }
+            __syncwarp();                                    // (the fence between these stores and the MMAs is the issuing thread's)
+            if (lane == 0) {
+                mbar_arrive(full(c % ST));
+                mbar_arrive(raw_empty(c % Sh::kSlots));
+            }
+        };
+        const auto room = [&](int c) { return c < ST || guard.wait_all(empty(c % ST), (c / ST - 1) & 1); };
+        const auto codes_there = [&](int c) { return guard.wait_all(raw_full(c % Sh::kSlots), c / Sh::kSlots & 1); };
+        for (int i = 0; i < n; ++i) {                        // (a warp that gave up goes on meeting the others)
+            const int j0 = first_key(i);
+            const bool masked = masks(j0);
+            ok = ok && codes_there(2 * i);
+            const unsigned there = groups_there[2 * i % Sh::kSlots];
+            uint32_t scale[G], top = 0;
+            {                                                // of one row, of keys or values (those that nobody sees may hold anything)
+                const int j = j0 + own_row;
+                const bool on = (there >> (own_row >> 4) & 1u) && j < len && some_sees(lo, hi, j, a.window, a.n_sink);
+                const uint8_t* const b = ring + 2 * i % Sh::kSlots * Sh::kSlot + Sh::kCodes + dt * G;
+#pragma unroll
+                for (int g = 0; g < G; ++g) {
+                    scale[g] = on ? b[g] : 0u;
+                    top = max(top, scale[g]);
+                }
+            }
+            top = __reduce_max_sync(0xffffffffu, top);
+            if (lane == 0) warp_top[warp - Sh::kDecodes] = top;
+            meet();                                          // (and nobody is with the last tile's factors any more)
+            const int refs_here[2] = {static_cast<int>(max(max(warp_top[0], warp_top[1]), 10u)), static_cast<int>(max(max(warp_top[2], warp_top[3]), 10u))};
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const int e = static_cast<int>(scale[g]) - refs_here[side] + kCodeLift + 15;
+                factors[side][own_row][g] = static_cast<uint32_t>(max(e, 0)) * 0x04000400u;
+            }
+            ok = ok && room(2 * i);                          // (the references of kTileRefs tiles ago have been read by then)
+            if (ok && dt == 0) refs[i % kTileRefs] = make_int2(refs_here[0], refs_here[1]);
+            meet();
+            if (ok) decode(2 * i, masked, j0, there);
+            ok = ok && codes_there(2 * i + 1) && room(2 * i + 1);
+            if (ok) decode(2 * i + 1, masked, j0, there);
+        }
+    } else if (warp == Sh::kIssues && n > 0) {
+        const uint32_t idesc_s = idesc_16<true>(kKeys), idesc_o = idesc_16<true>(D) | kRowsAreContraction;
+        const bool one = elect_one();
+        const auto fence = [] { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); };
+        const auto scores = [&](int i) {                     // S of tile i; its keys' stage is free when it is there
+            const int st = 2 * i % ST;
+#pragma unroll
+            for (int b = 0; b < Sh::kDB; ++b)
+                umma_box(2, tmem + (i & 1) * kKeys, smem_desc_sw128(q_at + b * kRows * 128), smem_desc_sw128(kv_at + st * Sh::kStage + b * kKeys * 128), idesc_s, min(4, D / 16 - 4 * b), b > 0);
+            umma_commit(s_full + 8 * (i & 1));
+            umma_commit(empty(st));
+        };
+        bool ok = guard.wait_all(q_full, 0) && guard.wait_all(full(0), 0);
+        if (ok && one) {
+            fence();
+            tc_fence_after();
+            scores(0);
+        }
+        __syncwarp();
+        for (int i = 0; i < n && ok; ++i) {
+            if (i + 1 < n) {
+                ok = guard.wait_all(full((2 * i + 2) % ST), (2 * i + 2) / ST & 1);
+                if (ok && one) {
+                    fence();
+                    tc_fence_after();
+                    scores(i + 1);
+                }
+                __syncwarp();
+            }
+            const int c = 2 * i + 1, st = c % ST;
+            ok = ok && guard.wait_all(full(st), c / ST & 1) && guard.wait_all(p_full + 8 * (i & 1), i / 2 & 1);
+            if (ok && one) {
+                fence();
+                tc_fence_after();
+                for (int k = 0; k < kKeys / 16; ++k)
+                    umma_bf16_ts(tmem + Sh::kO, tmem + (i & 1) * kKeys + 8 * k, smem_desc_rows_sw128(kv_at + st * Sh::kStage + k * 2048, kKeys * 128), idesc_o, i > 0 || k > 0);
+                umma_commit(o_step);
+                umma_commit(empty(st));
+            }
+            __syncwarp();
+        }
+        if (one) umma_commit(ok ? o_full : ended);
+        __syncwarp();
+        guard.settle(ok ? o_full : ended, 0);                // (whoever else gave up, the tensor memory is not given back under an MMA)
+    } else if (warp < 4) {
+        // ---- softmax, a thread per row
+        const int i_row = q0 + t / a.pack, head = head0 + t % a.pack;
+        const bool mine = t < per * a.pack && i_row < s.n_q;
+        const int p = mine ? query_pos(a, s, len, i_row) : -1;
+        float q_scale = a.scale_log2 * two_to(-kCodeLift);   // of the scores, less the tile's
+        if (n > 0) {                                         // this row's queries, in fp16
+            const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.q) + ((s.q_row + i_row) * a.n_heads + head) * D;
+            uint32_t top = 0;
+            if (mine) {
+#pragma unroll
+                for (int c = 0; c < D; c += 8) {
+                    const uint4 w = *reinterpret_cast<const uint4*>(q + c);
+                    constexpr uint32_t m = 0x7FFF7FFFu;
+                    top = __vmaxu2(top, __vmaxu2(__vmaxu2(w.x & m, w.y & m), __vmaxu2(w.z & m, w.w & m)));
+                }
+            }
+            top = max(top & 0xFFFFu, top >> 16);
+            const int e = top ? min(max(14 - (static_cast<int>(top >> 7) - 127), -113), 126) : 0;      // (2^126 times the smallest ones at most)
+            const float lift = two_to(e);
+            q_scale *= two_to(-e);
+#pragma unroll 4
+            for (int c = 0; c < D; c += 8) {
+                uint4 w = make_uint4(0, 0, 0, 0);
+                if (mine) w = *reinterpret_cast<const uint4*>(q + c);
+                uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[i] = two_f16(__uint_as_float(x[i] << 16) * lift, __uint_as_float(x[i] & 0xFFFF0000u) * lift);
+                store16(q_at + swizzled(t, c / 8, kRows), x);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(q_full);
+        }
+        const uint32_t lanes = static_cast<uint32_t>(warp) << 21;            // this warp's 32 lanes
+        const uint32_t o_col = tmem + Sh::kO + lanes;
+        float m = -CUDART_INF_F, l = 0.f;                    // reference (scaled), sum (of weights against the reference less kF16Lift)
+        int unit = 0;                                        // byte of the scale that O is counted in
+        bool masked = false;
+        uint32_t visible[kKeys / 32];                        // a bit for every key of the tile that the row sees
+        const auto look = [&](int i) {
+            const int j0 = first_key(i);
+            masked = masks(j0);
+            if (!masked) return;
+            const int past = min(p, len - 1) - j0 + 1, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
+#pragma unroll
+            for (int w = 0; w < kKeys / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
+        };
+        const auto scores_there = [&](int i) { return guard.wait_all(s_full + 8 * (i & 1), i / 2 & 1); };
+        const auto weigh = [&](int i) {
+            const int buf = i & 1;
+            tc_fence_after();
+            const int2 ref_of = refs[i % kTileRefs];
+            const float scale = q_scale * two_to(ref_of.x - 127);
+            const uint32_t s_col = tmem + buf * kKeys + lanes;
+            float top;
+            {
+                float x[kKeys];
+                tmem_ld_cols<kKeys>(s_col, x);
+                if (masked) {
+#pragma unroll
+                    for (int c = 0; c < kKeys; ++c) x[c] = visible[c / 32] >> (c & 31) & 1u ? x[c] : -CUDART_INF_F;
+                }
+                float tops[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                for (int c = 4; c < kKeys; c += 8) {         // (three at a time)
+#pragma unroll
+                    for (int b = 0; b < 4; ++b) tops[b] = c + 4 + b < kKeys ? fmaxf(fmaxf(tops[b], x[c + b]), x[c + 4 + b]) : fmaxf(tops[b], x[c + b]);
+                }
+                top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+            }
+            top *= scale;                                    // (scale is positive)
+            const bool move = top > m + kMoveAt;
+            if (i == 0) unit = min(ref_of.y + 2, 253);
+            const bool larger = ref_of.y > unit;             // (of all rows alike)
+            if (i > 0 && (larger || __any_sync(0xffffffffu, move))) {
+                // (the step before may still be adding; the one before that was complete before this S was)
+                if (!guard.wait_all(o_step, (i - 1) & 1)) return false;
+                tc_fence_after();
+                const float f = move ? ex2_approx(m - top) : 1.f, by = larger ? f * two_to(max(unit - ref_of.y, -126)) : f;
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    float o[32];
+                    uint32_t w[32];
+                    tmem_ld_cols<32>(o_col + c, o);
+#pragma unroll
+                    for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(o[k] * by);
+                    tmem_st_cols<32>(o_col + c, w);
+                }
+                l *= f;
+            }
+            if (larger) unit = ref_of.y;
+            if (move) m = top;
+            const int down = min(unit - ref_of.y, 64);       // this tile's values are counted in units 2^down larger than their own (more than 64: nothing is left of them)
+            const float ref = m == -CUDART_INF_F ? 0.f : m - kF16Lift + static_cast<float>(down);
+            const uint64_t scale2 = two_f32(scale, scale), ref2 = two_f32(-ref, -ref);
+            uint64_t sums[2] = {0, 0};
+#pragma unroll
+            for (int c0 = 0; c0 < kKeys; c0 += 32) {
+                float x[32];
+                uint32_t w[16];
+                tmem_ld_cols<32>(s_col + c0, x);
+                if (masked) {
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) x[c] = visible[c0 / 32] >> c & 1u ? x[c] : -CUDART_INF_F;
+                }
+#pragma unroll
+                for (int c = 0; c < 32; c += 2) {
+                    float y, z;
+                    split_f32(fma_f32x2(two_f32(x[c], x[c + 1]), scale2, ref2), y, z);
+                    y = ex2_approx(y);
+                    z = ex2_approx(z);
+                    sums[c / 2 & 1] = add_f32x2(sums[c / 2 & 1], two_f32(y, z));
+                    w[c / 2] = two_f16(y, z);                // (rounded for the product alone)
+                }
+                tmem_st_cols<16>(s_col + c0 / 2, w);
+            }
+            float even, odd;
+            split_f32(add_f32x2(sums[0], sums[1]), even, odd);
+            l = fmaf(even + odd, two_to(down), l);
+            tmem_st_wait();
+            tc_fence_before();
+            mbar_arrive(p_full + 8 * buf);
+            return true;
+        };
+        bool ok = walk_tiles(0, n, 1, look, scores_there, weigh);
+        // ---- the rows
+        if (ok && n > 0) ok = guard.wait_all(o_full, 0);
+        tc_fence_after();
+        const int64_t part = s.part0 + static_cast<int64_t>(piece_of_seq) * s.n_q + i_row;
+        const float by = (l > 0.f ? two_to(unit - 127) * (s.parts > 1 ? 1.f : 1.f / l) : 0.f) * two_to(-kCodeLift);
+        m -= kF16Lift;
+        for (int c = 0; c < D && ok; c += 32) {
+            float o[32];
+            if (n > 0) tmem_ld_cols<32>(o_col + c, o);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? o[k] * by : 0.f;
+            if (!mine) continue;
+            if (s.parts > 1) {
+                float* const dst = a.part_o + (part * a.n_heads + head) * D + c;
+#pragma unroll
+                for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(dst + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
+            } else {
+                __nv_bfloat16* const dst = static_cast<__nv_bfloat16*>(a.out) + ((s.q_row + i_row) * a.n_heads + head) * D + c;
+#pragma unroll
+                for (int k = 0; k < 32; k += 8) store8(dst + k, o + k);
+            }
+        }
+        if (mine && ok) {
+            if (s.parts > 1) a.part_ml[part * a.n_heads + head] = make_float2(m, l);
+            else if (a.lse) a.lse[(s.q_row + i_row) * a.n_heads + head] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
+        }
+        tc_fence_before();
+    }
+    __syncthreads();
+    if (warp == Sh::kIssues) {
+        tc_fence_after();
+        tmem_dealloc(tmem, Sh::kColumns);
+    }
+}
+
+template <int KIND, int D32>
+cudaError_t attend(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
+{
+    static KernelSetup setup;
+    using Sh = PageTileShape<KIND, D32>;
+    const size_t smem = smem_for_tmem(Sh::kSmem, Sh::kColumns);              // (no CTA more than there is tensor memory for)
+    const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(page_tile_kernel<KIND, D32>), smem, Sh::kColumns);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack));
+    cfg.blockDim = dim3(Sh::kWarps * 32);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, page_tile_kernel<KIND, D32>, a, pool);
+}
+template <int KIND>
+cudaError_t by_dim(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
+{
+    switch (a.head_dim / 32) {
+    case 2: return attend<KIND, 2>(a, pool, stream);
+    case 3: return attend<KIND, 3>(a, pool, stream);
+    case 4: return attend<KIND, 4>(a, pool, stream);
+    case 5: return attend<KIND, 5>(a, pool, stream);
+    case 6: return attend<KIND, 6>(a, pool, stream);
+    case 7: return attend<KIND, 7>(a, pool, stream);
+    default: return attend<KIND, 8>(a, pool, stream);
+    }
+}
+
+}  // namespace
+
+cudaError_t launch_page_decode(int kind, const AttArgs& a, const PagePool& pool, cudaStream_t stream)
+{
+    return kind == MVLA_PAGE_E4M3 ? by_dim<MVLA_PAGE_E4M3>(a, pool, stream) : by_dim<MVLA_PAGE_E2M1>(a, pool, stream);
+}
+
+}  // namespace mvla
