@@ -115,12 +115,14 @@ def attention(pool, kind, seqs, table, q, P, window=None, n_sink=0, scale=0.0, k
 
 
 def tolerance(r, d, dtype, kind, tokens):
-    """out: as serve_util.attention_tolerance (sums, exponentials, what a weight meets the values in).  Tokens over quantised pages: weights
+    """`tokens`: the call has at most 16 query rows to a key head.  out: as serve_util.attention_tolerance (sums, exponentials, what a weight meets the values in).  Tokens over quantised pages: weights
     times scales in fp16, half a step relative, and where that type has no normal number left 2^-25 in units of 2^-7 of the largest such product, times a
     code: keys 2^-31 of the largest value; e2m1 values below 2^-27 of their row's largest scale are nothing (six times that, 2^-24 of the
     largest value at most, with 6 the largest code, and keys whose scores shift as much are inside the logits' error where the data is even)."""
-    if dtype == torch.float32 or not tokens or kind == ROWS:
+    if dtype == torch.float32 or kind == ROWS:
         return U.attention_tolerance(r, d, dtype)
+    if not tokens:                                             # (fp16 or bf16 weights: the coarser; units up to four times the largest values seen)
+        return U.attention_tolerance(r, d, dtype) + r["keys"] * 2.0 ** -29 * r["largest"]
     per_weight = 2 * U.logit_error(r["reach"], d) + 2.0 ** -20 + 2 * r["keys"] * 2.0 ** -24 + U.HALF[torch.float16]
     own = per_weight[..., None] * r["weight"] + r["keys"] * 2.0 ** -31 * r["largest"]
     if kind == E2M1:
