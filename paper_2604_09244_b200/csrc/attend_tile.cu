@@ -65,7 +65,7 @@ constexpr int kTwin = 32;                    // (a warp's lanes)
 static_assert(kTokenRows <= kTwin, "the rows of a warp");
 
 // PAGED: keys and values lie in pages (a tile is the rows of one, or of several side by side), positions are counted, and every sequence is cut into parts
-// of its own number: a.n_blocks counts its blocks of queries times its parts.
+// of its own number: a.n_blocks counts its blocks of queries times its parts.  A part is a cluster's, whose CTAs join their sums through shared memory.
 template <bool F16, int DB, bool TOKENS, bool PAGED>
 __global__ void __launch_bounds__(TileShape<DB>::kWarps * 32, TileShape<DB>::kCtas)
 attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
@@ -80,6 +80,8 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     __shared__ uint32_t seen_by[4][4][kKeys / 32];           // of the last tiles: the keys that some row of a warp sees
     __shared__ int n_list, dead;
     __shared__ uint32_t tmem_base;
+    __shared__ float2 row_ml[PAGED ? kRows : 1];
+    static_assert(ST * Sh::kStage >= DB * 64 * kRows * 4, "room for the sums of a cluster's CTA");
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t q_at = base, kv_at = base + Sh::kQBytes;
     const uint32_t bar0 = smem_u32(bars);
@@ -111,10 +113,12 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     // (only now: what holds tensor memory ahead of this kernel in the stream is complete, and nothing that holds some waits for this CTA)
     if (warp == Sh::kIssues) tmem_alloc(smem_u32(&tmem_base), Sh::kColumns);
     // the block: the last ones, which see most keys, first
-    const int heads = a.n_heads / a.pack, blk = a.n_blocks - 1 - static_cast<int>(blockIdx.x) / heads, head0 = static_cast<int>(blockIdx.x) % heads * a.pack;
+    const int ranks = PAGED ? cluster_ctas() : 1, cta = static_cast<int>(blockIdx.x) / ranks;
+    const int heads = a.n_heads / a.pack, blk = a.n_blocks - 1 - cta / heads, head0 = cta % heads * a.pack;
     const AttSeq& s = a.s[seq_of_block(a, blk)];
     const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack;      // queries of the tile
-    const int parts = PAGED ? s.parts : a.splits, piece = PAGED ? (blk - s.blk0) % s.parts : static_cast<int>(blockIdx.y);
+    const int part_of_seq = PAGED ? (blk - s.blk0) % s.parts : static_cast<int>(blockIdx.y);       // (pages: a cluster's)
+    const int parts = PAGED ? s.parts * ranks : a.splits, piece = PAGED && ranks > 1 ? part_of_seq * ranks + static_cast<int>(cluster_ctarank()) : part_of_seq;
     const int q0 = (PAGED ? (blk - s.blk0) / s.parts : blk - s.blk0) * per, len = seq_len(a, s);
     const bool twins = TOKENS && static_cast<int64_t>(s.n_q) * (a.n_heads / a.kv_heads) <= kTokenRows;
     int lo, hi;
@@ -403,11 +407,13 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         // ---- the rows
         if (ok && n > 0) ok = guard.wait_all(o_full, 0);
         tc_fence_after();
-        const int64_t part = s.part0 + static_cast<int64_t>(piece) * s.n_q + i_row;
+        const int64_t part = s.part0 + static_cast<int64_t>(part_of_seq) * s.n_q + i_row;
+        const bool joined = PAGED && ranks > 1, split = PAGED ? s.parts > 1 : a.splits > 1;
         const float inv = l > 0.f ? 1.f / l : 0.f;
         m -= kLift;
+        float* const sums = reinterpret_cast<float*>(raw + (kv_at - smem_u32(raw)));      // of a cluster's CTA: element by element, the rows side by side
         // the twins' rows of O, for the others (the keys and values have been read): element by element, the rows side by side
-        float* const beside = reinterpret_cast<float*>(raw + (kv_at - smem_u32(raw)));
+        float* const beside = reinterpret_cast<float*>(raw + ((PAGED ? q_at : kv_at) - smem_u32(raw)));
         if (TOKENS && twins && t < 2 * kTwin) {
             if (twin && ok && n > 0) {
                 for (int c = 0; c < a.head_dim; c += 32) {
@@ -427,9 +433,14 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                 for (int k = 0; k < 32; ++k) o[k] += beside[(c + k) * kTwin + r];
             }
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? (parts > 1 ? o[k] : o[k] * inv) : 0.f;
+            for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? (joined || split ? o[k] : o[k] * inv) : 0.f;
+            if (joined) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) sums[(c + k) * kRows + t] = o[k];
+                continue;
+            }
             if (!mine) continue;
-            if (parts > 1) {
+            if (split) {
                 float* const dst = a.part_o + (part * a.n_heads + head) * a.head_dim + c;
 #pragma unroll
                 for (int k = 0; k < 32; k += 4) *reinterpret_cast<float4*>(dst + k) = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
@@ -439,8 +450,9 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                 for (int k = 0; k < 32; k += 8) store8(dst + k, o + k);
             }
         }
-        if (mine && ok && !twin) {
-            if (parts > 1) {
+        if (joined) row_ml[t] = make_float2(m, l);
+        if (mine && ok && !twin && !joined) {
+            if (split) {
                 a.part_ml[part * a.n_heads + head] = make_float2(m, l);
             } else {
                 const float z = l > 0.f ? m + log2f(l) : -CUDART_INF_F;
@@ -451,6 +463,13 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         tc_fence_before();
     }
     __syncthreads();
+    if (PAGED && ranks > 1) {                                // (reached by all CTAs of the cluster, whoever gave up)
+        cluster_arrive_release();
+        cluster_wait_acquire();
+        if (t < kRows) join_cluster(a, s, kv_at, smem_u32(row_ml), ranks, t, q0, per, head0, part_of_seq);
+        cluster_arrive_release();                            // (nobody's sums are gone while another reads them)
+        cluster_wait_acquire();
+    }
     if (warp == Sh::kIssues) {
         tc_fence_after();
         tmem_dealloc(tmem, Sh::kColumns);
@@ -687,7 +706,7 @@ attend_weights_kernel(const __grid_constant__ AttArgs a, const __grid_constant__
 }
 
 template <class K>
-cudaError_t launch(KernelSetup& setup, K kernel, dim3 grid, int threads, int columns, size_t smem, const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
+cudaError_t launch(KernelSetup& setup, K kernel, dim3 grid, int threads, int columns, size_t smem, const AttArgs& a, const AttMaps& maps, cudaStream_t stream, int cluster = 1)
 {
     smem = smem_for_tmem(smem, columns);                     // (no CTA more than there is tensor memory for)
     const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(kernel), smem, columns);
@@ -697,9 +716,12 @@ cudaError_t launch(KernelSetup& setup, K kernel, dim3 grid, int threads, int col
     cfg.blockDim = dim3(static_cast<unsigned>(threads));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cudaLaunchAttribute attr[2] = {pdl_attribute(), {}};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kernel, a, maps.q, maps.k, maps.v);
 }
 
@@ -707,9 +729,10 @@ template <bool F16, int DB, bool TOKENS, bool PAGED>
 cudaError_t attend(const AttArgs& a, const AttMaps& maps, cudaStream_t stream)
 {
     static KernelSetup setup;
-    const dim3 grid(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack), PAGED ? 1u : static_cast<unsigned>(a.splits));
+    const int cluster = PAGED ? a.cluster : 1;
+    const dim3 grid(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack) * static_cast<unsigned>(cluster), PAGED ? 1u : static_cast<unsigned>(a.splits));
     using Sh = TileShape<DB>;
-    return launch(setup, attend_tile_kernel<F16, DB, TOKENS, PAGED>, grid, Sh::kWarps * 32, Sh::kColumns, Sh::kSmem, a, maps, stream);
+    return launch(setup, attend_tile_kernel<F16, DB, TOKENS, PAGED>, grid, Sh::kWarps * 32, Sh::kColumns, Sh::kSmem, a, maps, stream, cluster);
 }
 
 template <bool F16, int DB>

@@ -136,4 +136,78 @@ struct Guard {
     }
 };
 
+// ---- parts of a block of rows joined inside a cluster
+
+__device__ __forceinline__ int cluster_ctas()
+{
+    int n;
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
+    return n;
+}
+// From the shared memory of CTA `rank` of this cluster, at the offset of `addr`.
+__device__ __forceinline__ float2 ld_peer2(uint32_t addr, int rank)
+{
+    uint32_t remote;
+    float2 x;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(remote) : "memory");
+    return x;
+}
+__device__ __forceinline__ float ld_peer(uint32_t addr, int rank)
+{
+    uint32_t remote;
+    float x;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(remote) : "memory");
+    return x;
+}
+// By 128 threads of every CTA of a cluster (a barrier of the cluster before and behind): the sums of the block's rows, [head_dim][128] at `sums`, and their references
+// and sums of exponentials, [128] at `ml`, of all its CTAs.  A CTA joins a share of the rows, a thread one row's pieces of eight elements, in the CTAs' order.
+__device__ __forceinline__ void join_cluster(const AttArgs& a, const AttSeq& s, uint32_t sums, uint32_t ml, int ranks, int t, int q0, int per, int head0, int part)
+{
+    const int rows = kRows / ranks, row = static_cast<int>(cluster_ctarank()) * rows + t % rows, i_row = q0 + row / a.pack, head = head0 + row % a.pack;
+    if (row >= per * a.pack || i_row >= s.n_q) return;
+    float2 z[kMaxCluster];
+#pragma unroll
+    for (int k = 0; k < kMaxCluster; ++k)
+        if (k < ranks) z[k] = ld_peer2(ml + 8u * row, k);
+    float m = -CUDART_INF_F, l = 0.f, f[kMaxCluster];
+#pragma unroll
+    for (int k = 0; k < kMaxCluster; ++k)
+        if (k < ranks) m = fmaxf(m, z[k].x);
+    const float ref = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+    for (int k = 0; k < kMaxCluster; ++k) {
+        f[k] = k < ranks ? exp2f(z[k].x - ref) : 0.f;
+        if (k < ranks) l = fmaf(z[k].y, f[k], l);
+    }
+    const bool whole = s.parts == 1;
+    const float by = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
+    const int64_t at = whole ? (s.q_row + i_row) * a.n_heads + head : (s.part0 + static_cast<int64_t>(part) * s.n_q + i_row) * a.n_heads + head;
+    for (int piece = t / rows; piece < a.head_dim / 8; piece += ranks) {
+        float o[8] = {};
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k) {
+            if (k >= ranks) break;
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = ld_peer(sums + 4u * ((piece * 8 + e) * kRows + row), k);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = fmaf(x[e], f[k], o[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] *= by;
+        if (whole) {
+            store8(static_cast<__nv_bfloat16*>(a.out) + at * a.head_dim + piece * 8, o);
+        } else {
+            float* const dst = a.part_o + at * a.head_dim + piece * 8;
+            *reinterpret_cast<float4*>(dst) = make_float4(o[0], o[1], o[2], o[3]);
+            *reinterpret_cast<float4*>(dst + 4) = make_float4(o[4], o[5], o[6], o[7]);
+        }
+    }
+    if (t >= rows) return;
+    if (!whole) a.part_ml[at] = make_float2(m, l);
+    else if (a.lse) a.lse[at] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
+}
+
 }  // namespace mvla

@@ -225,16 +225,18 @@ inline AttendPlan plan_tokens(const ServeShape& c, int32_t batch, const mvla_seq
     return p;
 }
 
-// Blocks of queries by tiles of 128 rows, every sequence's keys cut into parts of about the same length over the whole batch (a multiple of 64, at least
-// 256 keys), so that their CTAs fill whole rounds of those that fit: of one to four rounds, or no cut at all, what ends first.  In tiles of a CTA (1.3 us with
-// another one beside it): its longest part and 4 for its start and end; 4 for the join, and what the parts' sums, written and read, take at 6 TB/s.
-inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink)
+// Blocks of queries by tiles of 128 rows, every sequence's keys cut into parts (clusters of 1, 2, 4 or 8 CTAs) of about the same length over the whole batch (a
+// multiple of 64 keys to a CTA, at least 128), so that their CTAs fill whole rounds of those that fit: of one to four rounds, or no cut at all, what ends
+// first.  In us: the tiles of its longest part and 4 for its start and end, `tile` each (with another CTA beside it); 1 where a cluster joins; 5 for the kernel that joins
+// parts, and what their sums, written and read, take at 6 TB/s.
+constexpr double kTileUs = 1.3, kUnpackedTileUs = 2.2;
+inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, double tile)
 {
     AttendPlan p;
     p.form = kFormPageTile;
     p.pack = pack_of(c.n_heads / c.kv_heads);
     p.queries = 128 / p.pack;
-    const int64_t packs = c.n_heads / p.pack, slots = (c.head_dim <= 128 ? 2 : 1) * static_cast<int64_t>(c.sm_count);
+    const int64_t packs = c.n_heads / p.pack, each = c.head_dim <= 128 ? 2 : 1, slots = each * static_cast<int64_t>(c.sm_count);
     int64_t work = 0, longest = 1;
     const auto blocks_of = [&](const mvla_seq& s) { return (static_cast<int64_t>(s.n_q) + p.queries - 1) / p.queries; };
     for (int b = 0; b < batch; ++b) {
@@ -246,31 +248,39 @@ inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla
         longest = std::max(longest, keys);
     }
     int64_t ctas = 0, part_q = 0;
-    const auto cut = [&](int64_t part) {
-        p.part_keys = part;
-        ctas = part_q = 0;
+    const auto cut = [&](int cluster, int64_t part) {        // `part` keys to a CTA
+        p.cluster = cluster;
+        p.part_keys = part * cluster;
+        p.blocks = part_q = 0;
         p.splits = 1;
         for (int b = 0; b < batch; ++b) {
             const int32_t n = parts_of(p, seqs[b], counted, window, n_sink);
-            ctas += blocks_of(seqs[b]) * n * packs;
+            p.blocks += blocks_of(seqs[b]) * n;
             part_q += static_cast<int64_t>(seqs[b].n_q) * n;
             p.splits = std::max(p.splits, n);
         }
+        ctas = p.blocks * packs * cluster;
     };
     int64_t best = 0;
+    int best_cluster = 1;
     double best_cost = 0;
-    for (int rounds = 0; rounds <= 4; ++rounds) {
-        int64_t part = rounds ? (work + rounds * slots - 1) / (rounds * slots) : longest;
-        part = std::max<int64_t>({part, 256, (longest + 63) / 64});
-        part = (part + 63) / 64 * 64;
-        cut(part);
-        for (int tries = 0; rounds && ctas > rounds * slots && part < longest && tries < 16; ++tries) cut(part += std::max<int64_t>(64, part / 16 / 64 * 64));
-        const double join = p.splits > 1 ? 4.0 + static_cast<double>(part_q) * c.n_heads * c.head_dim * 8 / 8e6 : 0.0;
-        const double cost = static_cast<double>((ctas + slots - 1) / slots) * (static_cast<double>(std::min(part, longest)) / 64 + 4) + join;
-        if (!best || cost < best_cost) { best = part; best_cost = cost; }
+    for (int cluster = 1; cluster <= 8; cluster *= 2) {
+        // (a cluster lies inside a group of multiprocessors, whose number need not divide)
+        const int lost = cluster == 1 ? 0 : cluster == 2 ? 3 : cluster == 4 ? (each == 2 ? 6 : 11) : each == 2 ? 10 : 19;
+        const int64_t at_once = slots - slots * lost / 100;
+        for (int rounds = 0; rounds <= 4; ++rounds) {
+            int64_t part = rounds ? (work + rounds * at_once - 1) / (rounds * at_once) : (longest + cluster - 1) / cluster;
+            part = std::max<int64_t>({part, 128, (longest + 64 * cluster - 1) / (64 * cluster)});
+            part = (part + 63) / 64 * 64;
+            cut(cluster, part);
+            for (int tries = 0; rounds && ctas > rounds * at_once && part * cluster < longest && tries < 16; ++tries) cut(cluster, part += std::max<int64_t>(64, part / 16 / 64 * 64));
+            const double join = (cluster > 1 ? 1.0 : 0.0) + (p.splits > 1 ? 5.0 + static_cast<double>(part_q) * c.n_heads * c.head_dim * 8 / 6e6 : 0.0);
+            const double mine = static_cast<double>(std::min(part, (longest + cluster - 1) / cluster));
+            const double cost = static_cast<double>((ctas + at_once - 1) / at_once) * (mine / 64 + 4) * tile + join;
+            if (!best || cost < best_cost) { best = part; best_cost = cost; best_cluster = cluster; }
+        }
     }
-    cut(best);
-    for (int b = 0; b < batch; ++b) p.blocks += blocks_of(seqs[b]) * parts_of(p, seqs[b], counted, window, n_sink);
+    cut(best_cluster, best);
     if (p.splits > 1) {
         Workspace w;
         p.part_o = w.take(part_q * c.n_heads * c.head_dim * static_cast<int64_t>(sizeof(float)));
@@ -292,10 +302,11 @@ inline bool page_by_tokens(int kind, int64_t rows, int64_t keys_and_heads)
 // Whether so few blocks of queries go over a sequence's pages that each had better unpack them for itself: unpacking first costs 0.15 us for 1000 rows of a head (their
 // bytes, twice), on the way 0.06 us for every block that does.  us, on the way / first, 32 heads in groups of 4, e4m3: 5 tokens over 60000 rows (a block) 61 / 121;
 // 4 chunks of 56 over 2000 to 6000 (two) 52 / 57, of 33 over 4000 (two) 48 / 51; 100 over 4096 (four) 36 / 31; 512 over 8192 (16) 141 / 98.
-inline bool unpacks_on_the_way(const AttendPlan& p, int32_t batch, const mvla_seq* seqs)
+inline bool unpacks_on_the_way(const ServeShape& c, int32_t batch, const mvla_seq* seqs)
 {
+    const int64_t queries = 128 / pack_of(c.n_heads / c.kv_heads);
     int64_t most = 0;
-    for (int b = 0; b < batch; ++b) most = std::max(most, (static_cast<int64_t>(seqs[b].n_q) + p.queries - 1) / p.queries);
+    for (int b = 0; b < batch; ++b) most = std::max(most, (static_cast<int64_t>(seqs[b].n_q) + queries - 1) / queries);
     return most <= 2;
 }
 
@@ -326,15 +337,12 @@ inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, co
     int64_t keys = 0;
     for (int b = 0; b < batch; ++b) keys += seqs[b].n_q ? visible_keys(seqs[b], counted, a->window, a->n_sink) : 0;
     const bool tokens = h.dtype != MVLA_DTYPE_FP32 && page_by_tokens(a->pages.kind, most_rows, keys * v.kv_heads);
+    p.unpack = h.dtype != MVLA_DTYPE_FP32 && a->pages.kind != MVLA_PAGE_ROWS && !tokens && unpacks_on_the_way(h, batch, seqs);
     p.attend = h.dtype == MVLA_DTYPE_FP32 ? plan_page_fma(h, batch, seqs, counted, a->window, a->n_sink)
              : tokens ? plan_tokens(h, batch, seqs, counted, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32))
-                      : plan_page_tiles(h, batch, seqs, counted, a->window, a->n_sink);
+                      : plan_page_tiles(h, batch, seqs, counted, a->window, a->n_sink, p.unpack ? kUnpackedTileUs : kTileUs);
     p.bytes = p.attend.bytes;
-    if (a->pages.kind == MVLA_PAGE_ROWS || tokens) return p;
-    if (p.attend.form == kFormPageTile && unpacks_on_the_way(p.attend, batch, seqs)) {
-        p.unpack = true;
-        return p;
-    }
+    if (a->pages.kind == MVLA_PAGE_ROWS || tokens || p.unpack) return p;
     Workspace w;
     w.take(p.attend.bytes);
     for (int b = 0; b < batch; ++b) p.dense_tiles += seen_tiles(seqs[b], a->window, a->n_sink);

@@ -74,6 +74,8 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
     __shared__ int2 refs[kTileRefs];                         // bytes of the largest scales of a tile's keys and values
     __shared__ int dead;
     __shared__ uint32_t tmem_base;
+    __shared__ float2 row_ml[kRows];
+    static_assert(Sh::kSmem - 1024 >= D * kRows * 4, "room for the sums of a cluster's CTA");
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t q_at = base, kv_at = base + Sh::kQBytes;
     const uint32_t bar0 = smem_u32(bars);
@@ -102,13 +104,15 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
     pdl_wait();
     // (only now: what holds tensor memory ahead of this kernel in the stream is complete, and nothing that holds some waits for this CTA)
     if (warp == Sh::kIssues) tmem_alloc(smem_u32(&tmem_base), Sh::kColumns);
-    const int heads = a.n_heads / a.pack, blk = a.n_blocks - 1 - static_cast<int>(blockIdx.x) / heads, head0 = static_cast<int>(blockIdx.x) % heads * a.pack;
+    const int ranks = cluster_ctas(), cta = static_cast<int>(blockIdx.x) / ranks;
+    const int heads = a.n_heads / a.pack, blk = a.n_blocks - 1 - cta / heads, head0 = cta % heads * a.pack;
     const AttSeq& s = a.s[seq_of_block(a, blk)];
     const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack;      // queries of the tile
-    const int piece_of_seq = (blk - s.blk0) % s.parts, q0 = (blk - s.blk0) / s.parts * per, len = seq_len(a, s);
+    const int part_of_seq = (blk - s.blk0) % s.parts, parts = s.parts * ranks, piece_of_seq = ranks > 1 ? part_of_seq * ranks + static_cast<int>(cluster_ctarank()) : part_of_seq;
+    const int q0 = (blk - s.blk0) / s.parts * per, len = seq_len(a, s);
     const int lo = query_pos(a, s, len, q0), hi = query_pos(a, s, len, min(q0 + per, s.n_q) - 1);
     const TileRange range = tile_range(a, len, lo, hi, kKeys);
-    const int per_part = (range.count + s.parts - 1) / s.parts, v0 = piece_of_seq * per_part, n = max(0, min(range.count - v0, per_part));
+    const int per_part = (range.count + parts - 1) / parts, v0 = piece_of_seq * per_part, n = max(0, min(range.count - v0, per_part));
     const auto first_key = [&](int i) { return range.tile(v0 + i) * kKeys; };
     const auto masks = [&](int j0) {                         // whether some row does not see some key of a tile
         return span_flags(a, lo, hi, counted_span(len, j0, kKeys)) != kNeed;
@@ -400,14 +404,20 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         // ---- the rows
         if (ok && n > 0) ok = guard.wait_all(o_full, 0);
         tc_fence_after();
-        const int64_t part = s.part0 + static_cast<int64_t>(piece_of_seq) * s.n_q + i_row;
-        const float by = (l > 0.f ? two_to(unit - 127) * (s.parts > 1 ? 1.f : 1.f / l) : 0.f) * two_to(-kCodeLift);
+        const int64_t part = s.part0 + static_cast<int64_t>(part_of_seq) * s.n_q + i_row;
+        float* const sums = reinterpret_cast<float*>(raw + (q_at - smem_u32(raw)));       // of a cluster's CTA: element by element, the rows side by side
+        const float by = (l > 0.f ? two_to(unit - 127) * (s.parts > 1 || ranks > 1 ? 1.f : 1.f / l) : 0.f) * two_to(-kCodeLift);
         m -= kF16Lift;
         for (int c = 0; c < D && ok; c += 32) {
             float o[32];
             if (n > 0) tmem_ld_cols<32>(o_col + c, o);
 #pragma unroll
             for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? o[k] * by : 0.f;
+            if (ranks > 1) {
+#pragma unroll
+                for (int k = 0; k < 32; ++k) sums[(c + k) * kRows + t] = o[k];
+                continue;
+            }
             if (!mine) continue;
             if (s.parts > 1) {
                 float* const dst = a.part_o + (part * a.n_heads + head) * D + c;
@@ -419,13 +429,21 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                 for (int k = 0; k < 32; k += 8) store8(dst + k, o + k);
             }
         }
-        if (mine && ok) {
+        if (ranks > 1) row_ml[t] = make_float2(m, l);
+        if (mine && ok && ranks == 1) {
             if (s.parts > 1) a.part_ml[part * a.n_heads + head] = make_float2(m, l);
             else if (a.lse) a.lse[(s.q_row + i_row) * a.n_heads + head] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
         }
         tc_fence_before();
     }
     __syncthreads();
+    if (ranks > 1) {                                         // (reached by all CTAs of the cluster, whoever gave up)
+        cluster_arrive_release();
+        cluster_wait_acquire();
+        if (t < kRows) join_cluster(a, s, q_at, smem_u32(row_ml), ranks, t, q0, per, head0, part_of_seq);
+        cluster_arrive_release();                            // (nobody's sums are gone while another reads them)
+        cluster_wait_acquire();
+    }
     if (warp == Sh::kIssues) {
         tc_fence_after();
         tmem_dealloc(tmem, Sh::kColumns);
@@ -441,13 +459,16 @@ cudaError_t attend(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
     const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(page_tile_kernel<KIND, D32>), smem, Sh::kColumns);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack));
+    cfg.gridDim = dim3(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack) * static_cast<unsigned>(a.cluster));
     cfg.blockDim = dim3(Sh::kWarps * 32);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1] = {pdl_attribute()};
+    cudaLaunchAttribute attr[2] = {pdl_attribute(), {}};
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = static_cast<unsigned>(a.cluster);
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = a.cluster > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, page_tile_kernel<KIND, D32>, a, pool);
 }
 template <int KIND>

@@ -13,7 +13,7 @@
 // parts, what the type holds and what it leaves; fp16 ones are one part, in units of 2^-kF16Lift of their reference.
 //   A sequence's visible keys are cut into parts of about the same length over the whole batch; a CTA is four warps that take the part's tiles in turn.  The
 // parts of a cluster are joined through its shared memory, and clusters (where a sequence has more than one) by a kernel behind.
-#include "attend.cuh"
+#include "attend_tile.cuh"
 #include "page.cuh"
 
 namespace mvla {
@@ -104,21 +104,6 @@ struct Tile {
     }
 };
 
-// CTAs of this cluster; two words of the shared memory of one of them, at the offset of `addr`.
-__device__ __forceinline__ int cluster_ctas()
-{
-    int n;
-    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(n));
-    return n;
-}
-__device__ __forceinline__ float2 ld_peer(uint32_t addr, int rank)
-{
-    uint32_t remote;
-    float2 x;
-    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(remote) : "memory");
-    return x;
-}
 // N runs that lie next to one another (16 bytes at most).
 template <int N, class W>
 __device__ __forceinline__ void load_runs(const uint8_t* p, W* w)
@@ -633,14 +618,14 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_
         if (ranks == 1) continue;
         cluster_arrive_release();
         cluster_wait_acquire();
-        if (t < 8 * ranks) peer_ml[t >> 3][t & 7] = ld_peer(smem_u32(&cta_ml[8 * n + (t & 7)]), t >> 3);
+        if (t < 8 * ranks) peer_ml[t >> 3][t & 7] = ld_peer2(smem_u32(&cta_ml[8 * n + (t & 7)]), t >> 3);
         __syncthreads();
         for (int u = rank * kWarps * 32 + t; u < pairs; u += ranks * kWarps * 32) {
             const int r = u / (D / 2), col = u % (D / 2) * 2;
             float2 x2[kMaxCluster];
 #pragma unroll
             for (int k = 0; k < kMaxCluster; ++k)
-                if (k < ranks) x2[k] = ld_peer(smem_u32(&merge_o[0][r][col]), k);
+                if (k < ranks) x2[k] = ld_peer2(smem_u32(&merge_o[0][r][col]), k);
             float m = -CUDART_INF_F, l = 0.f, y = 0.f, z = 0.f;
             for (int k = 0; k < ranks; ++k) m = fmaxf(m, peer_ml[k][r].x);
             const float base = m == -CUDART_INF_F ? 0.f : m;
