@@ -339,7 +339,7 @@ inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, co
     const bool tokens = h.dtype != MVLA_DTYPE_FP32 && page_by_tokens(a->pages.kind, most_rows, keys * v.kv_heads);
     p.unpack = h.dtype != MVLA_DTYPE_FP32 && a->pages.kind != MVLA_PAGE_ROWS && !tokens && unpacks_on_the_way(h, batch, seqs);
     p.attend = h.dtype == MVLA_DTYPE_FP32 ? plan_page_fma(h, batch, seqs, counted, a->window, a->n_sink)
-             : tokens ? plan_tokens(h, batch, seqs, counted, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32))
+             : tokens ? plan_tokens(h, batch, seqs, counted, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32, most_rows <= 8 ? 1 : 2))
                       : plan_page_tiles(h, batch, seqs, counted, a->window, a->n_sink, p.unpack ? kUnpackedTileUs : kTileUs);
     p.bytes = p.attend.bytes;
     if (a->pages.kind == MVLA_PAGE_ROWS || tokens || p.unpack) return p;

@@ -21,7 +21,7 @@ MVLA_BOTH constexpr int page_row_bytes(int kind, int d, int wide) { return kind 
 MVLA_BOTH constexpr int page_row_scales(int kind, int d) { return kind == MVLA_PAGE_ROWS ? 0 : kind == MVLA_PAGE_E4M3 ? 1 : d / kPageGroup; }
 
 // Single tokens (page_token.cu): subtiles of 16 keys in a warp's tile, bytes of a tile in shared memory (in whole groups of 64 columns of the values),
-// tiles of a warp, and the CTAs that fit on a multiprocessor (four at most: by registers).
+// tiles of a warp, and the CTAs that fit on a multiprocessor.
 constexpr int kPageTokenStages = 2;
 MVLA_BOTH constexpr int page_token_sub(int kind, int pieces_of_32) { return pieces_of_32 <= 2 || (kind != MVLA_PAGE_ROWS && pieces_of_32 <= 4) ? 2 : 1; }
 MVLA_BOTH constexpr int page_token_tile(int kind, int pieces_of_32)
@@ -29,12 +29,13 @@ MVLA_BOTH constexpr int page_token_tile(int kind, int pieces_of_32)
     const int run = kind == MVLA_PAGE_ROWS ? 16 : kind == MVLA_PAGE_E4M3 ? 8 : 4, scales = kind == MVLA_PAGE_ROWS ? 0 : kind == MVLA_PAGE_E4M3 ? 1 : pieces_of_32;
     return page_token_sub(kind, pieces_of_32) * ((2 * pieces_of_32 + 4 * ((pieces_of_32 + 1) / 2)) * 32 * run + 32 * scales);
 }
-MVLA_BOTH constexpr int page_token_ctas(int kind, int pieces_of_32)
+// (`groups`: of eight query rows)
+MVLA_BOTH constexpr int page_token_ctas(int kind, int pieces_of_32, int groups)
 {
-    // (queries of 16 rows, factors of the scales, and what the system takes)
-    const int fixed = 1024 * pieces_of_32 + (kind == MVLA_PAGE_E2M1 ? 256 * page_token_sub(kind, pieces_of_32) * pieces_of_32 : 0) + 2048;
-    const int n = 227 * 1024 / (4 * kPageTokenStages * page_token_tile(kind, pieces_of_32) + fixed);
-    return n > 4 ? 4 : n < 1 ? 1 : n;
+    // queries, factors of the scales, and what the system takes; registers: four CTAs leave 128 to a thread, three 168, two 255
+    const int fixed = 512 * groups * pieces_of_32 + (kind == MVLA_PAGE_E2M1 ? 256 * page_token_sub(kind, pieces_of_32) * pieces_of_32 : 0) + 3072;
+    const int n = 227 * 1024 / (4 * kPageTokenStages * page_token_tile(kind, pieces_of_32) + fixed), most = groups == 1 ? (pieces_of_32 <= 6 ? 4 : 3) : pieces_of_32 <= 2 ? 3 : 2;
+    return n > most ? most : n < 1 ? 1 : n;
 }
 
 }  // namespace mvla

@@ -310,7 +310,8 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) page_read_kernel(const __g
         for (int b0 = s.first; b0 < n; b0 += kAhead * s.step) {
             // (rows that are not there: codes of zero)
             Codes w[kAhead][kPieces];
-            uint32_t byte[kAhead][kPieces];
+            constexpr int kBytes = KIND == MVLA_PAGE_E2M1 ? kPieces : 1;
+            uint32_t byte[kAhead][kBytes];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
                 const int r = b0 + u * s.step;
@@ -320,14 +321,14 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) page_read_kernel(const __g
                 for (int i = 0; i < kPieces; ++i) {
                     const int piece = i * LANES + s.lane;
                     const bool there = from >= 0 && on[i];
-                    byte[u][i] = 127;
+                    if (i < kBytes) byte[u][i] = 127;
                     if constexpr (KIND == MVLA_PAGE_ROWS) {
                         w[u][i].clear();
                         if (there) w[u][i].load(src + piece * 8 * kWide);
                     } else {
                         w[u][i] = Codes{};
                         if (there) w[u][i] = *reinterpret_cast<const Codes*>(src + piece * (KIND == MVLA_PAGE_E4M3 ? 8 : 4));
-                        if (there) byte[u][i] = scales[at[r].scale + (KIND == MVLA_PAGE_E4M3 ? 0 : piece / (kPageGroup / 8))];
+                        if (i < kBytes && from >= 0) byte[u][i] = scales[at[r].scale + (KIND == MVLA_PAGE_E4M3 || !on[i] ? 0 : piece / (kPageGroup / 8))];
                     }
                 }
             }
@@ -344,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) page_read_kernel(const __g
                     } else {
                         float x[8];
                         code_values(w[u][i], x);
-                        const float scale = scale_value(byte[u][i]);
+                        const float scale = scale_value(byte[u][i < kBytes ? i : 0]);
 #pragma unroll
                         for (int k = 0; k < 8; ++k) x[k] *= scale;
                         y.set(x);
@@ -393,11 +394,9 @@ cudaError_t by_lanes(PageRowsArgs& a, cudaStream_t stream)
 template <Way WAY, class T>
 cudaError_t by_kind(int kind, PageRowsArgs& a, cudaStream_t stream)
 {
-    switch (kind) {
-    case MVLA_PAGE_ROWS: return by_lanes<WAY, T, MVLA_PAGE_ROWS>(a, stream);
-    case MVLA_PAGE_E4M3: return by_lanes<WAY, T, MVLA_PAGE_E4M3>(a, stream);
-    default: return by_lanes<WAY, T, MVLA_PAGE_E2M1>(a, stream);
-    }
+    if constexpr (WAY != kTiles)                             // (tiles are made of quantised pages)
+        if (kind == MVLA_PAGE_ROWS) return by_lanes<WAY, T, MVLA_PAGE_ROWS>(a, stream);
+    return kind == MVLA_PAGE_E4M3 ? by_lanes<WAY, T, MVLA_PAGE_E4M3>(a, stream) : by_lanes<WAY, T, MVLA_PAGE_E2M1>(a, stream);
 }
 
 }  // namespace

@@ -123,7 +123,7 @@ __device__ __forceinline__ void load_runs(const uint8_t* p, W* w)
 __device__ __forceinline__ float byte_float(uint32_t byte, int off) { return __uint_as_float(0x4B000000u + byte) - static_cast<float>(8388608 + off); }
 
 template <int KIND, int D32, int NR>
-__global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32)) page_token_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ PagePool pool)
+__global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) page_token_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ PagePool pool)
 {
     using Sh = Tile<KIND, D32>;
     using Word = typename Run<KIND>::Word;
@@ -667,7 +667,9 @@ cudaError_t attend(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
 template <int KIND, int D32>
 cudaError_t by_rows(const AttArgs& a, const PagePool& pool, int rows, cudaStream_t stream)
 {
-    return rows <= 8 ? attend<KIND, D32, 1>(a, pool, stream) : attend<KIND, D32, 2>(a, pool, stream);
+    if constexpr (KIND != MVLA_PAGE_ROWS)                    // (rows of their own type: eight at most, page_by_tokens)
+        if (rows > 8) return attend<KIND, D32, 2>(a, pool, stream);
+    return attend<KIND, D32, 1>(a, pool, stream);
 }
 template <int KIND>
 cudaError_t by_dim(const AttArgs& a, const PagePool& pool, int rows, cudaStream_t stream)

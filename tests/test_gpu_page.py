@@ -145,6 +145,25 @@ def test_rows_at_device_lengths_and_one_of_the_two_alone():
     assert same(k.double(), want)
 
 
+@pytest.mark.parametrize("kind", [ROWS, E4M3, E2M1])
+def test_rows_read_into_slices_of_one_tensor(kind):
+    gen = generator(6)
+    G, d, page_rows = 4, 96, 32
+    ctx = context(G=G, d=d)
+    table, n_pages = P.make_table(gen, [75, 20], page_rows)
+    pool = P.make_pool(gen, n_pages, G, page_rows, d, kind, BF16)
+    seqs = [mvla.Seq(q_row=30, n_q=75, n_kv=75), mvla.Seq(q_row=2, n_q=11, n_kv=20)]
+    both = torch.full((110, 3, G, d), 7.0, dtype=BF16, device="cuda")
+    k, v = ctx.page_read(pool, seqs, table, k_out=both[:, 2], v_out=both[:, 0])
+    assert k.data_ptr() == both[:, 2].data_ptr() and v.data_ptr() == both.data_ptr()
+    left = torch.ones(110, dtype=torch.bool, device="cuda")
+    for b, s in enumerate(seqs):
+        for at, want in zip((2, 0), P.rows_of(pool, kind, table, b, s.n_kv, page_rows)):
+            assert same(both[s.q_row:s.q_row + s.n_q, at].double(), want[s.n_kv - s.n_q:])
+        left[s.q_row:s.q_row + s.n_q] = False
+    assert (both[left] == 7.0).all() and (both[:, 1] == 7.0).all()
+
+
 def test_pages_outside_the_pool():
     """Written rows are dropped, read rows are zeros, attention sees rows of zeros."""
     gen = generator(4)
