@@ -77,7 +77,7 @@ __device__ __forceinline__ Span key_span(const AttArgs& a, const AttSeq& s, int 
         if (c < 0) hidden = true;
         else { lo = min(lo, c); hi = max(hi, c); }
     }
-    return {__reduce_min_sync(0xffffffffu, lo), __reduce_max_sync(0xffffffffu, hi), __any_sync(0xffffffffu, hidden)};
+    return {__reduce_min_sync(0xffffffffu, lo), __reduce_max_sync(0xffffffffu, hi), __any_sync(0xffffffffu, hidden) != 0};
 }
 __device__ __forceinline__ Span counted_span(int len, int j0, int n)
 {

@@ -79,6 +79,7 @@ def rows_call(shim, seqs, pool, write, dtype=BF16, **kw):
 
 
 ONE = [dict(n_q=3, n_kv=40)]
+MANY = [dict(n_q=400, n_kv=500)]           # unpacked first: a call that needs a workspace
 KINDS = dict(e4m3=dict(kind=mvla.PAGE_E4M3), e2m1=dict(kind=mvla.PAGE_E2M1))
 
 
@@ -129,7 +130,7 @@ def attention_call(shim, seqs, pool, dtype=BF16, heads=(8, 4, 64), **kw):
 
 
 @pytest.mark.parametrize("want,seqs,pool,kw", [
-    (OK, ONE, {}, {}), (OK, ONE, KINDS["e4m3"], {}), (OK, ONE, KINDS["e2m1"], dict(lse=4 * MB)), (OK, [dict(n_q=0, n_kv=40)], {}, dict(q=None, out=None, table=None)),
+    (OK, ONE, {}, {}), (OK, ONE, KINDS["e4m3"], {}), (OK, ONE, KINDS["e2m1"], dict(lse=4 * MB)), (OK, MANY, KINDS["e4m3"], dict(q_rows=400, out=5 * MB)), (OK, [dict(n_q=0, n_kv=40)], {}, dict(q=None, out=None, table=None)),
     (OK, [dict(n_q=2, n_kv=0)], {}, dict(table=None)), (OK, [dict(n_q=1, n_kv=40), dict(q_row=1, n_q=1, n_kv=40)], {}, {}),
     (CAP, ONE * 5, {}, {}), (BAD, [], {}, {}), (BAD, [dict(n_q=-1, n_kv=40)], {}, {}), (BAD, [dict(q_row=98, n_q=3, n_kv=4)], {}, {}), (BAD, [dict(n_q=1, n_kv=513)], {}, {}),
     (BAD, [dict(n_q=2, n_kv=4), dict(q_row=1, n_q=2, n_kv=4)], {}, {}), (BAD, ONE, {}, dict(window=0)), (BAD, ONE, {}, dict(n_sink=-1)),
@@ -138,8 +139,8 @@ def attention_call(shim, seqs, pool, dtype=BF16, heads=(8, 4, 64), **kw):
     (BAD, ONE, {}, dict(out=16 * MB)), (BAD, ONE, KINDS["e4m3"], dict(out=48 * MB)), (BAD, ONE, {}, dict(out=1 * MB)), (BAD, ONE, {}, dict(lse=3 * MB)),
     (BAD, ONE, {}, dict(lse=4 * MB + 2)), (BAD, ONE, {}, dict(kv_len=4 * MB, lse=4 * MB)), (BAD, ONE, {}, dict(q_rows=-1)), (BAD, ONE, {}, dict(q_rows=1 << 60)),
     (BAD, ONE, dict(k=None), {}), (UNSUP, ONE, dict(page_rows=20), {}),
-    (BAD, [dict(n_q=60, n_kv=500)], KINDS["e4m3"], dict(workspace=None)), (BAD, [dict(n_q=60, n_kv=500)], KINDS["e4m3"], dict(workspace_bytes=100)),
-    (BAD, [dict(n_q=60, n_kv=500)], KINDS["e4m3"], dict(workspace=64 * MB + 16)), (BAD, [dict(n_q=60, n_kv=500)], KINDS["e4m3"], dict(workspace=16 * MB)),
+    (BAD, MANY, KINDS["e4m3"], dict(workspace=None, q_rows=400, out=5 * MB)), (BAD, MANY, KINDS["e4m3"], dict(workspace_bytes=100, q_rows=400, out=5 * MB)),
+    (BAD, MANY, KINDS["e4m3"], dict(workspace=64 * MB + 16, q_rows=400, out=5 * MB)), (BAD, MANY, KINDS["e4m3"], dict(workspace=16 * MB, q_rows=400, out=5 * MB)),
 ])
 def test_refusals_of_attention(shim, want, seqs, pool, kw):
     assert attention_call(shim, seqs, pages(**pool), **kw)[0] == want
