@@ -46,7 +46,7 @@ cudaError_t launch_page_tiles(int hidden_dtype, int kind, PageRowsArgs& a, cudaS
 // Single tokens (launch_attend_token's), over pages; q and out bf16.  Behind it: launch_attend_finish.
 cudaError_t launch_page_token(int kind, const AttArgs& a, const PagePool& pool, int rows, cudaStream_t stream);
 
-// Blocks of query rows over quantised pages, unpacked on the way (launch_page_tile's blocks and parts); q and out bf16.  Behind it: launch_attend_join.
-cudaError_t launch_page_decode(int kind, const AttArgs& a, const PagePool& pool, cudaStream_t stream);
+// Blocks of `row_tiles` (1, or 2 for heads of up to 128 elements) tiles of 128 query rows over quantised pages, unpacked on the way; q and out bf16.  Behind it: launch_attend_join.
+cudaError_t launch_page_decode(int kind, int row_tiles, const AttArgs& a, const PagePool& pool, cudaStream_t stream);
 
 }  // namespace mvla

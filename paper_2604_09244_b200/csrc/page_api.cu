@@ -153,7 +153,7 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     }
     cudaError_t e;
     if (plan.unpack) {
-        e = launch_page_decode(a->pages.kind, t, pool, st);
+        e = launch_page_decode(a->pages.kind, plan.unpack, t, pool, st);
     } else if (plan.attend.form == kFormFma) {
         e = launch_page_fma(t, plan.attend.rows, st);
     } else {

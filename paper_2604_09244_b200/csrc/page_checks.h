@@ -103,7 +103,7 @@ struct PageAttendPlan {
     AttendPlan attend;
     // quantised pages that are no single tokens': the tiles that some query sees, as elements of the hidden type (-1: there are none)
     int64_t dense_k = -1, dense_v = -1, dense_tiles = 0, bytes = 0;
-    bool unpack = false;         // ... or the tile form unpacks them on the way
+    int32_t unpack = 0;          // ... or the tile form unpacks them on the way, for so many tiles of query rows at a time
 };
 
 // Tiles that a sequence's queries see, at most.
@@ -229,14 +229,14 @@ inline AttendPlan plan_tokens(const ServeShape& c, int32_t batch, const mvla_seq
 // multiple of 64 keys to a CTA, at least 128), so that their CTAs fill whole rounds of those that fit: of one to four rounds, or no cut at all, what ends
 // first.  In us: the tiles of its longest part and 4 for its start and end, `tile` each (with another CTA beside it); 1 where a cluster joins; 5 for the kernel that joins
 // parts, and what their sums, written and read, take at 6 TB/s.
-constexpr double kTileUs = 1.3, kUnpackedTileUs = 2.2;
-inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, double tile)
+constexpr double kTileUs = 1.3, kUnpackedTileUs = 2.2, kUnpackedPairUs = 1.4;
+inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, int row_tiles, double tile)
 {
     AttendPlan p;
     p.form = kFormPageTile;
     p.pack = pack_of(c.n_heads / c.kv_heads);
-    p.queries = 128 / p.pack;
-    const int64_t packs = c.n_heads / p.pack, each = c.head_dim <= 128 ? 2 : 1, slots = each * static_cast<int64_t>(c.sm_count);
+    p.queries = 128 / p.pack * row_tiles;
+    const int64_t packs = c.n_heads / p.pack, each = c.head_dim <= 128 && row_tiles == 1 ? 2 : 1, slots = each * static_cast<int64_t>(c.sm_count);
     int64_t work = 0, longest = 1;
     const auto blocks_of = [&](const mvla_seq& s) { return (static_cast<int64_t>(s.n_q) + p.queries - 1) / p.queries; };
     for (int b = 0; b < batch; ++b) {
@@ -302,12 +302,13 @@ inline bool page_by_tokens(int kind, int64_t rows, int64_t keys_and_heads)
 // Whether so few blocks of queries go over a sequence's pages that each had better unpack them for itself: unpacking first costs 0.15 us for 1000 rows of a head (their
 // bytes, twice), on the way 0.06 us for every block that does.  us, on the way / first, 32 heads in groups of 4, e4m3: 5 tokens over 60000 rows (a block) 61 / 121;
 // 4 chunks of 56 over 2000 to 6000 (two) 52 / 57, of 33 over 4000 (two) 48 / 51; 100 over 4096 (four) 36 / 31; 512 over 8192 (16) 141 / 98.
-inline bool unpacks_on_the_way(const ServeShape& c, int32_t batch, const mvla_seq* seqs)
+inline int32_t unpacked_row_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs)
 {
     const int64_t queries = 128 / pack_of(c.n_heads / c.kv_heads);
     int64_t most = 0;
     for (int b = 0; b < batch; ++b) most = std::max(most, (static_cast<int64_t>(seqs[b].n_q) + queries - 1) / queries);
-    return most <= 2;
+    if (most <= 1) return 1;
+    return c.head_dim <= 128 ? (most <= 1000 ? 2 : 0) : most <= 2 ? 1 : 0;
 }
 
 // fp32: as packed rows, but in blocks of 8 query rows where the call is so short that the CTAs of those run at once and a block's keys are few (208 rows of 8 heads of 64,
@@ -337,10 +338,10 @@ inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, co
     int64_t keys = 0;
     for (int b = 0; b < batch; ++b) keys += seqs[b].n_q ? visible_keys(seqs[b], counted, a->window, a->n_sink) : 0;
     const bool tokens = h.dtype != MVLA_DTYPE_FP32 && page_by_tokens(a->pages.kind, most_rows, keys * v.kv_heads);
-    p.unpack = h.dtype != MVLA_DTYPE_FP32 && a->pages.kind != MVLA_PAGE_ROWS && !tokens && unpacks_on_the_way(h, batch, seqs);
+    if (h.dtype != MVLA_DTYPE_FP32 && a->pages.kind != MVLA_PAGE_ROWS && !tokens) p.unpack = unpacked_row_tiles(h, batch, seqs);
     p.attend = h.dtype == MVLA_DTYPE_FP32 ? plan_page_fma(h, batch, seqs, counted, a->window, a->n_sink)
              : tokens ? plan_tokens(h, batch, seqs, counted, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32, most_rows <= 8 ? 1 : 2))
-                      : plan_page_tiles(h, batch, seqs, counted, a->window, a->n_sink, p.unpack ? kUnpackedTileUs : kTileUs);
+                      : plan_page_tiles(h, batch, seqs, counted, a->window, a->n_sink, p.unpack == 2 ? 2 : 1, p.unpack == 2 ? kUnpackedPairUs : p.unpack ? kUnpackedTileUs : kTileUs);
     p.bytes = p.attend.bytes;
     if (a->pages.kind == MVLA_PAGE_ROWS || tokens || p.unpack) return p;
     Workspace w;

@@ -27,20 +27,23 @@ template <int KIND> struct Codes;
 template <> struct Codes<MVLA_PAGE_E4M3> { using Word = uint2; static constexpr int kLift = 7; };       // eight elements; room above the codes in fp16
 template <> struct Codes<MVLA_PAGE_E2M1> { using Word = uint32_t; static constexpr int kLift = 13; };
 
-template <int KIND, int D32>
+// T: tiles of 128 query rows to a CTA, which share what is unpacked: one and two CTAs to a multiprocessor (heads of up to 128 elements), or two and one CTA.
+template <int KIND, int D32, int T>
 struct PageTileShape {
     static constexpr int kDB = (D32 + 1) / 2;                // boxes of 64 elements
-    static constexpr int kIssues = 4, kLoads = 5, kDecodes = 6, kDecoders = 4, kWarps = kDecodes + kDecoders;
-    static constexpr int kO = 2 * kKeys, kColumns = kO + kDB * 64 <= 256 ? 256 : 512;       // of tensor memory: S (two buffers, P in the same columns), then O
-    static constexpr int kCtas = kTmemColsPerSm / kColumns;
-    static constexpr int kQBytes = kDB * kRows * 128, kStage = kDB * kKeys * 128;
+    static constexpr int kIssues = 4 * T, kLoads = kIssues + 1, kDecodes = kIssues + 2, kDecoders = 4, kWarps = kDecodes + kDecoders;
+    static constexpr int kO = 2 * kKeys, kOf = kO + kDB * 64;       // columns of tensor memory of a tile of rows: S (two buffers, P in the same columns), then O
+    static constexpr int kColumns = T * kOf <= 256 ? 256 : 512;
+    static_assert(T * kOf <= kTmemColsPerSm, "shape");
+    static constexpr int kCtas = T == 1 ? kTmemColsPerSm / kColumns : 1;
+    static constexpr int kQBytes = T * kDB * kRows * 128, kStage = kDB * kKeys * 128;
     // the ring: codes of a tile's keys, with the scales of its keys and values, or codes of its values
     static constexpr int kRowBytes = page_row_bytes(KIND, D32 * 32, 2), kGroups = page_row_scales(KIND, D32 * 32);
-    static constexpr int kCodes = kKeys * kRowBytes, kSlot = kCodes + 2 * kKeys * kGroups, kSlots = 3;
-    static constexpr int kRoom = ((kCtas == 2 ? kSmemPerSm / 2 - kSmemReservedPerCta : kSmemMaxPerCta) - 6 * 1024 - kQBytes - kSlots * kSlot) / kStage;
+    static constexpr int kCodes = kKeys * kRowBytes, kSlot = kCodes + 2 * kKeys * kGroups, kSlots = T == 1 ? 3 : 4;
+    static constexpr int kRoom = ((kCtas == 2 ? kSmemPerSm / 2 - kSmemReservedPerCta : kSmemMaxPerCta) - (T == 1 ? 6 : 8) * 1024 - kQBytes - kSlots * kSlot) / kStage;
     static constexpr int kStages = kRoom > kMaxStages ? kMaxStages : kRoom;
     static constexpr int kSmem = 1024 + kQBytes + kStages * kStage + kSlots * kSlot;
-    static constexpr int kPieces = 2 * D32;                  // of eight elements, of a decoding thread, in a tile of keys or of values
+    static constexpr int kPieces = 8 * D32 / kDecoders;      // of eight elements, of a decoding thread, in a tile of keys or of values
     static_assert(kStages >= 3 && kSlot % 16 == 0, "shape");
 };
 constexpr int kTileRefs = 8;                 // tiles whose references are kept
@@ -63,41 +66,47 @@ __device__ __forceinline__ void store16(uint32_t at, const uint32_t (&w)[4])
 // Where eight elements of a row lie in a tile of such rows, in boxes of 64 elements of `rows` rows.
 __device__ __forceinline__ uint32_t swizzled(int row, int piece, int rows) { return piece / 8 * rows * 128 + row * 128 + ((piece & 7) ^ (row & 7)) * 16; }
 
-template <int KIND, int D32>
-__global__ void __launch_bounds__(PageTileShape<KIND, D32>::kWarps * 32, PageTileShape<KIND, D32>::kCtas)
+template <int KIND, int D32, int T>
+__global__ void __launch_bounds__(PageTileShape<KIND, D32, T>::kWarps * 32, PageTileShape<KIND, D32, T>::kCtas)
 page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ PagePool pool)
 {
-    using Sh = PageTileShape<KIND, D32>;
+    using Sh = PageTileShape<KIND, D32, T>;
     using Word = typename Codes<KIND>::Word;
     constexpr bool kE2m1 = KIND == MVLA_PAGE_E2M1;
     constexpr int D = D32 * 32, ST = Sh::kStages, P = Sh::kPieces, G = kE2m1 ? D32 : 1, kCodeLift = Codes<KIND>::kLift, kRowBytes = Sh::kRowBytes;
     extern __shared__ uint8_t raw[];
-    __shared__ uint64_t bars[2 * kMaxStages + 8 + 2 * Sh::kSlots];
+    __shared__ uint64_t bars[2 * kMaxStages + 3 + 5 * T + 2 * Sh::kSlots];
     __shared__ unsigned groups_there[Sh::kSlots];            // of a slot: a bit to every 16 rows that have a page
     __shared__ uint32_t factors[2][kKeys][G];                // of a tile's keys and values: fp16, twice
-    __shared__ uint32_t warp_top[Sh::kDecoders];
+    __shared__ uint32_t warp_top[4];
     __shared__ int2 refs[kTileRefs];                         // bytes of the largest scales of a tile's keys and values
     __shared__ int dead;
     __shared__ uint32_t tmem_base;
-    __shared__ float2 row_ml[kRows];
-    static_assert(Sh::kSmem - 1024 >= D * kRows * 4, "room for the sums of a cluster's CTA");
+    __shared__ float2 row_ml[T][kRows];
+    static_assert(Sh::kSmem - 1024 >= T * D * kRows * 4, "room for the sums of a cluster's CTA");
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t q_at = base, kv_at = base + Sh::kQBytes;
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int i) { return bar0 + 8u * i; };
     const auto empty = [&](int i) { return bar0 + 8u * (kMaxStages + i); };
-    const uint32_t q_full = bar0 + 8u * (2 * kMaxStages), s_full = q_full + 8, p_full = q_full + 24, o_step = q_full + 40, o_full = q_full + 48, ended = q_full + 56;
+    const uint32_t q_full = bar0 + 8u * (2 * kMaxStages), o_full = q_full + 8, ended = q_full + 16, first = q_full + 24;
+    // of tile `w` of rows, of S buffer `buf`
+    const auto s_full = [&](int w, int buf) { return first + 8u * (5 * w + buf); };
+    const auto p_full = [&](int w, int buf) { return first + 8u * (5 * w + 2 + buf); };
+    const auto o_step = [&](int w) { return first + 8u * (5 * w + 4); };
     const uint32_t ring_at = kv_at + ST * Sh::kStage;
     const uint8_t* const ring = raw + (ring_at - smem_u32(raw));
-    const auto raw_full = [&](int i) { return ended + 8u * (1 + i); };
-    const auto raw_empty = [&](int i) { return ended + 8u * (1 + Sh::kSlots + i); };
+    const auto raw_full = [&](int i) { return first + 8u * (5 * T + i); };
+    const auto raw_empty = [&](int i) { return first + 8u * (5 * T + Sh::kSlots + i); };
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31;
 
     if (warp == Sh::kIssues && lane == 0) {
         for (int i = 0; i < ST; ++i) { mbar_init(full(i), Sh::kDecoders); mbar_init(empty(i), 1); }
-        mbar_init(q_full, 4);
-        for (int i = 0; i < 2; ++i) { mbar_init(s_full + 8 * i, 1); mbar_init(p_full + 8 * i, 128); }
-        mbar_init(o_step, 1);
+        mbar_init(q_full, 4 * T);
+        for (int w = 0; w < T; ++w) {
+            for (int i = 0; i < 2; ++i) { mbar_init(s_full(w, i), 1); mbar_init(p_full(w, i), 128); }
+            mbar_init(o_step(w), 1);
+        }
         mbar_init(o_full, 1);
         mbar_init(ended, 1);
         for (int i = 0; i < Sh::kSlots; ++i) { mbar_init(raw_full(i), 1); mbar_init(raw_empty(i), Sh::kDecoders); }
@@ -114,8 +123,8 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
     const AttSeq& s = a.s[seq_of_block(a, blk)];
     const int hk = head0 / (a.n_heads / a.kv_heads), per = kRows / a.pack;      // queries of the tile
     const int part_of_seq = (blk - s.blk0) % s.parts, parts = s.parts * ranks, piece_of_seq = ranks > 1 ? part_of_seq * ranks + static_cast<int>(cluster_ctarank()) : part_of_seq;
-    const int q0 = (blk - s.blk0) / s.parts * per, len = seq_len(a, s);
-    const int lo = query_pos(a, s, len, q0), hi = query_pos(a, s, len, min(q0 + per, s.n_q) - 1);
+    const int q0 = (blk - s.blk0) / s.parts * (T * per), len = seq_len(a, s);
+    const int lo = query_pos(a, s, len, q0), hi = query_pos(a, s, len, min(q0 + T * per, s.n_q) - 1);
     const TileRange range = tile_range(a, len, lo, hi, kKeys);
     const int per_part = (range.count + parts - 1) / parts, v0 = piece_of_seq * per_part, n = max(0, min(range.count - v0, per_part));
     const auto first_key = [&](int i) { return range.tile(v0 + i) * kKeys; };
@@ -131,7 +140,10 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
     const uint32_t tmem = tmem_base;
 
     if (warp == Sh::kLoads) {
-        // ---- codes and scales: chunk 2 i the keys of tile i and both scales, chunk 2 i + 1 its values; a lane to every 16 rows
+        // ---- codes and scales: chunk 2 i the keys of tile i and both scales, chunk 2 i + 1 its values; a lane to every 16 rows, of which the first of a page copies
+        // what the tile has of it (a copy is dear, however small: 16 rows at a time a tile takes 1.5 times as long)
+        const int rows = min(kKeys, 1 << pool.page_shift);
+        const bool copies = lane < 4 && (16 * lane & (rows - 1)) == 0;
         const auto look_up = [&](int i) {
             if (i >= n || lane >= 4) return -1;
             const int j = first_key(i) + 16 * lane;
@@ -145,28 +157,29 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                 ahead = look_up(c / 2 + 1);
             }
             if (c >= Sh::kSlots && !guard.wait_all(raw_empty(slot), (c / Sh::kSlots - 1) & 1)) break;
-            const unsigned there = __ballot_sync(0xffffffffu, page >= 0);
+            const unsigned there = __ballot_sync(0xffffffffu, page >= 0), from = __ballot_sync(0xffffffffu, page >= 0 && copies);
             if (lane == 0) {
                 groups_there[slot] = there;
-                mbar_expect_tx(raw_full(slot), __popc(there) * (16 * kRowBytes + (c & 1 ? 0 : 2 * 16 * G)));
+                mbar_expect_tx(raw_full(slot), __popc(from) * rows * (kRowBytes + (c & 1 ? 0 : 2 * G)));
             }
             __syncwarp();
-            if (page >= 0) {
+            if (page >= 0 && copies) {
                 const int64_t row = page_row(pool, page, hk, first_key(c / 2) + 16 * lane);
                 const uint32_t to = ring_at + slot * Sh::kSlot;
-                bulk_load(to + 16 * lane * kRowBytes, static_cast<const uint8_t*>(c & 1 ? pool.v : pool.k) + row * kRowBytes, 16 * kRowBytes, raw_full(slot));
+                bulk_load(to + 16 * lane * kRowBytes, static_cast<const uint8_t*>(c & 1 ? pool.v : pool.k) + row * kRowBytes, rows * kRowBytes, raw_full(slot));
                 if (!(c & 1)) {
-                    bulk_load(to + Sh::kCodes + 16 * lane * G, pool.k_scale + row * G, 16 * G, raw_full(slot));
-                    bulk_load(to + Sh::kCodes + (kKeys + 16 * lane) * G, pool.v_scale + row * G, 16 * G, raw_full(slot));
+                    bulk_load(to + Sh::kCodes + 16 * lane * G, pool.k_scale + row * G, rows * G, raw_full(slot));
+                    bulk_load(to + Sh::kCodes + (kKeys + 16 * lane) * G, pool.v_scale + row * G, rows * G, raw_full(slot));
                 }
             }
         }
         for (int i = max(0, c - Sh::kSlots); i < c; ++i) guard.settle(raw_full(i % Sh::kSlots), i / Sh::kSlots & 1);      // (whoever gave up, what is under way lands)
     } else if (warp >= Sh::kDecodes) {
         // ---- codes into fp16
-        const int dt = t - Sh::kDecodes * 32, side = dt >> 6, own_row = dt & 63;
+        constexpr int kThreads = Sh::kDecoders * 32;
+        const int dt = t - Sh::kDecodes * 32, side = dt >> 6, own_row = dt & 63;             // (scales: of the first 128)
         bool ok = true;
-        const auto meet = [] { asm volatile("bar.sync 1, 128;" ::: "memory"); };
+        const auto meet = [] { asm volatile("bar.sync 1, %0;" ::"n"(kThreads) : "memory"); };
         uint8_t* const stages = raw + (kv_at - smem_u32(raw));
         const auto one_piece = [&](uint8_t* stage, int u, Word w, uint32_t f, bool out) {
             uint32_t h[4];
@@ -184,14 +197,14 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                 uint32_t f[P];
 #pragma unroll
                 for (int k = 0; k < P; ++k) {
-                    w[k] = codes[dt + 128 * k];
-                    f[k] = factor(dt + 128 * k);
+                    w[k] = codes[dt + kThreads * k];
+                    f[k] = factor(dt + kThreads * k);
                 }
 #pragma unroll
-                for (int k = 0; k < P; ++k) one_piece(stage, dt + 128 * k, w[k], f[k], false);
+                for (int k = 0; k < P; ++k) one_piece(stage, dt + kThreads * k, w[k], f[k], false);
             } else {
 #pragma unroll 1
-                for (int u = dt; u < 128 * P; u += 128) {
+                for (int u = dt; u < kThreads * P; u += kThreads) {
                     const int row = u / (4 * D32);
                     one_piece(stage, u, codes[u], factor(u), !(there >> (row >> 4) & 1u) || !(j0 + row < len && some_sees(lo, hi, j0 + row, a.window, a.n_sink)));
                 }
@@ -210,7 +223,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             ok = ok && codes_there(2 * i);
             const unsigned there = groups_there[2 * i % Sh::kSlots];
             uint32_t scale[G], top = 0;
-            {                                                // of one row, of keys or values (those that nobody sees may hold anything)
+            if (dt < 128) {                                  // of one row, of keys or values (those that nobody sees may hold anything)
                 const int j = j0 + own_row;
                 const bool on = (there >> (own_row >> 4) & 1u) && j < len && some_sees(lo, hi, j, a.window, a.n_sink);
                 const uint8_t* const b = ring + 2 * i % Sh::kSlots * Sh::kSlot + Sh::kCodes + dt * G;
@@ -219,15 +232,17 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                     scale[g] = on ? b[g] : 0u;
                     top = max(top, scale[g]);
                 }
+                top = __reduce_max_sync(0xffffffffu, top);
+                if (lane == 0) warp_top[warp - Sh::kDecodes] = top;
             }
-            top = __reduce_max_sync(0xffffffffu, top);
-            if (lane == 0) warp_top[warp - Sh::kDecodes] = top;
             meet();                                          // (and nobody is with the last tile's factors any more)
             const int refs_here[2] = {static_cast<int>(max(max(warp_top[0], warp_top[1]), 10u)), static_cast<int>(max(max(warp_top[2], warp_top[3]), 10u))};
+            if (dt < 128) {
 #pragma unroll
-            for (int g = 0; g < G; ++g) {
-                const int e = static_cast<int>(scale[g]) - refs_here[side] + kCodeLift + 15;
-                factors[side][own_row][g] = static_cast<uint32_t>(max(e, 0)) * 0x04000400u;
+                for (int g = 0; g < G; ++g) {
+                    const int e = static_cast<int>(scale[g]) - refs_here[side] + kCodeLift + 15;
+                    factors[side][own_row][g] = static_cast<uint32_t>(max(e, 0)) * 0x04000400u;
+                }
             }
             ok = ok && room(2 * i);                          // (the references of kTileRefs tiles ago have been read by then)
             if (ok && dt == 0) refs[i % kTileRefs] = make_int2(refs_here[0], refs_here[1]);
@@ -243,9 +258,13 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         const auto scores = [&](int i) {                     // S of tile i; its keys' stage is free when it is there
             const int st = 2 * i % ST;
 #pragma unroll
-            for (int b = 0; b < Sh::kDB; ++b)
-                umma_box(2, tmem + (i & 1) * kKeys, smem_desc_sw128(q_at + b * kRows * 128), smem_desc_sw128(kv_at + st * Sh::kStage + b * kKeys * 128), idesc_s, min(4, D / 16 - 4 * b), b > 0);
-            umma_commit(s_full + 8 * (i & 1));
+            for (int w = 0; w < T; ++w) {
+#pragma unroll
+                for (int b = 0; b < Sh::kDB; ++b)
+                    umma_box(2, tmem + w * Sh::kOf + (i & 1) * kKeys, smem_desc_sw128(q_at + (w * Sh::kDB + b) * kRows * 128), smem_desc_sw128(kv_at + st * Sh::kStage + b * kKeys * 128), idesc_s,
+                             min(4, D / 16 - 4 * b), b > 0);
+                umma_commit(s_full(w, i & 1));
+            }
             umma_commit(empty(st));
         };
         bool ok = guard.wait_all(q_full, 0) && guard.wait_all(full(0), 0);
@@ -266,24 +285,29 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                 __syncwarp();
             }
             const int c = 2 * i + 1, st = c % ST;
-            ok = ok && guard.wait_all(full(st), c / ST & 1) && guard.wait_all(p_full + 8 * (i & 1), i / 2 & 1);
-            if (ok && one) {
-                fence();
-                tc_fence_after();
-                for (int k = 0; k < kKeys / 16; ++k)
-                    umma_bf16_ts(tmem + Sh::kO, tmem + (i & 1) * kKeys + 8 * k, smem_desc_rows_sw128(kv_at + st * Sh::kStage + k * 2048, kKeys * 128), idesc_o, i > 0 || k > 0);
-                umma_commit(o_step);
-                umma_commit(empty(st));
+            ok = ok && guard.wait_all(full(st), c / ST & 1);
+            for (int w = 0; w < T && ok; ++w) {
+                ok = guard.wait_all(p_full(w, i & 1), i / 2 & 1);
+                if (ok && one) {
+                    fence();
+                    tc_fence_after();
+                    for (int k = 0; k < kKeys / 16; ++k)
+                        umma_bf16_ts(tmem + w * Sh::kOf + Sh::kO, tmem + w * Sh::kOf + (i & 1) * kKeys + 8 * k, smem_desc_rows_sw128(kv_at + st * Sh::kStage + k * 2048, kKeys * 128), idesc_o,
+                                     i > 0 || k > 0);
+                    umma_commit(o_step(w));
+                }
+                __syncwarp();
             }
+            if (ok && one) umma_commit(empty(st));
             __syncwarp();
         }
         if (one) umma_commit(ok ? o_full : ended);
         __syncwarp();
         guard.settle(ok ? o_full : ended, 0);                // (whoever else gave up, the tensor memory is not given back under an MMA)
-    } else if (warp < 4) {
+    } else if (warp < 4 * T) {
         // ---- softmax, a thread per row
-        const int i_row = q0 + t / a.pack, head = head0 + t % a.pack;
-        const bool mine = t < per * a.pack && i_row < s.n_q;
+        const int w = warp >> 2, r = t & (kRows - 1), i_row = q0 + w * per + r / a.pack, head = head0 + r % a.pack;
+        const bool mine = r < per * a.pack && i_row < s.n_q;
         const int p = mine ? query_pos(a, s, len, i_row) : -1;
         float q_scale = a.scale_log2 * two_to(-kCodeLift);   // of the scores, less the tile's
         if (n > 0) {                                         // this row's queries, in fp16
@@ -292,9 +316,9 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             if (mine) {
 #pragma unroll
                 for (int c = 0; c < D; c += 8) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(q + c);
-                    constexpr uint32_t m = 0x7FFF7FFFu;
-                    top = __vmaxu2(top, __vmaxu2(__vmaxu2(w.x & m, w.y & m), __vmaxu2(w.z & m, w.w & m)));
+                    const uint4 y = *reinterpret_cast<const uint4*>(q + c);
+                    constexpr uint32_t some = 0x7FFF7FFFu;
+                    top = __vmaxu2(top, __vmaxu2(__vmaxu2(y.x & some, y.y & some), __vmaxu2(y.z & some, y.w & some)));
                 }
             }
             top = max(top & 0xFFFFu, top >> 16);
@@ -303,19 +327,19 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             q_scale *= two_to(-e);
 #pragma unroll 4
             for (int c = 0; c < D; c += 8) {
-                uint4 w = make_uint4(0, 0, 0, 0);
-                if (mine) w = *reinterpret_cast<const uint4*>(q + c);
-                uint32_t x[4] = {w.x, w.y, w.z, w.w};
+                uint4 y = make_uint4(0, 0, 0, 0);
+                if (mine) y = *reinterpret_cast<const uint4*>(q + c);
+                uint32_t x[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) x[i] = two_f16(__uint_as_float(x[i] << 16) * lift, __uint_as_float(x[i] & 0xFFFF0000u) * lift);
-                store16(q_at + swizzled(t, c / 8, kRows), x);
+                store16(q_at + w * (Sh::kDB * kRows * 128) + swizzled(r, c / 8, kRows), x);
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
             if (lane == 0) mbar_arrive(q_full);
         }
-        const uint32_t lanes = static_cast<uint32_t>(warp) << 21;            // this warp's 32 lanes
-        const uint32_t o_col = tmem + Sh::kO + lanes;
+        const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;        // this warp's 32 lanes
+        const uint32_t o_col = tmem + w * Sh::kOf + Sh::kO + lanes;
         float m = -CUDART_INF_F, l = 0.f;                    // reference (scaled), sum (of weights against the reference less kF16Lift)
         int unit = 0;                                        // byte of the scale that O is counted in
         bool masked = false;
@@ -324,17 +348,17 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             const int j0 = first_key(i);
             masked = masks(j0);
             if (!masked) return;
-            const int past = min(p, len - 1) - j0 + 1, first = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
+            const int past = min(p, len - 1) - j0 + 1, from = max(p - a.window + 1, 0) - j0, sink = a.n_sink - j0;
 #pragma unroll
-            for (int w = 0; w < kKeys / 32; ++w) visible[w] = below(past - 32 * w) & (~below(first - 32 * w) | below(sink - 32 * w));
+            for (int x = 0; x < kKeys / 32; ++x) visible[x] = below(past - 32 * x) & (~below(from - 32 * x) | below(sink - 32 * x));
         };
-        const auto scores_there = [&](int i) { return guard.wait_all(s_full + 8 * (i & 1), i / 2 & 1); };
+        const auto scores_there = [&](int i) { return guard.wait_all(s_full(w, i & 1), i / 2 & 1); };
         const auto weigh = [&](int i) {
             const int buf = i & 1;
             tc_fence_after();
             const int2 ref_of = refs[i % kTileRefs];
             const float scale = q_scale * two_to(ref_of.x - 127);
-            const uint32_t s_col = tmem + buf * kKeys + lanes;
+            const uint32_t s_col = tmem + w * Sh::kOf + buf * kKeys + lanes;
             float top;
             {
                 float x[kKeys];
@@ -357,17 +381,17 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             const bool larger = ref_of.y > unit;             // (of all rows alike)
             if (i > 0 && (larger || __any_sync(0xffffffffu, move))) {
                 // (the step before may still be adding; the one before that was complete before this S was)
-                if (!guard.wait_all(o_step, (i - 1) & 1)) return false;
+                if (!guard.wait_all(o_step(w), (i - 1) & 1)) return false;
                 tc_fence_after();
                 const float f = move ? ex2_approx(m - top) : 1.f, by = larger ? f * two_to(max(unit - ref_of.y, -126)) : f;
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     float o[32];
-                    uint32_t w[32];
+                    uint32_t y[32];
                     tmem_ld_cols<32>(o_col + c, o);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) w[k] = __float_as_uint(o[k] * by);
-                    tmem_st_cols<32>(o_col + c, w);
+                    for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(o[k] * by);
+                    tmem_st_cols<32>(o_col + c, y);
                 }
                 l *= f;
             }
@@ -380,7 +404,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
 #pragma unroll
             for (int c0 = 0; c0 < kKeys; c0 += 32) {
                 float x[32];
-                uint32_t w[16];
+                uint32_t weights[16];
                 tmem_ld_cols<32>(s_col + c0, x);
                 if (masked) {
 #pragma unroll
@@ -393,16 +417,16 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                     y = ex2_approx(y);
                     z = ex2_approx(z);
                     sums[c / 2 & 1] = add_f32x2(sums[c / 2 & 1], two_f32(y, z));
-                    w[c / 2] = two_f16(y, z);                // (rounded for the product alone)
+                    weights[c / 2] = two_f16(y, z);          // (rounded for the product alone)
                 }
-                tmem_st_cols<16>(s_col + c0 / 2, w);
+                tmem_st_cols<16>(s_col + c0 / 2, weights);
             }
             float even, odd;
             split_f32(add_f32x2(sums[0], sums[1]), even, odd);
             l = fmaf(even + odd, two_to(down), l);
             tmem_st_wait();
             tc_fence_before();
-            mbar_arrive(p_full + 8 * buf);
+            mbar_arrive(p_full(w, buf));
             return true;
         };
         bool ok = walk_tiles(0, n, 1, look, scores_there, weigh);
@@ -410,7 +434,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         if (ok && n > 0) ok = guard.wait_all(o_full, 0);
         tc_fence_after();
         const int64_t part = s.part0 + static_cast<int64_t>(part_of_seq) * s.n_q + i_row;
-        float* const sums = reinterpret_cast<float*>(raw + (q_at - smem_u32(raw)));       // of a cluster's CTA: element by element, the rows side by side
+        float* const sums = reinterpret_cast<float*>(raw + (q_at - smem_u32(raw))) + w * D * kRows;       // of a cluster's CTA: element by element, the rows side by side
         const float by = (l > 0.f ? two_to(unit - 127) * (s.parts > 1 || ranks > 1 ? 1.f : 1.f / l) : 0.f) * two_to(-kCodeLift);
         m -= kF16Lift;
         for (int c = 0; c < D && ok; c += 32) {
@@ -420,7 +444,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? o[k] * by : 0.f;
             if (ranks > 1) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) sums[(c + k) * kRows + t] = o[k];
+                for (int k = 0; k < 32; ++k) sums[(c + k) * kRows + r] = o[k];
                 continue;
             }
             if (!mine) continue;
@@ -434,7 +458,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                 for (int k = 0; k < 32; k += 8) store8(dst + k, o + k);
             }
         }
-        if (ranks > 1) row_ml[t] = make_float2(m, l);
+        if (ranks > 1) row_ml[w][r] = make_float2(m, l);
         if (mine && ok && ranks == 1) {
             if (s.parts > 1) a.part_ml[part * a.n_heads + head] = make_float2(m, l);
             else if (a.lse) a.lse[(s.q_row + i_row) * a.n_heads + head] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
@@ -445,7 +469,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
     if (ranks > 1) {                                         // (reached by all CTAs of the cluster, whoever gave up)
         cluster_arrive_release();
         cluster_wait_acquire();
-        if (t < kRows) join_cluster(a, s, q_at, smem_u32(row_ml), ranks, t, q0, per, head0, part_of_seq);
+        if (t < T * kRows) join_cluster(a, s, q_at + (t / kRows) * D * kRows * 4, smem_u32(row_ml[t / kRows]), ranks, t % kRows, q0 + t / kRows * per, per, head0, part_of_seq);
         cluster_arrive_release();                            // (nobody's sums are gone while another reads them)
         cluster_wait_acquire();
     }
@@ -455,13 +479,13 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
     }
 }
 
-template <int KIND, int D32>
+template <int KIND, int D32, int T>
 cudaError_t attend(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
 {
     static KernelSetup setup;
-    using Sh = PageTileShape<KIND, D32>;
+    using Sh = PageTileShape<KIND, D32, T>;
     const size_t smem = smem_for_tmem(Sh::kSmem, Sh::kColumns);              // (no CTA more than there is tensor memory for)
-    const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(page_tile_kernel<KIND, D32>), smem, Sh::kColumns);
+    const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(page_tile_kernel<KIND, D32, T>), smem, Sh::kColumns);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(static_cast<unsigned>(a.n_blocks) * static_cast<unsigned>(a.n_heads / a.pack) * static_cast<unsigned>(a.cluster));
@@ -474,27 +498,34 @@ cudaError_t attend(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = a.cluster > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, page_tile_kernel<KIND, D32>, a, pool);
+    return cudaLaunchKernelEx(&cfg, page_tile_kernel<KIND, D32, T>, a, pool);
+}
+template <int KIND, int D32>
+cudaError_t by_tiles(int row_tiles, const AttArgs& a, const PagePool& pool, cudaStream_t stream)
+{
+    if constexpr (D32 <= 4)                                  // (two tiles of rows of larger heads have no room in tensor memory)
+        if (row_tiles == 2) return attend<KIND, D32, 2>(a, pool, stream);
+    return attend<KIND, D32, 1>(a, pool, stream);
 }
 template <int KIND>
-cudaError_t by_dim(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
+cudaError_t by_dim(int row_tiles, const AttArgs& a, const PagePool& pool, cudaStream_t stream)
 {
     switch (a.head_dim / 32) {
-    case 2: return attend<KIND, 2>(a, pool, stream);
-    case 3: return attend<KIND, 3>(a, pool, stream);
-    case 4: return attend<KIND, 4>(a, pool, stream);
-    case 5: return attend<KIND, 5>(a, pool, stream);
-    case 6: return attend<KIND, 6>(a, pool, stream);
-    case 7: return attend<KIND, 7>(a, pool, stream);
-    default: return attend<KIND, 8>(a, pool, stream);
+    case 2: return by_tiles<KIND, 2>(row_tiles, a, pool, stream);
+    case 3: return by_tiles<KIND, 3>(row_tiles, a, pool, stream);
+    case 4: return by_tiles<KIND, 4>(row_tiles, a, pool, stream);
+    case 5: return by_tiles<KIND, 5>(row_tiles, a, pool, stream);
+    case 6: return by_tiles<KIND, 6>(row_tiles, a, pool, stream);
+    case 7: return by_tiles<KIND, 7>(row_tiles, a, pool, stream);
+    default: return by_tiles<KIND, 8>(row_tiles, a, pool, stream);
     }
 }
 
 }  // namespace
 
-cudaError_t launch_page_decode(int kind, const AttArgs& a, const PagePool& pool, cudaStream_t stream)
+cudaError_t launch_page_decode(int kind, int row_tiles, const AttArgs& a, const PagePool& pool, cudaStream_t stream)
 {
-    return kind == MVLA_PAGE_E4M3 ? by_dim<MVLA_PAGE_E4M3>(a, pool, stream) : by_dim<MVLA_PAGE_E2M1>(a, pool, stream);
+    return kind == MVLA_PAGE_E4M3 ? by_dim<MVLA_PAGE_E4M3>(row_tiles, a, pool, stream) : by_dim<MVLA_PAGE_E2M1>(row_tiles, a, pool, stream);
 }
 
 }  // namespace mvla
