@@ -229,7 +229,7 @@ inline AttendPlan plan_tokens(const ServeShape& c, int32_t batch, const mvla_seq
 // multiple of 64 keys to a CTA, at least 128), so that their CTAs fill whole rounds of those that fit: of one to four rounds, or no cut at all, what ends
 // first.  In us: the tiles of its longest part and 4 for its start and end, `tile` each (with another CTA beside it); 1 where a cluster joins; 5 for the kernel that joins
 // parts, and what their sums, written and read, take at 6 TB/s.
-constexpr double kTileUs = 1.3, kUnpackedTileUs = 2.2, kUnpackedPairUs = 1.4;
+constexpr double kTileUs = 1.3, kUnpackedTileUs = 2.2, kUnpackedPairUs = 1.7;
 inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, int row_tiles, double tile)
 {
     AttendPlan p;
@@ -299,16 +299,16 @@ inline bool page_by_tokens(int kind, int64_t rows, int64_t keys_and_heads)
     return rows <= kTokenRows && (kind != MVLA_PAGE_ROWS || (rows <= 8 && keys_and_heads < 32768));
 }
 
-// Whether so few blocks of queries go over a sequence's pages that each had better unpack them for itself: unpacking first costs 0.15 us for 1000 rows of a head (their
-// bytes, twice), on the way 0.06 us for every block that does.  us, on the way / first, 32 heads in groups of 4, e4m3: 5 tokens over 60000 rows (a block) 61 / 121;
-// 4 chunks of 56 over 2000 to 6000 (two) 52 / 57, of 33 over 4000 (two) 48 / 51; 100 over 4096 (four) 36 / 31; 512 over 8192 (16) 141 / 98.
+// Tiles of query rows that share what is unpacked on the way, 0: unpacked first.  Unpacking first costs 0.15 us for 1000 rows of a head (their bytes, twice), on the way every
+// CTA does it for one tile of rows or two (heads of up to 128 elements).  us, on the way / first, 32 heads in groups of 4, e4m3: 5 tokens over 60000 rows (one tile) 58 / 121; 4 chunks of
+// 56 over 3100 to 5500 (two) 48 / 57, of 33 over 4000 (two) 38 / 45; 100 over 4096 (four) 35 / 29; 512 over 8192 (16) 112 / 90.
 inline int32_t unpacked_row_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs)
 {
     const int64_t queries = 128 / pack_of(c.n_heads / c.kv_heads);
     int64_t most = 0;
     for (int b = 0; b < batch; ++b) most = std::max(most, (static_cast<int64_t>(seqs[b].n_q) + queries - 1) / queries);
     if (most <= 1) return 1;
-    return c.head_dim <= 128 ? (most <= 1000 ? 2 : 0) : most <= 2 ? 1 : 0;
+    return most > 2 ? 0 : c.head_dim <= 128 ? 2 : 1;
 }
 
 // fp32: as packed rows, but in blocks of 8 query rows where the call is so short that the CTAs of those run at once and a block's keys are few (208 rows of 8 heads of 64,

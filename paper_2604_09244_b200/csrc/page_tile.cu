@@ -2,18 +2,18 @@
 //
 // As attend_tile.cu: a CTA has a tile of 128 query rows that share a key head and walks the tiles of 64 keys of its part,
 //     S = Q K^T  ->  P = 2^(S - reference) in fp16, back into the columns of S  ->  O += P V,
-// a thread to a row in the softmax (warps 0-3), S double-buffered, one warp that issues the MMAs.  A warp copies codes and scales into a ring, 16 rows of a page at
-// a time; four warps turn them into fp16 and store them as the MMAs read them (128-byte swizzle).
+// a thread to a row in the softmax (warps 0-3), S double-buffered, one warp that issues the MMAs.  A warp copies codes and scales into a ring, what a tile has of
+// a page at a time; four warps turn them into fp16 and store them as the MMAs read them (128-byte swizzle).
 // Scales are powers of two.  A tile's largest scale of its keys becomes a factor of its scores and the largest one of its values a factor of its weights (both the same
 // for the whole tile); what a row, or 32 elements, have less is multiplied into the codes, which have as much room above in fp16 (2^7 for e4m3, 2^13 for e2m1): rows or
 // groups below 2^-21 (2^-27) of their tile's largest scale count as nothing.  Outputs are summed in units of the largest values so far (and four
 // times more); where a tile's are larger still, the sums are taken down, as they are when a row's reference moves.  Queries are fp16 too, every row times a
 // power of two that puts its largest element between 2^14 and 2^15.
 //
-// Two CTAs to a multiprocessor (heads of up to 128 elements; 96 registers, 40 bytes spill, and the softmax reads S twice).  B200, 32 query heads over 8 heads of 128, e4m3: 5 tokens over 60000
-// rows 60 us, 4 chunks of 56 over 3100 to 5500 rows 51 with the join behind, 45 without.  A tile takes 2.2 us, 1.9 without unpacking all but an eighth; no pipe is busy half of the time:
-// what takes it is its way from warp to warp.  The codes a tile ahead in registers instead of a ring: half as long again (a warp's loads wait for one another).  Four tiles of fp16
-// instead of three, two slots of the ring instead of three: the same.
+// A CTA has one tile of query rows (two CTAs to a multiprocessor, heads of up to 128 elements; 96 registers, 40 bytes spill), or two that share what is unpacked (one CTA); the softmax reads S
+// twice, once for its maximum.  B200, 32 query heads over 8 heads of 128, e4m3: 5 tokens over 60000 rows 58 us, 4 chunks of 56 over 3100 to 5500 rows 48 (one tile of rows to a CTA: 51), of 33
+// over 4000 rows 38 (45).  Two tiles of rows and 64 keys take 1.7 us, as in attend_tile.cu: without the exponentials, without most of the unpacking or of the second product 0 to 10 % less, so that it
+// is the way of a tile from warp to warp.  The codes a tile ahead in registers instead of a ring: half as long again (a warp's loads wait for one another); twice the ring: the same.
 #include "attend_tile.cuh"
 #include "attend_walk.h"
 #include "page.cuh"
@@ -141,7 +141,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
 
     if (warp == Sh::kLoads) {
         // ---- codes and scales: chunk 2 i the keys of tile i and both scales, chunk 2 i + 1 its values; a lane to every 16 rows, of which the first of a page copies
-        // what the tile has of it (a copy is dear, however small: 16 rows at a time a tile takes 1.5 times as long)
+        // what the tile has of it (4 chunks of 56: 16 rows at a time, and from pages of 16, 51.5 us, 64 rows 48)
         const int rows = min(kKeys, 1 << pool.page_shift);
         const bool copies = lane < 4 && (16 * lane & (rows - 1)) == 0;
         const auto look_up = [&](int i) {
