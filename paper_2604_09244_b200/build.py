@@ -17,7 +17,7 @@ CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libmvla_prune.so")
 EXT = os.path.join(PKG, "_native" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cu", "salience.cu", "fused.cu", "stream.cu", "select.cu", "compact.cu", "step.cu", "patch.cu", "patch_step.cu", "salience_noalloc.cu",
-           "serve_api.cu", "page_api.cu", "page_rows.cu", "page_token.cu", "page_tile.cu", "rope.cu", "attend_fma.cu", "attend_tile.cu", "attend_token.cu", "attend_join.cu", "evict.cu"]
+           "serve_api.cu", "page_api.cu", "page_rows.cu", "page_fma.cu", "page_token.cu", "page_tile.cu", "rope.cu", "attend_fma.cu", "attend_tile.cu", "attend_token.cu", "attend_join.cu", "evict.cu"]
 BINDING = "binding.cpp"
 HEADER = os.path.join(ROOT, "include", "mvla_prune.h")
 

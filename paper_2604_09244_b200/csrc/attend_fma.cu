@@ -41,15 +41,6 @@ __device__ __forceinline__ void copy_keys(float* dst, int pitch, const float* sr
         for (int c = threadIdx.x % 8 * 4; c < d; c += 32) copy16(dst + r * pitch + c, row + c, there);
     }
 }
-// The same of rows that lie anywhere, `at` of them (negative: zeros), of d elements each.
-__device__ __forceinline__ void copy_keys_at(float* dst, int pitch, const float* src, const int64_t* at, int d, const int* pos)
-{
-    for (int r = threadIdx.x / 8; r < kTile; r += kThreads / 8) {
-        const bool there = pos[r] >= 0 && at[r] >= 0;
-        const float* const row = there ? src + at[r] * d : src;
-        for (int c = threadIdx.x % 8 * 4; c < d; c += 32) copy16(dst + r * pitch + c, row + c, there);
-    }
-}
 // n rows from rr on (query rr / group, head rr % group of the group) of a sequence whose queries begin at `q`; zeros up to R.
 template <int R>
 __device__ __forceinline__ void copy_queries(float* dst, const float* q, int rr, int n, int group, int n_heads, int d)
@@ -91,14 +82,13 @@ __device__ __forceinline__ void dots(float (&s)[RT][kKeys], const float* q, cons
 
 size_t attend_smem(int rows, int d) { return sizeof(float) * (static_cast<size_t>(rows) * (d + kPitch) + kTile * (2 * d + 4)); }
 
-// RT: rows of a half warp.  NC: columns of a thread, in fours, 64 apart.  PAGED: keys and values lie in pages; positions are counted.
-template <int RT, int NC, bool PAGED>
+// RT: rows of a half warp.  NC: columns of a thread, in fours, 64 apart.
+template <int RT, int NC>
 __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_constant__ AttArgs a)
 {
     constexpr int R = 8 * RT;
     extern __shared__ __align__(16) float sm[];
     __shared__ int row_p[R], pos[2][kTile];
-    __shared__ int64_t at[2][PAGED ? kTile : 1];             // where a tile's rows lie, in rows
     const int d = a.head_dim, t = threadIdx.x;
     float* const ks = sm;
     float* const vs = ks + kTile * (d + 4);
@@ -121,40 +111,23 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
     const int per_split = (range.count + a.splits - 1) / a.splits;
     const int t0 = static_cast<int>(blockIdx.z) * per_split, t1 = min(range.count, t0 + per_split);
     const int64_t stride = static_cast<int64_t>(a.kv_heads) * d;
-    const float* const k = static_cast<const float*>(a.k) + (PAGED ? 0 : s.kv_row * stride + static_cast<int64_t>(hk) * d);
-    const float* const v = static_cast<const float*>(a.v) + (PAGED ? 0 : s.kv_row * stride + static_cast<int64_t>(hk) * d);
-    const TileRange all = PAGED && !a.table ? tile_range(a, len, query_pos(a, s, len, 0), query_pos(a, s, len, s.n_q - 1), kTile) : TileRange{0, 0, 0};
-    // page of this thread's key of tile `it` (without a table: the tile's place among those that the sequence's queries see)
-    const auto page_at = [&](int it) {
-        if (!PAGED || t >= kTile || it >= t1) return -1;
-        const int tile = range.tile(it), j = tile * kTile + t;
-        if (j >= len) return -1;
-        if (!a.table) return s.km_row + (tile < all.sinks ? tile : tile - all.first + all.sinks);
-        const int page = a.table[s.index * a.table_stride + (j >> a.page_shift)];
-        return page >= 0 && page < a.n_pages ? page : -1;
-    };
-    const auto copy = [&](float* dst, int pitch, const float* src, int it, int buf) {
-        if constexpr (PAGED) copy_keys_at(dst, pitch, src, at[buf], d, pos[buf]);
-        else copy_keys(dst, pitch, src + range.tile(it) * static_cast<int64_t>(kTile) * stride, stride, d, pos[buf]);
-    };
+    const float* const k = static_cast<const float*>(a.k) + s.kv_row * stride + static_cast<int64_t>(hk) * d;
+    const float* const v = static_cast<const float*>(a.v) + s.kv_row * stride + static_cast<int64_t>(hk) * d;
 
     // The first tile from `it` on with a key that some row sees (t1: none), its positions in pos[buf], -1 for keys that no row sees (what they hold
     // is left out then); a barrier of the CTA at least once.
     const auto look = [&](int it) { return t < kTile && it < t1 ? key_pos(a, s, len, range.tile(it) * kTile + t) : -1; };
-    const auto find = [&](int it, int c, int page, int buf) {
+    const auto find = [&](int it, int c, int buf) {
         while (true) {
             bool seen = some_sees(lo, hi, c, a.window, a.n_sink);
-            if (!PAGED && seen && a.q_pos) {                           // (queries may lie far apart)
+            if (seen && a.q_pos) {                           // (queries may lie far apart)
                 seen = false;
                 for (int r = 0; r < n_rows && !seen; ++r) seen = sees(row_p[r], c, a.window, a.n_sink);
             }
             if (t < kTile) pos[buf][t] = seen ? c : -1;
-            if (PAGED && t < kTile)
-                at[buf][t] = page < 0 ? -1 : ((static_cast<int64_t>(page) * a.kv_heads + hk) << a.page_shift) + ((range.tile(it) * kTile + t) & ((1 << a.page_shift) - 1));
             if (__syncthreads_or(seen)) return it;
             if (it >= t1) return t1;
             c = look(++it);
-            page = page_at(it);
         }
     };
     const int rq = t / 16 * RT, kq = t % 16;
@@ -163,14 +136,14 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
     int p[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) { m[i] = -CUDART_INF_F; l[i] = 0.f; p[i] = row_p[rq + i]; }
-    int buf = 0, it = find(t0, look(t0), page_at(t0), 0);
-    if (it < t1) copy(ks, d + 4, k, it, 0);
+    int buf = 0, it = find(t0, look(t0), 0);
+    if (it < t1) copy_keys(ks, d + 4, k + range.tile(it) * static_cast<int64_t>(kTile) * stride, stride, d, pos[0]);
     copies_issued();
     while (it < t1) {
-        const int c_next = look(it + 1), page_next = page_at(it + 1);
+        const int c_next = look(it + 1);
         wait_copies<0>();
         __syncthreads();                                     // the keys are there; nobody reads the values any more
-        copy(vs, d, v, it, buf);
+        copy_keys(vs, d, v + range.tile(it) * static_cast<int64_t>(kTile) * stride, stride, d, pos[buf]);
         copies_issued();
         float x[RT][kKeys], f[RT] = {};
         if (works) {
@@ -200,8 +173,8 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
             }
         }
         wait_copies<0>();
-        const int next = find(it + 1, c_next, page_next, buf ^ 1);      // the values are there; nobody reads the keys any more
-        if (next < t1) copy(ks, d + 4, k, next, buf ^ 1);
+        const int next = find(it + 1, c_next, buf ^ 1);      // the values are there; nobody reads the keys any more
+        if (next < t1) copy_keys(ks, d + 4, k + range.tile(next) * static_cast<int64_t>(kTile) * stride, stride, d, pos[buf ^ 1]);
         copies_issued();
         if (works) {
 #pragma unroll
@@ -254,7 +227,7 @@ __global__ void __launch_bounds__(kThreads) attend_fma_kernel(const __grid_const
         if (whole) {
             const float z = l[i] > 0.f ? m[i] + log2f(l[i]) : -CUDART_INF_F;
             if (a.lse) a.lse[(s.q_row + query) * a.n_heads + h] = z * 0.69314718055994531f;      // ln 2
-            if (!PAGED && a.mass) a.lse2[static_cast<int64_t>(s.qp0 + query) * a.n_heads + h] = z;
+            if (a.mass) a.lse2[static_cast<int64_t>(s.qp0 + query) * a.n_heads + h] = z;
         } else {
             a.part_ml[part] = make_float2(m[i], l[i]);
         }
@@ -356,31 +329,27 @@ cudaError_t launch(KernelSetup& setup, K kernel, dim3 grid, size_t smem, const A
     return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
-template <int RT, int NC, bool PAGED>
+template <int RT, int NC>
 cudaError_t attend(const AttArgs& a, cudaStream_t stream)
 {
     static KernelSetup setup;
-    return launch(setup, attend_fma_kernel<RT, NC, PAGED>, dim3(static_cast<unsigned>(a.n_blocks), static_cast<unsigned>(a.kv_heads), static_cast<unsigned>(a.splits)),
+    return launch(setup, attend_fma_kernel<RT, NC>, dim3(static_cast<unsigned>(a.n_blocks), static_cast<unsigned>(a.kv_heads), static_cast<unsigned>(a.splits)),
                   attend_smem(8 * RT, a.head_dim), a, stream);
 }
-template <int RT, bool PAGED>
+template <int RT>
 cudaError_t attend(const AttArgs& a, cudaStream_t stream)
 {
     switch ((a.head_dim + 63) / 64) {
-    case 1: return attend<RT, 1, PAGED>(a, stream);
-    case 2: return attend<RT, 2, PAGED>(a, stream);
-    case 3: return attend<RT, 3, PAGED>(a, stream);
-    default: return attend<RT, 4, PAGED>(a, stream);                // (256 at most: the context's rule)
+    case 1: return attend<RT, 1>(a, stream);
+    case 2: return attend<RT, 2>(a, stream);
+    case 3: return attend<RT, 3>(a, stream);
+    default: return attend<RT, 4>(a, stream);                // (256 at most: the context's rule)
     }
 }
 
 }  // namespace
 
-cudaError_t launch_attend_fma(const AttArgs& a, int rows, cudaStream_t stream)
-{
-    return rows == 8 ? attend<1, false>(a, stream) : attend<4, false>(a, stream);
-}
-cudaError_t launch_page_fma(const AttArgs& a, int rows, cudaStream_t stream) { return rows == 8 ? attend<1, true>(a, stream) : attend<4, true>(a, stream); }
+cudaError_t launch_attend_fma(const AttArgs& a, int rows, cudaStream_t stream) { return rows == 8 ? attend<1>(a, stream) : attend<4>(a, stream); }
 
 cudaError_t launch_mass_fma(const AttArgs& a, cudaStream_t stream)
 {

@@ -49,4 +49,7 @@ cudaError_t launch_page_token(int kind, const AttArgs& a, const PagePool& pool, 
 // Blocks of `row_tiles` (1, or 2 for heads of up to 128 elements) tiles of 128 query rows over quantised pages, unpacked on the way; q and out bf16.  Behind it: launch_attend_join.
 cudaError_t launch_page_decode(int kind, int row_tiles, const AttArgs& a, const PagePool& pool, cudaStream_t stream);
 
+// fp32, by FMAs, in blocks of 8 query rows.  Behind it: launch_attend_join.
+cudaError_t launch_page_fma(const AttArgs& a, cudaStream_t stream);
+
 }  // namespace mvla

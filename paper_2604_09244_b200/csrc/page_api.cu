@@ -155,7 +155,7 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     if (plan.unpack) {
         e = launch_page_decode(a->pages.kind, plan.unpack, t, pool, st);
     } else if (plan.attend.form == kFormFma) {
-        e = launch_page_fma(t, plan.attend.rows, st);
+        e = launch_page_fma(t, st);
     } else {
         bool tokens = false;
         for (int b = 0; b < batch; ++b) {

@@ -97,7 +97,7 @@ inline int32_t check_page_rows(const ServeShape& v, int32_t batch, const mvla_se
 
 // ---- attention over pages
 
-constexpr int kPageTile = 64;                // keys of a tile (attend_tile.cu, attend_fma.cu)
+constexpr int kPageTile = 64;                // keys of a tile (attend_tile.cu), rows of an unpacked one
 
 struct PageAttendPlan {
     AttendPlan attend;
@@ -311,19 +311,32 @@ inline int32_t unpacked_row_tiles(const ServeShape& c, int32_t batch, const mvla
     return most > 2 ? 0 : c.head_dim <= 128 ? 2 : 1;
 }
 
-// fp32: as packed rows, but in blocks of 8 query rows where the call is so short that the CTAs of those run at once and a block's keys are few (208 rows of 8 heads of 64,
-// window 64, 16.6 us instead of 22.4; 64 queries of 32 heads of 128 over 564 rows would take 82 instead of 44: a block copies all keys).
+// fp32: blocks of 8 query rows, every sequence's keys cut into as many parts, 64 at most: of all such cuts the one that ends first, in rounds of a CTA's warps over 16 keys
+// each (2 us): those of its longest part and 1.5 for its start and end, for every round of the CTAs that fit, and 2 for the kernel that joins parts (one token over 2000 rows of 8 heads
+// of 64: 7 parts of three rounds 12.5 us, 16 of one 8.0; over 300 rows of heads of 128 one part 14.5, five 8.0).
 inline AttendPlan plan_page_fma(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink)
 {
-    AttendPlan p = plan_attend(c, batch, seqs, counted, window, n_sink, false);
-    int64_t blocks = 0, longest = 0;
+    AttendPlan p;
+    p.rows = 8;
+    int64_t longest = 0;
     for (int b = 0; b < batch; ++b) {
-        blocks += (static_cast<int64_t>(seqs[b].n_q) * (c.n_heads / c.kv_heads) + 7) / 8;
+        p.total_q += seqs[b].n_q;
+        p.total_kv += seqs[b].n_kv;
+        p.blocks += (static_cast<int64_t>(seqs[b].n_q) * (c.n_heads / c.kv_heads) + 7) / 8;
         if (seqs[b].n_q) longest = std::max(longest, visible_keys(seqs[b], counted, window, n_sink));
     }
-    if (p.splits == 1 && blocks * c.kv_heads <= 2 * static_cast<int64_t>(c.sm_count) && longest * c.head_dim <= 16384) {
-        p.rows = 8;
-        p.blocks = blocks;
+    const int64_t slots = static_cast<int64_t>(c.sm_count) * page_fma_ctas(c.head_dim / 32), keys = 16 * page_fma_warps(c.head_dim / 32);
+    double best = 0;
+    for (int64_t n = 1; n <= 64; ++n) {
+        const int64_t part = (longest + n - 1) / n;
+        const double cost = static_cast<double>((p.blocks * c.kv_heads * n + slots - 1) / slots) * (static_cast<double>((part + keys - 1) / keys) + 1.5) + (n > 1 ? 2 : 0);
+        if (n == 1 || cost < best) { best = cost; p.splits = static_cast<int32_t>(n); }
+    }
+    if (p.splits > 1) {
+        Workspace w;
+        p.part_o = w.take(p.total_q * p.splits * c.n_heads * c.head_dim * static_cast<int64_t>(sizeof(float)));
+        p.part_ml = w.take(p.total_q * p.splits * c.n_heads * 2 * static_cast<int64_t>(sizeof(float)));
+        p.bytes = w.bytes;
     }
     return p;
 }

@@ -33,9 +33,13 @@ MVLA_BOTH constexpr int page_token_tile(int kind, int pieces_of_32)
 MVLA_BOTH constexpr int page_token_ctas(int kind, int pieces_of_32, int groups)
 {
     // queries, factors of the scales, and what the system takes; registers: four CTAs leave 128 to a thread, three 168, two 255
-    const int fixed = 512 * groups * pieces_of_32 + (kind == MVLA_PAGE_E2M1 ? 256 * page_token_sub(kind, pieces_of_32) * pieces_of_32 : 0) + 3072;
+    const int fixed = 512 * groups * pieces_of_32 + (kind == MVLA_PAGE_E2M1 ? 256 * page_token_sub(kind, pieces_of_32) * pieces_of_32 : 0) + 3 * 1024;
     const int n = 227 * 1024 / (4 * kPageTokenStages * page_token_tile(kind, pieces_of_32) + fixed), most = groups == 1 ? (pieces_of_32 <= 6 ? 4 : 3) : pieces_of_32 <= 2 ? 3 : 2;
     return n > most ? most : n < 1 ? 1 : n;
 }
+
+// Few fp32 rows (page_fma.cu): warps of a CTA, and the CTAs that fit on a multiprocessor.
+MVLA_BOTH constexpr int page_fma_warps(int pieces_of_32) { return pieces_of_32 <= 2 ? 8 : 4; }
+MVLA_BOTH constexpr int page_fma_ctas(int pieces_of_32) { return pieces_of_32 <= 2 ? 2 : pieces_of_32 <= 4 ? 3 : pieces_of_32 <= 6 ? 2 : 1; }
 
 }  // namespace mvla

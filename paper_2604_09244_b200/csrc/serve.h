@@ -63,8 +63,6 @@ struct AttArgs {
 
 // fp32, by FMAs: any shape, in blocks of `rows` (8 or 32) query rows.
 cudaError_t launch_attend_fma(const AttArgs& a, int rows, cudaStream_t stream);
-// The same over pages.
-cudaError_t launch_page_fma(const AttArgs& a, int rows, cudaStream_t stream);
 // The weights of every cached row over the queries of its sequence, by key head, into part_mass (by FMAs in 32 bits).
 cudaError_t launch_mass_fma(const AttArgs& a, cudaStream_t stream);
 // bf16 (f16: what launch_widen made) by tiles of 128 rows on the tensor cores; at most kMaxTiles tiles of keys to a split.
@@ -89,10 +87,8 @@ cudaError_t launch_attend_join(int dtype, const AttArgs& a, cudaStream_t stream)
 // mass += part_mass over its parts.
 cudaError_t launch_mass_add(const AttArgs& a, cudaStream_t stream);
 
-// What the kernels of a checked call are given; what it enqueues, and its status.
+// What the kernels of a checked call are given.
 void fill_attention(AttArgs& k, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan);
-int32_t enqueue_attention(mvla_ctx* ctx, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan,
-                          cudaStream_t stream);
 
 // ---- eviction by accumulated weight
 

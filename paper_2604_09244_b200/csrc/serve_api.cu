@@ -132,27 +132,6 @@ void fill_attention(AttArgs& k, const CtxView& v, int32_t batch, const mvla_seq*
     }
 }
 
-int32_t enqueue_attention(mvla_ctx* ctx, const CtxView& v, int32_t batch, const mvla_seq* seqs, const mvla_attention* a, const AttendPlan& plan, cudaStream_t st)
-{
-    AttArgs k;
-    fill_attention(k, v, batch, seqs, a, plan);
-    cudaError_t e = cudaSuccess;
-    if (plan.form == kFormTile) {
-        const int32_t rc = attend_by_tiles(v, k, a, plan, &e, st);
-        if (rc != MVLA_OK) return rc;
-    } else if (plan.form == kFormToken) {
-        e = launch_attend_token(v.dtype, k, plan.rows, st);
-        if (e == cudaSuccess && (plan.splits > 1 || a->mass)) e = launch_attend_finish(k, st);
-        return close_call(ctx, e);
-    } else {
-        e = launch_attend_fma(k, plan.rows, st);
-        if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);
-        if (e == cudaSuccess && a->mass) e = launch_mass_fma(k, st);
-    }
-    if (e == cudaSuccess && a->mass) e = launch_mass_add(k, st);
-    return close_call(ctx, e);
-}
-
 }  // namespace mvla
 
 namespace {
@@ -171,7 +150,24 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
     DeviceGuard guard(v.device);
     if (!guard.ok) return MVLA_ERR_CUDA;
     note_work(ctx);
-    return enqueue_attention(ctx, v, batch, seqs, a, plan, static_cast<cudaStream_t>(stream));
+    AttArgs k;
+    fill_attention(k, v, batch, seqs, a, plan);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    cudaError_t e = cudaSuccess;
+    if (plan.form == kFormTile) {
+        rc = attend_by_tiles(v, k, a, plan, &e, st);
+        if (rc != MVLA_OK) return rc;
+    } else if (plan.form == kFormToken) {
+        e = launch_attend_token(v.dtype, k, plan.rows, st);
+        if (e == cudaSuccess && (plan.splits > 1 || a->mass)) e = launch_attend_finish(k, st);
+        return close_call(ctx, e);
+    } else {
+        e = launch_attend_fma(k, plan.rows, st);
+        if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);
+        if (e == cudaSuccess && a->mass) e = launch_mass_fma(k, st);
+    }
+    if (e == cudaSuccess && a->mass) e = launch_mass_add(k, st);
+    return close_call(ctx, e);
 }
 
 int32_t evict_workspace_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const mvla_eviction* a, int64_t* bytes)

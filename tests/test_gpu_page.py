@@ -277,3 +277,50 @@ def test_rows_that_nobody_sees_may_hold_anything(kind, n_q):
     got = ctx.page_attention(pool, seqs, table, q, window=window, n_sink=2)
     want = ctx.page_attention(mvla.PagePool(*clean), seqs, table, q, window=window, n_sink=2)
     assert torch.isfinite(got).all() and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("kind", [ROWS, E4M3])
+@pytest.mark.parametrize("H,G,d,page_rows,seqs,window,n_sink", [
+    (8, 8, 64, 16, [(1, 1), (1, 17), (1, 4000)], None, 0),                  # cut into parts, more of them than the short ones have rows
+    (6, 2, 96, 32, [(3, 900), (0, 5), (5, 40)], None, 0),                   # rows of two queries in a block
+    (16, 2, 128, 64, [(1, 700), (2, 130)], 100, 5),
+    (4, 4, 160, 256, [(33, 33), (7, 300)], 31, 0),
+    (8, 4, 192, 128, [(2, 0), (5, 3), (9, 500)], None, 0),                  # more rows than are cached: those before row 0 see nothing
+    (7, 7, 224, 16, [(20, 2000)], 1, 40),
+    (8, 1, 256, 64, [(5, 1000), (1, 63)], 640, 64),
+])
+def test_fp32_blocks(kind, H, G, d, page_rows, seqs, window, n_sink):
+    """Blocks of 8 query rows, warps with a granule of 16 keys each and without, every size of heads."""
+    gen = generator(d + kind)
+    ctx = context(FP32, H, G, d)
+    lengths = [n for _, n in seqs]
+    table, n_pages = P.make_table(gen, lengths, page_rows)
+    pool = P.make_pool(gen, n_pages, G, page_rows, d, kind, FP32)
+    rows = [0]
+    for n_q, _ in seqs:
+        rows.append(rows[-1] + n_q + 1)
+    q = torch.randn(rows[-1], H, d, generator=gen, device="cuda")
+    seqs = [mvla.Seq(q_row=r, n_q=n_q, n_kv=n) for r, (n_q, n) in zip(rows, seqs)]
+    check_attention(ctx, pool, kind, seqs, table, q, page_rows, window=window, n_sink=n_sink)
+
+
+@pytest.mark.parametrize("n_q", [1, 3, 40])
+def test_fp32_rows_that_nobody_sees_may_hold_anything(n_q):
+    gen = generator(40 + n_q)
+    G, d, page_rows, n, window = 4, 64, 32, 1500, 90
+    ctx = context(FP32, 8, G, d)
+    table, n_pages = P.make_table(gen, [n], page_rows)
+    pool = P.make_pool(gen, n_pages, G, page_rows, d, ROWS, FP32)
+    clean = mvla.PagePool(pool.k.clone(), pool.v.clone())
+    seen = torch.zeros(n_pages, page_rows, dtype=torch.bool, device="cuda")
+    j = torch.arange(n - 9 - n_q - window + 1, n - 9, device="cuda")         # (nine rows of the descriptor's are not there yet)
+    seen[table[0].long()[j // page_rows], j % page_rows] = True
+    seen[table[0, 0], :3] = True
+    for t in (pool.k, pool.v):
+        t.masked_fill_(~seen[:, None, :, None], float("nan"))
+    q = torch.randn(n_q, 8, d, generator=gen, device="cuda")
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    kv_len = torch.tensor([n - 9], dtype=torch.int32, device="cuda")
+    got = ctx.page_attention(pool, seqs, table, q, window=window, n_sink=3, kv_len=kv_len)
+    want = ctx.page_attention(clean, seqs, table, q, window=window, n_sink=3, kv_len=kv_len)
+    assert torch.isfinite(got).all() and torch.equal(got, want)

@@ -116,3 +116,20 @@ def test_parts_cover_and_fit(shim, seed):
         assert p["splits"] == max(parts for parts, _ in per)
         if p["splits"] > 1:
             assert p["part_ml"] >= p["part_o"] + results * heads[0] * heads[2] * 4 and p["attend_bytes"] >= p["part_ml"] + results * heads[0] * 8
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_fp32_parts_fit(shim, seed):
+    rng = random.Random(seed + 20)
+    for _ in range(300):
+        heads = rng.choice([(32, 8, 128), (8, 8, 64), (16, 16, 256), (28, 4, 96), (64, 1, 64)])
+        seqs = [(rng.randint(0, rng.choice([1, 3, 400])), rng.choice([0, 1, rng.randint(1, 1 << rng.randint(1, 20))])) for _ in range(rng.choice([1, 3, 64]))]
+        kind = rng.choice([ROWS, E4M3])
+        p, per = plan(shim, seqs, kind=kind, dtype=FP32, heads=heads)
+        assert p["form"] == FMA and 1 <= p["splits"] <= 64
+        for (q, _), (parts, _) in zip(seqs, per):
+            assert parts == (p["splits"] if q else 0)
+        if p["splits"] > 1:
+            results = p["splits"] * sum(q for q, _ in seqs)
+            assert p["part_ml"] >= p["part_o"] + results * heads[0] * heads[2] * 4 and p["attend_bytes"] >= p["part_ml"] + results * heads[0] * 8
+            assert kind == ROWS or p["dense_k"] < 0 or p["dense_k"] >= p["attend_bytes"]
