@@ -290,13 +290,19 @@ inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla
     return p;
 }
 
-// Few query rows to a key head: the token form unpacks quantised rows as it reads them, where the tile form has them unpacked first.  Rows of their own type
-// go to the tile form, whose larger copies win although its rows are mostly empty, but for the shortest calls (us, token / tile form, one token of 32 heads
-// over 8 heads of 128: 800 rows 13.3 / 17.4, 4000 19.5 / 19.5, 16000 35.8 / 29.7, 131071 138 / 112; over 32 heads: 800 rows 17.4 / 19.5, 4000 31.7 / 29.7; four tokens
-// over 200 rows 25.6 / 15.4; 16 tokens over 500 to 4000 rows 60 / 50).
-inline bool page_by_tokens(int kind, int64_t rows, int64_t keys_and_heads)
+// Few query rows to a key head: the token form unpacks quantised rows as it reads them, where the tile form has them unpacked first.  Rows of their own type: the tile form's
+// larger copies win over long sequences, although its rows are mostly empty; its start and end take 3 to 10 us longer.  `keys`: of the batch, `mean`: of a sequence.  us, token / tile
+// form.  Heads of 64, 32 over 8: one token over 1000 rows 6.3 / 10.2, over 60000 35 / 35, 64 requests over 500 to 1500 39 / 53; four tokens over 8000 17.4 / 15.2, 64 requests 48 / 52.  Of
+// 96, 16 heads: one token over 60000 rows 82 / 79, 16 requests over 1300 to 4000 66 / 72.  Of 128, 32 over 8: one token over 1000 7.7 / 12.8, over 8000 16.7 / 15.5, over 60000
+// 63 / 50, 64 requests over 170 to 500 33 / 34, 16 over 1300 to 4000 49 / 44; four tokens over 1000 11.1 / 13.0, 16 requests over 130 to 400 16.7 / 16.2, over 500 to 1500 29 / 27.  Of 256,
+// 32 over 8: one token over 1000 10.4 / 18.4, 16 requests over 500 to 1500 54 / 46, 64 over 170 to 500 78 / 76; 16 over 2, over 8000 24 / 19; ten tokens of 16 heads over 200 21 / 17.
+inline bool page_by_tokens(int kind, int head_dim, int64_t rows, int64_t keys, int64_t mean, int kv_heads)
 {
-    return rows <= kTokenRows && (kind != MVLA_PAGE_ROWS || (rows <= 8 && keys_and_heads < 32768));
+    if (rows > kTokenRows) return false;
+    if (kind != MVLA_PAGE_ROWS) return true;
+    const int64_t all = keys * kv_heads;
+    if (rows > 8) return head_dim <= 64 ? mean <= 4096 : head_dim <= 192 && mean <= 1280 && all <= 16384;
+    return head_dim <= 96 || mean <= (head_dim <= 192 ? 1280 : 512) || (all <= 32768 && (head_dim <= 192 || mean <= 1280));
 }
 
 // Tiles of query rows that share what is unpacked on the way, 0: unpacked first.  Unpacking first costs 0.15 us for 1000 rows of a head (their bytes, twice), on the way every
@@ -348,9 +354,13 @@ inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, co
     const bool counted = !a->kv_len;
     int64_t most_rows = 0;
     for (int b = 0; b < batch; ++b) most_rows = std::max(most_rows, seqs[b].n_q * static_cast<int64_t>(v.n_heads / v.kv_heads));
-    int64_t keys = 0;
-    for (int b = 0; b < batch; ++b) keys += seqs[b].n_q ? visible_keys(seqs[b], counted, a->window, a->n_sink) : 0;
-    const bool tokens = h.dtype != MVLA_DTYPE_FP32 && page_by_tokens(a->pages.kind, most_rows, keys * v.kv_heads);
+    int64_t keys = 0, active = 0;
+    for (int b = 0; b < batch; ++b) {
+        if (seqs[b].n_q == 0) continue;
+        keys += visible_keys(seqs[b], counted, a->window, a->n_sink);
+        ++active;
+    }
+    const bool tokens = h.dtype != MVLA_DTYPE_FP32 && page_by_tokens(a->pages.kind, v.head_dim, most_rows, keys, keys / std::max<int64_t>(active, 1), v.kv_heads);
     if (h.dtype != MVLA_DTYPE_FP32 && a->pages.kind != MVLA_PAGE_ROWS && !tokens) p.unpack = unpacked_row_tiles(h, batch, seqs);
     p.attend = h.dtype == MVLA_DTYPE_FP32 ? plan_page_fma(h, batch, seqs, counted, a->window, a->n_sink)
              : tokens ? plan_tokens(h, batch, seqs, counted, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32, most_rows <= 8 ? 1 : 2))

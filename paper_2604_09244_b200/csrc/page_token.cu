@@ -1,4 +1,4 @@
-// Attention of single tokens over a cache in pages: at most 16 query rows of a sequence share a key head.  e4m3 or e2m1, and for the shortest calls the rows' own type
+// Attention of single tokens over a cache in pages: at most 16 query rows of a sequence share a key head.  e4m3 or e2m1, and for small heads and short sequences the rows' own type
 // (bf16).
 //
 // Bound by the bytes of the pages, and by unpacking them.  A warp takes tiles of 16 or 32 keys as the registers that the tensor cores read (m16n8k16):
@@ -672,7 +672,7 @@ cudaError_t attend(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
 template <int KIND, int D32>
 cudaError_t by_rows(const AttArgs& a, const PagePool& pool, int rows, cudaStream_t stream)
 {
-    if constexpr (KIND != MVLA_PAGE_ROWS)                    // (rows of their own type: eight at most, page_by_tokens)
+    if constexpr (KIND != MVLA_PAGE_ROWS || D32 <= 6)        // (page_by_tokens)
         if (rows > 8) return attend<KIND, D32, 2>(a, pool, stream);
     return attend<KIND, D32, 1>(a, pool, stream);
 }

@@ -324,3 +324,19 @@ def test_fp32_rows_that_nobody_sees_may_hold_anything(n_q):
     got = ctx.page_attention(pool, seqs, table, q, window=window, n_sink=3, kv_len=kv_len)
     want = ctx.page_attention(clean, seqs, table, q, window=window, n_sink=3, kv_len=kv_len)
     assert torch.isfinite(got).all() and torch.equal(got, want)
+
+
+@pytest.mark.parametrize("d", [64, 96, 128, 160, 192, 224, 256])
+@pytest.mark.parametrize("H,G,n_q", [(4, 4, 1), (8, 2, 2), (6, 2, 3), (2, 1, 8), (2, 2, 16)])
+def test_few_rows_of_their_own_type(d, H, G, n_q):
+    """Short sequences over bf16 pages, up to 16 query rows to a key head, every size of heads; rows that see nothing."""
+    gen = generator(d + n_q)
+    page_rows = 16
+    ctx = context(BF16, H, G, d)
+    lengths = [n_q, 0, 300, 65, 1]
+    table, n_pages = P.make_table(gen, lengths, page_rows)
+    pool = P.make_pool(gen, n_pages, G, page_rows, d, ROWS, BF16)
+    seqs = [mvla.Seq(q_row=20 * i, n_q=n_q, n_kv=n) for i, n in enumerate(lengths)]
+    q = torch.randn(100, H, d, generator=gen, device="cuda").to(BF16)
+    check_attention(ctx, pool, ROWS, seqs, table, q, page_rows)
+    check_attention(ctx, pool, ROWS, seqs, table, q, page_rows, window=40, n_sink=2)
