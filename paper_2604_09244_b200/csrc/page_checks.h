@@ -292,16 +292,16 @@ inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla
 
 // Few query rows to a key head: the token form unpacks quantised rows as it reads them, where the tile form has them unpacked first.  Rows of their own type: the tile form's
 // larger copies win over long sequences, although its rows are mostly empty; its start and end take 3 to 10 us longer.  `keys`: of the batch, `mean`: of a sequence.  us, token / tile
-// form.  Heads of 64, 32 over 8: one token over 1000 rows 6.3 / 10.2, over 60000 35 / 35, 64 requests over 500 to 1500 39 / 53; four tokens over 8000 17.4 / 15.2, 64 requests 48 / 52.  Of
+// form.  Heads of 64, 32 over 8: one token over 1000 rows 6.3 / 10.2, over 60000 35 / 35, 64 requests over 500 to 1500 39 / 53; four tokens over 1000 7.2 / 10.4, over 8000 15.5 / 15.2, 64 requests 48 / 52.  Of
 // 96, 16 heads: one token over 60000 rows 82 / 79, 16 requests over 1300 to 4000 66 / 72.  Of 128, 32 over 8: one token over 1000 7.7 / 12.8, over 8000 16.7 / 15.5, over 60000
-// 63 / 50, 64 requests over 170 to 500 33 / 34, 16 over 1300 to 4000 49 / 44; four tokens over 1000 11.1 / 13.0, 16 requests over 130 to 400 16.7 / 16.2, over 500 to 1500 29 / 27.  Of 256,
-// 32 over 8: one token over 1000 10.4 / 18.4, 16 requests over 500 to 1500 54 / 46, 64 over 170 to 500 78 / 76; 16 over 2, over 8000 24 / 19; ten tokens of 16 heads over 200 21 / 17.
+// 63 / 50, 64 requests over 170 to 500 33 / 34, 16 over 1300 to 4000 49 / 44; four tokens over 1000 9.6 / 13.0, four requests over 500 to 1500 13.7 / 15.9, 16 29.7 / 26.8.  Of 256,
+// 32 over 8: one token over 1000 10.4 / 18.4, 16 requests over 500 to 1500 54 / 46, 64 over 170 to 500 78 / 76; 16 over 2, over 8000 24 / 19.
 inline bool page_by_tokens(int kind, int head_dim, int64_t rows, int64_t keys, int64_t mean, int kv_heads)
 {
     if (rows > kTokenRows) return false;
     if (kind != MVLA_PAGE_ROWS) return true;
     const int64_t all = keys * kv_heads;
-    if (rows > 8) return head_dim <= 64 ? mean <= 4096 : head_dim <= 192 && mean <= 1280 && all <= 16384;
+    if (rows > 8) return head_dim <= 64 ? mean <= 4096 : head_dim <= 192 && mean <= 1280 && all <= 40960;
     return head_dim <= 96 || mean <= (head_dim <= 192 ? 1280 : 512) || (all <= 32768 && (head_dim <= 192 || mean <= 1280));
 }
 

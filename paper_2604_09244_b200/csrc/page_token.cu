@@ -139,7 +139,7 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ uint4 q_frag[D32][NR][32];
     __shared__ float merge_m[kWarps][16], merge_f[kWarps][16], merge_l[kWarps][16];
-    __shared__ float2 cta_ml[16], peer_ml[kMaxCluster][8];
+    __shared__ float2 cta_ml[16], peer_ml[kMaxCluster][8 * NR];
     __shared__ float q_lift[16], q_scale[16];                // what a row's queries are multiplied by; what that makes of the scores' scale
     __shared__ __align__(4) uint16_t factors[kE2m1 ? kWarps : 1][kE2m1 ? U : 1][2][kE2m1 ? D32 : 1][16];      // of the groups of a tile's rows, fp16
     pdl_wait();
@@ -552,7 +552,7 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
         }
         if constexpr (kE2m1) __syncwarp();                   // (the factors are read)
     }
-    // ---- the warps' sums, eight rows at a time (where the tiles were: their copies have all been waited for), then the cluster's
+    // ---- the warps' sums (where the tiles were: their copies have all been waited for), then the cluster's
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
@@ -593,67 +593,65 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
             if (col == 0) a.part_ml[at] = make_float2(m, l);
         }
     };
-    float (*const merge_o)[8][D] = reinterpret_cast<float (*)[8][D]>(ring);
+    float (*const merge_o)[8 * NR][D] = reinterpret_cast<float (*)[8 * NR][D]>(ring);
 #pragma unroll
-    for (int n = 0; n < NR; ++n) {
-        if (8 * n >= n_rows) break;                          // (in all CTAs of a cluster: they share the sequence)
-        if (n > 0) __syncthreads();
+    for (int n = 0; n < NR; ++n)
 #pragma unroll
         for (int m = 0; m < M64; ++m)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (m < D32 / 2 || g < 4) {
-                    *reinterpret_cast<float2*>(&merge_o[warp][2 * c][Sh::column(m, g) + 2 * i]) = make_float2(o[m][i][n][0], o[m][i][n][2]);
-                    *reinterpret_cast<float2*>(&merge_o[warp][2 * c + 1][Sh::column(m, g) + 2 * i]) = make_float2(o[m][i][n][1], o[m][i][n][3]);
+                    *reinterpret_cast<float2*>(&merge_o[warp][8 * n + 2 * c][Sh::column(m, g) + 2 * i]) = make_float2(o[m][i][n][0], o[m][i][n][2]);
+                    *reinterpret_cast<float2*>(&merge_o[warp][8 * n + 2 * c + 1][Sh::column(m, g) + 2 * i]) = make_float2(o[m][i][n][1], o[m][i][n][3]);
                 }
-        __syncthreads();
-        const int pairs = min(8, n_rows - 8 * n) * (D / 2);
-        for (int u = t; u < pairs; u += kWarps * 32) {
-            const int r = u / (D / 2), col = u % (D / 2) * 2;
-            float y = 0.f, z = 0.f;
+    __syncthreads();
+    const int pairs = n_rows * (D / 2);
+    for (int u = t; u < pairs; u += kWarps * 32) {
+        const int r = u / (D / 2), col = u % (D / 2) * 2;
+        float y = 0.f, z = 0.f;
 #pragma unroll
-            for (int w = 0; w < kWarps; ++w) {
-                const float2 x2 = *reinterpret_cast<const float2*>(&merge_o[w][r][col]);
-                y = fmaf(x2.x, merge_f[w][8 * n + r], y);
-                z = fmaf(x2.y, merge_f[w][8 * n + r], z);
-            }
-            if (ranks == 1) give(8 * n + r, col, y, z, cta_ml[8 * n + r].x, cta_ml[8 * n + r].y);
-            else *reinterpret_cast<float2*>(&merge_o[0][r][col]) = make_float2(y, z);
+        for (int w = 0; w < kWarps; ++w) {
+            const float2 x2 = *reinterpret_cast<const float2*>(&merge_o[w][r][col]);
+            y = fmaf(x2.x, merge_f[w][r], y);
+            z = fmaf(x2.y, merge_f[w][r], z);
         }
-        if (ranks == 1) continue;
-        cluster_arrive_release();
-        cluster_wait_acquire();
-        if (t < 8 * ranks) peer_ml[t >> 3][t & 7] = ld_peer2(smem_u32(&cta_ml[8 * n + (t & 7)]), t >> 3);
-        __syncthreads();
-        for (int u = rank * kWarps * 32 + t; u < pairs; u += ranks * kWarps * 32) {
-            const int r = u / (D / 2), col = u % (D / 2) * 2;
-            float2 x2[kMaxCluster];
-#pragma unroll
-            for (int k = 0; k < kMaxCluster; ++k)
-                if (k < ranks) x2[k] = ld_peer2(smem_u32(&merge_o[0][r][col]), k);
-            float m = -CUDART_INF_F, l = 0.f, y = 0.f, z = 0.f;
-            for (int k = 0; k < ranks; ++k) m = fmaxf(m, peer_ml[k][r].x);
-            const float base = m == -CUDART_INF_F ? 0.f : m;
-#pragma unroll
-            for (int k = 0; k < kMaxCluster; ++k)
-                if (k < ranks) {
-                    const float f = exp2f(peer_ml[k][r].x - base);
-                    l = fmaf(peer_ml[k][r].y, f, l);
-                    y = fmaf(x2[k].x, f, y);
-                    z = fmaf(x2[k].y, f, z);
-                }
-            give(8 * n + r, col, y, z, m, l);
-        }
-        cluster_arrive_release();                            // (nobody's sums are written over, or gone, while another reads them)
-        cluster_wait_acquire();
+        if (ranks == 1) give(r, col, y, z, cta_ml[r].x, cta_ml[r].y);
+        else *reinterpret_cast<float2*>(&merge_o[0][r][col]) = make_float2(y, z);
     }
+    if (ranks == 1) return;                                  // (all CTAs of a launch alike)
+    cluster_arrive_release();
+    cluster_wait_acquire();
+    if (t < 8 * NR * ranks) peer_ml[t / (8 * NR)][t % (8 * NR)] = ld_peer2(smem_u32(&cta_ml[t % (8 * NR)]), t / (8 * NR));
+    __syncthreads();
+    for (int u = rank * kWarps * 32 + t; u < pairs; u += ranks * kWarps * 32) {
+        const int r = u / (D / 2), col = u % (D / 2) * 2;
+        float2 x2[kMaxCluster];
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k)
+            if (k < ranks) x2[k] = ld_peer2(smem_u32(&merge_o[0][r][col]), k);
+        float m = -CUDART_INF_F, l = 0.f, y = 0.f, z = 0.f;
+        for (int k = 0; k < ranks; ++k) m = fmaxf(m, peer_ml[k][r].x);
+        const float base = m == -CUDART_INF_F ? 0.f : m;
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k)
+            if (k < ranks) {
+                const float f = exp2f(peer_ml[k][r].x - base);
+                l = fmaf(peer_ml[k][r].y, f, l);
+                y = fmaf(x2[k].x, f, y);
+                z = fmaf(x2[k].y, f, z);
+            }
+        give(r, col, y, z, m, l);
+    }
+    cluster_arrive_release();                                // (nobody's sums are gone while another reads them)
+    cluster_wait_acquire();
 }
 
 template <int KIND, int D32, int NR>
 cudaError_t attend(const AttArgs& a, const PagePool& pool, cudaStream_t stream)
 {
     static KernelSetup setup;
-    constexpr int smem = kWarps * kStages * Tile<KIND, D32>::kBytes;
+    constexpr int tiles = kWarps * kStages * Tile<KIND, D32>::kBytes, sums = kWarps * 8 * NR * D32 * 128, smem = tiles > sums ? tiles : sums;
+    static_assert(smem == tiles || page_token_ctas(KIND, D32, NR) * (smem + 12 * 1024) <= 227 * 1024, "shape");
     const cudaError_t e = setup_kernel(setup, reinterpret_cast<const void*>(page_token_kernel<KIND, D32, NR>), smem, 0);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
