@@ -305,16 +305,17 @@ inline bool page_by_tokens(int kind, int head_dim, int64_t rows, int64_t keys, i
     return head_dim <= 96 || mean <= (head_dim <= 192 ? 1280 : 512) || (all <= 32768 && (head_dim <= 192 || mean <= 1280));
 }
 
-// Tiles of query rows that share what is unpacked on the way, 0: unpacked first.  Unpacking first costs 0.15 us for 1000 rows of a head (their bytes, twice), on the way every
-// CTA does it for one tile of rows or two (heads of up to 128 elements).  us, on the way / first, 32 heads in groups of 4, e4m3: 5 tokens over 60000 rows (one tile) 58 / 121; 4 chunks of
-// 56 over 3100 to 5500 (two) 48 / 57, of 33 over 4000 (two) 38 / 45; 100 over 4096 (four) 35 / 29; 512 over 8192 (16) 112 / 90.
-inline int32_t unpacked_row_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs)
+// Tiles of query rows that share what is unpacked on the way, 0: unpacked first.  Unpacking first costs 0.15 us for 1000 rows of a head (their bytes, twice) and a kernel's start, on the
+// way every CTA does it for one tile of rows or two (heads of up to 128 elements).  `keys`: of the batch, `mean`: of a sequence.  us, on the way / first, 32 heads in groups of 4, e4m3: 5 tokens
+// over 60000 rows (one tile) 58 / 121; 4 chunks of 56 over 3100 to 5500 (two) 48 / 57, of 33 over 4000 (two) 38 / 45, of 60 over 400 to 800 24 / 22, one over 4000 29 / 27; 100 over 4096
+// (four) 35 / 29; 512 over 8192 (16) 112 / 90.  16 heads of 64: 200 over 4000 (two) 38 / 27, over 30000 95 / 105.
+inline int32_t unpacked_row_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, int64_t keys, int64_t mean)
 {
     const int64_t queries = 128 / pack_of(c.n_heads / c.kv_heads);
     int64_t most = 0;
     for (int b = 0; b < batch; ++b) most = std::max(most, (static_cast<int64_t>(seqs[b].n_q) + queries - 1) / queries);
     if (most <= 1) return 1;
-    return most > 2 ? 0 : c.head_dim <= 128 ? 2 : 1;
+    return most > 2 || mean < 2048 || keys * c.kv_heads <= 65536 ? 0 : c.head_dim <= 128 ? 2 : 1;
 }
 
 // fp32: blocks of 8 query rows, every sequence's keys cut into as many parts, 64 at most: of all such cuts the one that ends first, in rounds of a CTA's warps over 16 keys
@@ -360,8 +361,9 @@ inline PageAttendPlan plan_page_attention(const ServeShape& v, int32_t batch, co
         keys += visible_keys(seqs[b], counted, a->window, a->n_sink);
         ++active;
     }
-    const bool tokens = h.dtype != MVLA_DTYPE_FP32 && page_by_tokens(a->pages.kind, v.head_dim, most_rows, keys, keys / std::max<int64_t>(active, 1), v.kv_heads);
-    if (h.dtype != MVLA_DTYPE_FP32 && a->pages.kind != MVLA_PAGE_ROWS && !tokens) p.unpack = unpacked_row_tiles(h, batch, seqs);
+    const int64_t mean = keys / std::max<int64_t>(active, 1);
+    const bool tokens = h.dtype != MVLA_DTYPE_FP32 && page_by_tokens(a->pages.kind, v.head_dim, most_rows, keys, mean, v.kv_heads);
+    if (h.dtype != MVLA_DTYPE_FP32 && a->pages.kind != MVLA_PAGE_ROWS && !tokens) p.unpack = unpacked_row_tiles(h, batch, seqs, keys, mean);
     p.attend = h.dtype == MVLA_DTYPE_FP32 ? plan_page_fma(h, batch, seqs, counted, a->window, a->n_sink)
              : tokens ? plan_tokens(h, batch, seqs, counted, a->window, a->n_sink, page_token_ctas(a->pages.kind, v.head_dim / 32, most_rows <= 8 ? 1 : 2))
                       : plan_page_tiles(h, batch, seqs, counted, a->window, a->n_sink, p.unpack == 2 ? 2 : 1, p.unpack == 2 ? kUnpackedPairUs : p.unpack ? kUnpackedTileUs : kTileUs);

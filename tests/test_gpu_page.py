@@ -340,3 +340,21 @@ def test_few_rows_of_their_own_type(d, H, G, n_q):
     q = torch.randn(100, H, d, generator=gen, device="cuda").to(BF16)
     check_attention(ctx, pool, ROWS, seqs, table, q, page_rows)
     check_attention(ctx, pool, ROWS, seqs, table, q, page_rows, window=40, n_sink=2)
+
+
+@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("H,G,d,n_q,page_rows,window,n_sink", [
+    (32, 32, 64, 200, 16, None, 0), (32, 32, 96, 129, 64, None, 0), (32, 32, 128, 256, 32, 2100, 70), (96, 32, 128, 80, 128, None, 0),     # two tiles of rows that share what is unpacked
+    (24, 24, 160, 140, 16, None, 0), (24, 24, 256, 256, 64, 2500, 1),                                                                     # one each
+])
+def test_two_blocks_over_long_sequences(kind, H, G, d, n_q, page_rows, window, n_sink):
+    gen = generator(d + n_q + kind)
+    ctx = context(BF16, H, G, d)
+    lengths = [2900, 2777, 3000]
+    table, n_pages = P.make_table(gen, lengths, page_rows)
+    pool = P.make_pool(gen, n_pages, G, page_rows, d, kind, BF16)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=2900), mvla.Seq(q_row=n_q, n_q=0, n_kv=2777), mvla.Seq(q_row=n_q + 1, n_q=n_q // 2 - 3, n_kv=3000)]
+    q = torch.randn(2 * n_q, H, d, generator=gen, device="cuda").to(BF16)
+    check_attention(ctx, pool, kind, seqs, table, q, page_rows, window=window, n_sink=n_sink)
+    kv_len = torch.tensor([2500, 5, 61], dtype=torch.int32, device="cuda")
+    check_attention(ctx, pool, kind, seqs, table, q, page_rows, window=window, n_sink=n_sink, kv_len=kv_len)

@@ -52,13 +52,14 @@ def plan(shim, seqs, kind=E4M3, dtype=BF16, heads=(32, 8, 128), window=mvla.WIND
 
 @pytest.mark.parametrize("want,kw", [
     ((TOKEN, 0), dict(seqs=[(1, 4000)])), ((TOKEN, 0), dict(seqs=[(4, 60000)], kind=E2M1)), ((PAGE_TILE, 1), dict(seqs=[(5, 60000)])),
-    ((PAGE_TILE, 2), dict(seqs=[(64, 4000), (1, 9)])), ((PAGE_TILE, 1), dict(seqs=[(64, 4000)], heads=(16, 4, 256))), ((PAGE_TILE, 0), dict(seqs=[(65, 4000)])), ((PAGE_TILE, 0), dict(seqs=[(65, 4000)], kind=ROWS)),
+    ((PAGE_TILE, 2), dict(seqs=[(64, 9000), (1, 4000)])), ((PAGE_TILE, 1), dict(seqs=[(64, 20000)], heads=(16, 4, 256))), ((PAGE_TILE, 0), dict(seqs=[(64, 9000)] + [(1, 9)] * 9)),
+    ((PAGE_TILE, 0), dict(seqs=[(64, 8000)])), ((PAGE_TILE, 0), dict(seqs=[(65, 4000)])), ((PAGE_TILE, 0), dict(seqs=[(65, 4000)], kind=ROWS)),
     ((TOKEN, 0), dict(seqs=[(1, 800)], kind=ROWS)), ((PAGE_TILE, 0), dict(seqs=[(1, 8000)], kind=ROWS)), ((TOKEN, 0), dict(seqs=[(4, 200)], kind=ROWS)),
     ((TOKEN, 0), dict(seqs=[(4, 1200)] * 4, kind=ROWS)), ((PAGE_TILE, 0), dict(seqs=[(4, 200)] * 40, kind=ROWS)), ((TOKEN, 0), dict(seqs=[(2, 200)] * 40, kind=ROWS)), ((TOKEN, 0), dict(seqs=[(4, 4000)], kind=ROWS, heads=(32, 8, 64))), ((PAGE_TILE, 0), dict(seqs=[(4, 5000)], kind=ROWS, heads=(32, 8, 64))),
     ((TOKEN, 0), dict(seqs=[(1, 60000)], kind=ROWS, heads=(32, 8, 64))), ((PAGE_TILE, 0), dict(seqs=[(5, 200)], kind=ROWS)), ((PAGE_TILE, 0), dict(seqs=[(4, 200)], kind=ROWS, heads=(32, 8, 256))),
     ((TOKEN, 0), dict(seqs=[(2, 60000)], kind=ROWS, heads=(32, 8, 96))), ((PAGE_TILE, 0), dict(seqs=[(3, 60000)], kind=ROWS, heads=(32, 8, 96))),
     ((PAGE_TILE, 0), dict(seqs=[(1, 8000)], kind=ROWS, heads=(16, 2, 256))), ((TOKEN, 0), dict(seqs=[(1, 300)] * 30 + [(0, 90000)], kind=ROWS, heads=(16, 16, 256))),
-    ((PAGE_TILE, 2), dict(seqs=[(5, 800)], heads=(64, 1, 64))), ((FMA, 0), dict(seqs=[(1, 800)], dtype=FP32)), ((FMA, 0), dict(seqs=[(300, 800)], dtype=FP32, kind=ROWS)),
+    ((PAGE_TILE, 2), dict(seqs=[(5, 80000)], heads=(64, 1, 64))), ((FMA, 0), dict(seqs=[(1, 800)], dtype=FP32)), ((FMA, 0), dict(seqs=[(300, 800)], dtype=FP32, kind=ROWS)),
 ])
 def test_forms(shim, want, kw):
     p, _ = plan(shim, **kw)
