@@ -7,9 +7,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWarps = kThreads / 32;
-// Up to so many parts a warp joins those of a (query, head), beyond a CTA does.  Tokens of 16 requests over 500 to 4000 e4m3 rows, 1 to 8 parts:
-// 31.5 us so, 35.4 with CTAs; one token over 800 rows of 32 heads 11.6, with CTAs 11.1; 131072 rows, a hundred parts and more: CTAs.
-constexpr int kFewParts = 8;
 constexpr int kMassKeys = 128;               // keys of a CTA (AttSeq::tile0 counts such tiles)
 constexpr int kRowGroups = kThreads / kMassKeys;
 constexpr int kFinishRows = 4 * kWarps;      // rows (queries and heads) whose scores are added up at a time: eight lanes to a row's parts
@@ -208,10 +205,10 @@ cudaError_t launch(K kernel, int64_t blocks, cudaStream_t stream, Args... args)
 
 }  // namespace
 
-cudaError_t launch_attend_join(int dtype, const AttArgs& a, cudaStream_t stream)
+cudaError_t launch_attend_join(int dtype, bool by_ctas, const AttArgs& a, cudaStream_t stream)
 {
     const int64_t units = static_cast<int64_t>(a.total_q) * a.n_heads, blocks = (units + kWarps - 1) / kWarps;
-    if (a.splits > kFewParts)
+    if (by_ctas)
         return dtype == MVLA_DTYPE_FP32 ? launch(attend_join_cta_kernel<float>, units, stream, a) : launch(attend_join_cta_kernel<__nv_bfloat16>, units, stream, a);
     return dtype == MVLA_DTYPE_FP32 ? launch(attend_join_kernel<float>, blocks, stream, a) : launch(attend_join_kernel<__nv_bfloat16>, blocks, stream, a);
 }

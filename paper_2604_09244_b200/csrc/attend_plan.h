@@ -85,6 +85,10 @@ struct AttendPlan {
     int32_t cluster = 1;         // single tokens over pages: CTAs that share a part
 };
 
+// Up to so many parts a warp joins those of a (query, head), beyond a CTA does.  Tokens of 16 requests over 500 to 4000 e4m3 rows, 1 to 8 parts:
+// 31.5 us so, 35.4 with CTAs; one token over 800 rows of 32 heads 11.6, with CTAs 11.1; 131072 rows, a hundred parts and more: CTAs.
+constexpr int kFewParts = 8;
+
 // Parts that a sequence's visible keys are cut into.
 inline int32_t parts_of(const AttendPlan& p, const mvla_seq& s, bool counted, int32_t window, int32_t n_sink)
 {

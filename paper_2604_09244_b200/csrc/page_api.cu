@@ -168,7 +168,7 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
             return MVLA_ERR_CUDA;
         e = launch_page_tile(tokens, t, maps, st);
     }
-    if (e == cudaSuccess && plan.attend.splits > 1) e = launch_attend_join(h.dtype, t, st);
+    if (e == cudaSuccess && plan.attend.splits > 1) e = launch_attend_join(h.dtype, joined_by_ctas(h, plan.attend), t, st);
     return close_call(ctx, e);
 }
 

@@ -99,6 +99,10 @@ inline int32_t check_page_rows(const ServeShape& v, int32_t batch, const mvla_se
 
 constexpr int kPageTile = 64;                // keys of a tile (attend_tile.cu), rows of an unpacked one
 
+// Whether CTAs join the parts of every (query, head): many parts, and no more CTAs than run at once.  us: 200 queries of 16 heads, 9 parts, 24 by CTAs, 7 by warps; 30 of 8
+// heads of 128, 18 parts, 2 less by CTAs.
+inline bool joined_by_ctas(const ServeShape& c, const AttendPlan& p) { return p.splits > kFewParts && p.total_q * c.n_heads <= 8 * static_cast<int64_t>(c.sm_count); }
+
 struct PageAttendPlan {
     AttendPlan attend;
     // quantised pages that are no single tokens': the tiles that some query sees, as elements of the hidden type (-1: there are none)
@@ -308,7 +312,7 @@ inline bool page_by_tokens(int kind, int head_dim, int64_t rows, int64_t keys, i
 // Tiles of query rows that share what is unpacked on the way, 0: unpacked first.  Unpacking first costs 0.15 us for 1000 rows of a head (their bytes, twice) and a kernel's start, on the
 // way every CTA does it for one tile of rows or two (heads of up to 128 elements).  `keys`: of the batch, `mean`: of a sequence.  us, on the way / first, 32 heads in groups of 4, e4m3: 5 tokens
 // over 60000 rows (one tile) 58 / 121; 4 chunks of 56 over 3100 to 5500 (two) 48 / 57, of 33 over 4000 (two) 38 / 45, of 60 over 400 to 800 24 / 22, one over 4000 29 / 27; 100 over 4096
-// (four) 35 / 29; 512 over 8192 (16) 112 / 90.  16 heads of 64: 200 over 4000 (two) 38 / 27, over 30000 95 / 105.
+// (four) 35 / 29; 512 over 8192 (16) 112 / 90.  16 heads of 64: 200 over 4000 (two) 25 / 27, over 30000 95 / 105.
 inline int32_t unpacked_row_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, int64_t keys, int64_t mean)
 {
     const int64_t queries = 128 / pack_of(c.n_heads / c.kv_heads);

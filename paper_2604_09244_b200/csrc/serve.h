@@ -83,7 +83,7 @@ cudaError_t launch_attend_token(int dtype, const AttArgs& a, int rows, cudaStrea
 // Behind it: the parts joined, and mass += the weights that the kept scores stand for.
 cudaError_t launch_attend_finish(const AttArgs& a, cudaStream_t stream);
 // part_o / part_ml -> out, lse, lse2.
-cudaError_t launch_attend_join(int dtype, const AttArgs& a, cudaStream_t stream);
+cudaError_t launch_attend_join(int dtype, bool by_ctas, const AttArgs& a, cudaStream_t stream);
 // mass += part_mass over its parts.
 cudaError_t launch_mass_add(const AttArgs& a, cudaStream_t stream);
 

@@ -79,7 +79,7 @@ int32_t attend_by_tiles(const CtxView& v, AttArgs& k, const mvla_attention* a, c
     if (plan.total_kv > 0 && (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, kKeys) || !row_map(v, &maps.v, vv, v.kv_heads, kv_rows, 1, kKeys))) return MVLA_ERR_CUDA;
     *e = widen ? launch_widen(k, ws + plan.wide_q, ws + plan.wide_k, ws + plan.wide_v, st) : cudaSuccess;
     if (*e == cudaSuccess) *e = launch_attend_tile(widen, tokens, k, maps, st);
-    if (*e == cudaSuccess && plan.splits > 1) *e = launch_attend_join(v.dtype, k, st);
+    if (*e == cudaSuccess && plan.splits > 1) *e = launch_attend_join(v.dtype, plan.splits > kFewParts, k, st);
     if (*e == cudaSuccess && a->mass && plan.total_kv > 0) {
         if (!row_map(v, &maps.k, kk, v.kv_heads, kv_rows, 1, 128)) return MVLA_ERR_CUDA;
         *e = launch_attend_weights(widen, k, maps, st);
@@ -163,7 +163,7 @@ int32_t attention_impl(mvla_ctx* ctx, int32_t batch, const mvla_seq* seqs, const
         return close_call(ctx, e);
     } else {
         e = launch_attend_fma(k, plan.rows, st);
-        if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, k, st);
+        if (e == cudaSuccess && plan.splits > 1) e = launch_attend_join(v.dtype, plan.splits > kFewParts, k, st);
         if (e == cudaSuccess && a->mass) e = launch_mass_fma(k, st);
     }
     if (e == cudaSuccess && a->mass) e = launch_mass_add(k, st);
