@@ -75,7 +75,8 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     constexpr int ST = Sh::kStages;
     extern __shared__ uint8_t raw[];
     __shared__ uint64_t bars[2 * kMaxStages + 8];
-    __shared__ uint16_t list[kMaxTiles];
+    __shared__ __align__(16) uint16_t list[kMaxTiles];
+    static_assert(sizeof list >= 4 * kJoinFloats, "room for the factors of a cluster's rows");
     __shared__ int key_at[kKeys];
     __shared__ uint32_t seen_by[4][4][kKeys / 32];           // of the last tiles: the keys that some row of a warp sees
     __shared__ int n_list, dead;
@@ -161,17 +162,13 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         return page >= 0 && page < a.n_pages ? page * a.kv_heads + hk : -1;
     };
     int here = 0, ahead = 0;
-    const auto load = [&](int c) {                           // tiles of keys and values in turn
+    const auto load_box = [&](int c) {                       // (pages: this lane's box of chunk c, on page `here`)
         const int st = c % ST, j0 = first_key(c / 2);
         const CUtensorMap* const map = c & 1 ? &map_v : &map_k;
         if constexpr (!PAGED) {
             mbar_expect_tx(full(st), Sh::kStage);
             for (int b = 0; b < DB; ++b) tma_load_3d(kv_at + st * Sh::kStage + b * kKeys * 128, map, b * 64, hk, s.km_row + j0, full(st));
         } else {
-            if (!(c & 1)) {
-                here = ahead;
-                ahead = look_up(c / 2 + 1);
-            }
             if (lane == 0) mbar_expect_tx(full(st), Sh::kStage);
             __syncwarp();
             if (lane < boxes)
@@ -179,14 +176,33 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
                             (j0 + row_of_box) & ((1 << a.page_shift) - 1), here, full(st));
         }
     };
+    const auto load = [&](int c) {                           // tiles of keys and values in turn
+        if (PAGED && !(c & 1)) {
+            here = ahead;
+            ahead = look_up(c / 2 + 1);
+        }
+        load_box(c);
+    };
     const int at_once = min(ST, 2 * n);
     if (warp == Sh::kLoads && (PAGED || lane == 0) && n > 0) {
         if (lane == 0) {
             mbar_expect_tx(q_full, DB * per * a.pack * 128);
             for (int b = 0; b < DB; ++b) tma_load_3d(q_at + b * kRows * 128, &map_q, b * 64, head0, s.qm_row + q0, q_full);
         }
-        ahead = look_up(0);
-        for (int c = 0; c < at_once; ++c) load(c);
+        if constexpr (PAGED) {                               // (the pages of the first tiles, all at once)
+            int pages[(ST + 1) / 2 + 1];
+#pragma unroll
+            for (int i = 0; i <= (ST + 1) / 2; ++i) pages[i] = look_up(i);
+#pragma unroll
+            for (int c = 0; c < ST; ++c)
+                if (c < at_once) {
+                    here = pages[c / 2];
+                    load_box(c);
+                }
+            ahead = pages[(ST + 1) / 2];
+        } else {
+            for (int c = 0; c < at_once; ++c) load(c);
+        }
     }
     __syncwarp();
     tc_fence_before();
@@ -411,7 +427,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         const bool joined = PAGED && ranks > 1, split = PAGED ? s.parts > 1 : a.splits > 1;
         const float inv = l > 0.f ? 1.f / l : 0.f;
         m -= kLift;
-        float* const sums = reinterpret_cast<float*>(raw + (kv_at - smem_u32(raw)));      // of a cluster's CTA: element by element, the rows side by side
+        float4* const sums = reinterpret_cast<float4*>(raw + (kv_at - smem_u32(raw)));      // of a cluster's CTA (sums_at)
         // the twins' rows of O, for the others (the keys and values have been read): element by element, the rows side by side
         float* const beside = reinterpret_cast<float*>(raw + ((PAGED ? q_at : kv_at) - smem_u32(raw)));
         if (TOKENS && twins && t < 2 * kTwin) {
@@ -436,7 +452,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? (joined || split ? o[k] : o[k] * inv) : 0.f;
             if (joined) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) sums[(c + k) * kRows + t] = o[k];
+                for (int k = 0; k < 32; k += 4) sums[sums_at(t, (c + k) / 4, a.head_dim)] = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                 continue;
             }
             if (!mine) continue;
@@ -466,7 +482,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
     if (PAGED && ranks > 1) {                                // (reached by all CTAs of the cluster, whoever gave up)
         cluster_arrive_release();
         cluster_wait_acquire();
-        if (t < kRows) join_cluster(a, s, kv_at, smem_u32(row_ml), ranks, t, q0, per, head0, part_of_seq);
+        join_cluster<1>(a, s, kv_at, smem_u32(row_ml), reinterpret_cast<float*>(list), ranks, q0, per, head0, part_of_seq);      // (no list of counted positions)
         cluster_arrive_release();                            // (nobody's sums are gone while another reads them)
         cluster_wait_acquire();
     }

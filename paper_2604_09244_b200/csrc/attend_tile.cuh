@@ -153,61 +153,84 @@ __device__ __forceinline__ float2 ld_peer2(uint32_t addr, int rank)
     asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(x.x), "=f"(x.y) : "r"(remote) : "memory");
     return x;
 }
-__device__ __forceinline__ float ld_peer(uint32_t addr, int rank)
+__device__ __forceinline__ float4 ld_peer4(uint32_t addr, int rank)
 {
     uint32_t remote;
-    float x;
+    float4 x;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(x) : "r"(remote) : "memory");
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(remote) : "memory");
     return x;
 }
-// By 128 threads of every CTA of a cluster (a barrier of the cluster before and behind): the sums of the block's rows, [head_dim][128] at `sums`, and their references
-// and sums of exponentials, [128] at `ml`, of all its CTAs.  A CTA joins a share of the rows, a thread one row's pieces of eight elements, in the CTAs' order.
-__device__ __forceinline__ void join_cluster(const AttArgs& a, const AttSeq& s, uint32_t sums, uint32_t ml, int ranks, int t, int q0, int per, int head0, int part)
+// Where four elements, `piece` of a row's fours, lie among a CTA's sums, in fours: eight rows side by side, or eight pieces, share no bank.
+__device__ __forceinline__ int sums_at(int row, int piece, int head_dim) { return row * (head_dim / 4) + (piece ^ (row & 7)); }
+constexpr int kJoinFloats = kRows / 2 * (kMaxCluster + 2);               // of `factors`, for a tile of rows
+
+// By all threads of every CTA of a cluster (a barrier of the cluster before and behind): the sums of T tiles of rows at `sums` (sums_at), and their references and sums of
+// exponentials, [T 128] at `ml`, of all its CTAs.  A CTA joins a share of the rows, in the CTAs' order: factors first, then a thread four elements of a row at a time.
+template <int T>
+__device__ __forceinline__ void join_cluster(const AttArgs& a, const AttSeq& s, uint32_t sums, uint32_t ml, float* factors, int ranks, int q0, int per, int head0, int part)
 {
-    const int rows = kRows / ranks, row = static_cast<int>(cluster_ctarank()) * rows + t % rows, i_row = q0 + row / a.pack, head = head0 + row % a.pack;
-    if (row >= per * a.pack || i_row >= s.n_q) return;
-    float2 z[kMaxCluster];
-#pragma unroll
-    for (int k = 0; k < kMaxCluster; ++k)
-        if (k < ranks) z[k] = ld_peer2(ml + 8u * row, k);
-    float m = -CUDART_INF_F, l = 0.f, f[kMaxCluster];
-#pragma unroll
-    for (int k = 0; k < kMaxCluster; ++k)
-        if (k < ranks) m = fmaxf(m, z[k].x);
-    const float ref = m == -CUDART_INF_F ? 0.f : m;
-#pragma unroll
-    for (int k = 0; k < kMaxCluster; ++k) {
-        f[k] = k < ranks ? exp2f(z[k].x - ref) : 0.f;
-        if (k < ranks) l = fmaf(z[k].y, f[k], l);
-    }
+    const int t = threadIdx.x, rows = T * kRows / ranks, first = static_cast<int>(cluster_ctarank()) * rows, D = a.head_dim;
     const bool whole = s.parts == 1;
-    const float by = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
-    const int64_t at = whole ? (s.q_row + i_row) * a.n_heads + head : (s.part0 + static_cast<int64_t>(part) * s.n_q + i_row) * a.n_heads + head;
-    for (int piece = t / rows; piece < a.head_dim / 8; piece += ranks) {
-        float o[8] = {};
+    // the query of a row of the tiles (negative: nobody's), and where its results lie, in heads
+    const auto query = [&](int row) {
+        const int r = row % kRows, i = q0 + row / kRows * per + r / a.pack;
+        return r < per * a.pack && i < s.n_q ? i : -1;
+    };
+    const auto place = [&](int row, int i) {
+        return (whole ? s.q_row + i : s.part0 + static_cast<int64_t>(part) * s.n_q + i) * a.n_heads + head0 + row % kRows % a.pack;
+    };
+    if (t < rows) {
+        const int row = first + t, i = query(row);
+        float2 z[kMaxCluster];
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k)
+            if (k < ranks) z[k] = ld_peer2(ml + 8u * row, k);
+        float m = -CUDART_INF_F, l = 0.f, f[kMaxCluster];
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k)
+            if (k < ranks) m = fmaxf(m, z[k].x);
+        const float ref = m == -CUDART_INF_F ? 0.f : m;
 #pragma unroll
         for (int k = 0; k < kMaxCluster; ++k) {
-            if (k >= ranks) break;
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = ld_peer(sums + 4u * ((piece * 8 + e) * kRows + row), k);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) o[e] = fmaf(x[e], f[k], o[e]);
+            f[k] = k < ranks ? exp2f(z[k].x - ref) : 0.f;
+            if (k < ranks) l = fmaf(z[k].y, f[k], l);
         }
+        const float by = whole ? (l > 0.f ? 1.f / l : 0.f) : 1.f;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) o[e] *= by;
-        if (whole) {
-            store8(static_cast<__nv_bfloat16*>(a.out) + at * a.head_dim + piece * 8, o);
-        } else {
-            float* const dst = a.part_o + at * a.head_dim + piece * 8;
-            *reinterpret_cast<float4*>(dst) = make_float4(o[0], o[1], o[2], o[3]);
-            *reinterpret_cast<float4*>(dst + 4) = make_float4(o[4], o[5], o[6], o[7]);
+        for (int k = 0; k < kMaxCluster; ++k)
+            if (k < ranks) factors[t * kMaxCluster + k] = f[k];
+        factors[rows * kMaxCluster + t] = by;
+        if (i >= 0) {
+            if (!whole) a.part_ml[place(row, i)] = make_float2(m, l);
+            else if (a.lse) a.lse[place(row, i)] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
         }
     }
-    if (t >= rows) return;
-    if (!whole) a.part_ml[at] = make_float2(m, l);
-    else if (a.lse) a.lse[at] = l > 0.f ? (m + log2f(l)) * 0.69314718055994531f : -CUDART_INF_F;      // ln 2
+    __syncthreads();
+    const int pieces = D / 4;
+    for (int u = t; u < rows * pieces; u += static_cast<int>(blockDim.x)) {
+        const int mine = u / pieces, piece = u - mine * pieces, row = first + mine, i = query(row);
+        if (i < 0) continue;
+        const uint32_t at = sums + 16u * sums_at(row, piece, D);
+        float4 x[kMaxCluster];
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k)
+            if (k < ranks) x[k] = ld_peer4(at, k);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < kMaxCluster; ++k) {
+            if (k >= ranks) continue;
+            const float f = factors[mine * kMaxCluster + k];
+            o.x = fmaf(x[k].x, f, o.x);
+            o.y = fmaf(x[k].y, f, o.y);
+            o.z = fmaf(x[k].z, f, o.z);
+            o.w = fmaf(x[k].w, f, o.w);
+        }
+        const float by = factors[rows * kMaxCluster + mine];
+        const int64_t to = place(row, i) * D + 4 * piece;
+        if (whole) *reinterpret_cast<uint2*>(static_cast<__nv_bfloat16*>(a.out) + to) = make_uint2(two_bf16(o.x * by, o.y * by), two_bf16(o.z * by, o.w * by));
+        else *reinterpret_cast<float4*>(a.part_o + to) = o;
+    }
 }
 
 }  // namespace mvla

@@ -279,8 +279,8 @@ inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla
             cut(cluster, part);
             for (int tries = 0; rounds && ctas > rounds * at_once && part * cluster < longest && tries < 16; ++tries) cut(cluster, part += std::max<int64_t>(64, part / 16 / 64 * 64));
             const double join = (cluster > 1 ? 1.0 : 0.0) + (p.splits > 1 ? 5.0 + static_cast<double>(part_q) * c.n_heads * c.head_dim * 8 / 6e6 : 0.0);
-            const double mine = static_cast<double>(std::min(part, (longest + cluster - 1) / cluster));
-            const double cost = static_cast<double>((ctas + at_once - 1) / at_once) * (mine / 64 + 4) * tile + join;
+            const int64_t mine = (std::min(part, (longest + cluster - 1) / cluster) + 63) / 64;
+            const double cost = static_cast<double>((ctas + at_once - 1) / at_once) * static_cast<double>(mine + 4) * tile + join;
             if (!best || cost < best_cost) { best = part; best_cost = cost; best_cluster = cluster; }
         }
     }

@@ -83,7 +83,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
     __shared__ int dead;
     __shared__ uint32_t tmem_base;
     __shared__ float2 row_ml[T][kRows];
-    static_assert(Sh::kSmem - 1024 >= T * D * kRows * 4, "room for the sums of a cluster's CTA");
+    static_assert(Sh::kSmem - 1024 >= T * (D * kRows + kJoinFloats) * 4, "room for the sums of a cluster's CTA");
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t q_at = base, kv_at = base + Sh::kQBytes;
     const uint32_t bar0 = smem_u32(bars);
@@ -434,7 +434,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         if (ok && n > 0) ok = guard.wait_all(o_full, 0);
         tc_fence_after();
         const int64_t part = s.part0 + static_cast<int64_t>(part_of_seq) * s.n_q + i_row;
-        float* const sums = reinterpret_cast<float*>(raw + (q_at - smem_u32(raw))) + w * D * kRows;       // of a cluster's CTA: element by element, the rows side by side
+        float4* const sums = reinterpret_cast<float4*>(raw + (q_at - smem_u32(raw)));         // of a cluster's CTA (sums_at)
         const float by = (l > 0.f ? two_to(unit - 127) * (s.parts > 1 || ranks > 1 ? 1.f : 1.f / l) : 0.f) * two_to(-kCodeLift);
         m -= kF16Lift;
         for (int c = 0; c < D && ok; c += 32) {
@@ -444,7 +444,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? o[k] * by : 0.f;
             if (ranks > 1) {
 #pragma unroll
-                for (int k = 0; k < 32; ++k) sums[(c + k) * kRows + r] = o[k];
+                for (int k = 0; k < 32; k += 4) sums[sums_at(w * kRows + r, (c + k) / 4, D)] = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);
                 continue;
             }
             if (!mine) continue;
@@ -469,7 +469,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
     if (ranks > 1) {                                         // (reached by all CTAs of the cluster, whoever gave up)
         cluster_arrive_release();
         cluster_wait_acquire();
-        if (t < T * kRows) join_cluster(a, s, q_at + (t / kRows) * D * kRows * 4, smem_u32(row_ml[t / kRows]), ranks, t % kRows, q0 + t / kRows * per, per, head0, part_of_seq);
+        join_cluster<T>(a, s, q_at, smem_u32(row_ml), reinterpret_cast<float*>(raw + (q_at - smem_u32(raw)) + T * D * kRows * 4), ranks, q0, per, head0, part_of_seq);
         cluster_arrive_release();                            // (nobody's sums are gone while another reads them)
         cluster_wait_acquire();
     }
