@@ -163,8 +163,8 @@ inline int32_t check_page_attention(const ServeShape& v, int32_t batch, const mv
 }
 
 // Parts (clusters of 1, 2, 4 or 8 CTAs) of about the same length over the whole batch, a multiple of 64 keys to a CTA, so that their CTAs fill whole rounds
-// of those that fit, or a cluster to a sequence: what ends first, in keys of a CTA (about 30 a microsecond): its keys and 256 for its start and end in every round, and where a
-// sequence has several clusters 128 for the kernel that joins them and 4 for every one of the most there are (one token over 131072 e4m3 rows: the join 7.3 us
+// of those that fit, or a cluster to a sequence: what ends first, in keys of a CTA (about 30 a microsecond): its keys and 256 for its start and end in every round, 56 where a cluster joins
+// (16 requests of one token over 30 to 100 rows 7.3 us in clusters, 5.3 without), and where a sequence has several clusters 128 for the kernel that joins them and 4 for every one of the most there are (one token over 131072 e4m3 rows: the join 7.3 us
 // of 68 with 74 parts).  256 parts to a sequence at most.
 inline void cut_page_tokens(AttendPlan& p, int64_t fit, int kv_heads, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink)
 {
@@ -200,7 +200,7 @@ inline void cut_page_tokens(AttendPlan& p, int64_t fit, int kv_heads, int32_t ba
             cut(cluster, part);
             for (int tries = 0; rounds && ctas > rounds * at_once && part * cluster < longest && tries < 8; ++tries) cut(cluster, part += (part / 16 + 63) / 64 * 64);
             const int64_t mine = std::min(part, (longest + cluster - 1) / cluster);
-            const int64_t cost = (ctas + at_once - 1) / at_once * (mine + 256) + (p.splits > 1 ? 128 + 4 * p.splits : 0);
+            const int64_t cost = (ctas + at_once - 1) / at_once * (mine + 256) + (p.splits > 1 ? 128 + 4 * p.splits : 0) + (cluster > 1 ? 56 : 0);
             if (!best || cost < best_cost) { best = part; best_cost = cost; best_cluster = cluster; }
         }
     cut(best_cluster, best);
@@ -231,8 +231,8 @@ inline AttendPlan plan_tokens(const ServeShape& c, int32_t batch, const mvla_seq
 
 // Blocks of queries by tiles of 128 rows, every sequence's keys cut into parts (clusters of 1, 2, 4 or 8 CTAs) of about the same length over the whole batch (a
 // multiple of 64 keys to a CTA, at least 128), so that their CTAs fill whole rounds of those that fit: of one to four rounds, or no cut at all, what ends
-// first.  In us: the tiles of its longest part and 4 for its start and end, `tile` each (with another CTA beside it); 1 where a cluster joins; 5 for the kernel that joins
-// parts, and what their sums, written and read, take at 6 TB/s.
+// first.  In us: the tiles of its longest part and 4 for its start and end, `tile` each (with another CTA beside it); 1 and a 32nd of a head's elements where a cluster joins (with 1 alone 100
+// queries of 32 heads of 128 had clusters of two, 11.8 us for 8.0); 5 for the kernel that joins parts, and what their sums, written and read, take at 6 TB/s.
 constexpr double kTileUs = 1.3, kUnpackedTileUs = 2.2, kUnpackedPairUs = 1.7;
 inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, bool counted, int32_t window, int32_t n_sink, int row_tiles, double tile)
 {
@@ -278,7 +278,7 @@ inline AttendPlan plan_page_tiles(const ServeShape& c, int32_t batch, const mvla
             part = (part + 63) / 64 * 64;
             cut(cluster, part);
             for (int tries = 0; rounds && ctas > rounds * at_once && part * cluster < longest && tries < 16; ++tries) cut(cluster, part += std::max<int64_t>(64, part / 16 / 64 * 64));
-            const double join = (cluster > 1 ? 1.0 : 0.0) + (p.splits > 1 ? 5.0 + static_cast<double>(part_q) * c.n_heads * c.head_dim * 8 / 6e6 : 0.0);
+            const double join = (cluster > 1 ? 1.0 + c.head_dim / 32.0 : 0.0) + (p.splits > 1 ? 5.0 + static_cast<double>(part_q) * c.n_heads * c.head_dim * 8 / 6e6 : 0.0);
             const int64_t mine = (std::min(part, (longest + cluster - 1) / cluster) + 63) / 64;
             const double cost = static_cast<double>((ctas + at_once - 1) / at_once) * static_cast<double>(mine + 4) * tile + join;
             if (!best || cost < best_cost) { best = part; best_cost = cost; best_cluster = cluster; }
