@@ -128,3 +128,13 @@ def tolerance(r, d, dtype, kind, tokens):
     if kind == E2M1:
         own = own + 2.0 ** -24 * r["largest"]
     return own + U.HALF[torch.bfloat16] * (r["out"].abs() + own) + 1e-30
+
+
+# (kind, heads, key heads, elements, sequences of (queries, rows)) -> (tiles of rows that share what is unpacked, CTAs to a cluster, several clusters to a sequence) of calls on tiles
+CLUSTERS = {
+    (ROWS, 24, 24, 64, ((20, 600),) * 4): (0, 2, False), (ROWS, 16, 16, 128, ((20, 600),) * 4): (0, 4, False), (ROWS, 2, 2, 96, ((20, 500),)): (0, 8, False),
+    (ROWS, 8, 8, 192, ((250, 500),)): (0, 4, False), (ROWS, 8, 8, 256, ((400, 900), (400, 1000), (1, 2))): (0, 2, False), (ROWS, 32, 8, 64, ((400, 9000),)): (0, 4, True),
+    (E4M3, 32, 32, 128, ((20, 600),) * 4): (1, 2, False), (E2M1, 16, 16, 64, ((20, 600),) * 4): (1, 4, False), (E4M3, 2, 2, 192, ((20, 500),)): (1, 8, False),
+    (E4M3, 16, 16, 128, ((130, 2900), (62, 3000))): (2, 4, False), (E2M1, 32, 32, 64, ((130, 2900), (62, 3000))): (2, 2, False), (E4M3, 4, 1, 128, ((60, 70000),)): (2, 4, True),
+    (E4M3, 2, 2, 64, ((130, 500),)): (0, 8, False),
+}

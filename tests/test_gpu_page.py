@@ -358,3 +358,21 @@ def test_two_blocks_over_long_sequences(kind, H, G, d, n_q, page_rows, window, n
     check_attention(ctx, pool, kind, seqs, table, q, page_rows, window=window, n_sink=n_sink)
     kv_len = torch.tensor([2500, 5, 61], dtype=torch.int32, device="cuda")
     check_attention(ctx, pool, kind, seqs, table, q, page_rows, window=window, n_sink=n_sink, kv_len=kv_len)
+
+
+@pytest.mark.parametrize("call", list(P.CLUSTERS))
+def test_clusters(call):
+    """Parts of a block of queries joined inside clusters of two, four and eight CTAs, and behind clusters."""
+    kind, H, G, d, lengths = call
+    gen = generator(d + H)
+    page_rows = 64
+    ctx = context(BF16, H, G, d)
+    table, n_pages = P.make_table(gen, [n for _, n in lengths], page_rows)
+    pool = P.make_pool(gen, n_pages, G, page_rows, d, kind, BF16)
+    seqs, row = [], 0
+    for n_q, n in lengths:
+        seqs.append(mvla.Seq(q_row=row, n_q=n_q, n_kv=n))
+        row += n_q + 1
+    q = torch.randn(row, H, d, generator=gen, device="cuda").to(BF16)
+    check_attention(ctx, pool, kind, seqs, table, q, page_rows)
+    check_attention(ctx, pool, kind, seqs, table, q, page_rows, kv_len=torch.tensor([n // 3 for _, n in lengths], dtype=torch.int32, device="cuda"))

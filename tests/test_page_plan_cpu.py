@@ -7,6 +7,7 @@ import subprocess
 
 import pytest
 
+import page_util
 from paper_2604_09244_b200 import mvla
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -138,3 +139,10 @@ def test_fp32_parts_fit(shim, seed):
             results = p["splits"] * sum(q for q, _ in seqs)
             assert p["part_ml"] >= p["part_o"] + results * heads[0] * heads[2] * 4 and p["attend_bytes"] >= p["part_ml"] + results * heads[0] * 8
             assert kind == ROWS or p["dense_k"] < 0 or p["dense_k"] >= p["attend_bytes"]
+
+
+@pytest.mark.parametrize("call", list(page_util.CLUSTERS))
+def test_clusters(shim, call):
+    kind, H, G, d, seqs = call
+    p, _ = plan(shim, list(seqs), kind=kind, heads=(H, G, d))
+    assert (p["form"], p["unpack"], p["cluster"], p["splits"] > 1) == (PAGE_TILE, *page_util.CLUSTERS[call])
