@@ -11,7 +11,7 @@
 // power of two that puts its largest element between 2^14 and 2^15.
 //
 // A CTA has one tile of query rows (two CTAs to a multiprocessor, heads of up to 128 elements; 96 registers, 40 bytes spill), or two that share what is unpacked (one CTA); the softmax reads S
-// twice, once for its maximum.  B200, 32 query heads over 8 heads of 128, e4m3: 5 tokens over 60000 rows 58 us, 4 chunks of 56 over 3100 to 5500 rows 48 (one tile of rows to a CTA: 51), of 33
+// twice, once for its maximum.  B200, 32 query heads over 8 heads of 128, e4m3: 5 tokens over 60000 rows 58 us, 4 chunks of 56 over 3100 to 5500 rows 46 (one tile of rows to a CTA: 51), of 33
 // over 4000 rows 38 (45).  Two tiles of rows and 64 keys take 1.7 us, as in attend_tile.cu: without the exponentials, without most of the unpacking or of the second product 0 to 10 % less, so that it
 // is the way of a tile from warp to warp.  The codes a tile ahead in registers instead of a ring: half as long again (a warp's loads wait for one another); twice the ring: the same.
 #include "attend_tile.cuh"
