@@ -20,6 +20,26 @@ constexpr int kScaleLeast = -117, kScaleMostE4m3 = 119, kScaleMostE2m1 = 125;
 MVLA_BOTH constexpr int page_row_bytes(int kind, int d, int wide) { return kind == MVLA_PAGE_ROWS ? d * wide : kind == MVLA_PAGE_E4M3 ? d : d / 2; }
 MVLA_BOTH constexpr int page_row_scales(int kind, int d) { return kind == MVLA_PAGE_ROWS ? 0 : kind == MVLA_PAGE_E4M3 ? 1 : d / kPageGroup; }
 
+// Rows into pages and out (page_rows.cu): a thread's place in the rows of its CTA, which tensor, head and lane of the head it has, and in which rows.
+constexpr int kRowThreads = 256;
+struct RowSlot {
+    bool values, on;
+    int head, lane, first, step;
+};
+MVLA_BOTH constexpr RowSlot row_slot(int thread, int column, int lanes, int kv_heads, bool keys, bool values)
+{
+    const int heads = (keys ? kv_heads : 0) + (values ? kv_heads : 0), slots = heads * lanes;
+    int u = column * kRowThreads + thread, first = 0, step = 1;
+    if (slots < kRowThreads) {
+        step = kRowThreads / slots;
+        first = thread / slots;
+        u = first < step ? thread - first * slots : slots;
+    }
+    const bool on = u < slots;
+    const int h = on ? u / lanes : 0;                        // (the surplus threads copy nothing; what they form addresses of is there all the same)
+    return {!keys || h >= kv_heads, on, keys && h >= kv_heads ? h - kv_heads : h, u % lanes, first, step};
+}
+
 // Single tokens (page_token.cu): subtiles of 16 keys in a warp's tile, bytes of a tile in shared memory (in whole groups of 64 columns of the values),
 // tiles of a warp, and the CTAs that fit on a multiprocessor.
 constexpr int kPageTokenStages = 2;

@@ -18,7 +18,7 @@
 namespace mvla {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kThreads = kRowThreads;
 constexpr int kBlockRows = 32;               // of a CTA at a time, at most
 constexpr int kPieces = 2;
 constexpr int kWriteAhead = 2;               // rows of a thread on their way
@@ -165,35 +165,6 @@ __device__ __forceinline__ Place locate(const PageRowsArgs& a, int r)
     return p;
 }
 
-// A thread's place in the rows of its CTA: which tensor, head and elements it has, and in which rows.
-struct Slot {
-    bool values, on;
-    int head, lane, first, step;
-};
-template <int LANES>
-__device__ __forceinline__ Slot slot_of(const PageRowsArgs& a)
-{
-    const int heads = (a.k ? a.pool.kv_heads : 0) + (a.v ? a.pool.kv_heads : 0), slots = heads * LANES;
-    const int t = threadIdx.x;
-    Slot s;
-    int u;
-    if (slots >= kThreads) {
-        u = static_cast<int>(blockIdx.y) * kThreads + t;
-        s.first = 0;
-        s.step = 1;
-    } else {
-        s.step = kThreads / slots;
-        s.first = t / slots;
-        u = s.first < s.step ? t - s.first * slots : slots;
-    }
-    s.lane = u % LANES;
-    const int h = u / LANES;
-    s.values = !a.k || h >= a.pool.kv_heads;
-    s.head = s.values && a.k ? h - a.pool.kv_heads : h;
-    s.on = u < slots;
-    return s;
-}
-
 // Goes over this CTA's blocks of rows: work(places, rows) of each.
 template <int KIND, bool TILES, int WIDE, class Work>
 __device__ __forceinline__ void over_blocks(const PageRowsArgs& a, Place (*places)[kBlockRows], Work work)
@@ -223,7 +194,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) page_write_kernel(const __
     __shared__ Place places[2][kBlockRows];
     pdl_wait();
     pdl_trigger();
-    const Slot s = slot_of<LANES>(a);
+    const RowSlot s = row_slot(threadIdx.x, blockIdx.y, LANES, a.pool.kv_heads, a.k != nullptr, a.v != nullptr);
     const int d = a.pool.head_dim, row_bytes = page_row_bytes(KIND, d, kWide), groups = page_row_scales(KIND, d);
     const char* const src = static_cast<const char*>(s.values ? a.v : a.k) + s.head * (s.values ? a.v_head : a.k_head) * kWide;
     const int64_t head = static_cast<int64_t>(s.head) << a.pool.page_shift;
@@ -300,7 +271,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) page_read_kernel(const __g
     __shared__ Place places[2][kBlockRows];
     pdl_wait();
     pdl_trigger();
-    const Slot s = slot_of<LANES>(a);
+    const RowSlot s = row_slot(threadIdx.x, blockIdx.y, LANES, a.pool.kv_heads, a.k != nullptr, a.v != nullptr);
     const int d = a.pool.head_dim, row_bytes = page_row_bytes(KIND, d, kWide), groups = page_row_scales(KIND, d);
     char* const dst = static_cast<char*>(s.values ? a.v : a.k) + s.head * (s.values ? a.v_head : a.k_head) * kWide;
     const int64_t head = static_cast<int64_t>(s.head) << a.pool.page_shift;
@@ -331,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) page_read_kernel(const __g
                     } else {
                         w[u][i] = Codes{};
                         if (there) w[u][i] = *reinterpret_cast<const Codes*>(src + piece * (KIND == MVLA_PAGE_E4M3 ? 8 : 4));
-                        if (i < kBytes && from >= 0) byte[u][i] = scales[at[r].scale + (KIND == MVLA_PAGE_E4M3 || !on[i] ? 0 : piece / (kPageGroup / 8))];
+                        if (i < kBytes && from >= 0 && s.on) byte[u][i] = scales[at[r].scale + (KIND == MVLA_PAGE_E4M3 || !on[i] ? 0 : piece / (kPageGroup / 8))];
                     }
                 }
             }
