@@ -479,16 +479,17 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
         tc_fence_before();
     }
     __syncthreads();
+    // (before the cluster meets: who holds tensor memory waits for no other CTA, which may wait for some of it behind another launch's)
+    if (warp == Sh::kIssues) {
+        tc_fence_after();
+        tmem_dealloc(tmem, Sh::kColumns);
+    }
     if (PAGED && ranks > 1) {                                // (reached by all CTAs of the cluster, whoever gave up)
         cluster_arrive_release();
         cluster_wait_acquire();
         join_cluster<1>(a, s, kv_at, smem_u32(row_ml), reinterpret_cast<float*>(list), ranks, q0, per, head0, part_of_seq);      // (no list of counted positions)
         cluster_arrive_release();                            // (nobody's sums are gone while another reads them)
         cluster_wait_acquire();
-    }
-    if (warp == Sh::kIssues) {
-        tc_fence_after();
-        tmem_dealloc(tmem, Sh::kColumns);
     }
 }
 

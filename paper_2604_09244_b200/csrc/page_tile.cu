@@ -466,16 +466,17 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         tc_fence_before();
     }
     __syncthreads();
+    // (before the cluster meets: who holds tensor memory waits for no other CTA, which may wait for some of it behind another launch's)
+    if (warp == Sh::kIssues) {
+        tc_fence_after();
+        tmem_dealloc(tmem, Sh::kColumns);
+    }
     if (ranks > 1) {                                         // (reached by all CTAs of the cluster, whoever gave up)
         cluster_arrive_release();
         cluster_wait_acquire();
         join_cluster<T>(a, s, q_at, smem_u32(row_ml), reinterpret_cast<float*>(raw + (q_at - smem_u32(raw)) + T * D * kRows * 4), ranks, q0, per, head0, part_of_seq);
         cluster_arrive_release();                            // (nobody's sums are gone while another reads them)
         cluster_wait_acquire();
-    }
-    if (warp == Sh::kIssues) {
-        tc_fence_after();
-        tmem_dealloc(tmem, Sh::kColumns);
     }
 }
 

@@ -11,8 +11,8 @@
 // check of this: it answers one CTA per multiprocessor for every kernel that allocates tensor memory, where three of the
 // scoring kernel's do run side by side.)
 // That bounds the CTAs of one launch.  Launches of other shapes, streams or contexts may share the multiprocessor, with
-// other columns per byte of shared memory: so the latency-shaped kernel gives its columns back before it waits for its
-// cluster, and the streaming kernel (below) leaves no room for any other holder.
+// other columns per byte of shared memory: so the latency-shaped kernel and the attention kernels by tiles give their columns back before they
+// wait for their clusters, and the streaming kernel (below) leaves no room for any other holder.
 #pragma once
 
 #include <stddef.h>
