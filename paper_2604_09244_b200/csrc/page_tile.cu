@@ -19,6 +19,7 @@
 #include "page.cuh"
 
 #include <algorithm>
+#include <cfloat>
 
 namespace mvla {
 namespace {
@@ -357,7 +358,8 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             const int buf = i & 1;
             tc_fence_after();
             const int2 ref_of = refs[i % kTileRefs];
-            const float scale = q_scale * two_to(ref_of.x - 127);
+            // (not zero, whatever the sizes: zero times the -infinity of a row that is not seen is no number; scores that small are as good as zero)
+            const float scale = fmaxf(q_scale * two_to(ref_of.x - 127), FLT_MIN);
             const uint32_t s_col = tmem + w * Sh::kOf + buf * kKeys + lanes;
             float top;
             {

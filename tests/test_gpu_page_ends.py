@@ -4,7 +4,9 @@ import torch
 
 import page_util as P
 from page_util import E2M1, E4M3, ROWS
+from page_strict import check
 from paper_2604_09244_b200 import mvla
+from test_page_plan_cpu import PAGE_TILE, TOKEN, plan, shim  # noqa: F401
 from test_gpu_page import BF16, FP32, context, generator, same
 
 pytestmark = pytest.mark.gpu
@@ -53,3 +55,64 @@ def test_clusters_of_two_shapes_on_two_streams():
     torch.cuda.synchronize()
     for call, out in zip(calls, outs):
         assert all(torch.equal(x, call[5]) for x in out)
+
+
+# (heads, key heads, elements, queries, rows) of calls over quantised pages, and the form that they take: tokens; tiles unpacked on the way, for one and two blocks of
+# query rows; unpacked first
+CALLS = [(8, 4, 64, 1, 300), (8, 2, 96, 4, 700), (8, 4, 64, 37, 300), (8, 4, 128, 60, 900), (4, 2, 256, 20, 500), (32, 8, 128, 50, 9000), (8, 4, 64, 200, 500)]
+
+
+def form_of(shim, kind, H, G, d, n_q, n, **kw):
+    """Whether weights meet the values in fp16, and the form."""
+    p, _ = plan(shim, [(n_q, n)], kind=kind, heads=(H, G, d), **kw)
+    return p["form"] == TOKEN or p["unpack"] > 0, (p["form"], p["unpack"])
+
+
+def test_calls_take_every_form(shim):
+    assert {form_of(shim, E4M3, *c)[1] for c in CALLS} == {(TOKEN, 0), (PAGE_TILE, 1), (PAGE_TILE, 2), (PAGE_TILE, 0)}
+
+
+@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("call", CALLS)
+def test_scales_of_all_sizes(shim, call, kind):
+    """Scores that are as good as zero, or whose queries or keys are far from one: rows that a mask hides stay hidden."""
+    H, G, d, n_q, n = call
+    gen = generator(n_q + d)
+    ctx = context(BF16, H, G, d)
+    table, n_pages = P.make_table(gen, [n], 32)
+    pool = P.make_pool(gen, n_pages, G, 32, d, kind, BF16)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    window = 150 if n < 1000 else 8400
+    fp16, _ = form_of(shim, kind, *call, window=window)
+    x = torch.randn(n_q, H, d, generator=gen, device="cuda")
+    for size, scale in ((1.0, 1e-30), (1.0, 1e-36), (1.0, 1e-37), (1.0, 9e-39), (2.0 ** -112, 0.0), (2.0 ** -125, 0.0), (2.0 ** -60, 2.0 ** -70)):
+        check(ctx, pool, kind, seqs, table, (x * size).to(BF16), 32, fp16, window=window, scale=scale)
+
+
+@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("call", CALLS)
+def test_tiles_of_nothing(shim, call, kind):
+    """Whole tiles on pages outside the pool, or of rows of zeros as they are written, under the diagonal and at a window's edge, with queries of small elements."""
+    H, G, d, n_q, n = call
+    gen = generator(n_q + 2 * d)
+    ctx = context(BF16, H, G, d)
+    table, n_pages = P.make_table(gen, [n], 64)
+    pool = P.make_pool(gen, n_pages, G, 64, d, kind, BF16)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    last = (n - 1) // 64
+    window = n % 64 + n_q + 80 if n < 1000 else n - 70
+    edge = max(0, n - window) // 64
+    pages = table[0, [last, edge]].long()
+    zero = P.quantise(torch.zeros(1, d, device="cuda", dtype=BF16), kind)
+    fp16, _ = form_of(shim, kind, *call, window=window)
+    x = torch.randn(n_q, H, d, generator=gen, device="cuda")
+    for outside in (True, False):
+        if outside:
+            table[0, [last, edge]] = -1
+        else:
+            table[0, [last, edge]] = pages.to(torch.int32)
+            for codes, scale in ((pool.k, pool.k_scale), (pool.v, pool.v_scale)):
+                P.bits(codes)[pages] = P.bits(zero[1])[0]
+                scale[pages] = zero[2][0]
+        for size in (2.0 ** -4, 2.0 ** -12, 2.0 ** -40):
+            check(ctx, pool, kind, seqs, table, (x * size).to(BF16), 64, fp16, window=window)
