@@ -6,9 +6,9 @@
 // a page at a time; four warps turn them into fp16 and store them as the MMAs read them (128-byte swizzle).
 // Scales are powers of two.  A tile's largest scale of its keys becomes a factor of its scores and the largest one of its values a factor of its weights (both the same
 // for the whole tile); what a row, or 32 elements, have less is multiplied into the codes, which have as much room above in fp16 (2^7 for e4m3, 2^13 for e2m1): rows or
-// groups below 2^-21 (2^-27) of their tile's largest scale count as nothing.  Outputs are summed in units of the largest values so far (and four
-// times more); where a tile's are larger still, the sums are taken down, as they are when a row's reference moves.  Queries are fp16 too, every row times a
-// power of two that puts its largest element between 2^14 and 2^15.
+// groups of keys below 2^-21 (2^-27) of their tile's largest scale count as nothing.  Values: the products of weights and scales that make up a row's output are of other sizes than its weights, so
+// that they have a reference of their own, in which O is counted.  Where the scales of a tile's values lie more than 2^kSpread apart, every row's is part of its weight (two exponentials to a key).
+// Queries are fp16 too, every row times a power of two that puts its largest element between 2^14 and 2^15.
 //
 // A CTA has one tile of query rows (two CTAs to a multiprocessor, heads of up to 128 elements; 96 registers, 40 bytes spill), or two that share what is unpacked (one CTA); the softmax reads S
 // twice, once for its maximum.  B200, 32 query heads over 8 heads of 128, e4m3: 5 tokens over 60000 rows 58 us, 4 chunks of 56 over 3100 to 5500 rows 46 (one tile of rows to a CTA: 51), of 33
@@ -41,13 +41,24 @@ struct PageTileShape {
     // the ring: codes of a tile's keys, with the scales of its keys and values, or codes of its values
     static constexpr int kRowBytes = page_row_bytes(KIND, D32 * 32, 2), kGroups = page_row_scales(KIND, D32 * 32);
     static constexpr int kCodes = kKeys * kRowBytes, kSlot = kCodes + 2 * kKeys * kGroups, kSlots = T == 1 ? 3 : 4;
-    static constexpr int kRoom = ((kCtas == 2 ? kSmemPerSm / 2 - kSmemReservedPerCta : kSmemMaxPerCta) - (T == 1 ? 6 : 8) * 1024 - kQBytes - kSlots * kSlot) / kStage;
+    static constexpr int kFixed = (T == 2 ? 8 : KIND == MVLA_PAGE_E4M3 ? 6 : 9) * 1024;      // static shared memory, and what the tiles' alignment takes
+    static constexpr int kRoom = ((kCtas == 2 ? kSmemPerSm / 2 - kSmemReservedPerCta : kSmemMaxPerCta) - kFixed - kQBytes - kSlots * kSlot) / kStage;
     static constexpr int kStages = kRoom > kMaxStages ? kMaxStages : kRoom;
     static constexpr int kSmem = 1024 + kQBytes + kStages * kStage + kSlots * kSlot;
     static constexpr int kPieces = 8 * D32 / kDecoders;      // of eight elements, of a decoding thread, in a tile of keys or of values
     static_assert(kStages >= 3 && kSlot % 16 == 0, "shape");
 };
-constexpr int kTileRefs = 8;                 // tiles whose references are kept
+// Of a tile, for the softmax: of every row of values the exponent of its scale, the largest and the least of them, and whether they are far apart; the byte of the largest scale of its keys.
+struct __align__(16) TileScales {
+    float exponent[kKeys];
+    float most, least;
+    int far, keys;
+};
+// The reference of weights times scales is the largest one, or (where a tile's are not far apart) at most 2^kSpread below; against the tile's largest scale no weight is more than 2^kMoveAt
+// above the reference, and with its own, which counts where they are far apart, none either: 2^(kMoveAt + kF16Lift) is a number of fp16.
+constexpr int kSpread = 6;
+constexpr float kMoveScaledAt = kMoveAt - kSpread;
+constexpr int kTileScales = 4;               // tiles whose scales are kept
 
 __device__ __forceinline__ void codes_f16(uint2 w, uint32_t (&h)[4])
 {
@@ -60,6 +71,8 @@ __device__ __forceinline__ uint32_t times2(uint32_t x, uint32_t f)
     const __half2 h = __hmul2(*reinterpret_cast<const __half2*>(&x), *reinterpret_cast<const __half2*>(&f));
     return *reinterpret_cast<const uint32_t*>(&h);
 }
+// Bits of 2^e in fp16, e at most 15: below 2^-24 zero.
+__device__ __forceinline__ uint32_t power_f16(int e) { return e > -15 ? static_cast<uint32_t>(e + 15) << 10 : e >= -24 ? 1u << (e + 24) : 0u; }
 __device__ __forceinline__ void store16(uint32_t at, const uint32_t (&w)[4])
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
@@ -79,11 +92,12 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
     __shared__ uint64_t bars[2 * kMaxStages + 3 + 5 * T + 2 * Sh::kSlots];
     __shared__ unsigned groups_there[Sh::kSlots];            // of a slot: a bit to every 16 rows that have a page
     __shared__ uint32_t factors[2][kKeys][G];                // of a tile's keys and values: fp16, twice
-    __shared__ uint32_t warp_top[4];
-    __shared__ int2 refs[kTileRefs];                         // bytes of the largest scales of a tile's keys and values
+    __shared__ uint2 warp_top[4];                            // largest and least byte of 32 rows' scales
+    __shared__ TileScales scales[kTileScales];
     __shared__ int dead;
     __shared__ uint32_t tmem_base;
     __shared__ float2 row_ml[T][kRows];
+    static_assert(sizeof bars + sizeof factors + sizeof scales + sizeof row_ml + 128 + 1024 <= Sh::kFixed, "room beside the tiles");
     static_assert(Sh::kSmem - 1024 >= T * (D * kRows + kJoinFloats) * 4, "room for the sums of a cluster's CTA");
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t q_at = base, kv_at = base + Sh::kQBytes;
@@ -223,30 +237,39 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             const bool masked = masks(j0);
             ok = ok && codes_there(2 * i);
             const unsigned there = groups_there[2 * i % Sh::kSlots];
-            uint32_t scale[G], top = 0;
-            if (dt < 128) {                                  // of one row, of keys or values (those that nobody sees may hold anything)
+            uint32_t scale[G], own = kScaleLeast + 127;
+            if (dt < 128) {                                  // of one row, of keys or values (those that nobody sees may hold anything; without a page the least scale)
                 const int j = j0 + own_row;
-                const bool on = (there >> (own_row >> 4) & 1u) && j < len && some_sees(lo, hi, j, a.window, a.n_sink);
+                const bool on = j < len && some_sees(lo, hi, j, a.window, a.n_sink), holds = on && (there >> (own_row >> 4) & 1u);
                 const uint8_t* const b = ring + 2 * i % Sh::kSlots * Sh::kSlot + Sh::kCodes + dt * G;
 #pragma unroll
                 for (int g = 0; g < G; ++g) {
-                    scale[g] = on ? b[g] : 0u;
-                    top = max(top, scale[g]);
+                    scale[g] = holds ? b[g] : 0u;
+                    own = max(own, scale[g]);
                 }
-                top = __reduce_max_sync(0xffffffffu, top);
-                if (lane == 0) warp_top[warp - Sh::kDecodes] = top;
+                const uint32_t top = __reduce_max_sync(0xffffffffu, own), low = __reduce_min_sync(0xffffffffu, on ? own : 255u);
+                if (lane == 0) warp_top[warp - Sh::kDecodes] = make_uint2(top, low);
             }
             meet();                                          // (and nobody is with the last tile's factors any more)
-            const int refs_here[2] = {static_cast<int>(max(max(warp_top[0], warp_top[1]), 10u)), static_cast<int>(max(max(warp_top[2], warp_top[3]), 10u))};
+            const int refs_here[2] = {static_cast<int>(max(warp_top[0].x, warp_top[1].x)), static_cast<int>(max(warp_top[2].x, warp_top[3].x))};
+            const int least = static_cast<int>(min(warp_top[2].y, warp_top[3].y));
+            const bool far = refs_here[1] - least > kSpread;
             if (dt < 128) {
+                const int ref = side == 1 && far ? static_cast<int>(own) : refs_here[side];
 #pragma unroll
-                for (int g = 0; g < G; ++g) {
-                    const int e = static_cast<int>(scale[g]) - refs_here[side] + kCodeLift + 15;
-                    factors[side][own_row][g] = static_cast<uint32_t>(max(e, 0)) * 0x04000400u;
-                }
+                for (int g = 0; g < G; ++g) factors[side][own_row][g] = power_f16(static_cast<int>(scale[g]) - ref + kCodeLift) * 0x10001u;
             }
-            ok = ok && room(2 * i);                          // (the references of kTileRefs tiles ago have been read by then)
-            if (ok && dt == 0) refs[i % kTileRefs] = make_int2(refs_here[0], refs_here[1]);
+            ok = ok && room(2 * i);                          // (the scales of kTileScales tiles ago have been read by then: stages hold three tiles at most, and the softmax is one behind)
+            if (ok && dt < 128) {
+                TileScales& to = scales[i % kTileScales];
+                if (dt == 0) {
+                    to.keys = refs_here[0];
+                    to.most = static_cast<float>(refs_here[1] - 127 - kCodeLift);
+                    to.least = static_cast<float>(least - 127 - kCodeLift);
+                    to.far = far;
+                }
+                if (side == 1) to.exponent[own_row] = static_cast<float>(static_cast<int>(own) - 127 - kCodeLift);
+            }
             meet();
             if (ok) decode(2 * i, masked, j0, there);
             ok = ok && codes_there(2 * i + 1) && room(2 * i + 1);
@@ -341,8 +364,8 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         }
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;        // this warp's 32 lanes
         const uint32_t o_col = tmem + w * Sh::kOf + Sh::kO + lanes;
-        float m = -CUDART_INF_F, l = 0.f;                    // reference (scaled), sum (of weights against the reference less kF16Lift)
-        int unit = 0;                                        // byte of the scale that O is counted in
+        // references of the scores and of weights times scales (in powers of two), sum of the weights (against the first, less kF16Lift); O: against the second, likewise
+        float m = -CUDART_INF_F, m_w = -CUDART_INF_F, l = 0.f;
         bool masked = false;
         uint32_t visible[kKeys / 32];                        // a bit for every key of the tile that the row sees
         const auto look = [&](int i) {
@@ -357,11 +380,20 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         const auto weigh = [&](int i) {
             const int buf = i & 1;
             tc_fence_after();
-            const int2 ref_of = refs[i % kTileRefs];
+            const TileScales& of = scales[i % kTileScales];
             // (not zero, whatever the sizes: zero times the -infinity of a row that is not seen is no number; scores that small are as good as zero)
-            const float scale = fmaxf(q_scale * two_to(ref_of.x - 127), FLT_MIN);
+            const float scale = fmaxf(q_scale * two_to(of.keys - 127), FLT_MIN);
+            const uint64_t scale2 = two_f32(scale, scale);
             const uint32_t s_col = tmem + w * Sh::kOf + buf * kKeys + lanes;
-            float top;
+            const auto scores_of = [&](int c0, float (&x)[32]) {
+                tmem_ld_cols<32>(s_col + c0, x);
+                if (masked) {
+                    const uint32_t sees = c0 ? visible[1] : visible[0];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) x[c] = sees >> c & 1u ? x[c] : -CUDART_INF_F;
+                }
+            };
+            float tops[4];
             {
                 float x[kKeys];
                 tmem_ld_cols<kKeys>(s_col, x);
@@ -369,63 +401,96 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
 #pragma unroll
                     for (int c = 0; c < kKeys; ++c) x[c] = visible[c / 32] >> (c & 31) & 1u ? x[c] : -CUDART_INF_F;
                 }
-                float tops[4] = {x[0], x[1], x[2], x[3]};
+#pragma unroll
+                for (int b = 0; b < 4; ++b) tops[b] = x[b];
 #pragma unroll
                 for (int c = 4; c < kKeys; c += 8) {         // (three at a time)
 #pragma unroll
                     for (int b = 0; b < 4; ++b) tops[b] = c + 4 + b < kKeys ? fmaxf(fmaxf(tops[b], x[c + b]), x[c + 4 + b]) : fmaxf(tops[b], x[c + b]);
                 }
-                top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
             }
-            top *= scale;                                    // (scale is positive)
-            const bool move = top > m + kMoveAt;
-            if (i == 0) unit = min(ref_of.y + 2, 253);
-            const bool larger = ref_of.y > unit;             // (of all rows alike)
-            if (i > 0 && (larger || __any_sync(0xffffffffu, move))) {
-                // (the step before may still be adding; the one before that was complete before this S was)
-                if (!guard.wait_all(o_step(w), (i - 1) & 1)) return false;
-                tc_fence_after();
-                const float f = move ? ex2_approx(m - top) : 1.f, by = larger ? f * two_to(max(unit - ref_of.y, -126)) : f;
+            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;      // (scale is positive)
+            const bool far = of.far != 0;
+            if (top > m + kMoveAt) {
+                l *= ex2_approx(m - top);
+                m = top;
+            }
+            if (__any_sync(0xffffffffu, top + of.most > m_w + kMoveAt)) {
+                float top_w = top + of.least;
+                if (far) {                                   // with every row's own scale: what other queries see does not count
+                    top_w = -CUDART_INF_F;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) {
-                    float o[32];
-                    uint32_t y[32];
-                    tmem_ld_cols<32>(o_col + c, o);
+                    for (int c0 = 0; c0 < kKeys; c0 += 32) {
+                        float x[32];
+                        scores_of(c0, x);
 #pragma unroll
-                    for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(o[k] * by);
-                    tmem_st_cols<32>(o_col + c, y);
+                        for (int c = 0; c < 32; ++c) top_w = fmaxf(top_w, fmaf(x[c], scale, of.exponent[c0 + c]));
+                    }
                 }
-                l *= f;
+                const bool move = top_w > m_w + kMoveScaledAt;
+                if (i > 0 && __any_sync(0xffffffffu, move)) {
+                    // (the step before may still be adding; the one before that was complete before this S was)
+                    if (!guard.wait_all(o_step(w), (i - 1) & 1)) return false;
+                    tc_fence_after();
+                    const float f = move ? ex2_approx(m_w - top_w) : 1.f;
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        float o[32];
+                        uint32_t y[32];
+                        tmem_ld_cols<32>(o_col + c, o);
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) y[k] = __float_as_uint(o[k] * f);
+                        tmem_st_cols<32>(o_col + c, y);
+                    }
+                }
+                if (move) m_w = top_w;
             }
-            if (larger) unit = ref_of.y;
-            if (move) m = top;
-            const int down = min(unit - ref_of.y, 64);       // this tile's values are counted in units 2^down larger than their own (more than 64: nothing is left of them)
-            const float ref = m == -CUDART_INF_F ? 0.f : m - kF16Lift + static_cast<float>(down);
-            const uint64_t scale2 = two_f32(scale, scale), ref2 = two_f32(-ref, -ref);
+            // The weights as they meet the values are those that have the sum, in other units, as long as a tile's values have one scale (2^64 above the scores' reference nothing is left of the
+            // tile's values, and the units may be smaller).
+            const float ref = m == -CUDART_INF_F ? 0.f : far ? m : fminf(m_w - of.most, m + 64.f);
+            const uint64_t ref2 = two_f32(kF16Lift - ref, kF16Lift - ref);
             uint64_t sums[2] = {0, 0};
+            if (!far) {
 #pragma unroll
-            for (int c0 = 0; c0 < kKeys; c0 += 32) {
-                float x[32];
-                uint32_t weights[16];
-                tmem_ld_cols<32>(s_col + c0, x);
-                if (masked) {
+                for (int c0 = 0; c0 < kKeys; c0 += 32) {
+                    float x[32];
+                    uint32_t weights[16];
+                    scores_of(c0, x);
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) x[c] = visible[c0 / 32] >> c & 1u ? x[c] : -CUDART_INF_F;
+                    for (int c = 0; c < 32; c += 2) {
+                        float y, z;
+                        split_f32(fma_f32x2(two_f32(x[c], x[c + 1]), scale2, ref2), y, z);
+                        y = ex2_approx(y);
+                        z = ex2_approx(z);
+                        sums[c / 2 & 1] = add_f32x2(sums[c / 2 & 1], two_f32(y, z));
+                        weights[c / 2] = two_f16(y, z);      // (rounded for the product alone)
+                    }
+                    tmem_st_cols<16>(s_col + c0 / 2, weights);
                 }
+            } else {
+                const float to_w = m == -CUDART_INF_F ? 0.f : kF16Lift - m_w;
+                const uint64_t to_w2 = two_f32(to_w, to_w);
+#pragma unroll 1
+                for (int c0 = 0; c0 < kKeys; c0 += 32) {
+                    float x[32];
+                    uint32_t weights[16];
+                    scores_of(c0, x);
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    float y, z;
-                    split_f32(fma_f32x2(two_f32(x[c], x[c + 1]), scale2, ref2), y, z);
-                    y = ex2_approx(y);
-                    z = ex2_approx(z);
-                    sums[c / 2 & 1] = add_f32x2(sums[c / 2 & 1], two_f32(y, z));
-                    weights[c / 2] = two_f16(y, z);          // (rounded for the product alone)
+                    for (int c = 0; c < 32; c += 2) {
+                        const float2 e = *reinterpret_cast<const float2*>(of.exponent + c0 + c);
+                        const uint64_t x2 = two_f32(x[c], x[c + 1]);
+                        float y, z;
+                        split_f32(fma_f32x2(x2, scale2, ref2), y, z);
+                        sums[0] = add_f32x2(sums[0], two_f32(ex2_approx(y), ex2_approx(z)));
+                        split_f32(add_f32x2(fma_f32x2(x2, scale2, two_f32(e.x, e.y)), to_w2), y, z);
+                        weights[c / 2] = two_f16(ex2_approx(y), ex2_approx(z));
+                    }
+                    tmem_st_cols<16>(s_col + c0 / 2, weights);
                 }
-                tmem_st_cols<16>(s_col + c0 / 2, weights);
             }
             float even, odd;
             split_f32(add_f32x2(sums[0], sums[1]), even, odd);
-            l = fmaf(even + odd, two_to(down), l);
+            l = fmaf(even + odd, m == -CUDART_INF_F ? 1.f : ex2_approx(ref - m), l);
             tmem_st_wait();
             tc_fence_before();
             mbar_arrive(p_full(w, buf));
@@ -437,13 +502,14 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         tc_fence_after();
         const int64_t part = s.part0 + static_cast<int64_t>(part_of_seq) * s.n_q + i_row;
         float4* const sums = reinterpret_cast<float4*>(raw + (q_at - smem_u32(raw)));         // of a cluster's CTA (sums_at)
-        const float by = (l > 0.f ? two_to(unit - 127) * (s.parts > 1 || ranks > 1 ? 1.f : 1.f / l) : 0.f) * two_to(-kCodeLift);
+        // (by halves: of values near 2^-117 the factor is no normal number)
+        const float half = l > 0.f ? exp2f(0.5f * (m_w - m)) : 0.f, by = half * (s.parts > 1 || ranks > 1 || !(l > 0.f) ? 1.f : 1.f / l);
         m -= kF16Lift;
         for (int c = 0; c < D && ok; c += 32) {
             float o[32];
             if (n > 0) tmem_ld_cols<32>(o_col + c, o);
 #pragma unroll
-            for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? o[k] * by : 0.f;
+            for (int k = 0; k < 32; ++k) o[k] = l > 0.f ? o[k] * half * by : 0.f;
             if (ranks > 1) {
 #pragma unroll
                 for (int k = 0; k < 32; k += 4) sums[sums_at(w * kRows + r, (c + k) / 4, D)] = make_float4(o[k], o[k + 1], o[k + 2], o[k + 3]);

@@ -116,3 +116,51 @@ def test_tiles_of_nothing(shim, call, kind):
                 scale[pages] = zero[2][0]
         for size in (2.0 ** -4, 2.0 ** -12, 2.0 ** -40):
             check(ctx, pool, kind, seqs, table, (x * size).to(BF16), 64, fp16, window=window)
+
+
+def sized_pool(gen, kind, G, d, n, page_rows, k=None, v=None):
+    """(pool, table) of one sequence whose rows of keys and values [n, G, d] are random, times k and v."""
+    table, n_pages = P.make_table(gen, [n], page_rows, spare=0)
+    j = torch.arange(n, device="cuda")
+    out = []
+    for size in (k, v):
+        x = torch.randn(n, G, d, generator=gen, device="cuda")
+        rows = torch.zeros(n_pages, page_rows, G, d, device="cuda")
+        rows[table[0].long()[j // page_rows], j % page_rows] = x if size is None else size(x, j[:, None, None])
+        out.append(P.quantise(rows.transpose(1, 2).contiguous().to(BF16), kind))
+    return mvla.PagePool(out[0][1].contiguous(), out[1][1].contiguous(), out[0][2], out[1][2]), table
+
+
+@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("call", CALLS)
+def test_large_values_of_little_weight(shim, call, kind):
+    """The first rows, or one in 40, have values 2^24 to 2^110 larger than the others and scores far below them, to nearly nothing or to nothing at all."""
+    H, G, d, n_q, n = call
+    gen = generator(n_q + 3 * d)
+    ctx = context(BF16, H, G, d)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    fp16, _ = form_of(shim, kind, *call)
+    q = torch.randn(n_q, H, d, generator=gen, device="cuda")
+    q[..., 0] = 8
+    for faint in (lambda j: j < 64, lambda j: j % 40 == 7, lambda j: (j >= 64) & (j < 100)):
+        for size, low in ((2.0 ** 24, -64.0), (2.0 ** 30, -2000.0), (2.0 ** 110, -2000.0), (2.0 ** 24, 0.0)):
+            keys = lambda x, j: torch.where(faint(j) & (torch.arange(d, device="cuda") == 0), low, x)  # noqa: B023, E731
+            pool, table = sized_pool(gen, kind, G, d, n, 32, keys, lambda x, j: torch.where(faint(j), x * size, x))  # noqa: B023
+            check(ctx, pool, kind, seqs, table, q.to(BF16), 32, fp16)
+
+
+@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("call", CALLS)
+def test_values_of_all_sizes(shim, call, kind):
+    """Values that grow and shrink from row to row, over the whole range of the scales, those of rows that are not seen yet among them; values near its lower end."""
+    H, G, d, n_q, n = call
+    gen = generator(n_q + 5 * d)
+    ctx = context(BF16, H, G, d)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    fp16, _ = form_of(shim, kind, *call)
+    q = torch.randn(n_q, H, d, generator=gen, device="cuda").to(BF16)
+    new = n - n_q                                              # the first query's row
+    for e in (lambda j: (j - new).clamp(min=0) * (200.0 / max(n_q, 8)) - 100, lambda j: (j - new).clamp(min=0) * 1.5 - 20, lambda j: (n - j) * (200.0 / n) - 110,
+              lambda j: j * (200.0 / n) - 110, lambda j: j * 0.0 - 108, lambda j: j % 2 * 180.0 - 100, lambda j: j % 3 * 13.0 - 20):
+        pool, table = sized_pool(gen, kind, G, d, n, 64, None, lambda x, j: x * torch.exp2(e(j.float()).clamp(-110, 110)))  # noqa: B023
+        check(ctx, pool, kind, seqs, table, q, 64, fp16)
