@@ -26,6 +26,7 @@ namespace mvla {
 namespace {
 
 constexpr int kThreads = 320;                // attend_weights_kernel
+constexpr float kLargeScore = 65536.f;       // beyond, scores over pages are not scaled and taken from their reference in one step
 // Smallest and largest position of queries [i0, i1) of a sequence, by one warp.
 __device__ __forceinline__ void query_span(const AttArgs& a, const AttSeq& s, int len, int i0, int i1, int lane, int* lo, int* hi)
 {
@@ -372,8 +373,8 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
 #pragma unroll
                 for (int b = 0; b < 4; ++b) tops[b] = c + 4 + b < kKeys ? fmaxf(fmaxf(tops[b], x[c + b]), x[c + 4 + b]) : fmaxf(tops[b], x[c + b]);
             }
-            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;      // (scale is positive)
-            const bool move = top > m + kMoveAt;
+            const float top = __fmul_rn(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), scale);      // (scale is positive; rounded before anything is taken from it)
+            const bool move = PAGED ? top - m > kMoveAt : top > m + kMoveAt;
             if (i > 0 && __any_sync(0xffffffffu, move)) {
                 // (the step before may still be adding; the one before that was complete before this S was)
                 if (!guard.wait_all(o_step, (i - 1) & 1)) return false;
@@ -392,7 +393,13 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             }
             if (move) m = top;
             const float ref = m == -CUDART_INF_F ? 0.f : m - kLift;
-            const uint64_t ref2 = two_f32(-ref, -ref);
+            uint64_t by2 = scale2, ref2 = two_f32(-ref, -ref);
+            if (PAGED && __any_sync(0xffffffffu, fabsf(ref) > kLargeScore)) {        // (the largest score's distance from its reference is nothing, however large: rounded as that was)
+#pragma unroll
+                for (int c = 0; c < kKeys; ++c) x[c] = __fadd_rn(__fmul_rn(x[c], scale), -ref);
+                by2 = two_f32(1.f, 1.f);
+                ref2 = 0;
+            }
             uint64_t sums[2] = {0, 0};
 #pragma unroll
             for (int c0 = 0; c0 < kKeys; c0 += 32) {
@@ -400,7 +407,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
 #pragma unroll
                 for (int c = 0; c < 32; c += 2) {
                     float y, z;
-                    split_f32(fma_f32x2(two_f32(x[c0 + c], x[c0 + c + 1]), scale2, ref2), y, z);
+                    split_f32(fma_f32x2(two_f32(x[c0 + c], x[c0 + c + 1]), by2, ref2), y, z);
                     y = ex2_approx(y);
                     z = ex2_approx(z);
                     sums[c / 2 & 1] = add_f32x2(sums[c / 2 & 1], two_f32(y, z));

@@ -58,6 +58,7 @@ struct __align__(16) TileScales {
 // above the reference, and with its own, which counts where they are far apart, none either: 2^(kMoveAt + kF16Lift) is a number of fp16.
 constexpr int kSpread = 6;
 constexpr float kMoveScaledAt = kMoveAt - kSpread;
+constexpr float kLargeScore = 1024.f;        // beyond, scores and exponents of scales are not added up in one number (2^-13 of a weight is lost so), nor scores scaled and taken from their reference in one step
 constexpr int kTileScales = 4;               // tiles whose scales are kept
 
 __device__ __forceinline__ void codes_f16(uint2 w, uint32_t (&h)[4])
@@ -364,8 +365,9 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         }
         const uint32_t lanes = static_cast<uint32_t>(warp & 3) << 21;        // this warp's 32 lanes
         const uint32_t o_col = tmem + w * Sh::kOf + Sh::kO + lanes;
-        // references of the scores and of weights times scales (in powers of two), sum of the weights (against the first, less kF16Lift); O: against the second, likewise
-        float m = -CUDART_INF_F, m_w = -CUDART_INF_F, l = 0.f;
+        // Reference of the scores (in powers of two), what that of weights times scales lies above it, sum of the weights (against the first, less kF16Lift); O: against the second, likewise.  (The second is
+        // no number of its own: beside a score of 2^17 the exponents of scales lose their last bits.)
+        float m = -CUDART_INF_F, above = -CUDART_INF_F, l = 0.f;
         bool masked = false;
         uint32_t visible[kKeys / 32];                        // a bit for every key of the tile that the row sees
         const auto look = [&](int i) {
@@ -409,30 +411,33 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                     for (int b = 0; b < 4; ++b) tops[b] = c + 4 + b < kKeys ? fmaxf(fmaxf(tops[b], x[c + b]), x[c + 4 + b]) : fmaxf(tops[b], x[c + b]);
                 }
             }
-            const float top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])) * scale;      // (scale is positive)
-            const bool far = of.far != 0;
-            if (top > m + kMoveAt) {
-                l *= ex2_approx(m - top);
+            const float top = __fmul_rn(fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3])), scale);      // (scale is positive; rounded before anything is taken from it)
+            if (top - m > kMoveAt) {
+                const float up = top - m;                    // (infinite where there was nothing yet)
+                l *= ex2_approx(-up);
+                above -= up;
                 m = top;
             }
-            if (__any_sync(0xffffffffu, top + of.most > m_w + kMoveAt)) {
-                float top_w = top + of.least;
-                if (far) {                                   // with every row's own scale: what other queries see does not count
+            const bool some = m > -CUDART_INF_F, far = of.far != 0 || __any_sync(0xffffffffu, some && fabsf(m) > kLargeScore);
+            const float ref = some ? m : 0.f, here = top - ref;
+            if (__any_sync(0xffffffffu, here + of.most > above + kMoveAt)) {
+                float top_w = here + of.least;
+                if (of.far) {                                // with every row's own scale: what other queries see does not count
                     top_w = -CUDART_INF_F;
 #pragma unroll 1
                     for (int c0 = 0; c0 < kKeys; c0 += 32) {
                         float x[32];
                         scores_of(c0, x);
 #pragma unroll
-                        for (int c = 0; c < 32; ++c) top_w = fmaxf(top_w, fmaf(x[c], scale, of.exponent[c0 + c]));
+                        for (int c = 0; c < 32; ++c) top_w = fmaxf(top_w, __fadd_rn(__fmul_rn(x[c], scale), -ref) + of.exponent[c0 + c]);
                     }
                 }
-                const bool move = top_w > m_w + kMoveScaledAt;
+                const bool move = top_w > above + kMoveScaledAt;
                 if (i > 0 && __any_sync(0xffffffffu, move)) {
                     // (the step before may still be adding; the one before that was complete before this S was)
                     if (!guard.wait_all(o_step(w), (i - 1) & 1)) return false;
                     tc_fence_after();
-                    const float f = move ? ex2_approx(m_w - top_w) : 1.f;
+                    const float f = move ? ex2_approx(above - top_w) : 1.f;
 #pragma unroll 1
                     for (int c = 0; c < D; c += 32) {
                         float o[32];
@@ -443,12 +448,12 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                         tmem_st_cols<32>(o_col + c, y);
                     }
                 }
-                if (move) m_w = top_w;
+                if (move) above = top_w;
             }
             // The weights as they meet the values are those that have the sum, in other units, as long as a tile's values have one scale (2^64 above the scores' reference nothing is left of the
             // tile's values, and the units may be smaller).
-            const float ref = m == -CUDART_INF_F ? 0.f : far ? m : fminf(m_w - of.most, m + 64.f);
-            const uint64_t ref2 = two_f32(kF16Lift - ref, kF16Lift - ref);
+            const float off = far || !some ? 0.f : fminf(above - of.most, 64.f);
+            const uint64_t ref2 = two_f32(kF16Lift - (ref + off), kF16Lift - (ref + off));
             uint64_t sums[2] = {0, 0};
             if (!far) {
 #pragma unroll
@@ -468,8 +473,8 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                     tmem_st_cols<16>(s_col + c0 / 2, weights);
                 }
             } else {
-                const float to_w = m == -CUDART_INF_F ? 0.f : kF16Lift - m_w;
-                const uint64_t to_w2 = two_f32(to_w, to_w);
+                const float to_w = some ? kF16Lift - above : 0.f;
+                const uint64_t to_w2 = two_f32(to_w, to_w), to_sum2 = two_f32(kF16Lift, kF16Lift);
 #pragma unroll 1
                 for (int c0 = 0; c0 < kKeys; c0 += 32) {
                     float x[32];
@@ -477,12 +482,13 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                     scores_of(c0, x);
 #pragma unroll
                     for (int c = 0; c < 32; c += 2) {
-                        const float2 e = *reinterpret_cast<const float2*>(of.exponent + c0 + c);
-                        const uint64_t x2 = two_f32(x[c], x[c + 1]);
+                        const float2 e = of.far ? *reinterpret_cast<const float2*>(of.exponent + c0 + c) : make_float2(of.most, of.most);
+                        // (the largest score's, however large, is nothing: rounded as its reference.  Pairs of a product and a sum become one instruction, rounded once)
+                        const uint64_t from_ref = two_f32(__fadd_rn(__fmul_rn(x[c], scale), -ref), __fadd_rn(__fmul_rn(x[c + 1], scale), -ref));
                         float y, z;
-                        split_f32(fma_f32x2(x2, scale2, ref2), y, z);
+                        split_f32(add_f32x2(from_ref, to_sum2), y, z);
                         sums[0] = add_f32x2(sums[0], two_f32(ex2_approx(y), ex2_approx(z)));
-                        split_f32(add_f32x2(fma_f32x2(x2, scale2, two_f32(e.x, e.y)), to_w2), y, z);
+                        split_f32(add_f32x2(from_ref, add_f32x2(two_f32(e.x, e.y), to_w2)), y, z);
                         weights[c / 2] = two_f16(ex2_approx(y), ex2_approx(z));
                     }
                     tmem_st_cols<16>(s_col + c0 / 2, weights);
@@ -490,7 +496,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             }
             float even, odd;
             split_f32(add_f32x2(sums[0], sums[1]), even, odd);
-            l = fmaf(even + odd, m == -CUDART_INF_F ? 1.f : ex2_approx(ref - m), l);
+            l = fmaf(even + odd, ex2_approx(off), l);
             tmem_st_wait();
             tc_fence_before();
             mbar_arrive(p_full(w, buf));
@@ -503,7 +509,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         const int64_t part = s.part0 + static_cast<int64_t>(part_of_seq) * s.n_q + i_row;
         float4* const sums = reinterpret_cast<float4*>(raw + (q_at - smem_u32(raw)));         // of a cluster's CTA (sums_at)
         // (by halves: of values near 2^-117 the factor is no normal number)
-        const float half = l > 0.f ? exp2f(0.5f * (m_w - m)) : 0.f, by = half * (s.parts > 1 || ranks > 1 || !(l > 0.f) ? 1.f : 1.f / l);
+        const float half = l > 0.f ? exp2f(0.5f * above) : 0.f, by = half * (s.parts > 1 || ranks > 1 || !(l > 0.f) ? 1.f : 1.f / l);
         m -= kF16Lift;
         for (int c = 0; c < D && ok; c += 32) {
             float o[32];

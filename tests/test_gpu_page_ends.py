@@ -164,3 +164,23 @@ def test_values_of_all_sizes(shim, call, kind):
               lambda j: j * (200.0 / n) - 110, lambda j: j * 0.0 - 108, lambda j: j % 2 * 180.0 - 100, lambda j: j % 3 * 13.0 - 20):
         pool, table = sized_pool(gen, kind, G, d, n, 64, None, lambda x, j: x * torch.exp2(e(j.float()).clamp(-110, 110)))  # noqa: B023
         check(ctx, pool, kind, seqs, table, q, 64, fp16)
+
+
+@pytest.mark.parametrize("kind", [ROWS, E4M3, E2M1])
+@pytest.mark.parametrize("call", CALLS[2:])
+def test_large_scores(shim, call, kind):
+    """Scores from 2^10 to 2^120: where one row's decides, its values come out as they are; nothing leaves the numbers."""
+    H, G, d, n_q, n = call
+    gen = generator(n_q + 11 * d)
+    ctx = context(BF16, H, G, d)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    fp16, _ = form_of(shim, kind, *call)
+    q = torch.randn(n_q, H, d, generator=gen, device="cuda")
+    q[..., 0] = 8
+    for at in (5, 10, 17, 24, 30, 60, 110):
+        pool, table = sized_pool(gen, kind, G, d, n, 64, None, lambda x, j: x * torch.exp2(j % 3 * 20.0 - 40))
+        check(ctx, pool, kind, seqs, table, q.to(BF16), 64, fp16, scale=2.0 ** at)
+    # the scores of one row in 30 far above the others'
+    for at in (10, 17, 24, 60):
+        pool, table = sized_pool(gen, kind, G, d, n, 64, lambda x, j: torch.where((j % 30 == 11) & (torch.arange(d, device="cuda") == 0), 40.0 + j / 60, x), lambda x, j: x * torch.exp2(j % 5 * 2.0 - 4))
+        check(ctx, pool, kind, seqs, table, q.to(BF16), 64, fp16, scale=2.0 ** at)
