@@ -582,8 +582,8 @@ typedef struct mvla_paged_attention {
  * key head h / (n_heads / n_kv_heads).  out = softmax over the visible rows, times their values; scores, exponentials and sums in 32 bits.
  * For their product with the values weights are rounded.  Rows of the hidden type: as by mvla_window_attention for bf16 rows.  Quantised rows: to fp16 in
  * units of 2^-7 of the row's largest product of weight and scale (or less), 2^-11 of a weight at most; in bf16 contexts to bf16 where more than two blocks of 128
- * query rows go over a sequence (2^-8).  Codes are exact, but for scales that lie far apart: groups of 32 e2m1 elements below 2^-27 of
- * the largest scale in their row, and rows of keys below 2^-21 of the largest among the 64 that they are read with, count as nothing.
+ * query rows go over a sequence (2^-8).  Codes are exact, but groups of 32 e2m1 elements below 2^-27 of the largest scale
+ * in their row count as nothing.
  * A query that sees nothing: out 0, lse -infinity.  What is cached must be finite in rows that some query of the sequence sees; other rows, the
  * rest of the last page among them, may hold anything.  Rows of out and lse outside the sequences are left as they are; sequences must not share
  * query rows, and may share pages.  Batches of up to max_batch sequences (CAPACITY).  The workspace: as by mvla_window_attention.

@@ -5,10 +5,10 @@
 // a thread to a row in the softmax (warps 0-3), S double-buffered, one warp that issues the MMAs.  A warp copies codes and scales into a ring, what a tile has of
 // a page at a time; four warps turn them into fp16 and store them as the MMAs read them (128-byte swizzle).
 // Scales are powers of two.  A tile's largest scale of its keys becomes a factor of its scores and the largest one of its values a factor of its weights (both the same
-// for the whole tile); what a row, or 32 elements, have less is multiplied into the codes, which have as much room above in fp16 (2^7 for e4m3, 2^13 for e2m1): rows or
-// groups of keys below 2^-21 (2^-27) of their tile's largest scale count as nothing.  Values: the products of weights and scales that make up a row's output are of other sizes than its weights, so
-// that they have a reference of their own, in which O is counted.  Where the scales of a tile's values lie more than 2^kSpread apart, every row's is part of its weight (two exponentials to a key).
-// Queries are fp16 too, every row times a power of two that puts its largest element between 2^14 and 2^15.
+// for the whole tile); what a row, or 32 elements, have less is multiplied into the codes, which have as much room above in fp16 (2^7 for e4m3, 2^13 for e2m1) and keep their bits down to 2^-24.  Where
+// the scales of a tile lie further apart (kKeySpread, kSpread), codes are taken against their own row's largest scale (groups below 2^-27 of it count as nothing), which becomes a factor of that row's
+// scores, or part of its weights (two exponentials to a key): what other queries see takes no bits.  The products of weights and scales that make up a row's output are of other sizes than its
+// weights, so that they have a reference of their own, in which O is counted.  Queries are fp16 too, every row times a power of two that puts its largest element between 2^14 and 2^15.
 //
 // A CTA has one tile of query rows (two CTAs to a multiprocessor, heads of up to 128 elements; 96 registers, 40 bytes spill), or two that share what is unpacked (one CTA); the softmax reads S
 // twice, once for its maximum.  B200, 32 query heads over 8 heads of 128, e4m3: 5 tokens over 60000 rows 58 us, 4 chunks of 56 over 3100 to 5500 rows 46 (one tile of rows to a CTA: 51), of 33
@@ -48,15 +48,18 @@ struct PageTileShape {
     static constexpr int kPieces = 8 * D32 / kDecoders;      // of eight elements, of a decoding thread, in a tile of keys or of values
     static_assert(kStages >= 3 && kSlot % 16 == 0, "shape");
 };
-// Of a tile, for the softmax: of every row of values the exponent of its scale, the largest and the least of them, and whether they are far apart; the byte of the largest scale of its keys.
+// Of a tile, for the softmax: of every row of values the exponent of its scale, the largest and the least of them; of every row of keys that exponent, and the largest; which of the two are far apart.
+constexpr int kFarValues = 1, kFarKeys = 2;
 struct __align__(16) TileScales {
     float exponent[kKeys];
+    int key[kKeys];
     float most, least;
-    int far, keys;
+    int most_key, far;
 };
 // The reference of weights times scales is the largest one, or (where a tile's are not far apart) at most 2^kSpread below; against the tile's largest scale no weight is more than 2^kMoveAt
 // above the reference, and with its own, which counts where they are far apart, none either: 2^(kMoveAt + kF16Lift) is a number of fp16.
 constexpr int kSpread = 6;
+template <int KIND> constexpr int kKeySpread = KIND == MVLA_PAGE_E4M3 ? 21 : 9;
 constexpr float kMoveScaledAt = kMoveAt - kSpread;
 constexpr float kLargeScore = 1024.f;        // beyond, scores and exponents of scales are not added up in one number (2^-13 of a weight is lost so), nor scores scaled and taken from their reference in one step
 constexpr int kTileScales = 4;               // tiles whose scales are kept
@@ -77,6 +80,63 @@ __device__ __forceinline__ uint32_t power_f16(int e) { return e > -15 ? static_c
 __device__ __forceinline__ void store16(uint32_t at, const uint32_t (&w)[4])
 {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]) : "memory");
+}
+// What few tiles need, out of the way of the others (inside the loop over tiles it costs every one of them: 5 of 48 us).  Of this thread's row of S at `s_col`; `sees`: a bit to every key.
+__device__ __forceinline__ void load_scores(uint32_t s_col, uint32_t sees, float (&x)[32])
+{
+    tmem_ld_cols<32>(s_col, x);
+#pragma unroll
+    for (int c = 0; c < 32; ++c) x[c] = sees >> c & 1u ? x[c] : -CUDART_INF_F;
+}
+// fraction 2^(key - lifted), a normal number, whatever the sizes: zero times the -infinity of a row that is not seen is no number; scores that small are as good as zero, and larger ones are beyond 32 bits.
+__device__ __forceinline__ float score_scale(float fraction, int key, int lifted) { return fraction * two_to(min(max(key - lifted, -126), 127)); }
+// Every key's own scale: the scores as they are, in place.
+__device__ __noinline__ void scale_scores(uint32_t s_col, const int* key, float fraction, int lifted)
+{
+#pragma unroll 1
+    for (int c0 = 0; c0 < kKeys; c0 += 32) {
+        float x[32];
+        uint32_t y[32];
+        tmem_ld_cols<32>(s_col + c0, x);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) y[c] = __float_as_uint(x[c] * score_scale(fraction, key[c0 + c], lifted));
+        tmem_st_cols<32>(s_col + c0, y);
+    }
+    tmem_st_wait();
+}
+// The largest weight times scale, from the scores' reference on: what other queries see does not count.
+__device__ __noinline__ float top_product(uint32_t s_col, uint32_t sees0, uint32_t sees1, const float* exponent, float scale, float ref)
+{
+    float top = -CUDART_INF_F;
+#pragma unroll 1
+    for (int c0 = 0; c0 < kKeys; c0 += 32) {
+        float x[32];
+        load_scores(s_col + c0, c0 ? sees1 : sees0, x);
+#pragma unroll
+        for (int c = 0; c < 32; ++c) top = fmaxf(top, __fadd_rn(__fmul_rn(x[c], scale), -ref) + exponent[c0 + c]);
+    }
+    return top;
+}
+// The weights with their rows' scales (`exponent`, null: `most`), against `above` the scores' reference, in fp16 in the columns of S; returns the sum of those without.  (The largest score's distance from its
+// reference, however large they are, is nothing: rounded as that was.)
+__device__ __noinline__ float weigh_far(uint32_t s_col, uint32_t sees0, uint32_t sees1, const float* exponent, float most, float scale, float ref, float above)
+{
+    float sum = 0.f;
+#pragma unroll 1
+    for (int c0 = 0; c0 < kKeys; c0 += 32) {
+        float x[32];
+        uint32_t weights[16];
+        load_scores(s_col + c0, c0 ? sees1 : sees0, x);
+#pragma unroll
+        for (int c = 0; c < 32; c += 2) {
+            const float2 e = exponent ? *reinterpret_cast<const float2*>(exponent + c0 + c) : make_float2(most, most);
+            const float y = __fadd_rn(__fmul_rn(x[c], scale), -ref), z = __fadd_rn(__fmul_rn(x[c + 1], scale), -ref);
+            sum += ex2_approx(y + kF16Lift) + ex2_approx(z + kF16Lift);
+            weights[c / 2] = two_f16(ex2_approx(y + (e.x - above + kF16Lift)), ex2_approx(z + (e.y - above + kF16Lift)));
+        }
+        tmem_st_cols<16>(s_col + c0 / 2, weights);
+    }
+    return sum;
 }
 // Where eight elements of a row lie in a tile of such rows, in boxes of 64 elements of `rows` rows.
 __device__ __forceinline__ uint32_t swizzled(int row, int piece, int rows) { return piece / 8 * rows * 128 + row * 128 + ((piece & 7) ^ (row & 7)) * 16; }
@@ -254,9 +314,9 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             meet();                                          // (and nobody is with the last tile's factors any more)
             const int refs_here[2] = {static_cast<int>(max(warp_top[0].x, warp_top[1].x)), static_cast<int>(max(warp_top[2].x, warp_top[3].x))};
             const int least = static_cast<int>(min(warp_top[2].y, warp_top[3].y));
-            const bool far = refs_here[1] - least > kSpread;
+            const int far = (refs_here[1] - least > kSpread ? kFarValues : 0) | (refs_here[0] - static_cast<int>(min(warp_top[0].y, warp_top[1].y)) > kKeySpread<KIND> ? kFarKeys : 0);
             if (dt < 128) {
-                const int ref = side == 1 && far ? static_cast<int>(own) : refs_here[side];
+                const int ref = far & (side == 1 ? kFarValues : kFarKeys) ? static_cast<int>(own) : refs_here[side];
 #pragma unroll
                 for (int g = 0; g < G; ++g) factors[side][own_row][g] = power_f16(static_cast<int>(scale[g]) - ref + kCodeLift) * 0x10001u;
             }
@@ -264,12 +324,13 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             if (ok && dt < 128) {
                 TileScales& to = scales[i % kTileScales];
                 if (dt == 0) {
-                    to.keys = refs_here[0];
+                    to.most_key = refs_here[0] - 127;
                     to.most = static_cast<float>(refs_here[1] - 127 - kCodeLift);
                     to.least = static_cast<float>(least - 127 - kCodeLift);
                     to.far = far;
                 }
                 if (side == 1) to.exponent[own_row] = static_cast<float>(static_cast<int>(own) - 127 - kCodeLift);
+                else to.key[own_row] = static_cast<int>(own) - 127;
             }
             meet();
             if (ok) decode(2 * i, masked, j0, there);
@@ -334,7 +395,9 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
         const int w = warp >> 2, r = t & (kRows - 1), i_row = q0 + w * per + r / a.pack, head = head0 + r % a.pack;
         const bool mine = r < per * a.pack && i_row < s.n_q;
         const int p = mine ? query_pos(a, s, len, i_row) : -1;
-        float q_scale = a.scale_log2 * two_to(-kCodeLift);   // of the scores, less the tile's
+        // of a score: fraction 2^(key - lifted) for the exponent of its key's scale
+        const float fraction = __uint_as_float((__float_as_uint(a.scale_log2) & 0x7FFFFFu) | 0x3F800000u);
+        int lifted = kCodeLift - (static_cast<int>(__float_as_uint(a.scale_log2) >> 23) - 127);
         if (n > 0) {                                         // this row's queries, in fp16
             const __nv_bfloat16* const q = static_cast<const __nv_bfloat16*>(a.q) + ((s.q_row + i_row) * a.n_heads + head) * D;
             uint32_t top = 0;
@@ -349,7 +412,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             top = max(top & 0xFFFFu, top >> 16);
             const int e = top ? min(max(14 - (static_cast<int>(top >> 7) - 127), -113), 126) : 0;      // (2^126 times the smallest ones at most)
             const float lift = two_to(e);
-            q_scale *= two_to(-e);
+            lifted += e;
 #pragma unroll 4
             for (int c = 0; c < D; c += 8) {
                 uint4 y = make_uint4(0, 0, 0, 0);
@@ -383,16 +446,19 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
             const int buf = i & 1;
             tc_fence_after();
             const TileScales& of = scales[i % kTileScales];
-            // (not zero, whatever the sizes: zero times the -infinity of a row that is not seen is no number; scores that small are as good as zero)
-            const float scale = fmaxf(q_scale * two_to(of.keys - 127), FLT_MIN);
-            const uint64_t scale2 = two_f32(scale, scale);
             const uint32_t s_col = tmem + w * Sh::kOf + buf * kKeys + lanes;
+            float scale = score_scale(fraction, of.most_key, lifted);
+            if (of.far & kFarKeys) {
+                scale_scores(s_col, of.key, fraction, lifted);
+                scale = 1.f;
+            }
+            const uint32_t sees0 = masked ? visible[0] : 0xFFFFFFFFu, sees1 = masked ? visible[1] : 0xFFFFFFFFu;
+            const uint64_t scale2 = two_f32(scale, scale);
             const auto scores_of = [&](int c0, float (&x)[32]) {
                 tmem_ld_cols<32>(s_col + c0, x);
                 if (masked) {
-                    const uint32_t sees = c0 ? visible[1] : visible[0];
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) x[c] = sees >> c & 1u ? x[c] : -CUDART_INF_F;
+                    for (int c = 0; c < 32; ++c) x[c] = visible[c0 / 32] >> c & 1u ? x[c] : -CUDART_INF_F;
                 }
             };
             float tops[4];
@@ -418,20 +484,10 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                 above -= up;
                 m = top;
             }
-            const bool some = m > -CUDART_INF_F, far = of.far != 0 || __any_sync(0xffffffffu, some && fabsf(m) > kLargeScore);
+            const bool some = m > -CUDART_INF_F, far = (of.far & kFarValues) != 0 || __any_sync(0xffffffffu, some && fabsf(m) > kLargeScore);
             const float ref = some ? m : 0.f, here = top - ref;
             if (__any_sync(0xffffffffu, here + of.most > above + kMoveAt)) {
-                float top_w = here + of.least;
-                if (of.far) {                                // with every row's own scale: what other queries see does not count
-                    top_w = -CUDART_INF_F;
-#pragma unroll 1
-                    for (int c0 = 0; c0 < kKeys; c0 += 32) {
-                        float x[32];
-                        scores_of(c0, x);
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) top_w = fmaxf(top_w, __fadd_rn(__fmul_rn(x[c], scale), -ref) + of.exponent[c0 + c]);
-                    }
-                }
+                const float top_w = of.far & kFarValues ? top_product(s_col, sees0, sees1, of.exponent, scale, ref) : here + of.least;
                 const bool move = top_w > above + kMoveScaledAt;
                 if (i > 0 && __any_sync(0xffffffffu, move)) {
                     // (the step before may still be adding; the one before that was complete before this S was)
@@ -473,26 +529,7 @@ page_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ Page
                     tmem_st_cols<16>(s_col + c0 / 2, weights);
                 }
             } else {
-                const float to_w = some ? kF16Lift - above : 0.f;
-                const uint64_t to_w2 = two_f32(to_w, to_w), to_sum2 = two_f32(kF16Lift, kF16Lift);
-#pragma unroll 1
-                for (int c0 = 0; c0 < kKeys; c0 += 32) {
-                    float x[32];
-                    uint32_t weights[16];
-                    scores_of(c0, x);
-#pragma unroll
-                    for (int c = 0; c < 32; c += 2) {
-                        const float2 e = of.far ? *reinterpret_cast<const float2*>(of.exponent + c0 + c) : make_float2(of.most, of.most);
-                        // (the largest score's, however large, is nothing: rounded as its reference.  Pairs of a product and a sum become one instruction, rounded once)
-                        const uint64_t from_ref = two_f32(__fadd_rn(__fmul_rn(x[c], scale), -ref), __fadd_rn(__fmul_rn(x[c + 1], scale), -ref));
-                        float y, z;
-                        split_f32(add_f32x2(from_ref, to_sum2), y, z);
-                        sums[0] = add_f32x2(sums[0], two_f32(ex2_approx(y), ex2_approx(z)));
-                        split_f32(add_f32x2(from_ref, add_f32x2(two_f32(e.x, e.y), to_w2)), y, z);
-                        weights[c / 2] = two_f16(ex2_approx(y), ex2_approx(z));
-                    }
-                    tmem_st_cols<16>(s_col + c0 / 2, weights);
-                }
+                sums[0] = two_f32(weigh_far(s_col, sees0, sees1, of.far & kFarValues ? of.exponent : nullptr, of.most, scale, ref, some ? above : 0.f), 0.f);
             }
             float even, odd;
             split_f32(add_f32x2(sums[0], sums[1]), even, odd);

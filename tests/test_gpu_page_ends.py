@@ -184,3 +184,42 @@ def test_large_scores(shim, call, kind):
     for at in (10, 17, 24, 60):
         pool, table = sized_pool(gen, kind, G, d, n, 64, lambda x, j: torch.where((j % 30 == 11) & (torch.arange(d, device="cuda") == 0), 40.0 + j / 60, x), lambda x, j: x * torch.exp2(j % 5 * 2.0 - 4))
         check(ctx, pool, kind, seqs, table, q.to(BF16), 64, fp16, scale=2.0 ** at)
+
+
+@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("call", CALLS[2:])
+def test_keys_of_all_sizes(shim, call, kind):
+    """Keys that grow from row to row, those of rows that are not seen yet among them, with queries and a scale that fit the first ones, the last ones or those between; one in 40 rows larger, orthogonal
+    to the queries.  (No score leaves 32 bits.)"""
+    H, G, d, n_q, n = call
+    gen = generator(n_q + 7 * d)
+    ctx = context(BF16, H, G, d)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    fp16, _ = form_of(shim, kind, *call)
+    q = torch.randn(n_q, H, d, generator=gen, device="cuda").to(BF16)
+    q[..., 0] = 0
+    new = n - n_q                                              # the first query's row
+    for e, at in ((lambda j: (j - new).clamp(min=0) * (110.0 / max(n_q, 8)) - 100, 100.0), (lambda j: (j - new).clamp(min=0) * 1.5 - 20, 20.0), (lambda j: (n - j) * (200.0 / n) - 110, 0.0),
+                  (lambda j: j * (110.0 / n) - 100, 100.0), (lambda j: j * 0.0 - 108, 108.0), (lambda j: j % 3 * 13.0 - 20, 20.0), (lambda j: j * 0.0 + 100, -100.0)):
+        pool, table = sized_pool(gen, kind, G, d, n, 64, lambda x, j: x * torch.exp2(e(j.float()).clamp(-110, min(110, 105 - at))))  # noqa: B023
+        check(ctx, pool, kind, seqs, table, q, 64, fp16, scale=0.3 * 2.0 ** at)
+    for size in (2.0 ** 22, 2.0 ** 40, 2.0 ** 100):
+        along = lambda x, j: torch.where(j % 40 == 7, (torch.arange(d, device="cuda") == 0) * size, x)  # noqa: B023, E731
+        pool, table = sized_pool(gen, kind, G, d, n, 64, along)
+        check(ctx, pool, kind, seqs, table, q, 64, fp16)
+
+
+@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("call", CALLS[2:])
+def test_queries_and_keys_of_unlike_sizes(shim, call, kind):
+    """Scores of ordinary size whose factors are at the ends of their types: queries, keys, and the scale."""
+    H, G, d, n_q, n = call
+    gen = generator(n_q + 13 * d)
+    ctx = context(BF16, H, G, d)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    fp16, _ = form_of(shim, kind, *call)
+    x = torch.randn(n_q, H, d, generator=gen, device="cuda")
+    for query, key, scale in ((-118, 115, 0), (-110, 122, -12), (112, -110, 0), (120, -105, -15), (-100, -20, 120), (60, 60, -121), (-125, 122, 3), (122, -108, -14)):
+        for spread in (0.0, 24.0):
+            pool, table = sized_pool(gen, kind, G, d, n, 64, lambda x, j: x * torch.exp2(key + (j % 7 == 2) * -spread))  # noqa: B023
+            check(ctx, pool, kind, seqs, table, (x * 2.0 ** query).to(BF16), 64, fp16, scale=0.3 * 2.0 ** scale)
