@@ -7,8 +7,8 @@
 // another's but for the scales, which all of them read.  16 rows of a tile never cross a page, so that a page number is looked up once for 16 keys, a tile before its copies begin.
 //   Quantised keys and values become fp16 in registers, which holds every code; values of two keys are interleaved before that, in their 8 or 4 bits,
 // which makes them the second product's operand.  Scales are powers of two.  One a row (e4m3): a key's multiplies its scores; a value's is added to
-// the exponent of its weight, w = 2^(x + e - reference).  So there are two references and two exponentials: those of the weights that meet the values, and those
-// of the sum that divides them.  One for 32 elements (e2m1): the row's largest is taken as above, the rest of it multiplies the codes (2^13 times
+// the exponent of its weight, w = 2^((x - reference) + (e - above)).  So there are two references and two exponentials: those of the weights that meet the values, `above` the other, and those
+// of the sum that divides them.  (Scores are taken from their reference first: beside a score of 2^17 the exponents of scales lose their last bits.)  One for 32 elements (e2m1): the row's largest is taken as above, the rest of it multiplies the codes (2^13 times
 // the quotient of the scales: 6 2^13 is a number of fp16, and a group 2^-27 of the largest one is nothing).  Queries are fp16 too, every row
 // times a power of two that puts its largest element between 2^14 and 2^15.  bf16 weights (unquantised pages) meet the values in two
 // parts, what the type holds and what it leaves; fp16 ones are one part, in units of 2^-kF16Lift of their reference.
@@ -21,11 +21,14 @@
 #include "attend_tile.cuh"
 #include "page.cuh"
 
+#include <cfloat>
+
 namespace mvla {
 namespace {
 
 constexpr int kWarps = 4;
 constexpr int kStages = kPageTokenStages;
+constexpr float kNothing = -FLT_MAX;         // reference of a row that has seen nothing yet
 
 template <int BYTES>
 __device__ __forceinline__ void copy_async(uint32_t dst, const void* src, int there)
@@ -169,12 +172,12 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
         for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int n = 0; n < NR; ++n) o[m][i][n][0] = o[m][i][n][1] = o[m][i][n][2] = o[m][i][n][3] = 0.f;
-    // references of the sum, and of the weights as they meet the values (the same where there are no scales)
-    float ref[NR][2], ref_w[NR][2], sum[NR][2];
+    // reference of the sum, what that of the weights as they meet the values lies above it (nothing where there are no scales), the sum
+    float ref[NR][2], above[NR][2], sum[NR][2];
 #pragma unroll
     for (int n = 0; n < NR; ++n)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) { ref[n][e] = ref_w[n][e] = -CUDART_INF_F; sum[n][e] = 0.f; }
+        for (int e = 0; e < 2; ++e) { ref[n][e] = kNothing; above[n][e] = sum[n][e] = 0.f; }
 
     // Tile t0 + warp + kWarps u is this warp's u-th.  Page of its keys 16 (lane / 16) ... (of the first sixteen, where a tile has no more):
     const int mine = t1 > t0 + warp ? (t1 - t0 - warp + kWarps - 1) / kWarps : 0;
@@ -392,7 +395,7 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
                 for (int k = 0; k < 2; ++k) {
                     const float by = __uint_as_float(kbyte[k] << 23) * (kE2m1 ? 0x1p-13f : 1.f);     // (without the codes' lift)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) x[v][n][2 * k + e] *= kScaled ? q_by[n][e] * by : q_by[n][e];
+                    for (int e = 0; e < 2; ++e) x[v][n][2 * k + e] = __fmul_rn(x[v][n][2 * k + e], kScaled ? q_by[n][e] * by : q_by[n][e]);      // (rounded before anything is taken from it)
                 }
         }
         uint32_t seen[U][2] = {};                            // four bits for every key g + 8 k: which lanes have a row that sees it
@@ -415,38 +418,44 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
                 }
         }
         // references
-        float top[NR][2], top_w[NR][2];
+        float top[NR][2];
         bool move = false;
+        const auto top_product = [&](int n, int e) {         // from the reference on
+            float w = fmaxf((x[0][n][e] - ref[n][e]) + of_value[0][0], (x[0][n][2 + e] - ref[n][e]) + of_value[0][1]);
+            if (U > 1) w = fmaxf(w, fmaxf((x[U - 1][n][e] - ref[n][e]) + of_value[U - 1][0], (x[U - 1][n][2 + e] - ref[n][e]) + of_value[U - 1][1]));
+            return w;
+        };
 #pragma unroll
         for (int n = 0; n < NR; ++n)
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
                 top[n][e] = fmaxf(x[0][n][e], x[0][n][2 + e]);
-                top_w[n][e] = fmaxf(x[0][n][e] + of_value[0][0], x[0][n][2 + e] + of_value[0][1]);
-                if (U > 1) {
-                    top[n][e] = fmaxf(top[n][e], fmaxf(x[U - 1][n][e], x[U - 1][n][2 + e]));
-                    top_w[n][e] = fmaxf(top_w[n][e], fmaxf(x[U - 1][n][e] + of_value[U - 1][0], x[U - 1][n][2 + e] + of_value[U - 1][1]));
-                }
-                move |= top[n][e] > ref[n][e] + 8.f;
-                if (kScaled) move |= top_w[n][e] > ref_w[n][e] + 8.f;
+                if (U > 1) top[n][e] = fmaxf(top[n][e], fmaxf(x[U - 1][n][e], x[U - 1][n][2 + e]));
+                move |= top[n][e] - ref[n][e] > 8.f;
+                if (kScaled) move |= top_product(n, e) > above[n][e] + 8.f;
             }
         if (__any_sync(0xffffffffu, move)) {
 #pragma unroll
             for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float m = top[n][e], w = top_w[n][e];
+                    float m = top[n][e];
 #pragma unroll
-                    for (int k = 4; k < 32; k *= 2) {
-                        m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
-                        w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, k));
-                    }
+                    for (int k = 4; k < 32; k *= 2) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, k));
                     m = fmaxf(ref[n][e], m);
-                    w = kScaled ? fmaxf(ref_w[n][e], w) : m;
-                    sum[n][e] *= m == ref[n][e] ? 1.f : exp2f(ref[n][e] - m);
-                    const float f = w == ref_w[n][e] ? 1.f : exp2f(ref_w[n][e] - w);
+                    const float up = m - ref[n][e];
+                    float f = up == 0.f ? 1.f : exp2f(-up);
+                    sum[n][e] *= f;
                     ref[n][e] = m;
-                    ref_w[n][e] = w;
+                    if constexpr (kScaled) {
+                        float w = top_product(n, e);
+#pragma unroll
+                        for (int k = 4; k < 32; k *= 2) w = fmaxf(w, __shfl_xor_sync(0xffffffffu, w, k));
+                        const float old = above[n][e] - up;
+                        w = m == kNothing ? 0.f : fmaxf(old, w);
+                        f = w == old ? 1.f : exp2f(old - w);
+                        above[n][e] = w;
+                    }
 #pragma unroll
                     for (int mm = 0; mm < M64; ++mm)
 #pragma unroll
@@ -462,12 +471,11 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
                 float y[2][2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    const float b = ref[n][e] == -CUDART_INF_F ? 0.f : ref[n][e], b_w = ref_w[n][e] == -CUDART_INF_F ? 0.f : ref_w[n][e] - kLift;
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-                        const float z = ex2_approx(x[v][n][2 * k + e] - b);
+                        const float u = x[v][n][2 * k + e] - ref[n][e], z = ex2_approx(u);
                         sum[n][e] += z;
-                        y[k][e] = kScaled ? ex2_approx(x[v][n][2 * k + e] + of_value[v][k] - b_w) : z;
+                        y[k][e] = kScaled ? ex2_approx(u + (of_value[v][k] - (above[n][e] - kLift))) : z;
                     }
                 }
 #pragma unroll
@@ -560,8 +568,8 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
 #pragma unroll
             for (int w = 4; w < 32; w *= 2) sum[n][e] += __shfl_xor_sync(0xffffffffu, sum[n][e], w);
             if (g == 0) {
-                merge_m[warp][8 * n + 2 * c + e] = ref[n][e];
-                merge_f[warp][8 * n + 2 * c + e] = ref_w[n][e] - kLift;
+                merge_m[warp][8 * n + 2 * c + e] = ref[n][e] == kNothing ? -CUDART_INF_F : ref[n][e];
+                merge_f[warp][8 * n + 2 * c + e] = above[n][e] - kLift;
                 merge_l[warp][8 * n + 2 * c + e] = sum[n][e];
             }
         }
@@ -574,7 +582,7 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             l += merge_l[w][t] * exp2f(merge_m[w][t] - base);
-            merge_f[w][t] = exp2f(merge_f[w][t] - base);
+            merge_f[w][t] = exp2f(0.5f * ((merge_m[w][t] - base) + merge_f[w][t]));      // (by halves: of values near 2^-117 it is no normal number)
         }
         cta_ml[t] = make_float2(m, l);
     }
@@ -612,8 +620,9 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) {
             const float2 x2 = *reinterpret_cast<const float2*>(&merge_o[w][r][col]);
-            y = fmaf(x2.x, merge_f[w][r], y);
-            z = fmaf(x2.y, merge_f[w][r], z);
+            const float half = merge_f[w][r];
+            y = fmaf(x2.x * half, half, y);
+            z = fmaf(x2.y * half, half, z);
         }
         if (ranks == 1) give(r, col, y, z, cta_ml[r].x, cta_ml[r].y);
         else *reinterpret_cast<float2*>(&merge_o[0][r][col]) = make_float2(y, z);

@@ -167,7 +167,7 @@ def test_values_of_all_sizes(shim, call, kind):
 
 
 @pytest.mark.parametrize("kind", [ROWS, E4M3, E2M1])
-@pytest.mark.parametrize("call", CALLS[2:])
+@pytest.mark.parametrize("call", CALLS)
 def test_large_scores(shim, call, kind):
     """Scores from 2^10 to 2^120: where one row's decides, its values come out as they are; nothing leaves the numbers."""
     H, G, d, n_q, n = call
@@ -187,7 +187,7 @@ def test_large_scores(shim, call, kind):
 
 
 @pytest.mark.parametrize("kind", [E4M3, E2M1])
-@pytest.mark.parametrize("call", CALLS[2:])
+@pytest.mark.parametrize("call", CALLS)
 def test_keys_of_all_sizes(shim, call, kind):
     """Keys that grow from row to row, those of rows that are not seen yet among them, with queries and a scale that fit the first ones, the last ones or those between; one in 40 rows larger, orthogonal
     to the queries.  (No score leaves 32 bits.)"""
