@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
     __shared__ uint4 q_frag[D32][NR][32];
     __shared__ float merge_m[kWarps][16], merge_f[kWarps][16], merge_l[kWarps][16];
     __shared__ float2 cta_ml[16], peer_ml[kMaxCluster][8 * NR];
-    __shared__ float q_lift[16], q_scale[16];                // what a row's queries are multiplied by; what that makes of the scores' scale
+    __shared__ float q_lift[16], q_scale[16], q_half[16];    // what a row's queries are multiplied by; what that makes of the scores' scale, in two factors of about the same size
     __shared__ __align__(4) uint16_t factors[kE2m1 ? kWarps : 1][kE2m1 ? U : 1][2][kE2m1 ? D32 : 1][16];      // of the groups of a tile's rows, fp16
     pdl_wait();
     pdl_trigger();
@@ -255,8 +255,12 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
         top = __reduce_max_sync(0xffffffffu, max(top & 0xFFFFu, top >> 16));
         if (lane == 0) {
             const int e = kScaled && top ? max(14 - (static_cast<int>(top >> 7) - 127), -113) : 0;       // (2^126 times the smallest ones at most)
+            // (with their product, or with a key's scale in one step, the scale could leave the normal numbers though the scores do not)
+            const uint32_t bits = __float_as_uint(a.scale_log2);
+            const int power = static_cast<int>(bits >> 23) - 127 - min(e, 126), half = kScaled ? power >> 1 : 0;
             q_lift[r] = two_to(min(e, 126));
-            q_scale[r] = a.scale_log2 * two_to(-min(e, 126));
+            q_scale[r] = __uint_as_float((bits & 0x7FFFFFu) | 0x3F800000u) * two_to(power - half);
+            q_half[r] = two_to(half);
         }
     }
     __syncthreads();
@@ -274,9 +278,11 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
         q_frag[piece][n][l] = w;
     }
     __syncthreads();
-    float q_by[NR][2];
+    float q_by[NR][2], q_key[NR][2];
 #pragma unroll
-    for (int n = 0; n < NR; ++n) { q_by[n][0] = q_scale[8 * n + 2 * c]; q_by[n][1] = q_scale[8 * n + 2 * c + 1]; }
+    for (int n = 0; n < NR; ++n)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) { q_by[n][e] = q_scale[8 * n + 2 * c + e]; q_key[n][e] = q_half[8 * n + 2 * c + e]; }
 
     int stage = 0;
     for (int u = 0; u < mine; ++u, stage = stage + 1 < kStages ? stage + 1 : 0) {
@@ -393,9 +399,14 @@ __global__ void __launch_bounds__(kWarps * 32, page_token_ctas(KIND, D32, NR)) p
             for (int n = 0; n < NR; ++n)
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
-                    const float by = __uint_as_float(kbyte[k] << 23) * (kE2m1 ? 0x1p-13f : 1.f);     // (without the codes' lift)
+                    const float by = __uint_as_float(kbyte[k] ? kbyte[k] << 23 : 0x400000u) * (kE2m1 ? 0x1p-13f : 1.f);      // (without the codes' lift; the least byte is 2^-127)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) x[v][n][2 * k + e] = __fmul_rn(x[v][n][2 * k + e], kScaled ? q_by[n][e] * by : q_by[n][e]);      // (rounded before anything is taken from it)
+                    for (int e = 0; e < 2; ++e) {
+                        // (rounded before anything is taken from it; a score of nothing stays nothing)
+                        float& y = x[v][n][2 * k + e];
+                        y = __fmul_rn(y, q_by[n][e]);
+                        if (kScaled) y = __fmul_rn(y, fminf(by * q_key[n][e], FLT_MAX));
+                    }
                 }
         }
         uint32_t seen[U][2] = {};                            // four bits for every key g + 8 k: which lanes have a row that sees it

@@ -210,7 +210,7 @@ def test_keys_of_all_sizes(shim, call, kind):
 
 
 @pytest.mark.parametrize("kind", [E4M3, E2M1])
-@pytest.mark.parametrize("call", CALLS[2:])
+@pytest.mark.parametrize("call", CALLS)
 def test_queries_and_keys_of_unlike_sizes(shim, call, kind):
     """Scores of ordinary size whose factors are at the ends of their types: queries, keys, and the scale."""
     H, G, d, n_q, n = call
@@ -223,3 +223,25 @@ def test_queries_and_keys_of_unlike_sizes(shim, call, kind):
         for spread in (0.0, 24.0):
             pool, table = sized_pool(gen, kind, G, d, n, 64, lambda x, j: x * torch.exp2(key + (j % 7 == 2) * -spread))  # noqa: B023
             check(ctx, pool, kind, seqs, table, (x * 2.0 ** query).to(BF16), 64, fp16, scale=0.3 * 2.0 ** scale)
+
+
+@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("call", CALLS)
+def test_the_least_scale_bytes(shim, call, kind):
+    """Scales of 2^-127 to 2^-118, which rows are never given as they are written: what they stand for, in keys beside large queries, and in values."""
+    H, G, d, n_q, n = call
+    gen = generator(n_q + 17 * d)
+    ctx = context(BF16, H, G, d)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    fp16, _ = form_of(shim, kind, *call)
+    x = (torch.randn(n_q, H, d, generator=gen, device="cuda") * 2.0 ** 114).to(BF16)
+    for keys in (True, False):
+        pool, table = sized_pool(gen, kind, G, d, n, 64)
+        scale = pool.k_scale if keys else pool.v_scale
+        scale.copy_(torch.randint(0, 10, scale.shape, generator=gen, device="cuda"))
+        check(ctx, pool, kind, seqs, table, x if keys else x * 2.0 ** -114, 64, fp16)
+    for large in (0.0, 2.0 ** 126):                            # queries that meet zeros alone, beside the largest keys
+        pool, table = sized_pool(gen, kind, G, d, n, 64, lambda x, j: torch.where(torch.arange(d, device="cuda") < 32, x * 0, x * 2.0 ** 122))
+        q = torch.zeros(n_q, H, d, device="cuda")
+        q[..., 3] = large
+        check(ctx, pool, kind, seqs, table, q.to(BF16), 64, fp16)
