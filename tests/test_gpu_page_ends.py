@@ -72,7 +72,7 @@ def test_calls_take_every_form(shim):
     assert {form_of(shim, E4M3, *c)[1] for c in CALLS} == {(TOKEN, 0), (PAGE_TILE, 1), (PAGE_TILE, 2), (PAGE_TILE, 0)}
 
 
-@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("kind", [ROWS, E4M3, E2M1])
 @pytest.mark.parametrize("call", CALLS)
 def test_scales_of_all_sizes(shim, call, kind):
     """Scores that are as good as zero, or whose queries or keys are far from one: rows that a mask hides stay hidden."""
@@ -118,7 +118,7 @@ def test_tiles_of_nothing(shim, call, kind):
             check(ctx, pool, kind, seqs, table, (x * size).to(BF16), 64, fp16, window=window)
 
 
-def sized_pool(gen, kind, G, d, n, page_rows, k=None, v=None):
+def sized_pool(gen, kind, G, d, n, page_rows, k=None, v=None, wide=BF16):
     """(pool, table) of one sequence whose rows of keys and values [n, G, d] are random, times k and v."""
     table, n_pages = P.make_table(gen, [n], page_rows, spare=0)
     j = torch.arange(n, device="cuda")
@@ -127,11 +127,11 @@ def sized_pool(gen, kind, G, d, n, page_rows, k=None, v=None):
         x = torch.randn(n, G, d, generator=gen, device="cuda")
         rows = torch.zeros(n_pages, page_rows, G, d, device="cuda")
         rows[table[0].long()[j // page_rows], j % page_rows] = x if size is None else size(x, j[:, None, None])
-        out.append(P.quantise(rows.transpose(1, 2).contiguous().to(BF16), kind))
+        out.append(P.quantise(rows.transpose(1, 2).contiguous().to(wide), kind))
     return mvla.PagePool(out[0][1].contiguous(), out[1][1].contiguous(), out[0][2], out[1][2]), table
 
 
-@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("kind", [ROWS, E4M3, E2M1])
 @pytest.mark.parametrize("call", CALLS)
 def test_large_values_of_little_weight(shim, call, kind):
     """The first rows, or one in 40, have values 2^24 to 2^110 larger than the others and scores far below them, to nearly nothing or to nothing at all."""
@@ -149,7 +149,7 @@ def test_large_values_of_little_weight(shim, call, kind):
             check(ctx, pool, kind, seqs, table, q.to(BF16), 32, fp16)
 
 
-@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("kind", [ROWS, E4M3, E2M1])
 @pytest.mark.parametrize("call", CALLS)
 def test_values_of_all_sizes(shim, call, kind):
     """Values that grow and shrink from row to row, over the whole range of the scales, those of rows that are not seen yet among them; values near its lower end."""
@@ -186,7 +186,7 @@ def test_large_scores(shim, call, kind):
         check(ctx, pool, kind, seqs, table, q.to(BF16), 64, fp16, scale=2.0 ** at)
 
 
-@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("kind", [ROWS, E4M3, E2M1])
 @pytest.mark.parametrize("call", CALLS)
 def test_keys_of_all_sizes(shim, call, kind):
     """Keys that grow from row to row, those of rows that are not seen yet among them, with queries and a scale that fit the first ones, the last ones or those between; one in 40 rows larger, orthogonal
@@ -209,7 +209,7 @@ def test_keys_of_all_sizes(shim, call, kind):
         check(ctx, pool, kind, seqs, table, q, 64, fp16)
 
 
-@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("kind", [ROWS, E4M3, E2M1])
 @pytest.mark.parametrize("call", CALLS)
 def test_queries_and_keys_of_unlike_sizes(shim, call, kind):
     """Scores of ordinary size whose factors are at the ends of their types: queries, keys, and the scale."""
@@ -245,3 +245,26 @@ def test_the_least_scale_bytes(shim, call, kind):
         q = torch.zeros(n_q, H, d, device="cuda")
         q[..., 3] = large
         check(ctx, pool, kind, seqs, table, q.to(BF16), 64, fp16)
+
+
+@pytest.mark.parametrize("kind", [ROWS, E4M3, E2M1])
+@pytest.mark.parametrize("H,G,d,n_q,n", [(8, 4, 64, 1, 300), (4, 2, 128, 37, 300), (2, 2, 256, 90, 500)])
+def test_ends_of_fp32_contexts(H, G, d, n_q, n, kind):
+    """The same of fp32 rows, and of quantised ones beside fp32 queries: small and large scales, scores, keys and values; a tile on pages outside the pool."""
+    gen = generator(n_q + 19 * d)
+    ctx = context(FP32, H, G, d)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    q = torch.randn(n_q, H, d, generator=gen, device="cuda")
+    make = lambda k, v: sized_pool(gen, kind, G, d, n, 64, k, v, FP32)  # noqa: E731
+    pool, table = make(None, None)
+    for size, scale in ((1.0, 1e-36), (1.0, 9e-39), (2.0 ** -125, 0.0), (2.0 ** -60, 2.0 ** -70), (1.0, 2.0 ** 12), (1.0, 2.0 ** 24), (1.0, 2.0 ** 40), (1.0, 2.0 ** 100)):
+        check(ctx, pool, kind, seqs, table, q * size, 64, False, scale=scale)
+    table[0, n // 64] = -1
+    check(ctx, pool, kind, seqs, table, q * 2.0 ** -40, 64, False)
+    for v in (lambda x, j: torch.where(j < 64, x * 2.0 ** 60, x), lambda x, j: x * torch.exp2((j - (n - n_q)).clamp(min=0) * (160.0 / max(n_q, 8)) - 80), lambda x, j: x * 2.0 ** -108):
+        pool, table = make(lambda x, j: torch.where((j < 64) & (torch.arange(d, device="cuda") == 0), -2000.0, x), v)
+        q[..., 0] = 8
+        check(ctx, pool, kind, seqs, table, q, 64, False)
+    for query, key in ((-110, 110), (110, -110)):
+        pool, table = make(lambda x, j: x * 2.0 ** key, None)  # noqa: B023
+        check(ctx, pool, kind, seqs, table, q * 2.0 ** query, 64, False)
