@@ -720,7 +720,7 @@ PyObject* py_page_rows(PyObject*, PyObject* const* a, Py_ssize_t n)
         if (!expect(!write, "k or v is needed")) return nullptr;
         int64_t end = 0;
         for (int i = 0; i < s.n; ++i)
-            if (s.ptr[i].n_q > 0 && s.ptr[i].q_row >= 0 && s.ptr[i].q_row <= 0x7FFFFFFF) end = std::max<int64_t>(end, s.ptr[i].q_row + s.ptr[i].n_q);
+            if (s.ptr[i].n_q >= 0 && s.ptr[i].q_row >= 0 && s.ptr[i].q_row <= 0x7FFFFFFF) end = std::max<int64_t>(end, s.ptr[i].q_row + s.ptr[i].n_q);
         for (Held& h : rows) {
             h.take(THPVariable_Wrap(fresh_on({end, c.kv_heads, c.dim}, c.wide, c.device, a[16], st)));
             if (!h.o) return nullptr;

@@ -268,3 +268,15 @@ def test_ends_of_fp32_contexts(H, G, d, n_q, n, kind):
     for query, key in ((-110, 110), (110, -110)):
         pool, table = make(lambda x, j: x * 2.0 ** key, None)  # noqa: B023
         check(ctx, pool, kind, seqs, table, q * 2.0 ** query, 64, False)
+
+
+def test_idle_sequences_do_not_refuse_a_read():
+    """Rows read without outputs: a sequence without rows of its own may stand anywhere behind the others'."""
+    gen = generator(23)
+    ctx = context()
+    table, n_pages = P.make_table(gen, [40, 30], 16)
+    pool = P.make_pool(gen, n_pages, 4, 16, 64, E4M3, BF16)
+    k, v = ctx.page_read(pool, [mvla.Seq(q_row=0, n_q=40, n_kv=40), mvla.Seq(q_row=45, n_q=0, n_kv=30)], table)
+    assert k.shape[0] == v.shape[0] == 45
+    for got, want in zip((k, v), P.rows_of(pool, E4M3, table, 0, 40, 16)):
+        assert same(got[:40].double(), want)
