@@ -394,7 +394,7 @@ attend_tile_kernel(const __grid_constant__ AttArgs a, const __grid_constant__ CU
             if (move) m = top;
             const float ref = m == -CUDART_INF_F ? 0.f : m - kLift;
             uint64_t by2 = scale2, ref2 = two_f32(-ref, -ref);
-            if (PAGED && __any_sync(0xffffffffu, fabsf(ref) > kLargeScore)) {        // (the largest score's distance from its reference is nothing, however large: rounded as that was)
+            if (PAGED && fabsf(ref) > kLargeScore) {         // (the largest score's distance from its reference is nothing, however large: rounded as that was.  A row by itself: some are nobody's)
 #pragma unroll
                 for (int c = 0; c < kKeys; ++c) x[c] = __fadd_rn(__fmul_rn(x[c], scale), -ref);
                 by2 = two_f32(1.f, 1.f);

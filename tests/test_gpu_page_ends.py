@@ -280,3 +280,26 @@ def test_idle_sequences_do_not_refuse_a_read():
     assert k.shape[0] == v.shape[0] == 45
     for got, want in zip((k, v), P.rows_of(pool, E4M3, table, 0, 40, 16)):
         assert same(got[:40].double(), want)
+
+
+@pytest.mark.parametrize("kind,H,G,d,sizes", [(ROWS, 28, 4, 128, ((100, 66), (187, 365))), (E2M1, 24, 8, 192, ((4, 52), (168, 555), (183, 669), (78, 369))), (E4M3, 24, 8, 256, ((81, 651),)),
+                                              (E4M3, 12, 4, 64, ((30, 3000), (9, 100)))])
+def test_the_same_bits_every_time(kind, H, G, d, sizes):
+    """Groups of heads that do not fill a tile of 128 rows: what lies in the rows that are left over, from whatever ran before, changes no bit."""
+    gen = generator(29)
+    ctx = context(BF16, H, G, d)
+    table, n_pages = P.make_table(gen, [n for _, n in sizes], 64)
+    pool = P.make_pool(gen, n_pages, G, 64, d, kind, BF16)
+    seqs, at = [], 0
+    for n_q, n in sizes:
+        seqs.append(mvla.Seq(q_row=at, n_q=n_q, n_kv=n))
+        at += n_q
+    q = torch.randn(at, H, d, generator=gen, device="cuda").to(BF16)
+    noise = (torch.randn(at, H, d, generator=gen, device="cuda") * 1e30).to(BF16)
+    want = None
+    for _ in range(30):
+        lse = torch.empty(at, H, device="cuda")
+        out = ctx.page_attention(pool, seqs, table, q, lse=lse, n_sink=1, scale=2.0)
+        want = want or (out, lse)
+        assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
+        ctx.page_attention(pool, seqs, table, noise)
