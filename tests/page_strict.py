@@ -17,7 +17,8 @@ def reference(pool, kind, s, table, b, q, page_rows, fp16, window=None, n_sink=0
     exponents of scales, 2^-24 of 1024 and 256 at most, from which a tile's weights are taken; 2^-20 for the powers of two, 2 keys 2^-24 for sums and rescalings, half a step of the type in
     which the weight meets the values.  fp16: a weight times scale is counted in units of 2^-7 of the largest such product so far (2^-8 of which may be the reference): where no
     normal number is left it is off by 2^-25 2^-7 of the largest product, times a code, whose row's largest is half of the largest code at least: 2^-31 of the
-    largest weight times largest element; below 2^-126 of the largest a weight is nothing in 32 bits.  e2m1 values below 2^-27 of their row's largest scale: as above.  Then the rounding of the result."""
+    largest weight times largest element; a weight below 2^-126 of its reference is
+    nothing in 32 bits, and what was summed up is, where the reference rises by as much: at most 2^8 (a reference may lie so far below a weight) times 2^-126 of a value.  e2m1 values below 2^-27 of their row's largest scale: as above.  Then the rounding of the result."""
     H, d = q.shape[1], q.shape[2]
     n = s.n_kv if n is None else n
     k, v = P.rows_of(pool, kind, table, b, n, page_rows)
@@ -65,7 +66,7 @@ def reference(pool, kind, s, table, b, q, page_rows, fp16, window=None, n_sink=0
         own = own + keys * 2.0 ** -31 * (product.amax(-1) if n else w.sum(-1)).T[..., None]
         if kind == E2M1:
             own = own + torch.einsum("hij,jhd->ihd", w, torch.minimum(v.abs(), 2.0 ** -27 * v_top.T[..., None]))
-    own = own + 2.0 ** -126 * torch.einsum("ij,jhd->ihd", sees.double(), v.abs())
+    own = own + 2.0 ** -118 * torch.einsum("ij,jhd->ihd", sees.double(), v.abs())
     half = U.HALF[q.dtype]
     return {"out": out, "tol": own + half * (out.abs() + own) + 2.0 ** -134, "lse": lse.T, "rows": some,
             "lse_tol": below[..., 0] + 2.0 ** -18 + 2.0 ** -22 * torch.where(some[:, None], lse.T.abs(), 0.0)}
