@@ -36,7 +36,7 @@ MVLA_BOTH constexpr RowSlot row_slot(int thread, int column, int lanes, int kv_h
         u = first < step ? thread - first * slots : slots;
     }
     const bool on = u < slots;
-    const int h = on ? u / lanes : 0;                        // (the surplus threads copy nothing; what they form addresses of is there all the same)
+    const int h = on ? u / lanes : 0;                        // (the surplus threads copy nothing; what they form addresses of, and the scales that they read, are there all the same)
     return {!keys || h >= kv_heads, on, keys && h >= kv_heads ? h - kv_heads : h, u % lanes, first, step};
 }
 

@@ -302,7 +302,7 @@ __global__ void __launch_bounds__(kThreads, kCtas<T>) page_read_kernel(const __g
                     } else {
                         w[u][i] = Codes{};
                         if (there) w[u][i] = *reinterpret_cast<const Codes*>(src + piece * (KIND == MVLA_PAGE_E4M3 ? 8 : 4));
-                        if (i < kBytes && from >= 0 && s.on) byte[u][i] = scales[at[r].scale + (KIND == MVLA_PAGE_E4M3 || !on[i] ? 0 : piece / (kPageGroup / 8))];
+                        if (i < kBytes && from >= 0) byte[u][i] = scales[at[r].scale + (KIND == MVLA_PAGE_E4M3 || !on[i] ? 0 : piece / (kPageGroup / 8))];
                     }
                 }
             }
