@@ -581,8 +581,8 @@ typedef struct mvla_paged_attention {
  * Positions are counted: query i has position p = n - n_q + i and sees row j where j <= p and (p - j < window or j < n_sink); query head h reads
  * key head h / (n_heads / n_kv_heads).  out = softmax over the visible rows, times their values; scores, exponentials and sums in 32 bits.
  * For their product with the values weights are rounded.  Rows of the hidden type: as by mvla_window_attention for bf16 rows.  Quantised rows: to fp16 in
- * units of 2^-7 of the row's largest product of weight and scale (or less), 2^-11 of a weight at most; in bf16 contexts to bf16 where more than two blocks of 128
- * query rows go over a sequence (2^-8).  Codes are exact, but groups of 32 e2m1 elements below 2^-27 of the largest scale
+ * units of 2^-7 of the row's largest product of weight and scale (or less), 2^-11 of a weight at most; in bf16 contexts to bf16 (2^-8) where
+ * some sequence of the call has more than one block of 128 query rows (two, where the sequences are long).  Codes are exact, but groups of 32 e2m1 elements below 2^-27 of the largest scale
  * in their row count as nothing.
  * A query that sees nothing: out 0, lse -infinity.  What is cached must be finite in rows that some query of the sequence sees; other rows, the
  * rest of the last page among them, may hold anything.  Rows of out and lse outside the sequences are left as they are; sequences must not share

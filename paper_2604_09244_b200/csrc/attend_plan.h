@@ -82,7 +82,7 @@ struct AttendPlan {
     int64_t part_o = -1, part_ml = -1, lse2 = -1, part_mass = -1, wide_q = -1, wide_k = -1, wide_v = -1, logits = -1, bytes = 0;
     int64_t part_keys = 0;       // single tokens, tiles over pages: keys of a part
     int64_t logit_floats = 0;
-    int32_t cluster = 1;         // single tokens over pages: CTAs that share a part
+    int32_t cluster = 1;         // over pages (single tokens, tiles): CTAs that share a part
 };
 
 // Up to so many parts a warp joins those of a (query, head), beyond a CTA does.  Tokens of 16 requests over 500 to 4000 e4m3 rows, 1 to 8 parts:

@@ -42,7 +42,7 @@ template <bool F16>
 __device__ __forceinline__ uint32_t idesc_16(int n) { return F16 ? idesc_bf16_m128(n) & ~((1u << 7) | (1u << 10)) : idesc_bf16_m128(n); }
 constexpr uint32_t kRowsAreContraction = 1u << 16;      // instruction descriptor: B as above
 
-// Two neighbouring values of a 16-bit type: bf16, and for what came from e4m3 (exactly) fp16, whose weights are finer.
+// Two neighbouring values of a 16-bit type: bf16, and beside what came from 8 or 4 bits (exactly) fp16, whose weights are finer.
 __device__ __forceinline__ uint32_t two_f16(float lo, float hi)
 {
     const __half2 h = __floats2half2_rn(lo, hi);

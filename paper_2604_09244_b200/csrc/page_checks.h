@@ -311,8 +311,8 @@ inline bool page_by_tokens(int kind, int head_dim, int64_t rows, int64_t keys, i
 
 // Tiles of query rows that share what is unpacked on the way, 0: unpacked first.  Unpacking first costs 0.15 us for 1000 rows of a head (their bytes, twice) and a kernel's start, on the
 // way every CTA does it for one tile of rows or two (heads of up to 128 elements).  `keys`: of the batch, `mean`: of a sequence.  us, on the way / first, 32 heads in groups of 4, e4m3: 5 tokens
-// over 60000 rows (one tile) 58 / 121; 4 chunks of 56 over 3100 to 5500 (two) 48 / 57, of 33 over 4000 (two) 38 / 45, of 60 over 400 to 800 24 / 22, one over 4000 29 / 27; 100 over 4096
-// (four) 35 / 29; 512 over 8192 (16) 112 / 90.  16 heads of 64: 200 over 4000 (two) 25 / 27, over 30000 95 / 105.
+// over 60000 rows (one tile) 63 / 119; 4 chunks of 56 over 3100 to 5500 (two) 49 / 58, of 33 over 4000 (two) 40 / 49, 16 of 60 over 400 to 800 34.5 / 34.2, one over 4000 29 / 26, over 9000 36 / 37;
+// 100 over 4096 (four) 34 / 28; 512 over 8192 (16) 123 / 94.  16 heads of 64: 200 over 4000 (two) 25.4 / 24.7, over 30000 89 / 102.
 inline int32_t unpacked_row_tiles(const ServeShape& c, int32_t batch, const mvla_seq* seqs, int64_t keys, int64_t mean)
 {
     const int64_t queries = 128 / pack_of(c.n_heads / c.kv_heads);

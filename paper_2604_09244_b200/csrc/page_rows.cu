@@ -8,8 +8,8 @@
 // finite on top.  A thread keeps its head and pieces from row to row; a CTA goes over blocks of rows, and where the next block's rows lie (their
 // sequence, page and offsets) is looked up, a row by a thread, while one is worked on.
 //
-// B200: 12800 rows of 32 + 32 heads of 128 into bf16 pages 66 us (6.3 TB/s read and written); 65537 rows of 8 + 8 heads to e2m1 70 us (4.8 TB/s; integer instructions 71 % of their
-// pipe) and back 60; 131071 rows of 8 + 8 heads from e2m1 117 us (5.8 TB/s).  One piece to a lane and twice as many lanes: 149 us for the 65537 rows and back instead of 133 to 138.
+// B200: 12800 rows of 32 + 32 heads of 128 into bf16 pages 66 us (6.3 TB/s read and written), and out of them 65; 65537 rows of 8 + 8 heads to e2m1 70 us (4.8 TB/s; integer instructions 71 % of their
+// pipe) and back 60; 131071 rows of 8 + 8 heads from e2m1 115 us (5.9 TB/s; reads of quantised bf16 rows spill 16 bytes or less at 64 registers, which four CTAs leave).  One piece to a lane and twice as many lanes: 149 us for the 65537 rows and back instead of 133 to 138.
 #include "attend.cuh"
 #include "page.cuh"
 

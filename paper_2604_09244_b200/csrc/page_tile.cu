@@ -10,10 +10,11 @@
 // scores, or part of its weights (two exponentials to a key): what other queries see takes no bits.  The products of weights and scales that make up a row's output are of other sizes than its
 // weights, so that they have a reference of their own, in which O is counted.  Queries are fp16 too, every row times a power of two that puts its largest element between 2^14 and 2^15.
 //
-// A CTA has one tile of query rows (two CTAs to a multiprocessor, heads of up to 128 elements; 96 registers, 40 bytes spill), or two that share what is unpacked (one CTA); the softmax reads S
-// twice, once for its maximum.  B200, 32 query heads over 8 heads of 128, e4m3: 5 tokens over 60000 rows 58 us, 4 chunks of 56 over 3100 to 5500 rows 46 (one tile of rows to a CTA: 51), of 33
-// over 4000 rows 38 (45).  Two tiles of rows and 64 keys take 1.7 us, as in attend_tile.cu: without the exponentials, without most of the unpacking or of the second product 0 to 10 % less, so that it
+// A CTA has one tile of query rows (two CTAs to a multiprocessor, heads of up to 128 elements; 96 registers, 44 bytes spill), or two that share what is unpacked (one CTA); the softmax reads S
+// twice, once for its maximum.  B200, 32 query heads over 8 heads of 128, e4m3: 5 tokens over 60000 rows 63 us, 4 chunks of 56 over 3100 to 5500 rows 49 (one tile of rows to a CTA: 54), of 33
+// over 4000 rows 40 (48).  Two tiles of rows and 64 keys take 1.8 us, about as in attend_tile.cu: without the exponentials, without most of the unpacking or of the second product 0 to 10 % less, so that it
 // is the way of a tile from warp to warp.  The codes a tile ahead in registers instead of a ring: half as long again (a warp's loads wait for one another); twice the ring: the same.
+// The 4 chunks with all keys' scales far apart 61 us, with all values' 80 (unpacked first, whatever the scales, 58): such tiles are taken for rare ones.
 #include "attend_tile.cuh"
 #include "attend_walk.h"
 #include "page.cuh"

@@ -16,7 +16,7 @@
 // parts of a cluster are joined through its shared memory, and clusters (where a sequence has more than one) by a kernel behind.
 //
 // B200, 32 query heads over 8 heads of 128, with the join: 16 tokens over 500 to 4000 e4m3 rows 27 us (75 MB; launch, the first copies and the end of a CTA 9, the join 4,
-// 5 TB/s in between); one token over 131072 rows of e4m3 66 us (4.1 TB/s), of e2m1 52 us: 64 conversions of two codes and as many products of pairs to 16 keys, of
+// 5 TB/s in between); one token over 131072 rows of e4m3 64 us (4.2 TB/s), of e2m1 53 us: 64 conversions of two codes and as many products of pairs to 16 keys, of
 // the instructions' pipe 47 %, latency beside them (16 warps to a multiprocessor).  Tiles of 32 keys with one ahead: 53 us, of 16 keys 55, two ahead 56 (three CTAs fit instead of four).
 #include "attend_tile.cuh"
 #include "page.cuh"

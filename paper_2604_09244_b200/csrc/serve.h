@@ -57,7 +57,7 @@ struct AttArgs {
     const int32_t* table;        // null: the tiles that a sequence's queries see lie one after another, from tile km_row on
     int64_t table_stride;
     int32_t n_pages, page_shift; // page_rows = 1 << page_shift
-    int32_t cluster;             // CTAs to a cluster (launch_page_token): a sequence's parts are its clusters
+    int32_t cluster;             // CTAs to a cluster (launch_page_token, launch_page_tile, launch_page_decode): a sequence's parts are its clusters
     AttSeq s[kMaxBatch];
 };
 
