@@ -303,3 +303,20 @@ def test_the_same_bits_every_time(kind, H, G, d, sizes):
         want = want or (out, lse)
         assert torch.equal(out, want[0]) and torch.equal(lse, want[1])
         ctx.page_attention(pool, seqs, table, noise)
+
+
+@pytest.mark.parametrize("kind", [E4M3, E2M1])
+@pytest.mark.parametrize("call", CALLS[2:])
+def test_scales_as_far_apart_as_a_tile_takes(shim, call, kind):
+    """Rows behind the first query's own 2^4 to 2^24 larger, in keys and in values: what it sees keeps every bit, whichever way the tile is read."""
+    H, G, d, n_q, n = call
+    gen = generator(n_q + 31 * d)
+    ctx = context(BF16, H, G, d)
+    seqs = [mvla.Seq(q_row=0, n_q=n_q, n_kv=n)]
+    fp16, _ = form_of(shim, kind, *call)
+    q = torch.randn(n_q, H, d, generator=gen, device="cuda").to(BF16)
+    for power in (4, 6, 7, 8, 9, 10, 12, 18, 20, 21, 22, 24):
+        larger = lambda x, j: torch.where(j > n - n_q, x * 2.0 ** power, x)  # noqa: B023, E731
+        for k, v in ((larger, None), (None, larger)):
+            pool, table = sized_pool(gen, kind, G, d, n, 64, k, v)
+            check(ctx, pool, kind, seqs, table, q, 64, fp16)
